@@ -288,6 +288,125 @@ laq_status laq_quantize_worker_static(const float* d_g, const float* d_qprev, in
                                       uint32_t* d_codes, float* d_R, double* d_norms, void* cuda_stream,
                                       char* errbuf, size_t errbuf_len);
 
+/* ---- Operators on the way from a worker's samples to its local gradient ----------------------------------------------
+ * The models above end at 16 classes and one hidden layer; a larger model's gradients come from outside
+ * (LAQ_MODEL_EXTERNAL, laq_set_gradients).  These calls are what such a model needs beside the quantizer: a layer's product
+ * with bias, activation and residual, two losses over rows of logits, and the gradients of all three.
+ *
+ * Common rules.  No context: like laq_quantize_worker_static every call takes its stream and, optionally, a HOST buffer for
+ * an error text (errbuf, errbuf_len).  All tensors are DEVICE, row-major, on the calling thread's current device (checked:
+ * LAQ_EINVAL otherwise), with unit stride within a row and any row stride (in elements) of at least the row's length; a
+ * pointer needs only the alignment of its element.  Calls are asynchronous, allocate nothing, copy nothing to the host and
+ * can be captured into a CUDA graph.  Zero rows are allowed and launch nothing.  Results do not depend on timing: sums
+ * are taken in a fixed order, in fp32, and there are no atomics on device memory. */
+typedef enum {
+  LAQ_F32 = 0,
+  LAQ_BF16 = 1,
+  LAQ_F16 = 2
+} laq_dtype;
+
+/* Log probabilities of given tokens, with entropy and top alternatives.  For a row x of `vocab` logits, s = x / temperature:
+ *   lse = log sum_j exp(s_j),  logprob = s_token - lse,  entropy = -sum_j p_j log p_j with p_j = exp(s_j - lse),
+ *   top: the top_k largest logits in descending order (equal ones by lowest index) with their s_j - lse.
+ * d_tokens [rows] int32, or NULL (then d_logprob must be NULL).  A negative token marks a row to be left out (padding): its
+ * logits do not matter, logprob, entropy and lse are 0 and it has no alternatives.  A token >= vocab gives logprob = NaN.
+ * d_logprob, d_entropy, d_lse: [rows] fp32, each may be NULL.  d_top_tokens, d_top_logprobs: [rows][top_k], top_k 0..32.
+ * Logits at -inf are masked: they have probability 0 and are no alternatives; places without one hold token -1 and -inf.  A
+ * row masked throughout has lse = -inf, entropy 0, logprob -inf.  A row with a NaN or +inf gives NaN (its top tokens are -1).
+ * Limits: vocab 1..2^31-256, rows < 2^28, temperature 1e-4..1e4. */
+laq_status laq_token_logprobs(const void* d_logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                              float temperature, const int32_t* d_tokens, int32_t top_k, float* d_logprob, float* d_entropy,
+                              float* d_lse, int32_t* d_top_tokens, float* d_top_logprobs, void* cuda_stream, char* errbuf,
+                              size_t errbuf_len);
+
+/* Its gradient: with g = d_grad_logprob, h = d_grad_entropy ([rows] fp32, each may be NULL and counts as 0), and lse and
+ * entropy as laq_token_logprobs gave them (d_entropy may be NULL without d_grad_entropy),
+ *   d_grad_logits_j = (g ([j = token] - p_j) - h p_j (log p_j + entropy)) / temperature
+ * in the logits' dtype.  d_grad_logits may be the logits themselves (same pointer and stride), or must not overlap them.
+ * Rows with a negative token, and rows masked throughout (lse <= -1e30), get zeros; a token >= vocab gives NaN. */
+laq_status laq_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                                       float temperature, const int32_t* d_tokens, const float* d_lse, const float* d_entropy,
+                                       const float* d_grad_logprob, const float* d_grad_entropy, void* d_grad_logits,
+                                       int64_t grad_row_stride, void* cuda_stream, char* errbuf, size_t errbuf_len);
+
+/* Distillation from a teacher's top logits.  A row of the teacher has teacher_k (1..128) entries: column a_i
+ * (d_teacher_tokens, int32, negative = no entry) and logit t_i (d_teacher_logits, fp32), both [rows] with row stride
+ * teacher_stride.  q = softmax of t / temperature over the row's entries, p = softmax of the student's logits / temperature:
+ *   loss = temperature^2 sum_i q_i (log q_i - log p_{a_i}),  d loss / d logits_j = temperature (p_j - sum_{i: a_i = j} q_i)
+ * A column may be named more than once.  Entries at -inf have q = 0.  A row without entries (or whose every entry is at
+ * -inf) has loss 0, lse 0 and gradient 0.  A column >= vocab makes the row's loss and gradient NaN.  A teacher's column that
+ * the student has masked (-inf) gives loss = +inf; so does a row that the student has masked throughout, whose gradient is 0.
+ * d_loss, d_lse: [rows] fp32.  d_grad_loss ([rows] fp32) and d_grad_logits (logits' dtype; the logits themselves or no overlap)
+ * come together or are both NULL: with them the call also writes d_grad_logits = d_grad_loss * d loss / d logits, reading the
+ * logits once where a row fits the registers of eight blocks (524288 bytes), else twice. */
+laq_status laq_distill(const void* d_logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride, float temperature,
+                       const int32_t* d_teacher_tokens, const float* d_teacher_logits, int32_t teacher_k, int64_t teacher_stride,
+                       float* d_loss, float* d_lse, const float* d_grad_loss, void* d_grad_logits, int64_t grad_row_stride,
+                       void* cuda_stream, char* errbuf, size_t errbuf_len);
+
+/* The gradient alone, for a d_grad_loss that is only known after the loss; d_lse as laq_distill gave it. */
+laq_status laq_distill_backward(const void* d_logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
+                                float temperature, const int32_t* d_teacher_tokens, const float* d_teacher_logits,
+                                int32_t teacher_k, int64_t teacher_stride, const float* d_lse, const float* d_grad_loss,
+                                void* d_grad_logits, int64_t grad_row_stride, void* cuda_stream, char* errbuf, size_t errbuf_len);
+
+typedef enum {
+  LAQ_ACT_NONE = 0,
+  LAQ_ACT_RELU = 1,
+  LAQ_ACT_GELU = 2,   /* tanh form: z sigmoid(2 sqrt(2/pi) (z + 0.044715 z^3)) */
+  LAQ_ACT_SILU = 3    /* z sigmoid(z) */
+} laq_activation;
+
+enum {
+  LAQ_LINEAR_STARVE = 1u  /* for testing the bounded waits: one block's loader issues no copies, waits have a short limit */
+};
+
+/* One layer:  z = x w^T + bias,  y = act(z) + residual;  x [M][K], w [N][K], bias [N], the others [M][N], all in `dtype`
+ * (LAQ_BF16 or LAQ_F16), accumulated in fp32 and rounded once.  Row strides in elements. */
+typedef struct {
+  int32_t dtype;             /* laq_dtype of x, w, bias, residual, z, y, dy, dx */
+  int32_t activation;        /* laq_activation */
+  int64_t M, N, K;           /* M >= 0 rows, N >= 1 outputs, K >= 1 inputs */
+  const void* x;
+  int64_t ld_x;
+  const void* w;
+  int64_t ld_w;
+  const void* bias;          /* forward: [N] or NULL */
+  const void* residual;      /* forward: [M][N] or NULL; may be y itself */
+  int64_t ld_residual;
+  void* y;                   /* forward: output */
+  int64_t ld_y;
+  void* z;                   /* forward: output, or NULL; backward: input, read unless activation is LAQ_ACT_NONE */
+  int64_t ld_z;
+  const void* dy;            /* backward: gradient of y (which is also the residual's) */
+  int64_t ld_dy;
+  void* dx;                  /* backward: [M][K], or NULL */
+  int64_t ld_dx;
+  void* dw;                  /* backward: [N][K] in dw_dtype, or NULL */
+  int64_t ld_dw;
+  float* db;                 /* backward: [N], or NULL */
+  int32_t dw_dtype;          /* the call's dtype, or LAQ_F32 with LAQ_ACT_NONE or LAQ_ACT_RELU */
+  uint32_t flags;            /* 0 or LAQ_LINEAR_STARVE */
+  uint32_t* status;          /* DEVICE, one word that the caller has zeroed once: a call whose bounded wait runs out sets
+                                bits in it and leaves (part of) its outputs unwritten; the context stays usable */
+} laq_linear_call;
+
+/* Device memory (256-byte aligned) that a call needs as d_workspace, 0 if none (or if the call is invalid): copies of
+ * operands whose address or row stride is no multiple of 16 bytes and, for the gradient, act'(z) dy in `dtype` and partial
+ * sums.  It depends on the call's sizes, pointers and strides.  Nothing in it outlives the call; calls that may run at the same
+ * time (two streams, two replayed graphs) need workspaces of their own. */
+size_t laq_linear_workspace_bytes(const laq_linear_call* call /* HOST */, int32_t backward);
+
+/* y (and z, if given).  Inputs must not overlap outputs, except that residual may be y itself. */
+laq_status laq_linear_forward(const laq_linear_call* call /* HOST */, void* d_workspace, size_t workspace_bytes, void* cuda_stream,
+                              char* errbuf, size_t errbuf_len);
+
+/* dz = dy act'(z), rounded once to `dtype` (exact for LAQ_ACT_NONE and LAQ_ACT_RELU);  dx = dz w,  dw = dz^T x,
+ * db = column sums of dz before that rounding.  dw in fp32 is offered where dz is exact: with the other activations 16 bits
+ * of dz would not justify 32 of dw.  M = 0 gives dw = 0 and db = 0. */
+laq_status laq_linear_backward(const laq_linear_call* call /* HOST */, void* d_workspace, size_t workspace_bytes,
+                               void* cuda_stream, char* errbuf, size_t errbuf_len);
+
 /* Text of the last failure on this context ("" if none).  Valid until the next call on ctx. */
 const char* laq_last_error(const laq_ctx* ctx);
 

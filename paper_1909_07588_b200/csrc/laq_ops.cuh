@@ -1,0 +1,167 @@
+// What the context-free operators (laq_ops_rows.cu, laq_ops_linear.cu) share: element types, argument checks that end
+// in a status and a text, and the check that the buffers live on the current device.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include <cstdarg>
+#include <cstdio>
+
+#include "laq.h"
+
+namespace laq {
+namespace ops {
+
+inline laq_status fail(char* errbuf, size_t errlen, laq_status st, const char* fmt, ...) {
+  if (errbuf && errlen) {
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(errbuf, errlen, fmt, ap);
+    va_end(ap);
+  }
+  return st;
+}
+
+inline int dtype_bytes(int dtype) { return dtype == LAQ_F32 ? 4 : (dtype == LAQ_BF16 || dtype == LAQ_F16) ? 2 : 0; }
+
+// The kernels of a call run on the current device: a buffer of another GPU is refused.  Returns null if all is well.
+inline const char* wrong_device(const void* ptr) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess) {
+    cudaGetLastError();
+    return "no current CUDA device";
+  }
+  cudaPointerAttributes attr;
+  if (cudaPointerGetAttributes(&attr, ptr) != cudaSuccess) {
+    cudaGetLastError();
+    return "a buffer is not a pointer the CUDA runtime knows";
+  }
+  if (attr.type != cudaMemoryTypeDevice && attr.type != cudaMemoryTypeManaged) return "a buffer is not device memory";
+  if (attr.type == cudaMemoryTypeDevice && attr.device != dev)
+    return "the buffers live on another GPU than the current device: make their device current for the call";
+  return nullptr;
+}
+
+// One element type each: conversion, 16-byte vectors of EV elements, the largest of a vector (a NaN wins).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float ex2(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+
+template <class T>
+struct Elem;
+
+template <>
+struct Elem<float> {
+  static constexpr int EV = 4;
+  static constexpr uint32_t kNegInf = 0xff800000u;     // 32 bits of -inf elements
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[4]) {
+    x[0] = __uint_as_float(v.x);
+    x[1] = __uint_as_float(v.y);
+    x[2] = __uint_as_float(v.z);
+    x[3] = __uint_as_float(v.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
+    return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ float to_float(float v) { return v; }
+  static __device__ __forceinline__ float from_float(float v) { return v; }
+  template <int N>
+  static __device__ __forceinline__ float largest(const uint4 (&v)[N]) {
+    float m = __uint_as_float(v[0].x);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      m = max_nan(max_nan(m, __uint_as_float(v[i].x)), __uint_as_float(v[i].y));
+      m = max_nan(max_nan(m, __uint_as_float(v[i].z)), __uint_as_float(v[i].w));
+    }
+    return m;
+  }
+};
+
+template <>
+struct Elem<__nv_bfloat16> {
+  static constexpr int EV = 8;
+  static constexpr uint32_t kNegInf = 0xff80ff80u;
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = __uint_as_float(w[i] << 16);
+      x[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+  static __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
+  static __device__ __forceinline__ __nv_bfloat162 pair(uint32_t w) { return *reinterpret_cast<__nv_bfloat162*>(&w); }
+  template <int N>
+  static __device__ __forceinline__ float largest(const uint4 (&v)[N]) {
+    __nv_bfloat162 m = pair(v[0].x);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      m = __hmax2_nan(__hmax2_nan(m, __hmax2_nan(pair(v[i].x), pair(v[i].y))), __hmax2_nan(pair(v[i].z), pair(v[i].w)));
+    return max_nan(__low2float(m), __high2float(m));
+  }
+};
+
+template <>
+struct Elem<__half> {
+  static constexpr int EV = 8;
+  static constexpr uint32_t kNegInf = 0xfc00fc00u;
+  static __device__ __forceinline__ __half2 pair(uint32_t w) { return *reinterpret_cast<__half2*>(&w); }
+  static __device__ __forceinline__ void unpack(const uint4& v, float (&x)[8]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(pair(w[i]));
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&x)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __half2 h = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+  static __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
+  template <int N>
+  static __device__ __forceinline__ float largest(const uint4 (&v)[N]) {
+    __half2 m = pair(v[0].x);
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      m = __hmax2_nan(__hmax2_nan(m, __hmax2_nan(pair(v[i].x), pair(v[i].y))), __hmax2_nan(pair(v[i].z), pair(v[i].w)));
+    return max_nan(__low2float(m), __high2float(m));
+  }
+};
+
+// Plain (coherent) 16-byte load and store: a gradient may be written over the tensor that it is computed from.
+__device__ __forceinline__ uint4 load16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
+  return v;
+}
+
+}  // namespace ops
+}  // namespace laq

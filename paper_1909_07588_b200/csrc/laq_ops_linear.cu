@@ -1,0 +1,792 @@
+// A layer's product with bias, activation and residual in its epilogue, and its gradient:
+//   Z = X W^T + b,  Y = act(Z) + R            X [M][K], W [N][K], b [N], R, Y, Z [M][N]
+//   dZ = dY act'(Z),  dX = dZ W,  dW = dZ^T X,  db = column sums of dZ
+// bf16 or fp16 operands, fp32 accumulation on the tcgen05 tensor cores, bias, activation and residual in fp32, one
+// rounding per stored value.  dZ is rounded once to the operands' type, which the two products of the gradient need
+// (exact for no activation and for ReLU).
+//
+// One kernel serves all five products, D[i][j] = sum_r A(i, r) B(j, r).  An operand is "K-major" (the summed index r is
+// contiguous in memory) or "MN-major" (the free index is contiguous); TMA brings 64 values of r a stage in either form
+// with the 128-byte swizzle and the matrix descriptors tell the tensor core which one it is, so nothing is transposed in
+// memory.  Warp 0 loads, warp 1 issues the products, warps 2-9 run the epilogue of one tile from tensor memory while the
+// next one accumulates (two accumulators).  For few rows the roles of the operands are swapped (W's rows fill the 128
+// lanes, the rows of X are the narrow side) and the summed axis is split over a thread-block cluster whose blocks join
+// their partial tiles through distributed shared memory in a fixed order.
+#include <cooperative_groups.h>
+
+#include <atomic>
+
+#include "laq_ops.cuh"
+#include "laq_umma_gemm.cuh"
+
+namespace cg = cooperative_groups;
+
+namespace laq {
+namespace ops {
+namespace {
+
+using umma::kBlockK;
+using umma::kTileM;
+
+constexpr int kSMs = 148;
+constexpr int kGemmThreads = 320;         // loader, tensor-core warp, eight epilogue warps
+constexpr int kEpiWarps = 8;
+constexpr int kMaxStages = 12;
+constexpr int kMaxRing = 224 * 1024;      // bytes of the stage ring
+constexpr int kMaxSplit = 8;
+constexpr uint32_t kStarvedLimit = 1u << 12;
+constexpr int kGroupTiles = 16;           // tile rows that are swept together, so that operands are found in L2
+
+struct GemmArgs {
+  int I, J, nkb;                 // rows and columns of D; 64-wide blocks of the summed axis
+  int nt, stages, split;         // tile width, ring depth, blocks per tile
+  int tiles_i, tiles_j;
+  int a_mn, b_mn;                // 1: the operand is MN-major
+  int fmt;                       // operand type of the instruction descriptor: 0 fp16, 1 bf16
+  int act, out_f32, starve;
+  long long ldo, ldz, ldr;       // row strides of out, z and residual (elements)
+  void* out;
+  void* z;                       // or null
+  const void* bias;              // or null
+  const void* residual;          // or null
+  uint32_t* status;
+};
+
+__device__ __forceinline__ uint64_t desc_k_major(uint32_t addr) { return umma::smem_desc_sw128(addr); }
+// MN-major tile with the 128-byte swizzle: [64 r][64 free] blocks of 128-byte rows; eight rows of r are 1024 bytes
+// apart (stride offset), the next 64 values of the free index 64 rows = 8192 bytes on (leading offset).
+__device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr) {
+  uint64_t d = 0;
+  d |= (uint64_t)((addr & 0x3ffffu) >> 4);
+  d |= (uint64_t)(8192 >> 4) << 16;
+  d |= (uint64_t)(1024 >> 4) << 32;
+  d |= (uint64_t)1 << 46;
+  d |= (uint64_t)2 << 61;
+  return d;
+}
+__device__ __forceinline__ uint32_t instr_desc(int fmt, int a_mn, int b_mn, int nt) {
+  return (1u << 4) | ((uint32_t)fmt << 7) | ((uint32_t)fmt << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
+         ((uint32_t)(nt >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
+}
+
+// z * sigmoid(k z ...): gelu is the tanh form, 0.5 z (1 + tanh u) = z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
+constexpr float kGeluC = 0.7978845608028654f, kGeluA = 0.044715f;
+__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
+__device__ __forceinline__ float activate(float z, int act) {
+  if (act == LAQ_ACT_RELU) return z > 0.f ? z : (z == z ? 0.f : z);
+  if (act == LAQ_ACT_SILU) return z * sigmoid(z);
+  if (act == LAQ_ACT_GELU) return z * sigmoid(2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
+  return z;
+}
+__device__ __forceinline__ float slope(float z, int act) {
+  if (act == LAQ_ACT_RELU) return z > 0.f ? 1.f : (z == z ? 0.f : z);
+  if (act == LAQ_ACT_SILU) {
+    const float s = sigmoid(z);
+    return s * fmaf(z, 1.f - s, 1.f);
+  }
+  if (act == LAQ_ACT_GELU) {
+    const float s = sigmoid(2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
+    // |z| > 20: s is 0 or 1 and s (1 - s) z^3 is zero long before z^3 overflows
+    const float zz = fminf(z * z, 400.f), zc = fminf(fmaxf(z, -20.f), 20.f);
+    return fmaf(zc * s * (1.f - s), 2.f * kGeluC * fmaf(3.f * kGeluA, zz, 1.f), s);
+  }
+  return 1.f;
+}
+
+// Eight values of one accumulator row.  TRANS = false: row i of D is a row of out, the eight are neighbours there;
+// TRANS = true: the eight are rows of out, i a column of it (neighbouring lanes write neighbouring columns).
+template <class T, bool TRANS>
+__device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float (&acc)[8], bool vec_ok) {
+  if (i >= A.I || j0 >= A.J) return;
+  const T* bias = reinterpret_cast<const T*>(A.bias);
+  const T* res = reinterpret_cast<const T*>(A.residual);
+  T* zp = reinterpret_cast<T*>(A.z);
+  if (TRANS) {
+    const float b = bias ? Elem<T>::to_float(bias[i]) : 0.f;
+    float r[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) r[e] = res && j0 + e < A.J ? Elem<T>::to_float(res[(long long)(j0 + e) * A.ldr + i]) : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (j0 + e >= A.J) break;
+      const float z = acc[e] + b;
+      if (zp) zp[(long long)(j0 + e) * A.ldz + i] = Elem<T>::from_float(z);
+      const float y = activate(z, A.act) + r[e];
+      if (A.out_f32) reinterpret_cast<float*>(A.out)[(long long)(j0 + e) * A.ldo + i] = y;
+      else reinterpret_cast<T*>(A.out)[(long long)(j0 + e) * A.ldo + i] = Elem<T>::from_float(y);
+    }
+    return;
+  }
+  if (vec_ok && j0 + 8 <= A.J) {
+    float r[8];
+    if (res) Elem<T>::unpack(*reinterpret_cast<const uint4*>(res + (long long)i * A.ldr + j0), r);
+    if (bias) {
+      float b[8];
+      Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(bias + j0)), b);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += b[e];
+    }
+    if (zp) *reinterpret_cast<uint4*>(zp + (long long)i * A.ldz + j0) = Elem<T>::pack(acc);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      acc[e] = activate(acc[e], A.act);
+      if (res) acc[e] += r[e];
+    }
+    if (A.out_f32) {
+      float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(A.out) + (long long)i * A.ldo + j0);
+      o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+      o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+    } else {
+      *reinterpret_cast<uint4*>(reinterpret_cast<T*>(A.out) + (long long)i * A.ldo + j0) = Elem<T>::pack(acc);
+    }
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int j = j0 + e;
+    if (j >= A.J) break;
+    const float z = acc[e] + (bias ? Elem<T>::to_float(bias[j]) : 0.f);
+    if (zp) zp[(long long)i * A.ldz + j] = Elem<T>::from_float(z);
+    const float y = activate(z, A.act) + (res ? Elem<T>::to_float(res[(long long)i * A.ldr + j]) : 0.f);
+    if (A.out_f32) reinterpret_cast<float*>(A.out)[(long long)i * A.ldo + j] = y;
+    else reinterpret_cast<T*>(A.out)[(long long)i * A.ldo + j] = Elem<T>::from_float(y);
+  }
+}
+
+__device__ __forceinline__ bool aligned16(const void* p, long long ld_bytes) {
+  return (((uintptr_t)p | (uintptr_t)ld_bytes) & 15u) == 0;
+}
+
+// Work item `w` -> tile origin.  Tile rows are swept in groups of kGroupTiles, column by column within a group.
+__device__ __forceinline__ void tile_of(const GemmArgs& A, int w, int& i0, int& j0) {
+  const int group = kGroupTiles * A.tiles_j;
+  const int g = w / group, in = w - g * group;
+  const int first = g * kGroupTiles;
+  const int rows = min(kGroupTiles, A.tiles_i - first);
+  i0 = (first + in % rows) * kTileM;
+  j0 = (in / rows) * A.nt;
+}
+
+template <class T, bool TRANS>
+__global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
+                                                                      const __grid_constant__ CUtensorMap tmB,
+                                                                      const GemmArgs A) {
+  extern __shared__ unsigned char gemm_smem_raw[];
+  __shared__ uint64_t bars[2 * kMaxStages + 5];
+  __shared__ uint32_t tmem_base_sh;
+  __shared__ int abort_sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = umma::smem_u32(gemm_smem_raw), smem0 = (base + 1023u) & ~1023u;
+  float* partial = reinterpret_cast<float*>(gemm_smem_raw + (smem0 - base));      // [nt][128], once the ring is idle
+  const int nt = A.nt, stages = A.stages, split = A.split;
+  const uint32_t a_bytes = kTileM * kBlockK * 2, st_bytes = a_bytes + (uint32_t)nt * kBlockK * 2;
+  const uint32_t full0 = umma::smem_u32(&bars[0]), empty0 = umma::smem_u32(&bars[kMaxStages]);
+  const uint32_t acc_full0 = umma::smem_u32(&bars[2 * kMaxStages]), acc_empty0 = acc_full0 + 16, drain = acc_full0 + 32;
+  // Two accumulators of at most 256 columns; one for a split tile, which has no successor.  Two blocks of a cluster on one
+  // SM must be able to hold theirs at the same time (each waits for the other), and two is all that fits by shared memory.
+  const uint32_t acc_cols = umma::tmem_cols(nt), held_cols = split > 1 ? acc_cols : 2 * acc_cols;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      umma::mbar_init(full0 + 8 * s, 1);
+      umma::mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      umma::mbar_init(acc_full0 + 8 * b, 1);
+      umma::mbar_init(acc_empty0 + 8 * b, kEpiWarps);
+    }
+    umma::mbar_init(drain, 1);
+    abort_sh = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(umma::smem_u32(&tmem_base_sh)),
+                 "r"(held_cols)
+                 : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = tmem_base_sh;
+
+  const int tiles = A.tiles_i * A.tiles_j;
+  const int rank = split > 1 ? (int)(blockIdx.x % (unsigned)split) : 0;
+  const int first = (int)(blockIdx.x / (unsigned)split), step = (int)(gridDim.x / (unsigned)split);
+  const int kb_per = (A.nkb + split - 1) / split;
+  const int kb0 = min(rank * kb_per, A.nkb), nkb = min(kb0 + kb_per, A.nkb) - kb0;    // > 0: the plan leaves no block idle
+  const bool starved = A.starve && blockIdx.x == 0;
+  const uint32_t limit = A.starve ? kStarvedLimit : umma::kWaitLimit;
+  volatile int* abort_flag = &abort_sh;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int n = 0;                       // stages handed out so far
+      bool ok = !starved;
+      for (int w = first; w < tiles && ok; w += step) {
+        int i0, j0;
+        tile_of(A, w, i0, j0);
+        for (int kb = 0; kb < nkb; ++kb, ++n) {
+          const int s = n % stages;
+          ok = umma::mbar_wait_abortable(empty0 + 8 * s, ((uint32_t)(n / stages) & 1u) ^ 1u, limit, abort_flag, A.status, 1u);
+          if (!ok) break;
+          const uint32_t bar = full0 + 8 * s, sa = smem0 + s * st_bytes, sb = sa + a_bytes;
+          const int r = (kb0 + kb) * kBlockK;
+          umma::mbar_expect_tx(bar, st_bytes);
+          if (A.a_mn) {
+            umma::tma_load_2d(sa, &tmA, bar, i0, r);
+            umma::tma_load_2d(sa + 8192, &tmA, bar, i0 + 64, r);
+          } else {
+            umma::tma_load_2d(sa, &tmA, bar, r, i0);
+          }
+          if (A.b_mn) {
+            for (int b = 0; b < nt; b += 64) umma::tma_load_2d(sb + b * 128, &tmB, bar, j0 + b, r);
+          } else {
+            umma::tma_load_2d(sb, &tmB, bar, r, j0);
+          }
+        }
+      }
+      if (!ok)                          // given up: the copies in flight still land in this block's memory
+        for (int m = n > stages ? n - stages : 0; m < n; ++m)
+          for (uint32_t it = 0; it < umma::kWaitLimit && !umma::mbar_try_wait(full0 + 8 * (m % stages), (uint32_t)(m / stages) & 1u); ++it) {
+          }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint32_t idesc = instr_desc(A.fmt, A.a_mn, A.b_mn, nt);
+      // 16 values of r: 32 bytes on within the rows of a K-major tile, two groups of 8 rows (2048 bytes) on in an MN-major one
+      const uint32_t step_a = A.a_mn ? 128u : 2u, step_b = A.b_mn ? 128u : 2u;
+      int n = 0, it = 0;
+      bool ok = true;
+      for (int w = first; w < tiles && ok; w += step, ++it) {
+        const int b = it & 1;
+        ok = umma::mbar_wait_abortable(acc_empty0 + 8 * b, ((uint32_t)(it >> 1) & 1u) ^ 1u, limit, abort_flag, A.status, 2u);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        const uint32_t d = tmem_base + (uint32_t)b * acc_cols;
+        for (int kb = 0; kb < nkb; ++kb, ++n) {
+          const int s = n % stages;
+          ok = umma::mbar_wait_abortable(full0 + 8 * s, (uint32_t)(n / stages) & 1u, limit, abort_flag, A.status, 4u);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t sa = smem0 + s * st_bytes, sb = sa + a_bytes;
+          const uint64_t da = A.a_mn ? desc_mn_major(sa) : desc_k_major(sa), db = A.b_mn ? desc_mn_major(sb) : desc_k_major(sb);
+#pragma unroll
+          for (int kk = 0; kk < kBlockK / 16; ++kk)
+            umma::mma_bf16_ss(d, da + kk * step_a, db + kk * step_b, idesc, (kb | kk) != 0 ? 1u : 0u);
+          umma::mma_commit(empty0 + 8 * s);
+        }
+        if (ok) umma::mma_commit(acc_full0 + 8 * b);
+      }
+      if (!ok) {                        // products under way still read the ring and write tensor memory
+        umma::mma_commit(drain);
+        for (uint32_t i = 0; i < umma::kWaitLimit && !umma::mbar_try_wait(drain, 0u); ++i) {
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    const int q = warp & 3, set = (warp - 2) >> 2;
+    const int row = q * 32 + lane;
+    const bool vec_ok = aligned16(A.out, A.ldo * (A.out_f32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
+                        (!A.residual || aligned16(A.residual, A.ldr * 2)) && (!A.bias || aligned16(A.bias, 0));
+    int it = 0;
+    for (int w = first; w < tiles; w += step, ++it) {
+      const int b = it & 1;
+      const bool ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(it >> 1) & 1u, limit,
+                                                                        abort_flag, A.status, 8u));
+      if (!ok) break;
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+      int i0, j0;
+      tile_of(A, w, i0, j0);
+      const uint32_t t0 = tmem_base + (uint32_t)b * acc_cols + ((uint32_t)(q * 32) << 16);
+      for (int c0 = 16 * set; c0 < nt; c0 += 32) {
+        uint32_t v[16];
+        umma::tmem_load_16(t0 + (uint32_t)c0, v);
+        float x[2][8];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[e >> 3][e & 7] = __uint_as_float(v[e]);
+        if (split > 1) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) partial[(c0 + e) * kTileM + row] = x[e >> 3][e & 7];
+        } else {
+          finish8<T, TRANS>(A, i0 + row, j0 + c0, x[0], vec_ok);
+          finish8<T, TRANS>(A, i0 + row, j0 + c0 + 8, x[1], vec_ok);
+        }
+      }
+      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+      __syncwarp();
+      if (lane == 0) umma::mbar_arrive(acc_empty0 + 8 * b);
+    }
+  }
+  if (split > 1) {          // one tile per cluster: its blocks share the columns of the join
+    cg::cluster_group cluster = cg::this_cluster();
+    __syncwarp();
+    cluster.sync();
+    if (warp >= 2) {
+      const int q = warp & 3, set = (warp - 2) >> 2, row = q * 32 + lane;
+      int gone = 0;
+      for (int r = 0; r < split; ++r) gone |= *cluster.map_shared_rank(&abort_sh, r);
+      const bool vec_ok = aligned16(A.out, A.ldo * (A.out_f32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
+                          (!A.residual || aligned16(A.residual, A.ldr * 2)) && (!A.bias || aligned16(A.bias, 0));
+      int i0, j0;
+      tile_of(A, first, i0, j0);
+      for (int g = rank * 2 + set; g < nt / 8 && !gone; g += 2 * split) {
+        float x[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+        for (int r = 0; r < split; ++r) {
+          const float* p = cluster.map_shared_rank(partial, r) + (size_t)g * 8 * kTileM + row;
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] += p[e * kTileM];
+        }
+        finish8<T, TRANS>(A, i0 + row, j0 + g * 8, x, vec_ok);
+      }
+    }
+    __syncwarp();
+    cluster.sync();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  __syncthreads();
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(held_cols) : "memory");
+  }
+}
+
+// ---- dZ and the column sums ---------------------------------------------------------------------------------------------
+// A block takes 256 columns (32 threads of eight) and a run of rows (8 threads): dZ = dY act'(Z), stored once if dz is
+// given, and the sum of its columns over the run, in fp32 of the UNROUNDED products, to part[run][N].
+constexpr int kDzCols = 256, kDzThreads = 256;
+
+template <class T>
+__global__ void __launch_bounds__(kDzThreads) linear_dz_kernel(const T* dy, long long lddy, const T* z, long long ldz, T* dz,
+                                                               long long lddz, float* part, long long M, int N, int act,
+                                                               int rows_per, int vec_ok) {
+  __shared__ float sh[8][kDzCols];
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const int c0 = blockIdx.x * kDzCols + tx * 8;
+  const long long r0 = (long long)blockIdx.y * rows_per, r1 = min(r0 + (long long)rows_per, M);
+  float sum[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
+  if (c0 < N) {
+    const bool full = vec_ok && c0 + 8 <= N;
+#pragma unroll 2
+    for (long long r = r0 + ty; r < r1; r += 8) {
+      float g[8], x[8];
+      if (full) {
+        Elem<T>::unpack(load16(dy + r * lddy + c0), g);
+        if (act != LAQ_ACT_NONE) Elem<T>::unpack(load16(z + r * ldz + c0), x);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          g[e] = c0 + e < N ? Elem<T>::to_float(dy[r * lddy + c0 + e]) : 0.f;
+          x[e] = act != LAQ_ACT_NONE && c0 + e < N ? Elem<T>::to_float(z[r * ldz + c0 + e]) : 0.f;
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (act == LAQ_ACT_RELU) g[e] = x[e] > 0.f ? g[e] : (x[e] == x[e] ? 0.f : x[e]);
+        else if (act != LAQ_ACT_NONE) g[e] *= slope(x[e], act);
+        sum[e] += g[e];
+      }
+      if (dz) {                       // the workspace's rows are 16-byte aligned and padded to eight columns
+        *reinterpret_cast<uint4*>(dz + r * lddz + c0) = Elem<T>::pack(g);
+      }
+    }
+  }
+  if (!part) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sh[ty][tx * 8 + e] = sum[e];
+  __syncthreads();
+  const int c = blockIdx.x * kDzCols + (int)threadIdx.x;
+  if (c < N) {
+    float t = 0.f;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) t += sh[y][threadIdx.x];
+    part[(long long)blockIdx.y * N + c] = t;
+  }
+}
+
+__global__ void __launch_bounds__(256) linear_db_kernel(const float* part, int runs, int N, float* db) {
+  __shared__ float sh[8][33];
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
+  float s = 0.f;
+  if (c < N)
+    for (int r = ty; r < runs; r += 8) s += part[(long long)r * N + c];
+  sh[ty][tx] = s;
+  __syncthreads();
+  if (ty == 0 && c < N) {
+    float t = 0.f;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) t += sh[y][tx];
+    db[c] = t;
+  }
+}
+
+// Rows that a tensor map cannot describe (an address or a row pitch that is no multiple of 16 bytes) are copied once
+// into the workspace with a pitch of a multiple of eight elements.
+__global__ void __launch_bounds__(256) linear_pack_kernel(const uint16_t* src, long long ld, uint16_t* dst, long long pitch,
+                                                          long long rows, int cols) {
+  const int groups = (cols + 7) / 8;
+  const long long n = rows * groups, stride = (long long)gridDim.x * blockDim.x;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) {
+    const long long r = i / groups;
+    const int c = (int)(i - r * groups) * 8;
+    const uint16_t* s = src + r * ld + c;
+    uint16_t v[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? s[e] : (uint16_t)0;
+    uint4 o;
+    o.x = v[0] | ((uint32_t)v[1] << 16);
+    o.y = v[2] | ((uint32_t)v[3] << 16);
+    o.z = v[4] | ((uint32_t)v[5] << 16);
+    o.w = v[6] | ((uint32_t)v[7] << 16);
+    *reinterpret_cast<uint4*>(dst + r * pitch + c) = o;
+  }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+size_t align256(size_t x) { return (x + 255) / 256 * 256; }
+long long pad8(long long x) { return (x + 7) / 8 * 8; }
+bool mappable(const void* p, long long ld) { return ((uintptr_t)p & 15u) == 0 && (ld % 8) == 0; }
+
+struct Operand {                // a 2-byte matrix [rows][cols]
+  const void* p;
+  long long ld, rows, cols;
+  bool mappable_() const { return mappable(p, ld); }
+  size_t pack_bytes() const { return mappable_() ? 0 : align256((size_t)rows * pad8(cols) * 2); }
+};
+
+struct Plan {
+  int swap, nt, split, stages;
+  double cost;
+};
+
+// Tile width, split and orientation by an estimate of the time in SM cycles: a stage costs the larger of its products
+// (two cycles per column of the tile) and of its bytes at what an SM takes from L2, a tile a fixed start and its epilogue.
+// `swappable`: the epilogue may write the transposed tile (only worth it for few columns).
+Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable) {
+  Plan best{0, 128, 1, 4, 1e300};
+  const long long nkb = (R + kBlockK - 1) / kBlockK;
+  for (int swap = 0; swap <= (swappable ? 1 : 0); ++swap) {
+    const long long i = swap ? J : I, j = swap ? I : J;
+    const bool bmn = swap ? a_mn : b_mn;
+    static const int widths[] = {16, 32, 64, 96, 112, 128, 160, 192, 208, 224, 256};
+    for (int nt : widths) {
+      if (bmn && nt % 64) continue;
+      if (swap && nt > 128) continue;
+      for (int split = 1; split <= kMaxSplit; split *= 2) {
+        if (split > 1 && (nkb + split - 1) / split * (split - 1) >= nkb) continue;     // a block would have nothing to do
+        const size_t stage = (size_t)(kTileM + nt) * kBlockK * 2;
+        const size_t room = split > 1 || nt <= 32 ? 110 * 1024 : 220 * 1024;
+        int stages = (int)(room / stage);
+        if (stages > kMaxStages) stages = kMaxStages;
+        if (split > 1) {
+          const size_t need = (size_t)kTileM * nt * 4;                                 // the partial tile in the ring
+          while ((size_t)stages * stage < need || stages < 3) ++stages;
+        }
+        if (stages * stage > (size_t)kMaxRing) continue;
+        const int per_sm = stages * stage > 112 * 1024 ? 1 : 2;
+        const long long tiles = ((i + kTileM - 1) / kTileM) * ((j + nt - 1) / nt);
+        const long long kb = (nkb + split - 1) / split;
+        const double mma = 2.0 * nt, load = stage / 48.0;
+        const double per_stage = mma > load ? mma : load;
+        const double epi = 16.0 * nt * (swap ? 2 : 1);
+        double cost;
+        if (split == 1) {
+          const long long waves = (tiles + kSMs - 1) / kSMs;
+          const double main = kb * per_stage;
+          cost = 2500 + waves * (main > epi ? main : epi) + epi;
+        } else {
+          if (tiles * split > 2ll * kSMs * per_sm) continue;
+          const double waves = (double)((tiles * split + kSMs - 1) / kSMs);
+          cost = 4500 + waves * (kb * per_stage + epi / split + 8.0 * nt);
+        }
+        if (cost < best.cost) best = Plan{swap, nt, split, stages, cost};
+      }
+    }
+  }
+  return best;
+}
+
+struct Err {
+  char* buf;
+  size_t len;
+};
+
+template <class T, bool TRANS>
+laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, cudaStream_t st) {
+  auto kernel = linear_gemm_kernel<T, TRANS>;
+  const size_t smem = (size_t)A.stages * (kTileM + A.nt) * kBlockK * 2 + 1024;
+  // the kernel's shared memory limit is raised once per device
+  static std::atomic<uint64_t> raised{0};
+  int dev = 0;
+  cudaGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev >= 64 || !(raised.load(std::memory_order_acquire) & bit)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing + 1024) != cudaSuccess) {
+      cudaGetLastError();
+      return fail(e.buf, e.len, LAQ_ECUDA, "shared memory of the product kernel was refused");
+    }
+    raised.fetch_or(bit, std::memory_order_release);
+  }
+  const long long tiles = (long long)A.tiles_i * A.tiles_j;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(A.split > 1 ? tiles * A.split : tiles < kSMs ? tiles : kSMs));
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute at[1];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = (unsigned)A.split;
+  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cfg.attrs = at;
+  cfg.numAttrs = A.split > 1 ? 1 : 0;
+  const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, ma, mb, A);
+  if (rc != cudaSuccess) {
+    cudaGetLastError();
+    return fail(e.buf, e.len, LAQ_ECUDA, "kernel launch failed: %s", cudaGetErrorString(rc));
+  }
+  return LAQ_OK;
+}
+
+struct Epilogue {
+  void* out = nullptr;
+  long long ldo = 0;
+  int out_f32 = 0, act = LAQ_ACT_NONE;
+  const void *bias = nullptr, *residual = nullptr;
+  long long ldr = 0;
+  void* z = nullptr;
+  long long ldz = 0;
+};
+
+// D[i][j] = sum_r A(i, r) B(j, r): a_mn ? A is stored [r][i] : [i][r], the same for B.  Both are mappable.
+laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const Operand& b, bool b_mn, const Epilogue& ep,
+                   uint32_t* status, int starve, bool swappable, cudaStream_t st) {
+  const long long I = a_mn ? a.cols : a.rows, R = a_mn ? a.rows : a.cols, J = b_mn ? b.cols : b.rows;
+  const Plan pl = make_plan(I, J, R, a_mn, b_mn, swappable);
+  const Operand& A0 = pl.swap ? b : a;
+  const Operand& B0 = pl.swap ? a : b;
+  const bool amn = pl.swap ? b_mn : a_mn, bmn = pl.swap ? a_mn : b_mn;
+  CUtensorMap ma, mb;
+  if (!umma::make_map_bf16_2d(&ma, A0.p, A0.rows, A0.cols, A0.ld * 2, amn ? 64 : kTileM) ||
+      !umma::make_map_bf16_2d(&mb, B0.p, B0.rows, B0.cols, B0.ld * 2, bmn ? 64 : pl.nt))
+    return fail(e.buf, e.len, LAQ_ECUDA, "a tensor map was refused");
+  GemmArgs A = {};
+  A.I = (int)(pl.swap ? J : I);
+  A.J = (int)(pl.swap ? I : J);
+  A.nkb = (int)((R + kBlockK - 1) / kBlockK);
+  A.nt = pl.nt;
+  A.stages = pl.stages;
+  A.split = pl.split;
+  A.tiles_i = (A.I + kTileM - 1) / kTileM;
+  A.tiles_j = (A.J + pl.nt - 1) / pl.nt;
+  A.a_mn = amn;
+  A.b_mn = bmn;
+  A.fmt = dtype == LAQ_BF16 ? 1 : 0;
+  A.act = ep.act;
+  A.out_f32 = ep.out_f32;
+  A.starve = starve;
+  A.ldo = ep.ldo;
+  A.ldz = ep.ldz;
+  A.ldr = ep.ldr;
+  A.out = ep.out;
+  A.z = ep.z;
+  A.bias = ep.bias;
+  A.residual = ep.residual;
+  A.status = status;
+  if (dtype == LAQ_BF16)
+    return pl.swap ? launch_gemm<__nv_bfloat16, true>(e, ma, mb, A, st) : launch_gemm<__nv_bfloat16, false>(e, ma, mb, A, st);
+  return pl.swap ? launch_gemm<__half, true>(e, ma, mb, A, st) : launch_gemm<__half, false>(e, ma, mb, A, st);
+}
+
+// Copies an operand that a tensor map cannot describe to `ws` (advanced past it).
+laq_status make_mappable(const Err& e, Operand& o, char*& ws, cudaStream_t st) {
+  const size_t bytes = o.pack_bytes();
+  if (!bytes) return LAQ_OK;
+  const long long pitch = pad8(o.cols), items = o.rows * (pitch / 8);
+  const long long want = (items + 255) / 256, most = 8 * kSMs;
+  linear_pack_kernel<<<(unsigned)(want < most ? want : most), 256, 0, st>>>((const uint16_t*)o.p, o.ld, (uint16_t*)ws, pitch, o.rows,
+                                                                           (int)o.cols);
+  if (cudaGetLastError() != cudaSuccess) return fail(e.buf, e.len, LAQ_ECUDA, "kernel launch failed");
+  o.p = ws;
+  o.ld = pitch;
+  ws += bytes;
+  return LAQ_OK;
+}
+
+bool sizes_ok(const laq_linear_call* c) {
+  const long long most = 0x7fffff00ll;
+  return c && c->M >= 0 && c->M <= most && c->N >= 1 && c->N <= most && c->K >= 1 && c->K <= most &&
+         (c->dtype == LAQ_BF16 || c->dtype == LAQ_F16);
+}
+
+int dz_rows_per(long long M, long long N) {
+  // enough blocks for four an SM, no fewer than 32 rows each, and no more than 65535 runs (a grid dimension)
+  const long long cols = (N + kDzCols - 1) / kDzCols;
+  long long runs = (4 * kSMs + cols - 1) / cols;
+  long long per = (M + runs - 1) / runs;
+  per = per < 32 ? 32 : per;
+  while ((M + per - 1) / per > 65535) per *= 2;
+  return (int)per;
+}
+
+// What the gradient keeps in the workspace: dZ (unless dY itself serves), the column sums' partials, packed operands.
+struct BackwardNeeds {
+  bool own_dz;
+  size_t dz_bytes, part_bytes;
+  Operand x, w, dz;
+  explicit BackwardNeeds(const laq_linear_call* c) {
+    const Operand dy{c->dy, c->ld_dy, c->M, c->N};
+    own_dz = (c->dx || c->dw) && (c->activation != LAQ_ACT_NONE || !dy.mappable_());
+    dz_bytes = own_dz ? align256((size_t)c->M * pad8(c->N) * 2) : 0;
+    const int per = dz_rows_per(c->M, c->N);
+    part_bytes = c->db ? align256((size_t)((c->M + per - 1) / per) * c->N * 4) : 0;
+    x = Operand{c->x, c->ld_x, c->M, c->K};
+    w = Operand{c->w, c->ld_w, c->N, c->K};
+    dz = dy;
+  }
+  size_t bytes(const laq_linear_call* c) const {
+    return dz_bytes + part_bytes + (c->dw ? x.pack_bytes() : 0) + (c->dx ? w.pack_bytes() : 0);
+  }
+};
+
+laq_status check_call(const Err& e, const laq_linear_call* c, void* ws, size_t ws_bytes, size_t need) {
+  if (e.buf && e.len) e.buf[0] = 0;
+  if (!c) return fail(e.buf, e.len, LAQ_EINVAL, "null pointer");
+  if (c->dtype != LAQ_BF16 && c->dtype != LAQ_F16) return fail(e.buf, e.len, LAQ_EINVAL, "dtype must be LAQ_BF16 or LAQ_F16");
+  if (!sizes_ok(c)) return fail(e.buf, e.len, LAQ_EINVAL, "M must be 0..2^31-256, N and K 1..2^31-256");
+  if (c->activation < LAQ_ACT_NONE || c->activation > LAQ_ACT_SILU) return fail(e.buf, e.len, LAQ_EINVAL, "unknown activation");
+  if (!c->status) return fail(e.buf, e.len, LAQ_EINVAL, "status must point to a word of device memory");
+  if (need && (!ws || ((uintptr_t)ws & 255u) || ws_bytes < need))
+    return fail(e.buf, e.len, LAQ_EWORKSPACE, "workspace missing, misaligned (256 bytes) or too small: %zu bytes needed", need);
+  const char* msg = wrong_device(c->status);
+  return msg ? fail(e.buf, e.len, LAQ_EINVAL, "%s", msg) : LAQ_OK;
+}
+
+// One tensor of a call: there if it must be, rows no shorter than their length, aligned to its elements.
+laq_status check_tensor(const Err& e, const char* name, const void* p, bool required, int64_t ld, int64_t cols, int bytes) {
+  if (!p) return required ? fail(e.buf, e.len, LAQ_EINVAL, "%s is null", name) : LAQ_OK;
+  if (ld < cols) return fail(e.buf, e.len, LAQ_EINVAL, "the row stride of %s is shorter than its rows", name);
+  if (((uintptr_t)p % (uintptr_t)bytes) != 0) return fail(e.buf, e.len, LAQ_EINVAL, "%s is not aligned to its element size", name);
+  return LAQ_OK;
+}
+
+#define LAQ_TRY(call)                \
+  do {                               \
+    const laq_status st_ = (call);   \
+    if (st_ != LAQ_OK) return st_;   \
+  } while (0)
+
+}  // namespace
+}  // namespace ops
+}  // namespace laq
+
+using namespace laq::ops;
+
+extern "C" size_t laq_linear_workspace_bytes(const laq_linear_call* c, int32_t backward) {
+  if (!sizes_ok(c)) return 0;
+  if (backward) return BackwardNeeds(c).bytes(c);
+  return Operand{c->x, c->ld_x, c->M, c->K}.pack_bytes() + Operand{c->w, c->ld_w, c->N, c->K}.pack_bytes();
+}
+
+extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream,
+                                         char* errbuf, size_t errbuf_len) {
+  const Err e{errbuf, errbuf_len};
+  LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, laq_linear_workspace_bytes(c, 0)));
+  if (c->M == 0) return LAQ_OK;
+  LAQ_TRY(check_tensor(e, "x", c->x, true, c->ld_x, c->K, 2));
+  LAQ_TRY(check_tensor(e, "w", c->w, true, c->ld_w, c->K, 2));
+  LAQ_TRY(check_tensor(e, "bias", c->bias, false, c->N, c->N, 2));
+  LAQ_TRY(check_tensor(e, "residual", c->residual, false, c->ld_residual, c->N, 2));
+  LAQ_TRY(check_tensor(e, "y", c->y, true, c->ld_y, c->N, 2));
+  LAQ_TRY(check_tensor(e, "z", c->z, false, c->ld_z, c->N, 2));
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  char* ws = (char*)d_workspace;
+  Operand x{c->x, c->ld_x, c->M, c->K}, w{c->w, c->ld_w, c->N, c->K};
+  LAQ_TRY(make_mappable(e, x, ws, st));
+  LAQ_TRY(make_mappable(e, w, ws, st));
+  Epilogue ep;
+  ep.out = c->y;
+  ep.ldo = c->ld_y;
+  ep.act = c->activation;
+  ep.bias = c->bias;
+  ep.residual = c->residual;
+  ep.ldr = c->ld_residual;
+  ep.z = c->z;
+  ep.ldz = c->ld_z;
+  return product(e, c->dtype, x, false, w, false, ep, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, st);
+}
+
+extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream,
+                                          char* errbuf, size_t errbuf_len) {
+  const Err e{errbuf, errbuf_len};
+  LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, laq_linear_workspace_bytes(c, 1)));
+  if (!c->dx && !c->dw && !c->db) return LAQ_OK;
+  const bool act = c->activation != LAQ_ACT_NONE;
+  const int dw_bytes = c->dw_dtype == LAQ_F32 ? 4 : 2;
+  if (c->dw && c->dw_dtype != c->dtype && c->dw_dtype != LAQ_F32)
+    return fail(errbuf, errbuf_len, LAQ_EINVAL, "dw_dtype must be the call's dtype or LAQ_F32");
+  if (c->dw && c->dw_dtype == LAQ_F32 && act && c->activation != LAQ_ACT_RELU)
+    return fail(errbuf, errbuf_len, LAQ_EINVAL,
+                "dw in fp32 needs no activation or ReLU: with the others dZ is rounded to 16 bits before the product");
+  LAQ_TRY(check_tensor(e, "dw", c->dw, false, c->ld_dw, c->K, dw_bytes));
+  LAQ_TRY(check_tensor(e, "db", c->db, false, c->N, c->N, 4));
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  if (c->M == 0) {               // sums over no rows
+    if (c->dw && cudaMemset2DAsync(c->dw, (size_t)c->ld_dw * dw_bytes, 0, (size_t)c->K * dw_bytes, (size_t)c->N, st) != cudaSuccess)
+      return fail(errbuf, errbuf_len, LAQ_ECUDA, "cudaMemset2DAsync failed");
+    if (c->db && cudaMemsetAsync(c->db, 0, (size_t)c->N * 4, st) != cudaSuccess)
+      return fail(errbuf, errbuf_len, LAQ_ECUDA, "cudaMemsetAsync failed");
+    return LAQ_OK;
+  }
+  LAQ_TRY(check_tensor(e, "dy", c->dy, true, c->ld_dy, c->N, 2));
+  LAQ_TRY(check_tensor(e, "z", c->z, act, c->ld_z, c->N, 2));
+  LAQ_TRY(check_tensor(e, "x", c->x, c->dw != nullptr, c->ld_x, c->K, 2));
+  LAQ_TRY(check_tensor(e, "w", c->w, c->dx != nullptr, c->ld_w, c->K, 2));
+  LAQ_TRY(check_tensor(e, "dx", c->dx, false, c->ld_dx, c->K, 2));
+  BackwardNeeds need(c);
+  char* ws = (char*)d_workspace;
+  const bool starve = (c->flags & LAQ_LINEAR_STARVE) != 0;
+  if (need.own_dz || c->db) {
+    void* dz = need.own_dz ? ws : nullptr;
+    float* part = c->db ? (float*)(ws + need.dz_bytes) : nullptr;
+    ws += need.dz_bytes + need.part_bytes;
+    const int per = dz_rows_per(c->M, c->N), runs = (int)((c->M + per - 1) / per), N = (int)c->N;
+    const dim3 grid((unsigned)((c->N + kDzCols - 1) / kDzCols), (unsigned)runs);
+    const int vec_ok = mappable(c->dy, c->ld_dy) && (!act || mappable(c->z, c->ld_z));
+    if (c->dtype == LAQ_BF16)
+      linear_dz_kernel<__nv_bfloat16><<<grid, kDzThreads, 0, st>>>((const __nv_bfloat16*)c->dy, c->ld_dy, (const __nv_bfloat16*)c->z,
+                                                                   c->ld_z, (__nv_bfloat16*)dz, pad8(c->N), part, c->M, N,
+                                                                   c->activation, per, vec_ok);
+    else
+      linear_dz_kernel<__half><<<grid, kDzThreads, 0, st>>>((const __half*)c->dy, c->ld_dy, (const __half*)c->z, c->ld_z, (__half*)dz,
+                                                            pad8(c->N), part, c->M, N, c->activation, per, vec_ok);
+    if (cudaGetLastError() != cudaSuccess) return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
+    if (c->db) {
+      linear_db_kernel<<<(unsigned)((c->N + 31) / 32), 256, 0, st>>>(part, runs, N, c->db);
+      if (cudaGetLastError() != cudaSuccess) return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
+    }
+    if (need.own_dz) {
+      need.dz.p = dz;
+      need.dz.ld = pad8(c->N);
+    }
+  }
+  if (c->dx) {
+    LAQ_TRY(make_mappable(e, need.w, ws, st));
+    Epilogue ep;
+    ep.out = c->dx;
+    ep.ldo = c->ld_dx;
+    LAQ_TRY(product(e, c->dtype, need.dz, false, need.w, true, ep, c->status, starve, true, st));
+  }
+  if (c->dw) {
+    LAQ_TRY(make_mappable(e, need.x, ws, st));
+    Epilogue ep;
+    ep.out = c->dw;
+    ep.ldo = c->ld_dw;
+    ep.out_f32 = c->dw_dtype == LAQ_F32;
+    LAQ_TRY(product(e, c->dtype, need.dz, true, need.x, true, ep, c->status, starve, false, st));
+  }
+  return LAQ_OK;
+}

@@ -20,7 +20,9 @@ FLAG_STORE_G = 4
 FLAG_SPARSE_X = 8
 
 EXPORTS = ["laq_workspace_bytes", "laq_init", "laq_load_shards", "laq_set_gradients", "laq_step", "laq_step_local", "laq_local_uploads", "laq_apply_uploads", "laq_sync",
-           "laq_get_state", "laq_get_worker", "laq_set_state", "laq_kernel_launches", "laq_tune", "laq_query", "laq_set_profiling", "laq_kernel_times", "laq_quantize_worker_static", "laq_last_error", "laq_destroy"]
+           "laq_get_state", "laq_get_worker", "laq_set_state", "laq_kernel_launches", "laq_tune", "laq_query", "laq_set_profiling", "laq_kernel_times", "laq_quantize_worker_static",
+           "laq_token_logprobs", "laq_token_logprobs_backward", "laq_distill", "laq_distill_backward",
+           "laq_linear_workspace_bytes", "laq_linear_forward", "laq_linear_backward", "laq_last_error", "laq_destroy"]
 
 
 class LaqError(RuntimeError):
@@ -49,6 +51,15 @@ class laq_state(C.Structure):
                 ("clock", C.c_void_p), ("ring", C.c_void_p), ("counters", C.c_void_p), ("g", C.c_void_p),
                 ("codes", C.c_void_p), ("R", C.c_void_p), ("n_dq", C.c_void_p), ("n_eps", C.c_void_p),
                 ("skip", C.c_void_p)]
+
+
+class laq_linear_call(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32), ("M", C.c_int64), ("N", C.c_int64), ("K", C.c_int64),
+                ("x", C.c_void_p), ("ld_x", C.c_int64), ("w", C.c_void_p), ("ld_w", C.c_int64), ("bias", C.c_void_p),
+                ("residual", C.c_void_p), ("ld_residual", C.c_int64), ("y", C.c_void_p), ("ld_y", C.c_int64),
+                ("z", C.c_void_p), ("ld_z", C.c_int64), ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("dx", C.c_void_p),
+                ("ld_dx", C.c_int64), ("dw", C.c_void_p), ("ld_dw", C.c_int64), ("db", C.c_void_p),
+                ("dw_dtype", C.c_int32), ("flags", C.c_uint32), ("status", C.c_void_p)]
 
 
 _lib = None
@@ -84,6 +95,17 @@ def load_library():
     L.laq_kernel_times.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p]
     L.laq_quantize_worker_static.argtypes = [C.c_void_p, C.c_void_p, C.c_int64, C.c_int32, C.c_void_p, C.c_void_p,
                                              C.c_void_p, C.c_void_p, C.c_char_p, C.c_size_t]
+    rows = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, C.c_float]     # logits, dtype, rows, vocab, stride, temperature
+    tail = [C.c_void_p, C.c_char_p, C.c_size_t]                                    # stream, error text
+    teacher = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int64]
+    L.laq_token_logprobs.argtypes = rows + [C.c_void_p, C.c_int32] + [C.c_void_p] * 5 + tail
+    L.laq_token_logprobs_backward.argtypes = rows + [C.c_void_p] * 6 + [C.c_int64] + tail
+    L.laq_distill.argtypes = rows + teacher + [C.c_void_p] * 4 + [C.c_int64] + tail
+    L.laq_distill_backward.argtypes = rows + teacher + [C.c_void_p] * 3 + [C.c_int64] + tail
+    L.laq_linear_workspace_bytes.argtypes = [C.POINTER(laq_linear_call), C.c_int32]
+    L.laq_linear_workspace_bytes.restype = C.c_size_t
+    L.laq_linear_forward.argtypes = [C.POINTER(laq_linear_call), C.c_void_p, C.c_size_t] + tail
+    L.laq_linear_backward.argtypes = [C.POINTER(laq_linear_call), C.c_void_p, C.c_size_t] + tail
     L.laq_last_error.argtypes = [C.c_void_p]
     L.laq_last_error.restype = C.c_char_p
     L.laq_destroy.argtypes = [C.c_void_p]
