@@ -5,6 +5,7 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
+#include <float.h>
 #include <stdint.h>
 
 #include <cstdarg>
@@ -57,6 +58,35 @@ __device__ __forceinline__ float ex2(float x) {
   return r;
 }
 
+// Two fp32 numbers in a register pair: one instruction for both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair_of(float a, float b) {
+  f32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ void split(f32x2 p, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(p)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+  f32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 mul2(f32x2 a, f32x2 b) {
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ f32x2 ex2x2(f32x2 p) {
+  float a, b;
+  split(p, a, b);
+  return pair_of(ex2(a), ex2(b));
+}
+
 template <class T>
 struct Elem;
 
@@ -72,6 +102,15 @@ struct Elem<float> {
   }
   static __device__ __forceinline__ uint4 pack(const float (&x)[4]) {
     return make_uint4(__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
+  }
+  static __device__ __forceinline__ void pairs(const uint4& v, f32x2 (&p)[2]) {
+    p[0] = pair_of(__uint_as_float(v.x), __uint_as_float(v.y));
+    p[1] = pair_of(__uint_as_float(v.z), __uint_as_float(v.w));
+  }
+  // a bound no larger than `lo`, as a word of elements; 0 if the type has no finite one
+  static __device__ __forceinline__ uint32_t bound(float lo) { return fabsf(lo) < FLT_MAX ? __float_as_uint(lo) : 0u; }
+  static __device__ __forceinline__ uint32_t at_least1(uint32_t w, uint32_t lo) {
+    return __float_as_uint(max_nan(__uint_as_float(w), __uint_as_float(lo)));
   }
   static __device__ __forceinline__ float to_float(float v) { return v; }
   static __device__ __forceinline__ float from_float(float v) { return v; }
@@ -107,6 +146,31 @@ struct Elem<__nv_bfloat16> {
       w[i] = *reinterpret_cast<const uint32_t*>(&h);
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ void pairs(const uint4& v, f32x2 (&p)[4]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = pair_of(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
+  }
+  static __device__ __forceinline__ uint4 pack_pairs(const f32x2 (&p)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b;
+      split(p[i], a, b);
+      const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ uint32_t bound(float lo) {
+    const __nv_bfloat16 h = __float2bfloat16_rd(lo);
+    const uint32_t b = *reinterpret_cast<const uint16_t*>(&h);
+    return fabsf(__bfloat162float(h)) < INFINITY ? b | (b << 16) : 0u;
+  }
+  static __device__ __forceinline__ uint32_t at_least1(uint32_t w, uint32_t lo) {
+    const __nv_bfloat162 r = __hmax2_nan(pair(w), pair(lo));
+    return *reinterpret_cast<const uint32_t*>(&r);
   }
   static __device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
   static __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bfloat16_rn(v); }
@@ -144,6 +208,34 @@ struct Elem<__half> {
     }
     return make_uint4(w[0], w[1], w[2], w[3]);
   }
+  static __device__ __forceinline__ void pairs(const uint4& v, f32x2 (&p)[4]) {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 f = __half22float2(pair(w[i]));
+      p[i] = pair_of(f.x, f.y);
+    }
+  }
+  static __device__ __forceinline__ uint4 pack_pairs(const f32x2 (&p)[4]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float a, b;
+      split(p[i], a, b);
+      const __half2 h = __floats2half2_rn(a, b);
+      w[i] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ uint32_t bound(float lo) {
+    const __half h = __float2half_rd(lo);
+    const uint32_t b = *reinterpret_cast<const uint16_t*>(&h);
+    return fabsf(__half2float(h)) < INFINITY ? b | (b << 16) : 0u;
+  }
+  static __device__ __forceinline__ uint32_t at_least1(uint32_t w, uint32_t lo) {
+    const __half2 r = __hmax2_nan(pair(w), pair(lo));
+    return *reinterpret_cast<const uint32_t*>(&r);
+  }
   static __device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
   static __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
   template <int N>
@@ -156,11 +248,28 @@ struct Elem<__half> {
   }
 };
 
+// Every element of a vector raised to at least the bound of Elem<T>::bound (a NaN stays).
+template <class T>
+__device__ __forceinline__ uint4 at_least(const uint4& v, uint32_t lo) {
+  return make_uint4(Elem<T>::at_least1(v.x, lo), Elem<T>::at_least1(v.y, lo), Elem<T>::at_least1(v.z, lo), Elem<T>::at_least1(v.w, lo));
+}
+
 // Plain (coherent) 16-byte load and store: a gradient may be written over the tensor that it is computed from.
 __device__ __forceinline__ uint4 load16(const void* p) {
   uint4 v;
   asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
   return v;
+}
+
+// 16 bytes from global to shared memory in the background; a thread waits for its own copies and reads only those, so no
+// barrier is involved.  Commits group the copies; wait<N> returns when all but the last N groups have landed.
+__device__ __forceinline__ void copy16(void* smem, const void* p) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(smem)), "l"(p) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
 }
 
 }  // namespace ops

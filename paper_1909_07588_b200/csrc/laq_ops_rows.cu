@@ -18,6 +18,8 @@
 #include <cooperative_groups.h>
 #include <float.h>
 
+#include <atomic>
+
 #include "laq_ops.cuh"
 
 namespace cg = cooperative_groups;
@@ -27,12 +29,17 @@ namespace ops {
 namespace {
 
 constexpr int kBlock = 256;
+constexpr int kHalfBlock = 128;        // block of the forward pass over rows of middling length, when there are many
+constexpr int kHalfVectors = 2048;     // ... up to this many 16-byte vectors
 constexpr int kWarpBlock = 128;        // block of the kernels whose rows belong to one warp each
 constexpr int kWarpRow = 1024;         // longest row that one warp takes
+constexpr int kWarpVectors = 512;      // ... and in 16-byte vectors, where there are many rows
 constexpr int kMaxCluster = 8;
 constexpr int kMaxTopK = 32;
 constexpr int kMaxTeacher = 128;
 constexpr int kBatch = 4;              // vectors of the streaming loop that a thread has in flight
+constexpr int kRing = 2;               // batches of the streaming loop's ring
+constexpr int kForwardBlocks = 4;      // blocks of it on an SM (by shared memory: ring and alternatives)
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kUnset = -FLT_MAX;     // reference of a thread that has seen nothing above -inf
@@ -78,58 +85,99 @@ struct Slice {
 };
 
 // ---- running softmax statistics ---------------------------------------------------------------------------------------
-// With d = (x - ref) c, c = log2(e) / tau:  s = sum 2^d, u = sum d 2^d.  ref is any number that no x exceeds by more than
-// kSlack / c; it moves only when it must, so the common path has no rescaling.  All of it in fp32; x - ref is taken
-// before the product with c, so that neither the reference nor masks at the type's lowest value lose digits.
+// d = (x - ref) c with c = log2(e) / tau;  s = sum 2^d, u = sum d 2^d.  ref is any number that no x exceeds by more than
+// kSlack / c: it moves only when it must, so the common path has no rescaling.  Two forms of d:
+//   |ref| < kFar   x c - rho with rho = fp32(ref c): one fused operation.  rho itself is the reference then, so its
+//                  rounding does not matter; c's rounding is a change of temperature by 2^-25, the same for all.
+//   otherwise      (x - ref) c.  Such a ref is a mask at the type's lowest value (nothing else has been seen), whose product
+//                  with c may overflow.  A NaN or +inf also ends here and stays.
+constexpr float kFar = 1e30f;
+
 struct Stat {
   float ref, s, u;
 };
 
+__device__ __forceinline__ bool near_ref(float ref) { return fabsf(ref) < kFar; }
+__device__ __forceinline__ float scaled(float x, float ref, float c) {
+  return near_ref(ref) ? fmaf(x, c, -(ref * c)) : (x - ref) * c;
+}
+
 __device__ __forceinline__ void move_ref(Stat& a, float ref, float c) {    // ref >= a.ref, or NaN
-  const float d = max_nan((a.ref - ref) * c, -1e4f);
+  float d = near_ref(ref) && near_ref(a.ref) ? a.ref * c - ref * c : (a.ref - ref) * c;
+  d = max_nan(d, -1e4f);
   const float f = ex2(d);
   a.u = fmaf(d, a.s, a.u) * f;
   a.s *= f;
   a.ref = ref;
 }
 
-template <int N, bool ENTROPY>
-__device__ __forceinline__ void add_elements(Stat& a, const float (&x)[N], float c) {
-  float s0 = 0.f, s1 = 0.f, u0 = 0.f, u1 = 0.f;
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float d = (x[i] - a.ref) * c;
-    if (ENTROPY) d = max_nan(d, -1e4f);       // -inf: 2^d is 0 and so is its share of u
-    const float e = ex2(d);
-    if (i & 1) {
-      s1 += e;
-      if (ENTROPY) u1 = fmaf(e, d, u1);
-    } else {
-      s0 += e;
-      if (ENTROPY) u0 = fmaf(e, d, u0);
+// The statistics while a thread runs over its vectors: two interleaved sums, two elements an instruction.  With ENTROPY
+// the elements are first raised to a bound where 2^d is 0 but d finite (-inf would make 0 * inf of its share of u);
+// `plain` is false where there is no such bound or ref is a mask, and the elements then go one by one.
+template <class T, bool ENTROPY>
+struct Running {
+  f32x2 s2, u2, c2, rho2;
+  float ref, c;
+  uint32_t lo;
+  bool plain;
+
+  __device__ __forceinline__ explicit Running(float c_) : s2(0ull), u2(0ull), c2(pair_of(c_, c_)), rho2(0ull), ref(kUnset), c(c_), lo(0u), plain(false) {}
+  __device__ __forceinline__ Stat get() const {
+    float a, b, d, e;
+    split(s2, a, b);
+    split(u2, d, e);
+    return Stat{ref, a + b, d + e};
+  }
+  __device__ __forceinline__ void set_ref(float r) {
+    ref = r;
+    rho2 = pair_of(-(r * c), -(r * c));
+    plain = near_ref(r);
+    if (ENTROPY) {
+      lo = plain ? Elem<T>::bound(r - 200.f / c) : 0u;
+      plain = plain && lo != 0u;
     }
   }
-  a.s += s0 + s1;
-  if (ENTROPY) a.u += u0 + u1;
-}
-
-__device__ __forceinline__ void follow(Stat& a, float mx, float c) {
-  if (!((mx - a.ref) * c <= kSlack)) move_ref(a, mx, c);      // also taken for NaN, which then stays
-}
-
-template <class T, int N, bool ENTROPY>
-__device__ __forceinline__ void add_vectors(Stat& a, float& top, const uint4 (&v)[N], float c) {
-  constexpr int EV = Elem<T>::EV;
-  const float mx = Elem<T>::largest(v);
-  top = max_nan(top, mx);
-  follow(a, mx, c);
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    float x[EV];
-    Elem<T>::unpack(v[i], x);
-    add_elements<EV, ENTROPY>(a, x, c);
+  __device__ __forceinline__ void follow(float mx) {
+    if (!((mx - ref) * c <= kSlack)) {          // also taken for NaN
+      Stat a = get();
+      move_ref(a, mx, c);
+      s2 = pair_of(a.s, 0.f);
+      u2 = pair_of(a.u, 0.f);
+      set_ref(mx);
+    }
   }
-}
+  __device__ __forceinline__ void one(float x) {
+    float d = scaled(x, ref, c);
+    if (ENTROPY) d = max_nan(d, -1e4f);
+    const float e = ex2(d);
+    s2 = add2(s2, pair_of(e, 0.f));
+    if (ENTROPY) u2 = add2(u2, pair_of(e * d, 0.f));
+  }
+  template <int N>
+  __device__ __forceinline__ void add(const uint4 (&v)[N]) {
+    if (plain) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        f32x2 p[Elem<T>::EV / 2];
+        Elem<T>::pairs(ENTROPY ? at_least<T>(v[i], lo) : v[i], p);
+#pragma unroll
+        for (int e = 0; e < Elem<T>::EV / 2; ++e) {
+          const f32x2 d = fma2(p[e], c2, rho2), w = ex2x2(d);
+          s2 = add2(s2, w);
+          if (ENTROPY) u2 = fma2(w, d, u2);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        float x[Elem<T>::EV];
+        Elem<T>::unpack(v[i], x);
+#pragma unroll
+        for (int e = 0; e < Elem<T>::EV; ++e) one(x[e]);
+      }
+    }
+  }
+};
 
 __device__ __forceinline__ Stat join(Stat a, Stat b, float c) {
   const float r = max_nan(a.ref, b.ref);
@@ -153,27 +201,27 @@ __device__ __forceinline__ Stat warp_join(Stat a, float c) {
   return a;
 }
 
-// What a row needs of its statistics.
+// What a row needs of its statistics.  unit = 1 / (tau c): from powers of two back to natural logarithms, with c as it is.
 struct RowSum {
-  float ref, log2s, lse, entropy;
+  float ref, log2s, lse, entropy, c, unit;
   bool empty;       // nothing above -inf
-  __device__ __forceinline__ RowSum(const Stat& a, float inv_tau) {
+  __device__ __forceinline__ RowSum(const Stat& a, float c_, float unit_, float inv_tau) : c(c_), unit(unit_) {
     empty = a.s == 0.f;
     ref = a.ref;
     log2s = log2f(a.s);
-    lse = empty ? -INFINITY : fmaf(a.ref, inv_tau, log2s * kLn2);
-    entropy = empty ? 0.f : max_nan((log2s - a.u / a.s) * kLn2, 0.f);
+    lse = empty ? -INFINITY : near_ref(ref) ? (ref * c + log2s) * unit : fmaf(ref, inv_tau, log2s * unit);
+    entropy = empty ? 0.f : max_nan((log2s - a.u / a.s) * unit, 0.f);
   }
-  __device__ __forceinline__ float logp(float x, float c) const {
+  __device__ __forceinline__ float logp(float x) const {
     if (x == -INFINITY) return log2s != log2s ? log2s : x;
-    return fmaf(x - ref, c, -log2s) * kLn2;
+    return (scaled(x, ref, c) - log2s) * unit;
   }
 };
 
 // ---- top alternatives -------------------------------------------------------------------------------------------------
 // Candidates are 64-bit keys that order by logit, then by lowest index.  Logits at -inf are no alternatives.
 constexpr uint32_t kKeyNegInf = 0x007fffffu;     // order_bits(-inf)
-constexpr int kCandBlock = 1024, kCandWarp = 128;
+constexpr int kCandBlock = 512, kCandWarp = 128;
 
 __device__ __forceinline__ uint32_t order_bits(float x) {
   const uint32_t b = __float_as_uint(x + 0.f);   // -0 counts as 0
@@ -186,6 +234,8 @@ __device__ __forceinline__ unsigned long long cand_key(uint32_t bits, int j) {
   return ((unsigned long long)bits << 32) | (0xffffffffu - (uint32_t)j);
 }
 
+constexpr int kSlots = 8, kMaxHits = 512;
+
 template <int NT>
 struct TopShared {
   static constexpr int kCap = NT == 32 ? kCandWarp : kCandBlock;
@@ -194,23 +244,70 @@ struct TopShared {
   unsigned long long wmax[Group<NT>::kWarps];
   uint32_t wthr[Group<NT>::kWarps];
   int wcount[Group<NT>::kWarps];
-  int n;
+  int n, nhit;
+  float slot[NT == 32 ? 1 : kSlots][NT == 32 ? 1 : NT];      // largest logit of each thread's runs of batches
+  uint16_t hit[NT == 32 ? 1 : kMaxHits];
 };
 
-// Calls f(order bits, index) for every element of this thread.
-template <class T, int NT, class F>
-__device__ __forceinline__ void each_element(const Slice<T>& sl, F f) {
-  constexpr int EV = Elem<T>::EV;
-  const int t = Group<NT>::tid();
-#pragma unroll 2
-  for (int v = sl.v0 + t; v < sl.v1; v += NT) {
-    float x[EV];
-    Elem<T>::unpack(load16(sl.vec(v)), x);
-#pragma unroll
-    for (int i = 0; i < EV; ++i) f(order_bits(x[i]), sl.head + v * EV + i);
+// How a thread's vectors fall into batches of kBatch (those it reads together), runs of 2^shift batches (a slot each)
+// and a rest of fewer than kBatch vectors and its edge element.
+template <class T, int NT>
+struct Batches {
+  int span, shift;
+  __device__ __forceinline__ explicit Batches(const Slice<T>& sl) : span(sl.v1 - sl.v0), shift(0) {
+    const int most = (span + kBatch * NT - 1) / (kBatch * NT);
+    while ((max(most, 1) - 1) >> shift >= kSlots) ++shift;
   }
+  __device__ __forceinline__ int of(int t) const {
+    const int left = span - t - (kBatch - 1) * NT;
+    return left > 0 ? (left + kBatch * NT - 1) / (kBatch * NT) : 0;
+  }
+};
+
+// f(x, index) for the elements of a vector that are at least thr.
+template <class T, class F>
+__device__ __forceinline__ void pick(const uint4& v, int j0, float thr, F f) {
+  constexpr int EV = Elem<T>::EV;
+  const uint4 one[1] = {v};
+  if (Elem<T>::largest(one) >= thr) {
+    float x[EV];
+    Elem<T>::unpack(v, x);
+#pragma unroll
+    for (int i = 0; i < EV; ++i)
+      if (x[i] >= thr) f(x[i], j0 + i);
+  }
+}
+
+// Hands the elements of a vector that are at least thr to the group's candidates, one reservation for all of them.
+template <class T, int NT>
+__device__ __forceinline__ void take_vector(TopShared<NT>& sh, const uint4& v, int j0, float thr) {
+  constexpr int EV = Elem<T>::EV;
+  float x[EV];
+  Elem<T>::unpack(v, x);
+  int count = 0;
+#pragma unroll
+  for (int i = 0; i < EV; ++i) count += x[i] >= thr;
+  if (count == 0) return;
+  int at = atomicAdd(&sh.n, count);
+#pragma unroll
+  for (int i = 0; i < EV; ++i)
+    if (x[i] >= thr) {
+      if (at < TopShared<NT>::kCap) sh.cand[at] = cand_key(order_bits(x[i]), j0 + i);
+      ++at;
+    }
+}
+
+// The same for all elements of this thread.
+template <class T, int NT, class F>
+__device__ __forceinline__ void each_element(const Slice<T>& sl, float thr, F f) {
+  const int t = Group<NT>::tid();
+#pragma unroll 4
+  for (int v = sl.v0 + t; v < sl.v1; v += NT) pick<T>(load16(sl.vec(v)), sl.head + v * Elem<T>::EV, thr, f);
   const int j = sl.edge(t);
-  if (j >= 0) f(order_bits(Elem<T>::to_float(sl.row[j])), j);
+  if (j >= 0) {
+    const float x = Elem<T>::to_float(sl.row[j]);
+    if (x >= thr) f(x, j);
+  }
 }
 
 // The k largest of sh.cand[0..n) in order into sh.best (0 where there are fewer): a candidate's place is the number of
@@ -230,51 +327,88 @@ __device__ __forceinline__ void rank_candidates(TopShared<NT>& sh, int n, int k)
   Group<NT>::sync();
 }
 
-// The k best of the group's slice into sh.best.  `top` is this thread's largest logit (-inf if it has none).
+// The k best of the group's slice into sh.best.  `top` is this thread's largest logit (-inf if it has none), `rest` that of
+// its vectors outside the batches.
 //
 // Threshold: every warp names its ceil(k / warps)-th largest of its lanes' maxima; the smallest of those has at least k
-// elements at or above it, so only the elements that reach it can be among the k best, typically a few dozen: the few
-// threads that own them read their part of the row again (from L2) and hand them over.  When more than kCap reach it
-// (thousands of equal logits), elements above it are taken first and the ones equal to it by a scan in index order that
-// ends as soon as enough are found; and when even too many lie above it, k rounds of an arg-max do it.
+// elements at or above it, so only the elements that reach it can be among the k best, typically some dozens.  The
+// batches that hold them are known from the slots' maxima: the block lists those and reads them once more (from L2), a
+// vector a thread, instead of every thread its whole part.  When more than kCap elements (or kMaxHits runs) reach the
+// threshold (thousands of equal logits), elements above it are taken first and the ones equal to it by a scan in index order
+// that ends as soon as enough are found; and when even too many lie above it, k rounds of an arg-max do it.
 template <class T, int NT>
-__device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, float top, int k) {
+__device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, const uint4* ring, float top, float rest, int k) {
   using G = Group<NT>;
   constexpr int kCap = TopShared<NT>::kCap;
   const int t = G::tid(), lane = threadIdx.x & 31, w = NT == 32 ? 0 : (int)(threadIdx.x >> 5);
   const uint32_t mine = order_bits(top);
-  uint32_t left = mine, thr = 0;
+  uint32_t left = mine, key = 0;
   for (int i = (k + G::kWarps - 1) / G::kWarps; i > 0; --i) {
-    thr = __reduce_max_sync(0xffffffffu, left);
-    const uint32_t who = __ballot_sync(0xffffffffu, left == thr);
+    key = __reduce_max_sync(0xffffffffu, left);
+    const uint32_t who = __ballot_sync(0xffffffffu, left == key);
     if (lane == __ffs(who) - 1) left = 0;
   }
-  if (t == 0) sh.n = 0;
-  if (lane == 0) sh.wthr[w] = thr;
+  if (t == 0) sh.n = sh.nhit = 0;
+  if (lane == 0) sh.wthr[w] = key;
   G::sync();
-  thr = sh.wthr[0];
+  key = sh.wthr[0];
 #pragma unroll
-  for (int i = 1; i < G::kWarps; ++i) thr = min(thr, sh.wthr[i]);
-  thr = max(thr, kKeyNegInf + 1);
-  if (mine >= thr)
-    each_element<T, NT>(sl, [&](uint32_t b, int j) {
-      if (b >= thr) {
-        const int at = atomicAdd(&sh.n, 1);
-        if (at < kCap) sh.cand[at] = cand_key(b, j);
+  for (int i = 1; i < G::kWarps; ++i) key = min(key, sh.wthr[i]);
+  key = max(key, kKeyNegInf + 1);
+  const float thr = from_order_bits(key);
+  auto take = [&](float x, int j) {
+    const int at = atomicAdd(&sh.n, 1);
+    if (at < kCap) sh.cand[at] = cand_key(order_bits(x), j);
+  };
+  if constexpr (NT == 32) {
+    if (mine >= key) each_element<T, NT>(sl, thr, take);
+    G::sync();
+  } else {
+    const Batches<T, NT> bt(sl);
+    if (mine >= key) {
+      const int slots = (bt.of(t) + (1 << bt.shift) - 1) >> bt.shift;
+      for (int i = 0; i <= slots; ++i) {
+        const bool last = i == slots;
+        if ((last ? rest : sh.slot[i][t]) >= thr) {
+          const int at = atomicAdd(&sh.nhit, 1);
+          if (at < kMaxHits) sh.hit[at] = (uint16_t)((last ? kSlots : i) << 8 | t);
+        }
       }
-    });
-  G::sync();
+    }
+    __syncthreads();
+    const int hits = sh.nhit, per = kBatch << bt.shift;
+    if (hits <= kMaxHits) {
+      for (int i = t; i < hits * per; i += NT) {
+        const int h = sh.hit[i / per], in = i % per, who = h & 255, slot = h >> 8, mb = bt.of(who);
+        const int batch = slot == kSlots ? mb : (slot << bt.shift) + in / kBatch;
+        if (slot == kSlots ? in >= kBatch : batch >= mb) continue;
+        if (slot == kSlots && in == kBatch - 1) {          // the rest has at most kBatch - 1 vectors, and the edge
+          const int j = sl.edge(who);
+          if (j >= 0) {
+            const float x = Elem<T>::to_float(sl.row[j]);
+            if (x >= thr) take(x, j);
+          }
+          continue;
+        }
+        const int v = sl.v0 + who + NT * (kBatch * batch + in % kBatch);
+        // the last batches are still in the ring
+        if (v < sl.v1)
+          take_vector<T, NT>(sh, slot != kSlots && batch + kRing >= mb ? ring[((batch % kRing) * kBatch + in % kBatch) * NT + who] : load16(sl.vec(v)),
+                             sl.head + v * Elem<T>::EV, thr);
+      }
+    } else if (t == 0) {
+      sh.n = kCap + 1;
+    }
+    __syncthreads();
+  }
   int n = sh.n;
   if (n > kCap) {
     G::sync();
     if (t == 0) sh.n = 0;
     G::sync();
-    if (mine > thr)
-      each_element<T, NT>(sl, [&](uint32_t b, int j) {
-        if (b > thr) {
-          const int at = atomicAdd(&sh.n, 1);
-          if (at < kCap) sh.cand[at] = cand_key(b, j);
-        }
+    if (mine > key)
+      each_element<T, NT>(sl, thr, [&](float x, int j) {
+        if (x > thr) take(x, j);
       });
     G::sync();
     n = sh.n;
@@ -283,9 +417,9 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, float top, i
       int found = 0;
       for (; found < k; ++found) {
         unsigned long long best = 0ull;
-        each_element<T, NT>(sl, [&](uint32_t b, int j) {
-          const unsigned long long key = cand_key(b, j);
-          if (b > kKeyNegInf && key < last && key > best) best = key;
+        each_element<T, NT>(sl, -FLT_MAX, [&](float x, int j) {
+          const unsigned long long c = cand_key(order_bits(x), j);
+          if (c < last && c > best) best = c;
         });
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) {
@@ -306,8 +440,8 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, float top, i
     } else {
       for (int base = sl.e0; n < k && base < sl.e1; base += NT) {     // ties at the threshold, lowest index first
         const int j = base + t;
-        const bool hit = j < sl.e1 && order_bits(Elem<T>::to_float(sl.row[j])) == thr;
-        const uint32_t b = __ballot_sync(0xffffffffu, hit);
+        const bool same = j < sl.e1 && Elem<T>::to_float(sl.row[j]) == thr;
+        const uint32_t b = __ballot_sync(0xffffffffu, same);
         if (lane == 0) sh.wcount[w] = __popc(b);
         G::sync();
         int before = __popc(b & ((1u << lane) - 1u)), all = 0;
@@ -315,7 +449,7 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, float top, i
           if (i < w) before += sh.wcount[i];
           all += sh.wcount[i];
         }
-        if (hit && n + before < k) sh.cand[n + before] = cand_key(thr, j);
+        if (same && n + before < k) sh.cand[n + before] = cand_key(key, j);
         n = min(n + all, k);
         G::sync();
       }
@@ -325,60 +459,99 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, float top, i
 }
 
 // ---- the teacher's side of one row ------------------------------------------------------------------------------------
-// One warp: entry i = lane + 32 e.  q and log q (natural), a column index or -1 where there is no entry.
+// One warp reads the entries and leaves them in shared memory: q and log q (natural), the column or -1 where there is no
+// entry, the student's logit there.
 struct Teacher {
-  float q[kMaxTeacher / 32], logq[kMaxTeacher / 32];
-  int a[kMaxTeacher / 32];
-  bool any, bad;       // a live entry; an index outside the vocabulary
+  alignas(16) float q[kMaxTeacher];
+  alignas(16) int a[kMaxTeacher];
+  float logq[kMaxTeacher], x[kMaxTeacher], mass[kMaxTeacher];
+  int any, bad;        // a live entry; a column outside the vocabulary
 
-  __device__ __forceinline__ void read(const int32_t* idx, const float* val, int K, int V, float inv_tau) {
+  // `need(column)`: whether this warp's block uses the student's logit of the column
+  template <class T, class F>
+  __device__ __forceinline__ void read(const int32_t* idx, const float* val, const T* row, int K, int V, float inv_tau, F need) {
+    constexpr int E = kMaxTeacher / 32;
     const int lane = threadIdx.x & 31;
-    float x[kMaxTeacher / 32];
+    int col[E];
+    float t[E];
     float mx = -INFINITY;
     bool have = false, out = false;
 #pragma unroll
-    for (int e = 0; e < kMaxTeacher / 32; ++e) {
+    for (int e = 0; e < E; ++e) {
       const int i = lane + 32 * e;
-      a[e] = i < K ? idx[i] : -1;
-      if (a[e] >= V) {
-        out = true;
-        a[e] = -1;
-      }
-      x[e] = a[e] >= 0 ? val[i] : -INFINITY;
-      have |= a[e] >= 0;
-      mx = max_nan(mx, x[e]);
+      col[e] = i < K ? idx[i] : -1;
+      t[e] = i < K ? val[i] : -INFINITY;
     }
-    any = __any_sync(0xffffffffu, have || out);
-    bad = __any_sync(0xffffffffu, out);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int i = lane + 32 * e;
+      if (col[e] >= V) {
+        out = true;
+        col[e] = -1;
+      }
+      x[i] = col[e] >= 0 && need(col[e]) ? Elem<T>::to_float(row[col[e]]) : 0.f;
+      if (col[e] < 0) t[e] = -INFINITY;
+      have |= col[e] >= 0;
+      mx = max_nan(mx, t[e]);
+    }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) mx = max_nan(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    if (mx == -INFINITY && !bad) any = false;       // a teacher whose every entry is masked asks for nothing
+    out = __any_sync(0xffffffffu, out);
+    // a teacher whose every entry is masked asks for nothing
+    have = (__any_sync(0xffffffffu, have) && mx != -INFINITY) || out;
     float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < kMaxTeacher / 32; ++e) {
-      x[e] = x[e] == -INFINITY ? -INFINITY : (x[e] - mx) * inv_tau;
-      q[e] = expf(x[e]);
-      sum += q[e];
+    for (int e = 0; e < E; ++e) {
+      t[e] = t[e] == -INFINITY ? -INFINITY : (t[e] - mx) * inv_tau;
+      sum += expf(t[e]);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float ls = logf(sum), inv = 1.f / sum;
 #pragma unroll
-    for (int e = 0; e < kMaxTeacher / 32; ++e) {
-      q[e] *= inv;
-      logq[e] = x[e] - ls;
-      if (a[e] < 0 || !any) q[e] = 0.f;
+    for (int e = 0; e < E; ++e) {
+      const int i = lane + 32 * e;
+      q[i] = col[e] >= 0 && have ? expf(t[e]) * inv : 0.f;
+      logq[i] = t[e] - ls;
+      a[i] = col[e];
     }
+    if (lane == 0) {
+      any = have;
+      bad = out;
+    }
+    __syncwarp();
   }
-  // sum_i q_i (log q_i - log p_i) over the warp's entries, x: the student's logits at the entries
-  __device__ __forceinline__ float divergence(const float (&x)[kMaxTeacher / 32], const RowSum& r, float c) const {
-    float kl = 0.f;
+  // mass[i]: all of the teacher's probability in entry i's column, which may come more than once
+  __device__ __forceinline__ void gather_mass(int K) {
+    constexpr int E = kMaxTeacher / 32;
+    const int lane = threadIdx.x & 31;
+    float m[E] = {};
+    for (int o = 0; o < K; o += 4) {       // entries past K have column -1 and probability 0
+      const int4 ao = *reinterpret_cast<const int4*>(&a[o]);
+      const float4 qo = *reinterpret_cast<const float4*>(&q[o]);
 #pragma unroll
-    for (int e = 0; e < kMaxTeacher / 32; ++e)
-      if (!(q[e] == 0.f)) kl += q[e] * (logq[e] - r.logp(x[e], c));
+      for (int e = 0; e < E; ++e) {
+        if (32 * e >= K) break;
+        const int j = a[lane + 32 * e];
+        m[e] += (ao.x == j ? qo.x : 0.f) + (ao.y == j ? qo.y : 0.f);
+        m[e] += (ao.z == j ? qo.z : 0.f) + (ao.w == j ? qo.w : 0.f);
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) mass[lane + 32 * e] = m[e];
+    __syncwarp();
+  }
+  // loss of the row / tau^2, by the warp that read it: sum_i q_i (log q_i - log p_i)
+  __device__ __forceinline__ float divergence(const RowSum& r, int K) const {
+    if (!any) return 0.f;
+    if (bad) return __int_as_float(0x7fc00000);
+    if (r.empty) return INFINITY;
+    float kl = 0.f;
+    for (int i = threadIdx.x & 31; i < K; i += 32)
+      if (!(q[i] == 0.f)) kl += q[i] * (logq[i] - r.logp(x[i]));
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) kl += __shfl_xor_sync(0xffffffffu, kl, o);
-    return bad ? __int_as_float(0x7fc00000) : kl;
+    return kl;
   }
 };
 
@@ -388,7 +561,7 @@ struct ForwardArgs {
   long long ld, T;
   int V, ranks, k, K;
   long long ld_teacher;
-  float c, inv_tau, tau;
+  float c, inv_tau, tau, unit;
   const int32_t* tokens;
   float *logprob, *entropy, *lse;
   int32_t* top_tokens;
@@ -400,16 +573,18 @@ struct ForwardArgs {
 
 // One pass over the logits: DISTILL = false for token_logprobs, true for the loss of distill without its gradient.
 template <class T, int NT, bool DISTILL>
-__global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, NT == 32 ? 8 : 4) rows_forward_kernel(const ForwardArgs A) {
+__global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kForwardBlocks * kBlock / NT) rows_forward_kernel(const ForwardArgs A) {
   using G = Group<NT>;
-  __shared__ TopShared<NT> top_sh[G::kRowsPerBlock];
+  __shared__ TopShared<NT> top_sh[DISTILL ? 1 : G::kRowsPerBlock];
+  __shared__ Teacher teacher_sh[DISTILL ? G::kRowsPerBlock : 1];
   __shared__ Stat wstat[G::kRowsPerBlock][G::kWarps];
   const int t = G::tid(), lane = threadIdx.x & 31, w = NT == 32 ? 0 : (int)(threadIdx.x >> 5);
   const int ranks = NT == 32 ? 1 : A.ranks;
   const int rank = NT == 32 ? 0 : (int)(blockIdx.x % (unsigned)ranks);
   const long long row = NT == 32 ? (long long)blockIdx.x * G::kRowsPerBlock + G::slot() : (long long)(blockIdx.x / (unsigned)ranks);
   if (NT == 32 && row >= A.T) return;
-  TopShared<NT>& sh = top_sh[G::slot()];
+  TopShared<NT>& sh = top_sh[DISTILL ? 0 : G::slot()];
+  Teacher& te = teacher_sh[DISTILL ? G::slot() : 0];
   const T* xr = reinterpret_cast<const T*>(A.x) + row * A.ld;
   const int k = DISTILL ? 0 : A.k;
 
@@ -417,50 +592,83 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, NT == 32 ? 8 :
   const float c = A.c;
   int token = -1;
   if (!DISTILL && A.tokens) token = A.tokens[row];
-  // the first batch is on its way before anything is known about the row
+  // The first batches are on their way before anything is known about the row.  A block's threads keep kRing batches
+  // each in flight through shared memory (a warp's row is short: one batch ahead in registers).
+  extern __shared__ uint4 ring[];        // [kRing][kBatch][NT], a thread's own column
+  const Batches<T, NT> bt(sl);
+  const int batches = bt.of(t);
   int v = sl.v0 + t;
-  uint4 x[kBatch];
-  bool more = v + (kBatch - 1) * NT < sl.v1;
-  if (more) {
+  auto fetch = [&](int b) {              // batch b into its place of the ring
+    if (b < batches) {
 #pragma unroll
-    for (int i = 0; i < kBatch; ++i) x[i] = load16(sl.vec(v + i * NT));
-  }
-  const bool bad_token = token >= A.V;
-  bool live = DISTILL || !A.tokens || token >= 0;
-  Teacher te;
-  if (DISTILL && w == 0 && rank == 0) {
-    te.read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, A.K, A.V, A.inv_tau);
-    live = te.any;                       // this warp writes the row's result; the row is read in any case
-  }
-  Stat a{kUnset, 0.f, 0.f};
-  float top = -INFINITY;
-  if (DISTILL || live) {
-    while (more) {
-      uint4 y[kBatch];
-      v += kBatch * NT;
-      more = v + (kBatch - 1) * NT < sl.v1;
-      if (more) {
-#pragma unroll
-        for (int i = 0; i < kBatch; ++i) y[i] = load16(sl.vec(v + i * NT));
-      }
-      add_vectors<T, kBatch, !DISTILL>(a, top, x, c);
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) x[i] = y[i];
+      for (int i = 0; i < kBatch; ++i) copy16(&ring[((b % kRing) * kBatch + i) * NT + t], sl.vec(v + (b * kBatch + i) * NT));
     }
+    copy_commit();
+  };
+  uint4 x[kBatch];
+  if constexpr (NT == 32) {
+    if (batches > 0) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) x[i] = load16(sl.vec(v + i * NT));
+    }
+  } else {
+#pragma unroll
+    for (int b = 0; b < kRing - 1; ++b) fetch(b);
+  }
+  const bool bad_token = token >= A.V, live = DISTILL || !A.tokens || token >= 0;
+  if (DISTILL && w == 0 && rank == 0)
+    te.read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, xr, A.K, A.V, A.inv_tau,
+            [](int) { return true; });
+  Running<T, !DISTILL> run(c);
+  float top = -INFINITY, rest = -INFINITY;
+  if (live) {
+    float high = -INFINITY;              // of the slot
+    for (int b = 0; b < batches; ++b) {
+      uint4 y[NT == 32 ? kBatch : 1];
+      if constexpr (NT == 32) {
+        if (b + 1 < batches) {
+#pragma unroll
+          for (int i = 0; i < kBatch; ++i) y[i] = load16(sl.vec(v + ((b + 1) * kBatch + i) * NT));
+        }
+      } else {
+        fetch(b + kRing - 1);
+        copy_wait<kRing - 1>();
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) x[i] = ring[((b % kRing) * kBatch + i) * NT + t];
+      }
+      const float mx = Elem<T>::largest(x);
+      run.follow(mx);
+      run.add(x);
+      if (NT > 32 && k > 0) {
+        high = max_nan(high, mx);
+        sh.slot[b >> bt.shift][t] = high;
+        if (((b + 1) & ((1 << bt.shift) - 1)) == 0) high = -INFINITY;
+      }
+      top = max_nan(top, mx);
+      if constexpr (NT == 32) {
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) x[i] = y[i];
+      }
+    }
+    v += batches * kBatch * NT;
     for (; v < sl.v1; v += NT) {
-      uint4 y[1];
-      y[0] = load16(sl.vec(v));
-      add_vectors<T, 1, !DISTILL>(a, top, y, c);
+      const uint4 y[1] = {load16(sl.vec(v))};
+      const float mx = Elem<T>::largest(y);
+      rest = max_nan(rest, mx);
+      run.follow(mx);
+      run.add(y);
     }
     const int j = sl.edge(t);
     if (j >= 0) {
-      const float e[1] = {Elem<T>::to_float(xr[j])};
-      top = max_nan(top, e[0]);
-      follow(a, e[0], c);
-      add_elements<1, !DISTILL>(a, e, c);
+      const float e = Elem<T>::to_float(xr[j]);
+      rest = max_nan(rest, e);
+      run.follow(e);
+      run.one(e);
     }
+    top = max_nan(top, rest);
   }
-  a = warp_join(a, c);
+  if (NT > 32) copy_wait<0>();           // of a row that was not looked at
+  Stat a = warp_join(run.get(), c);
   if (NT > 32) {
     if (lane == 0) wstat[0][w] = a;
     __syncthreads();
@@ -469,7 +677,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, NT == 32 ? 8 :
     for (int i = 1; i < G::kWarps; ++i) a = join(a, wstat[0][i], c);
   }
   const bool alternatives = !DISTILL && k > 0 && live;
-  if (alternatives) top_of_slice<T, NT>(sh, sl, top, k);
+  if (alternatives) top_of_slice<T, NT>(sh, sl, ring, top, rest, k);
   if (ranks > 1) {       // the first block of the cluster takes the others' results
     cg::cluster_group cluster = cg::this_cluster();
     __syncthreads();
@@ -478,34 +686,28 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, NT == 32 ? 8 :
     if (rank == 0) {
       for (int r = 1; r < ranks; ++r) a = join(a, *cluster.map_shared_rank(&wstat[0][0], r), c);
       if (alternatives) {
-        for (int i = t; i < ranks * kMaxTopK; i += NT)
-          sh.cand[i] = i % kMaxTopK < k ? cluster.map_shared_rank(sh.best, i / kMaxTopK)[i % kMaxTopK] : 0ull;
+        if (t < ranks * kMaxTopK && t % kMaxTopK < k)
+          sh.cand[t / kMaxTopK * k + t % kMaxTopK] = cluster.map_shared_rank(sh.best, t / kMaxTopK)[t % kMaxTopK];
         __syncthreads();
       }
     }
     cluster.sync();
     if (rank != 0) return;
-    if (alternatives) rank_candidates<NT>(sh, ranks * kMaxTopK, k);
+    if (alternatives) rank_candidates<NT>(sh, ranks * k, k);
   }
-  const RowSum r(a, A.inv_tau);
+  const RowSum r(a, c, A.unit, A.inv_tau);
   if (DISTILL) {
     if (w == 0) {
-      float kl = 0.f;
-      if (live) {
-        float xs[kMaxTeacher / 32];
-#pragma unroll
-        for (int e = 0; e < kMaxTeacher / 32; ++e) xs[e] = te.a[e] >= 0 ? Elem<T>::to_float(xr[te.a[e]]) : 0.f;
-        kl = r.empty && !te.bad ? INFINITY : te.divergence(xs, r, c);
-      }
+      const float kl = te.divergence(r, A.K);
       if (lane == 0) {
-        A.loss[row] = live ? A.tau * A.tau * kl : 0.f;
-        if (A.lse) A.lse[row] = live ? r.lse : 0.f;
+        A.loss[row] = A.tau * A.tau * kl;
+        A.lse[row] = te.any ? r.lse : 0.f;
       }
     }
     return;
   }
   if (t == 0) {
-    if (A.logprob) A.logprob[row] = !live ? 0.f : bad_token ? __int_as_float(0x7fc00000) : r.logp(Elem<T>::to_float(xr[token]), c);
+    if (A.logprob) A.logprob[row] = !live ? 0.f : bad_token ? __int_as_float(0x7fc00000) : r.logp(Elem<T>::to_float(xr[token]));
     if (A.entropy) A.entropy[row] = live ? r.entropy : 0.f;
     if (A.lse) A.lse[row] = live ? r.lse : 0.f;
   }
@@ -513,7 +715,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, NT == 32 ? 8 :
     const bool nan = live && r.log2s != r.log2s;
     const unsigned long long key = live && !nan ? sh.best[i] : 0ull;
     A.top_tokens[row * k + i] = key ? (int32_t)(0xffffffffu - (uint32_t)key) : -1;
-    A.top_logprobs[row * k + i] = nan ? r.log2s : key ? r.logp(from_order_bits((uint32_t)(key >> 32)), c) : -INFINITY;
+    A.top_logprobs[row * k + i] = nan ? r.log2s : key ? r.logp(from_order_bits((uint32_t)(key >> 32))) : -INFINITY;
   }
 }
 
@@ -524,7 +726,7 @@ struct GradArgs {
   long long ld, ld_d, T;
   int V, ranks, K;
   long long ld_teacher;
-  float c, inv_tau, inv_tau_lo, tau;
+  float c, inv_tau, inv_tau_lo, tau, unit;
   const int32_t* tokens;
   const float *lse_in, *entropy, *d_logprob, *d_entropy;
   const int32_t* teacher_tokens;
@@ -545,50 +747,51 @@ __device__ __forceinline__ void store_vec(T* dst, const float (&y)[Elem<T>::EV],
   }
 }
 
-// log p of x, natural, from an lse handed over in fp32.  For fp32 logits 1 / tau is taken as two fp32 terms: its
-// rounding alone would shift every log p by 2^-24 of s, which the fp32 gradient shows.
-template <class T>
-__device__ __forceinline__ float logp_from_lse(float x, const GradArgs& A, float lse) {
-  if (sizeof(T) == 4) return fmaf(x, A.inv_tau, fmaf(x == -INFINITY ? 0.f : x, A.inv_tau_lo, -lse));
-  return fmaf(x, A.inv_tau, -lse);
-}
-
 // A thread keeps its R vectors of the row in registers, so the gradient in the same call as the loss reads the logits
 // once: all loads, the statistics, their join over the group, all stores.  With the statistics handed over (kLogprobsGrad,
 // kDistillGrad) there is no join and `ranks` is any number of independent pieces of the row.
+//
+// dx_j = p_j (ca + cb log2 p_j), then the entries that have a term of their own.  16-bit logits take log2 p as one fused
+// x c - kappa, two elements an instruction.  fp32 logits take (x / tau - lse) first and 1 / tau as two fp32 terms: the
+// rounding of either would shift every log p by 2^-24 of s, which an fp32 gradient shows.
 template <class T, int NT, int R, int MODE>
 __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R > 4 ? 3 : 4) rows_gradient_kernel(const GradArgs A) {
   using G = Group<NT>;
   constexpr int EV = Elem<T>::EV;
-  constexpr bool kTeacher = MODE != kLogprobsGrad, kStep = MODE == kDistillStep;
+  constexpr bool kTeacher = MODE != kLogprobsGrad, kStep = MODE == kDistillStep, kNarrow = sizeof(T) == 2;
   __shared__ Stat wstat[G::kRowsPerBlock][G::kWarps];
   __shared__ Stat cstat[kMaxCluster];
-  __shared__ float sh_q[kTeacher ? G::kRowsPerBlock : 1][kMaxTeacher], sh_x[kTeacher ? G::kRowsPerBlock : 1][kMaxTeacher];
-  __shared__ int sh_a[kTeacher ? G::kRowsPerBlock : 1][kMaxTeacher], sh_flags[G::kRowsPerBlock];
-  const int t = G::tid(), lane = threadIdx.x & 31, w = NT == 32 ? 0 : (int)(threadIdx.x >> 5), slot = G::slot();
+  __shared__ Teacher teacher_sh[kTeacher ? G::kRowsPerBlock : 1];
+  const int t = G::tid(), lane = threadIdx.x & 31, w = NT == 32 ? 0 : (int)(threadIdx.x >> 5);
   const int ranks = NT == 32 ? 1 : A.ranks;
   const int rank = NT == 32 ? 0 : (int)(blockIdx.x % (unsigned)ranks);
-  const long long row = NT == 32 ? (long long)blockIdx.x * G::kRowsPerBlock + slot : (long long)(blockIdx.x / (unsigned)ranks);
+  const long long row = NT == 32 ? (long long)blockIdx.x * G::kRowsPerBlock + G::slot() : (long long)(blockIdx.x / (unsigned)ranks);
   if (NT == 32 && row >= A.T) return;
+  Teacher& te = teacher_sh[kTeacher ? G::slot() : 0];
   const T* xr = reinterpret_cast<const T*>(A.x) + row * A.ld;
   T* dr = reinterpret_cast<T*>(A.dx) + row * A.ld_d;
   const Slice<T> sl(xr, A.V, rank, ranks);
   const bool aligned = ((((uintptr_t)xr) ^ ((uintptr_t)dr)) & 15u) == 0;   // vectors of x are vectors of dx
   const int edge = sl.edge(t);
   const float c = A.c;
+
+  // the row's vectors are on their way before anything else of it is looked at; a row that asks for nothing is read for
+  // nothing in the step, and not at all where there is a token to tell
   int token = -1;
-  bool live = true;
+  bool zero = false;
+  float lse = 0.f;
   if (!kTeacher) {
     token = A.tokens[row];
-    live = token >= 0;
+    zero = token < 0;
   }
-  const float lse = kStep ? 0.f : A.lse_in[row];
-  if (!kStep && lse <= kEmptyLse) live = false;       // nothing left by the masks
-
-  // the row's vectors are on their way before the teacher's entries are looked at; a row without any is read for nothing
+  if (!kStep) {
+    lse = A.lse_in[row];
+    zero = zero || lse <= kEmptyLse;       // nothing left by the masks
+  }
   uint4 v[R];
   float xe = -INFINITY;
-  if (kStep) {
+  const int per_turn = R * NT;
+  if (kStep || !zero) {
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int at = sl.v0 + t + i * NT;
@@ -597,38 +800,20 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
     }
     if (edge >= 0) xe = Elem<T>::to_float(xr[edge]);
   }
-  float xs[kMaxTeacher / 32];
-  Teacher te;
-  if (kTeacher && w == 0) {
-    te.read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, A.K, A.V, A.inv_tau);
-    if (lane == 0) sh_flags[slot] = (te.any ? 1 : 0) | (te.bad ? 2 : 0);
-    live = live && te.any;
-#pragma unroll
-    for (int e = 0; e < kMaxTeacher / 32; ++e) {
-      // the first rank needs all of them for the loss, every rank its own slice's for the gradient
-      const bool need = te.a[e] >= 0 && live && ((kStep && rank == 0) || (te.a[e] >= sl.e0 && te.a[e] < sl.e1));
-      xs[e] = need ? Elem<T>::to_float(xr[te.a[e]]) : 0.f;
-      sh_a[slot][lane + 32 * e] = te.a[e];
-      sh_q[slot][lane + 32 * e] = te.q[e];
-      sh_x[slot][lane + 32 * e] = xs[e];
-    }
-  }
+  if (kTeacher && w == 0)
+    // the first rank needs all of the student's logits for the loss, every rank its own slice's for the gradient
+    te.read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, xr, A.K, A.V, A.inv_tau,
+            [&](int j) { return (kStep && rank == 0) || (j >= sl.e0 && j < sl.e1); });
 
   float ref = 0.f, log2s = 0.f;
-  bool empty = false;
   if (kStep) {
     cg::cluster_group cluster = cg::this_cluster();
     if (ranks > 1) cluster.barrier_arrive();          // every block of the cluster runs before its memory is written
-    Stat a{max_nan(max_nan(Elem<T>::largest(v), xe), kUnset), 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      float x[EV];
-      Elem<T>::unpack(v[i], x);
-      add_elements<EV, false>(a, x, c);
-    }
-    const float e1[1] = {xe};
-    add_elements<1, false>(a, e1, c);
-    a = warp_join(a, c);
+    Running<T, false> run(c);
+    run.set_ref(max_nan(max_nan(Elem<T>::largest(v), xe), kUnset));
+    run.add(v);
+    run.one(xe);
+    Stat a = warp_join(run.get(), c);
     if (NT > 32) {
       if (lane == 0) wstat[0][w] = a;
       __syncthreads();
@@ -643,75 +828,100 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
       a = cstat[0];
       for (int i = 1; i < ranks; ++i) a = join(a, cstat[i], c);
     }
-    const RowSum r(a, A.inv_tau);
+    const RowSum r(a, c, A.unit, A.inv_tau);
     ref = r.ref;
     log2s = r.log2s;
-    empty = r.empty;
+    zero = r.empty;
     if (rank == 0 && w == 0) {
-      const float kl = !live ? 0.f : empty && !te.bad ? INFINITY : te.divergence(xs, r, c);
+      const float kl = te.divergence(r, A.K);
       if (lane == 0) {
-        A.loss[row] = live ? A.tau * A.tau * kl : 0.f;
-        if (A.lse_out) A.lse_out[row] = live ? r.lse : 0.f;
+        A.loss[row] = A.tau * A.tau * kl;
+        A.lse_out[row] = te.any ? r.lse : 0.f;
       }
     }
   }
 
-  // dx_j = p_j (ca + cb log p_j), then the entries that have a term of their own
   float ca, cb = 0.f, cy = 0.f;
   bool bad = false;
   if (kTeacher) {
     G::sync();
-    live = live && (sh_flags[slot] & 1);
-    bad = (sh_flags[slot] & 2) != 0;
-    ca = bad ? __int_as_float(0x7fc00000) : A.d_loss[row] * A.tau;
+    zero = zero || !te.any;
+    bad = te.bad != 0;
+    ca = A.d_loss[row] * A.tau;
   } else {
     const float g = A.d_logprob ? A.d_logprob[row] : 0.f, h = A.d_entropy ? A.d_entropy[row] : 0.f;
     cb = -h * A.inv_tau;
     ca = -(g + (A.d_entropy ? h * A.entropy[row] : 0.f)) * A.inv_tau;
     cy = g * A.inv_tau;
-    if (token >= A.V) ca = __int_as_float(0x7fc00000);
+    bad = token >= A.V;
   }
-  const bool zero = !live || empty;
+  if (bad) ca = __int_as_float(0x7fc00000);
+  // log2 p = x c - kappa, for 16-bit logits whose reference is no mask
+  const float kappa = kStep ? ref * c + log2s : lse * kLog2e;
+  const bool packed = kNarrow && (!kStep || near_ref(ref));
+  const f32x2 c2 = pair_of(c, c), k2 = pair_of(-kappa, -kappa), ca2 = pair_of(ca, ca), cb2 = pair_of(cb * kLn2, cb * kLn2);
+  // with a term in log p, -inf is raised to a bound where p is 0 and log p finite; without such a bound: one by one
+  const uint32_t lo = MODE == kLogprobsGrad && kNarrow ? Elem<T>::bound((kappa - 200.f) / c) : 0u;
+  auto prob = [&](float x, float& lp) -> float {       // p, and log p (natural)
+    if (kStep) {
+      lp = (scaled(x, ref, c) - log2s) * A.unit;
+      return ex2(scaled(x, ref, c) - log2s);
+    }
+    lp = kNarrow ? fmaf(x, c, -kappa) * kLn2 : fmaf(x, A.inv_tau, fmaf(x == -INFINITY ? 0.f : x, A.inv_tau_lo, -lse));
+    return ex2(lp * kLog2e);
+  };
   auto grad = [&](float x) -> float {
-    if (kStep) return ca * ex2(fmaf(x - ref, c, -log2s));
-    float lp = logp_from_lse<T>(x, A, lse);
-    if (MODE == kDistillGrad) return ca * ex2(lp * kLog2e);
-    lp = max_nan(lp, -1e4f);
-    return ex2(lp * kLog2e) * fmaf(cb, lp, ca);
+    float lp;
+    const float p = prob(x, lp);
+    return MODE == kLogprobsGrad ? p * fmaf(cb, max_nan(lp, -1e4f), ca) : p * ca;
   };
   auto put = [&](const uint4& xv, int at) {
+    const int j0 = sl.head + at * EV;
+    if (zero) {
+      const float y[EV] = {};
+      store_vec<T>(dr + j0, y, aligned);
+      return;
+    }
+    if constexpr (kNarrow) {
+      if (packed && (MODE != kLogprobsGrad || lo) && aligned) {
+        f32x2 p[EV / 2];
+        Elem<T>::pairs(MODE == kLogprobsGrad ? at_least<T>(xv, lo) : xv, p);
+#pragma unroll
+        for (int i = 0; i < EV / 2; ++i) {
+          const f32x2 lp = fma2(p[i], c2, k2), e = ex2x2(lp);
+          p[i] = mul2(e, MODE == kLogprobsGrad ? fma2(cb2, lp, ca2) : ca2);
+        }
+        if (MODE == kLogprobsGrad && (unsigned)(token - j0) < (unsigned)EV) {
+#pragma unroll
+          for (int i = 0; i < EV / 2; ++i)
+            p[i] = add2(p[i], pair_of(j0 + 2 * i == token ? cy : 0.f, j0 + 2 * i + 1 == token ? cy : 0.f));
+        }
+        *reinterpret_cast<uint4*>(dr + j0) = Elem<T>::pack_pairs(p);
+        return;
+      }
+    }
     float x[EV], y[EV];
     Elem<T>::unpack(xv, x);
-    const int j0 = sl.head + at * EV;
 #pragma unroll
-    for (int i = 0; i < EV; ++i) {
-      y[i] = zero ? 0.f : grad(x[i]);
-    }
-    if (!kTeacher && !zero && (unsigned)(token - j0) < (unsigned)EV) {
+    for (int i = 0; i < EV; ++i) y[i] = grad(x[i]);
+    if (MODE == kLogprobsGrad && (unsigned)(token - j0) < (unsigned)EV) {
 #pragma unroll
       for (int i = 0; i < EV; ++i)
         if (j0 + i == token) y[i] += cy;
     }
     store_vec<T>(dr + j0, y, aligned);
   };
-  if (kStep) {
+  for (int b = sl.v0 + t;;) {
 #pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int at = sl.v0 + t + i * NT;
-      if (at < sl.v1) put(v[i], at);
-    }
-  } else {
-    for (int b = sl.v0 + t; b < sl.v1; b += R * NT) {
-      if (!zero) {
-#pragma unroll
-        for (int i = 0; i < R; ++i)
-          if (b + i * NT < sl.v1) v[i] = load16(sl.vec(b + i * NT));
-      }
+    for (int i = 0; i < R; ++i)
+      if (b + i * NT < sl.v1) put(v[i], b + i * NT);
+    b += per_turn;
+    if (kStep || b >= sl.v1) break;        // the step's plan makes a slice fit R vectors a thread
+    if (!zero) {
 #pragma unroll
       for (int i = 0; i < R; ++i)
-        if (b + i * NT < sl.v1) put(v[i], b + i * NT);
+        if (b + i * NT < sl.v1) v[i] = load16(sl.vec(b + i * NT));
     }
-    if (edge >= 0 && !zero) xe = Elem<T>::to_float(xr[edge]);
   }
   if (edge >= 0) {
     float y = zero ? 0.f : grad(xe);
@@ -724,26 +934,213 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
     G::sync();
     if (zero || bad) return;
     for (int i = t; i < A.K; i += NT) {
-      const int j = sh_a[slot][i];
+      const int j = te.a[i];
       if (j < sl.e0 || j >= sl.e1) continue;
       float q = 0.f;
       for (int o = 0; o < A.K; ++o)
-        if (sh_a[slot][o] == j) q += sh_q[slot][o];
-      const float x = sh_x[slot][i];
-      const float p = kStep ? ex2(fmaf(x - ref, c, -log2s)) : ex2(logp_from_lse<T>(x, A, lse) * kLog2e);
-      dr[j] = Elem<T>::from_float(ca * (p - q));
+        if (te.a[o] == j) q += te.q[o];
+      float lp;
+      dr[j] = Elem<T>::from_float(ca * (prob(te.x[i], lp) - q));
     }
   }
+}
+
+// The teacher's gradients for rows longer than a warp's.  A block runs over items (a row in the step, each block of a
+// cluster its slice; a piece of a row with the statistics handed over): eight warps hold the item's vectors in registers
+// while the next two items are on their way through shared memory, so that memory never waits for the barriers between
+// load and store.  A ninth warp prepares the next item's teacher entries meanwhile and, when the vectors' gradient is stored,
+// writes the teacher's columns over it.
+constexpr int kDistillThreads = kBlock + 32;
+template <int ID>
+__device__ __forceinline__ void bar_sync() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(kDistillThreads) : "memory"); }
+template <int ID>
+__device__ __forceinline__ void bar_arrive() { asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kDistillThreads) : "memory"); }
+
+template <class T, int R, bool STEP>
+__global__ void __launch_bounds__(kDistillThreads, R > 8 ? 1 : R > 4 ? 3 : 4) rows_distill_kernel(const GradArgs A) {
+  constexpr int EV = Elem<T>::EV, NT = kBlock, kWarps = NT / 32;
+  constexpr bool kNarrow = sizeof(T) == 2;
+  extern __shared__ uint4 buffer[];                // [2][R][NT], a thread's own column
+  __shared__ Stat wstat[2][kWarps];
+  __shared__ Stat cstat[2][kMaxCluster];
+  __shared__ Teacher teacher[2];
+  const int t = threadIdx.x, lane = t & 31, w = t >> 5, ranks = A.ranks;
+  const int my_rank = (int)(blockIdx.x % (unsigned)ranks);
+  const long long items = STEP ? A.T : A.T * ranks;
+  const long long q0 = STEP ? blockIdx.x / (unsigned)ranks : blockIdx.x, step = STEP ? gridDim.x / (unsigned)ranks : gridDim.x;
+  const float c = A.c;
+  auto row_of = [&](long long q) { return STEP ? q : q / ranks; };
+  auto slice_of = [&](long long q) {
+    return Slice<T>(reinterpret_cast<const T*>(A.x) + row_of(q) * A.ld, A.V, STEP ? my_rank : (int)(q % ranks), ranks);
+  };
+  // the statistics of an item's row, the same in every thread of the cluster
+  auto row_sum = [&](int b) {
+    Stat a = wstat[b][0];
+#pragma unroll
+    for (int i = 1; i < kWarps; ++i) a = join(a, wstat[b][i], c);
+    if (ranks > 1) {
+      cg::cluster_group cluster = cg::this_cluster();
+      if (t < ranks) *cluster.map_shared_rank(&cstat[b][my_rank], t) = a;
+      cluster.sync();
+      a = cstat[b][0];
+      for (int i = 1; i < ranks; ++i) a = join(a, cstat[b][i], c);
+    }
+    return RowSum(a, c, A.unit, A.inv_tau);
+  };
+  // p of a logit, from the row's statistics or from an lse handed over (see rows_gradient_kernel for the two forms)
+  auto prob = [&](float x, float ref, float log2s, float lse) -> float {
+    if (STEP) return ex2(scaled(x, ref, c) - log2s);
+    if (kNarrow) return ex2(fmaf(x, c, -lse * kLog2e));
+    return ex2(fmaf(x, A.inv_tau, fmaf(x == -INFINITY ? 0.f : x, A.inv_tau_lo, -lse)) * kLog2e);
+  };
+  // every block of the cluster runs before its memory is written
+  if (STEP && ranks > 1) cg::this_cluster().sync();
+
+  if (w == kWarps) {
+    auto prepare = [&](long long q, int b) {
+      if (q >= items) return;
+      const long long row = row_of(q);
+      const Slice<T> sl = slice_of(q);
+      teacher[b].read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, sl.row, A.K, A.V, A.inv_tau,
+                      [&](int j) { return (STEP && my_rank == 0) || (j >= sl.e0 && j < sl.e1); });
+      teacher[b].gather_mass(A.K);
+    };
+    prepare(q0, 0);
+    int b = 0;
+    for (long long q = q0; q < items; q += step, b ^= 1) {
+      const long long row = row_of(q);
+      const Teacher& te = teacher[b];
+      const float lse = STEP ? 0.f : A.lse_in[row], ca = A.d_loss[row] * A.tau;
+      bar_sync<1>();
+      float ref = 0.f, log2s = 0.f;
+      bool zero = !te.any || te.bad || (!STEP && lse <= kEmptyLse);
+      if (STEP) {
+        const RowSum r = row_sum(b);
+        ref = r.ref;
+        log2s = r.log2s;
+        zero = zero || r.empty;
+        if (my_rank == 0) {
+          const float kl = te.divergence(r, A.K);
+          if (lane == 0) {
+            A.loss[row] = A.tau * A.tau * kl;
+            A.lse_out[row] = te.any ? r.lse : 0.f;
+          }
+        }
+      }
+      prepare(q + step, b ^ 1);
+      bar_sync<2>();
+      if (!zero) {
+        const Slice<T> sl = slice_of(q);
+        T* dr = reinterpret_cast<T*>(A.dx) + row * A.ld_d;
+        for (int i = lane; i < A.K; i += 32) {
+          const int j = te.a[i];
+          if (j >= sl.e0 && j < sl.e1) dr[j] = Elem<T>::from_float(ca * (prob(te.x[i], ref, log2s, lse) - te.mass[i]));
+        }
+      }
+      __syncwarp();
+    }
+    return;
+  }
+
+  float next_edge = -INFINITY, next_lse = 0.f, next_g = 0.f;
+  auto fetch = [&](long long q, int b) {           // the item's vectors into buffer b
+    if (q < items) {
+      const Slice<T> sl = slice_of(q);
+#pragma unroll
+      for (int i = 0; i < R; ++i) {
+        const int at = sl.v0 + t + i * NT;
+        if (at < sl.v1) copy16(&buffer[(b * R + i) * NT + t], sl.vec(at));
+      }
+    }
+    copy_commit();
+  };
+  auto peek = [&](long long q) {                   // what it needs beside them
+    if (q >= items) return;
+    const Slice<T> sl = slice_of(q);
+    const int j = sl.edge(t);
+    next_edge = j >= 0 ? Elem<T>::to_float(sl.row[j]) : -INFINITY;
+    next_g = A.d_loss[row_of(q)];
+    if (!STEP) next_lse = A.lse_in[row_of(q)];
+  };
+  fetch(q0, 0);
+  fetch(q0 + step, 1);
+  peek(q0);
+  int b = 0;
+  for (long long q = q0; q < items; q += step, b ^= 1) {
+    const long long row = row_of(q);
+    const Slice<T> sl = slice_of(q);
+    T* dr = reinterpret_cast<T*>(A.dx) + row * A.ld_d;
+    const bool aligned = ((((uintptr_t)sl.row) ^ ((uintptr_t)dr)) & 15u) == 0;   // vectors of x are vectors of dx
+    const float xe = next_edge, lse = next_lse;
+    float ca = next_g * A.tau;
+    copy_wait<1>();
+    uint4 v[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      if (sl.v0 + t + i * NT < sl.v1) v[i] = buffer[(b * R + i) * NT + t];
+      else v[i] = make_uint4(Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf);
+    }
+    fetch(q + 2 * step, b);
+    peek(q + step);
+    if (STEP) {
+      Running<T, false> run(c);
+      run.set_ref(max_nan(max_nan(Elem<T>::largest(v), xe), kUnset));
+      run.add(v);
+      run.one(xe);
+      const Stat a = warp_join(run.get(), c);
+      if (lane == 0) wstat[b][w] = a;
+    }
+    bar_sync<1>();
+    bool zero = !teacher[b].any || (!STEP && lse <= kEmptyLse);
+    if (teacher[b].bad) ca = __int_as_float(0x7fc00000);
+    float ref = 0.f, log2s = 0.f;
+    if (STEP) {
+      const RowSum r = row_sum(b);
+      ref = r.ref;
+      log2s = r.log2s;
+      zero = zero || r.empty;
+    }
+    const float kappa = STEP ? ref * c + log2s : lse * kLog2e;
+    const f32x2 c2 = pair_of(c, c), k2 = pair_of(-kappa, -kappa), ca2 = pair_of(ca, ca);
+    const bool packed = kNarrow && aligned && !zero && (!STEP || near_ref(ref));
+#pragma unroll
+    for (int i = 0; i < R; ++i) {
+      const int at = sl.v0 + t + i * NT;
+      if (at >= sl.v1) break;
+      T* dst = dr + sl.head + at * EV;
+      if constexpr (kNarrow) {
+        if (packed) {
+          f32x2 p[EV / 2];
+          Elem<T>::pairs(v[i], p);
+#pragma unroll
+          for (int e = 0; e < EV / 2; ++e) p[e] = mul2(ex2x2(fma2(p[e], c2, k2)), ca2);
+          *reinterpret_cast<uint4*>(dst) = Elem<T>::pack_pairs(p);
+          continue;
+        }
+      }
+      float x[EV];
+      Elem<T>::unpack(v[i], x);
+#pragma unroll
+      for (int e = 0; e < EV; ++e) x[e] = zero ? 0.f : ca * prob(x[e], ref, log2s, lse);
+      store_vec<T>(dst, x, aligned);
+    }
+    const int edge = sl.edge(t);
+    if (edge >= 0) dr[edge] = Elem<T>::from_float(zero ? 0.f : ca * prob(xe, ref, log2s, lse));
+    __threadfence_block();
+    bar_arrive<2>();
+  }
+  copy_wait<0>();
 }
 
 // ---- host -------------------------------------------------------------------------------------------------------------
 constexpr int kSMs = 148;
 
 template <class Args>
-cudaError_t launch(void (*kernel)(const Args), const Args& A, long long blocks, int threads, int cluster, cudaStream_t st) {
+cudaError_t launch(void (*kernel)(const Args), const Args& A, long long blocks, int threads, size_t smem, int cluster, cudaStream_t st) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)blocks);
   cfg.blockDim = dim3((unsigned)threads);
+  cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
@@ -754,38 +1151,102 @@ cudaError_t launch(void (*kernel)(const Args), const Args& A, long long blocks, 
   return cudaLaunchKernelEx(&cfg, kernel, A);
 }
 
-// Blocks per row of a forward pass: rows alone fill the GPU (four blocks an SM) or are split, down to two vectors a
-// thread, over up to eight blocks.
+// What a kernel with dynamic shared memory needs to know of the device, found once per device: its limit is raised, and the
+// blocks of it that run at the same time in clusters of 1, 2, 4 and 8.
+struct Resident {
+  std::atomic<int> blocks[64][4] = {};
+  template <class Args>
+  cudaError_t get(void (*kernel)(const Args), int threads, size_t smem, int cluster, int& out) {
+    int dev = 0;
+    cudaError_t rc = cudaGetDevice(&dev);
+    if (rc != cudaSuccess) return rc;
+    std::atomic<int>& slot = blocks[dev & 63][cluster == 8 ? 3 : cluster / 2];
+    out = dev < 64 ? slot.load(std::memory_order_acquire) : 0;
+    if (out > 0) return cudaSuccess;
+    rc = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if (rc != cudaSuccess) return rc;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(cluster * kSMs));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = smem;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)cluster;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    int n = 0;
+    rc = cudaOccupancyMaxActiveClusters(&n, kernel, &cfg);
+    if (rc != cudaSuccess) return rc;
+    out = (n < 1 ? 1 : n) * cluster;
+    slot.store(out, std::memory_order_release);
+    return cudaSuccess;
+  }
+};
+
+// Rows that one warp takes: short ones, and longer ones when there are enough of them to fill the GPU.
+template <class T>
+bool warp_rows(long long T_, long long V) {
+  const long long nvec = V / Elem<T>::EV;
+  return V <= kWarpRow || (nvec <= kWarpVectors && T_ >= 16 * kSMs);
+}
+
+// Blocks per row of a forward pass: rows alone fill the GPU or are split, down to two vectors a thread, over up to eight
+// blocks.
 int forward_ranks(long long T, long long nvec) {
   int ranks = 1;
-  while (ranks < kMaxCluster && T * ranks < 4 * kSMs && nvec > (long long)ranks * 2 * kBlock) ranks *= 2;
+  while (ranks < kMaxCluster && T * ranks < kForwardBlocks * kSMs && nvec > (long long)ranks * 2 * kBlock) ranks *= 2;
   return ranks;
 }
 
 template <class T, bool DISTILL>
 cudaError_t forward(ForwardArgs& A, cudaStream_t st) {
-  if (A.V <= kWarpRow) {
+  if (warp_rows<T>(A.T, A.V)) {
     A.ranks = 1;
-    return launch(rows_forward_kernel<T, 32, DISTILL>, A, (A.T + 3) / 4, kWarpBlock, 1, st);
+    return launch(rows_forward_kernel<T, 32, DISTILL>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
   }
-  A.ranks = forward_ranks(A.T, A.V / Elem<T>::EV);
-  return launch(rows_forward_kernel<T, kBlock, DISTILL>, A, A.T * A.ranks, kBlock, A.ranks, st);
+  const long long nvec = A.V / Elem<T>::EV;
+  if (nvec <= kHalfVectors && A.T >= 2 * kForwardBlocks * kSMs) {
+    A.ranks = 1;
+    return launch(rows_forward_kernel<T, kHalfBlock, DISTILL>, A, A.T, kHalfBlock, (size_t)kRing * kBatch * kHalfBlock * 16, 1, st);
+  }
+  A.ranks = forward_ranks(A.T, nvec);
+  return launch(rows_forward_kernel<T, kBlock, DISTILL>, A, A.T * A.ranks, kBlock, (size_t)kRing * kBatch * kBlock * 16, A.ranks, st);
+}
+
+template <class T, int R, bool STEP>
+cudaError_t distill_blocks(GradArgs& A, cudaStream_t st) {
+  constexpr size_t smem = (size_t)2 * R * kBlock * 16;
+  static Resident resident;
+  int blocks = 0;
+  const int cluster = STEP ? A.ranks : 1;
+  const cudaError_t rc = resident.get(rows_distill_kernel<T, R, STEP>, kDistillThreads, smem, cluster, blocks);
+  if (rc != cudaSuccess) return rc;
+  const long long want = A.T * A.ranks;
+  return launch(rows_distill_kernel<T, R, STEP>, A, want < blocks ? want : blocks, kDistillThreads, smem, cluster, st);
 }
 
 template <class T, int MODE>
 cudaError_t gradient(GradArgs& A, cudaStream_t st) {
   const long long nvec = A.V / Elem<T>::EV;
-  if (A.V <= kWarpRow) {
+  if (warp_rows<T>(A.T, A.V)) {
     A.ranks = 1;
     constexpr int R = kWarpRow / Elem<T>::EV / 32;
-    return launch(rows_gradient_kernel<T, 32, R, MODE>, A, (A.T + 3) / 4, kWarpBlock, 1, st);
+    if (A.V <= kWarpRow || MODE == kLogprobsGrad) return launch(rows_gradient_kernel<T, 32, R, MODE>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
+    if constexpr (MODE != kLogprobsGrad)
+      return launch(rows_gradient_kernel<T, 32, kWarpVectors / 32, MODE>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
   }
-  if constexpr (MODE != kDistillStep) {
+  if constexpr (MODE == kLogprobsGrad) {
     // pieces of 4 vectors a thread, at least one; larger where the grid would pass 2^31 blocks
     long long ranks = (nvec + 4 * kBlock - 1) / (4 * kBlock);
     while (A.T * ranks > 0x7fffffffll) ranks = (ranks + 1) / 2;
     A.ranks = ranks < 1 ? 1 : (int)ranks;
-    return launch(rows_gradient_kernel<T, kBlock, 4, MODE>, A, A.T * A.ranks, kBlock, 1, st);
+    return launch(rows_gradient_kernel<T, kBlock, 4, MODE>, A, A.T * A.ranks, kBlock, 0, 1, st);
+  } else if constexpr (MODE == kDistillGrad) {
+    A.ranks = (int)((nvec + 8 * kBlock - 1) / (8 * kBlock));
+    while (A.T * A.ranks < 3 * kSMs && nvec > (long long)A.ranks * 2 * kBlock) A.ranks *= 2;
+    const long long per = (nvec + A.ranks - 1) / A.ranks;
+    return per <= 4 * kBlock ? distill_blocks<T, 4, false>(A, st) : distill_blocks<T, 8, false>(A, st);
   } else {
     int ranks = 1;
     while (ranks < kMaxCluster &&
@@ -793,9 +1254,9 @@ cudaError_t gradient(GradArgs& A, cudaStream_t st) {
       ranks *= 2;
     A.ranks = ranks;
     const long long per = (nvec + ranks - 1) / ranks;
-    if (per <= 4 * kBlock) return launch(rows_gradient_kernel<T, kBlock, 4, MODE>, A, A.T * ranks, kBlock, ranks, st);
-    if (per <= 8 * kBlock) return launch(rows_gradient_kernel<T, kBlock, 8, MODE>, A, A.T * ranks, kBlock, ranks, st);
-    return launch(rows_gradient_kernel<T, kBlock, 16, MODE>, A, A.T * ranks, kBlock, ranks, st);
+    if (per <= 4 * kBlock) return distill_blocks<T, 4, true>(A, st);
+    if (per <= 8 * kBlock) return distill_blocks<T, 8, true>(A, st);
+    return distill_blocks<T, 16, true>(A, st);
   }
 }
 
@@ -861,12 +1322,14 @@ void set_temperature(ForwardArgs& A, float tau) {
   A.tau = tau;
   A.inv_tau = (float)(1.0 / (double)tau);
   A.c = (float)(1.4426950408889634 / (double)tau);
+  A.unit = (float)(1.0 / ((double)tau * (double)A.c));
 }
 void set_temperature(GradArgs& A, float tau) {
   A.tau = tau;
   A.inv_tau = (float)(1.0 / (double)tau);
   A.inv_tau_lo = (float)(1.0 / (double)tau - (double)A.inv_tau);
   A.c = (float)(1.4426950408889634 / (double)tau);
+  A.unit = (float)(1.0 / ((double)tau * (double)A.c));
 }
 
 }  // namespace
