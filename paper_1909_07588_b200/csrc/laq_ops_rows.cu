@@ -63,13 +63,13 @@ template <class T>
 struct Slice {
   const T* row;
   int head, nvec, v0, v1, e0, e1, tail0, V;
-  __device__ __forceinline__ Slice(const T* r, int V_, int rank, int ranks) : row(r), V(V_) {
+  // per: vectors of a rank, at least ceil(V / EV / ranks)
+  __device__ __forceinline__ Slice(const T* r, int V_, int rank, int ranks, int per) : row(r), V(V_) {
     constexpr int EV = Elem<T>::EV;
-    const int mis = (int)(((uintptr_t)r & 15u) / sizeof(T));
-    head = mis ? min(EV - mis, V) : 0;
-    nvec = (V - head) / EV;
+    const unsigned mis = (unsigned)((uintptr_t)r & 15u) / (unsigned)sizeof(T);
+    head = min((int)((EV - mis) % EV), V);
+    nvec = (int)((unsigned)(V - head) / EV);
     tail0 = head + nvec * EV;
-    const int per = (nvec + ranks - 1) / ranks;
     v0 = min(rank * per, nvec);
     v1 = min(v0 + per, nvec);
     e0 = rank == 0 ? 0 : head + v0 * EV;
@@ -188,15 +188,17 @@ __device__ __forceinline__ Stat join(Stat a, Stat b, float c) {
   return a;
 }
 
+// The joint statistics of a warp's first LANES lanes (a power of two; the others mirror them), in every lane.
+template <int LANES, bool ENTROPY>
 __device__ __forceinline__ Stat warp_join(Stat a, float c) {
   float r = a.ref;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) r = max_nan(r, __shfl_xor_sync(0xffffffffu, r, o));
+  for (int o = LANES / 2; o > 0; o >>= 1) r = max_nan(r, __shfl_xor_sync(0xffffffffu, r, o));
   move_ref(a, r, c);
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
+  for (int o = LANES / 2; o > 0; o >>= 1) {
     a.s += __shfl_xor_sync(0xffffffffu, a.s, o);
-    a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
+    if (ENTROPY) a.u += __shfl_xor_sync(0xffffffffu, a.u, o);
   }
   return a;
 }
@@ -459,39 +461,53 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, const uint4*
 }
 
 // ---- the teacher's side of one row ------------------------------------------------------------------------------------
-// One warp reads the entries and leaves them in shared memory: q and log q (natural), the column or -1 where there is no
-// entry, the student's logit there.
-struct Teacher {
-  alignas(16) float q[kMaxTeacher];
-  alignas(16) int a[kMaxTeacher];
-  float logq[kMaxTeacher], x[kMaxTeacher], mass[kMaxTeacher];
-  int any, bad;        // a live entry; a column outside the vocabulary
+// One warp works on a row: lane holds the entries lane + 32 e.  The loads are steps of their own, so that a warp that goes
+// over rows can have the next row's under way.
+constexpr int kPerLane = kMaxTeacher / 32;
 
-  // `need(column)`: whether this warp's block uses the student's logit of the column
-  template <class T, class F>
-  __device__ __forceinline__ void read(const int32_t* idx, const float* val, const T* row, int K, int V, float inv_tau, F need) {
-    constexpr int E = kMaxTeacher / 32;
+struct Entries {                 // column (or -1 where there is no entry) and logit
+  int col[kPerLane];
+  float t[kPerLane];
+  __device__ __forceinline__ void load(const int32_t* idx, const float* val, int K) {
     const int lane = threadIdx.x & 31;
-    int col[E];
-    float t[E];
-    float mx = -INFINITY;
-    bool have = false, out = false;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < kPerLane; ++e) {
       const int i = lane + 32 * e;
       col[e] = i < K ? idx[i] : -1;
       t[e] = i < K ? val[i] : -INFINITY;
     }
+  }
+  // the student's logits at the columns, where need(column)
+  template <class T, class F>
+  __device__ __forceinline__ void student(const T* row, int V, float (&x)[kPerLane], F need) const {
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const int i = lane + 32 * e;
-      if (col[e] >= V) {
-        out = true;
-        col[e] = -1;
-      }
-      x[i] = col[e] >= 0 && need(col[e]) ? Elem<T>::to_float(row[col[e]]) : 0.f;
-      if (col[e] < 0) t[e] = -INFINITY;
-      have |= col[e] >= 0;
+    for (int e = 0; e < kPerLane; ++e)
+      x[e] = col[e] >= 0 && col[e] < V && need(col[e]) ? Elem<T>::to_float(row[col[e]]) : 0.f;
+  }
+};
+
+// A row's entries in shared memory: q, log q (natural) and the student's logit of all of them, for the loss, and a list of
+// those whose column lies in the block's slice, for the gradient.
+struct Teacher {
+  float q[kMaxTeacher], logq[kMaxTeacher], x[kMaxTeacher];
+  alignas(16) int col[kMaxTeacher];
+  alignas(16) float colq[kMaxTeacher];
+  float colx[kMaxTeacher], mass[kMaxTeacher];
+  int n;               // of the list
+  int any, bad;        // a live entry; a column outside the vocabulary
+
+  // e0, e1: the slice's columns
+  __device__ __forceinline__ void set(const Entries& in, const float (&xs)[kPerLane], int V, float inv_tau, int e0, int e1) {
+    const int lane = threadIdx.x & 31;
+    float t[kPerLane];
+    float mx = -INFINITY;
+    bool have = false, out = false;
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e) {
+      out |= in.col[e] >= V;
+      const bool there = in.col[e] >= 0 && in.col[e] < V;
+      have |= there;
+      t[e] = there ? in.t[e] : -INFINITY;
       mx = max_nan(mx, t[e]);
     }
 #pragma unroll
@@ -499,47 +515,65 @@ struct Teacher {
     out = __any_sync(0xffffffffu, out);
     // a teacher whose every entry is masked asks for nothing
     have = (__any_sync(0xffffffffu, have) && mx != -INFINITY) || out;
-    float sum = 0.f;
+    float sum = 0.f, e_[kPerLane];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < kPerLane; ++e) {
       t[e] = t[e] == -INFINITY ? -INFINITY : (t[e] - mx) * inv_tau;
-      sum += expf(t[e]);
+      e_[e] = ex2(t[e] * kLog2e);
+      sum += e_[e];
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
     const float ls = logf(sum), inv = 1.f / sum;
+    int listed = 0;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
+    for (int e = 0; e < kPerLane; ++e) {
       const int i = lane + 32 * e;
-      q[i] = col[e] >= 0 && have ? expf(t[e]) * inv : 0.f;
+      const bool there = in.col[e] >= 0 && in.col[e] < V, mine = there && in.col[e] >= e0 && in.col[e] < e1;
+      const float p = there && have ? e_[e] * inv : 0.f;
+      q[i] = p;
       logq[i] = t[e] - ls;
-      a[i] = col[e];
+      x[i] = xs[e];
+      const uint32_t who = __ballot_sync(0xffffffffu, mine);
+      if (mine) {
+        const int at = listed + __popc(who & ((1u << lane) - 1u));
+        col[at] = in.col[e];
+        colq[at] = p;
+        colx[at] = xs[e];
+      }
+      listed += __popc(who);
+    }
+    if (lane < 3 && listed + lane < kMaxTeacher) {       // the list is read four at a time
+      col[listed + lane] = -1;
+      colq[listed + lane] = 0.f;
     }
     if (lane == 0) {
+      n = listed;
       any = have;
       bad = out;
     }
     __syncwarp();
-  }
-  // mass[i]: all of the teacher's probability in entry i's column, which may come more than once
-  __device__ __forceinline__ void gather_mass(int K) {
-    constexpr int E = kMaxTeacher / 32;
-    const int lane = threadIdx.x & 31;
-    float m[E] = {};
-    for (int o = 0; o < K; o += 4) {       // entries past K have column -1 and probability 0
-      const int4 ao = *reinterpret_cast<const int4*>(&a[o]);
-      const float4 qo = *reinterpret_cast<const float4*>(&q[o]);
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (32 * e >= K) break;
-        const int j = a[lane + 32 * e];
-        m[e] += (ao.x == j ? qo.x : 0.f) + (ao.y == j ? qo.y : 0.f);
-        m[e] += (ao.z == j ? qo.z : 0.f) + (ao.w == j ? qo.w : 0.f);
+    // mass: all of the teacher's probability in a listed entry's column, which may come more than once
+    for (int i = lane; i < listed; i += 32) {
+      const int j = col[i];
+      float m = 0.f;
+      for (int o = 0; o < listed; o += 4) {
+        const int4 co = *reinterpret_cast<const int4*>(&col[o]);
+        const float4 qo = *reinterpret_cast<const float4*>(&colq[o]);
+        m += (co.x == j ? qo.x : 0.f) + (co.y == j ? qo.y : 0.f);
+        m += (co.z == j ? qo.z : 0.f) + (co.w == j ? qo.w : 0.f);
       }
+      mass[i] = m;
     }
-#pragma unroll
-    for (int e = 0; e < E; ++e) mass[lane + 32 * e] = m[e];
     __syncwarp();
+  }
+  template <class T>
+  __device__ __forceinline__ void read(const int32_t* idx, const float* val, const T* row, int K, int V, float inv_tau) {
+    Entries in;
+    float xs[kPerLane];
+    in.load(idx, val, K);
+    in.student(row, V, xs, [](int) { return true; });
+    set(in, xs, V, inv_tau, 0, V);
   }
   // loss of the row / tau^2, by the warp that read it: sum_i q_i (log q_i - log p_i)
   __device__ __forceinline__ float divergence(const RowSum& r, int K) const {
@@ -559,7 +593,7 @@ struct Teacher {
 struct ForwardArgs {
   const void* x;
   long long ld, T;
-  int V, ranks, k, K;
+  int V, ranks, per, k, K;
   long long ld_teacher;
   float c, inv_tau, tau, unit;
   const int32_t* tokens;
@@ -588,7 +622,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kFo
   const T* xr = reinterpret_cast<const T*>(A.x) + row * A.ld;
   const int k = DISTILL ? 0 : A.k;
 
-  const Slice<T> sl(xr, A.V, rank, ranks);
+  const Slice<T> sl(xr, A.V, rank, ranks, A.per);
   const float c = A.c;
   int token = -1;
   if (!DISTILL && A.tokens) token = A.tokens[row];
@@ -617,8 +651,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kFo
   }
   const bool bad_token = token >= A.V, live = DISTILL || !A.tokens || token >= 0;
   if (DISTILL && w == 0 && rank == 0)
-    te.read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, xr, A.K, A.V, A.inv_tau,
-            [](int) { return true; });
+    te.read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, xr, A.K, A.V, A.inv_tau);
   Running<T, !DISTILL> run(c);
   float top = -INFINITY, rest = -INFINITY;
   if (live) {
@@ -668,13 +701,11 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kFo
     top = max_nan(top, rest);
   }
   if (NT > 32) copy_wait<0>();           // of a row that was not looked at
-  Stat a = warp_join(run.get(), c);
+  Stat a = warp_join<32, !DISTILL>(run.get(), c);
   if (NT > 32) {
     if (lane == 0) wstat[0][w] = a;
     __syncthreads();
-    a = wstat[0][0];
-#pragma unroll
-    for (int i = 1; i < G::kWarps; ++i) a = join(a, wstat[0][i], c);
+    a = warp_join<G::kWarps, !DISTILL>(wstat[0][lane % G::kWarps], c);
   }
   const bool alternatives = !DISTILL && k > 0 && live;
   if (alternatives) top_of_slice<T, NT>(sh, sl, ring, top, rest, k);
@@ -724,7 +755,7 @@ struct GradArgs {
   const void* x;
   void* dx;
   long long ld, ld_d, T;
-  int V, ranks, K;
+  int V, ranks, per, K;
   long long ld_teacher;
   float c, inv_tau, inv_tau_lo, tau, unit;
   const int32_t* tokens;
@@ -747,20 +778,27 @@ __device__ __forceinline__ void store_vec(T* dst, const float (&y)[Elem<T>::EV],
   }
 }
 
-// A thread keeps its R vectors of the row in registers, so the gradient in the same call as the loss reads the logits
-// once: all loads, the statistics, their join over the group, all stores.  With the statistics handed over (kLogprobsGrad,
-// kDistillGrad) there is no join and `ranks` is any number of independent pieces of the row.
+// A thread keeps its R vectors of the row in registers, so the gradient in the same call as the loss (rows of a warp here,
+// longer ones in rows_distill_kernel) reads the logits once.  With the statistics handed over (kLogprobsGrad, kDistillGrad)
+// `ranks` is any number of independent pieces of the row.
 //
 // dx_j = p_j (ca + cb log2 p_j), then the entries that have a term of their own.  16-bit logits take log2 p as one fused
 // x c - kappa, two elements an instruction.  fp32 logits take (x / tau - lse) first and 1 / tau as two fp32 terms: the
 // rounding of either would shift every log p by 2^-24 of s, which an fp32 gradient shows.
+template <int NT, int MODE>
+constexpr int kGradientThreads = MODE == kDistillGrad ? NT + 32 : NT;
+template <int ID, int THREADS>
+__device__ __forceinline__ void bar_sync() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(THREADS) : "memory"); }
+template <int ID, int THREADS>
+__device__ __forceinline__ void bar_arrive() { asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(THREADS) : "memory"); }
+
 template <class T, int NT, int R, int MODE>
-__global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R > 4 ? 3 : 4) rows_gradient_kernel(const GradArgs A) {
+__global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, MODE>, 4) rows_gradient_kernel(const GradArgs A) {
   using G = Group<NT>;
   constexpr int EV = Elem<T>::EV;
   constexpr bool kTeacher = MODE != kLogprobsGrad, kStep = MODE == kDistillStep, kNarrow = sizeof(T) == 2;
-  __shared__ Stat wstat[G::kRowsPerBlock][G::kWarps];
-  __shared__ Stat cstat[kMaxCluster];
+  constexpr bool kOwnWarp = MODE == kDistillGrad && NT > 32;     // the teacher's entries have a warp of their own
+  static_assert(!kStep || NT == 32, "longer rows of the step: rows_step_kernel");
   __shared__ Teacher teacher_sh[kTeacher ? G::kRowsPerBlock : 1];
   const int t = G::tid(), lane = threadIdx.x & 31, w = NT == 32 ? 0 : (int)(threadIdx.x >> 5);
   const int ranks = NT == 32 ? 1 : A.ranks;
@@ -770,7 +808,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
   Teacher& te = teacher_sh[kTeacher ? G::slot() : 0];
   const T* xr = reinterpret_cast<const T*>(A.x) + row * A.ld;
   T* dr = reinterpret_cast<T*>(A.dx) + row * A.ld_d;
-  const Slice<T> sl(xr, A.V, rank, ranks);
+  const Slice<T> sl(xr, A.V, rank, ranks, A.per);
   const bool aligned = ((((uintptr_t)xr) ^ ((uintptr_t)dr)) & 15u) == 0;   // vectors of x are vectors of dx
   const int edge = sl.edge(t);
   const float c = A.c;
@@ -788,6 +826,27 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
     lse = A.lse_in[row];
     zero = zero || lse <= kEmptyLse;       // nothing left by the masks
   }
+  constexpr int kThreads = kGradientThreads<NT, MODE>;
+  const bool in_place = A.x == A.dx;
+  if (kOwnWarp && w == G::kWarps) {
+    // this piece's columns of the teacher: prepared while the other warps work, written over what they store
+    const int32_t* idx = A.teacher_tokens + row * A.ld_teacher;
+    Entries in;
+    float xs[kPerLane];
+    in.load(idx, A.teacher_logits + row * A.ld_teacher, A.K);
+    in.student(xr, A.V, xs, [&](int j) { return j >= sl.e0 && j < sl.e1; });
+    te.set(in, xs, A.V, A.inv_tau, sl.e0, sl.e1);
+    if (in_place) bar_sync<1, kThreads>();          // the student's logits are read before they are written over
+    bar_sync<2, kThreads>();
+    const float ca = A.d_loss[row] * A.tau;
+    if (zero || !te.any || te.bad) return;
+    for (int i = lane; i < te.n; i += 32) {
+      const float x = te.colx[i];
+      const float lp = kNarrow ? fmaf(x, c, -lse * kLog2e) : fmaf(x, A.inv_tau, fmaf(x == -INFINITY ? 0.f : x, A.inv_tau_lo, -lse)) * kLog2e;
+      dr[te.col[i]] = Elem<T>::from_float(ca * (ex2(lp) - te.mass[i]));
+    }
+    return;
+  }
   uint4 v[R];
   float xe = -INFINITY;
   const int per_turn = R * NT;
@@ -800,34 +859,30 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
     }
     if (edge >= 0) xe = Elem<T>::to_float(xr[edge]);
   }
-  if (kTeacher && w == 0)
-    // the first rank needs all of the student's logits for the loss, every rank its own slice's for the gradient
-    te.read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, xr, A.K, A.V, A.inv_tau,
-            [&](int j) { return (kStep && rank == 0) || (j >= sl.e0 && j < sl.e1); });
+  bool bad = false;
+  if constexpr (kOwnWarp) {
+    Entries in;                       // is there anything to learn from: every warp looks for itself
+    in.load(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, A.K);
+    bool any = false;
+#pragma unroll
+    for (int e = 0; e < kPerLane; ++e) {
+      bad = bad || in.col[e] >= A.V;
+      any = any || (in.col[e] >= 0 && !(in.t[e] == -INFINITY));
+    }
+    bad = __any_sync(0xffffffffu, bad);
+    zero = zero || !(__any_sync(0xffffffffu, any) || bad);
+    if (in_place) bar_sync<1, kThreads>();
+  }
+  if (kTeacher && !kOwnWarp && w == 0)
+    te.read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, xr, A.K, A.V, A.inv_tau);
 
   float ref = 0.f, log2s = 0.f;
   if (kStep) {
-    cg::cluster_group cluster = cg::this_cluster();
-    if (ranks > 1) cluster.barrier_arrive();          // every block of the cluster runs before its memory is written
     Running<T, false> run(c);
     run.set_ref(max_nan(max_nan(Elem<T>::largest(v), xe), kUnset));
     run.add(v);
     run.one(xe);
-    Stat a = warp_join(run.get(), c);
-    if (NT > 32) {
-      if (lane == 0) wstat[0][w] = a;
-      __syncthreads();
-      a = wstat[0][0];
-#pragma unroll
-      for (int i = 1; i < G::kWarps; ++i) a = join(a, wstat[0][i], c);
-    }
-    if (ranks > 1) {
-      cluster.barrier_wait();
-      if (t < ranks) *cluster.map_shared_rank(&cstat[rank], t) = a;
-      cluster.sync();
-      a = cstat[0];
-      for (int i = 1; i < ranks; ++i) a = join(a, cstat[i], c);
-    }
+    const Stat a = warp_join<32, false>(run.get(), c);
     const RowSum r(a, c, A.unit, A.inv_tau);
     ref = r.ref;
     log2s = r.log2s;
@@ -842,11 +897,12 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
   }
 
   float ca, cb = 0.f, cy = 0.f;
-  bool bad = false;
   if (kTeacher) {
-    G::sync();
-    zero = zero || !te.any;
-    bad = te.bad != 0;
+    if (!kOwnWarp) {
+      G::sync();
+      zero = zero || !te.any;
+      bad = te.bad != 0;
+    }
     ca = A.d_loss[row] * A.tau;
   } else {
     const float g = A.d_logprob ? A.d_logprob[row] : 0.f, h = A.d_entropy ? A.d_entropy[row] : 0.f;
@@ -888,7 +944,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
         Elem<T>::pairs(MODE == kLogprobsGrad ? at_least<T>(xv, lo) : xv, p);
 #pragma unroll
         for (int i = 0; i < EV / 2; ++i) {
-          const f32x2 lp = fma2(p[i], c2, k2), e = ex2x2(lp);
+          const f32x2 lp = fma2(p[i], c2, k2), e = MODE == kDistillGrad ? exp2_by_fma(lp) : ex2x2(lp);
           p[i] = mul2(e, MODE == kLogprobsGrad ? fma2(cb2, lp, ca2) : ca2);
         }
         if (MODE == kLogprobsGrad && (unsigned)(token - j0) < (unsigned)EV) {
@@ -928,206 +984,204 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kBlock, R > 8 ? 2 : R 
     if (!kTeacher && !zero && edge == token) y += cy;
     dr[edge] = Elem<T>::from_float(y);
   }
-  if (kTeacher) {
+  if constexpr (kOwnWarp) {
+    bar_arrive<2, kThreads>();
+  } else if (kTeacher) {
     // the teacher's columns: p_j minus all of the teacher's mass there (the same column may come more than once; every
     // entry then writes the same value), over what the loop above wrote
     G::sync();
     if (zero || bad) return;
-    for (int i = t; i < A.K; i += NT) {
-      const int j = te.a[i];
-      if (j < sl.e0 || j >= sl.e1) continue;
-      float q = 0.f;
-      for (int o = 0; o < A.K; ++o)
-        if (te.a[o] == j) q += te.q[o];
+    for (int i = t; i < te.n; i += NT) {
       float lp;
-      dr[j] = Elem<T>::from_float(ca * (prob(te.x[i], lp) - q));
+      dr[te.col[i]] = Elem<T>::from_float(ca * (prob(te.colx[i], lp) - te.mass[i]));
     }
   }
 }
 
 // The teacher's gradients for rows longer than a warp's.  A block runs over items (a row in the step, each block of a
 // cluster its slice; a piece of a row with the statistics handed over): eight warps hold the item's vectors in registers
-// while the next two items are on their way through shared memory, so that memory never waits for the barriers between
-// load and store.  A ninth warp prepares the next item's teacher entries meanwhile and, when the vectors' gradient is stored,
-// writes the teacher's columns over it.
-constexpr int kDistillThreads = kBlock + 32;
-template <int ID>
-__device__ __forceinline__ void bar_sync() { asm volatile("bar.sync %0, %1;" ::"n"(ID), "n"(kDistillThreads) : "memory"); }
-template <int ID>
-__device__ __forceinline__ void bar_arrive() { asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(kDistillThreads) : "memory"); }
-
-template <class T, int R, bool STEP>
-__global__ void __launch_bounds__(kDistillThreads, R > 8 ? 1 : R > 4 ? 3 : 4) rows_distill_kernel(const GradArgs A) {
-  constexpr int EV = Elem<T>::EV, NT = kBlock, kWarps = NT / 32;
+// while the next item's are on their way to shared memory, so that memory never waits for the barriers between load and
+// store.  A ninth warp prepares the next item's teacher entries meanwhile and, when the vectors' gradient is stored, writes
+// the teacher's columns over it.
+template <class T, int NT, int R>
+__global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_step_kernel(const GradArgs A) {
+  constexpr int EV = Elem<T>::EV, kWarps = NT / 32, kThreads = NT + 32;
   constexpr bool kNarrow = sizeof(T) == 2;
-  extern __shared__ uint4 buffer[];                // [2][R][NT], a thread's own column
+  extern __shared__ uint4 buffer[];                // [R][NT], a thread's own column
   __shared__ Stat wstat[2][kWarps];
   __shared__ Stat cstat[2][kMaxCluster];
   __shared__ Teacher teacher[2];
   const int t = threadIdx.x, lane = t & 31, w = t >> 5, ranks = A.ranks;
-  const int my_rank = (int)(blockIdx.x % (unsigned)ranks);
-  const long long items = STEP ? A.T : A.T * ranks;
-  const long long q0 = STEP ? blockIdx.x / (unsigned)ranks : blockIdx.x, step = STEP ? gridDim.x / (unsigned)ranks : gridDim.x;
+  // a block stays with one rank and goes over rows
+  const int rank = (int)(blockIdx.x % (unsigned)ranks);
+  const int rows = (int)A.T, step = (int)(gridDim.x / (unsigned)ranks), first = (int)(blockIdx.x / (unsigned)ranks);
   const float c = A.c;
-  auto row_of = [&](long long q) { return STEP ? q : q / ranks; };
-  auto slice_of = [&](long long q) {
-    return Slice<T>(reinterpret_cast<const T*>(A.x) + row_of(q) * A.ld, A.V, STEP ? my_rank : (int)(q % ranks), ranks);
-  };
-  // the statistics of an item's row, the same in every thread of the cluster
+  auto slice_of = [&](int row) { return Slice<T>(reinterpret_cast<const T*>(A.x) + (long long)row * A.ld, A.V, rank, ranks, A.per); };
+  // the statistics of a row, the same in every thread of the cluster
   auto row_sum = [&](int b) {
-    Stat a = wstat[b][0];
-#pragma unroll
-    for (int i = 1; i < kWarps; ++i) a = join(a, wstat[b][i], c);
+    Stat a = warp_join<kWarps, false>(wstat[b][lane % kWarps], c);
     if (ranks > 1) {
       cg::cluster_group cluster = cg::this_cluster();
-      if (t < ranks) *cluster.map_shared_rank(&cstat[b][my_rank], t) = a;
+      if (t < ranks) *cluster.map_shared_rank(&cstat[b][rank], t) = a;
       cluster.sync();
-      a = cstat[b][0];
-      for (int i = 1; i < ranks; ++i) a = join(a, cstat[b][i], c);
+      Stat o{kUnset, 0.f, 0.f};
+      if (lane % kMaxCluster < ranks) o = cstat[b][lane % kMaxCluster];
+      a = warp_join<kMaxCluster, false>(o, c);
     }
     return RowSum(a, c, A.unit, A.inv_tau);
   };
-  // p of a logit, from the row's statistics or from an lse handed over (see rows_gradient_kernel for the two forms)
-  auto prob = [&](float x, float ref, float log2s, float lse) -> float {
-    if (STEP) return ex2(scaled(x, ref, c) - log2s);
-    if (kNarrow) return ex2(fmaf(x, c, -lse * kLog2e));
-    return ex2(fmaf(x, A.inv_tau, fmaf(x == -INFINITY ? 0.f : x, A.inv_tau_lo, -lse)) * kLog2e);
+  auto prob = [&](float x, float ref, float log2s) -> float {
+    return ex2(scaled(x, ref, c) - log2s);
   };
   // every block of the cluster runs before its memory is written
-  if (STEP && ranks > 1) cg::this_cluster().sync();
+  if (ranks > 1) cg::this_cluster().sync();
 
   if (w == kWarps) {
-    auto prepare = [&](long long q, int b) {
-      if (q >= items) return;
-      const long long row = row_of(q);
-      const Slice<T> sl = slice_of(q);
-      teacher[b].read(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, sl.row, A.K, A.V, A.inv_tau,
-                      [&](int j) { return (STEP && my_rank == 0) || (j >= sl.e0 && j < sl.e1); });
-      teacher[b].gather_mass(A.K);
+    auto load = [&](int row, Entries& in) {
+      if (row < rows) in.load(A.teacher_tokens + row * A.ld_teacher, A.teacher_logits + row * A.ld_teacher, A.K);
     };
-    prepare(q0, 0);
+    // the student's logits: the first rank needs all of them for the loss, every rank its own slice's for the gradient
+    auto look = [&](int row, const Entries& in, float (&xs)[kPerLane]) {
+      if (row >= rows) return;
+      const Slice<T> sl = slice_of(row);
+      in.student(sl.row, A.V, xs, [&](int j) { return rank == 0 || (j >= sl.e0 && j < sl.e1); });
+    };
+    auto prepare = [&](int row, const Entries& in, const float (&xs)[kPerLane], int b) {
+      if (row >= rows) return;
+      const Slice<T> sl = slice_of(row);
+      teacher[b].set(in, xs, A.V, A.inv_tau, sl.e0, sl.e1);
+    };
+    Entries now, next;
+    float xs[kPerLane], next_g = first < rows ? A.d_loss[first] : 0.f;
+    load(first, now);
+    load(first + step, next);
+    look(first, now, xs);
+    prepare(first, now, xs, 0);
+    now = next;
+    look(first + step, now, xs);
+    load(first + 2 * step, next);
     int b = 0;
-    for (long long q = q0; q < items; q += step, b ^= 1) {
-      const long long row = row_of(q);
+    for (int row = first; row < rows; row += step, b ^= 1) {
       const Teacher& te = teacher[b];
-      const float lse = STEP ? 0.f : A.lse_in[row], ca = A.d_loss[row] * A.tau;
-      bar_sync<1>();
-      float ref = 0.f, log2s = 0.f;
-      bool zero = !te.any || te.bad || (!STEP && lse <= kEmptyLse);
-      if (STEP) {
-        const RowSum r = row_sum(b);
-        ref = r.ref;
-        log2s = r.log2s;
-        zero = zero || r.empty;
-        if (my_rank == 0) {
-          const float kl = te.divergence(r, A.K);
-          if (lane == 0) {
-            A.loss[row] = A.tau * A.tau * kl;
-            A.lse_out[row] = te.any ? r.lse : 0.f;
-          }
+      const float ca = next_g * A.tau;
+      if (row + step < rows) next_g = A.d_loss[row + step];
+      // the next row's list is made while the other warps take this row's statistics; its loads are a turn old
+      prepare(row + step, now, xs, b ^ 1);
+      bar_sync<1, kThreads>();
+      now = next;
+      look(row + 2 * step, now, xs);
+      load(row + 3 * step, next);
+      const RowSum r = row_sum(b);
+      if (rank == 0) {
+        const float kl = te.divergence(r, A.K);
+        if (lane == 0) {
+          A.loss[row] = A.tau * A.tau * kl;
+          A.lse_out[row] = te.any ? r.lse : 0.f;
         }
       }
-      prepare(q + step, b ^ 1);
-      bar_sync<2>();
-      if (!zero) {
-        const Slice<T> sl = slice_of(q);
-        T* dr = reinterpret_cast<T*>(A.dx) + row * A.ld_d;
-        for (int i = lane; i < A.K; i += 32) {
-          const int j = te.a[i];
-          if (j >= sl.e0 && j < sl.e1) dr[j] = Elem<T>::from_float(ca * (prob(te.x[i], ref, log2s, lse) - te.mass[i]));
-        }
-      }
+      T* dr = reinterpret_cast<T*>(A.dx) + (long long)row * A.ld_d;
+      bar_sync<2, kThreads>();
+      if (te.any && !te.bad && !r.empty)
+        for (int i = lane; i < te.n; i += 32)
+          dr[te.col[i]] = Elem<T>::from_float(ca * (prob(te.colx[i], r.ref, r.log2s) - te.mass[i]));
       __syncwarp();
     }
     return;
   }
 
-  float next_edge = -INFINITY, next_lse = 0.f, next_g = 0.f;
-  auto fetch = [&](long long q, int b) {           // the item's vectors into buffer b
-    if (q < items) {
-      const Slice<T> sl = slice_of(q);
+  // What a thread knows of a row before its turn: where its vectors lie (they are on their way to its column of the
+  // buffer), the edge element and the row's scalars.
+  struct Turn {
+    const T* vec;          // its first vector
+    int mine, edge;        // vector i is this thread's if i NT < mine; column of the edge element or -1
+    float xe, g;
+  } next;
+  auto plan = [&](int row) {
+    next.mine = 0;
+    if (row >= rows) return;
+    const Slice<T> sl = slice_of(row);
+    next.vec = sl.vec(sl.v0 + t);
+    next.mine = sl.v1 - sl.v0 - t;
+    next.edge = sl.edge(t);
+    next.xe = next.edge >= 0 ? Elem<T>::to_float(sl.row[next.edge]) : -INFINITY;
+    next.g = A.d_loss[row];
+  };
+  auto fetch = [&](int i) {                        // the next row's vector i into the buffer
+    if (i * NT < next.mine) copy16(&buffer[i * NT + t], next.vec + i * NT * EV);
+  };
+  constexpr int B = R < kBatch ? R : kBatch;
+  plan(first);
+#pragma unroll
+  for (int i = 0; i < R; ++i) fetch(i);
+  copy_commit();
+  int b = 0;
+  for (int row = first; row < rows; row += step, b ^= 1) {
+    const Turn now = next;
+    const long long row_at = (long long)row * A.ld, drow_at = (long long)row * A.ld_d;
+    T* dst = reinterpret_cast<T*>(A.dx) + drow_at + (now.vec - (reinterpret_cast<const T*>(A.x) + row_at));
+    const bool aligned = (((uintptr_t)dst) & 15u) == 0;          // vectors of x are vectors of dx
+    float ca = now.g * A.tau;
+    copy_wait<0>();
+    {
+      Running<T, false> run(c);
+      run.follow(now.xe);
+      run.one(now.xe);
+#pragma unroll
+      for (int i0 = 0; i0 < R; i0 += B) {
+        uint4 v[B];
+#pragma unroll
+        for (int i = 0; i < B; ++i) {
+          v[i] = make_uint4(Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf);
+          if ((i0 + i) * NT < now.mine) v[i] = buffer[(i0 + i) * NT + t];
+        }
+        run.follow(Elem<T>::largest(v));
+        run.add(v);
+      }
+      const Stat a = warp_join<32, false>(run.get(), c);
+      if (lane == 0) wstat[b][w] = a;
+    }
+    bar_sync<1, kThreads>();
+    plan(row + step);
+    if (teacher[b].bad) ca = __int_as_float(0x7fc00000);
+    const RowSum r = row_sum(b);
+    const float ref = r.ref, log2s = r.log2s;
+    const bool zero = !teacher[b].any || r.empty;
+    if (aligned && !zero && near_ref(ref)) {
+      // two elements an instruction; a 16-bit gradient bears ref c + log2 s as one rounded number, an fp32 one does not
+      const float kappa = ref * c + (kNarrow ? log2s : 0.f);
+      const f32x2 c2 = pair_of(c, c), k2 = pair_of(-kappa, -kappa), ca2 = pair_of(ca, ca), l2 = pair_of(-log2s, -log2s);
 #pragma unroll
       for (int i = 0; i < R; ++i) {
-        const int at = sl.v0 + t + i * NT;
-        if (at < sl.v1) copy16(&buffer[(b * R + i) * NT + t], sl.vec(at));
+        if (i * NT < now.mine) {
+          f32x2 p[EV / 2];
+          Elem<T>::pairs(buffer[i * NT + t], p);
+#pragma unroll
+          for (int e = 0; e < EV / 2; ++e) {
+            p[e] = fma2(p[e], c2, k2);
+            if (!kNarrow) p[e] = add2(p[e], l2);
+            p[e] = mul2(kNarrow && e == 0 ? exp2_by_fma(p[e]) : ex2x2(p[e]), ca2);
+          }
+          *reinterpret_cast<uint4*>(dst + i * NT * EV) = Elem<T>::pack_pairs(p);
+        }
+        fetch(i);
+      }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < R; ++i) {
+        if (i * NT < now.mine) {
+          float x[EV];
+          Elem<T>::unpack(buffer[i * NT + t], x);
+#pragma unroll
+          for (int e = 0; e < EV; ++e) x[e] = zero ? 0.f : ca * prob(x[e], ref, log2s);
+          store_vec<T>(dst + i * NT * EV, x, aligned);
+        }
+        fetch(i);
       }
     }
     copy_commit();
-  };
-  auto peek = [&](long long q) {                   // what it needs beside them
-    if (q >= items) return;
-    const Slice<T> sl = slice_of(q);
-    const int j = sl.edge(t);
-    next_edge = j >= 0 ? Elem<T>::to_float(sl.row[j]) : -INFINITY;
-    next_g = A.d_loss[row_of(q)];
-    if (!STEP) next_lse = A.lse_in[row_of(q)];
-  };
-  fetch(q0, 0);
-  fetch(q0 + step, 1);
-  peek(q0);
-  int b = 0;
-  for (long long q = q0; q < items; q += step, b ^= 1) {
-    const long long row = row_of(q);
-    const Slice<T> sl = slice_of(q);
-    T* dr = reinterpret_cast<T*>(A.dx) + row * A.ld_d;
-    const bool aligned = ((((uintptr_t)sl.row) ^ ((uintptr_t)dr)) & 15u) == 0;   // vectors of x are vectors of dx
-    const float xe = next_edge, lse = next_lse;
-    float ca = next_g * A.tau;
-    copy_wait<1>();
-    uint4 v[R];
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      if (sl.v0 + t + i * NT < sl.v1) v[i] = buffer[(b * R + i) * NT + t];
-      else v[i] = make_uint4(Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf);
-    }
-    fetch(q + 2 * step, b);
-    peek(q + step);
-    if (STEP) {
-      Running<T, false> run(c);
-      run.set_ref(max_nan(max_nan(Elem<T>::largest(v), xe), kUnset));
-      run.add(v);
-      run.one(xe);
-      const Stat a = warp_join(run.get(), c);
-      if (lane == 0) wstat[b][w] = a;
-    }
-    bar_sync<1>();
-    bool zero = !teacher[b].any || (!STEP && lse <= kEmptyLse);
-    if (teacher[b].bad) ca = __int_as_float(0x7fc00000);
-    float ref = 0.f, log2s = 0.f;
-    if (STEP) {
-      const RowSum r = row_sum(b);
-      ref = r.ref;
-      log2s = r.log2s;
-      zero = zero || r.empty;
-    }
-    const float kappa = STEP ? ref * c + log2s : lse * kLog2e;
-    const f32x2 c2 = pair_of(c, c), k2 = pair_of(-kappa, -kappa), ca2 = pair_of(ca, ca);
-    const bool packed = kNarrow && aligned && !zero && (!STEP || near_ref(ref));
-#pragma unroll
-    for (int i = 0; i < R; ++i) {
-      const int at = sl.v0 + t + i * NT;
-      if (at >= sl.v1) break;
-      T* dst = dr + sl.head + at * EV;
-      if constexpr (kNarrow) {
-        if (packed) {
-          f32x2 p[EV / 2];
-          Elem<T>::pairs(v[i], p);
-#pragma unroll
-          for (int e = 0; e < EV / 2; ++e) p[e] = mul2(ex2x2(fma2(p[e], c2, k2)), ca2);
-          *reinterpret_cast<uint4*>(dst) = Elem<T>::pack_pairs(p);
-          continue;
-        }
-      }
-      float x[EV];
-      Elem<T>::unpack(v[i], x);
-#pragma unroll
-      for (int e = 0; e < EV; ++e) x[e] = zero ? 0.f : ca * prob(x[e], ref, log2s, lse);
-      store_vec<T>(dst, x, aligned);
-    }
-    const int edge = sl.edge(t);
-    if (edge >= 0) dr[edge] = Elem<T>::from_float(zero ? 0.f : ca * prob(xe, ref, log2s, lse));
-    __threadfence_block();
-    bar_arrive<2>();
+    if (now.edge >= 0)
+      reinterpret_cast<T*>(A.dx)[drow_at + now.edge] = Elem<T>::from_float(zero ? 0.f : ca * prob(now.xe, ref, log2s));
+    bar_arrive<2, kThreads>();
   }
   copy_wait<0>();
 }
@@ -1203,60 +1257,60 @@ template <class T, bool DISTILL>
 cudaError_t forward(ForwardArgs& A, cudaStream_t st) {
   if (warp_rows<T>(A.T, A.V)) {
     A.ranks = 1;
+    A.per = A.V / Elem<T>::EV;
     return launch(rows_forward_kernel<T, 32, DISTILL>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
   }
   const long long nvec = A.V / Elem<T>::EV;
   if (nvec <= kHalfVectors && A.T >= 2 * kForwardBlocks * kSMs) {
     A.ranks = 1;
+    A.per = (int)nvec;
     return launch(rows_forward_kernel<T, kHalfBlock, DISTILL>, A, A.T, kHalfBlock, (size_t)kRing * kBatch * kHalfBlock * 16, 1, st);
   }
   A.ranks = forward_ranks(A.T, nvec);
+  A.per = (int)((nvec + A.ranks - 1) / A.ranks);
   return launch(rows_forward_kernel<T, kBlock, DISTILL>, A, A.T * A.ranks, kBlock, (size_t)kRing * kBatch * kBlock * 16, A.ranks, st);
 }
 
-template <class T, int R, bool STEP>
-cudaError_t distill_blocks(GradArgs& A, cudaStream_t st) {
-  constexpr size_t smem = (size_t)2 * R * kBlock * 16;
+template <class T, int NT, int R>
+cudaError_t step_blocks(GradArgs& A, cudaStream_t st) {
+  constexpr size_t smem = (size_t)R * NT * 16;
   static Resident resident;
   int blocks = 0;
-  const int cluster = STEP ? A.ranks : 1;
-  const cudaError_t rc = resident.get(rows_distill_kernel<T, R, STEP>, kDistillThreads, smem, cluster, blocks);
+  const cudaError_t rc = resident.get(rows_step_kernel<T, NT, R>, NT + 32, smem, A.ranks, blocks);
   if (rc != cudaSuccess) return rc;
-  const long long want = A.T * A.ranks;
-  return launch(rows_distill_kernel<T, R, STEP>, A, want < blocks ? want : blocks, kDistillThreads, smem, cluster, st);
+  const long long at_once = blocks / A.ranks > 0 ? blocks / A.ranks : 1;          // rows
+  return launch(rows_step_kernel<T, NT, R>, A, (A.T < at_once ? A.T : at_once) * A.ranks, NT + 32, smem, A.ranks, st);
 }
 
 template <class T, int MODE>
 cudaError_t gradient(GradArgs& A, cudaStream_t st) {
   const long long nvec = A.V / Elem<T>::EV;
-  if (warp_rows<T>(A.T, A.V)) {
+  if (A.V <= kWarpRow || (MODE == kLogprobsGrad && warp_rows<T>(A.T, A.V))) {
     A.ranks = 1;
-    constexpr int R = kWarpRow / Elem<T>::EV / 32;
-    if (A.V <= kWarpRow || MODE == kLogprobsGrad) return launch(rows_gradient_kernel<T, 32, R, MODE>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
-    if constexpr (MODE != kLogprobsGrad)
-      return launch(rows_gradient_kernel<T, 32, kWarpVectors / 32, MODE>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
+    A.per = (int)nvec;
+    return launch(rows_gradient_kernel<T, 32, kWarpRow / Elem<T>::EV / 32, MODE>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
   }
-  if constexpr (MODE == kLogprobsGrad) {
-    // pieces of 4 vectors a thread, at least one; larger where the grid would pass 2^31 blocks
-    long long ranks = (nvec + 4 * kBlock - 1) / (4 * kBlock);
+  if constexpr (MODE != kDistillStep) {
+    // pieces of 8 vectors a thread, smaller ones while the rows do not fill the GPU, larger ones where the grid would pass
+    // 2^31 blocks
+    long long ranks = (nvec + 8 * kBlock - 1) / (8 * kBlock);
+    while (A.T * ranks < 4 * kSMs && nvec > ranks * 2 * kBlock) ranks *= 2;
     while (A.T * ranks > 0x7fffffffll) ranks = (ranks + 1) / 2;
     A.ranks = ranks < 1 ? 1 : (int)ranks;
-    return launch(rows_gradient_kernel<T, kBlock, 4, MODE>, A, A.T * A.ranks, kBlock, 0, 1, st);
-  } else if constexpr (MODE == kDistillGrad) {
-    A.ranks = (int)((nvec + 8 * kBlock - 1) / (8 * kBlock));
-    while (A.T * A.ranks < 3 * kSMs && nvec > (long long)A.ranks * 2 * kBlock) A.ranks *= 2;
-    const long long per = (nvec + A.ranks - 1) / A.ranks;
-    return per <= 4 * kBlock ? distill_blocks<T, 4, false>(A, st) : distill_blocks<T, 8, false>(A, st);
+    A.per = (int)((nvec + A.ranks - 1) / A.ranks);
+    return launch(rows_gradient_kernel<T, kBlock, 4, MODE>, A, A.T * A.ranks, kGradientThreads<kBlock, MODE>, 0, 1, st);
   } else {
+    // a row in one block of 128 threads (up to 16 vectors a thread), or in up to eight of 256; spread wider while the rows
+    // do not fill the GPU
     int ranks = 1;
-    while (ranks < kMaxCluster &&
-           (nvec > (long long)ranks * 8 * kBlock || (A.T * ranks < 3 * kSMs && nvec > (long long)ranks * 2 * kBlock)))
+    while (ranks < kMaxCluster && (nvec > (long long)ranks * 16 * kBlock || (A.T * ranks < 3 * kSMs && nvec > (long long)ranks * 2 * kHalfBlock)))
       ranks *= 2;
     A.ranks = ranks;
-    const long long per = (nvec + ranks - 1) / ranks;
-    if (per <= 4 * kBlock) return distill_blocks<T, 4, true>(A, st);
-    if (per <= 8 * kBlock) return distill_blocks<T, 8, true>(A, st);
-    return distill_blocks<T, 16, true>(A, st);
+    A.per = (int)((nvec + ranks - 1) / ranks);
+    if (A.per <= 4 * kHalfBlock) return step_blocks<T, kHalfBlock, 4>(A, st);
+    if (A.per <= 8 * kHalfBlock) return step_blocks<T, kHalfBlock, 8>(A, st);
+    if (A.per <= 16 * kHalfBlock) return step_blocks<T, kHalfBlock, 16>(A, st);
+    return step_blocks<T, kBlock, 16>(A, st);
   }
 }
 
