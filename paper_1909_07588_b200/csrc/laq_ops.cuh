@@ -87,29 +87,6 @@ __device__ __forceinline__ f32x2 ex2x2(f32x2 p) {
   return pair_of(ex2(a), ex2(b));
 }
 
-// 2^y without the special-function unit, for results of 16 bits: y = n + f with n the nearest integer (taken by adding and
-// subtracting 1.5 2^23, whose low mantissa bits then hold n), 2^f by a polynomial of degree 4 that was fitted to it on
-// [-1/2, 1/2] in the relative maximum norm with the constant 1 (error 2.8e-6), n added to the exponent.  y below -127 counts
-// as -127, where the result is 0; results below 2^-126 are subnormal or 0 and flushed by the product that follows.  A NaN is
-// not kept.
-__device__ __forceinline__ f32x2 exp2_by_fma(f32x2 y) {
-  const float kRound = 12582912.f, kC1 = 0.69312419f, kC2 = 0.24024099f, kC3 = 0.05590643f, kC4 = 0.00958285f;
-  float a, b, p0, p1, t0, t1;
-  split(y, a, b);
-  y = pair_of(fmaxf(a, -127.f), fmaxf(b, -127.f));
-  const f32x2 t = add2(y, pair_of(kRound, kRound));
-  const f32x2 f = fma2(add2(t, pair_of(-kRound, -kRound)), pair_of(-1.f, -1.f), y);
-  f32x2 p = fma2(pair_of(kC4, kC4), f, pair_of(kC3, kC3));
-  p = fma2(p, f, pair_of(kC2, kC2));
-  p = fma2(p, f, pair_of(kC1, kC1));
-  p = fma2(p, f, pair_of(1.f, 1.f));
-  split(p, p0, p1);
-  split(t, t0, t1);
-  p0 = __int_as_float(__float_as_int(p0) + (__float_as_int(t0) << 23));
-  p1 = __int_as_float(__float_as_int(p1) + (__float_as_int(t1) << 23));
-  return pair_of(p0, p1);
-}
-
 template <class T>
 struct Elem;
 

@@ -793,7 +793,7 @@ template <int ID, int THREADS>
 __device__ __forceinline__ void bar_arrive() { asm volatile("bar.arrive %0, %1;" ::"n"(ID), "n"(THREADS) : "memory"); }
 
 template <class T, int NT, int R, int MODE>
-__global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, MODE>, 4) rows_gradient_kernel(const GradArgs A) {
+__global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, MODE>, NT == 32 ? 4 : 5) rows_gradient_kernel(const GradArgs A) {
   using G = Group<NT>;
   constexpr int EV = Elem<T>::EV;
   constexpr bool kTeacher = MODE != kLogprobsGrad, kStep = MODE == kDistillStep, kNarrow = sizeof(T) == 2;
@@ -944,7 +944,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
         Elem<T>::pairs(MODE == kLogprobsGrad ? at_least<T>(xv, lo) : xv, p);
 #pragma unroll
         for (int i = 0; i < EV / 2; ++i) {
-          const f32x2 lp = fma2(p[i], c2, k2), e = MODE == kDistillGrad ? exp2_by_fma(lp) : ex2x2(lp);
+          const f32x2 lp = fma2(p[i], c2, k2), e = ex2x2(lp);
           p[i] = mul2(e, MODE == kLogprobsGrad ? fma2(cb2, lp, ca2) : ca2);
         }
         if (MODE == kLogprobsGrad && (unsigned)(token - j0) < (unsigned)EV) {
@@ -1159,7 +1159,7 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
           for (int e = 0; e < EV / 2; ++e) {
             p[e] = fma2(p[e], c2, k2);
             if (!kNarrow) p[e] = add2(p[e], l2);
-            p[e] = mul2(kNarrow && e == 0 ? exp2_by_fma(p[e]) : ex2x2(p[e]), ca2);
+            p[e] = mul2(ex2x2(p[e]), ca2);
           }
           *reinterpret_cast<uint4*>(dst + i * NT * EV) = Elem<T>::pack_pairs(p);
         }
@@ -1291,9 +1291,9 @@ cudaError_t gradient(GradArgs& A, cudaStream_t st) {
     return launch(rows_gradient_kernel<T, 32, kWarpRow / Elem<T>::EV / 32, MODE>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
   }
   if constexpr (MODE != kDistillStep) {
-    // pieces of 8 vectors a thread, smaller ones while the rows do not fill the GPU, larger ones where the grid would pass
+    // pieces of 16 vectors a thread, smaller ones while the rows do not fill the GPU, larger ones where the grid would pass
     // 2^31 blocks
-    long long ranks = (nvec + 8 * kBlock - 1) / (8 * kBlock);
+    long long ranks = (nvec + 16 * kBlock - 1) / (16 * kBlock);
     while (A.T * ranks < 4 * kSMs && nvec > ranks * 2 * kBlock) ranks *= 2;
     while (A.T * ranks > 0x7fffffffll) ranks = (ranks + 1) / 2;
     A.ranks = ranks < 1 ? 1 : (int)ranks;

@@ -9,7 +9,7 @@ import os
 import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
-LIB_PATH = os.environ.get("LAQLIB") or os.path.join(_HERE, "csrc", "liblaq_b200.so")
+LIB_PATH = os.path.join(_HERE, "csrc", "liblaq_b200.so")
 
 LAQ_OK, LAQ_EINVAL, LAQ_EWORKSPACE, LAQ_ECUDA, LAQ_ENONFINITE, LAQ_ESTATE, LAQ_ETIMEOUT = range(7)
 STATUS_NAMES = ["LAQ_OK", "LAQ_EINVAL", "LAQ_EWORKSPACE", "LAQ_ECUDA", "LAQ_ENONFINITE", "LAQ_ESTATE", "LAQ_ETIMEOUT"]

@@ -12,6 +12,7 @@ given.  Calls run on ``stream`` (default: the current stream of the tensors' dev
 kernels only: there is no CPU fallback.  ``check_status`` reports a bounded wait of the product kernels that ran out.
 """
 import ctypes as C
+import threading
 
 import torch
 
@@ -29,76 +30,81 @@ def _refuse(message):
     raise ValueError(message)
 
 
-def _check(t, name, device, dtype=None, shape=None):
+# These checks run on every call, whose kernel may take a few microseconds: they use the cheapest forms of the questions.
+_current_device = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
+_local = threading.local()          # the calling thread's buffer for error texts
+
+
+def _check(t, name, index=None, dtype=None):
     if not isinstance(t, torch.Tensor) or not t.is_cuda:
         _refuse("%s must be a CUDA tensor" % name)
-    if device is not None and t.device != device:
-        _refuse("%s is on %s, the other tensors on %s" % (name, t.device, device))
-    if dtype is not None and t.dtype != dtype:
+    if index is not None and t.get_device() != index:
+        _refuse("%s is on %s, the other tensors on cuda:%d" % (name, t.device, index))
+    if dtype is not None and t.dtype is not dtype:
         _refuse("%s must be %s, not %s" % (name, dtype, t.dtype))
-    if shape is not None and tuple(t.shape) != shape:
-        _refuse("%s must have shape %s, not %s" % (name, shape, tuple(t.shape)))
-    return t
 
 
-def _rows(t, name, device=None, dtype=None, shape=None):
-    """A matrix with unit stride within its rows: (pointer, row stride)."""
-    _check(t, name, device, dtype, shape)
+def _rows(t, name, index=None, dtype=None, shape=None):
+    """A matrix with unit stride within its rows: (pointer, row stride, rows, columns)."""
+    _check(t, name, index, dtype)
     if t.dim() != 2:
         _refuse("%s must have two dimensions" % name)
     rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    if shape is not None and (rows, cols) != shape:
+        _refuse("%s must have shape %s, not %s" % (name, shape, (rows, cols)))
+    stride, within = t.stride()
+    if within != 1 and cols > 1:
         _refuse("%s must have unit stride within a row" % name)
-    stride = t.stride(0) if rows > 1 else cols
-    if stride < cols:
+    if rows <= 1:
+        stride = cols
+    elif stride < cols:
         _refuse("the rows of %s overlap" % name)
-    return t.data_ptr(), stride
+    return t.data_ptr(), stride, rows, cols
 
 
-def _vector(t, name, device, dtype, n):
+def _vector(t, name, index, dtype, n):
     """A contiguous vector of n elements, or None: its pointer."""
     if t is None:
         return None
-    _check(t, name, device, dtype, (n,))
+    _check(t, name, index, dtype)
+    if t.dim() != 1 or t.shape[0] != n:
+        _refuse("%s must have shape (%d,), not %s" % (name, n, tuple(t.shape)))
     if n > 1 and t.stride(0) != 1:
         _refuse("%s must be contiguous" % name)
     return t.data_ptr()
 
 
-class _On:
-    """The device of a call made current, and its stream: an output allocated inside belongs to that stream."""
-
-    def __init__(self, device, stream):
-        self.device, self.stream, self.guard = device, stream, None
-
-    def __enter__(self):
-        if self.stream is not None:
-            self.guard = torch.cuda.stream(self.stream)
-        elif torch.cuda.current_device() != self.device.index:
-            self.guard = torch.cuda.device(self.device)
-        if self.guard is not None:
-            self.guard.__enter__()
-        return self.stream.cuda_stream if self.stream is not None else torch.cuda.current_stream(self.device).cuda_stream
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _on(index, stream, body):
+    """body(raw stream) with the tensors' device current; outputs that it allocates belong to that stream."""
+    if stream is None:
+        if _current_device() == index:
+            return body(_raw_stream(index))
+        with torch.cuda.device(index):
+            return body(_raw_stream(index))
+    if stream.device.index != index:
+        _refuse("the stream belongs to %s, the tensors to cuda:%d" % (stream.device, index))
+    with torch.cuda.stream(stream):
+        return body(stream.cuda_stream)
 
 
 def _call(function, *args):
-    err = C.create_string_buffer(256)
+    err = getattr(_local, "err", None)
+    if err is None:
+        err = _local.err = C.create_string_buffer(256)
     rc = function(*args, err, 256)
     if rc != LAQ_OK:
         raise LaqError(rc, err.value.decode())
 
 
 def _logits(logits):
-    ptr, stride = _rows(logits, "logits")
-    if logits.dtype not in DTYPES:
+    ptr, stride, T, V = _rows(logits, "logits")
+    dtype = DTYPES.get(logits.dtype)
+    if dtype is None:
         _refuse("logits must be float32, bfloat16 or float16")
-    if logits.shape[1] < 1:
+    if V < 1:
         _refuse("logits have no columns")
-    return ptr, DTYPES[logits.dtype], logits.shape[0], logits.shape[1], stride
+    return (ptr, dtype, T, V, stride), T, logits.get_device()
 
 
 def token_logprobs(logits, tokens=None, top_k=0, temperature=1.0, stream=None):
@@ -108,30 +114,33 @@ def token_logprobs(logits, tokens=None, top_k=0, temperature=1.0, stream=None):
     Returns a dict: logprob, entropy, lse [rows] float32, and top_tokens [rows, top_k] int32 with top_logprobs float32.
     Without ``tokens`` there is no logprob.  A negative token leaves its row out: zeros and no alternatives.
     """
-    L = laq.load_library()
-    head = _logits(logits)
-    dev, T = logits.device, logits.shape[0]
-    tok = _vector(tokens, "tokens", dev, torch.int32, T)
+    head, T, index = _logits(logits)
+    tok = _vector(tokens, "tokens", index, torch.int32, T)
     if not 0 <= top_k <= 32:
         _refuse("top_k must be 0..32")
-    with _On(dev, stream) as st:
+
+    def body(raw):
+        dev = logits.device
         stats = torch.empty((3, T), dtype=torch.float32, device=dev)
-        out = dict(logprob=stats[0], entropy=stats[1], lse=stats[2])
-        if tokens is None:
-            del out["logprob"]
         p = stats.data_ptr()
+        logprob, entropy, lse = stats.unbind(0)
+        out = dict(entropy=entropy, lse=lse) if tok is None else dict(logprob=logprob, entropy=entropy, lse=lse)
+        tp = vp = None
         if top_k:
-            out["top_tokens"] = torch.empty((T, top_k), dtype=torch.int32, device=dev)
-            out["top_logprobs"] = torch.empty((T, top_k), dtype=torch.float32, device=dev)
-        _call(L.laq_token_logprobs, *head, temperature, tok, top_k, p if tokens is not None else None, p + 4 * T, p + 8 * T,
-              out["top_tokens"].data_ptr() if top_k else None, out["top_logprobs"].data_ptr() if top_k else None, st)
-    return out
+            out["top_tokens"] = a = torch.empty((T, top_k), dtype=torch.int32, device=dev)
+            out["top_logprobs"] = b = torch.empty((T, top_k), dtype=torch.float32, device=dev)
+            tp, vp = a.data_ptr(), b.data_ptr()
+        _call(laq.load_library().laq_token_logprobs, *head, temperature, tok, top_k, None if tok is None else p, p + 4 * T,
+              p + 8 * T, tp, vp, raw)
+        return out
+
+    return _on(index, stream, body)
 
 
 def _gradient_out(logits, out):
     if out is None:
-        out = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    ptr, stride = _rows(out, "out", logits.device, logits.dtype, tuple(logits.shape))
+        out = torch.empty_like(logits, memory_format=torch.contiguous_format)
+    ptr, stride, _, _ = _rows(out, "out", logits.get_device(), logits.dtype, tuple(logits.shape))
     return out, ptr, stride
 
 
@@ -139,28 +148,34 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, d_logprob=None, d
                             stream=None):
     """Gradient with respect to the logits of sum(d_logprob * logprob + d_entropy * entropy), given lse and entropy as
     ``token_logprobs`` returned them.  ``out`` may be ``logits`` itself."""
-    L = laq.load_library()
-    head = _logits(logits)
-    dev, T = logits.device, logits.shape[0]
+    head, T, index = _logits(logits)
     if tokens is None or lse is None:
         _refuse("tokens and lse are needed")
-    ptrs = [_vector(tokens, "tokens", dev, torch.int32, T)]
-    ptrs += [_vector(t, name, dev, torch.float32, T) for t, name in
-             ((lse, "lse"), (entropy, "entropy"), (d_logprob, "d_logprob"), (d_entropy, "d_entropy"))]
-    with _On(dev, stream) as st:
-        out, dptr, dstride = _gradient_out(logits, out)
-        _call(L.laq_token_logprobs_backward, *head, temperature, *ptrs, dptr, dstride, st)
-    return out
+    if d_entropy is not None and entropy is None:
+        _refuse("the gradient of the entropy needs the entropy")
+    f32 = torch.float32
+    ptrs = (_vector(tokens, "tokens", index, torch.int32, T), _vector(lse, "lse", index, f32, T),
+            _vector(entropy, "entropy", index, f32, T), _vector(d_logprob, "d_logprob", index, f32, T),
+            _vector(d_entropy, "d_entropy", index, f32, T))
+
+    def body(raw):
+        dx, dptr, dstride = _gradient_out(logits, out)
+        _call(laq.load_library().laq_token_logprobs_backward, *head, temperature, *ptrs, dptr, dstride, raw)
+        return dx
+
+    return _on(index, stream, body)
 
 
-def _teacher(tokens, values, device, rows):
-    tp, ts = _rows(tokens, "teacher_tokens", device, torch.int32)
-    vp, vs = _rows(values, "teacher_logits", device, torch.float32, tuple(tokens.shape))
-    if tokens.shape[0] != rows:
+def _teacher(tokens, values, index, T):
+    tp, ts, rows, k = _rows(tokens, "teacher_tokens", index, torch.int32)
+    if rows != T:
         _refuse("teacher_tokens must have a row for every row of the logits")
+    vp, vs, _, _ = _rows(values, "teacher_logits", index, torch.float32, (rows, k))
     if ts != vs:
         _refuse("teacher_tokens and teacher_logits must have the same row stride")
-    return tp, vp, tokens.shape[1], ts
+    if not 1 <= k <= 128:
+        _refuse("the teacher must have 1..128 entries per row")
+    return tp, vp, k, ts
 
 
 def distill(logits, teacher_tokens, teacher_logits, temperature=1.0, d_loss=None, out=None, stream=None):
@@ -170,62 +185,65 @@ def distill(logits, teacher_tokens, teacher_logits, temperature=1.0, d_loss=None
     Returns a dict: loss and lse [rows] float32.  With ``d_loss`` [rows] float32, the gradient of whatever the losses are
     summed into, the same call also returns dlogits (in ``out`` if given, which may be ``logits`` itself).
     """
-    L = laq.load_library()
-    head = _logits(logits)
-    dev, T = logits.device, logits.shape[0]
-    teacher = _teacher(teacher_tokens, teacher_logits, dev, T)
-    dl = _vector(d_loss, "d_loss", dev, torch.float32, T)
+    head, T, index = _logits(logits)
+    teacher = _teacher(teacher_tokens, teacher_logits, index, T)
+    dl = _vector(d_loss, "d_loss", index, torch.float32, T)
     if d_loss is None and out is not None:
         _refuse("out without d_loss")
-    with _On(dev, stream) as st:
-        stats = torch.empty((2, T), dtype=torch.float32, device=dev)
-        res = dict(loss=stats[0], lse=stats[1])
+
+    def body(raw):
+        stats = torch.empty((2, T), dtype=torch.float32, device=logits.device)
+        p = stats.data_ptr()
+        loss, lse = stats.unbind(0)
+        res = dict(loss=loss, lse=lse)
         dptr, dstride = None, 0
         if d_loss is not None:
             res["dlogits"], dptr, dstride = _gradient_out(logits, out)
-        p = stats.data_ptr()
-        _call(L.laq_distill, *head, temperature, *teacher, p, p + 4 * T, dl, dptr, dstride, st)
-    return res
+        _call(laq.load_library().laq_distill, *head, temperature, *teacher, p, p + 4 * T, dl, dptr, dstride, raw)
+        return res
+
+    return _on(index, stream, body)
 
 
 def distill_backward(logits, teacher_tokens, teacher_logits, lse, d_loss, temperature=1.0, out=None, stream=None):
     """The gradient of ``distill`` for a d_loss that is only known after the loss; lse as ``distill`` returned it."""
-    L = laq.load_library()
-    head = _logits(logits)
-    dev, T = logits.device, logits.shape[0]
-    teacher = _teacher(teacher_tokens, teacher_logits, dev, T)
+    head, T, index = _logits(logits)
+    teacher = _teacher(teacher_tokens, teacher_logits, index, T)
     if lse is None or d_loss is None:
         _refuse("lse and d_loss are needed")
-    ptrs = [_vector(lse, "lse", dev, torch.float32, T), _vector(d_loss, "d_loss", dev, torch.float32, T)]
-    with _On(dev, stream) as st:
-        out, dptr, dstride = _gradient_out(logits, out)
-        _call(L.laq_distill_backward, *head, temperature, *teacher, *ptrs, dptr, dstride, st)
-    return out
+    ptrs = (_vector(lse, "lse", index, torch.float32, T), _vector(d_loss, "d_loss", index, torch.float32, T))
+
+    def body(raw):
+        dx, dptr, dstride = _gradient_out(logits, out)
+        _call(laq.load_library().laq_distill_backward, *head, temperature, *teacher, *ptrs, dptr, dstride, raw)
+        return dx
+
+    return _on(index, stream, body)
 
 
 # --- the layer -------------------------------------------------------------------------------------------------------
 
-def _status_word(device):
-    word = _status.get(device.index)
+def _status_word(index):
+    word = _status.get(index)
     if word is None:
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError("call ops.init(device) before the first capture of a linear call on a device")
-        word = torch.zeros(1, dtype=torch.int32, device=device)
-        torch.cuda.synchronize(device)       # other streams may use it from now on
-        _status[device.index] = word
+        word = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
+        torch.cuda.synchronize(index)        # other streams may use it from now on
+        word = _status.setdefault(index, word)
     return word
 
 
 def init(device=None):
     """Set up the device's status word (done by the first linear call otherwise, which must then not be captured)."""
-    device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
-    with torch.cuda.device(device):
-        _status_word(torch.device("cuda", torch.cuda.current_device()))
+    index = torch.cuda.current_device() if device is None else torch.device(device).index or 0
+    with torch.cuda.device(index):
+        _status_word(index)
 
 
 def check_status(device=None):
     """Synchronises the device and raises LAQ_ETIMEOUT if a bounded wait of a linear call ran out since the last check."""
-    index = torch.cuda.current_device() if device is None else torch.device(device).index
+    index = torch.cuda.current_device() if device is None else torch.device(device).index or 0
     word = _status.get(index)
     if word is None:
         return
@@ -238,32 +256,31 @@ def check_status(device=None):
                                      "are not complete" % bits)
 
 
-def _layer_call(x, weight, activation, flags):
+def _layer_call(x, weight, activation, flags, index):
     c = laq.laq_linear_call()
-    c.x, c.ld_x = _rows(x, "x")
-    if x.dtype not in (torch.bfloat16, torch.float16):
+    c.x, c.ld_x, c.M, c.K = _rows(x, "x")
+    c.w, c.ld_w, c.N, inputs = _rows(weight, "weight", index, x.dtype)
+    if x.dtype is not torch.bfloat16 and x.dtype is not torch.float16:
         _refuse("x must be bfloat16 or float16")
-    if weight.dim() != 2 or weight.shape[1] != x.shape[1]:
-        _refuse("weight must be [outputs, %d]" % x.shape[1])
-    c.w, c.ld_w = _rows(weight, "weight", x.device, x.dtype)
-    if activation not in ACTIVATIONS:
+    if inputs != c.K:
+        _refuse("weight must be [outputs, %d]" % c.K)
+    act = ACTIVATIONS.get(activation)
+    if act is None:
         _refuse("activation must be one of %s" % ", ".join(sorted(ACTIVATIONS)))
-    if x.shape[1] < 1 or weight.shape[0] < 1:
+    if c.K < 1 or c.N < 1:
         _refuse("a layer needs inputs and outputs")
-    c.dtype, c.activation = DTYPES[x.dtype], ACTIVATIONS[activation]
-    c.M, c.N, c.K, c.flags = x.shape[0], weight.shape[0], x.shape[1], flags
-    c.status = _status_word(x.device).data_ptr()
+    c.dtype, c.activation, c.flags = DTYPES[x.dtype], act, flags
     return c
 
 
-def _workspace(L, c, backward, device, given):
+def _workspace(L, c, backward, index, given):
     need = L.laq_linear_workspace_bytes(C.byref(c), backward)
     if need == 0:
         return None, None, 0
     if given is None:
-        given = torch.empty(need, dtype=torch.uint8, device=device)
+        given = torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", index))
     else:
-        _check(given, "workspace", device, torch.uint8)
+        _check(given, "workspace", index, torch.uint8)
         if given.dim() != 1 or not given.is_contiguous():
             _refuse("workspace must be a contiguous vector of bytes")
     return given, given.data_ptr(), given.numel()
@@ -278,23 +295,27 @@ def linear(x, weight, bias=None, activation="none", residual=None, preact=False,
     laq_linear_workspace_bytes; calls that may overlap need workspaces of their own.
     """
     L = laq.load_library()
-    _rows(x, "x")
-    dev, dt = x.device, x.dtype
-    with _On(dev, stream) as st:
-        c = _layer_call(x, weight, activation, flags)
-        shape = (c.M, c.N)
-        c.bias = _vector(bias, "bias", dev, dt, c.N)
-        if residual is not None:
-            c.residual, c.ld_residual = _rows(residual, "residual", dev, dt, shape)
-        y = torch.empty(shape, dtype=dt, device=dev) if out is None else out
-        c.y, c.ld_y = _rows(y, "out", dev, dt, shape)
+    _check(x, "x")
+    index, dt = x.get_device(), x.dtype
+    c = _layer_call(x, weight, activation, flags, index)
+    shape = (c.M, c.N)
+    c.bias = _vector(bias, "bias", index, dt, c.N)
+    if residual is not None:
+        c.residual, c.ld_residual, _, _ = _rows(residual, "residual", index, dt, shape)
+
+    def body(raw):
+        c.status = _status_word(index).data_ptr()
+        y = torch.empty(shape, dtype=dt, device=x.device) if out is None else out
+        c.y, c.ld_y, _, _ = _rows(y, "out", index, dt, shape)
         z = None
         if preact:
-            z = torch.empty(shape, dtype=dt, device=dev)
+            z = torch.empty(shape, dtype=dt, device=x.device)
             c.z, c.ld_z = z.data_ptr(), c.N
-        ws, wp, wn = _workspace(L, c, 0, dev, workspace)
-        _call(L.laq_linear_forward, C.byref(c), wp, wn, st)
-    return (y, z) if preact else y
+        ws, wp, wn = _workspace(L, c, 0, index, workspace)
+        _call(L.laq_linear_forward, C.byref(c), wp, wn, raw)
+        return (y, z) if preact else y
+
+    return _on(index, stream, body)
 
 
 def linear_backward(dy, x, weight, z=None, activation="none", dx=True, dw=True, db=True, dw_dtype=None, workspace=None,
@@ -306,28 +327,32 @@ def linear_backward(dy, x, weight, z=None, activation="none", dx=True, dw=True, 
     is dy.
     """
     L = laq.load_library()
-    _rows(x, "x")
-    dev, dt = x.device, x.dtype
+    _check(x, "x")
+    index, dt = x.get_device(), x.dtype
     dw_dtype = dt if dw_dtype is None else dw_dtype
-    if dw and dw_dtype not in (dt, torch.float32):
+    if dw and dw_dtype is not dt and dw_dtype is not torch.float32:
         _refuse("dw_dtype must be %s or float32" % dt)
-    with _On(dev, stream) as st:
-        c = _layer_call(x, weight, activation, flags)
-        c.dy, c.ld_dy = _rows(dy, "dy", dev, dt, (c.M, c.N))
-        if activation != "none":
-            if z is None:
-                _refuse("the gradient of an activation needs z")
-            c.z, c.ld_z = _rows(z, "z", dev, dt, (c.M, c.N))
-        out = {}
+    c = _layer_call(x, weight, activation, flags, index)
+    c.dy, c.ld_dy, _, _ = _rows(dy, "dy", index, dt, (c.M, c.N))
+    if activation != "none":
+        if z is None:
+            _refuse("the gradient of an activation needs z")
+        c.z, c.ld_z, _, _ = _rows(z, "z", index, dt, (c.M, c.N))
+
+    def body(raw):
+        c.status = _status_word(index).data_ptr()
+        dev, res = x.device, {}
         if dx:
-            out["dx"] = torch.empty((c.M, c.K), dtype=dt, device=dev)
-            c.dx, c.ld_dx = out["dx"].data_ptr(), c.K
+            res["dx"] = t = torch.empty((c.M, c.K), dtype=dt, device=dev)
+            c.dx, c.ld_dx = t.data_ptr(), c.K
         if dw:
-            out["dw"] = torch.empty((c.N, c.K), dtype=dw_dtype, device=dev)
-            c.dw, c.ld_dw, c.dw_dtype = out["dw"].data_ptr(), c.K, DTYPES[dw_dtype]
+            res["dw"] = t = torch.empty((c.N, c.K), dtype=dw_dtype, device=dev)
+            c.dw, c.ld_dw, c.dw_dtype = t.data_ptr(), c.K, DTYPES[dw_dtype]
         if db:
-            out["db"] = torch.empty(c.N, dtype=torch.float32, device=dev)
-            c.db = out["db"].data_ptr()
-        ws, wp, wn = _workspace(L, c, 1, dev, workspace)
-        _call(L.laq_linear_backward, C.byref(c), wp, wn, st)
-    return out
+            res["db"] = t = torch.empty(c.N, dtype=torch.float32, device=dev)
+            c.db = t.data_ptr()
+        ws, wp, wn = _workspace(L, c, 1, index, workspace)
+        _call(L.laq_linear_backward, C.byref(c), wp, wn, raw)
+        return res
+
+    return _on(index, stream, body)
