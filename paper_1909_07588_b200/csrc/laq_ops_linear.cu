@@ -9,7 +9,9 @@
 // contiguous in memory) or "MN-major" (the free index is contiguous); TMA brings 64 values of r a stage in either form
 // with the 128-byte swizzle and the matrix descriptors tell the tensor core which one it is, so nothing is transposed in
 // memory.  Warp 0 loads, warp 1 issues the products, warps 2-9 run the epilogue of one tile from tensor memory while the
-// next one accumulates (two accumulators).  For few rows the roles of the operands are swapped (W's rows fill the 128
+// next one accumulates (two accumulators).  Large products run on pairs of SMs (cta_group::2, a 256-row tile): each SM of a
+// pair loads its own 128 rows of A and half of B's columns, 32 KB for the work that a lone SM loads 48 KB for, and what an
+// SM takes from L2 is what bounds the lone form (8192 x 4096 x 4096: 229 us alone).  For few rows the roles of the operands are swapped (W's rows fill the 128
 // lanes, the rows of X are the narrow side) and the summed axis is split over a thread-block cluster whose blocks join
 // their partial tiles through distributed shared memory in a fixed order.
 #include <cooperative_groups.h>
@@ -32,7 +34,8 @@ constexpr int kSMs = 148;
 constexpr int kGemmThreads = 320;         // loader, tensor-core warp, eight epilogue warps
 constexpr int kEpiWarps = 8;
 constexpr int kMaxStages = 12;
-constexpr int kMaxRing = 224 * 1024;      // bytes of the stage ring
+constexpr int kMaxRing = 192 * 1024;      // bytes of the stage ring
+constexpr int kStaging = kEpiWarps * 4096;   // ... and of the epilogue warps' pieces behind it
 constexpr int kMaxSplit = 8;
 constexpr uint32_t kStarvedLimit = 1u << 12;
 constexpr int kGroupTiles = 16;           // tile rows that are swept together, so that operands are found in L2
@@ -64,9 +67,41 @@ __device__ __forceinline__ uint64_t desc_mn_major(uint32_t addr) {
   d |= (uint64_t)2 << 61;
   return d;
 }
-__device__ __forceinline__ uint32_t instr_desc(int fmt, int a_mn, int b_mn, int nt) {
+__device__ __forceinline__ uint32_t instr_desc(int fmt, int a_mn, int b_mn, int nt, int rows) {
   return (1u << 4) | ((uint32_t)fmt << 7) | ((uint32_t)fmt << 10) | ((uint32_t)a_mn << 15) | ((uint32_t)b_mn << 16) |
-         ((uint32_t)(nt >> 3) << 17) | ((uint32_t)(kTileM >> 4) << 24);
+         ((uint32_t)(nt >> 3) << 17) | ((uint32_t)(rows >> 4) << 24);
+}
+
+// ---- the instructions of a pair of blocks -----------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t of_leader(uint32_t addr) {      // the same shared-memory address in the pair's first block
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+  return r;
+}
+// a tile into this block's memory whose bytes are counted by a barrier of either block of the pair
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+  asm volatile(
+      "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+      "l"(map), "r"(bar), "r"(x), "r"(y)
+      : "memory");
+}
+__device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n"
+      "}\n" ::"r"(d_tmem),
+      "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void commit_pair(uint32_t bar) {         // arrives at this barrier of both blocks
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+               "h"((uint16_t)3)
+               : "memory");
+}
+__device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
 // z * sigmoid(k z ...): gelu is the tanh form, 0.5 z (1 + tanh u) = z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
@@ -93,10 +128,11 @@ __device__ __forceinline__ float slope(float z, int act) {
   return 1.f;
 }
 
-// Eight values of one accumulator row.  TRANS = false: row i of D is a row of out, the eight are neighbours there;
-// TRANS = true: the eight are rows of out, i a column of it (neighbouring lanes write neighbouring columns).
+// Eight neighbours j0.. of row i of D.  TRANS = false: they are neighbours in a row of out; TRANS = true: i is a column of
+// out (neighbouring lanes hold neighbouring columns).  `vec`: all tensors of the call allow 16-byte accesses at multiples of
+// eight columns; `res8` is the residual's then, read beforehand.
 template <class T, bool TRANS>
-__device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float (&acc)[8], bool vec_ok) {
+__device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float (&acc)[8], bool vec, const uint4& res8) {
   if (i >= A.I || j0 >= A.J) return;
   const T* bias = reinterpret_cast<const T*>(A.bias);
   const T* res = reinterpret_cast<const T*>(A.residual);
@@ -117,9 +153,7 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
     }
     return;
   }
-  if (vec_ok && j0 + 8 <= A.J) {
-    float r[8];
-    if (res) Elem<T>::unpack(*reinterpret_cast<const uint4*>(res + (long long)i * A.ldr + j0), r);
+  if (vec && j0 + 8 <= A.J) {
     if (bias) {
       float b[8];
       Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(bias + j0)), b);
@@ -128,9 +162,12 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
     }
     if (zp) *reinterpret_cast<uint4*>(zp + (long long)i * A.ldz + j0) = Elem<T>::pack(acc);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      acc[e] = activate(acc[e], A.act);
-      if (res) acc[e] += r[e];
+    for (int e = 0; e < 8; ++e) acc[e] = activate(acc[e], A.act);
+    if (res) {
+      float r[8];
+      Elem<T>::unpack(res8, r);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] += r[e];
     }
     if (A.out_f32) {
       float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(A.out) + (long long)i * A.ldo + j0);
@@ -152,22 +189,39 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
     else reinterpret_cast<T*>(A.out)[(long long)i * A.ldo + j] = Elem<T>::from_float(y);
   }
 }
+template <class T>
+__device__ __forceinline__ uint4 residual8(const GemmArgs& A, int i, int j0, bool vec) {
+  uint4 r = make_uint4(0u, 0u, 0u, 0u);
+  if (vec && A.residual && i < A.I && j0 + 8 <= A.J) r = load16(reinterpret_cast<const T*>(A.residual) + (long long)i * A.ldr + j0);
+  return r;
+}
+
+// The fp32 values of a tile row by row in shared memory, 16-byte pieces permuted within a row so that a warp writes 32 rows
+// and reads along rows without bank conflicts.
+__device__ __forceinline__ int piece(int row, int p, int pieces) { return row * pieces + (p ^ (row & (pieces % 8 == 0 ? 7 : 3))); }
 
 __device__ __forceinline__ bool aligned16(const void* p, long long ld_bytes) {
   return (((uintptr_t)p | (uintptr_t)ld_bytes) & 15u) == 0;
 }
 
+__device__ __forceinline__ bool all_vectors(const GemmArgs& A) {
+  return aligned16(A.out, A.ldo * (A.out_f32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
+         (!A.residual || aligned16(A.residual, A.ldr * 2)) && (!A.bias || aligned16(A.bias, 0));
+}
+
 // Work item `w` -> tile origin.  Tile rows are swept in groups of kGroupTiles, column by column within a group.
+template <bool PAIR>
 __device__ __forceinline__ void tile_of(const GemmArgs& A, int w, int& i0, int& j0) {
-  const int group = kGroupTiles * A.tiles_j;
+  constexpr int kGroup = PAIR ? kGroupTiles / 2 : kGroupTiles;
+  const int group = kGroup * A.tiles_j;
   const int g = w / group, in = w - g * group;
-  const int first = g * kGroupTiles;
-  const int rows = min(kGroupTiles, A.tiles_i - first);
-  i0 = (first + in % rows) * kTileM;
+  const int first = g * kGroup;
+  const int rows = min(kGroup, A.tiles_i - first);
+  i0 = (first + in % rows) * (PAIR ? 2 * kTileM : kTileM);
   j0 = (in / rows) * A.nt;
 }
 
-template <class T, bool TRANS>
+template <class T, bool TRANS, bool PAIR>
 __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                                       const __grid_constant__ CUtensorMap tmB,
                                                                       const GemmArgs A) {
@@ -177,9 +231,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
   __shared__ int abort_sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t base = umma::smem_u32(gemm_smem_raw), smem0 = (base + 1023u) & ~1023u;
-  float* partial = reinterpret_cast<float*>(gemm_smem_raw + (smem0 - base));      // [nt][128], once the ring is idle
-  const int nt = A.nt, stages = A.stages, split = A.split;
-  const uint32_t a_bytes = kTileM * kBlockK * 2, st_bytes = a_bytes + (uint32_t)nt * kBlockK * 2;
+  uint4* ring4 = reinterpret_cast<uint4*>(gemm_smem_raw + (smem0 - base));        // a split tile, once the ring is idle
+  const int nt = A.nt, stages = A.stages, split = PAIR ? 1 : A.split;
+  const int b_rows = PAIR ? nt / 2 : nt;           // columns of the tile whose part of B this block loads
+  const uint32_t a_bytes = kTileM * kBlockK * 2, st_bytes = a_bytes + (uint32_t)b_rows * kBlockK * 2;
+  const int half = PAIR ? (int)(blockIdx.x & 1u) : 0;
   const uint32_t full0 = umma::smem_u32(&bars[0]), empty0 = umma::smem_u32(&bars[kMaxStages]);
   const uint32_t acc_full0 = umma::smem_u32(&bars[2 * kMaxStages]), acc_empty0 = acc_full0 + 16, drain = acc_full0 + 32;
   // Two accumulators of at most 256 columns; one for a split tile, which has no successor.  Two blocks of a cluster on one
@@ -192,26 +248,35 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
     }
     for (int b = 0; b < 2; ++b) {
       umma::mbar_init(acc_full0 + 8 * b, 1);
-      umma::mbar_init(acc_empty0 + 8 * b, kEpiWarps);
+      umma::mbar_init(acc_empty0 + 8 * b, PAIR ? 2 * kEpiWarps : kEpiWarps);
     }
     umma::mbar_init(drain, 1);
     abort_sh = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(umma::smem_u32(&tmem_base_sh)),
-                 "r"(held_cols)
-                 : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(umma::smem_u32(&tmem_base_sh)),
+                   "r"(held_cols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(umma::smem_u32(&tmem_base_sh)),
+                   "r"(held_cols)
+                   : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  __syncthreads();
+  if (PAIR) cg::this_cluster().sync();             // both blocks' barriers are there before either signals the other's
+  else __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = tmem_base_sh;
 
   const int tiles = A.tiles_i * A.tiles_j;
   const int rank = split > 1 ? (int)(blockIdx.x % (unsigned)split) : 0;
-  const int first = (int)(blockIdx.x / (unsigned)split), step = (int)(gridDim.x / (unsigned)split);
+  const unsigned per_tile = PAIR ? 2u : (unsigned)split;
+  const int first = (int)(blockIdx.x / per_tile), step = (int)(gridDim.x / per_tile);
   const int kb_per = (A.nkb + split - 1) / split;
   const int kb0 = min(rank * kb_per, A.nkb), nkb = min(kb0 + kb_per, A.nkb) - kb0;    // > 0: the plan leaves no block idle
   const bool starved = A.starve && blockIdx.x == 0;
@@ -224,13 +289,33 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       bool ok = !starved;
       for (int w = first; w < tiles && ok; w += step) {
         int i0, j0;
-        tile_of(A, w, i0, j0);
+        tile_of<PAIR>(A, w, i0, j0);
+        i0 += half * kTileM;
+        j0 += half * b_rows;
         for (int kb = 0; kb < nkb; ++kb, ++n) {
           const int s = n % stages;
           ok = umma::mbar_wait_abortable(empty0 + 8 * s, ((uint32_t)(n / stages) & 1u) ^ 1u, limit, abort_flag, A.status, 1u);
           if (!ok) break;
-          const uint32_t bar = full0 + 8 * s, sa = smem0 + s * st_bytes, sb = sa + a_bytes;
+          const uint32_t sa = smem0 + s * st_bytes, sb = sa + a_bytes;
           const int r = (kb0 + kb) * kBlockK;
+          if (PAIR) {
+            // the pair's first block counts the bytes of both; its phase cannot end before its own arrival here
+            if (half == 0) umma::mbar_expect_tx(full0 + 8 * s, 2 * st_bytes);
+            const uint32_t bar = of_leader(full0 + 8 * s);
+            if (A.a_mn) {
+              tma_load_2d_pair(sa, &tmA, bar, i0, r);
+              tma_load_2d_pair(sa + 8192, &tmA, bar, i0 + 64, r);
+            } else {
+              tma_load_2d_pair(sa, &tmA, bar, r, i0);
+            }
+            if (A.b_mn) {
+              for (int b = 0; b < b_rows; b += 64) tma_load_2d_pair(sb + b * 128, &tmB, bar, j0 + b, r);
+            } else {
+              tma_load_2d_pair(sb, &tmB, bar, r, j0);
+            }
+            continue;
+          }
+          const uint32_t bar = full0 + 8 * s;
           umma::mbar_expect_tx(bar, st_bytes);
           if (A.a_mn) {
             umma::tma_load_2d(sa, &tmA, bar, i0, r);
@@ -245,14 +330,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           }
         }
       }
-      if (!ok)                          // given up: the copies in flight still land in this block's memory
+      if (!ok && PAIR) {                // given up: the copies in flight still land in this block's memory, and are counted
+        for (int i = 0; i < 2000; ++i) __nanosleep(1000);        // by the other block: microseconds are enough, 2 ms ample
+      } else if (!ok) {
         for (int m = n > stages ? n - stages : 0; m < n; ++m)
           for (uint32_t it = 0; it < umma::kWaitLimit && !umma::mbar_try_wait(full0 + 8 * (m % stages), (uint32_t)(m / stages) & 1u); ++it) {
           }
+      }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      const uint32_t idesc = instr_desc(A.fmt, A.a_mn, A.b_mn, nt);
+    if (lane == 0 && half == 0) {       // the pair's first block issues the products of both
+      const uint32_t idesc = instr_desc(A.fmt, A.a_mn, A.b_mn, nt, PAIR ? 2 * kTileM : kTileM);
       // 16 values of r: 32 bytes on within the rows of a K-major tile, two groups of 8 rows (2048 bytes) on in an MN-major one
       const uint32_t step_a = A.a_mn ? 128u : 2u, step_b = A.b_mn ? 128u : 2u;
       int n = 0, it = 0;
@@ -271,14 +359,21 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           const uint32_t sa = smem0 + s * st_bytes, sb = sa + a_bytes;
           const uint64_t da = A.a_mn ? desc_mn_major(sa) : desc_k_major(sa), db = A.b_mn ? desc_mn_major(sb) : desc_k_major(sb);
 #pragma unroll
-          for (int kk = 0; kk < kBlockK / 16; ++kk)
-            umma::mma_bf16_ss(d, da + kk * step_a, db + kk * step_b, idesc, (kb | kk) != 0 ? 1u : 0u);
-          umma::mma_commit(empty0 + 8 * s);
+          for (int kk = 0; kk < kBlockK / 16; ++kk) {
+            if (PAIR) mma_pair(d, da + kk * step_a, db + kk * step_b, idesc, (kb | kk) != 0 ? 1u : 0u);
+            else umma::mma_bf16_ss(d, da + kk * step_a, db + kk * step_b, idesc, (kb | kk) != 0 ? 1u : 0u);
+          }
+          if (PAIR) commit_pair(empty0 + 8 * s);
+          else umma::mma_commit(empty0 + 8 * s);
         }
-        if (ok) umma::mma_commit(acc_full0 + 8 * b);
+        if (ok) {
+          if (PAIR) commit_pair(acc_full0 + 8 * b);
+          else umma::mma_commit(acc_full0 + 8 * b);
+        }
       }
       if (!ok) {                        // products under way still read the ring and write tensor memory
-        umma::mma_commit(drain);
+        if (PAIR) commit_pair(drain);
+        else umma::mma_commit(drain);
         for (uint32_t i = 0; i < umma::kWaitLimit && !umma::mbar_try_wait(drain, 0u); ++i) {
         }
       }
@@ -287,8 +382,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
   } else {
     const int q = warp & 3, set = (warp - 2) >> 2;
     const int row = q * 32 + lane;
-    const bool vec_ok = aligned16(A.out, A.ldo * (A.out_f32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
-                        (!A.residual || aligned16(A.residual, A.ldr * 2)) && (!A.bias || aligned16(A.bias, 0));
+    const bool vec = all_vectors(A);
+    uint4* stage4 = ring4 + (size_t)stages * st_bytes / 16 + (warp - 2) * 256;         // 4 KB of this warp
     int it = 0;
     for (int w = first; w < tiles; w += step, ++it) {
       const int b = it & 1;
@@ -297,25 +392,57 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       int i0, j0;
-      tile_of(A, w, i0, j0);
+      tile_of<PAIR>(A, w, i0, j0);
+      i0 += half * kTileM;
       const uint32_t t0 = tmem_base + (uint32_t)b * acc_cols + ((uint32_t)(q * 32) << 16);
-      for (int c0 = 16 * set; c0 < nt; c0 += 32) {
-        uint32_t v[16];
-        umma::tmem_load_16(t0 + (uint32_t)c0, v);
-        float x[2][8];
+      if (split > 1) {
+        for (int c0 = 16 * set; c0 < nt; c0 += 32) {
+          uint32_t v[16];
+          umma::tmem_load_16(t0 + (uint32_t)c0, v);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e >> 3][e & 7] = __uint_as_float(v[e]);
-        if (split > 1) {
+          for (int e = 0; e < 16; e += 4)
+            ring4[piece(row, (c0 + e) / 4, nt / 4)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        }
+      } else if (TRANS) {
+        for (int c0 = 16 * set; c0 < nt; c0 += 32) {
+          uint32_t v[16];
+          umma::tmem_load_16(t0 + (uint32_t)c0, v);
+          float x[2][8];
 #pragma unroll
-          for (int e = 0; e < 16; ++e) partial[(c0 + e) * kTileM + row] = x[e >> 3][e & 7];
-        } else {
-          finish8<T, TRANS>(A, i0 + row, j0 + c0, x[0], vec_ok);
-          finish8<T, TRANS>(A, i0 + row, j0 + c0 + 8, x[1], vec_ok);
+          for (int e = 0; e < 16; ++e) x[e >> 3][e & 7] = __uint_as_float(v[e]);
+          finish8<T, true>(A, i0 + row, j0 + c0, x[0], vec, make_uint4(0u, 0u, 0u, 0u));
+          finish8<T, true>(A, i0 + row, j0 + c0 + 8, x[1], vec, make_uint4(0u, 0u, 0u, 0u));
+        }
+      } else {
+        // 32 x 32 pieces: a lane takes its row from tensor memory and hands it on; four lanes then share a row, so that
+        // loads and stores of the layer's tensors are whole 64-byte stretches
+        for (int c0 = 32 * set; c0 < nt; c0 += 64) {
+          uint4 res[4];
+          const int jl = j0 + c0 + 8 * (lane & 3);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) res[k] = residual8<T>(A, i0 + q * 32 + 8 * k + (lane >> 2), jl, vec);
+          uint32_t v[32];
+          umma::tmem_load_32(t0 + (uint32_t)c0, v);          // past nt only where nt is no multiple of 32: not used below
+          __syncwarp();
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = 8 * k + (lane >> 2);
+            const uint4 lo = stage4[piece(r, 2 * (lane & 3), 8)], hi = stage4[piece(r, 2 * (lane & 3) + 1, 8)];
+            float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                          __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+            if (c0 + 8 * (lane & 3) < nt) finish8<T, false>(A, i0 + q * 32 + r, jl, x, vec, res[k]);
+          }
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
-      if (lane == 0) umma::mbar_arrive(acc_empty0 + 8 * b);
+      if (lane == 0) {
+        if (PAIR) arrive_at(of_leader(acc_empty0 + 8 * b));
+        else umma::mbar_arrive(acc_empty0 + 8 * b);
+      }
     }
   }
   if (split > 1) {          // one tile per cluster: its blocks share the columns of the join
@@ -323,33 +450,46 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
     __syncwarp();
     cluster.sync();
     if (warp >= 2) {
-      const int q = warp & 3, set = (warp - 2) >> 2, row = q * 32 + lane;
       int gone = 0;
       for (int r = 0; r < split; ++r) gone |= *cluster.map_shared_rank(&abort_sh, r);
-      const bool vec_ok = aligned16(A.out, A.ldo * (A.out_f32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
-                          (!A.residual || aligned16(A.residual, A.ldr * 2)) && (!A.bias || aligned16(A.bias, 0));
+      const bool vec = all_vectors(A);
       int i0, j0;
-      tile_of(A, first, i0, j0);
-      for (int g = rank * 2 + set; g < nt / 8 && !gone; g += 2 * split) {
-        float x[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = 0.f;
+      tile_of<false>(A, first, i0, j0);
+      // eight columns of a row at a time; lanes run along a row, or down the rows where out is transposed
+      const int groups = nt / 8, tid = (int)threadIdx.x - 64;
+      for (int item = rank * 256 + tid; item < kTileM * groups && !gone; item += 256 * split) {
+        const int r0 = TRANS ? item % kTileM : item / groups, g = TRANS ? item / kTileM : item % groups;
+        const uint4 res = TRANS ? make_uint4(0u, 0u, 0u, 0u) : residual8<T>(A, i0 + r0, j0 + g * 8, vec);
+        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         for (int r = 0; r < split; ++r) {
-          const float* p = cluster.map_shared_rank(partial, r) + (size_t)g * 8 * kTileM + row;
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] += p[e * kTileM];
+          const uint4* p = cluster.map_shared_rank(ring4, r);
+          const uint4 lo = p[piece(r0, 2 * g, nt / 4)], hi = p[piece(r0, 2 * g + 1, nt / 4)];
+          x[0] += __uint_as_float(lo.x);
+          x[1] += __uint_as_float(lo.y);
+          x[2] += __uint_as_float(lo.z);
+          x[3] += __uint_as_float(lo.w);
+          x[4] += __uint_as_float(hi.x);
+          x[5] += __uint_as_float(hi.y);
+          x[6] += __uint_as_float(hi.z);
+          x[7] += __uint_as_float(hi.w);
         }
-        finish8<T, TRANS>(A, i0 + row, j0 + g * 8, x, vec_ok);
+        finish8<T, TRANS>(A, i0 + r0, j0 + g * 8, x, vec, res);
       }
     }
     __syncwarp();
     cluster.sync();
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  __syncthreads();
+  if (PAIR) {
+    __syncwarp();
+    cg::this_cluster().sync();                     // neither block's memory is used by the other any more
+  } else {
+    __syncthreads();
+  }
   if (warp == 1) {
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(held_cols) : "memory");
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(held_cols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(held_cols) : "memory");
   }
 }
 
@@ -359,7 +499,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
 constexpr int kDzCols = 256, kDzThreads = 256;
 
 template <class T>
-__global__ void __launch_bounds__(kDzThreads) linear_dz_kernel(const T* dy, long long lddy, const T* z, long long ldz, T* dz,
+__global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, long long lddy, const T* z, long long ldz, T* dz,
                                                                long long lddz, float* part, long long M, int N, int act,
                                                                int rows_per, int vec_ok) {
   __shared__ float sh[8][kDzCols];
@@ -459,7 +599,7 @@ struct Operand {                // a 2-byte matrix [rows][cols]
 };
 
 struct Plan {
-  int swap, nt, split, stages;
+  int swap, nt, split, stages, pair;
   double cost;
 };
 
@@ -467,7 +607,7 @@ struct Plan {
 // (two cycles per column of the tile) and of its bytes at what an SM takes from L2, a tile a fixed start and its epilogue.
 // `swappable`: the epilogue may write the transposed tile (only worth it for few columns).
 Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable) {
-  Plan best{0, 128, 1, 4, 1e300};
+  Plan best{0, 128, 1, 4, 0, 1e300};
   const long long nkb = (R + kBlockK - 1) / kBlockK;
   for (int swap = 0; swap <= (swappable ? 1 : 0); ++swap) {
     const long long i = swap ? J : I, j = swap ? I : J;
@@ -479,7 +619,7 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
       for (int split = 1; split <= kMaxSplit; split *= 2) {
         if (split > 1 && (nkb + split - 1) / split * (split - 1) >= nkb) continue;     // a block would have nothing to do
         const size_t stage = (size_t)(kTileM + nt) * kBlockK * 2;
-        const size_t room = split > 1 || nt <= 32 ? 110 * 1024 : 220 * 1024;
+        const size_t room = split > 1 || nt <= 32 ? 78 * 1024 : kMaxRing;
         int stages = (int)(room / stage);
         if (stages > kMaxStages) stages = kMaxStages;
         if (split > 1) {
@@ -487,7 +627,7 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
           while ((size_t)stages * stage < need || stages < 3) ++stages;
         }
         if (stages * stage > (size_t)kMaxRing) continue;
-        const int per_sm = stages * stage > 112 * 1024 ? 1 : 2;
+        const int per_sm = stages * stage > 80 * 1024 ? 1 : 2;
         const long long tiles = ((i + kTileM - 1) / kTileM) * ((j + nt - 1) / nt);
         const long long kb = (nkb + split - 1) / split;
         const double mma = 2.0 * nt, load = stage / 48.0;
@@ -503,7 +643,19 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
           const double waves = (double)((tiles * split + kSMs - 1) / kSMs);
           cost = 4500 + waves * (kb * per_stage + epi / split + 8.0 * nt);
         }
-        if (cost < best.cost) best = Plan{swap, nt, split, stages, cost};
+        if (cost < best.cost) best = Plan{swap, nt, split, stages, 0, cost};
+      }
+      // pairs of SMs: 256 rows of D
+      if (!swap && nt % 128 == 0 && i > kTileM) {
+        const size_t stage = (size_t)(kTileM + nt / 2) * kBlockK * 2;
+        int stages = (int)(kMaxRing / stage);
+        if (stages > kMaxStages) stages = kMaxStages;
+        const long long tiles = ((i + 2 * kTileM - 1) / (2 * kTileM)) * ((j + nt - 1) / nt);
+        const long long waves = (tiles + kSMs / 2 - 1) / (kSMs / 2);
+        const double mma = 2.0 * nt, load = stage / 48.0, epi = 16.0 * nt;
+        const double main = nkb * (mma > load ? mma : load);
+        const double cost = 3500 + waves * (main > epi ? main : epi) + epi;
+        if (cost < best.cost) best = Plan{0, nt, 1, stages, 1, cost};
       }
     }
   }
@@ -515,17 +667,18 @@ struct Err {
   size_t len;
 };
 
-template <class T, bool TRANS>
+template <class T, bool TRANS, bool PAIR>
 laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, cudaStream_t st) {
-  auto kernel = linear_gemm_kernel<T, TRANS>;
-  const size_t smem = (size_t)A.stages * (kTileM + A.nt) * kBlockK * 2 + 1024;
+  auto kernel = linear_gemm_kernel<T, TRANS, PAIR>;
+  const size_t smem = (size_t)A.stages * (kTileM + (PAIR ? A.nt / 2 : A.nt)) * kBlockK * 2 + kStaging + 1024;
+  const int per_tile = PAIR ? 2 : A.split;
   // the kernel's shared memory limit is raised once per device
   static std::atomic<uint64_t> raised{0};
   int dev = 0;
   cudaGetDevice(&dev);
   const uint64_t bit = 1ull << (dev & 63);
   if (dev >= 64 || !(raised.load(std::memory_order_acquire) & bit)) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing + 1024) != cudaSuccess) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing + kStaging + 1024) != cudaSuccess) {
       cudaGetLastError();
       return fail(e.buf, e.len, LAQ_ECUDA, "shared memory of the product kernel was refused");
     }
@@ -533,16 +686,16 @@ laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& m
   }
   const long long tiles = (long long)A.tiles_i * A.tiles_j;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(A.split > 1 ? tiles * A.split : tiles < kSMs ? tiles : kSMs));
+  cfg.gridDim = dim3((unsigned)(PAIR ? 2 * (tiles < kSMs / 2 ? tiles : kSMs / 2) : A.split > 1 ? tiles * A.split : tiles < kSMs ? tiles : kSMs));
   cfg.blockDim = dim3(kGemmThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[1];
   at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)A.split;
+  at[0].val.clusterDim.x = (unsigned)per_tile;
   at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
   cfg.attrs = at;
-  cfg.numAttrs = A.split > 1 ? 1 : 0;
+  cfg.numAttrs = per_tile > 1 ? 1 : 0;
   const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, ma, mb, A);
   if (rc != cudaSuccess) {
     cudaGetLastError();
@@ -571,7 +724,7 @@ laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const O
   const bool amn = pl.swap ? b_mn : a_mn, bmn = pl.swap ? a_mn : b_mn;
   CUtensorMap ma, mb;
   if (!umma::make_map_bf16_2d(&ma, A0.p, A0.rows, A0.cols, A0.ld * 2, amn ? 64 : kTileM) ||
-      !umma::make_map_bf16_2d(&mb, B0.p, B0.rows, B0.cols, B0.ld * 2, bmn ? 64 : pl.nt))
+      !umma::make_map_bf16_2d(&mb, B0.p, B0.rows, B0.cols, B0.ld * 2, bmn ? 64 : pl.pair ? pl.nt / 2 : pl.nt))
     return fail(e.buf, e.len, LAQ_ECUDA, "a tensor map was refused");
   GemmArgs A = {};
   A.I = (int)(pl.swap ? J : I);
@@ -580,7 +733,8 @@ laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const O
   A.nt = pl.nt;
   A.stages = pl.stages;
   A.split = pl.split;
-  A.tiles_i = (A.I + kTileM - 1) / kTileM;
+  const int tile_rows = pl.pair ? 2 * kTileM : kTileM;
+  A.tiles_i = (A.I + tile_rows - 1) / tile_rows;
   A.tiles_j = (A.J + pl.nt - 1) / pl.nt;
   A.a_mn = amn;
   A.b_mn = bmn;
@@ -597,8 +751,12 @@ laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const O
   A.residual = ep.residual;
   A.status = status;
   if (dtype == LAQ_BF16)
-    return pl.swap ? launch_gemm<__nv_bfloat16, true>(e, ma, mb, A, st) : launch_gemm<__nv_bfloat16, false>(e, ma, mb, A, st);
-  return pl.swap ? launch_gemm<__half, true>(e, ma, mb, A, st) : launch_gemm<__half, false>(e, ma, mb, A, st);
+    return pl.pair   ? launch_gemm<__nv_bfloat16, false, true>(e, ma, mb, A, st)
+           : pl.swap ? launch_gemm<__nv_bfloat16, true, false>(e, ma, mb, A, st)
+                     : launch_gemm<__nv_bfloat16, false, false>(e, ma, mb, A, st);
+  return pl.pair   ? launch_gemm<__half, false, true>(e, ma, mb, A, st)
+         : pl.swap ? launch_gemm<__half, true, false>(e, ma, mb, A, st)
+                   : launch_gemm<__half, false, false>(e, ma, mb, A, st);
 }
 
 // Copies an operand that a tensor map cannot describe to `ws` (advanced past it).
