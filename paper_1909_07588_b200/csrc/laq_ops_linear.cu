@@ -119,14 +119,25 @@ __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
-// z * sigmoid(k z ...): gelu is the tanh form, 0.5 z (1 + tanh u) = z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
+// gelu is the tanh form: 0.5 z (1 + tanh u) = z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
 constexpr float kGeluC = 0.7978845608028654f, kGeluA = 0.044715f;
-__device__ __forceinline__ float sigmoid(float x) { return __fdividef(1.f, 1.f + __expf(-x)); }
-__device__ __forceinline__ float activate(float z, int act) {
-  if (act == LAQ_ACT_RELU) return z > 0.f ? z : (z == z ? 0.f : z);
-  if (act == LAQ_ACT_SILU) return z * sigmoid(z);
-  if (act == LAQ_ACT_GELU) return z * sigmoid(2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
-  return z;
+__device__ __forceinline__ float sigmoid(float x) {       // 0 and 1 for far x: 2^128 is +inf and its reciprocal 0
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2(-1.4426950408889634f * x)));
+  return r;
+}
+template <int N>
+__device__ __forceinline__ void activate(float (&z)[N], int act) {
+  if (act == LAQ_ACT_RELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] = max_nan(z[e], 0.f);
+  } else if (act == LAQ_ACT_SILU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] *= sigmoid(z[e]);
+  } else if (act == LAQ_ACT_GELU) {
+#pragma unroll
+    for (int e = 0; e < N; ++e) z[e] *= sigmoid(2.f * kGeluC * fmaf(kGeluA * z[e] * z[e], z[e], z[e]));
+  }
 }
 __device__ __forceinline__ float slope(float z, int act) {
   if (act == LAQ_ACT_RELU) return z > 0.f ? 1.f : (z == z ? 0.f : z);
@@ -159,10 +170,14 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
     for (int e = 0; e < 8; ++e) r[e] = res && j0 + e < A.J ? Elem<T>::to_float(res[(long long)(j0 + e) * A.ldr + i]) : 0.f;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
+      acc[e] += b;
+      if (zp && j0 + e < A.J) zp[(long long)(j0 + e) * A.ldz + i] = Elem<T>::from_float(acc[e]);
+    }
+    activate(acc, A.act);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
       if (j0 + e >= A.J) break;
-      const float z = acc[e] + b;
-      if (zp) zp[(long long)(j0 + e) * A.ldz + i] = Elem<T>::from_float(z);
-      const float y = activate(z, A.act) + r[e];
+      const float y = acc[e] + r[e];
       if (A.out_f32) reinterpret_cast<float*>(A.out)[(long long)(j0 + e) * A.ldo + i] = y;
       else reinterpret_cast<T*>(A.out)[(long long)(j0 + e) * A.ldo + i] = Elem<T>::from_float(y);
     }
@@ -176,8 +191,7 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
       for (int e = 0; e < 8; ++e) acc[e] += b[e];
     }
     if (zp) *reinterpret_cast<uint4*>(zp + (long long)i * A.ldz + j0) = Elem<T>::pack(acc);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] = activate(acc[e], A.act);
+    activate(acc, A.act);
     if (res) {
       float r[8];
       Elem<T>::unpack(res8, r);
@@ -197,9 +211,15 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
   for (int e = 0; e < 8; ++e) {
     const int j = j0 + e;
     if (j >= A.J) break;
-    const float z = acc[e] + (bias ? Elem<T>::to_float(bias[j]) : 0.f);
-    if (zp) zp[(long long)i * A.ldz + j] = Elem<T>::from_float(z);
-    const float y = activate(z, A.act) + (res ? Elem<T>::to_float(res[(long long)i * A.ldr + j]) : 0.f);
+    acc[e] += bias ? Elem<T>::to_float(bias[j]) : 0.f;
+    if (zp) zp[(long long)i * A.ldz + j] = Elem<T>::from_float(acc[e]);
+  }
+  activate(acc, A.act);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int j = j0 + e;
+    if (j >= A.J) break;
+    const float y = acc[e] + (res ? Elem<T>::to_float(res[(long long)i * A.ldr + j]) : 0.f);
     if (A.out_f32) reinterpret_cast<float*>(A.out)[(long long)i * A.ldo + j] = y;
     else reinterpret_cast<T*>(A.out)[(long long)i * A.ldo + j] = Elem<T>::from_float(y);
   }
@@ -402,13 +422,25 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
     int it = 0;
     for (int w = first; w < tiles; w += step, ++it) {
       const int b = it & 1;
+      int i0, j0;
+      tile_of<PAIR>(A, w, i0, j0);
+      i0 += half * kTileM;
+      // a tile that lies wholly inside D and allows vectors throughout goes without any checks; its residual is read one
+      // piece ahead, the first one's before the products are done
+      const bool whole = !TRANS && split == 1 && vec && i0 + kTileM <= A.I && j0 + nt <= A.J && nt % 32 == 0;
+      const long long row0 = i0 + q * 32 + (lane >> 2);
+      const int col0 = j0 + 8 * (lane & 3);
+      uint4 res[4];
+      auto ahead = [&](int c0) {
+        const T* p = reinterpret_cast<const T*>(A.residual) + row0 * A.ldr + col0 + c0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) res[k] = load16(p + 8 * k * A.ldr);
+      };
+      if (whole && A.residual && 32 * set < nt) ahead(32 * set);
       const bool ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(it >> 1) & 1u, limit,
                                                                         abort_flag, A.status, 8u));
       if (!ok) break;
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      int i0, j0;
-      tile_of<PAIR>(A, w, i0, j0);
-      i0 += half * kTileM;
       const uint32_t t0 = tmem_base + (uint32_t)b * acc_cols + ((uint32_t)(q * 32) << 16);
       if (split > 1) {
         for (int c0 = 16 * set; c0 < nt; c0 += 32) {
@@ -431,8 +463,48 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       } else {
         // 32 x 32 pieces: a lane takes its row from tensor memory and hands it on; four lanes then share a row, so that
         // loads and stores of the layer's tensors are whole 64-byte stretches
-        for (int c0 = 32 * set; c0 < nt; c0 += 64) {
-          uint4 res[4];
+        for (int c0 = 32 * set; c0 < nt && whole; c0 += 64) {
+          const int j = col0 + c0;
+          uint4 now[4];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) now[k] = res[k];
+          if (A.residual && c0 + 64 < nt) ahead(c0 + 64);
+          float bias[8] = {};
+          if (A.bias) Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + j)), bias);
+          uint32_t v[32];
+          umma::tmem_load_32(t0 + (uint32_t)c0, v);
+          __syncwarp();
+#pragma unroll
+          for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+          __syncwarp();
+          T* zp = A.z ? reinterpret_cast<T*>(A.z) + row0 * A.ldz + j : nullptr;
+          T* yp = reinterpret_cast<T*>(A.out) + row0 * A.ldo + j;
+          float* fp = reinterpret_cast<float*>(A.out) + row0 * A.ldo + j;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const int r = 8 * k + (lane >> 2);
+            const uint4 lo = stage4[piece(r, 2 * (lane & 3), 8)], hi = stage4[piece(r, 2 * (lane & 3) + 1, 8)];
+            float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                          __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += bias[e];
+            if (zp) *reinterpret_cast<uint4*>(zp + 8 * k * A.ldz) = Elem<T>::pack(x);
+            activate(x, A.act);
+            if (A.residual) {
+              float y[8];
+              Elem<T>::unpack(now[k], y);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] += y[e];
+            }
+            if (A.out_f32) {
+              *reinterpret_cast<float4*>(fp + 8 * k * A.ldo) = make_float4(x[0], x[1], x[2], x[3]);
+              *reinterpret_cast<float4*>(fp + 8 * k * A.ldo + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            } else {
+              *reinterpret_cast<uint4*>(yp + 8 * k * A.ldo) = Elem<T>::pack(x);
+            }
+          }
+        }
+        for (int c0 = 32 * set; c0 < nt && !whole; c0 += 64) {
           const int jl = j0 + c0 + 8 * (lane & 3);
 #pragma unroll
           for (int k = 0; k < 4; ++k) res[k] = residual8<T>(A, i0 + q * 32 + 8 * k + (lane >> 2), jl, vec);
@@ -563,20 +635,20 @@ __global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, l
   }
 }
 
-__global__ void __launch_bounds__(256) linear_db_kernel(const float* part, int runs, int N, float* db) {
-  __shared__ float sh[8][33];
+__global__ void __launch_bounds__(1024) linear_db_kernel(const float* part, int runs, int N, float* db) {
+  __shared__ float sh[32][33];
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
   float s = 0.f;
-  if (c < N)
-    for (int r = ty; r < runs; r += 8) s += part[(long long)r * N + c];
+  if (c < N) {
+#pragma unroll 4
+    for (int r = ty; r < runs; r += 32) s += part[(long long)r * N + c];
+  }
   sh[ty][tx] = s;
   __syncthreads();
-  if (ty == 0 && c < N) {
-    float t = 0.f;
+  float t = sh[tx][ty];                  // warp ty adds up column ty
 #pragma unroll
-    for (int y = 0; y < 8; ++y) t += sh[y][tx];
-    db[c] = t;
-  }
+  for (int o = 16; o > 0; o >>= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+  if (tx == 0 && blockIdx.x * 32 + ty < N) db[blockIdx.x * 32 + ty] = t;
 }
 
 // Rows that a tensor map cannot describe (an address or a row pitch that is no multiple of 16 bytes) are copied once
@@ -645,9 +717,9 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
         const int per_sm = stages * stage > 80 * 1024 ? 1 : 2;
         const long long tiles = ((i + kTileM - 1) / kTileM) * ((j + nt - 1) / nt);
         const long long kb = (nkb + split - 1) / split;
-        const double mma = 2.0 * nt, load = stage / 48.0;
+        const double mma = 2.2 * nt, load = stage / 44.0;
         const double per_stage = mma > load ? mma : load;
-        const double epi = 16.0 * nt * (swap ? 2 : 1);
+        const double epi = 600 + (swap ? 160.0 : 32.0) * nt;       // transposed stores go element by element
         double cost;
         if (split == 1) {
           const long long waves = (tiles + kSMs - 1) / kSMs;
@@ -667,7 +739,7 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
         if (stages > kMaxStages) stages = kMaxStages;
         const long long tiles = ((i + 2 * kTileM - 1) / (2 * kTileM)) * ((j + nt - 1) / nt);
         const long long waves = (tiles + kSMs / 2 - 1) / (kSMs / 2);
-        const double mma = 2.0 * nt, load = stage / 48.0, epi = 16.0 * nt;
+        const double mma = 2.2 * nt, load = stage / 44.0, epi = 600 + 32.0 * nt;
         const double main = nkb * (mma > load ? mma : load);
         const double cost = 3500 + waves * (main > epi ? main : epi) + epi;
         if (cost < best.cost) best = Plan{0, nt, 1, stages, 1, cost};
@@ -938,7 +1010,7 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
                                                             pad8(c->N), part, c->M, N, c->activation, per, vec_ok);
     if (cudaGetLastError() != cudaSuccess) return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
     if (c->db) {
-      linear_db_kernel<<<(unsigned)((c->N + 31) / 32), 256, 0, st>>>(part, runs, N, c->db);
+      linear_db_kernel<<<(unsigned)((c->N + 31) / 32), 1024, 0, st>>>(part, runs, N, c->db);
       if (cudaGetLastError() != cudaSuccess) return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
     }
     if (need.own_dz) {
