@@ -205,9 +205,9 @@ __device__ __forceinline__ Stat warp_join(Stat a, float c) {
 
 // What a row needs of its statistics.  unit = 1 / (tau c): from powers of two back to natural logarithms, with c as it is.
 struct RowSum {
-  float ref, log2s, lse, entropy, c, unit;
+  float ref, log2s, lse, entropy, c, unit, inv_tau;
   bool empty;       // nothing above -inf
-  __device__ __forceinline__ RowSum(const Stat& a, float c_, float unit_, float inv_tau) : c(c_), unit(unit_) {
+  __device__ __forceinline__ RowSum(const Stat& a, float c_, float unit_, float inv_tau_) : c(c_), unit(unit_), inv_tau(inv_tau_) {
     empty = a.s == 0.f;
     ref = a.ref;
     log2s = log2f(a.s);
@@ -216,6 +216,7 @@ struct RowSum {
   }
   __device__ __forceinline__ float logp(float x) const {
     if (x == -INFINITY) return log2s != log2s ? log2s : x;
+    if (near_ref(ref) && !near_ref(x)) return fmaf(x, inv_tau, -lse);     // a mask at the type's lowest value: x c overflows
     return (scaled(x, ref, c) - log2s) * unit;
   }
 };
