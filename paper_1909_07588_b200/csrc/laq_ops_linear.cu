@@ -139,19 +139,14 @@ __device__ __forceinline__ void activate(float (&z)[N], int act) {
     for (int e = 0; e < N; ++e) z[e] *= sigmoid(2.f * kGeluC * fmaf(kGeluA * z[e] * z[e], z[e], z[e]));
   }
 }
-__device__ __forceinline__ float slope(float z, int act) {
-  if (act == LAQ_ACT_RELU) return z > 0.f ? 1.f : (z == z ? 0.f : z);
-  if (act == LAQ_ACT_SILU) {
-    const float s = sigmoid(z);
-    return s * fmaf(z, 1.f - s, 1.f);
-  }
-  if (act == LAQ_ACT_GELU) {
-    const float s = sigmoid(2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
-    // |z| > 20: s is 0 or 1 and s (1 - s) z^3 is zero long before z^3 overflows
-    const float zz = fminf(z * z, 400.f), zc = fminf(fmaxf(z, -20.f), 20.f);
-    return fmaf(zc * s * (1.f - s), 2.f * kGeluC * fmaf(3.f * kGeluA, zz, 1.f), s);
-  }
-  return 1.f;
+__device__ __forceinline__ float slope_silu(float z) {
+  const float s = sigmoid(z);
+  return s * fmaf(z, 1.f - s, 1.f);
+}
+__device__ __forceinline__ float slope_gelu(float z) {
+  const float s = sigmoid(2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
+  // s (1 - s) is 0 long before z^2 passes 400, so that the product stays finite however far z is
+  return fmaf(z * s * (1.f - s), fmaf(6.f * kGeluC * kGeluA, fminf(z * z, 400.f), 2.f * kGeluC), s);
 }
 
 // Eight neighbours j0.. of row i of D.  TRANS = false: they are neighbours in a row of out; TRANS = true: i is a column of
@@ -581,45 +576,65 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
 }
 
 // ---- dZ and the column sums ---------------------------------------------------------------------------------------------
-// A block takes 256 columns (32 threads of eight) and a run of rows (8 threads): dZ = dY act'(Z), stored once if dz is
-// given, and the sum of its columns over the run, in fp32 of the UNROUNDED products, to part[run][N].
+// A block takes 256 columns (32 threads of eight) and a run of rows (8 threads, two rows at a time): dZ = dY act'(Z), stored
+// once if dz is given, and the sum of its columns over the run, in fp32 of the UNROUNDED products, to part[run][N].
 constexpr int kDzCols = 256, kDzThreads = 256;
 
 template <class T>
 __global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, long long lddy, const T* z, long long ldz, T* dz,
-                                                               long long lddz, float* part, long long M, int N, int act,
-                                                               int rows_per, int vec_ok) {
+                                                                  long long lddz, float* part, long long M, int N, int act,
+                                                                  int rows_per, int vec_ok) {
   __shared__ float sh[8][kDzCols];
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int c0 = blockIdx.x * kDzCols + tx * 8;
   const long long r0 = (long long)blockIdx.y * rows_per, r1 = min(r0 + (long long)rows_per, M);
-  float sum[8];
+  float sum[8] = {};
+  auto row = [&](long long r, float (&g)[8], float (&x)[8]) {
+    if (act == LAQ_ACT_RELU) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sum[e] = 0.f;
-  if (c0 < N) {
-    const bool full = vec_ok && c0 + 8 <= N;
-#pragma unroll 2
+      for (int e = 0; e < 8; ++e) g[e] = x[e] > 0.f ? g[e] : (x[e] == x[e] ? 0.f : x[e]);
+    } else if (act == LAQ_ACT_GELU) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] *= slope_gelu(x[e]);
+    } else if (act == LAQ_ACT_SILU) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) g[e] *= slope_silu(x[e]);
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum[e] += g[e];
+    // the workspace's rows are 16-byte aligned and padded to eight columns
+    if (dz) *reinterpret_cast<uint4*>(dz + r * lddz + c0) = Elem<T>::pack(g);
+  };
+  if (c0 < N && vec_ok && c0 + 8 <= N) {
+    const T* pg = dy + c0;
+    const T* px = z + c0;
+    for (long long r = r0 + ty; r < r1; r += 16) {
+      const bool two = r + 8 < r1;
+      uint4 g0 = load16(pg + r * lddy), g1 = two ? load16(pg + (r + 8) * lddy) : make_uint4(0u, 0u, 0u, 0u);
+      uint4 x0 = g0, x1 = g1;
+      if (act != LAQ_ACT_NONE) {
+        x0 = load16(px + r * ldz);
+        if (two) x1 = load16(px + (r + 8) * ldz);
+      }
+      float g[8], x[8];
+      Elem<T>::unpack(g0, g);
+      Elem<T>::unpack(x0, x);
+      row(r, g, x);
+      if (two) {
+        Elem<T>::unpack(g1, g);
+        Elem<T>::unpack(x1, x);
+        row(r + 8, g, x);
+      }
+    }
+  } else if (c0 < N) {
     for (long long r = r0 + ty; r < r1; r += 8) {
       float g[8], x[8];
-      if (full) {
-        Elem<T>::unpack(load16(dy + r * lddy + c0), g);
-        if (act != LAQ_ACT_NONE) Elem<T>::unpack(load16(z + r * ldz + c0), x);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          g[e] = c0 + e < N ? Elem<T>::to_float(dy[r * lddy + c0 + e]) : 0.f;
-          x[e] = act != LAQ_ACT_NONE && c0 + e < N ? Elem<T>::to_float(z[r * ldz + c0 + e]) : 0.f;
-        }
-      }
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        if (act == LAQ_ACT_RELU) g[e] = x[e] > 0.f ? g[e] : (x[e] == x[e] ? 0.f : x[e]);
-        else if (act != LAQ_ACT_NONE) g[e] *= slope(x[e], act);
-        sum[e] += g[e];
+        g[e] = c0 + e < N ? Elem<T>::to_float(dy[r * lddy + c0 + e]) : 0.f;
+        x[e] = act != LAQ_ACT_NONE && c0 + e < N ? Elem<T>::to_float(z[r * ldz + c0 + e]) : 0.f;
       }
-      if (dz) {                       // the workspace's rows are 16-byte aligned and padded to eight columns
-        *reinterpret_cast<uint4*>(dz + r * lddz + c0) = Elem<T>::pack(g);
-      }
+      row(r, g, x);
     }
   }
   if (!part) return;
