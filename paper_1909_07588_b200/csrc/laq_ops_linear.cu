@@ -542,19 +542,27 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       for (int item = rank * 256 + tid; item < kTileM * groups && !gone; item += 256 * split) {
         const int r0 = TRANS ? item % kTileM : item / groups, g = TRANS ? item / kTileM : item % groups;
         const uint4 res = TRANS ? make_uint4(0u, 0u, 0u, 0u) : residual8<T>(A, i0 + r0, j0 + g * 8, vec);
-        float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        for (int r = 0; r < split; ++r) {
-          const uint4* p = cluster.map_shared_rank(ring4, r);
-          const uint4 lo = p[piece(r0, 2 * g, nt / 4)], hi = p[piece(r0, 2 * g + 1, nt / 4)];
-          x[0] += __uint_as_float(lo.x);
-          x[1] += __uint_as_float(lo.y);
-          x[2] += __uint_as_float(lo.z);
-          x[3] += __uint_as_float(lo.w);
-          x[4] += __uint_as_float(hi.x);
-          x[5] += __uint_as_float(hi.y);
-          x[6] += __uint_as_float(hi.z);
-          x[7] += __uint_as_float(hi.w);
-        }
+        uint4 lo[kMaxSplit], hi[kMaxSplit];               // all blocks' parts on their way at once, added in order
+#pragma unroll
+        for (int r = 0; r < kMaxSplit; ++r)
+          if (r < split) {
+            const uint4* p = cluster.map_shared_rank(ring4, r);
+            lo[r] = p[piece(r0, 2 * g, nt / 4)];
+            hi[r] = p[piece(r0, 2 * g + 1, nt / 4)];
+          }
+        float x[8] = {};
+#pragma unroll
+        for (int r = 0; r < kMaxSplit; ++r)
+          if (r < split) {
+            x[0] += __uint_as_float(lo[r].x);
+            x[1] += __uint_as_float(lo[r].y);
+            x[2] += __uint_as_float(lo[r].z);
+            x[3] += __uint_as_float(lo[r].w);
+            x[4] += __uint_as_float(hi[r].x);
+            x[5] += __uint_as_float(hi[r].y);
+            x[6] += __uint_as_float(hi[r].z);
+            x[7] += __uint_as_float(hi[r].w);
+          }
         finish8<T, TRANS>(A, i0 + r0, j0 + g * 8, x, vec, res);
       }
     }
@@ -721,7 +729,8 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
       for (int split = 1; split <= kMaxSplit; split *= 2) {
         if (split > 1 && (nkb + split - 1) / split * (split - 1) >= nkb) continue;     // a block would have nothing to do
         const size_t stage = (size_t)(kTileM + nt) * kBlockK * 2;
-        const size_t room = split > 1 || nt <= 32 ? 78 * 1024 : kMaxRing;
+        const bool staged = !swap && split == 1;
+        const size_t room = split > 1 ? 110 * 1024 : nt <= 32 ? (staged ? 78 * 1024 : 110 * 1024) : kMaxRing;
         int stages = (int)(room / stage);
         if (stages > kMaxStages) stages = kMaxStages;
         if (split > 1) {
@@ -729,7 +738,7 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
           while ((size_t)stages * stage < need || stages < 3) ++stages;
         }
         if (stages * stage > (size_t)kMaxRing) continue;
-        const int per_sm = stages * stage > 80 * 1024 ? 1 : 2;
+        const int per_sm = stages * stage + (staged ? kStaging : 0) > 112 * 1024 ? 1 : 2;
         const long long tiles = ((i + kTileM - 1) / kTileM) * ((j + nt - 1) / nt);
         const long long kb = (nkb + split - 1) / split;
         const double mma = 2.2 * nt, load = stage / 44.0;
@@ -772,7 +781,7 @@ struct Err {
 template <class T, bool TRANS, bool PAIR>
 laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, cudaStream_t st) {
   auto kernel = linear_gemm_kernel<T, TRANS, PAIR>;
-  const size_t smem = (size_t)A.stages * (kTileM + (PAIR ? A.nt / 2 : A.nt)) * kBlockK * 2 + kStaging + 1024;
+  const size_t smem = (size_t)A.stages * (kTileM + (PAIR ? A.nt / 2 : A.nt)) * kBlockK * 2 + (TRANS || A.split > 1 ? 0 : kStaging) + 1024;
   const int per_tile = PAIR ? 2 : A.split;
   // the kernel's shared memory limit is raised once per device
   static std::atomic<uint64_t> raised{0};
