@@ -38,6 +38,10 @@ constexpr int kMaxRing = 192 * 1024;      // bytes of the stage ring
 constexpr int kStaging = kEpiWarps * 4096;   // ... and of the epilogue warps' pieces behind it
 constexpr int kMaxSplit = 8;
 constexpr uint32_t kStarvedLimit = 1u << 12;
+// The tensor core's fp32 sums are cut, not rounded: every 16 terms take up to an ulp off, always towards zero (8192 terms:
+// 9e-6 of the result, 512 terms: 5e-7).  16-bit results do not show it.  fp32 ones are added up in chunks of 512 terms, which
+// the epilogue's threads keep in registers and add with rounding while the next chunk is under way.
+constexpr int kChunk32 = 8;               // k-blocks
 constexpr int kGroupTiles = 16;           // tile rows that are swept together, so that operands are found in L2
 
 struct GemmArgs {
@@ -46,7 +50,7 @@ struct GemmArgs {
   int tiles_i, tiles_j;
   int a_mn, b_mn;                // 1: the operand is MN-major
   int fmt;                       // operand type of the instruction descriptor: 0 fp16, 1 bf16
-  int act, out_f32, starve;
+  int act, starve;
   long long ldo, ldz, ldr;       // row strides of out, z and residual (elements)
   void* out;
   void* z;                       // or null
@@ -152,7 +156,7 @@ __device__ __forceinline__ float slope_gelu(float z) {
 // Eight neighbours j0.. of row i of D.  TRANS = false: they are neighbours in a row of out; TRANS = true: i is a column of
 // out (neighbouring lanes hold neighbouring columns).  `vec`: all tensors of the call allow 16-byte accesses at multiples of
 // eight columns; `res8` is the residual's then, read beforehand.
-template <class T, bool TRANS>
+template <class T, bool TRANS, bool OUT32>
 __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float (&acc)[8], bool vec, const uint4& res8) {
   if (i >= A.I || j0 >= A.J) return;
   const T* bias = reinterpret_cast<const T*>(A.bias);
@@ -173,7 +177,7 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
     for (int e = 0; e < 8; ++e) {
       if (j0 + e >= A.J) break;
       const float y = acc[e] + r[e];
-      if (A.out_f32) reinterpret_cast<float*>(A.out)[(long long)(j0 + e) * A.ldo + i] = y;
+      if (OUT32) reinterpret_cast<float*>(A.out)[(long long)(j0 + e) * A.ldo + i] = y;
       else reinterpret_cast<T*>(A.out)[(long long)(j0 + e) * A.ldo + i] = Elem<T>::from_float(y);
     }
     return;
@@ -193,7 +197,7 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
 #pragma unroll
       for (int e = 0; e < 8; ++e) acc[e] += r[e];
     }
-    if (A.out_f32) {
+    if (OUT32) {
       float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(A.out) + (long long)i * A.ldo + j0);
       o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
       o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
@@ -215,7 +219,7 @@ __device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float 
     const int j = j0 + e;
     if (j >= A.J) break;
     const float y = acc[e] + (res ? Elem<T>::to_float(res[(long long)i * A.ldr + j]) : 0.f);
-    if (A.out_f32) reinterpret_cast<float*>(A.out)[(long long)i * A.ldo + j] = y;
+    if (OUT32) reinterpret_cast<float*>(A.out)[(long long)i * A.ldo + j] = y;
     else reinterpret_cast<T*>(A.out)[(long long)i * A.ldo + j] = Elem<T>::from_float(y);
   }
 }
@@ -234,8 +238,8 @@ __device__ __forceinline__ bool aligned16(const void* p, long long ld_bytes) {
   return (((uintptr_t)p | (uintptr_t)ld_bytes) & 15u) == 0;
 }
 
-__device__ __forceinline__ bool all_vectors(const GemmArgs& A) {
-  return aligned16(A.out, A.ldo * (A.out_f32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
+__device__ __forceinline__ bool all_vectors(const GemmArgs& A, bool out32) {
+  return aligned16(A.out, A.ldo * (out32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
          (!A.residual || aligned16(A.residual, A.ldr * 2)) && (!A.bias || aligned16(A.bias, 0));
 }
 
@@ -251,7 +255,7 @@ __device__ __forceinline__ void tile_of(const GemmArgs& A, int w, int& i0, int& 
   j0 = (in / rows) * A.nt;
 }
 
-template <class T, bool TRANS, bool PAIR>
+template <class T, bool TRANS, bool PAIR, bool OUT32>
 __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                                       const __grid_constant__ CUtensorMap tmB,
                                                                       const GemmArgs A) {
@@ -262,15 +266,17 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t base = umma::smem_u32(gemm_smem_raw), smem0 = (base + 1023u) & ~1023u;
   uint4* ring4 = reinterpret_cast<uint4*>(gemm_smem_raw + (smem0 - base));        // a split tile, once the ring is idle
+  constexpr int kChunk = OUT32 ? kChunk32 : 1 << 30;      // k-blocks that the tensor core adds up
   const int nt = A.nt, stages = A.stages, split = PAIR ? 1 : A.split;
   const int b_rows = PAIR ? nt / 2 : nt;           // columns of the tile whose part of B this block loads
   const uint32_t a_bytes = kTileM * kBlockK * 2, st_bytes = a_bytes + (uint32_t)b_rows * kBlockK * 2;
   const int half = PAIR ? (int)(blockIdx.x & 1u) : 0;
   const uint32_t full0 = umma::smem_u32(&bars[0]), empty0 = umma::smem_u32(&bars[kMaxStages]);
   const uint32_t acc_full0 = umma::smem_u32(&bars[2 * kMaxStages]), acc_empty0 = acc_full0 + 16, drain = acc_full0 + 32;
-  // Two accumulators of at most 256 columns; one for a split tile, which has no successor.  Two blocks of a cluster on one
-  // SM must be able to hold theirs at the same time (each waits for the other), and two is all that fits by shared memory.
-  const uint32_t acc_cols = umma::tmem_cols(nt), held_cols = split > 1 ? acc_cols : 2 * acc_cols;
+  // Two accumulators of at most 256 columns; one for a split tile, which has no successor (two of at most 128 for its
+  // chunks).  Two blocks of a cluster on one SM must be able to hold theirs at the same time (each waits for the other), and
+  // two is all that fits by shared memory.
+  const uint32_t acc_cols = umma::tmem_cols(nt), held_cols = split > 1 && !OUT32 ? acc_cols : 2 * acc_cols;
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
       umma::mbar_init(full0 + 8 * s, 1);
@@ -375,30 +381,33 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       const uint32_t step_a = A.a_mn ? 128u : 2u, step_b = A.b_mn ? 128u : 2u;
       int n = 0, it = 0;
       bool ok = true;
-      for (int w = first; w < tiles && ok; w += step, ++it) {
-        const int b = it & 1;
-        ok = umma::mbar_wait_abortable(acc_empty0 + 8 * b, ((uint32_t)(it >> 1) & 1u) ^ 1u, limit, abort_flag, A.status, 2u);
-        if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        const uint32_t d = tmem_base + (uint32_t)b * acc_cols;
-        for (int kb = 0; kb < nkb; ++kb, ++n) {
-          const int s = n % stages;
-          ok = umma::mbar_wait_abortable(full0 + 8 * s, (uint32_t)(n / stages) & 1u, limit, abort_flag, A.status, 4u);
+      for (int w = first; w < tiles && ok; w += step) {
+        for (int k0 = 0; k0 < nkb && ok; k0 += kChunk, ++it) {
+          const int b = it & 1, k1 = min(k0 + kChunk, nkb);
+          ok = umma::mbar_wait_abortable(acc_empty0 + 8 * b, ((uint32_t)(it >> 1) & 1u) ^ 1u, limit, abort_flag, A.status, 2u);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t sa = smem0 + s * st_bytes, sb = sa + a_bytes;
-          const uint64_t da = A.a_mn ? desc_mn_major(sa) : desc_k_major(sa), db = A.b_mn ? desc_mn_major(sb) : desc_k_major(sb);
+          const uint32_t d = tmem_base + (uint32_t)b * acc_cols;
+          for (int kb = k0; kb < k1; ++kb, ++n) {
+            const int s = n % stages;
+            ok = umma::mbar_wait_abortable(full0 + 8 * s, (uint32_t)(n / stages) & 1u, limit, abort_flag, A.status, 4u);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t sa = smem0 + s * st_bytes, sb = sa + a_bytes;
+            const uint64_t da = A.a_mn ? desc_mn_major(sa) : desc_k_major(sa), db = A.b_mn ? desc_mn_major(sb) : desc_k_major(sb);
 #pragma unroll
-          for (int kk = 0; kk < kBlockK / 16; ++kk) {
-            if (PAIR) mma_pair(d, da + kk * step_a, db + kk * step_b, idesc, (kb | kk) != 0 ? 1u : 0u);
-            else umma::mma_bf16_ss(d, da + kk * step_a, db + kk * step_b, idesc, (kb | kk) != 0 ? 1u : 0u);
+            for (int kk = 0; kk < kBlockK / 16; ++kk) {
+              const uint32_t more = kb != k0 || kk != 0 ? 1u : 0u;
+              if (PAIR) mma_pair(d, da + kk * step_a, db + kk * step_b, idesc, more);
+              else umma::mma_bf16_ss(d, da + kk * step_a, db + kk * step_b, idesc, more);
+            }
+            if (PAIR) commit_pair(empty0 + 8 * s);
+            else umma::mma_commit(empty0 + 8 * s);
           }
-          if (PAIR) commit_pair(empty0 + 8 * s);
-          else umma::mma_commit(empty0 + 8 * s);
-        }
-        if (ok) {
-          if (PAIR) commit_pair(acc_full0 + 8 * b);
-          else umma::mma_commit(acc_full0 + 8 * b);
+          if (ok) {
+            if (PAIR) commit_pair(acc_full0 + 8 * b);
+            else umma::mma_commit(acc_full0 + 8 * b);
+          }
         }
       }
       if (!ok) {                        // products under way still read the ring and write tensor memory
@@ -412,11 +421,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
   } else {
     const int q = warp & 3, set = (warp - 2) >> 2;
     const int row = q * 32 + lane;
-    const bool vec = all_vectors(A);
+    const bool vec = all_vectors(A, OUT32);
     uint4* stage4 = ring4 + (size_t)stages * st_bytes / 16 + (warp - 2) * 256;         // 4 KB of this warp
     int it = 0;
-    for (int w = first; w < tiles; w += step, ++it) {
-      const int b = it & 1;
+    bool ok = true;
+    for (int w = first; w < tiles && ok; w += step) {
       int i0, j0;
       tile_of<PAIR>(A, w, i0, j0);
       i0 += half * kTileM;
@@ -431,13 +440,67 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
 #pragma unroll
         for (int k = 0; k < 4; ++k) res[k] = load16(p + 8 * k * A.ldr);
       };
-      if (whole && A.residual && 32 * set < nt) ahead(32 * set);
-      const bool ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(it >> 1) & 1u, limit,
-                                                                        abort_flag, A.status, 8u));
-      if (!ok) break;
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const uint32_t t0 = tmem_base + (uint32_t)b * acc_cols + ((uint32_t)(q * 32) << 16);
-      if (split > 1) {
+      if (!OUT32 && whole && A.residual && 32 * set < nt) ahead(32 * set);
+      uint32_t t0 = 0;
+      // the next accumulator, and its return to the tensor-core warp
+      auto acquire = [&]() {
+        const int b = it & 1;
+        ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(it >> 1) & 1u, limit, abort_flag, A.status, 8u));
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        t0 = tmem_base + (uint32_t)b * acc_cols + ((uint32_t)(q * 32) << 16);
+      };
+      auto release = [&]() {
+        const int b = it & 1;
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) arrive_at(of_leader(acc_empty0 + 8 * b));
+          else umma::mbar_arrive(acc_empty0 + 8 * b);
+        }
+        ++it;
+      };
+      float sum[OUT32 ? 2 : 1][32];                    // fp32 results: the chunks' sums, this lane's row
+      if constexpr (OUT32) {
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+          for (int e = 0; e < 32; ++e) sum[p][e] = 0.f;
+        for (int k0 = 0; k0 < nkb; k0 += kChunk) {
+          acquire();
+          if (!ok) break;
+#pragma unroll
+          for (int p = 0; p < 2; ++p)
+            if (32 * set + 64 * p < nt) {
+              uint32_t v[32];
+              umma::tmem_load_32(t0 + (uint32_t)(32 * set + 64 * p), v);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) sum[p][e] += __uint_as_float(v[e]);
+            }
+          release();
+        }
+        if (!ok) break;
+      } else {
+        acquire();
+        if (!ok) break;
+      }
+      // the 32 values from column c0 on of this lane's row
+      auto values = [&](int c0, uint32_t (&v)[32]) {
+        if constexpr (OUT32) {
+#pragma unroll
+          for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(c0 >= 64 ? sum[1][e] : sum[0][e]);
+        } else {
+          umma::tmem_load_32(t0 + (uint32_t)c0, v);    // past nt only where nt is no multiple of 32: not used then
+        }
+      };
+      if (split > 1 && OUT32) {
+        for (int c0 = 32 * set; c0 < nt; c0 += 64) {
+          uint32_t v[32];
+          values(c0, v);
+#pragma unroll
+          for (int e = 0; e < 32; e += 4)
+            ring4[piece(row, (c0 + e) / 4, nt / 4)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        }
+      } else if (split > 1) {
         for (int c0 = 16 * set; c0 < nt; c0 += 32) {
           uint32_t v[16];
           umma::tmem_load_16(t0 + (uint32_t)c0, v);
@@ -452,22 +515,25 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           float x[2][8];
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[e >> 3][e & 7] = __uint_as_float(v[e]);
-          finish8<T, true>(A, i0 + row, j0 + c0, x[0], vec, make_uint4(0u, 0u, 0u, 0u));
-          finish8<T, true>(A, i0 + row, j0 + c0 + 8, x[1], vec, make_uint4(0u, 0u, 0u, 0u));
+          finish8<T, true, OUT32>(A, i0 + row, j0 + c0, x[0], vec, make_uint4(0u, 0u, 0u, 0u));
+          finish8<T, true, OUT32>(A, i0 + row, j0 + c0 + 8, x[1], vec, make_uint4(0u, 0u, 0u, 0u));
         }
       } else {
         // 32 x 32 pieces: a lane takes its row from tensor memory and hands it on; four lanes then share a row, so that
         // loads and stores of the layer's tensors are whole 64-byte stretches
+#pragma unroll 1
         for (int c0 = 32 * set; c0 < nt && whole; c0 += 64) {
           const int j = col0 + c0;
           uint4 now[4];
-#pragma unroll
-          for (int k = 0; k < 4; ++k) now[k] = res[k];
-          if (A.residual && c0 + 64 < nt) ahead(c0 + 64);
           float bias[8] = {};
-          if (A.bias) Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + j)), bias);
+          if constexpr (!OUT32) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) now[k] = res[k];
+            if (A.residual && c0 + 64 < nt) ahead(c0 + 64);
+            if (A.bias) Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + j)), bias);
+          }
           uint32_t v[32];
-          umma::tmem_load_32(t0 + (uint32_t)c0, v);
+          values(c0, v);
           __syncwarp();
 #pragma unroll
           for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
@@ -479,32 +545,34 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           for (int k = 0; k < 4; ++k) {
             const int r = 8 * k + (lane >> 2);
             const uint4 lo = stage4[piece(r, 2 * (lane & 3), 8)], hi = stage4[piece(r, 2 * (lane & 3) + 1, 8)];
-            float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
-                          __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] += bias[e];
-            if (zp) *reinterpret_cast<uint4*>(zp + 8 * k * A.ldz) = Elem<T>::pack(x);
-            activate(x, A.act);
-            if (A.residual) {
-              float y[8];
-              Elem<T>::unpack(now[k], y);
-#pragma unroll
-              for (int e = 0; e < 8; ++e) x[e] += y[e];
-            }
-            if (A.out_f32) {
-              *reinterpret_cast<float4*>(fp + 8 * k * A.ldo) = make_float4(x[0], x[1], x[2], x[3]);
-              *reinterpret_cast<float4*>(fp + 8 * k * A.ldo + 4) = make_float4(x[4], x[5], x[6], x[7]);
+            if constexpr (OUT32) {
+              *reinterpret_cast<uint4*>(fp + 8 * k * A.ldo) = lo;
+              *reinterpret_cast<uint4*>(fp + 8 * k * A.ldo + 4) = hi;
             } else {
+              float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                            __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] += bias[e];
+              if (zp) *reinterpret_cast<uint4*>(zp + 8 * k * A.ldz) = Elem<T>::pack(x);
+              activate(x, A.act);
+              if (A.residual) {
+                float y[8];
+                Elem<T>::unpack(now[k], y);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] += y[e];
+              }
               *reinterpret_cast<uint4*>(yp + 8 * k * A.ldo) = Elem<T>::pack(x);
             }
           }
         }
+#pragma unroll 1
         for (int c0 = 32 * set; c0 < nt && !whole; c0 += 64) {
           const int jl = j0 + c0 + 8 * (lane & 3);
+          uint4 some[4];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) res[k] = residual8<T>(A, i0 + q * 32 + 8 * k + (lane >> 2), jl, vec);
+          for (int k = 0; k < 4; ++k) some[k] = residual8<T>(A, i0 + q * 32 + 8 * k + (lane >> 2), jl, vec);
           uint32_t v[32];
-          umma::tmem_load_32(t0 + (uint32_t)c0, v);          // past nt only where nt is no multiple of 32: not used below
+          values(c0, v);
           __syncwarp();
 #pragma unroll
           for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
@@ -515,16 +583,11 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
             const uint4 lo = stage4[piece(r, 2 * (lane & 3), 8)], hi = stage4[piece(r, 2 * (lane & 3) + 1, 8)];
             float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
                           __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
-            if (c0 + 8 * (lane & 3) < nt) finish8<T, false>(A, i0 + q * 32 + r, jl, x, vec, res[k]);
+            if (c0 + 8 * (lane & 3) < nt) finish8<T, false, OUT32>(A, i0 + q * 32 + r, jl, x, vec, some[k]);
           }
         }
       }
-      asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      __syncwarp();
-      if (lane == 0) {
-        if (PAIR) arrive_at(of_leader(acc_empty0 + 8 * b));
-        else umma::mbar_arrive(acc_empty0 + 8 * b);
-      }
+      if (!OUT32) release();
     }
   }
   if (split > 1) {          // one tile per cluster: its blocks share the columns of the join
@@ -534,7 +597,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
     if (warp >= 2) {
       int gone = 0;
       for (int r = 0; r < split; ++r) gone |= *cluster.map_shared_rank(&abort_sh, r);
-      const bool vec = all_vectors(A);
+      const bool vec = all_vectors(A, OUT32);
       int i0, j0;
       tile_of<false>(A, first, i0, j0);
       // eight columns of a row at a time; lanes run along a row, or down the rows where out is transposed
@@ -563,7 +626,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
             x[6] += __uint_as_float(hi[r].z);
             x[7] += __uint_as_float(hi[r].w);
           }
-        finish8<T, TRANS>(A, i0 + r0, j0 + g * 8, x, vec, res);
+        finish8<T, TRANS, OUT32>(A, i0 + r0, j0 + g * 8, x, vec, res);
       }
     }
     __syncwarp();
@@ -719,8 +782,9 @@ struct Plan {
 // writes element by element; the epilogue of one tile runs beside the products of the next.  A pair's start costs 4500
 // more; the join of a split 6500 and 25 per column, and clusters of four and eight reach 136 and 128 SMs.  The form chosen by
 // it is within 3 % of the fastest in 22 of the 26 and at most 25 % slower in the others.
-// `swappable`: the epilogue may write the transposed tile.
-Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable) {
+// `swappable`: the epilogue may write the transposed tile.  An fp32 result's tile is a multiple of 64 wide (its operands are
+// MN-major).
+Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable, bool out32) {
   Plan best{0, 128, 1, 4, 0, 1e300};
   const long long nkb = (R + kBlockK - 1) / kBlockK;
   const auto persistent = [&](double waves, double main, double epi) {
@@ -732,7 +796,7 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
     static const int widths[] = {16, 32, 64, 96, 112, 128, 160, 192, 208, 224, 256};
     for (int nt : widths) {
       if (bmn && nt % 64) continue;
-      if (swap && nt > 128) continue;
+      if ((swap || out32) && nt > 128) continue;     // fp32 results: 64 sums a thread
       const double mma = 2.7 * nt, epi = 2000 + (swap ? 45.0 : 9.0) * nt;
       for (int split = 1; split <= kMaxSplit; split *= 2) {
         if (split > 1 && (nkb + split - 1) / split * (split - 1) >= nkb) continue;     // a block would have nothing to do
@@ -776,9 +840,9 @@ struct Err {
   size_t len;
 };
 
-template <class T, bool TRANS, bool PAIR>
+template <class T, bool TRANS, bool PAIR, bool OUT32>
 laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, cudaStream_t st) {
-  auto kernel = linear_gemm_kernel<T, TRANS, PAIR>;
+  auto kernel = linear_gemm_kernel<T, TRANS, PAIR, OUT32>;
   const size_t smem = (size_t)A.stages * (kTileM + (PAIR ? A.nt / 2 : A.nt)) * kBlockK * 2 + (TRANS || A.split > 1 ? 0 : kStaging) + 1024;
   const int per_tile = PAIR ? 2 : A.split;
   // the kernel's shared memory limit is raised once per device
@@ -813,6 +877,14 @@ laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& m
   return LAQ_OK;
 }
 
+template <class T>
+laq_status launch_form(const Err& e, const Plan& pl, bool out32, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A,
+                       cudaStream_t st) {
+  if (out32) return pl.pair ? launch_gemm<T, false, true, true>(e, ma, mb, A, st) : launch_gemm<T, false, false, true>(e, ma, mb, A, st);
+  if (pl.pair) return launch_gemm<T, false, true, false>(e, ma, mb, A, st);
+  return pl.swap ? launch_gemm<T, true, false, false>(e, ma, mb, A, st) : launch_gemm<T, false, false, false>(e, ma, mb, A, st);
+}
+
 struct Epilogue {
   void* out = nullptr;
   long long ldo = 0;
@@ -827,7 +899,7 @@ struct Epilogue {
 laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const Operand& b, bool b_mn, const Epilogue& ep,
                    uint32_t* status, int starve, bool swappable, cudaStream_t st) {
   const long long I = a_mn ? a.cols : a.rows, R = a_mn ? a.rows : a.cols, J = b_mn ? b.cols : b.rows;
-  const Plan pl = make_plan(I, J, R, a_mn, b_mn, swappable);
+  const Plan pl = make_plan(I, J, R, a_mn, b_mn, swappable, ep.out_f32 != 0);
   const Operand& A0 = pl.swap ? b : a;
   const Operand& B0 = pl.swap ? a : b;
   const bool amn = pl.swap ? b_mn : a_mn, bmn = pl.swap ? a_mn : b_mn;
@@ -849,7 +921,6 @@ laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const O
   A.b_mn = bmn;
   A.fmt = dtype == LAQ_BF16 ? 1 : 0;
   A.act = ep.act;
-  A.out_f32 = ep.out_f32;
   A.starve = starve;
   A.ldo = ep.ldo;
   A.ldz = ep.ldz;
@@ -859,13 +930,8 @@ laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const O
   A.bias = ep.bias;
   A.residual = ep.residual;
   A.status = status;
-  if (dtype == LAQ_BF16)
-    return pl.pair   ? launch_gemm<__nv_bfloat16, false, true>(e, ma, mb, A, st)
-           : pl.swap ? launch_gemm<__nv_bfloat16, true, false>(e, ma, mb, A, st)
-                     : launch_gemm<__nv_bfloat16, false, false>(e, ma, mb, A, st);
-  return pl.pair   ? launch_gemm<__half, false, true>(e, ma, mb, A, st)
-         : pl.swap ? launch_gemm<__half, true, false>(e, ma, mb, A, st)
-                   : launch_gemm<__half, false, false>(e, ma, mb, A, st);
+  return dtype == LAQ_BF16 ? launch_form<__nv_bfloat16>(e, pl, ep.out_f32 != 0, ma, mb, A, st)
+                           : launch_form<__half>(e, pl, ep.out_f32 != 0, ma, mb, A, st);
 }
 
 // Copies an operand that a tensor map cannot describe to `ws` (advanced past it).
