@@ -181,6 +181,18 @@ extern "C" laq_status laq_quantize_worker_static(const float* d_g, const float* 
         cudaGetLastError();
         return set_err(errbuf, errbuf_len, LAQ_ECUDA, "cudaGetSymbolAddress failed for the static scratch");
       }
+      // The runtime loads a kernel's code on its first use, which may take device memory for it: have all of this file's
+      // loaded now, so that no later call takes any, whichever b it has.
+      const void* kernels[] = {(const void*)static_radius_kernel, (const void*)static_quantize_kernel<1>,
+                               (const void*)static_quantize_kernel<2>, (const void*)static_quantize_kernel<4>,
+                               (const void*)static_quantize_kernel<8>, (const void*)static_quantize_kernel<16>};
+      for (const void* k : kernels) {
+        cudaFuncAttributes fa;
+        if (cudaFuncGetAttributes(&fa, k) != cudaSuccess) {
+          cudaGetLastError();
+          return set_err(errbuf, errbuf_len, LAQ_ECUDA, "cudaFuncGetAttributes failed for a kernel of the static-scratch variant");
+        }
+      }
       g_scratch_addr[dev] = (StaticScratch*)ptr;
     }
     sc = g_scratch_addr[dev];
