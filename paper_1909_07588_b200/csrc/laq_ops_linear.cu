@@ -317,6 +317,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
   const int kb0 = min(rank * kb_per, A.nkb), nkb = min(kb0 + kb_per, A.nkb) - kb0;    // > 0: the plan leaves no block idle
   const bool starved = A.starve && blockIdx.x == 0;
   const uint32_t limit = A.starve ? kStarvedLimit : umma::kWaitLimit;
+  // an accumulator takes its whole sum's time: one limit for every 2^16 k-blocks (some 30 ms) of it
+  const uint32_t acc_limit = A.starve ? kStarvedLimit : umma::kWaitLimit * (1u + (uint32_t)(min(nkb, kChunk) >> 16));
   volatile int* abort_flag = &abort_sh;
 
   if (warp == 0) {
@@ -445,7 +447,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       // the next accumulator, and its return to the tensor-core warp
       auto acquire = [&]() {
         const int b = it & 1;
-        ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(it >> 1) & 1u, limit, abort_flag, A.status, 8u));
+        ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(it >> 1) & 1u, acc_limit, abort_flag, A.status, 8u));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         t0 = tmem_base + (uint32_t)b * acc_cols + ((uint32_t)(q * 32) << 16);
       };
@@ -994,7 +996,9 @@ laq_status check_call(const Err& e, const laq_linear_call* c, void* ws, size_t w
   if (!c->status) return fail(e.buf, e.len, LAQ_EINVAL, "status must point to a word of device memory");
   if (need && (!ws || ((uintptr_t)ws & 255u) || ws_bytes < need))
     return fail(e.buf, e.len, LAQ_EWORKSPACE, "workspace missing, misaligned (256 bytes) or too small: %zu bytes needed", need);
+  if (c->flags & ~(uint32_t)LAQ_LINEAR_STARVE) return fail(e.buf, e.len, LAQ_EINVAL, "unknown flags");
   const char* msg = wrong_device(c->status);
+  if (!msg && c->M > 0 && c->w) msg = wrong_device(c->w);
   return msg ? fail(e.buf, e.len, LAQ_EINVAL, "%s", msg) : LAQ_OK;
 }
 

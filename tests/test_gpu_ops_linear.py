@@ -243,6 +243,39 @@ def test_workspaces_streams_and_graphs():
     ops.check_status()
 
 
+def test_first_calls_of_a_process_may_be_captured():
+    """Nothing that a first call sets up (shared-memory limits, occupancy, the driver's entry point) disturbs a capture."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_1909_07588_b200 import ops
+ops.init()
+x = torch.randn(300, 264, device="cuda").bfloat16(); w = torch.randn(3000, 264, device="cuda").bfloat16()
+tok = torch.randint(0, 3000, (300, 9), device="cuda").int(); val = torch.randn(300, 9, device="cuda"); one = torch.ones(300, device="cuda")
+y = torch.randint(0, 3000, (300,), device="cuda").int()
+def chain():
+    s = ops.linear(x, w)
+    a = ops.token_logprobs(s, y, top_k=3)
+    b = ops.distill(s, tok, val, d_loss=one)
+    g = ops.linear_backward(b["dlogits"], x, w, dw_dtype=torch.float32)
+    return [s, a["logprob"], ops.token_logprobs_backward(s, y, a["lse"], d_logprob=one), b["loss"], g["dx"], g["dw"], g["db"]]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = chain()
+graph.replay()
+torch.cuda.synchronize()
+assert all(torch.equal(p, q) for p, q in zip(got, chain()))
+ops.check_status()
+print("captured")
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    out = subprocess.run([sys.executable, "-c", code], cwd=root, capture_output=True, text=True, timeout=300)
+    assert out.returncode == 0 and "captured" in out.stdout, out.stderr[-2000:]
+
+
 def test_refusals():
     dt = torch.bfloat16
     x, w = _randn(4, 24, seed=1, dtype=dt), _randn(8, 24, seed=2, dtype=dt)

@@ -58,6 +58,7 @@ def _call(**kw):
 @pytest.mark.parametrize("bad, text", [
     (dict(dtype=0), "dtype"), (dict(M=-1), "M must"), (dict(N=0), "M must"), (dict(K=0), "M must"), (dict(K=1 << 31), "M must"),
     (dict(activation=4), "activation"), (dict(activation=-1), "activation"), (dict(status=None), "status"),
+    (dict(flags=2), "flags"),
 ])
 def test_linear_refuses(lib, bad, text):
     err = C.create_string_buffer(256)
