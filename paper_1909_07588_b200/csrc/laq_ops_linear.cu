@@ -789,47 +789,48 @@ struct Plan {
 Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable, bool out32) {
   Plan best{0, 128, 1, 4, 0, 1e300};
   const long long nkb = (R + kBlockK - 1) / kBlockK;
-  const auto persistent = [&](double waves, double main, double epi) {
+  const auto persistent = [](double waves, double main, double epi) {
     return waves * (main > epi ? main : epi) + 0.1 * (main > epi ? epi : main) + epi;
   };
   for (int swap = 0; swap <= (swappable ? 1 : 0); ++swap) {
     const long long i = swap ? J : I, j = swap ? I : J;
+    const long long rows = (i + kTileM - 1) / kTileM, row_pairs = (rows + 1) / 2;
     const bool bmn = swap ? a_mn : b_mn;
     static const int widths[] = {16, 32, 64, 96, 112, 128, 160, 192, 208, 224, 256};
     for (int nt : widths) {
       if (bmn && nt % 64) continue;
       if ((swap || out32) && nt > 128) continue;     // fp32 results: 64 sums a thread
       const double mma = 2.7 * nt, epi = 2000 + (swap ? 45.0 : 9.0) * nt;
-      for (int split = 1; split <= kMaxSplit; split *= 2) {
-        if (split > 1 && (nkb + split - 1) / split * (split - 1) >= nkb) continue;     // a block would have nothing to do
-        const size_t stage = (size_t)(kTileM + nt) * kBlockK * 2;
-        int stages = (int)((split > 1 ? 110 * 1024 : kMaxRing) / stage);
+      const int stage = (kTileM + nt) * kBlockK * 2;
+      const double per = mma > stage / 60.0 ? mma : stage / 60.0;
+      const long long cols = (j + nt - 1) / nt, tiles = rows * cols;
+      for (int log2 = 0; log2 <= 3; ++log2) {
+        const int split = 1 << log2;
+        const long long kb = (nkb + split - 1) >> log2;
+        if (split > 1 && kb * (split - 1) >= nkb) continue;           // a block would have nothing to do
+        int stages = (split > 1 ? 110 * 1024 : kMaxRing) / stage;
         if (stages > kMaxStages) stages = kMaxStages;
-        if (split > 1) {                                                                 // the partial tile in the ring
-          const size_t need = (size_t)kTileM * nt * 4;
-          while ((size_t)stages * stage < need || stages < 3) ++stages;
-        }
-        if (stages * stage > (size_t)kMaxRing) continue;
-        const long long tiles = ((i + kTileM - 1) / kTileM) * ((j + nt - 1) / nt);
-        const long long kb = (nkb + split - 1) / split;
-        const double load = stage / 60.0, main = kb * (mma > load ? mma : load);
+        if (split > 1)                                                 // the partial tile in the ring
+          while (stages * stage < kTileM * nt * 4 || stages < 3) ++stages;
+        if (stages * stage > kMaxRing) continue;
+        const double main = kb * per;
         double cost;
         if (split == 1) {
           cost = persistent((double)((tiles + kSMs - 1) / kSMs), main, epi);
         } else {
-          const long long at_once = split == 8 ? 128 : split == 4 ? 136 : kSMs;
-          cost = 6500 + (double)((tiles * split + at_once - 1) / at_once) * (main + 25.0 * nt) + epi / split;
+          const long long blocks = tiles << log2;
+          const long long waves = split == 8 ? (blocks + 127) / 128 : split == 4 ? (blocks + 135) / 136 : (blocks + kSMs - 1) / kSMs;
+          cost = 6500 + (double)waves * (main + 25.0 * nt) + epi / split;
         }
         if (cost < best.cost) best = Plan{swap, nt, split, stages, 0, cost};
       }
       // pairs of SMs: 256 rows of D
-      if (!swap && nt % 128 == 0 && i > kTileM) {
-        const size_t stage = (size_t)(kTileM + nt / 2) * kBlockK * 2;
-        int stages = (int)(kMaxRing / stage);
+      if (!swap && nt % 128 == 0 && rows > 1) {
+        const int half = (kTileM + nt / 2) * kBlockK * 2;
+        int stages = kMaxRing / half;
         if (stages > kMaxStages) stages = kMaxStages;
-        const long long tiles = ((i + 2 * kTileM - 1) / (2 * kTileM)) * ((j + nt - 1) / nt);
-        const double load = stage / 60.0, main = nkb * (mma > load ? mma : load);
-        const double cost = 4500 + persistent((double)((tiles + kSMs / 2 - 1) / (kSMs / 2)), main, epi);
+        const double main = nkb * (mma > half / 60.0 ? mma : half / 60.0);
+        const double cost = 4500 + persistent((double)((row_pairs * cols + kSMs / 2 - 1) / (kSMs / 2)), main, epi);
         if (cost < best.cost) best = Plan{0, nt, 1, stages, 1, cost};
       }
     }

@@ -64,6 +64,10 @@ def _rows(t, name, index=None, dtype=None, shape=None):
     return t.data_ptr(), stride, rows, cols
 
 
+def _table(rows, cols, dtype, device):
+    return torch.empty_strided((rows, cols), (cols, 1), dtype=dtype, device=device)
+
+
 def _vector(t, name, index, dtype, n):
     """A contiguous vector of n elements, or None: its pointer."""
     if t is None:
@@ -122,14 +126,14 @@ def token_logprobs(logits, tokens=None, top_k=0, temperature=1.0, stream=None):
 
     def body(raw):
         dev = logits.device
-        stats = torch.empty((3, T), dtype=torch.float32, device=dev)
+        stats = _table(3, T, torch.float32, dev)
         p = stats.data_ptr()
         logprob, entropy, lse = stats.unbind(0)
         out = dict(entropy=entropy, lse=lse) if tok is None else dict(logprob=logprob, entropy=entropy, lse=lse)
         tp = vp = None
         if top_k:
-            out["top_tokens"] = a = torch.empty((T, top_k), dtype=torch.int32, device=dev)
-            out["top_logprobs"] = b = torch.empty((T, top_k), dtype=torch.float32, device=dev)
+            out["top_tokens"] = a = _table(T, top_k, torch.int32, dev)
+            out["top_logprobs"] = b = _table(T, top_k, torch.float32, dev)
             tp, vp = a.data_ptr(), b.data_ptr()
         _call(laq.load_library().laq_token_logprobs, *head, temperature, tok, top_k, None if tok is None else p, p + 4 * T,
               p + 8 * T, tp, vp, raw)
@@ -193,7 +197,7 @@ def distill(logits, teacher_tokens, teacher_logits, temperature=1.0, d_loss=None
         _refuse("out without d_loss")
 
     def body(raw):
-        stats = torch.empty((2, T), dtype=torch.float32, device=logits.device)
+        stats = _table(2, T, torch.float32, logits.device)
         p = stats.data_ptr()
         loss, lse = stats.unbind(0)
         res = dict(loss=loss, lse=lse)
@@ -306,11 +310,11 @@ def linear(x, weight, bias=None, activation="none", residual=None, preact=False,
 
     def body(raw):
         c.status = _status_word(index).data_ptr()
-        y = torch.empty(shape, dtype=dt, device=x.device) if out is None else out
+        y = _table(*shape, dt, x.device) if out is None else out
         c.y, c.ld_y, _, _ = _rows(y, "out", index, dt, shape)
         z = None
         if preact:
-            z = torch.empty(shape, dtype=dt, device=x.device)
+            z = _table(*shape, dt, x.device)
             c.z, c.ld_z = z.data_ptr(), c.N
         ws, wp, wn = _workspace(L, c, 0, index, workspace)
         _call(L.laq_linear_forward, C.byref(c), wp, wn, raw)
@@ -344,10 +348,10 @@ def linear_backward(dy, x, weight, z=None, activation="none", dx=True, dw=True, 
         c.status = _status_word(index).data_ptr()
         dev, res = x.device, {}
         if dx:
-            res["dx"] = t = torch.empty((c.M, c.K), dtype=dt, device=dev)
+            res["dx"] = t = _table(c.M, c.K, dt, dev)
             c.dx, c.ld_dx = t.data_ptr(), c.K
         if dw:
-            res["dw"] = t = torch.empty((c.N, c.K), dtype=dw_dtype, device=dev)
+            res["dw"] = t = _table(c.N, c.K, dw_dtype, dev)
             c.dw, c.ld_dw, c.dw_dtype = t.data_ptr(), c.K, DTYPES[dw_dtype]
         if db:
             res["db"] = t = torch.empty(c.N, dtype=torch.float32, device=dev)
