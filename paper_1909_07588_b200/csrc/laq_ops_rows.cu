@@ -474,16 +474,22 @@ struct Entries {                 // column (or -1 where there is no entry) and l
 #pragma unroll
     for (int e = 0; e < kPerLane; ++e) {
       const int i = lane + 32 * e;
-      col[e] = i < K ? idx[i] : -1;
-      t[e] = i < K ? val[i] : -INFINITY;
+      col[e] = -1;
+      t[e] = -INFINITY;
+      if (32 * e < K && i < K) {
+        col[e] = idx[i];
+        t[e] = val[i];
+      }
     }
   }
   // the student's logits at the columns, where need(column)
   template <class T, class F>
-  __device__ __forceinline__ void student(const T* row, int V, float (&x)[kPerLane], F need) const {
+  __device__ __forceinline__ void student(const T* row, int K, int V, float (&x)[kPerLane], F need) const {
 #pragma unroll
-    for (int e = 0; e < kPerLane; ++e)
-      x[e] = col[e] >= 0 && col[e] < V && need(col[e]) ? Elem<T>::to_float(row[col[e]]) : 0.f;
+    for (int e = 0; e < kPerLane; ++e) {
+      x[e] = 0.f;
+      if (32 * e < K && col[e] >= 0 && col[e] < V && need(col[e])) x[e] = Elem<T>::to_float(row[col[e]]);
+    }
   }
 };
 
@@ -498,13 +504,15 @@ struct Teacher {
   int any, bad;        // a live entry; a column outside the vocabulary
 
   // e0, e1: the slice's columns
-  __device__ __forceinline__ void set(const Entries& in, const float (&xs)[kPerLane], int V, float inv_tau, int e0, int e1) {
+  __device__ __forceinline__ void set(const Entries& in, const float (&xs)[kPerLane], int K, int V, float inv_tau, int e0, int e1) {
     const int lane = threadIdx.x & 31;
     float t[kPerLane];
     float mx = -INFINITY;
     bool have = false, out = false;
 #pragma unroll
     for (int e = 0; e < kPerLane; ++e) {
+      t[e] = -INFINITY;
+      if (32 * e >= K) continue;
       out |= in.col[e] >= V;
       const bool there = in.col[e] >= 0 && in.col[e] < V;
       have |= there;
@@ -519,6 +527,8 @@ struct Teacher {
     float sum = 0.f, e_[kPerLane];
 #pragma unroll
     for (int e = 0; e < kPerLane; ++e) {
+      e_[e] = 0.f;
+      if (32 * e >= K) continue;
       t[e] = t[e] == -INFINITY ? -INFINITY : (t[e] - mx) * inv_tau;
       e_[e] = ex2(t[e] * kLog2e);
       sum += e_[e];
@@ -529,6 +539,7 @@ struct Teacher {
     int listed = 0;
 #pragma unroll
     for (int e = 0; e < kPerLane; ++e) {
+      if (32 * e >= K) continue;
       const int i = lane + 32 * e;
       const bool there = in.col[e] >= 0 && in.col[e] < V, mine = there && in.col[e] >= e0 && in.col[e] < e1;
       const float p = there && have ? e_[e] * inv : 0.f;
@@ -573,8 +584,8 @@ struct Teacher {
     Entries in;
     float xs[kPerLane];
     in.load(idx, val, K);
-    in.student(row, V, xs, [](int) { return true; });
-    set(in, xs, V, inv_tau, 0, V);
+    in.student(row, K, V, xs, [](int) { return true; });
+    set(in, xs, K, V, inv_tau, 0, V);
   }
   // loss of the row / tau^2, by the warp that read it: sum_i q_i (log q_i - log p_i)
   __device__ __forceinline__ float divergence(const RowSum& r, int K) const {
@@ -835,8 +846,8 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
     Entries in;
     float xs[kPerLane];
     in.load(idx, A.teacher_logits + row * A.ld_teacher, A.K);
-    in.student(xr, A.V, xs, [&](int j) { return j >= sl.e0 && j < sl.e1; });
-    te.set(in, xs, A.V, A.inv_tau, sl.e0, sl.e1);
+    in.student(xr, A.K, A.V, xs, [&](int j) { return j >= sl.e0 && j < sl.e1; });
+    te.set(in, xs, A.K, A.V, A.inv_tau, sl.e0, sl.e1);
     if (in_place) bar_sync<1, kThreads>();          // the student's logits are read before they are written over
     bar_sync<2, kThreads>();
     const float ca = A.d_loss[row] * A.tau;
@@ -1024,7 +1035,10 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
     if (ranks > 1) {
       cg::cluster_group cluster = cg::this_cluster();
       if (t < ranks) *cluster.map_shared_rank(&cstat[b][rank], t) = a;
-      cluster.sync();
+      // only the first warp has written to the others, and only the teacher's has read what they will write
+      if (w == 0 || w == kWarps) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+      else asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+      asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
       Stat o{kUnset, 0.f, 0.f};
       if (lane % kMaxCluster < ranks) o = cstat[b][lane % kMaxCluster];
       a = warp_join<kMaxCluster, false>(o, c);
@@ -1045,12 +1059,12 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
     auto look = [&](int row, const Entries& in, float (&xs)[kPerLane]) {
       if (row >= rows) return;
       const Slice<T> sl = slice_of(row);
-      in.student(sl.row, A.V, xs, [&](int j) { return rank == 0 || (j >= sl.e0 && j < sl.e1); });
+      in.student(sl.row, A.K, A.V, xs, [&](int j) { return rank == 0 || (j >= sl.e0 && j < sl.e1); });
     };
     auto prepare = [&](int row, const Entries& in, const float (&xs)[kPerLane], int b) {
       if (row >= rows) return;
       const Slice<T> sl = slice_of(row);
-      teacher[b].set(in, xs, A.V, A.inv_tau, sl.e0, sl.e1);
+      teacher[b].set(in, xs, A.K, A.V, A.inv_tau, sl.e0, sl.e1);
     };
     Entries now, next;
     float xs[kPerLane], next_g = first < rows ? A.d_loss[first] : 0.f;
@@ -1066,12 +1080,7 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
       const Teacher& te = teacher[b];
       const float ca = next_g * A.tau;
       if (row + step < rows) next_g = A.d_loss[row + step];
-      // the next row's list is made while the other warps take this row's statistics; its loads are a turn old
-      prepare(row + step, now, xs, b ^ 1);
       bar_sync<1, kThreads>();
-      now = next;
-      look(row + 2 * step, now, xs);
-      load(row + 3 * step, next);
       const RowSum r = row_sum(b);
       if (rank == 0) {
         const float kl = te.divergence(r, A.K);
@@ -1080,6 +1089,11 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
           A.lse_out[row] = te.any ? r.lse : 0.f;
         }
       }
+      // the next row's list is made while the other warps store this row's gradient; its loads are a turn old
+      prepare(row + step, now, xs, b ^ 1);
+      now = next;
+      look(row + 2 * step, now, xs);
+      load(row + 3 * step, next);
       T* dr = reinterpret_cast<T*>(A.dx) + (long long)row * A.ld_d;
       bar_sync<2, kThreads>();
       if (te.any && !te.bad && !r.empty)
@@ -1129,11 +1143,17 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
       run.one(now.xe);
 #pragma unroll
       for (int i0 = 0; i0 < R; i0 += B) {
+        if (i0 * NT >= now.mine) break;
         uint4 v[B];
+        if ((i0 + B - 1) * NT < now.mine) {
 #pragma unroll
-        for (int i = 0; i < B; ++i) {
-          v[i] = make_uint4(Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf);
-          if ((i0 + i) * NT < now.mine) v[i] = buffer[(i0 + i) * NT + t];
+          for (int i = 0; i < B; ++i) v[i] = buffer[(i0 + i) * NT + t];
+        } else {
+#pragma unroll
+          for (int i = 0; i < B; ++i) {
+            v[i] = make_uint4(Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf, Elem<T>::kNegInf);
+            if ((i0 + i) * NT < now.mine) v[i] = buffer[(i0 + i) * NT + t];
+          }
         }
         run.follow(Elem<T>::largest(v));
         run.add(v);
