@@ -153,74 +153,68 @@ __device__ __forceinline__ float slope_gelu(float z) {
   return fmaf(z * s * (1.f - s), fmaf(6.f * kGeluC * kGeluA, fminf(z * z, 400.f), 2.f * kGeluC), s);
 }
 
-// Eight neighbours j0.. of row i of D.  TRANS = false: they are neighbours in a row of out; TRANS = true: i is a column of
-// out (neighbouring lanes hold neighbouring columns).  `vec`: all tensors of the call allow 16-byte accesses at multiples of
-// eight columns; `res8` is the residual's then, read beforehand.
-template <class T, bool TRANS, bool OUT32>
-__device__ __forceinline__ void finish8(const GemmArgs& A, int i, int j0, float (&acc)[8], bool vec, const uint4& res8) {
-  if (i >= A.I || j0 >= A.J) return;
-  const T* bias = reinterpret_cast<const T*>(A.bias);
+// Eight rows row0.. of column `col` of out (rows x cols): the form for transposed tiles and for tensors that allow no
+// vectors.  Neighbouring lanes hold neighbouring columns.
+template <class T, bool OUT32>
+__device__ __forceinline__ void finish_column(const GemmArgs& A, int rows, int cols, int row0, int col, float (&x)[8]) {
+  if (col >= cols || row0 >= rows) return;
   const T* res = reinterpret_cast<const T*>(A.residual);
-  T* zp = reinterpret_cast<T*>(A.z);
-  if (TRANS) {
-    const float b = bias ? Elem<T>::to_float(bias[i]) : 0.f;
+  const int n = min(8, rows - row0);
+  const float b = A.bias ? Elem<T>::to_float(reinterpret_cast<const T*>(A.bias)[col]) : 0.f;
+  float r[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) r[e] = res && e < n ? Elem<T>::to_float(res[(long long)(row0 + e) * A.ldr + col]) : 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) x[e] += b;
+  if (A.z) {
+    T* z = reinterpret_cast<T*>(A.z) + (long long)row0 * A.ldz + col;
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) z[e * A.ldz] = Elem<T>::from_float(x[e]);
+  }
+  activate(x, A.act);
+  const long long at = (long long)row0 * A.ldo + col;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    if (e >= n) break;
+    if (OUT32) reinterpret_cast<float*>(A.out)[at + e * A.ldo] = x[e] + r[e];
+    else reinterpret_cast<T*>(A.out)[at + e * A.ldo] = Elem<T>::from_float(x[e] + r[e]);
+  }
+}
+
+// Eight neighbours j0.. of row i of out, for tensors that all allow 16-byte accesses at multiples of eight columns; `res8`:
+// the residual's, read beforehand.
+template <class T, bool OUT32>
+__device__ __forceinline__ void finish_row(const GemmArgs& A, int i, int j0, float (&x)[8], const uint4& res8) {
+  if (i >= A.I || j0 >= A.J) return;
+  if (j0 + 8 > A.J) {                       // the last columns of rows that end within a vector
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float one[8] = {x[e]};
+      finish_column<T, OUT32>(A, i + 1, A.J, i, j0 + e, one);
+    }
+    return;
+  }
+  if (A.bias) {
+    float b[8];
+    Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + j0)), b);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] += b[e];
+  }
+  if (A.z) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(A.z) + (long long)i * A.ldz + j0) = Elem<T>::pack(x);
+  activate(x, A.act);
+  if (A.residual) {
     float r[8];
+    Elem<T>::unpack(res8, r);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = res && j0 + e < A.J ? Elem<T>::to_float(res[(long long)(j0 + e) * A.ldr + i]) : 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      acc[e] += b;
-      if (zp && j0 + e < A.J) zp[(long long)(j0 + e) * A.ldz + i] = Elem<T>::from_float(acc[e]);
-    }
-    activate(acc, A.act);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (j0 + e >= A.J) break;
-      const float y = acc[e] + r[e];
-      if (OUT32) reinterpret_cast<float*>(A.out)[(long long)(j0 + e) * A.ldo + i] = y;
-      else reinterpret_cast<T*>(A.out)[(long long)(j0 + e) * A.ldo + i] = Elem<T>::from_float(y);
-    }
-    return;
+    for (int e = 0; e < 8; ++e) x[e] += r[e];
   }
-  if (vec && j0 + 8 <= A.J) {
-    if (bias) {
-      float b[8];
-      Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(bias + j0)), b);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += b[e];
-    }
-    if (zp) *reinterpret_cast<uint4*>(zp + (long long)i * A.ldz + j0) = Elem<T>::pack(acc);
-    activate(acc, A.act);
-    if (res) {
-      float r[8];
-      Elem<T>::unpack(res8, r);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] += r[e];
-    }
-    if (OUT32) {
-      float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(A.out) + (long long)i * A.ldo + j0);
-      o[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-      o[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-    } else {
-      *reinterpret_cast<uint4*>(reinterpret_cast<T*>(A.out) + (long long)i * A.ldo + j0) = Elem<T>::pack(acc);
-    }
-    return;
-  }
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int j = j0 + e;
-    if (j >= A.J) break;
-    acc[e] += bias ? Elem<T>::to_float(bias[j]) : 0.f;
-    if (zp) zp[(long long)i * A.ldz + j] = Elem<T>::from_float(acc[e]);
-  }
-  activate(acc, A.act);
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const int j = j0 + e;
-    if (j >= A.J) break;
-    const float y = acc[e] + (res ? Elem<T>::to_float(res[(long long)i * A.ldr + j]) : 0.f);
-    if (OUT32) reinterpret_cast<float*>(A.out)[(long long)i * A.ldo + j] = y;
-    else reinterpret_cast<T*>(A.out)[(long long)i * A.ldo + j] = Elem<T>::from_float(y);
+  if (OUT32) {
+    float4* o = reinterpret_cast<float4*>(reinterpret_cast<float*>(A.out) + (long long)i * A.ldo + j0);
+    o[0] = make_float4(x[0], x[1], x[2], x[3]);
+    o[1] = make_float4(x[4], x[5], x[6], x[7]);
+  } else {
+    *reinterpret_cast<uint4*>(reinterpret_cast<T*>(A.out) + (long long)i * A.ldo + j0) = Elem<T>::pack(x);
   }
 }
 template <class T>
@@ -517,8 +511,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           float x[2][8];
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[e >> 3][e & 7] = __uint_as_float(v[e]);
-          finish8<T, true, OUT32>(A, i0 + row, j0 + c0, x[0], vec, make_uint4(0u, 0u, 0u, 0u));
-          finish8<T, true, OUT32>(A, i0 + row, j0 + c0 + 8, x[1], vec, make_uint4(0u, 0u, 0u, 0u));
+          finish_column<T, OUT32>(A, A.J, A.I, j0 + c0, i0 + row, x[0]);
+          finish_column<T, OUT32>(A, A.J, A.I, j0 + c0 + 8, i0 + row, x[1]);
         }
       } else {
         // 32 x 32 pieces: a lane takes its row from tensor memory and hands it on; four lanes then share a row, so that
@@ -579,13 +573,23 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
 #pragma unroll
           for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
           __syncwarp();
+          if (!vec) {
+            for (int k = 0; k < 32 && c0 + lane < nt; k += 8) {
+              float x[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e)
+                x[e] = __uint_as_float(reinterpret_cast<const uint32_t*>(&stage4[piece(k + e, lane >> 2, 8)])[lane & 3]);
+              finish_column<T, OUT32>(A, A.I, A.J, i0 + q * 32 + k, j0 + c0 + lane, x);
+            }
+            continue;
+          }
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
             const int r = 8 * k + (lane >> 2);
             const uint4 lo = stage4[piece(r, 2 * (lane & 3), 8)], hi = stage4[piece(r, 2 * (lane & 3) + 1, 8)];
             float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
                           __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
-            if (c0 + 8 * (lane & 3) < nt) finish8<T, false, OUT32>(A, i0 + q * 32 + r, jl, x, vec, some[k]);
+            if (c0 + 8 * (lane & 3) < nt) finish_row<T, OUT32>(A, i0 + q * 32 + r, jl, x, some[k]);
           }
         }
       }
@@ -604,31 +608,45 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       tile_of<false>(A, first, i0, j0);
       // eight columns of a row at a time; lanes run along a row, or down the rows where out is transposed
       const int groups = nt / 8, tid = (int)threadIdx.x - 64;
-      for (int item = rank * 256 + tid; item < kTileM * groups && !gone; item += 256 * split) {
-        const int r0 = TRANS ? item % kTileM : item / groups, g = TRANS ? item / kTileM : item % groups;
-        const uint4 res = TRANS ? make_uint4(0u, 0u, 0u, 0u) : residual8<T>(A, i0 + r0, j0 + g * 8, vec);
-        uint4 lo[kMaxSplit], hi[kMaxSplit];               // all blocks' parts on their way at once, added in order
+      if (TRANS || vec) {
+        for (int item = rank * 256 + tid; item < kTileM * groups && !gone; item += 256 * split) {
+          const int r0 = TRANS ? item % kTileM : item / groups, g = TRANS ? item / kTileM : item % groups;
+          const uint4 res = TRANS ? make_uint4(0u, 0u, 0u, 0u) : residual8<T>(A, i0 + r0, j0 + g * 8, vec);
+          uint4 lo[kMaxSplit], hi[kMaxSplit];               // all blocks' parts on their way at once, added in order
 #pragma unroll
-        for (int r = 0; r < kMaxSplit; ++r)
-          if (r < split) {
+          for (int r = 0; r < kMaxSplit; ++r)
+            if (r < split) {
+              const uint4* p = cluster.map_shared_rank(ring4, r);
+              lo[r] = p[piece(r0, 2 * g, nt / 4)];
+              hi[r] = p[piece(r0, 2 * g + 1, nt / 4)];
+            }
+          float x[8] = {};
+#pragma unroll
+          for (int r = 0; r < kMaxSplit; ++r)
+            if (r < split) {
+              x[0] += __uint_as_float(lo[r].x);
+              x[1] += __uint_as_float(lo[r].y);
+              x[2] += __uint_as_float(lo[r].z);
+              x[3] += __uint_as_float(lo[r].w);
+              x[4] += __uint_as_float(hi[r].x);
+              x[5] += __uint_as_float(hi[r].y);
+              x[6] += __uint_as_float(hi[r].z);
+              x[7] += __uint_as_float(hi[r].w);
+            }
+          if (TRANS) finish_column<T, OUT32>(A, A.J, A.I, j0 + g * 8, i0 + r0, x);
+          else finish_row<T, OUT32>(A, i0 + r0, j0 + g * 8, x, res);
+        }
+      } else {                                   // eight rows of a column: lanes run along the columns
+        for (int item = rank * 256 + tid; item < kTileM / 8 * nt && !gone; item += 256 * split) {
+          const int r0 = item / nt * 8, c = item % nt;
+          float x[8] = {};
+          for (int r = 0; r < split; ++r) {
             const uint4* p = cluster.map_shared_rank(ring4, r);
-            lo[r] = p[piece(r0, 2 * g, nt / 4)];
-            hi[r] = p[piece(r0, 2 * g + 1, nt / 4)];
-          }
-        float x[8] = {};
 #pragma unroll
-        for (int r = 0; r < kMaxSplit; ++r)
-          if (r < split) {
-            x[0] += __uint_as_float(lo[r].x);
-            x[1] += __uint_as_float(lo[r].y);
-            x[2] += __uint_as_float(lo[r].z);
-            x[3] += __uint_as_float(lo[r].w);
-            x[4] += __uint_as_float(hi[r].x);
-            x[5] += __uint_as_float(hi[r].y);
-            x[6] += __uint_as_float(hi[r].z);
-            x[7] += __uint_as_float(hi[r].w);
+            for (int e = 0; e < 8; ++e) x[e] += reinterpret_cast<const float*>(p + piece(r0 + e, c >> 2, nt / 4))[c & 3];
           }
-        finish8<T, TRANS, OUT32>(A, i0 + r0, j0 + g * 8, x, vec, res);
+          finish_column<T, OUT32>(A, A.I, A.J, i0 + r0, j0 + c, x);
+        }
       }
     }
     __syncwarp();
