@@ -338,7 +338,7 @@ laq_status laq_token_logprobs_backward(const void* d_logits, int32_t dtype, int6
  * the student has masked (-inf) gives loss = +inf; so does a row that the student has masked throughout, whose gradient is 0.
  * d_loss, d_lse: [rows] fp32.  d_grad_loss ([rows] fp32) and d_grad_logits (logits' dtype; the logits themselves or no overlap)
  * come together or are both NULL: with them the call also writes d_grad_logits = d_grad_loss * d loss / d logits, reading the
- * logits once where a row fits the registers of eight blocks (524288 bytes), else twice. */
+ * logits once where a row fits the shared memory of eight blocks (524288 bytes), else twice. */
 laq_status laq_distill(const void* d_logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride, float temperature,
                        const int32_t* d_teacher_tokens, const float* d_teacher_logits, int32_t teacher_k, int64_t teacher_stride,
                        float* d_loss, float* d_lse, const float* d_grad_loss, void* d_grad_logits, int64_t grad_row_stride,

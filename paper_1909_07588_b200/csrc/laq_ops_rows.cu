@@ -618,6 +618,15 @@ struct ForwardArgs {
 };
 
 // One pass over the logits: DISTILL = false for token_logprobs, true for the loss of distill without its gradient.
+//
+// Per element of 16 bits: half a comparison for the maximum, half for the bound, one unpacking, one ex2 and one and a half
+// fused operations, 7.3 instructions with everything around them; memory and the special-function unit (8 cycles a warp's
+// ex2) are both near their limits, so what counts is that enough is under way: four blocks an SM, each thread two batches
+// of 64 bytes through shared memory.  4096 rows of 131072 bf16: 168 us, 6.4 TB/s (0.98 of the measured copy rate); with 20
+// alternatives 196 us (0.84): the selection after a row leaves its block without loads for about 3 us.  (Three batches and
+// three blocks: 177 and 209 us; two vectors a batch, five blocks: 191 and 229 us; vectors straight to registers: 241 us.)
+// Rows of one warp and of a block of 128 threads exist for short rows: a block's barriers and the selection cost a row about
+// 5 us whatever its length (32768 rows of 8192 bf16, 8 alternatives: 371 us by blocks of 256, 193 us by 128).
 template <class T, int NT, bool DISTILL>
 __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kForwardBlocks * kBlock / NT) rows_forward_kernel(const ForwardArgs A) {
   using G = Group<NT>;
@@ -790,6 +799,12 @@ __device__ __forceinline__ void store_vec(T* dst, const float (&y)[Elem<T>::EV],
   }
 }
 
+// Gradients whose statistics are known: bound by memory, each logit read and each gradient written once (4096 rows of 100003
+// bf16, starting at odd addresses: 254 us, 6.4 TB/s, 0.98 of the measured copy rate; the teacher's form, 2048 rows of 131072:
+// 167 us, 0.98).  16 vectors a thread and five blocks an SM: with four vectors what a block does once made two thirds of
+// its instructions (285 us).  The teacher's entries have a warp of their own, beside which the others load and store; in
+// the warps' path they cost 516 instead of 333 us at 8192 rows of 65536.
+//
 // A thread keeps its R vectors of the row in registers, so the gradient in the same call as the loss (rows of a warp here,
 // longer ones in rows_distill_kernel) reads the logits once.  With the statistics handed over (kLogprobsGrad, kDistillGrad)
 // `ranks` is any number of independent pieces of the row.
@@ -1010,11 +1025,18 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
   }
 }
 
-// The teacher's gradients for rows longer than a warp's.  A block runs over items (a row in the step, each block of a
-// cluster its slice; a piece of a row with the statistics handed over): eight warps hold the item's vectors in registers
-// while the next item's are on their way to shared memory, so that memory never waits for the barriers between load and
-// store.  A ninth warp prepares the next item's teacher entries meanwhile and, when the vectors' gradient is stored, writes
-// the teacher's columns over it.
+// The loss and its gradient in one reading, for rows longer than a warp's.  A block goes over rows (each block of a cluster
+// over its slice of them): a slice lies in shared memory, is read twice from there, for the statistics and for the gradient,
+// and the next row's is on its way into each vector's place as soon as the gradient has used it.  One more warp
+// prepares the next row's teacher entries while the gradient is stored, and then writes the teacher's columns over it: on
+// the other warps' path that had cost as much as the whole rest.
+//
+// 8192 rows of 65536 bf16, 64 entries: 390 us, 5.5 TB/s (0.84 of the measured copy rate; two clusters' halves of 64 KB, three
+// blocks an SM).  Two ex2 an element keep the special-function unit busy for 250 us of it, 14 instructions an element the
+// schedulers for 260 us, and the two phases of a block do not overlap with themselves: other blocks have to fill the
+// gaps.  Measured and dropped: slices held in registers (580 us: too few warps), 128 threads a block (510 us), part of
+// the exponentials as a polynomial (no gain: the schedulers are as busy), three buffers and one block of 512 threads an SM with
+// the cluster's join under the next row's statistics (592 us).
 template <class T, int NT, int R>
 __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_step_kernel(const GradArgs A) {
   constexpr int EV = Elem<T>::EV, kWarps = NT / 32, kThreads = NT + 32;
