@@ -806,7 +806,7 @@ __device__ __forceinline__ void store_vec(T* dst, const float (&y)[Elem<T>::EV],
 // the warps' path they cost 516 instead of 333 us at 8192 rows of 65536.
 //
 // A thread keeps its R vectors of the row in registers, so the gradient in the same call as the loss (rows of a warp here,
-// longer ones in rows_distill_kernel) reads the logits once.  With the statistics handed over (kLogprobsGrad, kDistillGrad)
+// longer ones in rows_step_kernel) reads the logits once.  With the statistics handed over (kLogprobsGrad, kDistillGrad)
 // `ranks` is any number of independent pieces of the row.
 //
 // dx_j = p_j (ca + cb log2 p_j), then the entries that have a term of their own.  16-bit logits take log2 p as one fused
@@ -1057,7 +1057,9 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
     if (ranks > 1) {
       cg::cluster_group cluster = cg::this_cluster();
       if (t < ranks) *cluster.map_shared_rank(&cstat[b][rank], t) = a;
-      // only the first warp has written to the others, and only the teacher's has read what they will write
+      __syncwarp();
+      // only the first warp has written to the others, and only the teacher's has read what they will write; the other warps'
+      // readings of this buffer two rows ago have long been used
       if (w == 0 || w == kWarps) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
       else asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
       asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
