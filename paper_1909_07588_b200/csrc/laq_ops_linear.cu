@@ -78,6 +78,14 @@ __device__ __forceinline__ uint32_t instr_desc(int fmt, int a_mn, int b_mn, int 
          ((uint32_t)(nt >> 3) << 17) | ((uint32_t)(rows >> 4) << 24);
 }
 
+// The kernels of one call follow each other closely: each allows the next to be set up beside it as soon as all of its
+// blocks run, and one that was launched so waits, before it touches anything that the one before reads or writes, until
+// that one has ended (a kernel launched in the ordinary way finds nothing to wait for).  No block asks for this before it
+// holds its tensor memory, so one that waits for memory held by the kernel before always gets it.  A backward pass of four
+// kernels: 64 x 200 x 784 38 -> 36 us, 8192 x 4096 x 1024 154 -> 150 us.
+__device__ __forceinline__ void allow_next() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // One lane of the (converged) warp.  The loader and the tensor-core warp are led by an elected lane and not by a fixed one:
 // the compiler then knows that one thread issues and needs no loop around every copy and product, which had left the tensor
 // pipe idle 45 % of the time (8192 x 4096 x 4096: 228 -> 191 us).
@@ -304,6 +312,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
   else __syncthreads();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem_base = tmem_base_sh;
+  allow_next();
+  await_previous();
 
   const int tiles = A.tiles_i * A.tiles_j;
   const int rank = split > 1 ? (int)(blockIdx.x % (unsigned)split) : 0;
@@ -679,6 +689,7 @@ __global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, l
                                                                   long long lddz, float* part, long long M, int N, int act,
                                                                   int rows_per, int vec_ok) {
   __shared__ float sh[8][kDzCols];
+  allow_next();
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
   const int c0 = blockIdx.x * kDzCols + tx * 8;
   const long long r0 = (long long)blockIdx.y * rows_per, r1 = min(r0 + (long long)rows_per, M);
@@ -746,6 +757,8 @@ __global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, l
 
 __global__ void __launch_bounds__(1024) linear_db_kernel(const float* part, int runs, int N, float* db) {
   __shared__ float sh[32][33];
+  allow_next();
+  await_previous();
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5, c = blockIdx.x * 32 + tx;
   float s = 0.f;
   if (c < N) {
@@ -764,6 +777,7 @@ __global__ void __launch_bounds__(1024) linear_db_kernel(const float* part, int 
 // into the workspace with a pitch of a multiple of eight elements.
 __global__ void __launch_bounds__(256) linear_pack_kernel(const uint16_t* src, long long ld, uint16_t* dst, long long pitch,
                                                           long long rows, int cols) {
+  allow_next();
   const int groups = (cols + 7) / 8;
   const long long n = rows * groups, stride = (long long)gridDim.x * blockDim.x;
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) {
@@ -865,7 +879,8 @@ struct Err {
 };
 
 template <class T, bool TRANS, bool PAIR, bool OUT32>
-laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, cudaStream_t st) {
+laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, bool follows,
+                       cudaStream_t st) {
   auto kernel = linear_gemm_kernel<T, TRANS, PAIR, OUT32>;
   const size_t smem = (size_t)A.stages * (kTileM + (PAIR ? A.nt / 2 : A.nt)) * kBlockK * 2 + (TRANS || A.split > 1 ? 0 : kStaging) + 1024;
   const int per_tile = PAIR ? 2 : A.split;
@@ -887,12 +902,19 @@ laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& m
   cfg.blockDim = dim3(kGemmThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
-  cudaLaunchAttribute at[1];
-  at[0].id = cudaLaunchAttributeClusterDimension;
-  at[0].val.clusterDim.x = (unsigned)per_tile;
-  at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+  cudaLaunchAttribute at[2];
   cfg.attrs = at;
-  cfg.numAttrs = per_tile > 1 ? 1 : 0;
+  if (per_tile > 1) {
+    at[cfg.numAttrs].id = cudaLaunchAttributeClusterDimension;
+    at[cfg.numAttrs].val.clusterDim.x = (unsigned)per_tile;
+    at[cfg.numAttrs].val.clusterDim.y = at[cfg.numAttrs].val.clusterDim.z = 1;
+    ++cfg.numAttrs;
+  }
+  if (follows) {
+    at[cfg.numAttrs].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
+    ++cfg.numAttrs;
+  }
   const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, ma, mb, A);
   if (rc != cudaSuccess) {
     cudaGetLastError();
@@ -903,10 +925,13 @@ laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& m
 
 template <class T>
 laq_status launch_form(const Err& e, const Plan& pl, bool out32, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A,
-                       cudaStream_t st) {
-  if (out32) return pl.pair ? launch_gemm<T, false, true, true>(e, ma, mb, A, st) : launch_gemm<T, false, false, true>(e, ma, mb, A, st);
-  if (pl.pair) return launch_gemm<T, false, true, false>(e, ma, mb, A, st);
-  return pl.swap ? launch_gemm<T, true, false, false>(e, ma, mb, A, st) : launch_gemm<T, false, false, false>(e, ma, mb, A, st);
+                       bool follows, cudaStream_t st) {
+  if (out32)
+    return pl.pair ? launch_gemm<T, false, true, true>(e, ma, mb, A, follows, st)
+                   : launch_gemm<T, false, false, true>(e, ma, mb, A, follows, st);
+  if (pl.pair) return launch_gemm<T, false, true, false>(e, ma, mb, A, follows, st);
+  return pl.swap ? launch_gemm<T, true, false, false>(e, ma, mb, A, follows, st)
+                 : launch_gemm<T, false, false, false>(e, ma, mb, A, follows, st);
 }
 
 struct Epilogue {
@@ -919,9 +944,10 @@ struct Epilogue {
   long long ldz = 0;
 };
 
-// D[i][j] = sum_r A(i, r) B(j, r): a_mn ? A is stored [r][i] : [i][r], the same for B.  Both are mappable.
+// D[i][j] = sum_r A(i, r) B(j, r): a_mn ? A is stored [r][i] : [i][r], the same for B.  Both are mappable.  `follows`: the
+// stream's last work is a kernel of the same call.
 laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const Operand& b, bool b_mn, const Epilogue& ep,
-                   uint32_t* status, int starve, bool swappable, cudaStream_t st) {
+                   uint32_t* status, int starve, bool swappable, bool follows, cudaStream_t st) {
   const long long I = a_mn ? a.cols : a.rows, R = a_mn ? a.rows : a.cols, J = b_mn ? b.cols : b.rows;
   const Plan pl = make_plan(I, J, R, a_mn, b_mn, swappable, ep.out_f32 != 0);
   const Operand& A0 = pl.swap ? b : a;
@@ -954,8 +980,8 @@ laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const O
   A.bias = ep.bias;
   A.residual = ep.residual;
   A.status = status;
-  return dtype == LAQ_BF16 ? launch_form<__nv_bfloat16>(e, pl, ep.out_f32 != 0, ma, mb, A, st)
-                           : launch_form<__half>(e, pl, ep.out_f32 != 0, ma, mb, A, st);
+  return dtype == LAQ_BF16 ? launch_form<__nv_bfloat16>(e, pl, ep.out_f32 != 0, ma, mb, A, follows, st)
+                           : launch_form<__half>(e, pl, ep.out_f32 != 0, ma, mb, A, follows, st);
 }
 
 // Copies an operand that a tensor map cannot describe to `ws` (advanced past it).
@@ -1075,7 +1101,8 @@ extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_works
   ep.ldr = c->ld_residual;
   ep.z = c->z;
   ep.ldz = c->ld_z;
-  return product(e, c->dtype, x, false, w, false, ep, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, st);
+  return product(e, c->dtype, x, false, w, false, ep, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, ws != d_workspace,
+                 st);
 }
 
 extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream,
@@ -1108,6 +1135,7 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
   BackwardNeeds need(c);
   char* ws = (char*)d_workspace;
   const bool starve = (c->flags & LAQ_LINEAR_STARVE) != 0;
+  bool follows = false;                   // a kernel of this call was the last thing put on the stream
   if (need.own_dz || c->db) {
     void* dz = need.own_dz ? ws : nullptr;
     float* part = c->db ? (float*)(ws + need.dz_bytes) : nullptr;
@@ -1123,9 +1151,21 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
       linear_dz_kernel<__half><<<grid, kDzThreads, 0, st>>>((const __half*)c->dy, c->ld_dy, (const __half*)c->z, c->ld_z, (__half*)dz,
                                                             pad8(c->N), part, c->M, N, c->activation, per, vec_ok);
     if (cudaGetLastError() != cudaSuccess) return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
+    follows = true;
     if (c->db) {
-      linear_db_kernel<<<(unsigned)((c->N + 31) / 32), 1024, 0, st>>>(part, runs, N, c->db);
-      if (cudaGetLastError() != cudaSuccess) return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3((unsigned)((c->N + 31) / 32));
+      cfg.blockDim = dim3(1024);
+      cfg.stream = st;
+      cudaLaunchAttribute at[1];
+      at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+      at[0].val.programmaticStreamSerializationAllowed = 1;
+      cfg.attrs = at;
+      cfg.numAttrs = 1;
+      if (cudaLaunchKernelEx(&cfg, linear_db_kernel, (const float*)part, runs, N, c->db) != cudaSuccess) {
+        cudaGetLastError();
+        return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
+      }
     }
     if (need.own_dz) {
       need.dz.p = dz;
@@ -1133,19 +1173,24 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
     }
   }
   if (c->dx) {
+    const char* before = ws;
     LAQ_TRY(make_mappable(e, need.w, ws, st));
+    follows = follows || ws != before;
     Epilogue ep;
     ep.out = c->dx;
     ep.ldo = c->ld_dx;
-    LAQ_TRY(product(e, c->dtype, need.dz, false, need.w, true, ep, c->status, starve, true, st));
+    LAQ_TRY(product(e, c->dtype, need.dz, false, need.w, true, ep, c->status, starve, true, follows, st));
+    follows = true;
   }
   if (c->dw) {
+    const char* before = ws;
     LAQ_TRY(make_mappable(e, need.x, ws, st));
+    follows = follows || ws != before;
     Epilogue ep;
     ep.out = c->dw;
     ep.ldo = c->ld_dw;
     ep.out_f32 = c->dw_dtype == LAQ_F32;
-    LAQ_TRY(product(e, c->dtype, need.dz, true, need.x, true, ep, c->status, starve, false, st));
+    LAQ_TRY(product(e, c->dtype, need.dz, true, need.x, true, ep, c->status, starve, false, follows, st));
   }
   return LAQ_OK;
 }

@@ -243,6 +243,30 @@ def test_workspaces_streams_and_graphs():
     ops.check_status()
 
 
+@pytest.mark.parametrize("M, N, K", [(64, 200, 784), (257, 133, 205), (2048, 1024, 512), (16, 1024, 2048)])
+def test_calls_without_a_pause(M, N, K):
+    # the kernels of a call, and those of the calls behind it, wait for what they read and for the memory that they reuse
+    w, z, b = (_randn(*s, seed=70 + i, dtype=torch.bfloat16) for i, s in enumerate([(N, K), (M, N), (N,)]))
+    xs = [_randn(M, K, seed=80 + i, dtype=torch.bfloat16) for i in range(3)]
+    dys = [_randn(M, N, seed=90 + i, dtype=torch.bfloat16) for i in range(3)]
+
+    def run(i):
+        g = ops.linear_backward(dys[i], xs[i], w, z=z, activation="gelu")
+        return ops.linear(xs[i], w, b, activation="gelu"), g["dx"], g["dw"], g["db"]
+
+    want = []
+    for i in range(3):
+        torch.cuda.synchronize()
+        want.append(run(i))
+        torch.cuda.synchronize()
+    wrong = torch.zeros((), dtype=torch.int64, device="cuda")
+    for it in range(60):
+        for got, one in zip(run(it % 3), want[it % 3]):
+            wrong += (got != one).sum()
+    assert int(wrong) == 0
+    ops.check_status()
+
+
 def test_first_calls_of_a_process_may_be_captured():
     """Nothing that a first call sets up (shared-memory limits, occupancy, the driver's entry point) disturbs a capture."""
     import os
