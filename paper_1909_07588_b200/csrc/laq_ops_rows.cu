@@ -29,15 +29,14 @@ namespace ops {
 namespace {
 
 constexpr int kBlock = 256;
-constexpr int kHalfBlock = 128;        // block of the forward pass over rows of middling length, when there are many
-constexpr int kHalfVectors = 2048;     // ... up to this many 16-byte vectors
+constexpr int kHalfBlock = 128;        // block of the forward pass when there are many rows
 constexpr int kWarpBlock = 128;        // block of the kernels whose rows belong to one warp each
 constexpr int kWarpRow = 1024;         // longest row that one warp takes
 constexpr int kWarpVectors = 512;      // ... and in 16-byte vectors, where there are many rows
 constexpr int kMaxCluster = 8;
 constexpr int kMaxTopK = 32;
 constexpr int kMaxTeacher = 128;
-constexpr int kBatch = 4;              // vectors of the streaming loop that a thread has in flight
+constexpr int kLogBatch = 2, kBatch = 1 << kLogBatch;  // vectors of the streaming loop that a thread has in flight
 constexpr int kRing = 2;               // batches of the streaming loop's ring
 constexpr int kForwardBlocks = 4;      // blocks of it on an SM (by shared memory: ring and alternatives)
 constexpr float kLog2e = 1.4426950408889634f;
@@ -237,18 +236,22 @@ __device__ __forceinline__ unsigned long long cand_key(uint32_t bits, int j) {
   return ((unsigned long long)bits << 32) | (0xffffffffu - (uint32_t)j);
 }
 
-constexpr int kSlots = 8, kMaxHits = 512;
+constexpr int kMaxHits = 512;
 
-template <int NT>
+template <class T, int NT>
 struct TopShared {
   static constexpr int kCap = NT == 32 ? kCandWarp : kCandBlock;
-  unsigned long long cand[kCap];
+  static constexpr int kSlots = NT == 32 ? 1 : 8192 / (NT * (int)sizeof(T));
+  union {                                      // the slots are done with before the first candidate is named
+    // largest logit of each thread's runs of batches, and behind the last of them that of its other elements
+    alignas(16) T slot[NT == 32 ? 1 : kSlots + 1][NT == 32 ? 16 / sizeof(T) : NT];
+    unsigned long long cand[kCap];
+  };
   unsigned long long best[kMaxTopK];           // the group's own k best, in order
   unsigned long long wmax[Group<NT>::kWarps];
   uint32_t wthr[Group<NT>::kWarps];
   int wcount[Group<NT>::kWarps];
   int n, nhit;
-  float slot[NT == 32 ? 1 : kSlots][NT == 32 ? 1 : NT];      // largest logit of each thread's runs of batches
   uint16_t hit[NT == 32 ? 1 : kMaxHits];
 };
 
@@ -259,12 +262,13 @@ struct Batches {
   int span, shift;
   __device__ __forceinline__ explicit Batches(const Slice<T>& sl) : span(sl.v1 - sl.v0), shift(0) {
     const int most = (span + kBatch * NT - 1) / (kBatch * NT);
-    while ((max(most, 1) - 1) >> shift >= kSlots) ++shift;
+    while ((max(most, 1) - 1) >> shift >= TopShared<T, NT>::kSlots) ++shift;
   }
   __device__ __forceinline__ int of(int t) const {
     const int left = span - t - (kBatch - 1) * NT;
     return left > 0 ? (left + kBatch * NT - 1) / (kBatch * NT) : 0;
   }
+  __device__ __forceinline__ int slots() const { return (of(0) + (1 << shift) - 1) >> shift; }      // of any thread at most
 };
 
 // f(x, index) for the elements of a vector that are at least thr.
@@ -283,7 +287,7 @@ __device__ __forceinline__ void pick(const uint4& v, int j0, float thr, F f) {
 
 // Hands the elements of a vector that are at least thr to the group's candidates, one reservation for all of them.
 template <class T, int NT>
-__device__ __forceinline__ void take_vector(TopShared<NT>& sh, const uint4& v, int j0, float thr) {
+__device__ __forceinline__ void take_vector(TopShared<T, NT>& sh, const uint4& v, int j0, float thr) {
   constexpr int EV = Elem<T>::EV;
   float x[EV];
   Elem<T>::unpack(v, x);
@@ -295,7 +299,7 @@ __device__ __forceinline__ void take_vector(TopShared<NT>& sh, const uint4& v, i
 #pragma unroll
   for (int i = 0; i < EV; ++i)
     if (x[i] >= thr) {
-      if (at < TopShared<NT>::kCap) sh.cand[at] = cand_key(order_bits(x[i]), j0 + i);
+      if (at < TopShared<T, NT>::kCap) sh.cand[at] = cand_key(order_bits(x[i]), j0 + i);
       ++at;
     }
 }
@@ -313,19 +317,20 @@ __device__ __forceinline__ void each_element(const Slice<T>& sl, float thr, F f)
   }
 }
 
-// The k largest of sh.cand[0..n) in order into sh.best (0 where there are fewer): a candidate's place is the number of
-// keys above it.
-template <int NT>
-__device__ __forceinline__ void rank_candidates(TopShared<NT>& sh, int n, int k) {
-  const int t = Group<NT>::tid();
-  for (int i = t; i < k; i += NT) sh.best[i] = 0ull;
-  Group<NT>::sync();
-  for (int i = t; i < n; i += NT) {
-    const unsigned long long key = sh.cand[i];
+// The k largest of sh.cand[0..n) in order into sh.best, which holds zeros: a candidate's place is the number of keys above
+// it, counted by four lanes.
+template <class T, int NT>
+__device__ __forceinline__ void rank_candidates(TopShared<T, NT>& sh, int n, int k) {
+  const int t = Group<NT>::tid(), part = t & 3;
+  for (int i0 = 0; i0 < n; i0 += NT / 4) {
+    const int i = i0 + (t >> 2);
+    const unsigned long long key = i < n ? sh.cand[i] : 0ull;
     int place = 0;
 #pragma unroll 4
-    for (int j = 0; j < n; ++j) place += sh.cand[j] > key;
-    if (place < k && key) sh.best[place] = key;
+    for (int j = part; j < n; j += 4) place += sh.cand[j] > key;
+    place += __shfl_xor_sync(0xffffffffu, place, 1);
+    place += __shfl_xor_sync(0xffffffffu, place, 2);
+    if (part == 0 && place < k && key) sh.best[place] = key;
   }
   Group<NT>::sync();
 }
@@ -336,13 +341,14 @@ __device__ __forceinline__ void rank_candidates(TopShared<NT>& sh, int n, int k)
 // Threshold: every warp names its ceil(k / warps)-th largest of its lanes' maxima; the smallest of those has at least k
 // elements at or above it, so only the elements that reach it can be among the k best, typically some dozens.  The
 // batches that hold them are known from the slots' maxima: the block lists those and reads them once more (from L2), a
-// vector a thread, instead of every thread its whole part.  When more than kCap elements (or kMaxHits runs) reach the
+// vector a thread, instead of every thread its whole part.  (Four vectors a thread under way at a time are slower, 16384 x
+// 16384 bf16 with 20 alternatives 148 -> 160 us: what counts in a selection is its instructions.)  When more than kCap elements (or kMaxHits runs) reach the
 // threshold (thousands of equal logits), elements above it are taken first and the ones equal to it by a scan in index order
 // that ends as soon as enough are found; and when even too many lie above it, k rounds of an arg-max do it.
 template <class T, int NT>
-__device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, const uint4* ring, float top, float rest, int k) {
+__device__ void top_of_slice(TopShared<T, NT>& sh, const Slice<T>& sl, const uint4* ring, float top, float rest, int k) {
   using G = Group<NT>;
-  constexpr int kCap = TopShared<NT>::kCap;
+  constexpr int kCap = TopShared<T, NT>::kCap;
   const int t = G::tid(), lane = threadIdx.x & 31, w = NT == 32 ? 0 : (int)(threadIdx.x >> 5);
   const uint32_t mine = order_bits(top);
   uint32_t left = mine, key = 0;
@@ -352,6 +358,7 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, const uint4*
     if (lane == __ffs(who) - 1) left = 0;
   }
   if (t == 0) sh.n = sh.nhit = 0;
+  for (int i = t; i < k; i += NT) sh.best[i] = 0ull;
   if (lane == 0) sh.wthr[w] = key;
   G::sync();
   key = sh.wthr[0];
@@ -368,24 +375,20 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, const uint4*
     G::sync();
   } else {
     const Batches<T, NT> bt(sl);
-    if (mine >= key) {
-      const int slots = (bt.of(t) + (1 << bt.shift) - 1) >> bt.shift;
-      for (int i = 0; i <= slots; ++i) {
-        const bool last = i == slots;
-        if ((last ? rest : sh.slot[i][t]) >= thr) {
-          const int at = atomicAdd(&sh.nhit, 1);
-          if (at < kMaxHits) sh.hit[at] = (uint16_t)((last ? kSlots : i) << 8 | t);
-        }
-      }
-    }
+    const int slots = bt.slots();
+    for (int i = t; i < (slots + 1) * (NT / Elem<T>::EV); i += NT)
+      pick<T>(*reinterpret_cast<const uint4*>(&sh.slot[0][i * Elem<T>::EV]), i * Elem<T>::EV, thr, [&](float, int j) {
+        const int at = atomicAdd(&sh.nhit, 1);
+        if (at < kMaxHits) sh.hit[at] = (uint16_t)j;
+      });
     __syncthreads();
-    const int hits = sh.nhit, per = kBatch << bt.shift;
+    const int hits = sh.nhit, log_per = kLogBatch + bt.shift;
     if (hits <= kMaxHits) {
-      for (int i = t; i < hits * per; i += NT) {
-        const int h = sh.hit[i / per], in = i % per, who = h & 255, slot = h >> 8, mb = bt.of(who);
-        const int batch = slot == kSlots ? mb : (slot << bt.shift) + in / kBatch;
-        if (slot == kSlots ? in >= kBatch : batch >= mb) continue;
-        if (slot == kSlots && in == kBatch - 1) {          // the rest has at most kBatch - 1 vectors, and the edge
+      for (int i = t; i < hits << log_per; i += NT) {
+        const int h = sh.hit[i >> log_per], in = i & ((1 << log_per) - 1), who = h % NT, slot = h / NT, mb = bt.of(who);
+        const int batch = slot == slots ? mb : (slot << bt.shift) + in / kBatch;
+        if (slot == slots ? in >= kBatch : batch >= mb) continue;
+        if (slot == slots && in == kBatch - 1) {          // the rest has at most kBatch - 1 vectors, and the edge
           const int j = sl.edge(who);
           if (j >= 0) {
             const float x = Elem<T>::to_float(sl.row[j]);
@@ -396,7 +399,7 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, const uint4*
         const int v = sl.v0 + who + NT * (kBatch * batch + in % kBatch);
         // the last batches are still in the ring
         if (v < sl.v1)
-          take_vector<T, NT>(sh, slot != kSlots && batch + kRing >= mb ? ring[((batch % kRing) * kBatch + in % kBatch) * NT + who] : load16(sl.vec(v)),
+          take_vector<T, NT>(sh, slot != slots && batch + kRing >= mb ? ring[((batch % kRing) * kBatch + in % kBatch) * NT + who] : load16(sl.vec(v)),
                              sl.head + v * Elem<T>::EV, thr);
       }
     } else if (t == 0) {
@@ -458,7 +461,7 @@ __device__ void top_of_slice(TopShared<NT>& sh, const Slice<T>& sl, const uint4*
       }
     }
   }
-  rank_candidates<NT>(sh, n, k);
+  rank_candidates<T, NT>(sh, n, k);
 }
 
 // ---- the teacher's side of one row ------------------------------------------------------------------------------------
@@ -621,16 +624,21 @@ struct ForwardArgs {
 //
 // Per element of 16 bits: half a comparison for the maximum, half for the bound, one unpacking, one ex2 and one and a half
 // fused operations, 7.3 instructions with everything around them; memory and the special-function unit (8 cycles a warp's
-// ex2) are both near their limits, so what counts is that enough is under way: four blocks an SM, each thread two batches
-// of 64 bytes through shared memory.  4096 rows of 131072 bf16: 168 us, 6.4 TB/s (0.98 of the measured copy rate); with 20
-// alternatives 196 us (0.84): the selection after a row leaves its block without loads for about 3 us.  (Three batches and
-// three blocks: 177 and 209 us; two vectors a batch, five blocks: 191 and 229 us; vectors straight to registers: 241 us.)
-// Rows of one warp and of a block of 128 threads exist for short rows: a block's barriers and the selection cost a row about
-// 5 us whatever its length (32768 rows of 8192 bf16, 8 alternatives: 371 us by blocks of 256, 193 us by 128).
+// ex2) are both near their limits, so what counts is that enough is under way: eight blocks of 128 threads or four of 256 an
+// SM, each thread two batches of 64 bytes through shared memory.  4096 rows of 131072 bf16: 162 us, 6.6 TB/s (1.01 of the
+// measured copy rate); with 20 alternatives 181 us (0.91): the selection after a row leaves its block without loads for about
+// 3 us.  (With blocks of 256, three batches and three blocks: 177 and 209 us; two vectors a batch, five blocks: 191 and 229 us;
+// vectors straight to registers: 241 us.  Blocks that stay and have the next row's first batch under way during the selection:
+// 204 and 225 us, since rows are then dealt out beforehand and the loop needs more instructions.)
+//
+// A row's selection and joins cost its block about 5 us whatever its length, and smaller blocks leave more of the others
+// streaming meanwhile: where every SM has eight rows, blocks of 128 (us by 256 and by 128 threads: 4096 x 131072 bf16 168 and
+// 162, with 20 alternatives 190 and 181; 6000 x 20000 bf16 65 and 53, 107 and 77; 2368 x 32000 fp32 58 and 55, 73 and 64; a
+// little more than one round of them loses, 1400 x 131072 bf16 66 and 72).  Rows of one warp exist for short rows.
 template <class T, int NT, bool DISTILL>
 __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kForwardBlocks * kBlock / NT) rows_forward_kernel(const ForwardArgs A) {
   using G = Group<NT>;
-  __shared__ TopShared<NT> top_sh[DISTILL ? 1 : G::kRowsPerBlock];
+  __shared__ TopShared<T, NT> top_sh[DISTILL ? 1 : G::kRowsPerBlock];
   __shared__ Teacher teacher_sh[DISTILL ? G::kRowsPerBlock : 1];
   __shared__ Stat wstat[G::kRowsPerBlock][G::kWarps];
   const int t = G::tid(), lane = threadIdx.x & 31, w = NT == 32 ? 0 : (int)(threadIdx.x >> 5);
@@ -638,7 +646,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kFo
   const int rank = NT == 32 ? 0 : (int)(blockIdx.x % (unsigned)ranks);
   const long long row = NT == 32 ? (long long)blockIdx.x * G::kRowsPerBlock + G::slot() : (long long)(blockIdx.x / (unsigned)ranks);
   if (NT == 32 && row >= A.T) return;
-  TopShared<NT>& sh = top_sh[DISTILL ? 0 : G::slot()];
+  TopShared<T, NT>& sh = top_sh[DISTILL ? 0 : G::slot()];
   Teacher& te = teacher_sh[DISTILL ? G::slot() : 0];
   const T* xr = reinterpret_cast<const T*>(A.x) + row * A.ld;
   const int k = DISTILL ? 0 : A.k;
@@ -695,7 +703,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kFo
       run.add(x);
       if (NT > 32 && k > 0) {
         high = max_nan(high, mx);
-        sh.slot[b >> bt.shift][t] = high;
+        sh.slot[b >> bt.shift][t] = Elem<T>::from_float(high);
         if (((b + 1) & ((1 << bt.shift) - 1)) == 0) high = -INFINITY;
       }
       top = max_nan(top, mx);
@@ -720,6 +728,11 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kFo
       run.one(e);
     }
     top = max_nan(top, rest);
+    if (NT > 32 && k > 0) {
+      const int slots = bt.slots();
+      for (int i = (batches + (1 << bt.shift) - 1) >> bt.shift; i < slots; ++i) sh.slot[i][t] = Elem<T>::from_float(-INFINITY);
+      sh.slot[slots][t] = Elem<T>::from_float(rest);
+    }
   }
   if (NT > 32) copy_wait<0>();           // of a row that was not looked at
   Stat a = warp_join<32, !DISTILL>(run.get(), c);
@@ -741,11 +754,13 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : NT, NT == 32 ? 8 : kFo
         if (t < ranks * kMaxTopK && t % kMaxTopK < k)
           sh.cand[t / kMaxTopK * k + t % kMaxTopK] = cluster.map_shared_rank(sh.best, t / kMaxTopK)[t % kMaxTopK];
         __syncthreads();
+        for (int i = t; i < k; i += NT) sh.best[i] = 0ull;
+        __syncthreads();
       }
     }
     cluster.sync();
     if (rank != 0) return;
-    if (alternatives) rank_candidates<NT>(sh, ranks * k, k);
+    if (alternatives) rank_candidates<T, NT>(sh, ranks * k, k);
   }
   const RowSum r(a, c, A.unit, A.inv_tau);
   if (DISTILL) {
@@ -1307,7 +1322,7 @@ cudaError_t forward(ForwardArgs& A, cudaStream_t st) {
     return launch(rows_forward_kernel<T, 32, DISTILL>, A, (A.T + 3) / 4, kWarpBlock, 0, 1, st);
   }
   const long long nvec = A.V / Elem<T>::EV;
-  if (nvec <= kHalfVectors && A.T >= 2 * kForwardBlocks * kSMs) {
+  if (A.T >= 2 * kForwardBlocks * kSMs) {
     A.ranks = 1;
     A.per = (int)nvec;
     return launch(rows_forward_kernel<T, kHalfBlock, DISTILL>, A, A.T, kHalfBlock, (size_t)kRing * kBatch * kHalfBlock * 16, 1, st);

@@ -43,6 +43,8 @@ def _sum_bound(s):
 
 def _close(got, want, bound, what):
     got, want = got.double(), want.double()
+    # what fp32 cannot hold rounds to an infinity: 2^128 (1 - 2^-25) lies halfway between its largest number and 2^128
+    want = torch.where(want.abs() >= 2.0 ** 128 * (1 - 2.0 ** -25), want.sign() * INF, want)
     same = torch.where(want.isnan(), got.isnan(), torch.where(want.isinf(), got == want, torch.ones_like(want, dtype=torch.bool)))
     assert bool(same.all()), what
     fine = want.isfinite()
@@ -136,6 +138,40 @@ def test_alternatives_among_equal_logits(V, dtype):
     x = torch.stack(rows).to("cuda").to(DTYPES[dtype])
     for k in (1, 8, 32):
         _check_forward(x, None, k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T, V", [(1184, 33001), (1300, 2111), (1250, 16421)])
+def test_forward_of_many_rows(T, V, dtype):
+    """Rows of small blocks, each with rows of its own kind among them: equal logits, masks, nothing left, not a number."""
+    x = _logits(T, V, dtype, seed=T)
+    j = torch.arange(V, device="cuda")
+    x[3] = 1.0
+    x[4] = (j % 3).to(x.dtype)
+    x[5] = torch.where(j >= V - 3, 2.0, 1.0).to(x.dtype)
+    x[6] = -INF
+    x[7, : V - 5] = -INF
+    x[8, 5:] = -INF
+    x[9] = torch.finfo(x.dtype).min
+    x[10, 17] = math.nan
+    x[11] = torch.where(j % 128 == 127, 0.01 * (j // 128 % 89), -1.0).to(x.dtype)
+    x[12, :-1] = -INF
+    tokens = torch.randint(0, V, (T,), generator=_gen(5), device="cuda").int()
+    tokens[::7] = -1
+    for k, tau in ((0, 1.0), (3, 0.7), (32, 1.0)):
+        _check_forward(x, tokens, k, tau)
+        _check_forward(x[:, 1:V - 1], None, k, tau)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+def test_alternatives_of_many_long_rows(dtype):
+    x = _logits(8, 140000, dtype, seed=8)
+    x[1] = 0.5
+    x[2] = torch.where(torch.arange(140000, device="cuda") % 1024 < 8, 3.0, 1.0).to(x.dtype)
+    for k in (1, 20, 32):
+        want = _check_forward(x, None, k)
+        got = ops.token_logprobs(x.repeat(150, 1), None, top_k=k)
+        assert torch.equal(got["top_tokens"], want["top_tokens"].repeat(150, 1))
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
