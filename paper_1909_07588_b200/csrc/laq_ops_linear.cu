@@ -13,12 +13,13 @@
 // pair loads its own 128 rows of A and half of B's columns, 32 KB for the work that a lone SM loads 48 KB for, and what an
 // SM takes from L2 is what bounds the lone form.  8192 x 4096 x 4096 bf16: 189 us, 1.45 PFLOP/s (0.90 of the measured library
 // rate); with gelu and residual 200 us.  What is left is the L2's rate (with a quarter of the products 160 us) and the
-// last wave.  For few rows the roles of the operands are swapped (W's rows fill the 128
-// lanes, the rows of X are the narrow side) and the summed axis is split over a thread-block cluster whose blocks join
-// their partial tiles through distributed shared memory in a fixed order.
+// last wave.  One to four rows of X are plain dot products (linear_few_rows_kernel).  For some more the roles of the
+// operands are swapped (W's rows fill the 128 lanes, the rows of X are the narrow side) and the summed axis is split over a
+// thread-block cluster whose blocks join their partial tiles through distributed shared memory in a fixed order.
 #include <cooperative_groups.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "laq_ops.cuh"
 #include "laq_umma_gemm.cuh"
@@ -35,6 +36,8 @@ using umma::kTileM;
 constexpr int kSMs = 148;
 constexpr int kGemmThreads = 320;         // loader, tensor-core warp, eight epilogue warps
 constexpr int kEpiWarps = 8;
+constexpr int kFewRows = 4;               // rows of X that plain dot products take
+constexpr int kFewCols = 4, kFewThreads = 128, kFewBlocks = 4;   // columns of a warp, threads of a block, blocks on an SM
 constexpr int kMaxStages = 12;
 constexpr int kMaxRing = 192 * 1024;      // bytes of the stage ring
 constexpr int kStaging = kEpiWarps * 4096;   // ... and of the epilogue warps' pieces behind it
@@ -773,6 +776,112 @@ __global__ void __launch_bounds__(1024) linear_db_kernel(const float* part, int 
   if (tx == 0 && blockIdx.x * 32 + ty < N) db[blockIdx.x * 32 + ty] = t;
 }
 
+// One to four rows: W is read once and nothing is used twice, so memory bounds it and plain dot products keep up.  A warp
+// takes four columns of Y (rows of W) and all or, of few columns, a part of the summed axis: the block's warps that share
+// columns join through shared memory in a fixed order.  A warp's sums are folded so that each step halves the values a lane
+// holds.  Each lane has AHEAD vectors of each of its four rows of W under way; X comes from the first-level cache.
+//
+// In us, by this kernel and by the tensor cores' (bias, silu and residual, weights that the L2 cache does not hold, launches
+// in a row):
+//   N x K        4096 x 4096    11008 x 4096    4096 x 11008    32000 x 2048    100000 x 512    200 x 784
+//   1 row          7.4  12.8       16.4  25.6      16.5  23.5      22.1  30.8      19.5  24.9     2.3   7.9
+//   2 rows         8.8  13.6       19.8  26.0      18.5  24.0      26.0  30.5      24.6  26.1     2.5   7.9
+//   4 rows        10.5  13.6       23.9  26.0      21.6  24.3      30.6  31.2      32.8  26.2     2.7   8.0
+// W is marked as read once: weights that stay in the L2 cache are not slower for it (4096 x 4096 6.3 us either way), and
+// those that do not are faster (32000 x 2048, one row: 23.6 -> 22.1).
+// (Blocks of 256 threads are dealt out less evenly, 11008 x 4096, one row: 19.5 us; vectors of X loaded ahead as well cost
+// the registers that more vectors of W need, 4096 x 4096: 8.8 us.)
+template <class T, int ROWS, int AHEAD>
+__global__ void __launch_bounds__(kFewThreads, ROWS <= 2 && AHEAD == 2 ? kFewBlocks + 2 : kFewBlocks)
+    linear_few_rows_kernel(const GemmArgs A, const T* x, long long ldx, const T* w, long long ldw, int K, int vec, int log_parts) {
+  constexpr int kRows2 = ROWS == 3 ? 4 : ROWS, kSums = kFewCols * kRows2, kWarps = kFewThreads / 32;
+  __shared__ float part[kWarps][kSums];
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, parts = 1 << log_parts;
+  const int col0 = (int)(blockIdx.x * (unsigned)(kWarps >> log_parts)) * kFewCols;
+  const int first = (warp & (parts - 1)) * 32 + lane, step = 32 << log_parts;
+  const T* wr[kFewCols];
+#pragma unroll
+  for (int c = 0; c < kFewCols; ++c) wr[c] = w + (long long)min(col0 + (warp >> log_parts) * kFewCols + c, A.J - 1) * ldw;
+  f32x2 sum[kFewCols][ROWS];
+#pragma unroll
+  for (int c = 0; c < kFewCols; ++c)
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m) sum[c][m] = 0ull;
+  const int nv = vec ? K / 8 : 0;                  // of the summed axis in vectors
+  auto batch = [&](int v0, auto whole) {           // whole: all of its vectors exist
+    uint4 a[AHEAD][kFewCols];
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int v = v0 + u * step;
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c)
+        a[u][c] = decltype(whole)::value || v < nv ? __ldcs(reinterpret_cast<const uint4*>(wr[c]) + v) : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      const int v = v0 + u * step;
+      f32x2 q[ROWS][4];
+#pragma unroll
+      for (int m = 0; m < ROWS; ++m)               // nothing of X where there is nothing of W: zero times an infinity would count
+        Elem<T>::pairs(decltype(whole)::value || v < nv ? __ldg(reinterpret_cast<const uint4*>(x + m * ldx) + v) : make_uint4(0u, 0u, 0u, 0u), q[m]);
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c) {
+        f32x2 p[4];
+        Elem<T>::pairs(a[u][c], p);
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[c][m] = fma2(p[e], q[m][e], sum[c][m]);
+      }
+    }
+  };
+  int v0 = first;
+  for (; v0 + (AHEAD - 1) * step < nv; v0 += AHEAD * step) batch(v0, std::true_type());
+  if (v0 < nv) batch(v0, std::false_type());
+  float s[kSums];
+#pragma unroll
+  for (int c = 0; c < kFewCols; ++c)
+#pragma unroll
+    for (int m = 0; m < kRows2; ++m) {
+      float lo = 0.f, hi = 0.f;
+      if (m < ROWS) split(sum[c][m < ROWS ? m : 0], lo, hi);
+      s[c * kRows2 + m] = lo + hi;
+    }
+#pragma unroll 4
+  for (int k = nv * 8 + first; k < K; k += step) {
+    float q[ROWS];
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m) q[m] = Elem<T>::to_float(x[m * ldx + k]);
+#pragma unroll
+    for (int c = 0; c < kFewCols; ++c) {
+      const float p = Elem<T>::to_float(wr[c][k]);
+#pragma unroll
+      for (int m = 0; m < ROWS; ++m) s[c * kRows2 + m] = fmaf(p, q[m], s[c * kRows2 + m]);
+    }
+  }
+  int o = 16;
+#pragma unroll
+  for (int n = kSums / 2; n > 0; n /= 2, o /= 2) {          // lanes with bit o keep the upper half of the sums
+    const bool upper = lane & o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const float other = __shfl_xor_sync(0xffffffffu, upper ? s[i] : s[i + n], o);
+      s[i] = (upper ? s[i + n] : s[i]) + other;
+    }
+  }
+#pragma unroll
+  for (; o > 0; o /= 2) s[0] += __shfl_xor_sync(0xffffffffu, s[0], o);
+  if (lane % (32 / kSums) == 0) part[warp][lane / (32 / kSums)] = s[0];
+  __syncthreads();
+  if (t < kFewCols * kWarps >> log_parts) {
+    float y[8] = {};
+    for (int i = 0; i < parts; ++i)
+#pragma unroll
+      for (int m = 0; m < ROWS; ++m) y[m] += part[(t / kFewCols << log_parts) + i][t % kFewCols * kRows2 + m];
+    finish_column<T, false>(A, A.I, A.J, 0, col0 + t, y);
+  }
+}
+
 // Rows that a tensor map cannot describe (an address or a row pitch that is no multiple of 16 bytes) are copied once
 // into the workspace with a pitch of a multiple of eight elements.
 __global__ void __launch_bounds__(256) linear_pack_kernel(const uint16_t* src, long long ld, uint16_t* dst, long long pitch,
@@ -984,6 +1093,66 @@ laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const O
                            : launch_form<__half>(e, pl, ep.out_f32 != 0, ma, mb, A, follows, st);
 }
 
+// Warps that share four columns: as many as fill the rounds of resident warps best, the fewer the better within a quarter
+// (4096 x 4096, one row: two 7.4 us, four 8.2 us; 11008 x 4096: one 18.5 us, two 16.7 us).
+int few_log_parts(long long groups, int items) {
+  const long long resident = (long long)kFewThreads / 32 * kFewBlocks * kSMs;
+  double best = 0.0;
+  int pick = 0;
+  for (int lp = 0; 1 << lp <= kFewThreads / 32 && (lp == 0 || items > 16 << lp); ++lp) {
+    const long long warps = groups << lp, rounds = (warps + resident - 1) / resident;
+    const double full = (double)warps / (double)(rounds * resident);
+    if (full > 1.25 * best) {
+      best = full;
+      pick = lp;
+    }
+  }
+  return pick;
+}
+
+template <class T, int ROWS>
+laq_status launch_few(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
+  const int K = (int)x.cols, vec = x.mappable_() && w.mappable_(), items = vec ? K / 8 : K;
+  const long long groups = (w.rows + kFewCols - 1) / kFewCols;
+  const int log_parts = few_log_parts(groups, items), per_block = kFewThreads / 32 >> log_parts;
+  const unsigned blocks = (unsigned)((groups + per_block - 1) / per_block);
+  // Four vectors of each row of W under way where a lane has as many and the registers hold them (one row, 4096 x 4096: 7.4 us
+  // against 8.7 us by two; 100000 x 512, where a lane has two: 26.7 us against 19.7 us).
+  if (ROWS <= 2 && items > 64 << log_parts)
+    linear_few_rows_kernel<T, ROWS, ROWS <= 2 ? 4 : 2><<<blocks, kFewThreads, 0, st>>>(A, (const T*)x.p, x.ld, (const T*)w.p, w.ld, K, vec, log_parts);
+  else
+    linear_few_rows_kernel<T, ROWS, 2><<<blocks, kFewThreads, 0, st>>>(A, (const T*)x.p, x.ld, (const T*)w.p, w.ld, K, vec, log_parts);
+  return cudaGetLastError() == cudaSuccess ? LAQ_OK : fail(e.buf, e.len, LAQ_ECUDA, "kernel launch failed");
+}
+
+template <class T>
+laq_status few_rows(const Err& e, const Operand& x, const Operand& w, const Epilogue& ep, cudaStream_t st) {
+  GemmArgs A = {};
+  A.I = (int)x.rows;
+  A.J = (int)w.rows;
+  A.act = ep.act;
+  A.out = ep.out;
+  A.ldo = ep.ldo;
+  A.z = ep.z;
+  A.ldz = ep.ldz;
+  A.bias = ep.bias;
+  A.residual = ep.residual;
+  A.ldr = ep.ldr;
+  switch (x.rows) {
+    case 1: return launch_few<T, 1>(e, A, x, w, st);
+    case 2: return launch_few<T, 2>(e, A, x, w, st);
+    case 3: return launch_few<T, 3>(e, A, x, w, st);
+    default: return launch_few<T, 4>(e, A, x, w, st);
+  }
+}
+
+// One or two rows always; three or four unless there are many short columns, where folding the sums costs more than the
+// products (100000 x 512: 33 us, by the tensor cores 27 us).
+bool takes_few_rows(const laq_linear_call* c) {
+  if (c->flags & LAQ_LINEAR_STARVE) return false;
+  return c->M <= 2 || (c->M <= kFewRows && (c->K >= 1024 || c->N <= kFewCols * kFewThreads / 32 * kFewBlocks * kSMs));
+}
+
 // Copies an operand that a tensor map cannot describe to `ws` (advanced past it).
 laq_status make_mappable(const Err& e, Operand& o, char*& ws, cudaStream_t st) {
   const size_t bytes = o.pack_bytes();
@@ -1073,6 +1242,7 @@ using namespace laq::ops;
 extern "C" size_t laq_linear_workspace_bytes(const laq_linear_call* c, int32_t backward) {
   if (!sizes_ok(c)) return 0;
   if (backward) return BackwardNeeds(c).bytes(c);
+  if (takes_few_rows(c)) return 0;
   return Operand{c->x, c->ld_x, c->M, c->K}.pack_bytes() + Operand{c->w, c->ld_w, c->N, c->K}.pack_bytes();
 }
 
@@ -1090,8 +1260,6 @@ extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_works
   cudaStream_t st = (cudaStream_t)cuda_stream;
   char* ws = (char*)d_workspace;
   Operand x{c->x, c->ld_x, c->M, c->K}, w{c->w, c->ld_w, c->N, c->K};
-  LAQ_TRY(make_mappable(e, x, ws, st));
-  LAQ_TRY(make_mappable(e, w, ws, st));
   Epilogue ep;
   ep.out = c->y;
   ep.ldo = c->ld_y;
@@ -1101,6 +1269,10 @@ extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_works
   ep.ldr = c->ld_residual;
   ep.z = c->z;
   ep.ldz = c->ld_z;
+  if (takes_few_rows(c))
+    return c->dtype == LAQ_BF16 ? few_rows<__nv_bfloat16>(e, x, w, ep, st) : few_rows<__half>(e, x, w, ep, st);
+  LAQ_TRY(make_mappable(e, x, ws, st));
+  LAQ_TRY(make_mappable(e, w, ws, st));
   return product(e, c->dtype, x, false, w, false, ep, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, ws != d_workspace,
                  st);
 }

@@ -243,6 +243,44 @@ def test_workspaces_streams_and_graphs():
     ops.check_status()
 
 
+FEW = [(1, 1), (3, 2), (5, 7), (4, 8), (17, 9), (130, 64), (10, 784), (200, 785), (131, 1000), (300, 2056), (1026, 4099), (4096, 512),
+       (9472, 520), (9473, 512), (9477, 1024), (19001, 263)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("N, K", FEW)
+def test_forward_of_few_rows(N, K, dtype):
+    dt = DTYPES[dtype]
+    for M in (1, 2, 3, 4, 5):
+        x, w = _randn(M, K, seed=1, dtype=dt), _randn(N, K, seed=2, dtype=dt, scale=K ** -0.5)
+        b, r = _randn(N, seed=3, dtype=dt), _randn(M, N, seed=4, dtype=dt)
+        for act, bias, res in (("none", None, None), ("gelu", b, r), ("silu", b, None)):
+            _check_forward(x, w, bias, act, res)
+        # columns of wider matrices: rows that start at any element, and rows that start at vectors
+        for at in (1, 8):
+            wide = _randn(N, K + 24, seed=5, dtype=dt, scale=K ** -0.5)
+            xs = _randn(M, K + 24, seed=6, dtype=dt)
+            _check_forward(xs[:, at:at + K], wide[:, at:at + K], b, "relu", r)
+    ops.check_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("K", [8, 264, 1000, 4097])
+def test_few_rows_with_infinities(K, dtype):
+    """An infinity gives infinities, or what is not a number where it meets a zero, in its own row and nowhere else."""
+    dt = DTYPES[dtype]
+    w = _randn(37, K, seed=2, dtype=dt).abs() + 0.5
+    for M in (1, 2, 3, 4):
+        for at in (0, K // 2, K - 1):
+            x = _randn(M, K, seed=1, dtype=dt)
+            x[0, at] = -math.inf
+            w[5, at] = 0.0
+            y = ops.linear(x, w)
+            assert bool(y[0, 5].isnan()) and bool((y[0, :5] == -math.inf).all()) and bool((y[0, 6:] == -math.inf).all())
+            assert bool(y[1:].isfinite().all())
+            w[5, at] = 1.0
+
+
 @pytest.mark.parametrize("M, N, K", [(64, 200, 784), (257, 133, 205), (2048, 1024, 512), (16, 1024, 2048)])
 def test_calls_without_a_pause(M, N, K):
     # the kernels of a call, and those of the calls behind it, wait for what they read and for the memory that they reuse
