@@ -86,23 +86,27 @@ struct Slice {
 // ---- running softmax statistics ---------------------------------------------------------------------------------------
 // d = (x - ref) c with c = log2(e) / tau;  s = sum 2^d, u = sum d 2^d.  ref is any number that no x exceeds by more than
 // kSlack / c: it moves only when it must, so the common path has no rescaling.  Two forms of d:
-//   |ref| < kFar   x c - rho with rho = fp32(ref c): one fused operation.  rho itself is the reference then, so its
-//                  rounding does not matter; c's rounding is a change of temperature by 2^-25, the same for all.
-//   otherwise      (x - ref) c.  Such a ref is a mask at the type's lowest value (nothing else has been seen), whose product
-//                  with c may overflow.  A NaN or +inf also ends here and stays.
-constexpr float kFar = 1e30f;
+//   |ref c| < kNear   x c - rho with rho = fp32(ref c): one fused operation.  rho itself is the reference then, at most a
+//                     quarter of a power of two from ref c; c's rounding is a change of temperature by 2^-25, the same for all.
+//   otherwise         (x - ref) c, exact up to two roundings of d itself.  Such a ref is a finite mask (-1e9, -1e10, the type's
+//                     lowest value: nothing else has been seen), whose product with c is rounded by many powers of two or
+//                     overflows: as a reference, rho would be off by as much.  A NaN or +inf also ends here and stays.
+constexpr float kNear = 4194304.f;     // 2^22
 
 struct Stat {
   float ref, s, u;
 };
 
-__device__ __forceinline__ bool near_ref(float ref) { return fabsf(ref) < kFar; }
+__device__ __forceinline__ bool near_ref(float ref, float c) { return fabsf(ref * c) < kNear; }
 __device__ __forceinline__ float scaled(float x, float ref, float c) {
-  return near_ref(ref) ? fmaf(x, c, -(ref * c)) : (x - ref) * c;
+  return near_ref(ref, c) ? fmaf(x, c, -(ref * c)) : (x - ref) * c;
 }
 
 __device__ __forceinline__ void move_ref(Stat& a, float ref, float c) {    // ref >= a.ref, or NaN
-  float d = near_ref(ref) && near_ref(a.ref) ? a.ref * c - ref * c : (a.ref - ref) * c;
+  // from where a's sums stand (rho or a.ref c, by its own form) to where the new reference's will
+  float d;
+  if (near_ref(ref, c)) d = near_ref(a.ref, c) ? a.ref * c - ref * c : fmaf(a.ref, c, -(ref * c));
+  else d = near_ref(a.ref, c) ? -fmaf(ref, c, -(a.ref * c)) : (a.ref - ref) * c;
   d = max_nan(d, -1e4f);
   const float f = ex2(d);
   a.u = fmaf(d, a.s, a.u) * f;
@@ -130,7 +134,7 @@ struct Running {
   __device__ __forceinline__ void set_ref(float r) {
     ref = r;
     rho2 = pair_of(-(r * c), -(r * c));
-    plain = near_ref(r);
+    plain = near_ref(r, c);
     if (ENTROPY) {
       lo = plain ? Elem<T>::bound(r - 200.f / c) : 0u;
       plain = plain && lo != 0u;
@@ -210,13 +214,14 @@ struct RowSum {
     empty = a.s == 0.f;
     ref = a.ref;
     log2s = log2f(a.s);
-    lse = empty ? -INFINITY : near_ref(ref) ? (ref * c + log2s) * unit : fmaf(ref, inv_tau, log2s * unit);
+    lse = empty ? -INFINITY : near_ref(ref, c) ? (ref * c + log2s) * unit : fmaf(ref, inv_tau, log2s * unit);
     entropy = empty ? 0.f : max_nan((log2s - a.u / a.s) * unit, 0.f);
   }
   __device__ __forceinline__ float logp(float x) const {
     if (x == -INFINITY) return log2s != log2s ? log2s : x;
-    if (near_ref(ref) && !near_ref(x)) return fmaf(x, inv_tau, -lse);     // a mask at the type's lowest value: x c overflows
-    return (scaled(x, ref, c) - log2s) * unit;
+    const float d = scaled(x, ref, c);
+    if (d == -INFINITY) return lse == -INFINITY ? lse : fmaf(x, inv_tau, -lse);     // a mask at the type's lowest value: x c overflows
+    return (d - log2s) * unit;
   }
 };
 
@@ -956,7 +961,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
   if (bad) ca = __int_as_float(0x7fc00000);
   // log2 p = x c - kappa, for 16-bit logits whose reference is no mask
   const float kappa = kStep ? ref * c + log2s : lse * kLog2e;
-  const bool packed = kNarrow && (!kStep || near_ref(ref));
+  const bool packed = kNarrow && (!kStep || near_ref(ref, c));
   const f32x2 c2 = pair_of(c, c), k2 = pair_of(-kappa, -kappa), ca2 = pair_of(ca, ca), cb2 = pair_of(cb * kLn2, cb * kLn2);
   // with a term in log p, -inf is raised to a bound where p is 0 and log p finite; without such a bound: one by one
   const uint32_t lo = MODE == kLogprobsGrad && kNarrow ? Elem<T>::bound((kappa - 200.f) / c) : 0u;
@@ -1206,7 +1211,7 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
     const RowSum r = row_sum(b);
     const float ref = r.ref, log2s = r.log2s;
     const bool zero = !teacher[b].any || r.empty;
-    if (aligned && !zero && near_ref(ref)) {
+    if (aligned && !zero && near_ref(ref, c)) {
       // two elements an instruction; a 16-bit gradient bears ref c + log2 s as one rounded number, an fp32 one does not
       const float kappa = ref * c + (kNarrow ? log2s : 0.f);
       const f32x2 c2 = pair_of(c, c), k2 = pair_of(-kappa, -kappa), ca2 = pair_of(ca, ca), l2 = pair_of(-log2s, -log2s);
