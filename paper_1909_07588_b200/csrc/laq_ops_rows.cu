@@ -43,7 +43,7 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr float kUnset = -FLT_MAX;     // reference of a thread that has seen nothing above -inf
 constexpr float kSlack = 32.f;         // a reference may lag the maximum by this many powers of two
-constexpr float kEmptyLse = -1e30f;    // an lse below this belongs to a row of masks only
+constexpr float kEmptyLse = -16777216.f;  // -2^24; an lse down here belongs to a row of masks only, see RowSum
 
 // ---- a group of NT threads that owns a row (or, in a cluster, a slice of it) ------------------------------------------
 template <int NT>
@@ -210,11 +210,14 @@ __device__ __forceinline__ Stat warp_join(Stat a, float c) {
 struct RowSum {
   float ref, log2s, lse, entropy, c, unit, inv_tau;
   bool empty;       // nothing above -inf
+  bool masked;      // nothing but masks, finite or not.  A gradient handed lse in fp32 cannot tell p where fp32 no longer
+                    // holds units (at -1e9 the rounding of lse is a factor of up to e^32): all gradients are 0 then
   __device__ __forceinline__ RowSum(const Stat& a, float c_, float unit_, float inv_tau_) : c(c_), unit(unit_), inv_tau(inv_tau_) {
     empty = a.s == 0.f;
     ref = a.ref;
     log2s = log2f(a.s);
     lse = empty ? -INFINITY : near_ref(ref, c) ? (ref * c + log2s) * unit : fmaf(ref, inv_tau, log2s * unit);
+    masked = lse <= kEmptyLse;
     entropy = empty ? 0.f : max_nan((log2s - a.u / a.s) * unit, 0.f);
   }
   __device__ __forceinline__ float logp(float x) const {
@@ -933,7 +936,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
     const RowSum r(a, c, A.unit, A.inv_tau);
     ref = r.ref;
     log2s = r.log2s;
-    zero = r.empty;
+    zero = r.masked;
     if (rank == 0 && w == 0) {
       const float kl = te.divergence(r, A.K);
       if (lane == 0) {
@@ -1140,7 +1143,7 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
       load(row + 3 * step, next);
       T* dr = reinterpret_cast<T*>(A.dx) + (long long)row * A.ld_d;
       bar_sync<2, kThreads>();
-      if (te.any && !te.bad && !r.empty)
+      if (te.any && !te.bad && !r.masked)
         for (int i = lane; i < te.n; i += 32)
           dr[te.col[i]] = Elem<T>::from_float(ca * (prob(te.colx[i], r.ref, r.log2s) - te.mass[i]));
       __syncwarp();
@@ -1210,7 +1213,7 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
     if (teacher[b].bad) ca = __int_as_float(0x7fc00000);
     const RowSum r = row_sum(b);
     const float ref = r.ref, log2s = r.log2s;
-    const bool zero = !teacher[b].any || r.empty;
+    const bool zero = !teacher[b].any || r.masked;
     if (aligned && !zero && near_ref(ref, c)) {
       // two elements an instruction; a 16-bit gradient bears ref c + log2 s as one rounded number, an fp32 one does not
       const float kappa = ref * c + (kNarrow ? log2s : 0.f);

@@ -117,3 +117,42 @@ def test_distill_under_finite_masks(V, dtype):
             for dx in (got["dlogits"], ops.distill_backward(x, tok, val, got["lse"], one, temperature=tau)):
                 off = (dx.double() - want["dlogits"].double()).abs()
                 assert bool((off <= half * want["dlogits"].double().abs() + tau * (2 * E[:, None] + 6 * R[:, None] * U) + tiny).all()), (m, tau)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [100, 3000, 50001, 300000])
+def test_gradients_of_rows_of_masks_alone(V, dtype):
+    """Nothing left in a row: by -inf, and by finite masks whose lse fp32 does not hold to a unit, every gradient is 0, in the
+    call with the loss (in one reading or, of the longest rows, in two) and in the call of its own.  Down to there the
+    gradient is the formula's, up to what the rounding of lse, u |lse|, and of its product with log2(e) make of p."""
+    dt = DTYPES[dtype]
+    for m in [-INF, -1.0, -300.0] + _masks(dtype):
+        for tau in (1.0, 0.5):
+            x = torch.full((3, V), m, device="cuda").to(dt)
+            x[1] = torch.randn(V, generator=_gen(1), device="cuda").to(dt)           # rows beside it are not concerned
+            tok = torch.tensor([[0, 3], [1, 2], [V - 1, 5]], device="cuda").int()
+            val = torch.tensor([[0.5, 0.25]] * 3, device="cuda")
+            d = torch.tensor([1.5, 1.0, -0.5], device="cuda")
+            step = ops.distill(x, tok, val, temperature=tau, d_loss=d)
+            alone = ops.distill_backward(x, tok, val, step["lse"], d, temperature=tau)
+            st = ops.token_logprobs(x, tok[:, 0].contiguous(), temperature=tau)
+            pg = ops.token_logprobs_backward(x, tok[:, 0].contiguous(), st["lse"], st["entropy"], d, d, temperature=tau)
+            s = float(x[0, 0]) / tau
+            for r in (0, 2):
+                if s + math.log(V) <= -2.0 ** 24:
+                    assert not bool(step["dlogits"][r].any()) and not bool(alone[r].any()) and not bool(pg[r].any()), (m, tau)
+                    continue
+                if s <= -2.0 ** 20:
+                    for dx in (step["dlogits"], alone, pg):
+                        assert float(dx[r].abs().max()) <= 8 * 1.5 * max(tau, 1 / tau), (m, tau)
+                    continue
+                q = torch.softmax(val[r].double() / tau, dim=0)
+                want = torch.full((V,), 1.0 / V, device="cuda", dtype=torch.float64)
+                want[tok[r].long()] -= q
+                want = want * tau * float(d[r])
+                rel = 6 * U * (abs(s) + math.log(V)) + 60 * U + V / 256 * U
+                rel = (torch.finfo(dt).eps / 2 if dt != torch.float32 else U) + 1.5 * rel
+                tiny = torch.finfo(dt).smallest_normal
+                for dx in (step["dlogits"], alone):
+                    assert bool(((dx[r].double() - want).abs() <= rel * (want.abs() + 1.0 / V * abs(tau * float(d[r]))) + tiny).all()), (m, tau)
+            assert bool(step["dlogits"][1].any()) and bool(alone[1].any()) and bool(pg[1].any())
