@@ -324,7 +324,7 @@ laq_status laq_token_logprobs(const void* d_logits, int32_t dtype, int64_t rows,
  *   d_grad_logits_j = (g ([j = token] - p_j) - h p_j (log p_j + entropy)) / temperature
  * in the logits' dtype.  d_grad_logits may be the logits themselves (same pointer and stride), or must not overlap them.
  * Rows with a negative token, and rows masked throughout, by -inf or by finite masks (lse <= -2^24: in fp32 it no longer tells
- * p), get zeros; a token >= vocab gives NaN. */
+ * p), get zeros; a token >= vocab gives NaN, in a masked row too. */
 laq_status laq_token_logprobs_backward(const void* d_logits, int32_t dtype, int64_t rows, int64_t vocab, int64_t row_stride,
                                        float temperature, const int32_t* d_tokens, const float* d_lse, const float* d_entropy,
                                        const float* d_grad_logprob, const float* d_grad_entropy, void* d_grad_logits,
@@ -335,7 +335,7 @@ laq_status laq_token_logprobs_backward(const void* d_logits, int32_t dtype, int6
  * teacher_stride.  q = softmax of t / temperature over the row's entries, p = softmax of the student's logits / temperature:
  *   loss = temperature^2 sum_i q_i (log q_i - log p_{a_i}),  d loss / d logits_j = temperature (p_j - sum_{i: a_i = j} q_i)
  * A column may be named more than once.  Entries at -inf have q = 0.  A row without entries (or whose every entry is at
- * -inf) has loss 0, lse 0 and gradient 0.  A column >= vocab makes the row's loss and gradient NaN.  A teacher's column that
+ * -inf) has loss 0, lse 0 and gradient 0.  A column >= vocab makes the row's loss and gradient NaN, however the row is masked.  A teacher's column that
  * the student has masked (-inf) gives loss = +inf; so does a row that the student has masked throughout by -inf.  A row masked
  * throughout, by -inf or by finite masks (lse <= -2^24, as above), has gradient 0, here and in laq_distill_backward.
  * d_loss, d_lse: [rows] fp32.  d_grad_loss ([rows] fp32) and d_grad_logits (logits' dtype; the logits themselves or no overlap)

@@ -874,7 +874,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
   }
   if (!kStep) {
     lse = A.lse_in[row];
-    zero = zero || lse <= kEmptyLse;       // nothing left by the masks
+    zero = zero || (lse <= kEmptyLse && token < A.V);       // nothing left by the masks
   }
   constexpr int kThreads = kGradientThreads<NT, MODE>;
   const bool in_place = A.x == A.dx;
@@ -900,7 +900,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
   uint4 v[R];
   float xe = -INFINITY;
   const int per_turn = R * NT;
-  if (kStep || !zero) {
+  if (kTeacher || !zero) {                 // a masked row of which the teacher asks for a bad column becomes NaN
 #pragma unroll
     for (int i = 0; i < R; ++i) {
       const int at = sl.v0 + t + i * NT;
@@ -920,7 +920,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
       any = any || (in.col[e] >= 0 && !(in.t[e] == -INFINITY));
     }
     bad = __any_sync(0xffffffffu, bad);
-    zero = zero || !(__any_sync(0xffffffffu, any) || bad);
+    zero = !bad && (zero || !__any_sync(0xffffffffu, any));
     if (in_place) bar_sync<1, kThreads>();
   }
   if (kTeacher && !kOwnWarp && w == 0)
@@ -950,8 +950,8 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
   if (kTeacher) {
     if (!kOwnWarp) {
       G::sync();
-      zero = zero || !te.any;
       bad = te.bad != 0;
+      zero = !bad && (zero || !te.any);
     }
     ca = A.d_loss[row] * A.tau;
   } else {
@@ -1213,7 +1213,7 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
     if (teacher[b].bad) ca = __int_as_float(0x7fc00000);
     const RowSum r = row_sum(b);
     const float ref = r.ref, log2s = r.log2s;
-    const bool zero = !teacher[b].any || r.masked;
+    const bool zero = !teacher[b].bad && (!teacher[b].any || r.masked);
     if (aligned && !zero && near_ref(ref, c)) {
       // two elements an instruction; a 16-bit gradient bears ref c + log2 s as one rounded number, an fp32 one does not
       const float kappa = ref * c + (kNarrow ? log2s : 0.f);

@@ -156,3 +156,23 @@ def test_gradients_of_rows_of_masks_alone(V, dtype):
                 for dx in (step["dlogits"], alone):
                     assert bool(((dx[r].double() - want).abs() <= rel * (want.abs() + 1.0 / V * abs(tau * float(d[r]))) + tiny).all()), (m, tau)
             assert bool(step["dlogits"][1].any()) and bool(alone[1].any()) and bool(pg[1].any())
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [80, 1500, 30000, 300000])
+@pytest.mark.parametrize("m", [-INF, -1e9, None])
+def test_a_bad_column_shows_in_masked_rows_too(V, m, dtype):
+    dt = DTYPES[dtype]
+    x = torch.full((4, V), torch.finfo(dt).min if m is None else m, device="cuda").to(dt)
+    x[3] = torch.randn(V, generator=_gen(1), device="cuda").to(dt)
+    one = torch.ones(4, device="cuda")
+    tok = torch.tensor([[3, V], [2, 5], [2 ** 31 - 1, -1], [1, 2]], device="cuda").int()
+    val = torch.zeros(4, 2, device="cuda")
+    step = ops.distill(x, tok, val, d_loss=one)
+    alone = ops.distill_backward(x, tok, val, step["lse"], one)
+    st = ops.token_logprobs(x, tok.amax(dim=1))
+    pg = ops.token_logprobs_backward(x, tok.amax(dim=1), st["lse"], st["entropy"], one, one)
+    assert step["loss"].isnan().tolist() == [True, False, True, False]
+    assert st["logprob"].isnan().tolist() == [True, False, True, False]
+    for dx in (step["dlogits"], alone, pg):
+        assert bool(dx[[0, 2]].isnan().all()) and not bool(dx[1].any()) and bool(dx[3].isfinite().all())
