@@ -1,0 +1,57 @@
+"""How precise the operators are where it is easy to lose precision: peaked rows, long sums, low temperatures.
+
+u = 2^-24.  A rounding to nearest is off by at most u of the value and, over many values, by u / sqrt(3) of it (root mean
+square); n independent ones by sqrt(n) of that."""
+import math
+
+import pytest
+import torch
+
+from paper_1909_07588_b200 import ops
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def _gen(seed):
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def _peaked(T, V, dt, seed):
+    """Rows like a trained model's: a broad body and one peak in each."""
+    x = torch.empty(T, V, dtype=dt, device="cuda")
+    g = _gen(seed)
+    for r in range(0, T, 200):
+        b = torch.randn(min(200, T - r), V, generator=g, device="cuda") * 2.5
+        b[torch.arange(b.shape[0], device="cuda"), torch.randint(0, V, (b.shape[0],), generator=g, device="cuda")] += 12.0
+        x[r:r + 200] = b.to(dt)
+    return x
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("T, V", [(1400, 131072), (300, 131072), (64, 100003), (3000, 2001)])
+@pytest.mark.parametrize("tau", [1.0, 0.7])
+def test_entropy_of_peaked_rows(T, V, dtype, tau):
+    """The entropy is log2 s - m, m = u / s the mean of d = (x - ref) c.  Root mean square over rows, in units of what a row's
+    independent roundings make of it:
+      n additions on the way to s and u (16 within a batch, a batch for every 512 threads' vectors, a rest of 3, the joins' 14),
+      sqrt(n / 3) u of s, and of sum |d| 2^d: log2(e) and sqrt(2) |d| of that, with |d| at most 8, what a reference may
+      lag, and 1 and log2(e) H for the body;
+      the exponentials' 4 u, u for each of d's, of the logarithm's and the quotient's rounding, with the same weights: 6 u;
+      c off by u at most: u times the variance of x / tau under p."""
+    dt = DTYPES[dtype]
+    x = _peaked(T, V, dt, V)
+    got = ops.token_logprobs(x, temperature=tau)["entropy"].double()
+    H, var = torch.empty_like(got), torch.empty_like(got)
+    for r in range(0, T, 100):
+        s = x[r:r + 100].double() / tau
+        logp = torch.log_softmax(s, dim=1)
+        p = logp.exp()
+        H[r:r + 100] = -(p * logp).sum(dim=1)
+        var[r:r + 100] = (p * logp * logp).sum(dim=1) - H[r:r + 100] ** 2
+    n = 16 + V / (512 * (16 / dt.itemsize)) + 3 + 14
+    size = math.log2(math.e) + math.sqrt(2) * (8 + 1 + math.log2(math.e) * H)
+    unit = U * (math.log(2) * (math.sqrt(n / 3) + 6) * size + var)
+    assert float(((got - H) / unit).square().mean().sqrt()) <= 1
