@@ -364,7 +364,9 @@ enum {
 };
 
 /* One layer:  z = x w^T + bias,  y = act(z) + residual;  x [M][K], w [N][K], bias [N], the others [M][N], all in `dtype`
- * (LAQ_BF16 or LAQ_F16), accumulated in fp32 and rounded once.  Row strides in elements. */
+ * (LAQ_BF16 or LAQ_F16), accumulated in fp32 and rounded once.  The tensor cores cut their fp32 sums: a sum of n terms loses some
+ * n 10^-9 of sum |terms|.  Sums with an fp32 result are therefore taken in chunks of 512 terms, longer ones than 65536 terms with
+ * a 16-bit result in chunks of 16384, and the chunks are added with rounding.  Row strides in elements. */
 typedef struct {
   int32_t dtype;             /* laq_dtype of x, w, bias, residual, z, y, dy, dx */
   int32_t activation;        /* laq_activation */

@@ -44,9 +44,14 @@ constexpr int kStaging = kEpiWarps * 4096;   // ... and of the epilogue warps' p
 constexpr int kMaxSplit = 8;
 constexpr uint32_t kStarvedLimit = 1u << 12;
 // The tensor core's fp32 sums are cut, not rounded: every 16 terms take up to an ulp off, always towards zero (8192 terms:
-// 9e-6 of the result, 512 terms: 5e-7).  16-bit results do not show it.  fp32 ones are added up in chunks of 512 terms, which
-// the epilogue's threads keep in registers and add with rounding while the next chunk is under way.
-constexpr int kChunk32 = 8;               // k-blocks
+// 9e-6 of the result, 512 terms: 5e-7).  fp32 results are added up in chunks of 512 terms, which the epilogue's threads keep
+// in registers and add with rounding while the next chunk is under way.  16-bit results show it in long sums alone: 65536 terms
+// lose 6e-5, an eighth of half a step of fp16, 2^20 would lose 8e-4.  Longer ones are added up in chunks of 16384 terms (1.6e-5),
+// whose sums wait in the second accumulator's tensor memory, so that tiles may still be 256 wide: the tensor cores stand still
+// for it for some 2000 cycles in a chunk's 180000.  (131072 rows, dW of 4096 x 1024 bf16: 866 us, without chunks 845 us, with the
+// sums in registers and tiles of 128 columns 1505 us.)
+constexpr int kChunk32 = 8, kChunkLong = 256;               // k-blocks
+constexpr int kLongSum = 65536;           // terms that a 16-bit result takes at once
 constexpr int kGroupTiles = 16;           // tile rows that are swept together, so that operands are found in L2
 
 struct GemmArgs {
@@ -103,6 +108,31 @@ __device__ __forceinline__ bool elect_one() {
       : "=r"(ok));
   return ok != 0;
 }
+
+// 32 or 16 columns of this warp's lanes of tensor memory
+__device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t (&v)[32]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+      "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};" ::"r"(v[0]),
+      "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+      "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(v[16]), "r"(v[17]), "r"(v[18]), "r"(v[19]), "r"(v[20]), "r"(v[21]),
+      "r"(v[22]), "r"(v[23]), "r"(v[24]), "r"(v[25]), "r"(v[26]), "r"(v[27]), "r"(v[28]), "r"(v[29]), "r"(v[30]), "r"(v[31]),
+      "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_store(uint32_t taddr, const uint32_t (&v)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(v[0]),
+      "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]), "r"(v[8]), "r"(v[9]), "r"(v[10]), "r"(v[11]),
+      "r"(v[12]), "r"(v[13]), "r"(v[14]), "r"(v[15]), "r"(taddr)
+      : "memory");
+  asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[32]) { umma::tmem_load_32(taddr, v); }
+__device__ __forceinline__ void tmem_load(uint32_t taddr, uint32_t (&v)[16]) { umma::tmem_load_16(taddr, v); }
 
 // ---- the instructions of a pair of blocks -----------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t of_leader(uint32_t addr) {      // the same shared-memory address in the pair's first block
@@ -262,7 +292,7 @@ __device__ __forceinline__ void tile_of(const GemmArgs& A, int w, int& i0, int& 
   j0 = (in / rows) * A.nt;
 }
 
-template <class T, bool TRANS, bool PAIR, bool OUT32>
+template <class T, bool TRANS, bool PAIR, bool OUT32, bool LONG>
 __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                                       const __grid_constant__ CUtensorMap tmB,
                                                                       const GemmArgs A) {
@@ -273,17 +303,19 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const uint32_t base = umma::smem_u32(gemm_smem_raw), smem0 = (base + 1023u) & ~1023u;
   uint4* ring4 = reinterpret_cast<uint4*>(gemm_smem_raw + (smem0 - base));        // a split tile, once the ring is idle
-  constexpr int kChunk = OUT32 ? kChunk32 : 1 << 30;      // k-blocks that the tensor core adds up
+  static_assert(!(OUT32 && (LONG || TRANS)), "fp32 results have chunks of their own, and their epilogue writes rows");
+  constexpr int kChunk = OUT32 ? kChunk32 : LONG ? kChunkLong : 1 << 30;      // k-blocks that the tensor core adds up
   const int nt = A.nt, stages = A.stages, split = PAIR ? 1 : A.split;
   const int b_rows = PAIR ? nt / 2 : nt;           // columns of the tile whose part of B this block loads
   const uint32_t a_bytes = kTileM * kBlockK * 2, st_bytes = a_bytes + (uint32_t)b_rows * kBlockK * 2;
   const int half = PAIR ? (int)(blockIdx.x & 1u) : 0;
   const uint32_t full0 = umma::smem_u32(&bars[0]), empty0 = umma::smem_u32(&bars[kMaxStages]);
   const uint32_t acc_full0 = umma::smem_u32(&bars[2 * kMaxStages]), acc_empty0 = acc_full0 + 16, drain = acc_full0 + 32;
-  // Two accumulators of at most 256 columns; one for a split tile, which has no successor (two of at most 128 for its
-  // chunks).  Two blocks of a cluster on one SM must be able to hold theirs at the same time (each waits for the other), and
-  // two is all that fits by shared memory.
-  const uint32_t acc_cols = umma::tmem_cols(nt), held_cols = split > 1 && !OUT32 ? acc_cols : 2 * acc_cols;
+  // Two accumulators of at most 256 columns; one for a split tile, which has no successor (two of at most 128 for the chunks
+  // of an fp32 result).  A long sum's chunks all go to the first, their sum is in the second.  Two blocks of a cluster on one
+  // SM must be able to hold theirs at the same time (each waits for the other), and two is all that fits by shared memory (one,
+  // where a split long sum is more than 128 columns wide).
+  const uint32_t acc_cols = umma::tmem_cols(nt), held_cols = split > 1 && !OUT32 && !LONG ? acc_cols : 2 * acc_cols;
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
       umma::mbar_init(full0 + 8 * s, 1);
@@ -394,8 +426,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       bool ok = true;
       for (int w = first; w < tiles && ok; w += step) {
         for (int k0 = 0; k0 < nkb && ok; k0 += kChunk, ++it) {
-          const int b = it & 1, k1 = min(k0 + kChunk, nkb);
-          ok = umma::mbar_wait_abortable(acc_empty0 + 8 * b, ((uint32_t)(it >> 1) & 1u) ^ 1u, limit, abort_flag, A.status, 2u);
+          const int b = LONG ? 0 : it & 1, turn = LONG ? it : it >> 1, k1 = min(k0 + kChunk, nkb);
+          ok = umma::mbar_wait_abortable(acc_empty0 + 8 * b, ((uint32_t)turn & 1u) ^ 1u, limit, abort_flag, A.status, 2u);
           if (!ok) break;
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t d = tmem_base + (uint32_t)b * acc_cols;
@@ -455,13 +487,13 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       uint32_t t0 = 0;
       // the next accumulator, and its return to the tensor-core warp
       auto acquire = [&]() {
-        const int b = it & 1;
-        ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(it >> 1) & 1u, acc_limit, abort_flag, A.status, 8u));
+        const int b = LONG ? 0 : it & 1, turn = LONG ? it : it >> 1;
+        ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)turn & 1u, acc_limit, abort_flag, A.status, 8u));
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         t0 = tmem_base + (uint32_t)b * acc_cols + ((uint32_t)(q * 32) << 16);
       };
       auto release = [&]() {
-        const int b = it & 1;
+        const int b = LONG ? 0 : it & 1;
         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
         __syncwarp();
         if (lane == 0) {
@@ -491,16 +523,55 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
         }
         if (!ok) break;
       } else {
+        if constexpr (LONG) {
+          // the chunks before the last; each warp adds up the columns that it will write out
+          const uint32_t total = tmem_base + acc_cols + ((uint32_t)(q * 32) << 16);
+          auto add_up = [&](auto& v, int c0, bool first_chunk) {
+            tmem_load(t0 + (uint32_t)c0, v);
+            if (!first_chunk) {
+              std::remove_reference_t<decltype(v)> sum_so_far;
+              tmem_load(total + (uint32_t)c0, sum_so_far);
+#pragma unroll
+              for (size_t e = 0; e < sizeof(v) / 4; ++e) v[e] = __float_as_uint(__uint_as_float(sum_so_far[e]) + __uint_as_float(v[e]));
+            }
+            tmem_store(total + (uint32_t)c0, v);
+          };
+          for (int k0 = 0; k0 + kChunk < nkb; k0 += kChunk) {
+            acquire();
+            if (!ok) break;
+            if (TRANS || split > 1) {
+              uint32_t v[16];
+              for (int c0 = 16 * set; c0 < nt; c0 += 32) add_up(v, c0, k0 == 0);
+            } else {
+              uint32_t v[32];
+              for (int c0 = 32 * set; c0 < nt; c0 += 64) add_up(v, c0, k0 == 0);
+            }
+            release();
+          }
+          if (!ok) break;
+        }
         acquire();
         if (!ok) break;
       }
-      // the 32 values from column c0 on of this lane's row
+      // the values from column c0 on of this lane's row: the accumulator's, and the sum of the chunks before it
+      auto loaded = [&](int c0, auto& v) {
+        tmem_load(t0 + (uint32_t)c0, v);    // past nt only where nt is no multiple of 32: not used then
+        if constexpr (LONG) {
+          if (nkb > kChunk) {
+            std::remove_reference_t<decltype(v)> sum_so_far;
+            tmem_load(tmem_base + acc_cols + ((uint32_t)(q * 32) << 16) + (uint32_t)c0, sum_so_far);
+#pragma unroll
+            for (size_t e = 0; e < sizeof(v) / 4; ++e) v[e] = __float_as_uint(__uint_as_float(sum_so_far[e]) + __uint_as_float(v[e]));
+          }
+        }
+      };
+      // 32 of them
       auto values = [&](int c0, uint32_t (&v)[32]) {
         if constexpr (OUT32) {
 #pragma unroll
           for (int e = 0; e < 32; ++e) v[e] = __float_as_uint(c0 >= 64 ? sum[1][e] : sum[0][e]);
         } else {
-          umma::tmem_load_32(t0 + (uint32_t)c0, v);    // past nt only where nt is no multiple of 32: not used then
+          loaded(c0, v);
         }
       };
       if (split > 1 && OUT32) {
@@ -514,7 +585,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       } else if (split > 1) {
         for (int c0 = 16 * set; c0 < nt; c0 += 32) {
           uint32_t v[16];
-          umma::tmem_load_16(t0 + (uint32_t)c0, v);
+          loaded(c0, v);
 #pragma unroll
           for (int e = 0; e < 16; e += 4)
             ring4[piece(row, (c0 + e) / 4, nt / 4)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
@@ -522,7 +593,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       } else if (TRANS) {
         for (int c0 = 16 * set; c0 < nt; c0 += 32) {
           uint32_t v[16];
-          umma::tmem_load_16(t0 + (uint32_t)c0, v);
+          loaded(c0, v);
           float x[2][8];
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[e >> 3][e & 7] = __uint_as_float(v[e]);
@@ -930,7 +1001,7 @@ struct Plan {
 // it is within 3 % of the fastest in 22 of the 26 and at most 25 % slower in the others.
 // `swappable`: the epilogue may write the transposed tile.  An fp32 result's tile is a multiple of 64 wide (its operands are
 // MN-major).
-Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable, bool out32) {
+Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable, bool out32, bool long_sum) {
   Plan best{0, 128, 1, 4, 0, 1e300};
   const long long nkb = (R + kBlockK - 1) / kBlockK;
   const auto persistent = [](double waves, double main, double epi) {
@@ -957,6 +1028,9 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
         if (split > 1)                                                 // the partial tile in the ring
           while (stages * stage < kTileM * nt * 4 || stages < 3) ++stages;
         if (stages * stage > kMaxRing) continue;
+        // A split long sum of more than 128 columns holds all of an SM's tensor memory: only where no other split tile's block
+        // (96 KB at least) fits beside it, since the two could keep one another from the clusters that they wait for.
+        if (split > 1 && long_sum && nt > 128 && stages * stage <= 128 * 1024) continue;
         const double main = kb * per;
         double cost;
         if (split == 1) {
@@ -987,10 +1061,10 @@ struct Err {
   size_t len;
 };
 
-template <class T, bool TRANS, bool PAIR, bool OUT32>
+template <class T, bool TRANS, bool PAIR, bool OUT32, bool LONG>
 laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, bool follows,
                        cudaStream_t st) {
-  auto kernel = linear_gemm_kernel<T, TRANS, PAIR, OUT32>;
+  auto kernel = linear_gemm_kernel<T, TRANS, PAIR, OUT32, LONG>;
   const size_t smem = (size_t)A.stages * (kTileM + (PAIR ? A.nt / 2 : A.nt)) * kBlockK * 2 + (TRANS || A.split > 1 ? 0 : kStaging) + 1024;
   const int per_tile = PAIR ? 2 : A.split;
   // the kernel's shared memory limit is raised once per device
@@ -1032,15 +1106,21 @@ laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& m
   return LAQ_OK;
 }
 
+template <class T, bool LONG>
+laq_status launch_16(const Err& e, const Plan& pl, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, bool follows,
+                     cudaStream_t st) {
+  if (pl.pair) return launch_gemm<T, false, true, false, LONG>(e, ma, mb, A, follows, st);
+  return pl.swap ? launch_gemm<T, true, false, false, LONG>(e, ma, mb, A, follows, st)
+                 : launch_gemm<T, false, false, false, LONG>(e, ma, mb, A, follows, st);
+}
+
 template <class T>
-laq_status launch_form(const Err& e, const Plan& pl, bool out32, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A,
-                       bool follows, cudaStream_t st) {
+laq_status launch_form(const Err& e, const Plan& pl, bool out32, bool long_sum, const CUtensorMap& ma, const CUtensorMap& mb,
+                       const GemmArgs& A, bool follows, cudaStream_t st) {
   if (out32)
-    return pl.pair ? launch_gemm<T, false, true, true>(e, ma, mb, A, follows, st)
-                   : launch_gemm<T, false, false, true>(e, ma, mb, A, follows, st);
-  if (pl.pair) return launch_gemm<T, false, true, false>(e, ma, mb, A, follows, st);
-  return pl.swap ? launch_gemm<T, true, false, false>(e, ma, mb, A, follows, st)
-                 : launch_gemm<T, false, false, false>(e, ma, mb, A, follows, st);
+    return pl.pair ? launch_gemm<T, false, true, true, false>(e, ma, mb, A, follows, st)
+                   : launch_gemm<T, false, false, true, false>(e, ma, mb, A, follows, st);
+  return long_sum ? launch_16<T, true>(e, pl, ma, mb, A, follows, st) : launch_16<T, false>(e, pl, ma, mb, A, follows, st);
 }
 
 struct Epilogue {
@@ -1058,7 +1138,8 @@ struct Epilogue {
 laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const Operand& b, bool b_mn, const Epilogue& ep,
                    uint32_t* status, int starve, bool swappable, bool follows, cudaStream_t st) {
   const long long I = a_mn ? a.cols : a.rows, R = a_mn ? a.rows : a.cols, J = b_mn ? b.cols : b.rows;
-  const Plan pl = make_plan(I, J, R, a_mn, b_mn, swappable, ep.out_f32 != 0);
+  const bool out32 = ep.out_f32 != 0, long_sum = !out32 && R > kLongSum;
+  const Plan pl = make_plan(I, J, R, a_mn, b_mn, swappable, out32, long_sum);
   const Operand& A0 = pl.swap ? b : a;
   const Operand& B0 = pl.swap ? a : b;
   const bool amn = pl.swap ? b_mn : a_mn, bmn = pl.swap ? a_mn : b_mn;
@@ -1089,8 +1170,8 @@ laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const O
   A.bias = ep.bias;
   A.residual = ep.residual;
   A.status = status;
-  return dtype == LAQ_BF16 ? launch_form<__nv_bfloat16>(e, pl, ep.out_f32 != 0, ma, mb, A, follows, st)
-                           : launch_form<__half>(e, pl, ep.out_f32 != 0, ma, mb, A, follows, st);
+  return dtype == LAQ_BF16 ? launch_form<__nv_bfloat16>(e, pl, out32, long_sum, ma, mb, A, follows, st)
+                           : launch_form<__half>(e, pl, out32, long_sum, ma, mb, A, follows, st);
 }
 
 // Warps that share four columns: as many as fill the rounds of resident warps best, the fewer the better within a quarter

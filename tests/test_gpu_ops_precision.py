@@ -55,3 +55,47 @@ def test_entropy_of_peaked_rows(T, V, dtype, tau):
     size = math.log2(math.e) + math.sqrt(2) * (8 + 1 + math.log2(math.e) * H)
     unit = U * (math.log(2) * (math.sqrt(n / 3) + 6) * size + var)
     assert float(((got - H) / unit).square().mean().sqrt()) <= 1
+
+
+def _chunked(n, chunk=16384):
+    """What a sum of n positive terms in chunks may lose of itself: a step for 16 of a chunk's terms, each cut by less than an ulp, and
+    a rounding for every chunk (and for a split's parts)."""
+    return chunk / 16 * 2.0 ** -23 + (n / chunk + 10) * U
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("act", ["none", "relu"])
+@pytest.mark.parametrize("M, N, K", [(1 << 20, 64, 136), (70001, 257, 129), (262144, 512, 256)])
+def test_weight_gradient_over_many_rows(M, N, K, dtype, act):
+    """Same-sign terms: a sum that is cut at every step would lose n 10^-9 of itself, 8e-4 over 2^20 rows."""
+    dt = DTYPES[dtype]
+    dy = (torch.rand(M, N, generator=_gen(1), device="cuda") * (1024.0 / M)).to(dt)
+    x = torch.rand(M, K, generator=_gen(2), device="cuda").to(dt)
+    w = torch.zeros(N, K, device="cuda", dtype=dt)
+    z = None if act == "none" else torch.ones(M, N, device="cuda", dtype=dt)
+    want = sum(dy[r:r + 65536].double().T @ x[r:r + 65536].double() for r in range(0, M, 65536))
+    got = ops.linear_backward(dy, x, w, z=z, activation=act, dx=False, db=False)["dw"].double()
+    half = torch.finfo(dt).eps / 2
+    assert float(((got - want).abs() / want).max()) <= _chunked(M) + half * (1 + _chunked(M))
+    ops.check_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M, N, K", [(33, 72, (1 << 20) + 24), (512, 512, 131080), (300, 1000, 65537), (7, 20, 70000)])
+def test_long_rows(M, N, K, dtype):
+    """The forward product and the input's gradient over a long axis, with everything that the epilogue does."""
+    dt = DTYPES[dtype]
+    half, c = torch.finfo(dt).eps / 2, _chunked(K)
+    x = torch.rand(M, K, generator=_gen(1), device="cuda").to(dt)
+    w = (torch.rand(N, K, generator=_gen(2), device="cuda") * (16.0 / K)).to(dt)
+    b, r = torch.rand(N, generator=_gen(3), device="cuda").to(dt), torch.rand(M, N, generator=_gen(4), device="cuda").to(dt)
+    want = x.double() @ w.double().T
+    y, z = ops.linear(x, w, b, activation="relu", residual=r, preact=True)
+    zw = want + b.double()
+    assert float(((z.double() - zw).abs() / zw).max()) <= c + 2 * U + half * (1 + c + 2 * U)
+    yw = zw + r.double()
+    assert float(((y.double() - yw).abs() / yw).max()) <= c + 4 * U + half * (1 + c + 4 * U)
+    # dX = dZ W has the layer's outputs as its terms: K of them, with x in the place of dZ
+    got = ops.linear_backward(x, torch.zeros(M, N, device="cuda", dtype=dt), w.T.contiguous(), dw=False, db=False)["dx"].double()
+    assert float(((got - want).abs() / want).max()) <= c + half * (1 + c)
+    ops.check_status()
