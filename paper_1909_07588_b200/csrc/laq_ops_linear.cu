@@ -44,7 +44,7 @@ constexpr int kStaging = kEpiWarps * 4096;   // ... and of the epilogue warps' p
 constexpr int kMaxSplit = 8;
 constexpr uint32_t kStarvedLimit = 1u << 12;
 // The tensor core's fp32 sums are cut, not rounded: every 16 terms take up to an ulp off, always towards zero (8192 terms:
-// 9e-6 of the result, 512 terms: 5e-7).  fp32 results are added up in chunks of 512 terms, which the epilogue's threads keep
+// 9e-6 of the result, 512 terms: 7e-7 with bf16 operands, 2.8e-6 with fp16 ones).  fp32 results are added up in chunks of 512 terms, which the epilogue's threads keep
 // in registers and add with rounding while the next chunk is under way.  16-bit results show it in long sums alone: 65536 terms
 // lose 6e-5, an eighth of half a step of fp16, 2^20 would lose 8e-4.  Longer ones are added up in chunks of 16384 terms (1.6e-5),
 // whose sums wait in the second accumulator's tensor memory, so that tiles may still be 256 wide: the tensor cores stand still

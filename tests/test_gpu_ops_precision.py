@@ -99,3 +99,19 @@ def test_long_rows(M, N, K, dtype):
     got = ops.linear_backward(x, torch.zeros(M, N, device="cuda", dtype=dt), w.T.contiguous(), dw=False, db=False)["dx"].double()
     assert float(((got - want).abs() / want).max()) <= c + half * (1 + c)
     ops.check_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M, N, K", [(8192, 64, 128), (16384, 200, 784), (65536, 256, 512), (1 << 19, 40, 72)])
+def test_fp32_weight_gradient_is_summed_in_chunks(M, N, K, dtype):
+    """fp32 dW of same-sign terms within what chunks of 512 terms may lose, 4e-6 for a chunk's cuts and 6e-8 a chunk.  One
+    uncut sum loses more from 8192 rows on with fp16 operands, from 65536 with bf16 ones."""
+    dt = DTYPES[dtype]
+    dy = torch.rand(M, N, generator=_gen(1), device="cuda").to(dt)
+    x = torch.rand(M, K, generator=_gen(2), device="cuda").to(dt)
+    want = sum(dy[r:r + 65536].double().T @ x[r:r + 65536].double() for r in range(0, M, 65536))
+    got = ops.linear_backward(dy, x, torch.zeros(N, K, device="cuda", dtype=dt), dx=False, db=False, dw_dtype=torch.float32)["dw"]
+    off = ((got.double() - want) / want).abs()
+    # the roundings of the chunks' additions are to nearest: sqrt(n / 3) of them, and four times that at the farthest
+    assert float(off.max()) <= 32 * 2.0 ** -23 + U * (4 * math.sqrt((M / 512 + 10) / 3) + 1)
+    ops.check_status()
