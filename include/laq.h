@@ -294,11 +294,12 @@ laq_status laq_quantize_worker_static(const float* d_g, const float* d_qprev, in
  * with bias, activation and residual, two losses over rows of logits, and the gradients of all three.
  *
  * Common rules.  No context: like laq_quantize_worker_static every call takes its stream and, optionally, a HOST buffer for
- * an error text (errbuf, errbuf_len).  All tensors are DEVICE, row-major, on the calling thread's current device (checked:
- * LAQ_EINVAL otherwise), with unit stride within a row and any row stride (in elements) of at least the row's length; a
- * pointer needs only the alignment of its element.  Calls are asynchronous, allocate nothing, copy nothing to the host and
- * can be captured into a CUDA graph.  Zero rows are allowed and launch nothing.  Results do not depend on timing: sums
- * are taken in a fixed order, in fp32, and there are no atomics on device memory. */
+ * an error text (errbuf, errbuf_len).  All tensors are DEVICE, row-major, on the calling thread's current device (checked
+ * for every pointer that the call reads or writes: LAQ_EINVAL otherwise), with unit stride within a row and any row stride
+ * (in elements) of at least the row's length; a pointer needs only the alignment of its element.  Calls are asynchronous,
+ * allocate nothing, copy nothing to the host and can be captured into a CUDA graph.  Zero rows are allowed and launch
+ * nothing.  Results do not depend on timing: sums are taken in a fixed order, in fp32, and there are no atomics on device
+ * memory. */
 typedef enum {
   LAQ_F32 = 0,
   LAQ_BF16 = 1,

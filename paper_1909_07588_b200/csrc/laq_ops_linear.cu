@@ -44,12 +44,12 @@ constexpr int kStaging = kEpiWarps * 4096;   // ... and of the epilogue warps' p
 constexpr int kMaxSplit = 8;
 constexpr uint32_t kStarvedLimit = 1u << 12;
 // The tensor core's fp32 sums are cut, not rounded: every 16 terms take up to an ulp off, always towards zero (8192 terms:
-// 9e-6 of the result, 512 terms: 7e-7 with bf16 operands, 2.8e-6 with fp16 ones).  fp32 results are added up in chunks of 512 terms, which the epilogue's threads keep
-// in registers and add with rounding while the next chunk is under way.  16-bit results show it in long sums alone: 65536 terms
-// lose 6e-5, an eighth of half a step of fp16, 2^20 would lose 8e-4.  Longer ones are added up in chunks of 16384 terms (1.6e-5),
-// whose sums wait in the second accumulator's tensor memory, so that tiles may still be 256 wide: the tensor cores stand still
-// for it for some 2000 cycles in a chunk's 180000.  (131072 rows, dW of 4096 x 1024 bf16: 866 us, without chunks 845 us, with the
-// sums in registers and tiles of 128 columns 1505 us.)
+// 9e-6 of the result, 512 terms: 7e-7 with bf16 operands, 2.8e-6 with fp16 ones).  fp32 results are added up in chunks of 512
+// terms, which the epilogue's threads keep in registers and add with rounding while the next chunk is under way.  16-bit
+// results show it in long sums alone: 65536 terms lose 6e-5, an eighth of half a step of fp16, 2^20 would lose 8e-4.  Longer
+// ones are added up in chunks of 16384 terms (1.6e-5), whose sums wait in the second accumulator's tensor memory, so that
+// tiles may still be 256 wide: the tensor cores stand still for it for some 2000 cycles in a chunk's 180000.  (131072 rows, dW
+// of 4096 x 1024 bf16: 866 us, without chunks 845 us, with the sums in registers and tiles of 128 columns 1505 us.)
 constexpr int kChunk32 = 8, kChunkLong = 256;               // k-blocks
 constexpr int kLongSum = 65536;           // terms that a 16-bit result takes at once
 constexpr int kGroupTiles = 16;           // tile rows that are swept together, so that operands are found in L2
@@ -1295,16 +1295,14 @@ laq_status check_call(const Err& e, const laq_linear_call* c, void* ws, size_t w
   if (need && (!ws || ((uintptr_t)ws & 255u) || ws_bytes < need))
     return fail(e.buf, e.len, LAQ_EWORKSPACE, "workspace missing, misaligned (256 bytes) or too small: %zu bytes needed", need);
   if (c->flags & ~(uint32_t)LAQ_LINEAR_STARVE) return fail(e.buf, e.len, LAQ_EINVAL, "unknown flags");
-  const char* msg = wrong_device(c->status);
-  if (!msg && c->M > 0 && c->w) msg = wrong_device(c->w);
-  return msg ? fail(e.buf, e.len, LAQ_EINVAL, "%s", msg) : LAQ_OK;
+  return LAQ_OK;
 }
 
-// One tensor of a call: there if it must be, rows no shorter than their length, aligned to its elements.
-laq_status check_tensor(const Err& e, const char* name, const void* p, bool required, int64_t ld, int64_t cols, int bytes) {
+// One tensor of a call: there if it must be, rows no shorter than their length.  It is added to the buffers.
+laq_status check_tensor(const Err& e, Buffers& buffers, const char* name, const void* p, bool required, int64_t ld, int64_t cols, int bytes) {
   if (!p) return required ? fail(e.buf, e.len, LAQ_EINVAL, "%s is null", name) : LAQ_OK;
   if (ld < cols) return fail(e.buf, e.len, LAQ_EINVAL, "the row stride of %s is shorter than its rows", name);
-  if (((uintptr_t)p % (uintptr_t)bytes) != 0) return fail(e.buf, e.len, LAQ_EINVAL, "%s is not aligned to its element size", name);
+  buffers.add(name, p, bytes);
   return LAQ_OK;
 }
 
@@ -1330,14 +1328,19 @@ extern "C" size_t laq_linear_workspace_bytes(const laq_linear_call* c, int32_t b
 extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream,
                                          char* errbuf, size_t errbuf_len) {
   const Err e{errbuf, errbuf_len};
-  LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, laq_linear_workspace_bytes(c, 0)));
+  const size_t need = laq_linear_workspace_bytes(c, 0);
+  LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, need));
   if (c->M == 0) return LAQ_OK;
-  LAQ_TRY(check_tensor(e, "x", c->x, true, c->ld_x, c->K, 2));
-  LAQ_TRY(check_tensor(e, "w", c->w, true, c->ld_w, c->K, 2));
-  LAQ_TRY(check_tensor(e, "bias", c->bias, false, c->N, c->N, 2));
-  LAQ_TRY(check_tensor(e, "residual", c->residual, false, c->ld_residual, c->N, 2));
-  LAQ_TRY(check_tensor(e, "y", c->y, true, c->ld_y, c->N, 2));
-  LAQ_TRY(check_tensor(e, "z", c->z, false, c->ld_z, c->N, 2));
+  Buffers buffers;
+  buffers.add("status", c->status, 4);
+  if (need) buffers.add("the workspace", d_workspace, 1);
+  LAQ_TRY(check_tensor(e, buffers, "x", c->x, true, c->ld_x, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "w", c->w, true, c->ld_w, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "bias", c->bias, false, c->N, c->N, 2));
+  LAQ_TRY(check_tensor(e, buffers, "residual", c->residual, false, c->ld_residual, c->N, 2));
+  LAQ_TRY(check_tensor(e, buffers, "y", c->y, true, c->ld_y, c->N, 2));
+  LAQ_TRY(check_tensor(e, buffers, "z", c->z, false, c->ld_z, c->N, 2));
+  LAQ_TRY(buffers.check(errbuf, errbuf_len));
   cudaStream_t st = (cudaStream_t)cuda_stream;
   char* ws = (char*)d_workspace;
   Operand x{c->x, c->ld_x, c->M, c->K}, w{c->w, c->ld_w, c->N, c->K};
@@ -1361,7 +1364,8 @@ extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_works
 extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream,
                                           char* errbuf, size_t errbuf_len) {
   const Err e{errbuf, errbuf_len};
-  LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, laq_linear_workspace_bytes(c, 1)));
+  const size_t ws_bytes = laq_linear_workspace_bytes(c, 1);
+  LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, ws_bytes));
   if (!c->dx && !c->dw && !c->db) return LAQ_OK;
   const bool act = c->activation != LAQ_ACT_NONE;
   const int dw_bytes = c->dw_dtype == LAQ_F32 ? 4 : 2;
@@ -1370,21 +1374,26 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
   if (c->dw && c->dw_dtype == LAQ_F32 && act && c->activation != LAQ_ACT_RELU)
     return fail(errbuf, errbuf_len, LAQ_EINVAL,
                 "dw in fp32 needs no activation or ReLU: with the others dZ is rounded to 16 bits before the product");
-  LAQ_TRY(check_tensor(e, "dw", c->dw, false, c->ld_dw, c->K, dw_bytes));
-  LAQ_TRY(check_tensor(e, "db", c->db, false, c->N, c->N, 4));
+  Buffers buffers;
+  buffers.add("status", c->status, 4);
+  if (ws_bytes) buffers.add("the workspace", d_workspace, 1);
+  LAQ_TRY(check_tensor(e, buffers, "dw", c->dw, false, c->ld_dw, c->K, dw_bytes));
+  LAQ_TRY(check_tensor(e, buffers, "db", c->db, false, c->N, c->N, 4));
   cudaStream_t st = (cudaStream_t)cuda_stream;
   if (c->M == 0) {               // sums over no rows
+    LAQ_TRY(buffers.check(errbuf, errbuf_len));
     if (c->dw && cudaMemset2DAsync(c->dw, (size_t)c->ld_dw * dw_bytes, 0, (size_t)c->K * dw_bytes, (size_t)c->N, st) != cudaSuccess)
       return fail(errbuf, errbuf_len, LAQ_ECUDA, "cudaMemset2DAsync failed");
     if (c->db && cudaMemsetAsync(c->db, 0, (size_t)c->N * 4, st) != cudaSuccess)
       return fail(errbuf, errbuf_len, LAQ_ECUDA, "cudaMemsetAsync failed");
     return LAQ_OK;
   }
-  LAQ_TRY(check_tensor(e, "dy", c->dy, true, c->ld_dy, c->N, 2));
-  LAQ_TRY(check_tensor(e, "z", c->z, act, c->ld_z, c->N, 2));
-  LAQ_TRY(check_tensor(e, "x", c->x, c->dw != nullptr, c->ld_x, c->K, 2));
-  LAQ_TRY(check_tensor(e, "w", c->w, c->dx != nullptr, c->ld_w, c->K, 2));
-  LAQ_TRY(check_tensor(e, "dx", c->dx, false, c->ld_dx, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "dy", c->dy, true, c->ld_dy, c->N, 2));
+  if (act) LAQ_TRY(check_tensor(e, buffers, "z", c->z, true, c->ld_z, c->N, 2));
+  if (c->dw) LAQ_TRY(check_tensor(e, buffers, "x", c->x, true, c->ld_x, c->K, 2));
+  if (c->dx) LAQ_TRY(check_tensor(e, buffers, "w", c->w, true, c->ld_w, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "dx", c->dx, false, c->ld_dx, c->K, 2));
+  LAQ_TRY(buffers.check(errbuf, errbuf_len));
   BackwardNeeds need(c);
   char* ws = (char*)d_workspace;
   const bool starve = (c->flags & LAQ_LINEAR_STARVE) != 0;

@@ -1427,15 +1427,12 @@ laq_status check_rows(const Err& e, const void* x, int dtype, int64_t T, int64_t
   if (!(tau >= 1e-4f && tau <= 1e4f)) return fail(e.buf, e.len, LAQ_EINVAL, "temperature must be 1e-4..1e4");
   if (T == 0) return LAQ_OK;
   if (!x) return fail(e.buf, e.len, LAQ_EINVAL, "null pointer");
-  if (((uintptr_t)x % (uintptr_t)bytes) != 0) return fail(e.buf, e.len, LAQ_EINVAL, "logits are not aligned to their element size");
-  const char* msg = wrong_device(x);
-  return msg ? fail(e.buf, e.len, LAQ_EINVAL, "%s", msg) : LAQ_OK;
+  return LAQ_OK;
 }
 
 laq_status check_gradient(const Err& e, const void* x, int64_t ld, const void* dx, int64_t ld_d, int dtype, int64_t T, int64_t V) {
   const int bytes = dtype_bytes(dtype);
   if (!dx) return fail(e.buf, e.len, LAQ_EINVAL, "null pointer");
-  if (((uintptr_t)dx % (uintptr_t)bytes) != 0) return fail(e.buf, e.len, LAQ_EINVAL, "the gradient is not aligned to its element size");
   if (ld_d < V) return fail(e.buf, e.len, LAQ_EINVAL, "a row stride must be at least vocab");
   const uintptr_t a0 = (uintptr_t)x, a1 = a0 + ((uintptr_t)(T - 1) * ld + V) * bytes;
   const uintptr_t b0 = (uintptr_t)dx, b1 = b0 + ((uintptr_t)(T - 1) * ld_d + V) * bytes;
@@ -1481,6 +1478,18 @@ extern "C" laq_status laq_token_logprobs(const void* d_logits, int32_t dtype, in
   if (rows == 0) return LAQ_OK;
   if (d_logprob && !d_tokens) return fail(errbuf, errbuf_len, LAQ_EINVAL, "log probabilities need tokens");
   if (top_k && (!d_top_tokens || !d_top_logprobs)) return fail(errbuf, errbuf_len, LAQ_EINVAL, "null pointer");
+  Buffers buffers;
+  buffers.add("logits", d_logits, dtype_bytes(dtype));
+  buffers.add("tokens", d_tokens, 4);
+  buffers.add("logprob", d_logprob, 4);
+  buffers.add("entropy", d_entropy, 4);
+  buffers.add("lse", d_lse, 4);
+  if (top_k) {
+    buffers.add("top_tokens", d_top_tokens, 4);
+    buffers.add("top_logprobs", d_top_logprobs, 4);
+  }
+  const laq_status ok = buffers.check(errbuf, errbuf_len);
+  if (ok != LAQ_OK) return ok;
   ForwardArgs A = {};
   A.x = d_logits;
   A.ld = row_stride;
@@ -1508,6 +1517,16 @@ extern "C" laq_status laq_token_logprobs_backward(const void* d_logits, int32_t 
   if (!d_tokens || !d_lse) return fail(errbuf, errbuf_len, LAQ_EINVAL, "null pointer");
   if (d_grad_entropy && !d_entropy) return fail(errbuf, errbuf_len, LAQ_EINVAL, "the gradient of the entropy needs the entropy");
   st = check_gradient(e, d_logits, row_stride, d_grad_logits, grad_row_stride, dtype, rows, vocab);
+  if (st != LAQ_OK) return st;
+  Buffers buffers;
+  buffers.add("logits", d_logits, dtype_bytes(dtype));
+  buffers.add("tokens", d_tokens, 4);
+  buffers.add("lse", d_lse, 4);
+  buffers.add("entropy", d_entropy, 4);
+  buffers.add("grad_logprob", d_grad_logprob, 4);
+  buffers.add("grad_entropy", d_grad_entropy, 4);
+  buffers.add("grad_logits", d_grad_logits, dtype_bytes(dtype));
+  st = buffers.check(errbuf, errbuf_len);
   if (st != LAQ_OK) return st;
   GradArgs A = {};
   A.x = d_logits;
@@ -1549,6 +1568,16 @@ extern "C" laq_status laq_distill(const void* d_logits, int32_t dtype, int64_t r
     st = check_gradient(e, d_logits, row_stride, d_grad_logits, grad_row_stride, dtype, rows, vocab);
     if (st != LAQ_OK) return st;
   }
+  Buffers buffers;
+  buffers.add("logits", d_logits, dtype_bytes(dtype));
+  buffers.add("teacher_tokens", d_teacher_tokens, 4);
+  buffers.add("teacher_logits", d_teacher_logits, 4);
+  buffers.add("loss", d_loss, 4);
+  buffers.add("lse", d_lse, 4);
+  buffers.add("grad_loss", d_grad_loss, 4);
+  buffers.add("grad_logits", d_grad_logits, dtype_bytes(dtype));
+  st = buffers.check(errbuf, errbuf_len);
+  if (st != LAQ_OK) return st;
   cudaStream_t s = (cudaStream_t)cuda_stream;
   const bool fits = dtype == LAQ_F32 ? step_fits<float>(vocab) : step_fits<__half>(vocab);
   if (!d_grad_logits || !fits) {
@@ -1600,6 +1629,15 @@ extern "C" laq_status laq_distill_backward(const void* d_logits, int32_t dtype, 
   if (st != LAQ_OK) return st;
   if (!d_lse || !d_grad_loss) return fail(errbuf, errbuf_len, LAQ_EINVAL, "null pointer");
   st = check_gradient(e, d_logits, row_stride, d_grad_logits, grad_row_stride, dtype, rows, vocab);
+  if (st != LAQ_OK) return st;
+  Buffers buffers;
+  buffers.add("logits", d_logits, dtype_bytes(dtype));
+  buffers.add("teacher_tokens", d_teacher_tokens, 4);
+  buffers.add("teacher_logits", d_teacher_logits, 4);
+  buffers.add("lse", d_lse, 4);
+  buffers.add("grad_loss", d_grad_loss, 4);
+  buffers.add("grad_logits", d_grad_logits, dtype_bytes(dtype));
+  st = buffers.check(errbuf, errbuf_len);
   if (st != LAQ_OK) return st;
   GradArgs A = {};
   A.x = d_logits;

@@ -1,0 +1,100 @@
+"""Every pointer of an operator's C call is looked at before the call touches the device: here (no GPU needed) that a
+misaligned one is refused by its name, whichever it is.  tests/test_gpu_ops_buffers.py does the same with host memory."""
+import ctypes as C
+
+import pytest
+
+from paper_1909_07588_b200 import build, laq
+
+
+@pytest.fixture(scope="module")
+def lib():
+    build.build()
+    return laq.load_library()
+
+
+T, V, K = 4, 16, 3
+A = 1 << 20         # addresses that lie far apart: nothing is ever read from them here
+ROWS = {
+    "laq_token_logprobs": dict(
+        order=["logits", 0, T, V, V, 1.0, "tokens", 2, "logprob", "entropy", "lse", "top_tokens", "top_logprobs"]),
+    "laq_token_logprobs_backward": dict(
+        order=["logits", 0, T, V, V, 1.0, "tokens", "lse", "entropy", "grad_logprob", "grad_entropy", "grad_logits", V]),
+    "laq_distill": dict(
+        order=["logits", 0, T, V, V, 1.0, "teacher_tokens", "teacher_logits", K, K, "loss", "lse", "grad_loss", "grad_logits", V]),
+    "laq_distill_backward": dict(
+        order=["logits", 0, T, V, V, 1.0, "teacher_tokens", "teacher_logits", K, K, "lse", "grad_loss", "grad_logits", V]),
+}
+
+
+def row_call(lib, name, place, dtype=0):
+    """(status, text) of the call with the pointers that `place` gives for the names of its arguments."""
+    args = [place(a) if isinstance(a, str) else a for a in ROWS[name]["order"]]
+    args[1] = dtype
+    err = C.create_string_buffer(256)
+    rc = getattr(lib, name)(*args, None, err, 256)
+    return rc, err.value.decode()
+
+
+def pointers(name):
+    return [a for a in ROWS[name]["order"] if isinstance(a, str)]
+
+
+LINEAR = {
+    0: ["x", "w", "bias", "residual", "y", "z", "status"],
+    1: ["dy", "z", "x", "w", "dx", "dw", "db", "status"],
+}
+COLS = dict(x=64, w=64, dx=64, dw=64)       # the others have rows of 48
+
+
+def linear_call(lib, backward, place, workspace=None, M=32):
+    c = laq.laq_linear_call()
+    c.dtype, c.activation, c.M, c.N, c.K, c.dw_dtype = 1, 1, M, 48, 64, 0
+    for name in LINEAR[backward]:
+        setattr(c, name, place(name))
+        if hasattr(c, "ld_" + name):
+            setattr(c, "ld_" + name, COLS.get(name, 48))
+    need = lib.laq_linear_workspace_bytes(C.byref(c), backward)
+    err = C.create_string_buffer(256)
+    f = lib.laq_linear_backward if backward else lib.laq_linear_forward
+    rc = f(C.byref(c), (workspace if need else None), need, None, err, 256)
+    return rc, err.value.decode()
+
+
+@pytest.mark.parametrize("name", sorted(ROWS))
+def test_row_calls_name_the_misaligned_buffer(lib, name):
+    at = {n: A * (i + 1) for i, n in enumerate(pointers(name))}
+    for bad in pointers(name):
+        rc, text = row_call(lib, name, lambda n: at[n] + (2 if n == bad else 0))
+        assert rc == laq.LAQ_EINVAL and "aligned" in text and bad in text
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+def test_linear_names_the_misaligned_buffer(lib, backward):
+    at = {n: A * (i + 1) for i, n in enumerate(LINEAR[backward])}
+    for bad in LINEAR[backward]:
+        rc, text = linear_call(lib, backward, lambda n: at[n] + (1 if n == bad else 0), workspace=64 * A)
+        assert rc == laq.LAQ_EINVAL and "aligned" in text and bad in text
+
+
+def test_buffers_that_a_call_does_not_use_do_not_matter(lib):
+    """Alternatives' places without alternatives; what only the other product of a gradient reads."""
+    err = C.create_string_buffer(256)
+    rc = lib.laq_token_logprobs(A, 0, T, V, V, 1.0, None, 0, None, 2 * A, 3 * A, 5, 7, None, err, 256)
+    assert "aligned" not in err.value.decode()
+    at = {n: A * (i + 1) for i, n in enumerate(LINEAR[1])}
+    for gone, unused in (("dw", "x"), ("dx", "w")):
+        _, text = linear_call(lib, 1, lambda n: None if n == gone else 5 if n == unused else at[n], workspace=64 * A)
+        assert "aligned" not in text
+
+
+def test_without_a_device_every_call_says_so(lib):
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("there is a device")
+    for name in ROWS:
+        rc, text = row_call(lib, name, lambda n: A * (pointers(name).index(n) + 1))
+        assert rc == laq.LAQ_EINVAL and "no current CUDA device" in text
+    for backward in (0, 1):
+        rc, text = linear_call(lib, backward, lambda n: A * (LINEAR[backward].index(n) + 1), workspace=64 * A)
+        assert rc == laq.LAQ_EINVAL and "no current CUDA device" in text
