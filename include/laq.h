@@ -402,7 +402,8 @@ typedef struct {
  * time (two streams, two replayed graphs) need workspaces of their own. */
 size_t laq_linear_workspace_bytes(const laq_linear_call* call /* HOST */, int32_t backward);
 
-/* y (and z, if given).  Inputs must not overlap outputs, except that residual may be y itself. */
+/* y (and z, if given).  An output that shares memory with another buffer of the call is refused (LAQ_EINVAL), except that residual
+ * may be y itself (same pointer and stride).  Rows may lie between another tensor's, as column halves of one matrix do. */
 laq_status laq_linear_forward(const laq_linear_call* call /* HOST */, void* d_workspace, size_t workspace_bytes, void* cuda_stream,
                               char* errbuf, size_t errbuf_len);
 

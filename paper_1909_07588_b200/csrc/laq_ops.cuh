@@ -11,6 +11,7 @@
 
 #include <cstdarg>
 #include <cstdio>
+#include <cstring>
 
 #include "laq.h"
 
@@ -43,16 +44,56 @@ inline PointerAttributesFn pointer_attributes_fn() {
   return fn;
 }
 
+// Bytes in rows: [p + i pitch, p + i pitch + width) for i < rows.
+struct Extent {
+  uintptr_t p;
+  unsigned long long rows, pitch, width;
+  uintptr_t end() const { return p + (rows - 1) * pitch + width; }
+  bool meets(uintptr_t a, uintptr_t b) const {      // a row of it and [a, b)
+    if (b <= p || end() <= a) return false;
+    const unsigned long long i = a < p + width ? 0 : (a - p - width) / pitch + 1;      // the first row that ends behind a
+    return i < rows && p + i * pitch < b;
+  }
+  // Rows of two matrices may lie between each other (halves of the columns of one, every other row): exact.
+  bool meets(const Extent& o) const {
+    if (!rows || !o.rows || !width || !o.width || o.end() <= p || end() <= o.p) return false;
+    if (pitch == o.pitch && rows > 1 && o.rows > 1) {      // all rows lie alike: o's row 0 is q rows and r bytes into this one
+      const bool behind = o.p >= p;
+      const unsigned long long d = behind ? o.p - p : p - o.p, q = d / pitch, r = d % pitch;
+      const Extent &a = behind ? *this : o, &b = behind ? o : *this;
+      // b's row i meets a's row q + i (r < a.width) or q + i + 1 (r + b.width > pitch)
+      return (r < a.width && q < a.rows) || (r + b.width > pitch && q + 1 < a.rows);
+    }
+    const Extent &few = rows <= o.rows ? *this : o, &many = rows <= o.rows ? o : *this;
+    for (unsigned long long i = 0; i < few.rows; ++i)
+      if (many.meets(few.p + i * few.pitch, few.p + i * few.pitch + few.width)) return true;
+    return false;
+  }
+};
+
 // The buffers of a call, all of which are looked at before its first kernel runs: each must be aligned to its elements and lie
-// in the memory of the current device, where the kernels run.  A null pointer (an optional buffer) is left out.
+// in the memory of the current device, where the kernels run, and one that is written may share no byte with any other.  A
+// null pointer (an optional buffer) is left out.
 class Buffers {
  public:
-  void add(const char* name, const void* p, int bytes) {
-    if (p && count_ < kMost) list_[count_++] = Buffer{name, (uintptr_t)p, bytes};
+  // rows x cols elements of `bytes` bytes, rows ld elements apart.  in_place: the name of the one buffer that an output may be
+  void in(const char* name, const void* p, int bytes, long long rows, long long cols, long long ld) { add(name, p, bytes, rows, cols, ld, false, ""); }
+  void out(const char* name, const void* p, int bytes, long long rows, long long cols, long long ld, const char* in_place = "") {
+    add(name, p, bytes, rows, cols, ld, true, in_place);
   }
   laq_status check(char* errbuf, size_t errlen) const {
+    for (int i = 0; i < count_; ++i) {
+      const Buffer& b = list_[i];
+      if (b.p % (uintptr_t)b.bytes) return fail(errbuf, errlen, LAQ_EINVAL, "%s is not aligned to its element size", b.name);
+      if ((double)b.x.rows * (double)b.x.pitch > kAddressable) return fail(errbuf, errlen, LAQ_EINVAL, "the rows of %s reach beyond any memory", b.name);
+    }
     for (int i = 0; i < count_; ++i)
-      if (list_[i].p % (uintptr_t)list_[i].bytes) return fail(errbuf, errlen, LAQ_EINVAL, "%s is not aligned to its element size", list_[i].name);
+      for (int j = 0; j < count_; ++j) {
+        const Buffer &a = list_[i], &b = list_[j];
+        if (!a.written || i == j || (b.written && j < i)) continue;
+        const bool itself = a.p == b.p && a.x.pitch == b.x.pitch && !strcmp(a.in_place, b.name);
+        if (!itself && a.x.meets(b.x)) return fail(errbuf, errlen, LAQ_EINVAL, "%s and %s overlap", a.name, b.name);
+      }
     int dev = -1;
     const PointerAttributesFn attributes = pointer_attributes_fn();
     if (cudaGetDevice(&dev) != cudaSuccess || !attributes) {
@@ -82,8 +123,18 @@ class Buffers {
     const char* name;
     uintptr_t p;
     int bytes;
+    bool written;
+    const char* in_place;
+    Extent x;
   };
+  void add(const char* name, const void* p, int bytes, long long rows, long long cols, long long ld, bool written, const char* in_place) {
+    if (!p || count_ == kMost) return;
+    const long long pitch = rows <= 1 ? cols : ld < kAddressable ? ld : (long long)kAddressable;
+    list_[count_++] = Buffer{name, (uintptr_t)p, bytes, written, in_place,
+                             Extent{(uintptr_t)p, (unsigned long long)rows, (unsigned long long)pitch * bytes, (unsigned long long)cols * bytes}};
+  }
   static constexpr int kMost = 16;       // more than any call has
+  static constexpr double kAddressable = 1.4e17;      // 2^57 bytes
   Buffer list_[kMost];
   int count_ = 0;
 };

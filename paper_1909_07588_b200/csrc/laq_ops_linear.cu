@@ -1299,10 +1299,13 @@ laq_status check_call(const Err& e, const laq_linear_call* c, void* ws, size_t w
 }
 
 // One tensor of a call: there if it must be, rows no shorter than their length.  It is added to the buffers.
-laq_status check_tensor(const Err& e, Buffers& buffers, const char* name, const void* p, bool required, int64_t ld, int64_t cols, int bytes) {
+enum Access { kRead, kWritten };
+laq_status check_tensor(const Err& e, Buffers& buffers, const char* name, Access access, const void* p, bool required, int64_t rows, int64_t ld,
+                        int64_t cols, int bytes, const char* in_place = "") {
   if (!p) return required ? fail(e.buf, e.len, LAQ_EINVAL, "%s is null", name) : LAQ_OK;
   if (ld < cols) return fail(e.buf, e.len, LAQ_EINVAL, "the row stride of %s is shorter than its rows", name);
-  buffers.add(name, p, bytes);
+  if (access == kWritten) buffers.out(name, p, bytes, rows, cols, ld, in_place);
+  else buffers.in(name, p, bytes, rows, cols, ld);
   return LAQ_OK;
 }
 
@@ -1332,14 +1335,14 @@ extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_works
   LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, need));
   if (c->M == 0) return LAQ_OK;
   Buffers buffers;
-  buffers.add("status", c->status, 4);
-  if (need) buffers.add("the workspace", d_workspace, 1);
-  LAQ_TRY(check_tensor(e, buffers, "x", c->x, true, c->ld_x, c->K, 2));
-  LAQ_TRY(check_tensor(e, buffers, "w", c->w, true, c->ld_w, c->K, 2));
-  LAQ_TRY(check_tensor(e, buffers, "bias", c->bias, false, c->N, c->N, 2));
-  LAQ_TRY(check_tensor(e, buffers, "residual", c->residual, false, c->ld_residual, c->N, 2));
-  LAQ_TRY(check_tensor(e, buffers, "y", c->y, true, c->ld_y, c->N, 2));
-  LAQ_TRY(check_tensor(e, buffers, "z", c->z, false, c->ld_z, c->N, 2));
+  buffers.out("status", c->status, 4, 1, 1, 1);
+  if (need) buffers.out("the workspace", d_workspace, 1, 1, (long long)need, (long long)need);
+  LAQ_TRY(check_tensor(e, buffers, "x", kRead, c->x, true, c->M, c->ld_x, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "w", kRead, c->w, true, c->N, c->ld_w, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "bias", kRead, c->bias, false, 1, c->N, c->N, 2));
+  LAQ_TRY(check_tensor(e, buffers, "residual", kRead, c->residual, false, c->M, c->ld_residual, c->N, 2));
+  LAQ_TRY(check_tensor(e, buffers, "y", kWritten, c->y, true, c->M, c->ld_y, c->N, 2, "residual"));
+  LAQ_TRY(check_tensor(e, buffers, "z", kWritten, c->z, false, c->M, c->ld_z, c->N, 2));
   LAQ_TRY(buffers.check(errbuf, errbuf_len));
   cudaStream_t st = (cudaStream_t)cuda_stream;
   char* ws = (char*)d_workspace;
@@ -1375,10 +1378,10 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
     return fail(errbuf, errbuf_len, LAQ_EINVAL,
                 "dw in fp32 needs no activation or ReLU: with the others dZ is rounded to 16 bits before the product");
   Buffers buffers;
-  buffers.add("status", c->status, 4);
-  if (ws_bytes) buffers.add("the workspace", d_workspace, 1);
-  LAQ_TRY(check_tensor(e, buffers, "dw", c->dw, false, c->ld_dw, c->K, dw_bytes));
-  LAQ_TRY(check_tensor(e, buffers, "db", c->db, false, c->N, c->N, 4));
+  buffers.out("status", c->status, 4, 1, 1, 1);
+  if (ws_bytes) buffers.out("the workspace", d_workspace, 1, 1, (long long)ws_bytes, (long long)ws_bytes);
+  LAQ_TRY(check_tensor(e, buffers, "dw", kWritten, c->dw, false, c->N, c->ld_dw, c->K, dw_bytes));
+  LAQ_TRY(check_tensor(e, buffers, "db", kWritten, c->db, false, 1, c->N, c->N, 4));
   cudaStream_t st = (cudaStream_t)cuda_stream;
   if (c->M == 0) {               // sums over no rows
     LAQ_TRY(buffers.check(errbuf, errbuf_len));
@@ -1388,11 +1391,11 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
       return fail(errbuf, errbuf_len, LAQ_ECUDA, "cudaMemsetAsync failed");
     return LAQ_OK;
   }
-  LAQ_TRY(check_tensor(e, buffers, "dy", c->dy, true, c->ld_dy, c->N, 2));
-  if (act) LAQ_TRY(check_tensor(e, buffers, "z", c->z, true, c->ld_z, c->N, 2));
-  if (c->dw) LAQ_TRY(check_tensor(e, buffers, "x", c->x, true, c->ld_x, c->K, 2));
-  if (c->dx) LAQ_TRY(check_tensor(e, buffers, "w", c->w, true, c->ld_w, c->K, 2));
-  LAQ_TRY(check_tensor(e, buffers, "dx", c->dx, false, c->ld_dx, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "dy", kRead, c->dy, true, c->M, c->ld_dy, c->N, 2));
+  if (act) LAQ_TRY(check_tensor(e, buffers, "z", kRead, c->z, true, c->M, c->ld_z, c->N, 2));
+  if (c->dw) LAQ_TRY(check_tensor(e, buffers, "x", kRead, c->x, true, c->M, c->ld_x, c->K, 2));
+  if (c->dx) LAQ_TRY(check_tensor(e, buffers, "w", kRead, c->w, true, c->N, c->ld_w, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "dx", kWritten, c->dx, false, c->M, c->ld_dx, c->K, 2));
   LAQ_TRY(buffers.check(errbuf, errbuf_len));
   BackwardNeeds need(c);
   char* ws = (char*)d_workspace;

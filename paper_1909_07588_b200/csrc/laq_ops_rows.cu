@@ -1479,14 +1479,14 @@ extern "C" laq_status laq_token_logprobs(const void* d_logits, int32_t dtype, in
   if (d_logprob && !d_tokens) return fail(errbuf, errbuf_len, LAQ_EINVAL, "log probabilities need tokens");
   if (top_k && (!d_top_tokens || !d_top_logprobs)) return fail(errbuf, errbuf_len, LAQ_EINVAL, "null pointer");
   Buffers buffers;
-  buffers.add("logits", d_logits, dtype_bytes(dtype));
-  buffers.add("tokens", d_tokens, 4);
-  buffers.add("logprob", d_logprob, 4);
-  buffers.add("entropy", d_entropy, 4);
-  buffers.add("lse", d_lse, 4);
+  buffers.in("logits", d_logits, dtype_bytes(dtype), rows, vocab, row_stride);
+  buffers.in("tokens", d_tokens, 4, 1, rows, rows);
+  buffers.out("logprob", d_logprob, 4, 1, rows, rows);
+  buffers.out("entropy", d_entropy, 4, 1, rows, rows);
+  buffers.out("lse", d_lse, 4, 1, rows, rows);
   if (top_k) {
-    buffers.add("top_tokens", d_top_tokens, 4);
-    buffers.add("top_logprobs", d_top_logprobs, 4);
+    buffers.out("top_tokens", d_top_tokens, 4, rows, top_k, top_k);
+    buffers.out("top_logprobs", d_top_logprobs, 4, rows, top_k, top_k);
   }
   const laq_status ok = buffers.check(errbuf, errbuf_len);
   if (ok != LAQ_OK) return ok;
@@ -1519,13 +1519,13 @@ extern "C" laq_status laq_token_logprobs_backward(const void* d_logits, int32_t 
   st = check_gradient(e, d_logits, row_stride, d_grad_logits, grad_row_stride, dtype, rows, vocab);
   if (st != LAQ_OK) return st;
   Buffers buffers;
-  buffers.add("logits", d_logits, dtype_bytes(dtype));
-  buffers.add("tokens", d_tokens, 4);
-  buffers.add("lse", d_lse, 4);
-  buffers.add("entropy", d_entropy, 4);
-  buffers.add("grad_logprob", d_grad_logprob, 4);
-  buffers.add("grad_entropy", d_grad_entropy, 4);
-  buffers.add("grad_logits", d_grad_logits, dtype_bytes(dtype));
+  buffers.in("logits", d_logits, dtype_bytes(dtype), rows, vocab, row_stride);
+  buffers.in("tokens", d_tokens, 4, 1, rows, rows);
+  buffers.in("lse", d_lse, 4, 1, rows, rows);
+  buffers.in("entropy", d_entropy, 4, 1, rows, rows);
+  buffers.in("grad_logprob", d_grad_logprob, 4, 1, rows, rows);
+  buffers.in("grad_entropy", d_grad_entropy, 4, 1, rows, rows);
+  buffers.out("grad_logits", d_grad_logits, dtype_bytes(dtype), rows, vocab, grad_row_stride, "logits");
   st = buffers.check(errbuf, errbuf_len);
   if (st != LAQ_OK) return st;
   GradArgs A = {};
@@ -1569,13 +1569,13 @@ extern "C" laq_status laq_distill(const void* d_logits, int32_t dtype, int64_t r
     if (st != LAQ_OK) return st;
   }
   Buffers buffers;
-  buffers.add("logits", d_logits, dtype_bytes(dtype));
-  buffers.add("teacher_tokens", d_teacher_tokens, 4);
-  buffers.add("teacher_logits", d_teacher_logits, 4);
-  buffers.add("loss", d_loss, 4);
-  buffers.add("lse", d_lse, 4);
-  buffers.add("grad_loss", d_grad_loss, 4);
-  buffers.add("grad_logits", d_grad_logits, dtype_bytes(dtype));
+  buffers.in("logits", d_logits, dtype_bytes(dtype), rows, vocab, row_stride);
+  buffers.in("teacher_tokens", d_teacher_tokens, 4, rows, teacher_k, teacher_stride);
+  buffers.in("teacher_logits", d_teacher_logits, 4, rows, teacher_k, teacher_stride);
+  buffers.out("loss", d_loss, 4, 1, rows, rows);
+  buffers.out("lse", d_lse, 4, 1, rows, rows);
+  buffers.in("grad_loss", d_grad_loss, 4, 1, rows, rows);
+  buffers.out("grad_logits", d_grad_logits, dtype_bytes(dtype), rows, vocab, grad_row_stride, "logits");
   st = buffers.check(errbuf, errbuf_len);
   if (st != LAQ_OK) return st;
   cudaStream_t s = (cudaStream_t)cuda_stream;
@@ -1631,12 +1631,12 @@ extern "C" laq_status laq_distill_backward(const void* d_logits, int32_t dtype, 
   st = check_gradient(e, d_logits, row_stride, d_grad_logits, grad_row_stride, dtype, rows, vocab);
   if (st != LAQ_OK) return st;
   Buffers buffers;
-  buffers.add("logits", d_logits, dtype_bytes(dtype));
-  buffers.add("teacher_tokens", d_teacher_tokens, 4);
-  buffers.add("teacher_logits", d_teacher_logits, 4);
-  buffers.add("lse", d_lse, 4);
-  buffers.add("grad_loss", d_grad_loss, 4);
-  buffers.add("grad_logits", d_grad_logits, dtype_bytes(dtype));
+  buffers.in("logits", d_logits, dtype_bytes(dtype), rows, vocab, row_stride);
+  buffers.in("teacher_tokens", d_teacher_tokens, 4, rows, teacher_k, teacher_stride);
+  buffers.in("teacher_logits", d_teacher_logits, 4, rows, teacher_k, teacher_stride);
+  buffers.in("lse", d_lse, 4, 1, rows, rows);
+  buffers.in("grad_loss", d_grad_loss, 4, 1, rows, rows);
+  buffers.out("grad_logits", d_grad_logits, dtype_bytes(dtype), rows, vocab, grad_row_stride, "logits");
   st = buffers.check(errbuf, errbuf_len);
   if (st != LAQ_OK) return st;
   GradArgs A = {};

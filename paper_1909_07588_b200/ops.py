@@ -8,9 +8,10 @@ The library's own models end at 16 classes and one hidden layer; a larger model'
 ``distill`` / ``distill_backward``                   divergence from a teacher's top logits; gradient, alone or with the loss
 
 Tensors are CUDA tensors with unit stride within a row and any row stride; outputs are allocated here unless ``out`` is
-given, which must not overlap the inputs other than where a call says so.  Gradients are calls of their own: none of this
-takes part in torch's autograd.  Calls run on ``stream`` (default: the current stream of the tensors' device) and do not synchronise.  They launch
-kernels only: there is no CPU fallback.  ``check_status`` reports a bounded wait of the product kernels that ran out.
+given, which is refused if it shares memory with another tensor of the call other than where a call says so.  Gradients
+are calls of their own: none of this takes part in torch's autograd.  Calls run on ``stream`` (default: the current stream
+of the tensors' device) and do not synchronise.  They launch kernels only: there is no CPU fallback.  ``check_status``
+reports a bounded wait of the product kernels that ran out.
 """
 import ctypes as C
 import threading

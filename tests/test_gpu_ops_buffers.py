@@ -66,3 +66,20 @@ def test_memory_of_a_private_pool_is_taken(lib):
     with torch.cuda.use_mem_pool(pool):
         y = x.clone()
     assert torch.equal(ops.token_logprobs(x)["lse"], ops.token_logprobs(y)["lse"])
+
+
+def test_linear_over_its_own_input_is_refused():
+    x, w = torch.randn(40, 64, device="cuda").bfloat16(), torch.randn(64, 64, device="cuda").bfloat16()
+    b = torch.randn(64, device="cuda").bfloat16()
+    before, want = x.clone(), ops.linear(x, w, b, residual=x)
+    for call in (lambda: ops.linear(x, w, out=x), lambda: ops.linear(x, w, b, residual=x, out=x), lambda: ops.linear(x[:39], w, out=x[1:]),
+                 lambda: ops.linear(x, w, out=w[:40]), lambda: ops.linear(x[:1], w, bias=b, out=b[None])):
+        with pytest.raises(laq.LaqError, match="overlap") as e:
+            call()
+        assert e.value.status == laq.LAQ_EINVAL
+    assert torch.equal(x, before)
+    # rows that lie between the input's rows are not its own
+    wide = torch.cat([x, torch.zeros_like(x)], dim=1)
+    y = ops.linear(wide[:, :64], w, b, residual=wide[:, :64], out=wide[:, 64:])
+    assert torch.equal(y, want) and torch.equal(wide[:, :64], x)
+    ops.check_status()

@@ -98,3 +98,62 @@ def test_without_a_device_every_call_says_so(lib):
     for backward in (0, 1):
         rc, text = linear_call(lib, backward, lambda n: A * (LINEAR[backward].index(n) + 1), workspace=64 * A)
         assert rc == laq.LAQ_EINVAL and "no current CUDA device" in text
+
+
+def _bytes(p, rows, cols, ld, size):
+    return {p + (r * ld + c) * size + b for r in range(rows) for c in range(cols) for b in range(size)}
+
+
+def test_linear_refuses_outputs_that_share_memory(lib):
+    """Exactly those: y against x over many geometries, byte sets deciding (w and the status lie elsewhere)."""
+    import random
+    rng = random.Random(3)
+    err = C.create_string_buffer(256)
+    seen = [0, 0]
+    for _ in range(4000):
+        M, N, K = rng.randint(1, 5), rng.randint(1, 6), rng.randint(1, 6)
+        c = laq.laq_linear_call()
+        c.dtype, c.M, c.N, c.K = 1, M, N, K
+        c.ld_x = K + rng.randint(0, 9)
+        c.ld_y = rng.choice([c.ld_x, N + rng.randint(0, 9)])
+        c.ld_y = max(c.ld_y, N)
+        c.x = A
+        c.y = A + 2 * rng.randint(-40, 40)
+        c.w, c.ld_w, c.status = 4 * A, K, 8 * A
+        shared = bool(_bytes(c.x, M, K, c.ld_x, 2) & _bytes(c.y, M, N, c.ld_y, 2))
+        need = lib.laq_linear_workspace_bytes(C.byref(c), 0)
+        rc = lib.laq_linear_forward(C.byref(c), 16 * A if need else None, need, None, err, 256)
+        assert rc == laq.LAQ_EINVAL and ("y and x overlap" if shared else "device") in err.value.decode()
+        seen[shared] += 1
+    assert min(seen) > 500
+
+
+@pytest.mark.parametrize("backward", [0, 1])
+def test_linear_refuses_every_pair_with_an_output(lib, backward):
+    at = {n: A * (i + 1) for i, n in enumerate(LINEAR[backward])}
+    outputs = ["dx", "dw", "db", "status"] if backward else ["y", "z", "status"]
+    for o in outputs:
+        for other in LINEAR[backward]:
+            if other == o:
+                continue
+            rc, text = linear_call(lib, backward, lambda n: at[other] if n == o else at[n], workspace=64 * A)
+            if (o, other) == ("y", "residual"):
+                assert "device" in text                 # the residual may be y itself
+            else:
+                assert rc == laq.LAQ_EINVAL and "overlap" in text and o in text and other in text
+    if backward:
+        rc, text = linear_call(lib, 1, lambda n: at[n], workspace=at["x"])
+        assert "workspace" in text and "overlap" in text
+        return
+    # y over a residual that is x as well would race with the product
+    rc, text = linear_call(lib, 0, lambda n: at["x"] if n in ("y", "residual") else at[n], workspace=64 * A)
+    assert "y and x overlap" in text or "x and y overlap" in text
+    rc, text = linear_call(lib, 0, lambda n: at["residual"] + 2 if n == "y" else at[n], workspace=64 * A)
+    assert "y and residual overlap" in text
+
+
+def test_strides_that_reach_beyond_any_memory_are_refused(lib):
+    err = C.create_string_buffer(256)
+    for ld in (1 << 60, 1 << 62, (1 << 63) - 1):
+        rc = lib.laq_token_logprobs(A, 0, T, V, ld, 1.0, None, 0, None, 2 * A, 3 * A, None, None, None, err, 256)
+        assert rc == laq.LAQ_EINVAL and "beyond" in err.value.decode()
