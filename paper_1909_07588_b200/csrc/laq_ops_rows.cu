@@ -1430,14 +1430,9 @@ laq_status check_rows(const Err& e, const void* x, int dtype, int64_t T, int64_t
   return LAQ_OK;
 }
 
-laq_status check_gradient(const Err& e, const void* x, int64_t ld, const void* dx, int64_t ld_d, int dtype, int64_t T, int64_t V) {
-  const int bytes = dtype_bytes(dtype);
+laq_status check_gradient(const Err& e, const void* dx, int64_t ld_d, int64_t V) {
   if (!dx) return fail(e.buf, e.len, LAQ_EINVAL, "null pointer");
   if (ld_d < V) return fail(e.buf, e.len, LAQ_EINVAL, "a row stride must be at least vocab");
-  const uintptr_t a0 = (uintptr_t)x, a1 = a0 + ((uintptr_t)(T - 1) * ld + V) * bytes;
-  const uintptr_t b0 = (uintptr_t)dx, b1 = b0 + ((uintptr_t)(T - 1) * ld_d + V) * bytes;
-  if (a0 < b1 && b0 < a1 && !(a0 == b0 && ld == ld_d))
-    return fail(e.buf, e.len, LAQ_EINVAL, "the gradient overlaps the logits: it may be the same tensor or a separate one");
   return LAQ_OK;
 }
 
@@ -1516,7 +1511,7 @@ extern "C" laq_status laq_token_logprobs_backward(const void* d_logits, int32_t 
   if (st != LAQ_OK || rows == 0) return st;
   if (!d_tokens || !d_lse) return fail(errbuf, errbuf_len, LAQ_EINVAL, "null pointer");
   if (d_grad_entropy && !d_entropy) return fail(errbuf, errbuf_len, LAQ_EINVAL, "the gradient of the entropy needs the entropy");
-  st = check_gradient(e, d_logits, row_stride, d_grad_logits, grad_row_stride, dtype, rows, vocab);
+  st = check_gradient(e, d_grad_logits, grad_row_stride, vocab);
   if (st != LAQ_OK) return st;
   Buffers buffers;
   buffers.in("logits", d_logits, dtype_bytes(dtype), rows, vocab, row_stride);
@@ -1565,7 +1560,7 @@ extern "C" laq_status laq_distill(const void* d_logits, int32_t dtype, int64_t r
   if ((d_grad_loss != nullptr) != (d_grad_logits != nullptr))
     return fail(errbuf, errbuf_len, LAQ_EINVAL, "the gradient needs both the gradient of the loss and a place for the result");
   if (d_grad_logits) {
-    st = check_gradient(e, d_logits, row_stride, d_grad_logits, grad_row_stride, dtype, rows, vocab);
+    st = check_gradient(e, d_grad_logits, grad_row_stride, vocab);
     if (st != LAQ_OK) return st;
   }
   Buffers buffers;
@@ -1628,7 +1623,7 @@ extern "C" laq_status laq_distill_backward(const void* d_logits, int32_t dtype, 
   st = check_teacher(e, d_teacher_tokens, d_teacher_logits, teacher_k, teacher_stride);
   if (st != LAQ_OK) return st;
   if (!d_lse || !d_grad_loss) return fail(errbuf, errbuf_len, LAQ_EINVAL, "null pointer");
-  st = check_gradient(e, d_logits, row_stride, d_grad_logits, grad_row_stride, dtype, rows, vocab);
+  st = check_gradient(e, d_grad_logits, grad_row_stride, vocab);
   if (st != LAQ_OK) return st;
   Buffers buffers;
   buffers.in("logits", d_logits, dtype_bytes(dtype), rows, vocab, row_stride);

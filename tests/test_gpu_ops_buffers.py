@@ -83,3 +83,29 @@ def test_linear_over_its_own_input_is_refused():
     y = ops.linear(wide[:, :64], w, b, residual=wide[:, :64], out=wide[:, 64:])
     assert torch.equal(y, want) and torch.equal(wide[:, :64], x)
     ops.check_status()
+
+
+@pytest.mark.parametrize("V", [100, 3000, 40001])
+def test_row_gradients_into_the_other_half_of_a_wide_buffer(V):
+    """Columns beside the logits' in the same rows, and the rows between them, are separate places."""
+    rows = 9
+    g = torch.Generator(device="cuda").manual_seed(V)
+    x = torch.randn(rows, V, generator=g, device="cuda").bfloat16()
+    tokens = torch.randint(0, V, (rows,), generator=g, device="cuda").int()
+    one = torch.ones(rows, device="cuda")
+    tok, val = tokens[:, None].contiguous(), torch.zeros(rows, 1, device="cuda")
+    st = ops.token_logprobs(x, tokens)
+    want = [ops.token_logprobs_backward(x, tokens, st["lse"], st["entropy"], one, one), ops.distill(x, tok, val, d_loss=one)["dlogits"],
+            ops.distill_backward(x, tok, val, st["lse"], one)]
+    calls = [lambda s, o: ops.token_logprobs_backward(s, tokens, st["lse"], st["entropy"], one, one, out=o),
+             lambda s, o: ops.distill(s, tok, val, d_loss=one, out=o)["dlogits"],
+             lambda s, o: ops.distill_backward(s, tok, val, st["lse"], one, out=o)]
+    for call, w in zip(calls, want):
+        for columns in (True, False):
+            wide = torch.zeros(rows, 2 * V, dtype=x.dtype, device="cuda") if columns else torch.zeros(2 * rows, V, dtype=x.dtype, device="cuda")
+            src, dst = (wide[:, :V], wide[:, V:]) if columns else (wide[::2], wide[1::2])
+            src.copy_(x)
+            got = call(src, dst)
+            # rows that start elsewhere within 16 bytes take their elements in another order: a step of the type at most
+            assert float((got.float() - w.float()).abs().max()) <= 2.0 ** -7 * float(w.float().abs().max())
+            assert torch.equal(src, x)

@@ -157,3 +157,47 @@ def test_strides_that_reach_beyond_any_memory_are_refused(lib):
     for ld in (1 << 60, 1 << 62, (1 << 63) - 1):
         rc = lib.laq_token_logprobs(A, 0, T, V, ld, 1.0, None, 0, None, 2 * A, 3 * A, None, None, None, err, 256)
         assert rc == laq.LAQ_EINVAL and "beyond" in err.value.decode()
+
+
+@pytest.mark.parametrize("name", ["laq_token_logprobs_backward", "laq_distill", "laq_distill_backward"])
+def test_row_gradients_refuse_exactly_what_overlaps(lib, name):
+    """The gradient's place against the logits: the logits themselves, rows between their rows (column halves of one matrix,
+    every other row) and separate memory are taken, any other common byte is refused."""
+    import random
+    rng = random.Random(4)
+    seen = [0, 0, 0]
+    for _ in range(3000):
+        rows, cols = rng.randint(1, 5), rng.randint(1, 6)
+        ld = cols + rng.randint(0, 14)
+        ld_d = rng.choice([ld, cols + rng.randint(0, 14)])
+        dtype = rng.choice([0, 1])
+        size = 4 if dtype == 0 else 2
+        x, dx = A, A + size * rng.randint(-40, 40) * rng.randint(0, 1)
+        args = list(ROWS[name]["order"])
+        grad_at = args.index("grad_logits")
+        args[2], args[3], args[4], args[grad_at + 1] = rows, cols, ld, ld_d
+        args = [(x if a == "logits" else dx if a == "grad_logits" else A * (i + 2)) if isinstance(a, str) else a for i, a in enumerate(args)]
+        args[1] = dtype
+        err = C.create_string_buffer(256)
+        rc = getattr(lib, name)(*args, None, err, 256)
+        itself = x == dx and (rows == 1 or ld == ld_d)
+        shared = bool(_bytes(x, rows, cols, ld, size) & _bytes(dx, rows, cols, ld_d, size))
+        refused = shared and not itself
+        assert rc == laq.LAQ_EINVAL and ("overlap" if refused else "device") in err.value.decode()
+        seen[2 if itself else int(shared)] += 1
+    assert min(seen) > 100
+
+
+@pytest.mark.parametrize("name", sorted(ROWS))
+def test_row_calls_refuse_every_pair_with_an_output(lib, name):
+    at = {n: A * (i + 1) for i, n in enumerate(pointers(name))}
+    outputs = {"laq_token_logprobs": ["logprob", "entropy", "lse", "top_tokens", "top_logprobs"], "laq_distill": ["loss", "lse", "grad_logits"]}
+    for o in outputs.get(name, ["grad_logits"]):
+        for other in pointers(name):
+            if other == o:
+                continue
+            rc, text = row_call(lib, name, lambda n: at[other] if n == o else at[n])
+            if (o, other) == ("grad_logits", "logits"):
+                assert "device" in text
+            else:
+                assert rc == laq.LAQ_EINVAL and "overlap" in text and o in text and other in text
