@@ -30,6 +30,22 @@ inline laq_status fail(char* errbuf, size_t errlen, laq_status st, const char* f
 
 inline int dtype_bytes(int dtype) { return dtype == LAQ_F32 ? 4 : (dtype == LAQ_BF16 || dtype == LAQ_F16) ? 2 : 0; }
 
+// The status of a launch by its own return value: an error that an earlier call of this thread has left behind is neither taken for
+// this one's nor cleared.
+inline laq_status launched(char* errbuf, size_t errlen, cudaError_t rc) {
+  if (rc == cudaSuccess) return LAQ_OK;
+  cudaGetLastError();
+  return fail(errbuf, errlen, LAQ_ECUDA, "kernel launch failed: %s", cudaGetErrorString(rc));
+}
+template <class... Params, class... Args>
+cudaError_t launch_plain(void (*kernel)(Params...), dim3 grid, unsigned threads, cudaStream_t st, Args... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.stream = st;
+  return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
+}
+
 // The driver's query of several properties of a pointer in one call (0.03 us; a call asks for up to 14 pointers).
 typedef CUresult (*PointerAttributesFn)(unsigned int, CUpointer_attribute*, void**, CUdeviceptr);
 inline PointerAttributesFn pointer_attributes_fn() {

@@ -1098,12 +1098,7 @@ laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& m
     at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
     ++cfg.numAttrs;
   }
-  const cudaError_t rc = cudaLaunchKernelEx(&cfg, kernel, ma, mb, A);
-  if (rc != cudaSuccess) {
-    cudaGetLastError();
-    return fail(e.buf, e.len, LAQ_ECUDA, "kernel launch failed: %s", cudaGetErrorString(rc));
-  }
-  return LAQ_OK;
+  return launched(e.buf, e.len, cudaLaunchKernelEx(&cfg, kernel, ma, mb, A));
 }
 
 template <class T, bool LONG>
@@ -1199,11 +1194,8 @@ laq_status launch_few(const Err& e, const GemmArgs& A, const Operand& x, const O
   const unsigned blocks = (unsigned)((groups + per_block - 1) / per_block);
   // Four vectors of each row of W under way where a lane has as many and the registers hold them (one row, 4096 x 4096: 7.4 us
   // against 8.7 us by two; 100000 x 512, where a lane has two: 26.7 us against 19.7 us).
-  if (ROWS <= 2 && items > 64 << log_parts)
-    linear_few_rows_kernel<T, ROWS, ROWS <= 2 ? 4 : 2><<<blocks, kFewThreads, 0, st>>>(A, (const T*)x.p, x.ld, (const T*)w.p, w.ld, K, vec, log_parts);
-  else
-    linear_few_rows_kernel<T, ROWS, 2><<<blocks, kFewThreads, 0, st>>>(A, (const T*)x.p, x.ld, (const T*)w.p, w.ld, K, vec, log_parts);
-  return cudaGetLastError() == cudaSuccess ? LAQ_OK : fail(e.buf, e.len, LAQ_ECUDA, "kernel launch failed");
+  const auto kernel = ROWS <= 2 && items > 64 << log_parts ? linear_few_rows_kernel<T, ROWS, ROWS <= 2 ? 4 : 2> : linear_few_rows_kernel<T, ROWS, 2>;
+  return launched(e.buf, e.len, launch_plain(kernel, dim3(blocks), kFewThreads, st, A, (const T*)x.p, x.ld, (const T*)w.p, w.ld, K, vec, log_parts));
 }
 
 template <class T>
@@ -1240,9 +1232,9 @@ laq_status make_mappable(const Err& e, Operand& o, char*& ws, cudaStream_t st) {
   if (!bytes) return LAQ_OK;
   const long long pitch = pad8(o.cols), items = o.rows * (pitch / 8);
   const long long want = (items + 255) / 256, most = 8 * kSMs;
-  linear_pack_kernel<<<(unsigned)(want < most ? want : most), 256, 0, st>>>((const uint16_t*)o.p, o.ld, (uint16_t*)ws, pitch, o.rows,
-                                                                           (int)o.cols);
-  if (cudaGetLastError() != cudaSuccess) return fail(e.buf, e.len, LAQ_ECUDA, "kernel launch failed");
+  const laq_status st_ = launched(e.buf, e.len, launch_plain(linear_pack_kernel, dim3((unsigned)(want < most ? want : most)), 256, st,
+                                                             (const uint16_t*)o.p, o.ld, (uint16_t*)ws, pitch, o.rows, (int)o.cols));
+  if (st_ != LAQ_OK) return st_;
   o.p = ws;
   o.ld = pitch;
   ws += bytes;
@@ -1385,10 +1377,8 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
   cudaStream_t st = (cudaStream_t)cuda_stream;
   if (c->M == 0) {               // sums over no rows
     LAQ_TRY(buffers.check(errbuf, errbuf_len));
-    if (c->dw && cudaMemset2DAsync(c->dw, (size_t)c->ld_dw * dw_bytes, 0, (size_t)c->K * dw_bytes, (size_t)c->N, st) != cudaSuccess)
-      return fail(errbuf, errbuf_len, LAQ_ECUDA, "cudaMemset2DAsync failed");
-    if (c->db && cudaMemsetAsync(c->db, 0, (size_t)c->N * 4, st) != cudaSuccess)
-      return fail(errbuf, errbuf_len, LAQ_ECUDA, "cudaMemsetAsync failed");
+    if (c->dw) LAQ_TRY(launched(errbuf, errbuf_len, cudaMemset2DAsync(c->dw, (size_t)c->ld_dw * dw_bytes, 0, (size_t)c->K * dw_bytes, (size_t)c->N, st)));
+    if (c->db) LAQ_TRY(launched(errbuf, errbuf_len, cudaMemsetAsync(c->db, 0, (size_t)c->N * 4, st)));
     return LAQ_OK;
   }
   LAQ_TRY(check_tensor(e, buffers, "dy", kRead, c->dy, true, c->M, c->ld_dy, c->N, 2));
@@ -1408,14 +1398,12 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
     const int per = dz_rows_per(c->M, c->N), runs = (int)((c->M + per - 1) / per), N = (int)c->N;
     const dim3 grid((unsigned)((c->N + kDzCols - 1) / kDzCols), (unsigned)runs);
     const int vec_ok = mappable(c->dy, c->ld_dy) && (!act || mappable(c->z, c->ld_z));
-    if (c->dtype == LAQ_BF16)
-      linear_dz_kernel<__nv_bfloat16><<<grid, kDzThreads, 0, st>>>((const __nv_bfloat16*)c->dy, c->ld_dy, (const __nv_bfloat16*)c->z,
-                                                                   c->ld_z, (__nv_bfloat16*)dz, pad8(c->N), part, c->M, N,
-                                                                   c->activation, per, vec_ok);
-    else
-      linear_dz_kernel<__half><<<grid, kDzThreads, 0, st>>>((const __half*)c->dy, c->ld_dy, (const __half*)c->z, c->ld_z, (__half*)dz,
-                                                            pad8(c->N), part, c->M, N, c->activation, per, vec_ok);
-    if (cudaGetLastError() != cudaSuccess) return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
+    const auto launch_dz = [&](auto zero) {
+      using T = decltype(zero);
+      return launch_plain(linear_dz_kernel<T>, grid, kDzThreads, st, (const T*)c->dy, c->ld_dy, (const T*)c->z, c->ld_z, (T*)dz, pad8(c->N),
+                          part, c->M, N, c->activation, per, vec_ok);
+    };
+    LAQ_TRY(launched(errbuf, errbuf_len, c->dtype == LAQ_BF16 ? launch_dz(__nv_bfloat16()) : launch_dz(__half())));
     follows = true;
     if (c->db) {
       cudaLaunchConfig_t cfg = {};
@@ -1427,10 +1415,7 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
       at[0].val.programmaticStreamSerializationAllowed = 1;
       cfg.attrs = at;
       cfg.numAttrs = 1;
-      if (cudaLaunchKernelEx(&cfg, linear_db_kernel, (const float*)part, runs, N, c->db) != cudaSuccess) {
-        cudaGetLastError();
-        return fail(errbuf, errbuf_len, LAQ_ECUDA, "kernel launch failed");
-      }
+      LAQ_TRY(launched(errbuf, errbuf_len, cudaLaunchKernelEx(&cfg, linear_db_kernel, (const float*)part, runs, N, c->db)));
     }
     if (need.own_dz) {
       need.dz.p = dz;

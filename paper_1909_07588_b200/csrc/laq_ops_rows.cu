@@ -1436,11 +1436,7 @@ laq_status check_gradient(const Err& e, const void* dx, int64_t ld_d, int64_t V)
   return LAQ_OK;
 }
 
-laq_status done(const Err& e, cudaError_t rc) {
-  const cudaError_t last = cudaGetLastError();
-  if (rc == cudaSuccess) rc = last;
-  return rc == cudaSuccess ? LAQ_OK : fail(e.buf, e.len, LAQ_ECUDA, "kernel launch failed: %s", cudaGetErrorString(rc));
-}
+laq_status done(const Err& e, cudaError_t rc) { return launched(e.buf, e.len, rc); }
 
 void set_temperature(ForwardArgs& A, float tau) {
   A.tau = tau;

@@ -1,0 +1,67 @@
+"""How calls of the operators stand beside each other and beside the rest of a program."""
+import os
+import subprocess
+import sys
+
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def _run(code, timeout=300):
+    """In a process of its own: what is tested is what a process does first, or what it has left behind."""
+    out = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True, timeout=timeout)
+    assert out.returncode == 0, out.stderr[-3000:]
+    return out.stdout
+
+
+def test_an_error_of_an_earlier_call_is_not_taken_for_an_operators():
+    """A library call that fails (a synchronisation on a stream under capture, refused on the host) leaves an error behind in
+    its thread; an operator that follows runs, says so, and gives the results that it gives without."""
+    assert "done" in _run("""
+import torch
+from paper_1909_07588_b200 import laq, ops
+bf = torch.bfloat16
+x, w = torch.randn(64, 96, device="cuda").to(bf), torch.randn(40, 96, device="cuda").to(bf)
+logits = torch.randn(6, 5000, device="cuda")
+tok = torch.randint(0, 5000, (6,), device="cuda").int()
+dy = torch.randn(64, 40, device="cuda").to(bf)
+one = torch.ones(6, device="cuda")
+long = torch.randn(2, 140000, device="cuda")         # distilled in two passes
+calls = [
+    lambda: [ops.token_logprobs(logits, tok, top_k=3)["logprob"]],
+    lambda: [ops.distill(logits, tok[:, None].contiguous(), one[:, None].contiguous(), d_loss=one)["dlogits"]],
+    lambda: [ops.distill(long, tok[:2, None].contiguous(), one[:2, None].contiguous(), d_loss=one[:2])["dlogits"]],
+    lambda: [ops.linear(x[:1], w)],
+    lambda: [ops.linear(x, w)],
+    lambda: [ops.linear(x[:, :95], w[:, 1:])],
+    lambda: list(ops.linear_backward(dy, x, w, z=dy, activation="gelu").values()),
+]
+want = [c() for c in calls]
+side = torch.cuda.Stream()
+with torch.cuda.stream(side):
+    ctx = laq.Laq(model=laq.MODEL_EXTERNAL, M=1, p=64, alpha=0.25, b=8, D=1, xi=[0.0], tbar=10)
+    ctx.sync()
+torch.cuda.synchronize()
+failed = 0
+for call, expected in zip(calls, want):
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        graph.capture_begin()
+        try:
+            ctx.sync()
+        except laq.LaqError:
+            failed += 1
+        try:
+            graph.capture_end()
+        except RuntimeError:
+            pass
+    got = call()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, expected))
+assert failed == len(calls)
+ops.check_status()
+print("done")
+""")
