@@ -297,9 +297,10 @@ laq_status laq_quantize_worker_static(const float* d_g, const float* d_qprev, in
  * an error text (errbuf, errbuf_len).  All tensors are DEVICE, row-major, on the calling thread's current device (checked
  * for every pointer that the call reads or writes: LAQ_EINVAL otherwise), with unit stride within a row and any row stride
  * (in elements) of at least the row's length; a pointer needs only the alignment of its element.  Calls are asynchronous,
- * allocate nothing, copy nothing to the host and can be captured into a CUDA graph.  Zero rows are allowed and launch
- * nothing.  Results do not depend on timing: sums are taken in a fixed order, in fp32, and there are no atomics on device
- * memory. */
+ * allocate nothing, copy nothing to the host and can be captured into a CUDA graph; the first call of a row operator and the
+ * first of a layer on a device load the code of all of their kernels, for which the runtime may take device memory (call
+ * once with small tensors at start-up where that matters).  Zero rows are allowed and launch nothing.  Results do not depend
+ * on timing: sums are taken in a fixed order, in fp32, and there are no atomics on device memory. */
 typedef enum {
   LAQ_F32 = 0,
   LAQ_BF16 = 1,

@@ -9,6 +9,7 @@
 #include <float.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
@@ -45,6 +46,29 @@ cudaError_t launch_plain(void (*kernel)(Params...), dim3 grid, unsigned threads,
   cfg.stream = st;
   return cudaLaunchKernelEx(&cfg, kernel, Params(args)...);
 }
+
+// The runtime loads a kernel's code on its first use, which may take device memory for it.  The first call on a device has all
+// of a file's kernels loaded (some 0.05 ms each), so that no later call takes any, whichever forms it needs.
+class Loaded {
+ public:
+  cudaError_t once(const void* const* kernels, int n) {
+    int dev = 0;
+    cudaError_t rc = cudaGetDevice(&dev);
+    if (rc != cudaSuccess) return rc;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (devices_.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    for (int i = 0; i < n; ++i) {
+      cudaFuncAttributes fa;
+      rc = cudaFuncGetAttributes(&fa, kernels[i]);
+      if (rc != cudaSuccess) return rc;
+    }
+    devices_.fetch_or(bit, std::memory_order_release);
+    return cudaSuccess;
+  }
+
+ private:
+  std::atomic<uint64_t> devices_{0};
+};
 
 // The driver's query of several properties of a pointer in one call (0.03 us; a call asks for up to 14 pointers).
 typedef CUresult (*PointerAttributesFn)(unsigned int, CUpointer_attribute*, void**, CUdeviceptr);

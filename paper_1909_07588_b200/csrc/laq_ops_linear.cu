@@ -1307,6 +1307,33 @@ laq_status check_tensor(const Err& e, Buffers& buffers, const char* name, Access
     if (st_ != LAQ_OK) return st_;   \
   } while (0)
 
+template <class T>
+void list_kernels(const void** list, int& n) {
+  const void* all[] = {
+      (const void*)linear_gemm_kernel<T, false, false, false, false>, (const void*)linear_gemm_kernel<T, true, false, false, false>,
+      (const void*)linear_gemm_kernel<T, false, true, false, false>,  (const void*)linear_gemm_kernel<T, false, false, false, true>,
+      (const void*)linear_gemm_kernel<T, true, false, false, true>,   (const void*)linear_gemm_kernel<T, false, true, false, true>,
+      (const void*)linear_gemm_kernel<T, false, false, true, false>,  (const void*)linear_gemm_kernel<T, false, true, true, false>,
+      (const void*)linear_few_rows_kernel<T, 1, 4>, (const void*)linear_few_rows_kernel<T, 1, 2>, (const void*)linear_few_rows_kernel<T, 2, 4>,
+      (const void*)linear_few_rows_kernel<T, 2, 2>, (const void*)linear_few_rows_kernel<T, 3, 2>, (const void*)linear_few_rows_kernel<T, 4, 2>,
+      (const void*)linear_dz_kernel<T>};
+  for (const void* k : all) list[n++] = k;
+}
+
+laq_status load_kernels(const Err& e) {
+  static Loaded loaded;
+  static const void* list[32];
+  static const int n = [] {
+    int count = 0;
+    list_kernels<__nv_bfloat16>(list, count);
+    list_kernels<__half>(list, count);
+    list[count++] = (const void*)linear_db_kernel;
+    list[count++] = (const void*)linear_pack_kernel;
+    return count;
+  }();
+  return launched(e.buf, e.len, loaded.once(list, n));
+}
+
 }  // namespace
 }  // namespace ops
 }  // namespace laq
@@ -1336,6 +1363,7 @@ extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_works
   LAQ_TRY(check_tensor(e, buffers, "y", kWritten, c->y, true, c->M, c->ld_y, c->N, 2, "residual"));
   LAQ_TRY(check_tensor(e, buffers, "z", kWritten, c->z, false, c->M, c->ld_z, c->N, 2));
   LAQ_TRY(buffers.check(errbuf, errbuf_len));
+  LAQ_TRY(load_kernels(e));
   cudaStream_t st = (cudaStream_t)cuda_stream;
   char* ws = (char*)d_workspace;
   Operand x{c->x, c->ld_x, c->M, c->K}, w{c->w, c->ld_w, c->N, c->K};
@@ -1387,6 +1415,7 @@ extern "C" laq_status laq_linear_backward(const laq_linear_call* c, void* d_work
   if (c->dx) LAQ_TRY(check_tensor(e, buffers, "w", kRead, c->w, true, c->N, c->ld_w, c->K, 2));
   LAQ_TRY(check_tensor(e, buffers, "dx", kWritten, c->dx, false, c->M, c->ld_dx, c->K, 2));
   LAQ_TRY(buffers.check(errbuf, errbuf_len));
+  LAQ_TRY(load_kernels(e));
   BackwardNeeds need(c);
   char* ws = (char*)d_workspace;
   const bool starve = (c->flags & LAQ_LINEAR_STARVE) != 0;

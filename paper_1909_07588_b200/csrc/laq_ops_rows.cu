@@ -1436,6 +1436,34 @@ laq_status check_gradient(const Err& e, const void* dx, int64_t ld_d, int64_t V)
   return LAQ_OK;
 }
 
+template <class T>
+void list_kernels(const void** list, int& n) {
+  const void* all[] = {
+      (const void*)rows_forward_kernel<T, 32, false>, (const void*)rows_forward_kernel<T, kHalfBlock, false>,
+      (const void*)rows_forward_kernel<T, kBlock, false>, (const void*)rows_forward_kernel<T, 32, true>,
+      (const void*)rows_forward_kernel<T, kHalfBlock, true>, (const void*)rows_forward_kernel<T, kBlock, true>,
+      (const void*)rows_gradient_kernel<T, 32, kWarpRow / Elem<T>::EV / 32, kLogprobsGrad>,
+      (const void*)rows_gradient_kernel<T, 32, kWarpRow / Elem<T>::EV / 32, kDistillGrad>,
+      (const void*)rows_gradient_kernel<T, 32, kWarpRow / Elem<T>::EV / 32, kDistillStep>,
+      (const void*)rows_gradient_kernel<T, kBlock, 4, kLogprobsGrad>, (const void*)rows_gradient_kernel<T, kBlock, 4, kDistillGrad>,
+      (const void*)rows_step_kernel<T, kHalfBlock, 4>, (const void*)rows_step_kernel<T, kHalfBlock, 8>,
+      (const void*)rows_step_kernel<T, kHalfBlock, 16>, (const void*)rows_step_kernel<T, kBlock, 16>};
+  for (const void* k : all) list[n++] = k;
+}
+
+laq_status load_kernels(const Err& e) {
+  static Loaded loaded;
+  static const void* list[48];
+  static const int n = [] {
+    int count = 0;
+    list_kernels<float>(list, count);
+    list_kernels<__nv_bfloat16>(list, count);
+    list_kernels<__half>(list, count);
+    return count;
+  }();
+  return launched(e.buf, e.len, loaded.once(list, n));
+}
+
 laq_status done(const Err& e, cudaError_t rc) { return launched(e.buf, e.len, rc); }
 
 void set_temperature(ForwardArgs& A, float tau) {
@@ -1479,7 +1507,8 @@ extern "C" laq_status laq_token_logprobs(const void* d_logits, int32_t dtype, in
     buffers.out("top_tokens", d_top_tokens, 4, rows, top_k, top_k);
     buffers.out("top_logprobs", d_top_logprobs, 4, rows, top_k, top_k);
   }
-  const laq_status ok = buffers.check(errbuf, errbuf_len);
+  laq_status ok = buffers.check(errbuf, errbuf_len);
+  if (ok == LAQ_OK) ok = load_kernels(e);
   if (ok != LAQ_OK) return ok;
   ForwardArgs A = {};
   A.x = d_logits;
@@ -1518,6 +1547,7 @@ extern "C" laq_status laq_token_logprobs_backward(const void* d_logits, int32_t 
   buffers.in("grad_entropy", d_grad_entropy, 4, 1, rows, rows);
   buffers.out("grad_logits", d_grad_logits, dtype_bytes(dtype), rows, vocab, grad_row_stride, "logits");
   st = buffers.check(errbuf, errbuf_len);
+  if (st == LAQ_OK) st = load_kernels(e);
   if (st != LAQ_OK) return st;
   GradArgs A = {};
   A.x = d_logits;
@@ -1568,6 +1598,7 @@ extern "C" laq_status laq_distill(const void* d_logits, int32_t dtype, int64_t r
   buffers.in("grad_loss", d_grad_loss, 4, 1, rows, rows);
   buffers.out("grad_logits", d_grad_logits, dtype_bytes(dtype), rows, vocab, grad_row_stride, "logits");
   st = buffers.check(errbuf, errbuf_len);
+  if (st == LAQ_OK) st = load_kernels(e);
   if (st != LAQ_OK) return st;
   cudaStream_t s = (cudaStream_t)cuda_stream;
   const bool fits = dtype == LAQ_F32 ? step_fits<float>(vocab) : step_fits<__half>(vocab);
@@ -1629,6 +1660,7 @@ extern "C" laq_status laq_distill_backward(const void* d_logits, int32_t dtype, 
   buffers.in("grad_loss", d_grad_loss, 4, 1, rows, rows);
   buffers.out("grad_logits", d_grad_logits, dtype_bytes(dtype), rows, vocab, grad_row_stride, "logits");
   st = buffers.check(errbuf, errbuf_len);
+  if (st == LAQ_OK) st = load_kernels(e);
   if (st != LAQ_OK) return st;
   GradArgs A = {};
   A.x = d_logits;

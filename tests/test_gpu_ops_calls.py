@@ -65,3 +65,54 @@ assert failed == len(calls)
 ops.check_status()
 print("done")
 """)
+
+
+def test_only_the_first_call_takes_device_memory_for_code():
+    """After one small call of a row operator and one of a layer, no form of any call takes device memory other than what the
+    framework's allocator takes for the outputs."""
+    assert "done" in _run("""
+import torch
+from paper_1909_07588_b200 import ops
+bf = torch.bfloat16
+
+def rows(dt, T, V):
+    x = torch.randn(T, V, device="cuda").to(dt)
+    tok = torch.zeros(T, dtype=torch.int32, device="cuda")
+    one = torch.ones(T, device="cuda")
+    s = ops.token_logprobs(x, tok, top_k=3)
+    ops.token_logprobs_backward(x, tok, s["lse"], s["entropy"], one, one)
+    r = ops.distill(x, tok[:, None].contiguous(), one[:, None].contiguous(), d_loss=one)
+    ops.distill(x, tok[:, None].contiguous(), one[:, None].contiguous())
+    ops.distill_backward(x, tok[:, None].contiguous(), one[:, None].contiguous(), r["lse"], one)
+
+def layer(dt, M, N, K, odd=0):
+    x, w = torch.randn(M, K + odd, device="cuda").to(dt)[:, odd:], torch.randn(N, K, device="cuda").to(dt)
+    dy = torch.randn(M, N, device="cuda").to(dt)
+    ops.linear(x, w, activation="gelu")
+    ops.linear_backward(dy, x, w, z=dy, activation="gelu")
+    ops.linear_backward(dy, x, w, dw_dtype=torch.float32)
+
+rows(torch.float32, 1, 8)
+layer(bf, 8, 8, 8)
+torch.cuda.synchronize()
+
+def used():
+    torch.cuda.synchronize()
+    return torch.cuda.mem_get_info()[0] + torch.cuda.memory_reserved()
+
+for dt in (torch.float32, bf, torch.float16):       # what the framework itself needs for the inputs
+    torch.randn(3, 4, device="cuda").to(dt)
+start = used()
+for dt in (torch.float32, bf, torch.float16):
+    for T, V in ((3, 500), (2, 5000), (2400, 1500), (1200, 2100), (2, 30000), (2, 140000), (1, 270000)):
+        rows(dt, T, V)
+        assert used() == start, (dt, T, V)
+for dt in (bf, torch.float16):
+    for M, N, K in ((1, 40, 4000), (1, 40, 40), (2, 40, 4000), (3, 40, 40), (4, 40, 40), (16, 512, 2048), (300, 300, 264), (2048, 2048, 512),
+                    (70000, 16, 24), (66000, 512, 512)):
+        for odd in (0, 1):
+            layer(dt, M, N, K, odd)
+            assert used() == start, (dt, M, N, K, odd)
+ops.check_status()
+print("done")
+""")
