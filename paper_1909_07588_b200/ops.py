@@ -240,16 +240,26 @@ def _status_word(index):
     return word
 
 
+def _device_index(device):
+    """The GPU that a device argument names: None and "cuda" are the current one."""
+    if device is None:
+        return torch.cuda.current_device()
+    device = torch.device(device)
+    if device.type != "cuda":
+        _refuse("%s is not a CUDA device" % device)
+    return torch.cuda.current_device() if device.index is None else device.index
+
+
 def init(device=None):
     """Set up the device's status word (done by the first linear call otherwise, which must then not be captured)."""
-    index = torch.cuda.current_device() if device is None else torch.device(device).index or 0
+    index = _device_index(device)
     with torch.cuda.device(index):
         _status_word(index)
 
 
 def check_status(device=None):
     """Synchronises the device and raises LAQ_ETIMEOUT if a bounded wait of a linear call ran out since the last check."""
-    index = torch.cuda.current_device() if device is None else torch.device(device).index or 0
+    index = _device_index(device)
     word = _status.get(index)
     if word is None:
         return
