@@ -70,18 +70,26 @@ class Loaded {
   std::atomic<uint64_t> devices_{0};
 };
 
-// The driver's query of several properties of a pointer in one call (0.03 us; a call asks for up to 14 pointers).
-typedef CUresult (*PointerAttributesFn)(unsigned int, CUpointer_attribute*, void**, CUdeviceptr);
-inline PointerAttributesFn pointer_attributes_fn() {
-  static const PointerAttributesFn fn = [] {
-    void* p = nullptr;
+// The driver's query of several properties of a pointer in one call (0.03 us; a call asks for up to 14 pointers), and that of
+// the calling thread's context.
+struct Driver {
+  CUresult (*pointer_attributes)(unsigned int, CUpointer_attribute*, void**, CUdeviceptr) = nullptr;
+  CUresult (*current_context)(CUcontext*) = nullptr;
+  Driver() {
+    find("cuPointerGetAttributes", (void**)&pointer_attributes);
+    find("cuCtxGetCurrent", (void**)&current_context);
+  }
+  static void find(const char* name, void** fn) {
     cudaDriverEntryPointQueryResult found;
-    const bool ok = cudaGetDriverEntryPoint("cuPointerGetAttributes", &p, cudaEnableDefault, &found) == cudaSuccess &&
-                    found == cudaDriverEntryPointSuccess;
-    if (!ok) cudaGetLastError();
-    return ok ? (PointerAttributesFn)p : nullptr;
-  }();
-  return fn;
+    if (cudaGetDriverEntryPoint(name, fn, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess) {
+      cudaGetLastError();
+      *fn = nullptr;
+    }
+  }
+};
+inline const Driver& driver() {
+  static const Driver d;
+  return d;
 }
 
 // Bytes in rows: [p + i pitch, p + i pitch + width) for i < rows.
@@ -135,22 +143,31 @@ class Buffers {
         if (!itself && a.x.meets(b.x)) return fail(errbuf, errlen, LAQ_EINVAL, "%s and %s overlap", a.name, b.name);
       }
     int dev = -1;
-    const PointerAttributesFn attributes = pointer_attributes_fn();
-    if (cudaGetDevice(&dev) != cudaSuccess || !attributes) {
+    const Driver& drv = driver();
+    if (cudaGetDevice(&dev) != cudaSuccess || !drv.pointer_attributes || !drv.current_context) {
       cudaGetLastError();
       return fail(errbuf, errlen, LAQ_EINVAL, "no current CUDA device");
+    }
+    // A thread that has made no call yet has no context, and without one the driver answers no question and encodes no tensor map.
+    CUcontext context = nullptr;
+    if (drv.current_context(&context) != CUDA_SUCCESS || !context) {
+      const cudaError_t rc = cudaSetDevice(dev);
+      if (rc != cudaSuccess) {
+        cudaGetLastError();
+        return fail(errbuf, errlen, LAQ_ECUDA, "the device cannot be used: %s", cudaGetErrorString(rc));
+      }
     }
     for (int i = 0; i < count_; ++i) {
       CUmemorytype type = (CUmemorytype)0;
       int on = -1;
       CUpointer_attribute what[2] = {CU_POINTER_ATTRIBUTE_MEMORY_TYPE, CU_POINTER_ATTRIBUTE_DEVICE_ORDINAL};
       void* out[2] = {&type, &on};
-      const bool known = attributes(2, what, out, (CUdeviceptr)list_[i].p) == CUDA_SUCCESS;
+      const bool known = drv.pointer_attributes(2, what, out, (CUdeviceptr)list_[i].p) == CUDA_SUCCESS;
       if (known && type == CU_MEMORYTYPE_DEVICE && on == dev) continue;
       unsigned managed = 0;                  // managed memory serves wherever it lies
       what[0] = CU_POINTER_ATTRIBUTE_IS_MANAGED;
       out[0] = &managed;
-      if (known && attributes(1, what, out, (CUdeviceptr)list_[i].p) == CUDA_SUCCESS && managed) continue;
+      if (known && drv.pointer_attributes(1, what, out, (CUdeviceptr)list_[i].p) == CUDA_SUCCESS && managed) continue;
       if (!known || type != CU_MEMORYTYPE_DEVICE)
         return fail(errbuf, errlen, LAQ_EINVAL, "%s is not device memory", list_[i].name);
       return fail(errbuf, errlen, LAQ_EINVAL, "%s lives on another GPU than the current device: make its device current for the call", list_[i].name);

@@ -116,3 +116,40 @@ for dt in (bf, torch.float16):
 ops.check_status()
 print("done")
 """)
+
+
+def test_first_calls_of_a_thread():
+    """Each operator as the first thing that a thread does with the device, and its results."""
+    assert "done" in _run("""
+import concurrent.futures as cf
+import torch
+from paper_1909_07588_b200 import ops
+bf = torch.bfloat16
+x, w, dy = torch.randn(300, 512, device="cuda").to(bf), torch.randn(40, 512, device="cuda").to(bf), torch.randn(300, 40, device="cuda").to(bf)
+logits = torch.randn(6, 5000, device="cuda")
+tok = torch.randint(0, 5000, (6,), device="cuda").int()
+one = torch.ones(6, device="cuda")
+out = torch.empty(300, 40, device="cuda", dtype=bf)
+calls = [
+    lambda: list(ops.token_logprobs(logits, tok, top_k=3).values()),
+    lambda: [ops.token_logprobs_backward(logits, tok, one, d_logprob=one)],
+    lambda: list(ops.distill(logits, tok[:, None], one[:, None]).values()),
+    lambda: list(ops.distill(logits, tok[:, None], one[:, None], d_loss=one).values()),
+    lambda: [ops.distill_backward(logits, tok[:, None], one[:, None], one, one)],
+    lambda: [ops.linear(x[:1], w)],
+    lambda: [ops.linear(x, w, out=out)],
+    lambda: [ops.linear(x[:, 1:], w[:, 1:])],
+    lambda: list(ops.linear_backward(dy, x, w, z=dy, activation="gelu").values()),
+]
+want = [[t.clone() for t in c()] for c in calls]
+torch.cuda.synchronize()
+for call, expected in zip(calls, want):
+    with cf.ThreadPoolExecutor(1) as pool:
+        got = pool.submit(call).result(timeout=60)
+        torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, expected))
+ops.check_status()
+print("done")
+""")
+
+
