@@ -26,6 +26,8 @@ ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
 LINEAR_STARVE = 1
 
 _status = {}        # per device: the word in which the product kernels record a bounded wait that ran out
+_failures = {}      # per device: how often the word was found set, and cleared
+_status_lock = threading.Lock()
 
 
 def _refuse(message):
@@ -35,7 +37,7 @@ def _refuse(message):
 # These checks run on every call, whose kernel may take a few microseconds: they use the cheapest forms of the questions.
 _current_device = torch._C._cuda_getDevice
 _raw_stream = torch._C._cuda_getCurrentRawStream
-_local = threading.local()          # the calling thread's buffer for error texts
+_local = threading.local()          # the calling thread's buffer for error texts, and the failures that it has been told of
 
 
 def _check(t, name, index=None, dtype=None):
@@ -237,7 +239,18 @@ def _status_word(index):
         word = torch.zeros(1, dtype=torch.int32, device=torch.device("cuda", index))
         torch.cuda.synchronize(index)        # other streams may use it from now on
         word = _status.setdefault(index, word)
+    seen = _seen()
+    if index not in seen:                    # this thread answers for what happens from now on
+        with _status_lock:
+            seen[index] = _failures.get(index, 0)
     return word
+
+
+def _seen():
+    seen = getattr(_local, "seen", None)
+    if seen is None:
+        seen = _local.seen = {}
+    return seen
 
 
 def _device_index(device):
@@ -258,18 +271,25 @@ def init(device=None):
 
 
 def check_status(device=None):
-    """Synchronises the device and raises LAQ_ETIMEOUT if a bounded wait of a linear call ran out since the last check."""
+    """Synchronises the device and raises LAQ_ETIMEOUT if a bounded wait of a linear call on it, of any thread, ran out since
+    this thread's last check (its first call on the device, if it has not checked before).  A wait that ran out is told to
+    every thread that checks, whichever finds it first: all of them share the device's status word."""
     index = _device_index(device)
     word = _status.get(index)
     if word is None:
         return
-    torch.cuda.synchronize(index)
-    bits = int(word.item())
-    if bits:
-        word.zero_()
+    seen = _seen()
+    with _status_lock:
         torch.cuda.synchronize(index)
-        raise LaqError(LAQ_ETIMEOUT, "a bounded wait inside a product kernel ran out (bits %d): outputs since the last check "
-                                     "are not complete" % bits)
+        bits = int(word.item())
+        if bits:
+            _failures[index] = _failures.get(index, 0) + 1       # before it is cleared: what comes between belongs to it
+            word.zero_()
+            torch.cuda.synchronize(index)
+        told, seen[index] = seen.get(index, 0), _failures.get(index, 0)
+    if told != seen[index]:
+        raise LaqError(LAQ_ETIMEOUT, "a bounded wait inside a product kernel ran out%s: outputs since the last check are not "
+                                     "complete" % (" (bits %d)" % bits if bits else ""))
 
 
 def _layer_call(x, weight, activation, flags, index):

@@ -153,3 +153,38 @@ print("done")
 """)
 
 
+def test_a_wait_that_ran_out_is_told_to_every_caller():
+    """The starved call's thread and another that called before it: each check tells the failure once."""
+    assert "done" in _run("""
+import threading, queue
+import torch
+from paper_1909_07588_b200 import laq, ops
+bf = torch.bfloat16
+x, w = torch.randn(300, 512, device="cuda").to(bf), torch.randn(300, 512, device="cuda").to(bf)
+ops.linear(x, w)
+orders, answers = queue.Queue(), queue.Queue()
+def status():
+    try:
+        ops.check_status()
+        return "ok"
+    except laq.LaqError as e:
+        return e.status
+def other():
+    while (f := orders.get()) is not None:
+        try:
+            answers.put(f())
+        except Exception as e:
+            answers.put(e)
+t = threading.Thread(target=other, daemon=True)
+t.start()
+ask = lambda f: (orders.put(f), answers.get(timeout=60))[1]
+def starve():
+    ops.linear(x, w, flags=ops.LINEAR_STARVE)
+    return status()
+assert ask(lambda: (ops.linear(x, w), status())[1]) == "ok" and status() == "ok"
+assert ask(starve) == laq.LAQ_ETIMEOUT
+assert status() == laq.LAQ_ETIMEOUT and status() == "ok" and ask(status) == "ok"
+orders.put(None)
+t.join()
+print("done")
+""")
