@@ -10,8 +10,9 @@ The library's own models end at 16 classes and one hidden layer; a larger model'
 Tensors are CUDA tensors with unit stride within a row and any row stride; outputs are allocated here unless ``out`` is
 given, which is refused if it shares memory with another tensor of the call other than where a call says so.  Gradients
 are calls of their own: none of this takes part in torch's autograd.  Calls run on ``stream`` (default: the current stream
-of the tensors' device) and do not synchronise.  They launch kernels only: there is no CPU fallback.  ``check_status``
-reports a bounded wait of the product kernels that ran out.
+of the tensors' device) and do not synchronise: their inputs must be ready in that stream's order, and may be let go of as
+soon as the call has returned.  They launch kernels only: there is no CPU fallback.  ``check_status`` reports a bounded wait
+of the product kernels that ran out.
 """
 import ctypes as C
 import threading
@@ -83,8 +84,9 @@ def _vector(t, name, index, dtype, n):
     return t.data_ptr()
 
 
-def _on(index, stream, body):
-    """body(raw stream) with the tensors' device current; outputs that it allocates belong to that stream."""
+def _on(index, stream, body, *tensors):
+    """body(raw stream) with the tensors' device current; outputs that it allocates belong to that stream.  `tensors` are those
+    that the caller has given: their memory is not handed out again before a stream of the call's own has done with it."""
     if stream is None:
         if _current_device() == index:
             return body(_raw_stream(index))
@@ -93,7 +95,11 @@ def _on(index, stream, body):
     if stream.device.index != index:
         _refuse("the stream belongs to %s, the tensors to cuda:%d" % (stream.device, index))
     with torch.cuda.stream(stream):
-        return body(stream.cuda_stream)
+        result = body(stream.cuda_stream)
+    for t in tensors:
+        if t is not None:
+            t.record_stream(stream)
+    return result
 
 
 def _call(function, *args):
@@ -142,7 +148,7 @@ def token_logprobs(logits, tokens=None, top_k=0, temperature=1.0, stream=None):
               p + 8 * T, tp, vp, raw)
         return out
 
-    return _on(index, stream, body)
+    return _on(index, stream, body, logits, tokens)
 
 
 def _gradient_out(logits, out):
@@ -171,7 +177,7 @@ def token_logprobs_backward(logits, tokens, lse, entropy=None, d_logprob=None, d
         _call(laq.load_library().laq_token_logprobs_backward, *head, temperature, *ptrs, dptr, dstride, raw)
         return dx
 
-    return _on(index, stream, body)
+    return _on(index, stream, body, logits, tokens, lse, entropy, d_logprob, d_entropy, out)
 
 
 def _teacher(tokens, values, index, T):
@@ -210,7 +216,7 @@ def distill(logits, teacher_tokens, teacher_logits, temperature=1.0, d_loss=None
         _call(laq.load_library().laq_distill, *head, temperature, *teacher, p, p + 4 * T, dl, dptr, dstride, raw)
         return res
 
-    return _on(index, stream, body)
+    return _on(index, stream, body, logits, teacher_tokens, teacher_logits, d_loss, out)
 
 
 def distill_backward(logits, teacher_tokens, teacher_logits, lse, d_loss, temperature=1.0, out=None, stream=None):
@@ -226,7 +232,7 @@ def distill_backward(logits, teacher_tokens, teacher_logits, lse, d_loss, temper
         _call(laq.load_library().laq_distill_backward, *head, temperature, *teacher, *ptrs, dptr, dstride, raw)
         return dx
 
-    return _on(index, stream, body)
+    return _on(index, stream, body, logits, teacher_tokens, teacher_logits, lse, d_loss, out)
 
 
 # --- the layer -------------------------------------------------------------------------------------------------------
@@ -351,7 +357,7 @@ def linear(x, weight, bias=None, activation="none", residual=None, preact=False,
         _call(L.laq_linear_forward, C.byref(c), wp, wn, raw)
         return (y, z) if preact else y
 
-    return _on(index, stream, body)
+    return _on(index, stream, body, x, weight, bias, residual, out, workspace)
 
 
 def linear_backward(dy, x, weight, z=None, activation="none", dx=True, dw=True, db=True, dw_dtype=None, workspace=None,
@@ -391,4 +397,4 @@ def linear_backward(dy, x, weight, z=None, activation="none", dx=True, dw=True, 
         _call(L.laq_linear_backward, C.byref(c), wp, wn, raw)
         return res
 
-    return _on(index, stream, body)
+    return _on(index, stream, body, dy, x, weight, z, workspace)

@@ -188,3 +188,50 @@ orders.put(None)
 t.join()
 print("done")
 """)
+
+
+def test_inputs_may_be_let_go_of_when_a_call_on_another_stream_has_returned():
+    """A call on a stream that is busy, its inputs dropped at once and their memory asked for again on the caller's stream:
+    what is written there meanwhile must not reach the call."""
+    assert "done" in _run("""
+import torch
+from paper_1909_07588_b200 import ops
+bf = torch.bfloat16
+side = torch.cuda.Stream()
+g = torch.Generator(device="cuda")
+
+def made():
+    # fresh tensors of the caller's stream, the same values every time
+    g.manual_seed(0)
+    rnd = lambda *s: torch.randn(*s, generator=g, device="cuda")
+    n, V, K = 64, 30000, 8
+    return dict(x=rnd(n, V).to(bf), tok=torch.randint(0, V, (n,), generator=g, device="cuda").int(), a=rnd(n), b=rnd(n), c=rnd(n),
+                tt=torch.randint(0, V, (n, K), generator=g, device="cuda").int(), tv=rnd(n, K), h=rnd(n, 2048).to(bf), w=rnd(1024, 2048).to(bf),
+                bias=rnd(1024).to(bf), r=rnd(n, 1024).to(bf), dy=rnd(n, 1024).to(bf))
+
+calls = [
+    lambda t, s: ops.token_logprobs(t["x"], t["tok"], top_k=4, stream=s),
+    lambda t, s: dict(dx=ops.token_logprobs_backward(t["x"], t["tok"], t["a"], t["b"], t["c"], t["a"], stream=s)),
+    lambda t, s: ops.distill(t["x"], t["tt"], t["tv"], d_loss=t["a"], stream=s),
+    lambda t, s: dict(dx=ops.distill_backward(t["x"], t["tt"], t["tv"], t["a"], t["b"], stream=s)),
+    lambda t, s: dict(y=ops.linear(t["h"], t["w"], t["bias"], activation="gelu", residual=t["r"], stream=s)),
+    lambda t, s: ops.linear_backward(t["dy"], t["h"], t["w"], z=t["r"], activation="gelu", stream=s),
+]
+for call in calls:
+    want = call(made(), None)
+    torch.cuda.synchronize()
+    t = made()
+    shapes = [(v.shape, v.dtype) for v in t.values()]
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)               # some 0.2 s
+    got = call(t, side)
+    t = None
+    for _ in range(3):                               # the memory is there again if the allocator hands it out
+        again = [torch.zeros(s, dtype=d, device="cuda") for s, d in shapes]
+    torch.cuda.synchronize()
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+ops.check_status()
+print("done")
+""")
