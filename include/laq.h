@@ -409,8 +409,8 @@ laq_status laq_linear_forward(const laq_linear_call* call /* HOST */, void* d_wo
                               char* errbuf, size_t errbuf_len);
 
 /* dz = dy act'(z), rounded once to `dtype` (exact for LAQ_ACT_NONE and LAQ_ACT_RELU);  dx = dz w,  dw = dz^T x,
- * db = column sums of dz before that rounding.  dw in fp32 is offered where dz is exact: with the other activations 16 bits
- * of dz would not justify 32 of dw.  M = 0 gives dw = 0 and db = 0. */
+ * db = column sums of dz before that rounding.  dw in fp32 is offered where dz is exact, with LAQ_ACT_NONE and
+ * LAQ_ACT_RELU.  M = 0 gives dw = 0 and db = 0. */
 laq_status laq_linear_backward(const laq_linear_call* call /* HOST */, void* d_workspace, size_t workspace_bytes,
                                void* cuda_stream, char* errbuf, size_t errbuf_len);
 
