@@ -95,6 +95,9 @@ struct Slice {
 //                     lowest value: nothing else has been seen), whose product with c is rounded by many powers of two or
 //                     overflows: as a reference, rho would be off by as much.  A NaN or +inf also ends here and stays.
 constexpr float kNear = 4194304.f;     // 2^22
+// A 16-bit gradient may bear ref c + log2 s as one rounded number up to here, where that is a factor of 2^(2^-13) at most, a sixth
+// of half a step of fp16 (at a temperature of 1e-4 and logits of 20 it would be 0.5 %); beyond, the difference comes first.
+constexpr float kOneNumber = 4096.f;
 
 struct Stat {
   float ref, s, u;
@@ -976,7 +979,7 @@ __global__ void __launch_bounds__(NT == 32 ? kWarpBlock : kGradientThreads<NT, M
   if (bad) ca = __int_as_float(0x7fc00000);
   // log2 p = x c - kappa, for 16-bit logits whose reference is no mask
   const float kappa = kStep ? ref * c + log2s : lse * kLog2e;
-  const bool packed = kNarrow && (!kStep || near_ref(ref, c));
+  const bool packed = kNarrow && (!kStep || fabsf(kappa) < kOneNumber);
   const f32x2 c2 = pair_of(c, c), k2 = pair_of(-kappa, -kappa), ca2 = pair_of(ca, ca), cb2 = pair_of(cb * kLn2, cb * kLn2);
   // with a term in log p, -inf is raised to a bound where p is 0 and log p finite; without such a bound: one by one
   const uint32_t lo = MODE == kLogprobsGrad && kNarrow ? Elem<T>::bound((kappa - 200.f) / c) : 0u;
@@ -1226,7 +1229,7 @@ __global__ void __launch_bounds__(NT + 32, NT > 128 ? 3 : R > 8 ? 4 : 6) rows_st
     const RowSum r = row_sum(b);
     const float ref = r.ref, log2s = r.log2s;
     const bool zero = !teacher[b].bad && (!teacher[b].any || r.masked);
-    if (aligned && !zero && near_ref(ref, c)) {
+    if (aligned && !zero && fabsf(ref * c) < (kNarrow ? kOneNumber : kNear)) {
       // two elements an instruction; a 16-bit gradient bears ref c + log2 s as one rounded number, an fp32 one does not
       const float kappa = ref * c + (kNarrow ? log2s : 0.f);
       const f32x2 c2 = pair_of(c, c), k2 = pair_of(-kappa, -kappa), ca2 = pair_of(ca, ca), l2 = pair_of(-log2s, -log2s);

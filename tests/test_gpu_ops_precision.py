@@ -115,3 +115,30 @@ def test_fp32_weight_gradient_is_summed_in_chunks(M, N, K, dtype):
     # the roundings of the chunks' additions are to nearest: sqrt(n / 3) of them, and four times that at the farthest
     assert float(off.max()) <= 32 * 2.0 ** -23 + U * (4 * math.sqrt((M / 512 + 10) / 3) + 1)
     ops.check_status()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("V", [500, 3000, 40000])
+@pytest.mark.parametrize("tau", [1.0, 1e-2, 1e-3, 1e-4])
+def test_step_gradient_at_low_temperatures(V, dtype, tau):
+    """Rows whose largest logit comes n times and whose others are 1 below: p is 1 / n there (and, but for tau = 1, 0 elsewhere).
+    Differences of equal logits are exact, so what is left is the sum's V / 256 + 40 roundings, the exponential's and the
+    logarithm's few, and the output's own; a reference near 20 / tau log2(e) rounded together with log2 s would be off by half
+    a step of it, 0.5 % of p at tau = 1e-4."""
+    dt = DTYPES[dtype]
+    tops = [20.0, -20.25, 7.5, 30.0, -3.0, 0.0]
+    x = torch.stack([torch.full((V,), t - 1.0, device="cuda") for t in tops])
+    n = [1, 2, 3, 7, 50, V // 3]
+    for r, (t, k) in enumerate(zip(tops, n)):
+        x[r, torch.randperm(V, generator=_gen(r), device="cuda")[:k]] = t
+    x = x.to(dt)
+    tok = x.argmin(dim=1, keepdim=True).int()
+    one = torch.full((6,), 1 / tau, device="cuda")
+    got = ops.distill(x, tok, torch.zeros(6, 1, device="cuda"), temperature=tau, d_loss=one)
+    want = torch.softmax(x.double() / tau, dim=1)
+    want.scatter_add_(1, tok.long(), torch.full((6, 1), -1.0, device="cuda", dtype=torch.float64))
+    half = torch.finfo(dt).eps / 2 if dt != torch.float32 else U
+    # c's rounding shifts the lower logits by u / tau; the other type's of ref c + log2 s, where it is taken, 2^-13 of log2
+    rel = half + (V / 256 + 60) * U + (2 * U / tau if tau == 1.0 else 0) + (2.0 ** -13 if dt != torch.float32 and tau >= 1e-2 else 0)
+    off = (got["dlogits"].double() - want).abs()
+    assert bool((off <= rel * want.abs() * (1 + rel) + 1e-7).all()), float((off / want.abs().clamp(min=1e-12)).max())
