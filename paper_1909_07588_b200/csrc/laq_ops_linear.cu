@@ -1034,8 +1034,9 @@ Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool
           while (stages * stage < kTileM * nt * 4 || stages < 3) ++stages;
         if (stages * stage > kMaxRing) continue;
         // A split long sum of more than 128 columns holds all of an SM's tensor memory: only where no other split tile's block
-        // (96 KB at least) fits beside it, since the two could keep one another from the clusters that they wait for.
-        if (split > 1 && long_sum && nt > 128 && stages * stage <= 128 * 1024) continue;
+        // (84 KB of ring at least, at 96 columns) fits beside it, since blocks of two calls could otherwise keep one another from
+        // the clusters that they wait for.  256 columns (144 KB) remain.
+        if (split > 1 && long_sum && nt > 128 && stages * stage <= 136 * 1024) continue;
         const double main = kb * per;
         double cost;
         if (split == 1) {

@@ -142,3 +142,44 @@ def test_step_gradient_at_low_temperatures(V, dtype, tau):
     rel = half + (V / 256 + 60) * U + (2 * U / tau if tau == 1.0 else 0) + (2.0 ** -13 if dt != torch.float32 and tau >= 1e-2 else 0)
     off = (got["dlogits"].double() - want).abs()
     assert bool((off <= rel * want.abs() * (1 + rel) + 1e-7).all()), float((off / want.abs().clamp(min=1e-12)).max())
+
+
+@pytest.mark.parametrize("M, N, K", [(16, 256, 70000), (300, 300, 70000), (2048, 1024, 66000)])
+def test_starved_long_sum_runs_out_and_is_reported(M, N, K):
+    """A split tile, single blocks and pairs whose sums are taken in chunks: every wait ends, and the same call works again."""
+    from paper_1909_07588_b200 import laq
+    x, w = torch.rand(M, K, generator=_gen(1), device="cuda").half(), (torch.rand(N, K, generator=_gen(2), device="cuda") / K).half()
+    want = ops.linear(x, w)
+    ops.check_status()
+    ops.linear(x, w, flags=ops.LINEAR_STARVE)
+    with pytest.raises(laq.LaqError) as e:
+        ops.check_status()
+    assert e.value.status == laq.LAQ_ETIMEOUT
+    ops.check_status()
+    assert torch.equal(ops.linear(x, w), want)
+    ops.check_status()
+
+
+def test_long_sums_beside_each_other():
+    """Long and short split sums on two streams at once, many times: each result as when alone."""
+    dt = torch.bfloat16
+    dy, x = torch.rand(131072, 1024, generator=_gen(1), device="cuda").to(dt), torch.rand(131072, 1024, generator=_gen(2), device="cuda").to(dt)
+    w = torch.rand(1024, 1024, generator=_gen(3), device="cuda").to(dt)
+    a, b = torch.rand(64, 4096, generator=_gen(4), device="cuda").to(dt), torch.rand(2048, 4096, generator=_gen(5), device="cuda").to(dt)
+    long = lambda: ops.linear_backward(dy, x, w, dx=False, db=False)["dw"]
+    short = lambda: ops.linear(a, b)
+    want_long, want_short = long(), short()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    torch.cuda.synchronize()
+    wrong = [torch.zeros((), dtype=torch.int64, device="cuda") for _ in streams]
+    for _ in range(20):
+        for s, n in zip(streams, wrong):
+            with torch.cuda.stream(s):
+                if s is streams[0]:
+                    n += (long() != want_long).sum()
+                else:
+                    for _ in range(6):
+                        n += (short() != want_short).sum()
+    torch.cuda.synchronize()
+    assert [int(n) for n in wrong] == [0, 0, 0]
+    ops.check_status()
