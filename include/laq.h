@@ -414,6 +414,78 @@ laq_status laq_linear_forward(const laq_linear_call* call /* HOST */, void* d_wo
 laq_status laq_linear_backward(const laq_linear_call* call /* HOST */, void* d_workspace, size_t workspace_bytes,
                                void* cuda_stream, char* errbuf, size_t errbuf_len);
 
+/* A matrix [rows][cols] in 8 bits: e4m3 codes (3 bits of mantissa, largest 448, NaN but no infinity) and an fp32 scale for each
+ * block of 128 columns of a row (block_rows 1) or for each tile of 128 rows and 128 columns (block_rows 128); the last block of a
+ * row, and the last tile of a column, end with the matrix.  value = code * scale. */
+typedef struct {
+  const void* codes;         /* DEVICE, [rows][cols] bytes (written by laq_pack_blocks and by a call that returns such a matrix) */
+  int64_t ld_codes;
+  const float* scales;       /* DEVICE, [ceil(rows / block_rows)][ceil(cols / 128)] (written likewise) */
+  int64_t ld_scales;
+  int32_t block_rows;        /* 1 or 128 */
+} laq_blocks;
+
+/* out (HOST struct) = x in 8 bits.  A block's scale is the least power of two s >= 2^-126 with |x| <= 448 s for its finite values
+ * (2^-126 where it has none but zeros), and a code is x / s rounded to the nearest, ties to even: off by at most 2^-4 |x|, or
+ * 2^-10 s where |x| < 2^-6 s.  NaN and infinities become NaN, and do not count for the scale.  x of any laq_dtype. */
+laq_status laq_pack_blocks(const void* d_x, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, const laq_blocks* out /* HOST */,
+                           void* cuda_stream, char* errbuf, size_t errbuf_len);
+
+/* d_out = the values of x in `dtype`, rounded to the nearest; a finite one beyond dtype's largest is that.  What laq_pack_blocks wrote is
+ * exact in LAQ_F32 and LAQ_BF16 (but for values that round to 2^128, beyond both types' largest), and in LAQ_F16 within its range. */
+laq_status laq_unpack_blocks(const laq_blocks* x /* HOST */, int64_t rows, int64_t cols, void* d_out, int32_t dtype, int64_t row_stride,
+                             void* cuda_stream, char* errbuf, size_t errbuf_len);
+
+/* A layer as above on operands in 8 bits: x [M][K] with block_rows 1 and w [N][K] with block_rows 128 come as HOST structs and replace
+ * the call's own, which are not looked at; bias, residual, z and y are in the call's dtype.  Sums of 128 products are added up by the
+ * tensor cores, scaled by both blocks' scales (whose product must be finite) and added in fp32 with rounding.
+ * Backward: any of x, w and z may come in 8 bits, with either block_rows (NULL: the call's own).  x and w are restored to `dtype` first
+ * (as laq_unpack_blocks does), z is read as it is.  The gradient is that of the layer on the restored operands. */
+size_t laq_linear_blocks_workspace_bytes(const laq_linear_call* call /* HOST */, const laq_blocks* x /* HOST */,
+                                         const laq_blocks* w /* HOST */, int32_t backward);
+laq_status laq_linear_blocks_forward(const laq_linear_call* call /* HOST */, const laq_blocks* x /* HOST */, const laq_blocks* w /* HOST */,
+                                     void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* errbuf, size_t errbuf_len);
+laq_status laq_linear_blocks_backward(const laq_linear_call* call /* HOST */, const laq_blocks* x /* HOST */, const laq_blocks* w /* HOST */,
+                                      const laq_blocks* z /* HOST */, void* d_workspace, size_t workspace_bytes, void* cuda_stream,
+                                      char* errbuf, size_t errbuf_len);
+
+/* A gated feed-forward block's two projections, activation and product:
+ *   z = x w^T + bias,  h = act(z[:, :F]) * z[:, F:];   x [M][K], w [2F][K] (the gates' rows first), bias [2F], z [M][2F], h [M][F]
+ * in `dtype` (LAQ_BF16 or LAQ_F16), summed in fp32 and rounded once.  Its gradient, with dz = [dh z[:, F:] act'(z[:, :F]) | dh act(z[:, :F])]
+ * rounded once to `dtype`:  dx = dz w,  dw = dz^T x,  db = column sums of dz before that rounding.  M = 0 gives dw = 0 and db = 0. */
+typedef struct {
+  int32_t dtype;             /* laq_dtype of all tensors but db */
+  int32_t activation;        /* laq_activation */
+  int64_t M, F, K;           /* M >= 0 rows, F >= 1 gates (below 2^30), K = 1..65536 inputs */
+  const void* x;
+  int64_t ld_x;
+  const void* w;
+  int64_t ld_w;
+  const void* bias;          /* forward: [2F] or NULL */
+  void* h;                   /* forward: output */
+  int64_t ld_h;
+  void* z;                   /* forward: output, or NULL; backward: input */
+  int64_t ld_z;
+  const void* dh;            /* backward: gradient of h */
+  int64_t ld_dh;
+  void* dx;                  /* backward: [M][K], or NULL */
+  int64_t ld_dx;
+  void* dw;                  /* backward: [2F][K], or NULL */
+  int64_t ld_dw;
+  float* db;                 /* backward: [2F], or NULL */
+  const laq_blocks* x_blocks;   /* HOST; backward: x in 8 bits, in x's place */
+  const laq_blocks* z_blocks;   /* HOST; z in 8 bits, in z's place: what laq_pack_blocks makes of z rounded to `dtype` */
+  uint32_t flags;            /* 0 or LAQ_LINEAR_STARVE */
+  uint32_t* status;          /* DEVICE, as in laq_linear_call */
+} laq_gated_call;
+
+/* Workspace as of laq_linear_workspace_bytes; outputs may share no memory with any other buffer of the call. */
+size_t laq_gated_workspace_bytes(const laq_gated_call* call /* HOST */, int32_t backward);
+laq_status laq_gated_forward(const laq_gated_call* call /* HOST */, void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* errbuf,
+                             size_t errbuf_len);
+laq_status laq_gated_backward(const laq_gated_call* call /* HOST */, void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* errbuf,
+                              size_t errbuf_len);
+
 /* Text of the last failure on this context ("" if none).  Valid until the next call on ctx. */
 const char* laq_last_error(const laq_ctx* ctx);
 

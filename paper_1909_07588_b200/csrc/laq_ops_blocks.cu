@@ -1,0 +1,556 @@
+// Matrices in 8 bits, and the product of two of them.
+//
+// A matrix is e4m3 codes with an fp32 scale for each block of 128 columns of a row (activations) or for each tile of 128 rows
+// and 128 columns (weights):  value = code scale.  The scale is the least power of two s >= 2^-126 with |v| <= 448 s for the
+// block's finite values, so that scaling is exact, a code's own rounding (half a step: 2^-4 of the value, 2^-10 s below 2^-6 s)
+// is all that is lost, and a value is a bf16 number (3 bits and a power of two).
+//
+//   Y = act(sum_b sx[m][b] sw[n / 128][b] (sum_{k in block b} qx[m][k] qw[n][k]) + bias) + R
+//
+// Products of two codes are exact and the tensor cores add up 128 of them; each block's sum is then scaled and added in fp32,
+// with rounding, by the epilogue's threads (linear_gemm_kernel, kCodes).
+#include "laq_ops_gemm.cuh"
+
+namespace laq {
+namespace ops {
+namespace {
+
+constexpr int kPackThreads = 256;
+constexpr int kLanes = 16;                // threads of a block's 128 columns, eight each
+constexpr int kPackAhead = 4;             // rows that a thread has under way
+
+// Eight neighbours in fp32; `vec`: they lie on a 16-byte boundary and all exist, else the first n are read one by one.
+template <class T>
+struct Eight {
+  static constexpr int kVectors = 8 / Elem<T>::EV;
+  uint4 v[kVectors];
+  __device__ __forceinline__ void read(const T* p, int n, bool vec) {
+    if (vec && n == 8) {
+#pragma unroll
+      for (int i = 0; i < kVectors; ++i) v[i] = load16(p + i * Elem<T>::EV);
+      return;
+    }
+    float x[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) x[e] = e < n ? Elem<T>::to_float(p[e]) : 0.f;
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+      float part[Elem<T>::EV];
+#pragma unroll
+      for (int e = 0; e < Elem<T>::EV; ++e) part[e] = x[i * Elem<T>::EV + e];
+      v[i] = Elem<T>::pack(part);                    // exact: the values are of type T
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int i = 0; i < kVectors; ++i) {
+      float part[Elem<T>::EV];
+      Elem<T>::unpack(v[i], part);
+#pragma unroll
+      for (int e = 0; e < Elem<T>::EV; ++e) x[i * Elem<T>::EV + e] = part[e];
+    }
+  }
+};
+
+__device__ __forceinline__ float largest_finite(const float (&x)[8]) {
+  float m = 0.f;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float a = fabsf(x[e]);
+    m = fmaxf(m, a < INFINITY ? a : 0.f);            // NaN compares false
+  }
+  return m;
+}
+
+// The power of two k >= -126 with largest <= 448 2^k: 448 = 1.75 2^8.
+__device__ __forceinline__ int scale_power(float largest) {
+  const uint32_t b = __float_as_uint(largest);
+  const int k = (int)(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return max(k, -126);
+}
+__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }      // -126..127
+
+__device__ __forceinline__ uint32_t encode2(float lo, float hi) {
+  unsigned short two;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
+  return two;
+}
+// Eight codes of values times `inverse` (a power of two: exact); what is not finite becomes NaN, which e4m3 has and infinity not.
+__device__ __forceinline__ uint2 encode8(const float (&x)[8], float inverse) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = fabsf(x[e]) < INFINITY ? x[e] * inverse : __uint_as_float(0x7fffffffu);
+  return make_uint2(encode2(v[0], v[1]) | (encode2(v[2], v[3]) << 16), encode2(v[4], v[5]) | (encode2(v[6], v[7]) << 16));
+}
+__device__ __forceinline__ void store_codes(uint8_t* p, uint2 codes, int n, bool vec) {
+  if (vec && n == 8) {
+    *reinterpret_cast<uint2*>(p) = codes;
+    return;
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (e < n) p[e] = (uint8_t)((e < 4 ? codes.x : codes.y) >> (8 * (e & 3)));
+}
+
+// A scale a row and 128 columns: 16 threads take a block.  Bound by memory.  A thread block has 16 such groups, side by side
+// along a row up to 1 << log_across of them, and each has kPackAhead rows under way.
+template <class T>
+__global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(const T* x, long long ld, long long rows, long long cols, uint8_t* codes, long long ldc,
+                                                                 float* scales, long long lds, int log_across, int vec_in, int vec_out) {
+  allow_next();
+  const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const int down = kPackThreads / kLanes >> log_across;          // groups above one another
+  const long long block = ((long long)blockIdx.x << log_across) + (group & ((1 << log_across) - 1));
+  const long long c0 = block * kBlock + lane * 8;
+  const int n = (int)max(0ll, min(8ll, cols - c0));
+  const bool there = block * kBlock < cols;
+  const long long step = (long long)gridDim.y * down * kPackAhead;
+  for (long long top = (long long)blockIdx.y * down * kPackAhead; top < rows; top += step) {      // the same turns for a whole warp
+    const long long r0 = top + (group >> log_across);
+    Eight<T> in[kPackAhead];
+#pragma unroll
+    for (int a = 0; a < kPackAhead; ++a) {
+      const long long r = r0 + a * down;
+      in[a].read(x + r * ld + c0, r < rows ? n : 0, vec_in);
+    }
+#pragma unroll
+    for (int a = 0; a < kPackAhead; ++a) {
+      const long long r = r0 + a * down;
+      float v[8];
+      in[a].get(v);
+      float m = largest_finite(v);
+#pragma unroll
+      for (int o = kLanes / 2; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const int k = scale_power(m);
+      if (r < rows && there) {
+        store_codes(codes + r * ldc + c0, encode8(v, power_of_two(-k)), n, vec_out);
+        if (lane == 0) scales[r * lds + block] = power_of_two(k);
+      }
+    }
+  }
+}
+
+// A scale a tile of 128 x 128: a thread block's 16 groups take eight rows each and hold them in registers.
+template <class T>
+__global__ void __launch_bounds__(kPackThreads) pack_tiles_kernel(const T* x, long long ld, long long rows, long long cols, uint8_t* codes, long long ldc,
+                                                                  float* scales, long long lds, long long across, int vec_in, int vec_out) {
+  __shared__ float part[kPackThreads / 32];
+  allow_next();
+  const long long down = blockIdx.x / across, block = blockIdx.x - down * across;
+  const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const long long c0 = block * kBlock + lane * 8, row0 = down * kBlock + group;
+  const int n = (int)max(0ll, min(8ll, cols - c0));
+  Eight<T> in[8];
+#pragma unroll
+  for (int a = 0; a < 8; ++a) in[a].read(x + (row0 + 16 * a) * ld + c0, row0 + 16 * a < rows ? n : 0, vec_in);
+  float m = 0.f, v[8];
+#pragma unroll
+  for (int a = 0; a < 8; ++a) {
+    in[a].get(v);
+    m = fmaxf(m, largest_finite(v));
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+  if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kPackThreads / 32; ++w) m = fmaxf(m, part[w]);
+  const int k = scale_power(m);
+#pragma unroll
+  for (int a = 0; a < 8; ++a) {
+    if (row0 + 16 * a >= rows) break;
+    in[a].get(v);
+    store_codes(codes + (row0 + 16 * a) * ldc + c0, encode8(v, power_of_two(-k)), n, vec_out);
+  }
+  if (threadIdx.x == 0) scales[down * lds + block] = power_of_two(k);
+}
+
+// A value rounded to T; a finite one beyond T's largest is that.
+template <class T>
+__device__ __forceinline__ float within(float v);
+template <>
+__device__ __forceinline__ float within<float>(float v) { return fabsf(v) == INFINITY ? copysignf(FLT_MAX, v) : v; }
+template <>
+__device__ __forceinline__ float within<__nv_bfloat16>(float v) { return fabsf(v) > 3.38953139e38f ? copysignf(3.38953139e38f, v) : v; }
+template <>
+__device__ __forceinline__ float within<__half>(float v) { return fabsf(v) > 65504.f ? copysignf(65504.f, v) : v; }
+
+// Codes to values, in the same arrangement.  Bound by memory.
+template <class T>
+__global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, long long rows, long long cols, T* out, long long ld, int log_across, int vec_in,
+                                                              int vec_out) {
+  allow_next();
+  const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
+  const int down = kPackThreads / kLanes >> log_across;
+  const long long block = ((long long)blockIdx.x << log_across) + (group & ((1 << log_across) - 1));
+  const long long c0 = block * kBlock + lane * 8;
+  const int n = (int)max(0ll, min(8ll, cols - c0));
+  if (n == 0) return;
+  const long long step = (long long)gridDim.y * down * kPackAhead;
+  for (long long r0 = (long long)blockIdx.y * down * kPackAhead + (group >> log_across); r0 < rows; r0 += step) {
+    uint2 in[kPackAhead];
+    float scale[kPackAhead];
+#pragma unroll
+    for (int a = 0; a < kPackAhead; ++a) {
+      const long long r = r0 + a * down;
+      in[a] = make_uint2(0u, 0u);
+      scale[a] = 0.f;
+      if (r >= rows) continue;
+      const uint8_t* p = q.p + r * q.ld + c0;
+      if (vec_in && n == 8) {
+        in[a] = load8(p);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const uint32_t code = e < n ? p[e] : 0u;
+          if (e < 4) in[a].x |= code << (8 * e);
+          else in[a].y |= code << (8 * (e - 4));
+        }
+      }
+      scale[a] = q.scale(r, c0);
+    }
+#pragma unroll
+    for (int a = 0; a < kPackAhead; ++a) {
+      const long long r = r0 + a * down;
+      if (r >= rows) break;
+      float v[8];
+      decode8(in[a], scale[a], v);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = within<T>(v[e]);
+      T* o = out + r * ld + c0;
+      if (vec_out && n == 8) {
+#pragma unroll
+        for (int i = 0; i < 8 / Elem<T>::EV; ++i) {
+          float part[Elem<T>::EV];
+#pragma unroll
+          for (int e = 0; e < Elem<T>::EV; ++e) part[e] = v[i * Elem<T>::EV + e];
+          *reinterpret_cast<uint4*>(o + i * Elem<T>::EV) = Elem<T>::pack(part);
+        }
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (e < n) o[e] = Elem<T>::from_float(v[e]);
+      }
+    }
+  }
+}
+
+// ---- one to four rows through a layer in 8 bits -----------------------------------------------------------------------
+// W's bytes are read once, by dot products as in linear_few_rows_kernel: a warp takes four columns and a lane 16 codes of each at
+// a time, whose products it adds up and scales together.
+constexpr int kCodesAhead = 2;
+template <class T, int ROWS>
+__global__ void __launch_bounds__(kFewThreads, kFewBlocks)
+    linear_few_codes_kernel(const GemmArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int vec, int log_parts) {
+  constexpr int kRows2 = ROWS == 3 ? 4 : ROWS, kSums = kFewCols * kRows2, kWarps = kFewThreads / 32;
+  __shared__ float part[kWarps][kSums];
+  const int t = threadIdx.x, lane = t & 31, warp = t >> 5, parts = 1 << log_parts;
+  const int col0 = (int)(blockIdx.x * (unsigned)(kWarps >> log_parts)) * kFewCols;
+  const int first = (warp & (parts - 1)) * 32 + lane, step = 32 << log_parts;
+  const int own = min(col0 + (warp >> log_parts) * kFewCols, A.J - 1);          // four columns lie in one tile of W
+  const float* sw = A.sw + (long long)(own / kBlock) * A.ldsw;
+  const uint8_t* wr[kFewCols];
+#pragma unroll
+  for (int c = 0; c < kFewCols; ++c) wr[c] = w + (long long)min(own + c, A.J - 1) * ldw;
+  float s[kSums] = {};
+  const int nv = vec ? (int)(K / 16) : 0;
+  for (int v0 = first; v0 < nv; v0 += kCodesAhead * step) {
+    uint4 a[kCodesAhead][kFewCols];
+#pragma unroll
+    for (int u = 0; u < kCodesAhead; ++u)
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c)
+        a[u][c] = v0 + u * step < nv ? __ldcs(reinterpret_cast<const uint4*>(wr[c]) + v0 + u * step) : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int u = 0; u < kCodesAhead; ++u) {
+      const int v = v0 + u * step;
+      if (v >= nv) break;
+      const float of_w = __ldg(sw + v / (kBlock / 16));
+      f32x2 q[ROWS][8];
+      float scale[ROWS];
+#pragma unroll
+      for (int m = 0; m < ROWS; ++m) {
+        const uint4 b = __ldg(reinterpret_cast<const uint4*>(x + m * ldx) + v);
+        const uint32_t words[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 f = decode2(words[i / 2] >> (16 * (i & 1)) & 0xffffu);
+          q[m][i] = pair_of(f.x, f.y);
+        }
+        scale[m] = __ldg(A.sx + m * A.ldsx + v / (kBlock / 16)) * of_w;
+      }
+#pragma unroll
+      for (int c = 0; c < kFewCols; ++c) {
+        const uint32_t words[4] = {a[u][c].x, a[u][c].y, a[u][c].z, a[u][c].w};
+        f32x2 sum[ROWS];
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m) sum[m] = 0ull;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float2 f = decode2(words[i / 2] >> (16 * (i & 1)) & 0xffffu);
+          const f32x2 p = pair_of(f.x, f.y);
+#pragma unroll
+          for (int m = 0; m < ROWS; ++m) sum[m] = fma2(p, q[m][i], sum[m]);
+        }
+#pragma unroll
+        for (int m = 0; m < ROWS; ++m) {
+          float lo, hi;
+          split(sum[m], lo, hi);
+          s[c * kRows2 + m] = fmaf(lo + hi, scale[m], s[c * kRows2 + m]);
+        }
+      }
+    }
+  }
+  for (long long k = (long long)nv * 16 + first; k < K; k += step) {
+    float q[ROWS];
+#pragma unroll
+    for (int m = 0; m < ROWS; ++m) q[m] = decode2(x[m * ldx + k]).x * (__ldg(A.sx + m * A.ldsx + k / kBlock) * __ldg(sw + k / kBlock));
+#pragma unroll
+    for (int c = 0; c < kFewCols; ++c) {
+      const float p = decode2(wr[c][k]).x;
+#pragma unroll
+      for (int m = 0; m < ROWS; ++m) s[c * kRows2 + m] = fmaf(p, q[m], s[c * kRows2 + m]);
+    }
+  }
+  fold(s, lane);
+  if (lane % (32 / kSums) == 0) part[warp][lane / (32 / kSums)] = s[0];
+  __syncthreads();
+  if (t < kFewCols * kWarps >> log_parts) {
+    float y[8] = {};
+    for (int i = 0; i < parts; ++i)
+#pragma unroll
+      for (int m = 0; m < ROWS; ++m) y[m] += part[(t / kFewCols << log_parts) + i][t % kFewCols * kRows2 + m];
+    finish_column<T, false>(A, A.I, A.J, 0, col0 + t, y);
+  }
+}
+
+// Codes that a tensor map cannot describe are copied with a pitch of a multiple of 16 bytes.
+__global__ void __launch_bounds__(256) copy_codes_kernel(const uint8_t* src, long long ld, uint8_t* dst, long long pitch, long long rows, long long cols) {
+  allow_next();
+  const long long groups = (cols + 15) / 16, n = rows * groups, stride = (long long)gridDim.x * blockDim.x;
+  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) {
+    const long long r = i / groups, c = (i - r * groups) * 16;
+    const uint8_t* s = src + r * ld + c;
+    uint32_t w[4] = {};
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+      if (c + e < cols) w[e / 4] |= (uint32_t)s[e] << (8 * (e % 4));
+    *reinterpret_cast<uint4*>(dst + r * pitch + c) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+long long pad16(long long x) { return (x + 15) / 16 * 16; }
+bool codes_mappable(const Operand& o) { return ((uintptr_t)o.p & 15u) == 0 && o.ld % 16 == 0; }
+size_t copy_bytes(const Operand& o) { return codes_mappable(o) ? 0 : align256((size_t)o.rows * pad16(o.cols)); }
+
+laq_status make_codes_mappable(const Err& e, Operand& o, char*& ws, cudaStream_t st) {
+  const size_t bytes = copy_bytes(o);
+  if (!bytes) return LAQ_OK;
+  const long long pitch = pad16(o.cols), want = (o.rows * (pitch / 16) + 255) / 256, most = 8 * kSMs;
+  LAQ_TRY(launched(e.buf, e.len, launch_plain(copy_codes_kernel, dim3((unsigned)(want < most ? want : most)), 256, st, (const uint8_t*)o.p, o.ld,
+                                              (uint8_t*)ws, pitch, o.rows, o.cols)));
+  o.p = ws;
+  o.ld = pitch;
+  ws += bytes;
+  return LAQ_OK;
+}
+
+struct Spread {                // of the 16 groups of a thread block over blocks of columns and rows
+  int log_across;
+  dim3 grid;
+  Spread(long long rows, long long cols) {
+    const long long across = blocks_across(cols);
+    log_across = across >= 16 ? 4 : across >= 8 ? 3 : across >= 4 ? 2 : across >= 2 ? 1 : 0;
+    const long long down = (kPackThreads / kLanes >> log_across) * kPackAhead, runs = (rows + down - 1) / down;
+    grid = dim3((unsigned)((across + (1 << log_across) - 1) >> log_across), (unsigned)(runs < 65535 ? runs : 65535));
+  }
+};
+
+template <class T>
+laq_status pack_typed(const Err& e, const T* x, long long rows, long long cols, long long ld, const laq_blocks& b, cudaStream_t st) {
+  uint8_t* codes = (uint8_t*)const_cast<void*>(b.codes);
+  float* scales = const_cast<float*>(b.scales);
+  const int vec_in = ((uintptr_t)x & 15u) == 0 && ld * (long long)sizeof(T) % 16 == 0, vec_out = Codes(&b).vectors(8);
+  if (b.block_rows == kBlock) {
+    const long long across = blocks_across(cols), tiles = across * ((rows + kBlock - 1) / kBlock);
+    return launched(e.buf, e.len, launch_plain(pack_tiles_kernel<T>, dim3((unsigned)tiles), kPackThreads, st, x, ld, rows, cols, codes, b.ld_codes, scales,
+                                               b.ld_scales, across, vec_in, vec_out));
+  }
+  const Spread s(rows, cols);
+  return launched(e.buf, e.len, launch_plain(pack_rows_kernel<T>, s.grid, kPackThreads, st, x, ld, rows, cols, codes, b.ld_codes, scales, b.ld_scales,
+                                             s.log_across, vec_in, vec_out));
+}
+
+template <class T>
+laq_status unpack_typed(const Err& e, const laq_blocks& b, long long rows, long long cols, T* out, long long ld, cudaStream_t st) {
+  const Spread s(rows, cols);
+  const int vec_out = ((uintptr_t)out & 15u) == 0 && ld * (long long)sizeof(T) % 16 == 0;
+  return launched(e.buf, e.len, launch_plain(unpack_kernel<T>, s.grid, kPackThreads, st, Codes(&b), rows, cols, out, ld, s.log_across,
+                                             (int)Codes(&b).vectors(8), vec_out));
+}
+
+template <class T>
+void list_block_kernels(const void** list, int& n) {
+  const void* all[] = {(const void*)pack_rows_kernel<T>, (const void*)pack_tiles_kernel<T>, (const void*)unpack_kernel<T>};
+  for (const void* k : all) list[n++] = k;
+}
+template <class T>
+void list_product_kernels(const void** list, int& n) {
+  const void* all[] = {(const void*)linear_gemm_kernel<T, false, false, false, false, kCodes>, (const void*)linear_gemm_kernel<T, true, false, false, false, kCodes>,
+                       (const void*)linear_gemm_kernel<T, false, true, false, false, kCodes>,  (const void*)linear_few_codes_kernel<T, 1>,
+                       (const void*)linear_few_codes_kernel<T, 2>, (const void*)linear_few_codes_kernel<T, 3>, (const void*)linear_few_codes_kernel<T, 4>};
+  for (const void* k : all) list[n++] = k;
+}
+
+laq_status check_matrix(const Err& e, int64_t rows, int64_t cols) {
+  const int64_t most = 0x7fffff00ll;
+  if (rows < 0 || rows > most || cols < 1 || cols > most) return fail(e.buf, e.len, LAQ_EINVAL, "rows must be 0..2^31-256, cols 1..2^31-256");
+  return LAQ_OK;
+}
+
+bool takes_few_codes(const laq_linear_call* c) { return !(c->flags & LAQ_LINEAR_STARVE) && c->M <= kFewRows; }
+
+Operand codes_of(const laq_blocks* b, long long rows, long long cols) { return Operand{b->codes, b->ld_codes, rows, cols}; }
+
+template <class T>
+laq_status few_codes(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
+  const int vec = codes_mappable(x) && codes_mappable(w);
+  const long long groups = (w.rows + kFewCols - 1) / kFewCols, items = vec ? w.cols / 16 : w.cols;
+  const int log_parts = few_log_parts(groups, items < (1 << 30) ? (int)items : 1 << 30), per_block = kFewThreads / 32 >> log_parts;
+  const auto kernel = x.rows == 1 ? linear_few_codes_kernel<T, 1> : x.rows == 2 ? linear_few_codes_kernel<T, 2>
+                      : x.rows == 3 ? linear_few_codes_kernel<T, 3> : linear_few_codes_kernel<T, 4>;
+  return launched(e.buf, e.len, launch_plain(kernel, dim3((unsigned)((groups + per_block - 1) / per_block)), kFewThreads, st, A, (const uint8_t*)x.p, x.ld,
+                                             (const uint8_t*)w.p, w.ld, w.cols, vec, log_parts));
+}
+
+}  // namespace
+
+laq_status load_block_kernels(const Err& e) {
+  static Loaded loaded;
+  static const void* list[32];
+  static const int n = [] {
+    int count = 0;
+    list_block_kernels<float>(list, count);
+    list_block_kernels<__nv_bfloat16>(list, count);
+    list_block_kernels<__half>(list, count);
+    list_product_kernels<__nv_bfloat16>(list, count);
+    list_product_kernels<__half>(list, count);
+    list[count++] = (const void*)copy_codes_kernel;
+    return count;
+  }();
+  return launched(e.buf, e.len, loaded.once(list, n));
+}
+
+laq_status pack_blocks(const Err& e, const void* x, int dtype, long long rows, long long cols, long long ld, const laq_blocks& b, cudaStream_t st) {
+  return dtype == LAQ_F32    ? pack_typed(e, (const float*)x, rows, cols, ld, b, st)
+         : dtype == LAQ_BF16 ? pack_typed(e, (const __nv_bfloat16*)x, rows, cols, ld, b, st)
+                             : pack_typed(e, (const __half*)x, rows, cols, ld, b, st);
+}
+
+laq_status unpack_blocks(const Err& e, const laq_blocks& b, long long rows, long long cols, int dtype, void* out, long long ld, cudaStream_t st) {
+  return dtype == LAQ_F32    ? unpack_typed(e, b, rows, cols, (float*)out, ld, st)
+         : dtype == LAQ_BF16 ? unpack_typed(e, b, rows, cols, (__nv_bfloat16*)out, ld, st)
+                             : unpack_typed(e, b, rows, cols, (__half*)out, ld, st);
+}
+
+laq_status check_blocks(const Err& e, Buffers& buffers, const char* name, const char* scales_name, Access access, const laq_blocks* b, int64_t rows,
+                        int64_t cols) {
+  if (!b || !b->codes || !b->scales) return fail(e.buf, e.len, LAQ_EINVAL, "the codes or the scales of %s are null", name);
+  if (b->block_rows != 1 && b->block_rows != kBlock) return fail(e.buf, e.len, LAQ_EINVAL, "block_rows of %s must be 1 or 128", name);
+  const int64_t down = b->block_rows == 1 ? rows : (rows + kBlock - 1) / kBlock;
+  LAQ_TRY(check_tensor(e, buffers, name, access, b->codes, true, rows, b->ld_codes, cols, 1));
+  return check_tensor(e, buffers, scales_name, access, b->scales, true, down, b->ld_scales, blocks_across(cols), 4);
+}
+
+}  // namespace ops
+}  // namespace laq
+
+using namespace laq::ops;
+
+extern "C" laq_status laq_pack_blocks(const void* d_x, int32_t dtype, int64_t rows, int64_t cols, int64_t row_stride, const laq_blocks* out,
+                                      void* cuda_stream, char* errbuf, size_t errbuf_len) {
+  const Err e{errbuf, errbuf_len};
+  if (errbuf && errbuf_len) errbuf[0] = 0;
+  if (!dtype_bytes(dtype)) return fail(errbuf, errbuf_len, LAQ_EINVAL, "dtype must be LAQ_F32, LAQ_BF16 or LAQ_F16");
+  LAQ_TRY(check_matrix(e, rows, cols));
+  if (rows == 0) return LAQ_OK;
+  Buffers buffers;
+  LAQ_TRY(check_tensor(e, buffers, "x", kRead, d_x, true, rows, row_stride, cols, dtype_bytes(dtype)));
+  LAQ_TRY(check_blocks(e, buffers, "out", "the scales of out", kWritten, out, rows, cols));
+  LAQ_TRY(buffers.check(errbuf, errbuf_len));
+  LAQ_TRY(load_block_kernels(e));
+  return pack_blocks(e, d_x, dtype, rows, cols, row_stride, *out, (cudaStream_t)cuda_stream);
+}
+
+extern "C" laq_status laq_unpack_blocks(const laq_blocks* x, int64_t rows, int64_t cols, void* d_out, int32_t dtype, int64_t row_stride,
+                                        void* cuda_stream, char* errbuf, size_t errbuf_len) {
+  const Err e{errbuf, errbuf_len};
+  if (errbuf && errbuf_len) errbuf[0] = 0;
+  if (!dtype_bytes(dtype)) return fail(errbuf, errbuf_len, LAQ_EINVAL, "dtype must be LAQ_F32, LAQ_BF16 or LAQ_F16");
+  LAQ_TRY(check_matrix(e, rows, cols));
+  if (rows == 0) return LAQ_OK;
+  Buffers buffers;
+  LAQ_TRY(check_blocks(e, buffers, "x", "the scales of x", kRead, x, rows, cols));
+  LAQ_TRY(check_tensor(e, buffers, "out", kWritten, d_out, true, rows, row_stride, cols, dtype_bytes(dtype)));
+  LAQ_TRY(buffers.check(errbuf, errbuf_len));
+  LAQ_TRY(load_block_kernels(e));
+  return unpack_blocks(e, *x, rows, cols, dtype, d_out, row_stride, (cudaStream_t)cuda_stream);
+}
+
+extern "C" laq_status laq_linear_blocks_forward(const laq_linear_call* c, const laq_blocks* xq, const laq_blocks* wq, void* d_workspace,
+                                                size_t workspace_bytes, void* cuda_stream, char* errbuf, size_t errbuf_len) {
+  const Err e{errbuf, errbuf_len};
+  if (errbuf && errbuf_len) errbuf[0] = 0;
+  if (!c || !xq || !wq) return fail(errbuf, errbuf_len, LAQ_EINVAL, "null pointer");
+  const size_t need = laq_linear_blocks_workspace_bytes(c, xq, wq, 0);
+  LAQ_TRY(check_layer(e, c->dtype, c->M, c->N, c->K, c->activation, c->status, c->flags, d_workspace, workspace_bytes, need));
+  if (c->M == 0) return LAQ_OK;
+  if (xq->block_rows != 1 && c->M > 1) return fail(errbuf, errbuf_len, LAQ_EINVAL, "x must have a scale for each row (block_rows 1)");
+  if (wq->block_rows != kBlock && c->N > 1) return fail(errbuf, errbuf_len, LAQ_EINVAL, "w must have a scale for each tile of 128 rows (block_rows 128)");
+  Buffers buffers;
+  buffers.out("status", c->status, 4, 1, 1, 1);
+  if (need) buffers.out("the workspace", d_workspace, 1, 1, (long long)need, (long long)need);
+  LAQ_TRY(check_blocks(e, buffers, "x", "the scales of x", kRead, xq, c->M, c->K));
+  LAQ_TRY(check_blocks(e, buffers, "w", "the scales of w", kRead, wq, c->N, c->K));
+  LAQ_TRY(check_tensor(e, buffers, "bias", kRead, c->bias, false, 1, c->N, c->N, 2));
+  LAQ_TRY(check_tensor(e, buffers, "residual", kRead, c->residual, false, c->M, c->ld_residual, c->N, 2));
+  LAQ_TRY(check_tensor(e, buffers, "y", kWritten, c->y, true, c->M, c->ld_y, c->N, 2, "residual"));
+  LAQ_TRY(check_tensor(e, buffers, "z", kWritten, c->z, false, c->M, c->ld_z, c->N, 2));
+  LAQ_TRY(buffers.check(errbuf, errbuf_len));
+  LAQ_TRY(load_block_kernels(e));
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  Operand x = codes_of(xq, c->M, c->K), w = codes_of(wq, c->N, c->K);
+  GemmArgs A = {};
+  A.I = (int)c->M;
+  A.J = (int)c->N;
+  A.act = c->activation;
+  A.starve = (c->flags & LAQ_LINEAR_STARVE) != 0;
+  A.out = c->y;
+  A.ldo = c->ld_y;
+  A.z = c->z;
+  A.ldz = c->ld_z;
+  A.bias = c->bias;
+  A.residual = c->residual;
+  A.ldr = c->ld_residual;
+  A.status = c->status;
+  A.sx = xq->scales;
+  A.ldsx = xq->ld_scales;
+  A.sw = wq->scales;
+  A.ldsw = wq->ld_scales;
+  if (takes_few_codes(c)) return c->dtype == LAQ_BF16 ? few_codes<__nv_bfloat16>(e, A, x, w, st) : few_codes<__half>(e, A, x, w, st);
+  char* ws = (char*)d_workspace;
+  LAQ_TRY(make_codes_mappable(e, x, ws, st));
+  LAQ_TRY(make_codes_mappable(e, w, ws, st));
+  const bool follows = ws != d_workspace;
+  return c->dtype == LAQ_BF16 ? product_in_mode<__nv_bfloat16, kCodes>(e, A, x, w, 0, follows, st) : product_in_mode<__half, kCodes>(e, A, x, w, 0, follows, st);
+}
+
+namespace laq {
+namespace ops {
+size_t blocks_forward_bytes(const laq_linear_call* c, const laq_blocks* xq, const laq_blocks* wq) {
+  if (!xq || !wq || takes_few_codes(c)) return 0;
+  return copy_bytes(codes_of(xq, c->M, c->K)) + copy_bytes(codes_of(wq, c->N, c->K));
+}
+}  // namespace ops
+}  // namespace laq

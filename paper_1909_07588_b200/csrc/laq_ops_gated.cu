@@ -1,0 +1,351 @@
+// A gated feed-forward block's two projections, its activation and their product, and the gradient:
+//   Z = X W^T + b,  W [2F][K]: F rows of gates G, then as many of ups U;   H = act(G) U         X [M][K], Z [M][2F], H [M][F]
+//   dG = dH U act'(G),  dU = dH act(G),  dZ = [dG | dU];   dX = dZ W,  dW = dZ^T X,  db = column sums of dZ
+// The forward pass is one product whose tiles hold as many columns of gates as of the ups that belong to them
+// (linear_gemm_kernel, kGated), so that H leaves the epilogue and Z is written only if it is asked for.  H is rounded once, from
+// sums in fp32.  With W as one matrix the gradient is two products as a layer's is; dZ is rounded once to the operands' type, as there.
+#include "laq_ops_gemm.cuh"
+
+namespace laq {
+namespace ops {
+namespace {
+
+// dZ and its column sums.  Bound by memory.  A block takes 256 columns of the gates and of the ups (32 threads of eight) and a run
+// of rows (8 threads); sums in fp32 of the unrounded products, to part[run][2F].  CODES: Z comes in 8 bits.  Without vectors
+// (odd sizes or addresses) a thread's eight columns lie 32 apart, so that neighbouring lanes have neighbouring columns.
+constexpr int kCols = 256, kThreads = 256;
+
+template <class T, bool CODES>
+__global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long long lddh, const T* z, long long ldz, const Codes zq, T* dz, long long lddz,
+                                                               float* part, long long M, long long F, int act, int rows_per, int vec_ok) {
+  __shared__ float sh[8][2 * kCols];
+  allow_next();
+  const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
+  const long long base = (long long)blockIdx.x * kCols;
+  const long long r0 = (long long)blockIdx.y * rows_per, r1 = min(r0 + (long long)rows_per, M);
+  float sum[2][8] = {};
+  // dG and dU of eight pairs, in place of the gates and the ups
+  const auto slopes = [&](const float (&d)[8], float (&g)[8], float (&u)[8]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      float value = g[e], slope = 1.f;
+      if (act == LAQ_ACT_RELU) {
+        slope = g[e] > 0.f ? 1.f : (g[e] == g[e] ? 0.f : g[e]);
+        value = max_nan(g[e], 0.f);
+      } else if (act == LAQ_ACT_GELU) {
+        gelu_both(g[e], value, slope);
+      } else if (act == LAQ_ACT_SILU) {
+        const float s = sigmoid(g[e]);
+        value = g[e] * s;
+        slope = s * fmaf(g[e], 1.f - s, 1.f);
+      }
+      g[e] = d[e] * u[e] * slope;
+      u[e] = d[e] * value;
+      sum[0][e] += g[e];
+      sum[1][e] += u[e];
+    }
+  };
+  if (vec_ok) {
+    const long long c0 = base + tx * 8;
+    if (c0 < F) {
+      for (long long r = r0 + ty; r < r1; r += 16) {
+        const bool two = r + 8 < r1;
+        uint4 d[2], g[2], u[2];
+        uint2 qg[2], qu[2];
+        float sg[2], su[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const long long row = two || i == 0 ? r + 8 * i : r;             // a row is read twice rather than beyond the last
+          d[i] = load16(dh + row * lddh + c0);
+          if constexpr (CODES) {
+            qg[i] = load8(zq.p + row * zq.ld + c0);
+            qu[i] = load8(zq.p + row * zq.ld + F + c0);
+            sg[i] = zq.scale(row, c0);
+            su[i] = zq.scale(row, F + c0);
+          } else {
+            g[i] = load16(z + row * ldz + c0);
+            u[i] = load16(z + row * ldz + F + c0);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (i == 1 && !two) break;
+          float df[8], gf[8], uf[8];
+          Elem<T>::unpack(d[i], df);
+          if constexpr (CODES) {
+            decode8(qg[i], sg[i], gf);
+            decode8(qu[i], su[i], uf);
+          } else {
+            Elem<T>::unpack(g[i], gf);
+            Elem<T>::unpack(u[i], uf);
+          }
+          slopes(df, gf, uf);
+          if (dz) {
+            T* o = dz + (r + 8 * i) * lddz + c0;
+            *reinterpret_cast<uint4*>(o) = Elem<T>::pack(gf);
+            *reinterpret_cast<uint4*>(o + F) = Elem<T>::pack(uf);
+          }
+        }
+      }
+    }
+  } else {
+    for (long long r = r0 + ty; r < r1; r += 8) {
+      float df[8], gf[8], uf[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const long long c = base + tx + 32 * e;
+        const bool there = c < F;
+        df[e] = there ? Elem<T>::to_float(dh[r * lddh + c]) : 0.f;
+        if constexpr (CODES) {
+          gf[e] = there ? zq.value(r, c) : 0.f;
+          uf[e] = there ? zq.value(r, F + c) : 0.f;
+        } else {
+          gf[e] = there ? Elem<T>::to_float(z[r * ldz + c]) : 0.f;
+          uf[e] = there ? Elem<T>::to_float(z[r * ldz + F + c]) : 0.f;
+        }
+      }
+      slopes(df, gf, uf);
+      if (dz) {
+        T* o = dz + r * lddz;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const long long c = base + tx + 32 * e;
+          if (c < F) {
+            o[c] = Elem<T>::from_float(gf[e]);
+            o[F + c] = Elem<T>::from_float(uf[e]);
+          }
+        }
+      }
+    }
+  }
+  if (!part) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sh[ty][h * kCols + (vec_ok ? tx * 8 + e : tx + 32 * e)] = sum[h][e];
+  __syncthreads();
+  const long long c = base + threadIdx.x;
+  if (c >= F) return;
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float t = 0.f;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) t += sh[y][h * kCols + threadIdx.x];
+    part[(long long)blockIdx.y * 2 * F + h * F + c] = t;
+  }
+}
+
+// ---- host -----------------------------------------------------------------------------------------------------------------
+constexpr long long kLongestSum = 65536;       // terms that a 16-bit result takes without chunks
+
+laq_status check_call(const Err& e, const laq_gated_call* c, void* ws, size_t ws_bytes, size_t need) {
+  if (e.buf && e.len) e.buf[0] = 0;
+  if (!c) return fail(e.buf, e.len, LAQ_EINVAL, "null pointer");
+  if (c->F < 1 || c->F > 0x3fffff00ll) return fail(e.buf, e.len, LAQ_EINVAL, "F must be 1..2^30-256");
+  if (c->K > kLongestSum) return fail(e.buf, e.len, LAQ_EINVAL, "K must be 1..65536");
+  return check_layer(e, c->dtype, c->M, 2 * c->F, c->K, c->activation, c->status, c->flags, ws, ws_bytes, need);
+}
+
+bool sizes_ok(const laq_gated_call* c) {
+  return c && c->M >= 0 && c->M <= 0x7fffff00ll && c->F >= 1 && c->F <= 0x3fffff00ll && c->K >= 1 && c->K <= kLongestSum &&
+         (c->dtype == LAQ_BF16 || c->dtype == LAQ_F16);
+}
+
+// By the same rule as a layer's (laq_ops_linear.cu), for as many rows of W.
+bool takes_few_rows(const laq_gated_call* c) {
+  if (c->flags & LAQ_LINEAR_STARVE) return false;
+  return c->M <= 2 || (c->M <= kFewRows && (c->K >= 1024 || 2 * c->F <= kFewCols * kFewThreads / 32 * kFewBlocks * kSMs));
+}
+
+struct ForwardNeeds {
+  Operand x, w;
+  size_t z_bytes;               // Z in 16 bits, before it is packed
+  explicit ForwardNeeds(const laq_gated_call* c) : x{c->x, c->ld_x, c->M, c->K}, w{c->w, c->ld_w, 2 * c->F, c->K} {
+    z_bytes = c->z_blocks ? align256((size_t)c->M * pad8(2 * c->F) * 2) : 0;
+  }
+  size_t bytes(const laq_gated_call* c) const { return z_bytes + (takes_few_rows(c) ? 0 : x.pack_bytes() + w.pack_bytes()); }
+};
+
+struct BackwardNeeds {
+  size_t dz_bytes, part_bytes, x_bytes;
+  Operand x, w, dz;
+  explicit BackwardNeeds(const laq_gated_call* c)
+      : x{c->x, c->ld_x, c->M, c->K}, w{c->w, c->ld_w, 2 * c->F, c->K}, dz{nullptr, pad8(2 * c->F), c->M, 2 * c->F} {
+    const int per = dz_rows_per(c->M, c->F);
+    dz_bytes = c->dx || c->dw ? align256((size_t)c->M * dz.ld * 2) : 0;
+    part_bytes = c->db ? align256((size_t)((c->M + per - 1) / per) * 2 * c->F * 4) : 0;
+    if (c->x_blocks) x = Operand{nullptr, pad8(c->K), c->M, c->K};
+    x_bytes = c->x_blocks && c->dw ? align256((size_t)c->M * x.ld * 2) : 0;
+  }
+  size_t bytes(const laq_gated_call* c) const {
+    return dz_bytes + part_bytes + x_bytes + (c->dw ? x.pack_bytes() : 0) + (c->dx ? w.pack_bytes() : 0);
+  }
+};
+
+template <class T, int ROWS>
+laq_status launch_few(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
+  const int K = (int)x.cols, vec = x.mappable_() && w.mappable_(), items = vec ? K / 8 : K;
+  const long long groups = (A.up + kFewCols / 2 - 1) / (kFewCols / 2);
+  const int log_parts = few_log_parts(groups, items), per_block = kFewThreads / 32 >> log_parts;
+  const auto kernel = ROWS <= 2 && items > 64 << log_parts ? linear_few_rows_kernel<T, ROWS, ROWS <= 2 ? 4 : 2, true>
+                                                          : linear_few_rows_kernel<T, ROWS, 2, true>;
+  return launched(e.buf, e.len, launch_plain(kernel, dim3((unsigned)((groups + per_block - 1) / per_block)), kFewThreads, st, A, (const T*)x.p, x.ld,
+                                             (const T*)w.p, w.ld, K, vec, log_parts));
+}
+
+template <class T>
+laq_status few_rows(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
+  switch (x.rows) {
+    case 1: return launch_few<T, 1>(e, A, x, w, st);
+    case 2: return launch_few<T, 2>(e, A, x, w, st);
+    case 3: return launch_few<T, 3>(e, A, x, w, st);
+    default: return launch_few<T, 4>(e, A, x, w, st);
+  }
+}
+
+template <class T>
+void list_kernels(const void** list, int& n) {
+  const void* all[] = {(const void*)linear_gemm_kernel<T, false, false, false, false, kGated>, (const void*)linear_gemm_kernel<T, true, false, false, false, kGated>,
+                       (const void*)linear_gemm_kernel<T, false, true, false, false, kGated>,
+                       (const void*)linear_few_rows_kernel<T, 1, 4, true>, (const void*)linear_few_rows_kernel<T, 1, 2, true>,
+                       (const void*)linear_few_rows_kernel<T, 2, 4, true>, (const void*)linear_few_rows_kernel<T, 2, 2, true>,
+                       (const void*)linear_few_rows_kernel<T, 3, 2, true>, (const void*)linear_few_rows_kernel<T, 4, 2, true>,
+                       (const void*)gated_dz_kernel<T, false>, (const void*)gated_dz_kernel<T, true>};
+  for (const void* k : all) list[n++] = k;
+}
+
+// Its own kernels, and those of the products and of the 8-bit matrices that its calls may use.
+laq_status load_kernels(const Err& e) {
+  static Loaded loaded;
+  static const void* list[32];
+  static const int n = [] {
+    int count = 0;
+    list_kernels<__nv_bfloat16>(list, count);
+    list_kernels<__half>(list, count);
+    return count;
+  }();
+  LAQ_TRY(launched(e.buf, e.len, loaded.once(list, n)));
+  LAQ_TRY(load_layer_kernels(e));
+  return load_block_kernels(e);
+}
+
+}  // namespace
+}  // namespace ops
+}  // namespace laq
+
+using namespace laq::ops;
+
+extern "C" size_t laq_gated_workspace_bytes(const laq_gated_call* c, int32_t backward) {
+  if (!sizes_ok(c)) return 0;
+  return backward ? BackwardNeeds(c).bytes(c) : ForwardNeeds(c).bytes(c);
+}
+
+extern "C" laq_status laq_gated_forward(const laq_gated_call* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* errbuf,
+                                        size_t errbuf_len) {
+  const Err e{errbuf, errbuf_len};
+  const size_t ws_bytes = laq_gated_workspace_bytes(c, 0);
+  LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, ws_bytes));
+  if (c->z && c->z_blocks) return fail(errbuf, errbuf_len, LAQ_EINVAL, "z and z_blocks are both given");
+  if (c->M == 0) return LAQ_OK;
+  const long long N = 2 * c->F;
+  Buffers buffers;
+  buffers.out("status", c->status, 4, 1, 1, 1);
+  if (ws_bytes) buffers.out("the workspace", d_workspace, 1, 1, (long long)ws_bytes, (long long)ws_bytes);
+  LAQ_TRY(check_tensor(e, buffers, "x", kRead, c->x, true, c->M, c->ld_x, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "w", kRead, c->w, true, N, c->ld_w, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "bias", kRead, c->bias, false, 1, N, N, 2));
+  LAQ_TRY(check_tensor(e, buffers, "h", kWritten, c->h, true, c->M, c->ld_h, c->F, 2));
+  if (c->z_blocks) LAQ_TRY(check_blocks(e, buffers, "z", "the scales of z", kWritten, c->z_blocks, c->M, N));
+  else LAQ_TRY(check_tensor(e, buffers, "z", kWritten, c->z, false, c->M, c->ld_z, N, 2));
+  LAQ_TRY(buffers.check(errbuf, errbuf_len));
+  LAQ_TRY(load_kernels(e));
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  ForwardNeeds need(c);
+  char* ws = (char*)d_workspace;
+  GemmArgs A = {};
+  A.I = (int)c->M;
+  A.J = (int)c->F;
+  A.up = c->F;
+  A.act = c->activation;
+  A.starve = (c->flags & LAQ_LINEAR_STARVE) != 0;
+  A.out = c->h;
+  A.ldo = c->ld_h;
+  A.z = c->z;
+  A.ldz = c->ld_z;
+  A.bias = c->bias;
+  A.status = c->status;
+  if (c->z_blocks) {
+    A.z = ws;
+    A.ldz = pad8(N);
+    ws += need.z_bytes;
+  }
+  const bool bf16 = c->dtype == LAQ_BF16;
+  if (takes_few_rows(c)) {
+    LAQ_TRY(bf16 ? few_rows<__nv_bfloat16>(e, A, need.x, need.w, st) : few_rows<__half>(e, A, need.x, need.w, st));
+  } else {
+    const char* before = ws;
+    LAQ_TRY(make_mappable(e, need.x, ws, st));
+    LAQ_TRY(make_mappable(e, need.w, ws, st));
+    const bool follows = ws != before;
+    LAQ_TRY(bf16 ? product_in_mode<__nv_bfloat16, kGated>(e, A, need.x, need.w, 1, follows, st)
+                 : product_in_mode<__half, kGated>(e, A, need.x, need.w, 0, follows, st));
+  }
+  if (c->z_blocks) return pack_blocks(e, A.z, c->dtype, c->M, N, A.ldz, *c->z_blocks, st);
+  return LAQ_OK;
+}
+
+extern "C" laq_status laq_gated_backward(const laq_gated_call* c, void* d_workspace, size_t workspace_bytes, void* cuda_stream, char* errbuf,
+                                         size_t errbuf_len) {
+  const Err e{errbuf, errbuf_len};
+  const size_t ws_bytes = laq_gated_workspace_bytes(c, 1);
+  LAQ_TRY(check_call(e, c, d_workspace, workspace_bytes, ws_bytes));
+  if (!c->dx && !c->dw && !c->db) return LAQ_OK;
+  if (c->z && c->z_blocks) return fail(errbuf, errbuf_len, LAQ_EINVAL, "z and z_blocks are both given");
+  if (c->x && c->x_blocks) return fail(errbuf, errbuf_len, LAQ_EINVAL, "x and x_blocks are both given");
+  const long long N = 2 * c->F;
+  cudaStream_t st = (cudaStream_t)cuda_stream;
+  Buffers buffers;
+  buffers.out("status", c->status, 4, 1, 1, 1);
+  if (ws_bytes) buffers.out("the workspace", d_workspace, 1, 1, (long long)ws_bytes, (long long)ws_bytes);
+  LAQ_TRY(check_tensor(e, buffers, "dw", kWritten, c->dw, false, N, c->ld_dw, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "db", kWritten, c->db, false, 1, N, N, 4));
+  const Gradients to{c->dx, c->ld_dx, c->dw, c->ld_dw, 0};
+  if (c->M == 0) {
+    LAQ_TRY(buffers.check(errbuf, errbuf_len));
+    return zero_gradients(e, to, c->db, N, c->K, st);
+  }
+  LAQ_TRY(check_tensor(e, buffers, "dh", kRead, c->dh, true, c->M, c->ld_dh, c->F, 2));
+  if (c->z_blocks) LAQ_TRY(check_blocks(e, buffers, "z", "the scales of z", kRead, c->z_blocks, c->M, N));
+  else LAQ_TRY(check_tensor(e, buffers, "z", kRead, c->z, true, c->M, c->ld_z, N, 2));
+  if (c->dw) {
+    if (c->x_blocks) LAQ_TRY(check_blocks(e, buffers, "x", "the scales of x", kRead, c->x_blocks, c->M, c->K));
+    else LAQ_TRY(check_tensor(e, buffers, "x", kRead, c->x, true, c->M, c->ld_x, c->K, 2));
+  }
+  if (c->dx) LAQ_TRY(check_tensor(e, buffers, "w", kRead, c->w, true, N, c->ld_w, c->K, 2));
+  LAQ_TRY(check_tensor(e, buffers, "dx", kWritten, c->dx, false, c->M, c->ld_dx, c->K, 2));
+  LAQ_TRY(buffers.check(errbuf, errbuf_len));
+  LAQ_TRY(load_kernels(e));
+  BackwardNeeds need(c);
+  char* ws = (char*)d_workspace;
+  void* dz = need.dz_bytes ? ws : nullptr;
+  float* part = c->db ? (float*)(ws + need.dz_bytes) : nullptr;
+  ws += need.dz_bytes + need.part_bytes;
+  const int per = dz_rows_per(c->M, c->F), runs = (int)((c->M + per - 1) / per);
+  const dim3 grid((unsigned)((c->F + kCols - 1) / kCols), (unsigned)runs);
+  const Codes zq(c->z_blocks);
+  const int vec_ok = c->F % 8 == 0 && mappable(c->dh, c->ld_dh) && (c->z_blocks ? zq.vectors(8) : mappable(c->z, c->ld_z));
+  const auto launch_dz = [&](auto zero) {
+    using T = decltype(zero);
+    return launch_plain(c->z_blocks ? gated_dz_kernel<T, true> : gated_dz_kernel<T, false>, grid, kThreads, st, (const T*)c->dh, c->ld_dh, (const T*)c->z,
+                        c->ld_z, zq, (T*)dz, need.dz.ld, part, c->M, c->F, c->activation, per, vec_ok);
+  };
+  LAQ_TRY(launched(errbuf, errbuf_len, c->dtype == LAQ_BF16 ? launch_dz(__nv_bfloat16()) : launch_dz(__half())));
+  if (c->db) LAQ_TRY(column_sums(e, part, runs, (int)N, c->db, st));
+  need.dz.p = dz;
+  if (need.x_bytes) {
+    need.x.p = ws;
+    ws += need.x_bytes;
+    LAQ_TRY(unpack_blocks(e, *c->x_blocks, c->M, c->K, c->dtype, const_cast<void*>(need.x.p), need.x.ld, st));
+  }
+  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, st);
+}

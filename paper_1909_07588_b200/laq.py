@@ -22,7 +22,9 @@ FLAG_SPARSE_X = 8
 EXPORTS = ["laq_workspace_bytes", "laq_init", "laq_load_shards", "laq_set_gradients", "laq_step", "laq_step_local", "laq_local_uploads", "laq_apply_uploads", "laq_sync",
            "laq_get_state", "laq_get_worker", "laq_set_state", "laq_kernel_launches", "laq_tune", "laq_query", "laq_set_profiling", "laq_kernel_times", "laq_quantize_worker_static",
            "laq_token_logprobs", "laq_token_logprobs_backward", "laq_distill", "laq_distill_backward",
-           "laq_linear_workspace_bytes", "laq_linear_forward", "laq_linear_backward", "laq_last_error", "laq_destroy"]
+           "laq_linear_workspace_bytes", "laq_linear_forward", "laq_linear_backward",
+           "laq_pack_blocks", "laq_unpack_blocks", "laq_linear_blocks_workspace_bytes", "laq_linear_blocks_forward", "laq_linear_blocks_backward",
+           "laq_gated_workspace_bytes", "laq_gated_forward", "laq_gated_backward", "laq_last_error", "laq_destroy"]
 
 
 class LaqError(RuntimeError):
@@ -60,6 +62,20 @@ class laq_linear_call(C.Structure):
                 ("z", C.c_void_p), ("ld_z", C.c_int64), ("dy", C.c_void_p), ("ld_dy", C.c_int64), ("dx", C.c_void_p),
                 ("ld_dx", C.c_int64), ("dw", C.c_void_p), ("ld_dw", C.c_int64), ("db", C.c_void_p),
                 ("dw_dtype", C.c_int32), ("flags", C.c_uint32), ("status", C.c_void_p)]
+
+
+class laq_blocks(C.Structure):
+    _fields_ = [("codes", C.c_void_p), ("ld_codes", C.c_int64), ("scales", C.c_void_p), ("ld_scales", C.c_int64),
+                ("block_rows", C.c_int32)]
+
+
+class laq_gated_call(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32), ("M", C.c_int64), ("F", C.c_int64), ("K", C.c_int64),
+                ("x", C.c_void_p), ("ld_x", C.c_int64), ("w", C.c_void_p), ("ld_w", C.c_int64), ("bias", C.c_void_p),
+                ("h", C.c_void_p), ("ld_h", C.c_int64), ("z", C.c_void_p), ("ld_z", C.c_int64), ("dh", C.c_void_p),
+                ("ld_dh", C.c_int64), ("dx", C.c_void_p), ("ld_dx", C.c_int64), ("dw", C.c_void_p), ("ld_dw", C.c_int64),
+                ("db", C.c_void_p), ("x_blocks", C.POINTER(laq_blocks)), ("z_blocks", C.POINTER(laq_blocks)),
+                ("flags", C.c_uint32), ("status", C.c_void_p)]
 
 
 _lib = None
@@ -106,6 +122,17 @@ def load_library():
     L.laq_linear_workspace_bytes.restype = C.c_size_t
     L.laq_linear_forward.argtypes = [C.POINTER(laq_linear_call), C.c_void_p, C.c_size_t] + tail
     L.laq_linear_backward.argtypes = [C.POINTER(laq_linear_call), C.c_void_p, C.c_size_t] + tail
+    call, blocks, gated = C.POINTER(laq_linear_call), C.POINTER(laq_blocks), C.POINTER(laq_gated_call)
+    L.laq_pack_blocks.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_int64, blocks] + tail
+    L.laq_unpack_blocks.argtypes = [blocks, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_int64] + tail
+    L.laq_linear_blocks_workspace_bytes.argtypes = [call, blocks, blocks, C.c_int32]
+    L.laq_linear_blocks_workspace_bytes.restype = C.c_size_t
+    L.laq_linear_blocks_forward.argtypes = [call, blocks, blocks, C.c_void_p, C.c_size_t] + tail
+    L.laq_linear_blocks_backward.argtypes = [call, blocks, blocks, blocks, C.c_void_p, C.c_size_t] + tail
+    L.laq_gated_workspace_bytes.argtypes = [gated, C.c_int32]
+    L.laq_gated_workspace_bytes.restype = C.c_size_t
+    L.laq_gated_forward.argtypes = [gated, C.c_void_p, C.c_size_t] + tail
+    L.laq_gated_backward.argtypes = [gated, C.c_void_p, C.c_size_t] + tail
     L.laq_last_error.argtypes = [C.c_void_p]
     L.laq_last_error.restype = C.c_char_p
     L.laq_destroy.argtypes = [C.c_void_p]

@@ -6,6 +6,10 @@ The library's own models end at 16 classes and one hidden layer; a larger model'
 ``linear`` / ``linear_backward``                     a layer's product with bias, activation and residual; its gradient
 ``token_logprobs`` / ``token_logprobs_backward``     log probabilities of given tokens, entropy, top alternatives; gradient
 ``distill`` / ``distill_backward``                   divergence from a teacher's top logits; gradient, alone or with the loss
+``gated`` / ``gated_backward``                       a gated feed-forward block's two projections and their product; its gradient
+``pack8`` / ``unpack8``                              a matrix in 8 bits with a scale for each block of 128 (``Packed8``), and back:
+                                                     activations that the gradients above read in that form
+``linear8``                                          a layer's product on two such matrices
 
 Tensors are CUDA tensors with unit stride within a row and any row stride; outputs are allocated here unless ``out`` is
 given, which is refused if it shares memory with another tensor of the call other than where a call says so.  Gradients
@@ -14,6 +18,7 @@ of the tensors' device) and do not synchronise: their inputs must be ready in th
 soon as the call has returned.  They launch kernels only: there is no CPU fallback.  ``check_status`` reports a bounded wait
 of the product kernels that ran out.
 """
+import collections
 import ctypes as C
 import threading
 
@@ -298,6 +303,13 @@ def check_status(device=None):
                                      "complete" % (" (bits %d)" % bits if bits else ""))
 
 
+def _activation(name):
+    act = ACTIVATIONS.get(name)
+    if act is None:
+        _refuse("activation must be one of %s" % ", ".join(sorted(ACTIVATIONS)))
+    return act
+
+
 def _layer_call(x, weight, activation, flags, index):
     c = laq.laq_linear_call()
     c.x, c.ld_x, c.M, c.K = _rows(x, "x")
@@ -306,17 +318,14 @@ def _layer_call(x, weight, activation, flags, index):
         _refuse("x must be bfloat16 or float16")
     if inputs != c.K:
         _refuse("weight must be [outputs, %d]" % c.K)
-    act = ACTIVATIONS.get(activation)
-    if act is None:
-        _refuse("activation must be one of %s" % ", ".join(sorted(ACTIVATIONS)))
+    act = _activation(activation)
     if c.K < 1 or c.N < 1:
         _refuse("a layer needs inputs and outputs")
     c.dtype, c.activation, c.flags = DTYPES[x.dtype], act, flags
     return c
 
 
-def _workspace(L, c, backward, index, given):
-    need = L.laq_linear_workspace_bytes(C.byref(c), backward)
+def _workspace(need, index, given):
     if need == 0:
         return None, None, 0
     if given is None:
@@ -353,7 +362,7 @@ def linear(x, weight, bias=None, activation="none", residual=None, preact=False,
         if preact:
             z = _table(*shape, dt, x.device)
             c.z, c.ld_z = z.data_ptr(), c.N
-        ws, wp, wn = _workspace(L, c, 0, index, workspace)
+        ws, wp, wn = _workspace(L.laq_linear_workspace_bytes(C.byref(c), 0), index, workspace)
         _call(L.laq_linear_forward, C.byref(c), wp, wn, raw)
         return (y, z) if preact else y
 
@@ -362,28 +371,42 @@ def linear(x, weight, bias=None, activation="none", residual=None, preact=False,
 
 def linear_backward(dy, x, weight, z=None, activation="none", dx=True, dw=True, db=True, dw_dtype=None, workspace=None,
                     stream=None, flags=0):
-    """Gradient of ``linear`` for dy [rows, outputs]; z as linear(preact=True) returned it (not needed for activation none).
+    """Gradient of ``linear`` for dy [rows, outputs]; z as linear(preact=True) returned it (not needed for activation none).  Any of
+    x, weight and z may be a ``Packed8``: the gradient is then that of the layer on the values it stands for, in dy's type.
 
     Returns a dict with those of dx [rows, inputs], dw [outputs, inputs] and db [outputs] float32 that are asked for.
     dw_dtype is the layer's type (default) or float32, the latter for activations none and relu.  The residual's gradient
     is dy.
     """
     L = laq.load_library()
-    _check(x, "x")
-    index, dt = x.get_device(), x.dtype
+    packed = isinstance(x, Packed8) or isinstance(weight, Packed8) or isinstance(z, Packed8)
+    typed = dy if packed else x
+    _check(typed, "dy" if packed else "x")
+    index, dt = typed.get_device(), typed.dtype
     dw_dtype = dt if dw_dtype is None else dw_dtype
     if dw and dw_dtype is not dt and dw_dtype is not torch.float32:
         _refuse("dw_dtype must be %s or float32" % dt)
-    c = _layer_call(x, weight, activation, flags, index)
+    xq = wq = zq = None
+    if packed:
+        c = laq.laq_linear_call()
+        c.dtype, c.activation, c.flags = _layer_type(dt, "dy"), _activation(activation), flags
+        c.x, c.ld_x, c.M, c.K, xq = _rows_or_codes(x, "x", index, dt)
+        c.w, c.ld_w, c.N, inputs, wq = _rows_or_codes(weight, "weight", index, dt)
+        if inputs != c.K:
+            _refuse("weight must be [outputs, %d]" % c.K)
+        if c.K < 1 or c.N < 1:
+            _refuse("a layer needs inputs and outputs")
+    else:
+        c = _layer_call(x, weight, activation, flags, index)
     c.dy, c.ld_dy, _, _ = _rows(dy, "dy", index, dt, (c.M, c.N))
     if activation != "none":
         if z is None:
             _refuse("the gradient of an activation needs z")
-        c.z, c.ld_z, _, _ = _rows(z, "z", index, dt, (c.M, c.N))
+        c.z, c.ld_z, _, _, zq = _rows_or_codes(z, "z", index, dt, (c.M, c.N))
 
     def body(raw):
         c.status = _status_word(index).data_ptr()
-        dev, res = x.device, {}
+        dev, res = dy.device, {}
         if dx:
             res["dx"] = t = _table(c.M, c.K, dt, dev)
             c.dx, c.ld_dx = t.data_ptr(), c.K
@@ -393,8 +416,246 @@ def linear_backward(dy, x, weight, z=None, activation="none", dx=True, dw=True, 
         if db:
             res["db"] = t = torch.empty(c.N, dtype=torch.float32, device=dev)
             c.db = t.data_ptr()
-        ws, wp, wn = _workspace(L, c, 1, index, workspace)
-        _call(L.laq_linear_backward, C.byref(c), wp, wn, raw)
+        if packed:
+            ws, wp, wn = _workspace(L.laq_linear_blocks_workspace_bytes(C.byref(c), xq, wq, 1), index, workspace)
+            _call(L.laq_linear_blocks_backward, C.byref(c), xq, wq, zq, wp, wn, raw)
+        else:
+            ws, wp, wn = _workspace(L.laq_linear_workspace_bytes(C.byref(c), 1), index, workspace)
+            _call(L.laq_linear_backward, C.byref(c), wp, wn, raw)
         return res
 
-    return _on(index, stream, body, dy, x, weight, z, workspace)
+    return _on(index, stream, body, dy, *_tensors(x), *_tensors(weight), *_tensors(z), workspace)
+
+
+# --- 8 bits ----------------------------------------------------------------------------------------------------------
+
+class Packed8(collections.namedtuple("Packed8", ("codes", "scales"))):
+    """A matrix in 8 bits: codes [rows, cols] float8_e4m3fn (unit stride within a row) and scales float32, either
+    [rows, ceil(cols / 128)], a scale for each 128 columns of a row, or [ceil(rows / 128), ceil(cols / 128)], a scale for each
+    tile of 128 rows and 128 columns.  It stands for codes * scales."""
+    __slots__ = ()
+
+    @property
+    def shape(self):
+        return self.codes.shape
+
+
+BLOCK = 128
+
+
+def _layer_type(dtype, name):
+    if dtype is not torch.bfloat16 and dtype is not torch.float16:
+        _refuse("%s must be bfloat16 or float16" % name)
+    return DTYPES[dtype]
+
+
+def _packed(p, name, index=None, shape=None):
+    """A Packed8: (laq_blocks, rows, columns)."""
+    if not isinstance(p, Packed8):
+        _refuse("%s must be a Packed8" % name)
+    q = laq.laq_blocks()
+    q.codes, q.ld_codes, rows, cols = _rows(p.codes, name + ".codes", index, torch.float8_e4m3fn, shape)
+    q.scales, q.ld_scales, down, across = _rows(p.scales, name + ".scales", p.codes.get_device(), torch.float32)
+    if across != -(-cols // BLOCK) or (down != rows and down != -(-rows // BLOCK)):
+        _refuse("%s.scales must have shape %s or %s, not %s" % (name, (rows, -(-cols // BLOCK)), (-(-rows // BLOCK), -(-cols // BLOCK)),
+                                                               (down, across)))
+    q.block_rows = 1 if down == rows else BLOCK
+    return q, rows, cols
+
+
+def _rows_or_codes(t, name, index, dtype, shape=None):
+    """A matrix of the layer's type or a Packed8: (pointer, row stride, rows, columns, laq_blocks or None)."""
+    if isinstance(t, Packed8):
+        q, rows, cols = _packed(t, name, index, shape)
+        return None, cols, rows, cols, q
+    return *_rows(t, name, index, dtype, shape), None
+
+
+def _tensors(t):
+    return tuple(t) if isinstance(t, Packed8) else (t,)
+
+
+def _new_packed(rows, cols, tiles, device):
+    """Uninitialised; rows of codes begin 16 bytes apart or multiples of that, as the product reads them best."""
+    codes = torch.empty_strided((rows, cols), (-(-cols // 16) * 16, 1), dtype=torch.float8_e4m3fn, device=device)
+    return Packed8(codes, _table(-(-rows // BLOCK) if tiles else rows, -(-cols // BLOCK), torch.float32, device))
+
+
+def pack8(x, tiles=False, out=None, stream=None):
+    """x [rows, cols] (float32, bfloat16 or float16) in 8 bits: a ``Packed8`` with a scale for each 128 columns of a row or, with
+    tiles=True (weights), for each tile of 128 x 128.
+
+    A scale is the least power of two that brings its block's largest finite value within 448, so that a value is off by half a
+    step of its code alone: 2^-4 of it, or 2^-10 of the scale below 2^-6 of that.  NaN and infinities become NaN.  ``out`` is a
+    Packed8 to write to.
+    """
+    _check(x, "x")
+    index = x.get_device()
+    ptr, stride, rows, cols = _rows(x, "x")
+    dtype = DTYPES.get(x.dtype)
+    if dtype is None:
+        _refuse("x must be float32, bfloat16 or float16")
+    if cols < 1:
+        _refuse("x has no columns")
+
+    def body(raw):
+        p = _new_packed(rows, cols, tiles, x.device) if out is None else out
+        q, _, _ = _packed(p, "out", index, (rows, cols))
+        if rows > 1 and (q.block_rows != 1) != bool(tiles):
+            _refuse("out.scales are not those of tiles=%s" % bool(tiles))
+        _call(laq.load_library().laq_pack_blocks, ptr, dtype, rows, cols, stride, C.byref(q), raw)
+        return p
+
+    return _on(index, stream, body, x, *(out or ()))
+
+
+def unpack8(packed, dtype=torch.bfloat16, out=None, stream=None):
+    """The values of a ``Packed8`` in dtype (float32, bfloat16 or float16), rounded to the nearest; finite values beyond its
+    largest are that.  Values that ``pack8`` wrote are exact in float32 and bfloat16."""
+    q, rows, cols = _packed(packed, "packed")
+    index = packed.codes.get_device()
+    if out is not None:
+        dtype = out.dtype
+    code = DTYPES.get(dtype)
+    if code is None:
+        _refuse("dtype must be float32, bfloat16 or float16")
+    if cols < 1:
+        _refuse("packed has no columns")
+
+    def body(raw):
+        t = _table(rows, cols, dtype, packed.codes.device) if out is None else out
+        ptr, stride, _, _ = _rows(t, "out", index, dtype, (rows, cols))
+        _call(laq.load_library().laq_unpack_blocks, C.byref(q), rows, cols, ptr, code, stride, raw)
+        return t
+
+    return _on(index, stream, body, *packed, out)
+
+
+def linear8(x, weight, bias=None, activation="none", residual=None, preact=False, dtype=torch.bfloat16, out=None, workspace=None,
+            stream=None, flags=0):
+    """``linear`` on operands in 8 bits: x [rows, inputs] a ``Packed8`` with a scale for each 128 columns of a row, weight
+    [outputs, inputs] one with a scale for each tile (``pack8(w, tiles=True)``); bias, residual and results in dtype, bfloat16 or
+    float16.  Its gradient is ``linear_backward`` with the same x and weight."""
+    L = laq.load_library()
+    xq, M, K = _packed(x, "x")
+    index = x.codes.get_device()
+    wq, N, inputs = _packed(weight, "weight", index)
+    c = laq.laq_linear_call()
+    c.dtype, c.activation, c.flags = _layer_type(dtype, "dtype"), _activation(activation), flags
+    if inputs != K:
+        _refuse("weight must be [outputs, %d]" % K)
+    if K < 1 or N < 1:
+        _refuse("a layer needs inputs and outputs")
+    if M > 1 and xq.block_rows != 1:
+        _refuse("x must have a scale for each row")
+    if N > 1 and wq.block_rows != BLOCK:
+        _refuse("weight must have a scale for each tile of 128 rows")
+    c.M, c.N, c.K = M, N, K
+    c.bias = _vector(bias, "bias", index, dtype, N)
+    if residual is not None:
+        c.residual, c.ld_residual, _, _ = _rows(residual, "residual", index, dtype, (M, N))
+
+    def body(raw):
+        c.status = _status_word(index).data_ptr()
+        y = _table(M, N, dtype, x.codes.device) if out is None else out
+        c.y, c.ld_y, _, _ = _rows(y, "out", index, dtype, (M, N))
+        z = None
+        if preact:
+            z = _table(M, N, dtype, x.codes.device)
+            c.z, c.ld_z = z.data_ptr(), N
+        ws, wp, wn = _workspace(L.laq_linear_blocks_workspace_bytes(C.byref(c), xq, wq, 0), index, workspace)
+        _call(L.laq_linear_blocks_forward, C.byref(c), xq, wq, wp, wn, raw)
+        return (y, z) if preact else y
+
+    return _on(index, stream, body, *x, *weight, bias, residual, out, workspace)
+
+
+# --- the gated block -------------------------------------------------------------------------------------------------
+
+def _gated_call(weight, M, K, activation, flags, index, dtype):
+    c = laq.laq_gated_call()
+    c.dtype, c.activation, c.flags = _layer_type(dtype, "x"), _activation(activation), flags
+    c.w, c.ld_w, rows, inputs = _rows(weight, "weight", index, dtype)
+    if inputs != K or rows % 2:
+        _refuse("weight must be [2 gates, %d]" % K)
+    if K < 1 or rows < 2:
+        _refuse("a block needs inputs and gates")
+    c.M, c.F, c.K = M, rows // 2, K
+    return c
+
+
+def gated(x, weight, bias=None, activation="silu", preact=False, out=None, workspace=None, stream=None, flags=0):
+    """act(g) * u for the two halves g and u [rows, gates] of z = x weight^T + bias: x [rows, inputs], weight [2 gates, inputs] (the
+    gates' rows first), bias [2 gates], all bfloat16 or all float16; at most 65536 inputs.
+
+    Returns h [rows, gates], or (h, z) for preact=True, z [rows, 2 gates], and for preact="packed", z in 8 bits, which is
+    ``pack8`` of the former.  ``gated_backward`` takes either.
+    """
+    L = laq.load_library()
+    _check(x, "x")
+    index, dt = x.get_device(), x.dtype
+    ptr, ld, M, K = _rows(x, "x")
+    c = _gated_call(weight, M, K, activation, flags, index, dt)
+    c.x, c.ld_x = ptr, ld
+    N = 2 * c.F
+    c.bias = _vector(bias, "bias", index, dt, N)
+    if preact not in (False, True, "packed"):
+        _refuse("preact must be False, True or \"packed\"")
+
+    def body(raw):
+        c.status = _status_word(index).data_ptr()
+        h = _table(M, c.F, dt, x.device) if out is None else out
+        c.h, c.ld_h, _, _ = _rows(h, "out", index, dt, (M, c.F))
+        z = q = None
+        if preact == "packed":
+            z = _new_packed(M, N, False, x.device)
+            q, _, _ = _packed(z, "z")
+            q.block_rows = 1
+            c.z_blocks = C.pointer(q)
+        elif preact:
+            z = _table(M, N, dt, x.device)
+            c.z, c.ld_z = z.data_ptr(), N
+        ws, wp, wn = _workspace(L.laq_gated_workspace_bytes(C.byref(c), 0), index, workspace)
+        _call(L.laq_gated_forward, C.byref(c), wp, wn, raw)
+        return (h, z) if preact else h
+
+    return _on(index, stream, body, x, weight, bias, out, workspace)
+
+
+def gated_backward(dh, x, weight, z, activation="silu", dx=True, dw=True, db=True, workspace=None, stream=None, flags=0):
+    """Gradient of ``gated`` for dh [rows, gates]; z as gated(preact=True) or gated(preact="packed") returned it, x as it was or
+    packed (``pack8``).
+
+    Returns a dict with those of dx [rows, inputs], dw [2 gates, inputs] and db [2 gates] float32 that are asked for.
+    """
+    L = laq.load_library()
+    _check(dh, "dh")
+    index, dt = dh.get_device(), dh.dtype
+    ptr, ld, M, K, xq = _rows_or_codes(x, "x", index, dt)
+    c = _gated_call(weight, M, K, activation, flags, index, dt)
+    c.x, c.ld_x = ptr, ld
+    N = 2 * c.F
+    c.dh, c.ld_dh, _, _ = _rows(dh, "dh", index, dt, (M, c.F))
+    c.z, c.ld_z, _, _, zq = _rows_or_codes(z, "z", index, dt, (M, N))
+    if xq is not None:
+        c.x_blocks = C.pointer(xq)
+    if zq is not None:
+        c.z_blocks = C.pointer(zq)
+
+    def body(raw):
+        c.status = _status_word(index).data_ptr()
+        dev, res = dh.device, {}
+        if dx:
+            res["dx"] = t = _table(M, K, dt, dev)
+            c.dx, c.ld_dx = t.data_ptr(), K
+        if dw:
+            res["dw"] = t = _table(N, K, dt, dev)
+            c.dw, c.ld_dw = t.data_ptr(), K
+        if db:
+            res["db"] = t = torch.empty(N, dtype=torch.float32, device=dev)
+            c.db = t.data_ptr()
+        ws, wp, wn = _workspace(L.laq_gated_workspace_bytes(C.byref(c), 1), index, workspace)
+        _call(L.laq_gated_backward, C.byref(c), wp, wn, raw)
+        return res
+
+    return _on(index, stream, body, dh, *_tensors(x), weight, *_tensors(z), workspace)
