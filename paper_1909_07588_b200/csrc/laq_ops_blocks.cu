@@ -324,6 +324,354 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
   }
 }
 
+// ---- the product of two matrices of codes ----------------------------------------------------------------------------------
+// A tile of 128 rows (256 on a pair of SMs) and NT columns.  The tensor cores add up one block of 128 at a time, into two accumulators
+// by turns, and sixteen warps add its sums, times the block's scales, to their own: one fused multiply-add of two numbers for two
+// elements, since a row's scale and a column tile's are one number for a thread's NT / 4 columns of its row.  The sums take up to 64
+// registers of a thread; the first four warps (a loader, the tensor cores' and two that bring the scales) leave theirs to them:
+// 128 x 32 + 512 x 112 of the block's 640 x 96.  The scales come through shared memory, eight blocks at a time: a load of one block's
+// scale by each lane touches 32 sectors, and the adding warps' own had cost a third of the time.
+constexpr int kAdders = 16, kFirstAdder = 4, kCodesThreads = 32 * (kFirstAdder + kAdders), kFewRegisters = 32, kManyRegisters = 112;
+constexpr int kScaleGroup = 8;                                        // blocks whose scales come together
+constexpr int kScaleFloats = kScaleGroup * (kTileM + 2);              // a group's: of 128 rows and of two column tiles
+constexpr int kCodesStaging = kAdders * 2048 + 2 * kScaleFloats * 4;
+
+__device__ __forceinline__ void mma_codes_pair(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n"
+      ".reg .pred p;\n"
+      "setp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n"
+      "}\n" ::"r"(d_tmem),
+      "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+// Without a fence over the thread's other memory accesses: what is handed back has been read from tensor memory, which wait::ld and
+// fence::before_thread_sync order.  (With one, 8192 x 4096 x 4096 took half as long again.)
+__device__ __forceinline__ void arrive_lightly(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+
+// 32 rows of four 16-byte pieces in shared memory, permuted so that a warp writes 32 rows and reads along rows without bank conflicts.
+__device__ __forceinline__ int narrow_piece(int row, int p) { return row * 4 + (p ^ ((row >> 1) & 3)); }
+
+template <class T, bool PAIR, int NT>
+__global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                                                                      const GemmArgs A) {
+  extern __shared__ unsigned char codes_smem_raw[];
+  __shared__ uint64_t bars[2 * kMaxStages + 9];
+  __shared__ uint32_t tmem_base_sh;
+  __shared__ int abort_sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, stages = A.stages, nkb = A.nkb;
+  const uint32_t base = umma::smem_u32(codes_smem_raw), smem0 = (base + 1023u) & ~1023u;
+  constexpr int b_rows = PAIR ? NT / 2 : NT;
+  constexpr uint32_t a_bytes = kTileM * kBlock, st_bytes = a_bytes + b_rows * kBlock;
+  constexpr uint32_t held_cols = 2 * NT;
+  const int half = PAIR ? (int)(blockIdx.x & 1u) : 0;
+  const uint32_t full0 = umma::smem_u32(&bars[0]), empty0 = umma::smem_u32(&bars[kMaxStages]);
+  const uint32_t acc_full0 = umma::smem_u32(&bars[2 * kMaxStages]), acc_empty0 = acc_full0 + 16, drain = acc_full0 + 32;
+  const uint32_t scales_full0 = drain + 8, scales_empty0 = drain + 24;
+  float* const staged = reinterpret_cast<float*>(codes_smem_raw + (smem0 - base) + stages * st_bytes + kAdders * 2048);     // two groups' scales
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      umma::mbar_init(full0 + 8 * s, 1);
+      umma::mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      umma::mbar_init(acc_full0 + 8 * b, 1);
+      umma::mbar_init(acc_empty0 + 8 * b, PAIR ? 2 * kAdders : kAdders);
+      umma::mbar_init(scales_full0 + 8 * b, 2);
+      umma::mbar_init(scales_empty0 + 8 * b, kAdders);
+    }
+    umma::mbar_init(drain, 1);
+    abort_sh = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(umma::smem_u32(&tmem_base_sh)), "r"(held_cols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(umma::smem_u32(&tmem_base_sh)), "r"(held_cols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  if (PAIR) cg::this_cluster().sync();             // both blocks' barriers are there before either signals the other's
+  else __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = tmem_base_sh;
+  allow_next();
+  await_previous();
+
+  const int tiles = A.tiles_i * A.tiles_j;
+  const int first = (int)blockIdx.x / (PAIR ? 2 : 1), step = (int)gridDim.x / (PAIR ? 2 : 1);
+  const bool starved = A.starve && blockIdx.x == 0;
+  const uint32_t limit = A.starve ? kStarvedLimit : umma::kWaitLimit;
+  volatile int* abort_flag = &abort_sh;
+
+  if (warp < kFirstAdder) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+    if (warp == 0) {
+      if (elect_one()) {
+        int n = 0;                       // stages handed out so far
+        bool ok = !starved;
+        for (int w = first; w < tiles && ok; w += step) {
+          int i0, j0;
+          tile_of<PAIR>(A, w, i0, j0);
+          i0 += half * kTileM;
+          j0 += half * b_rows;
+          for (int kb = 0; kb < nkb; ++kb, ++n) {
+            const int s = n % stages;
+            ok = umma::mbar_wait_abortable(empty0 + 8 * s, ((uint32_t)(n / stages) & 1u) ^ 1u, limit, abort_flag, A.status, 1u);
+            if (!ok) break;
+            const uint32_t sa = smem0 + s * st_bytes, sb = sa + a_bytes;
+            const int r = kb * kBlock;
+            if (PAIR) {
+              // the pair's first block counts the bytes of both; its phase cannot end before its own arrival here
+              if (half == 0) umma::mbar_expect_tx(full0 + 8 * s, 2 * st_bytes);
+              const uint32_t bar = of_leader(full0 + 8 * s);
+              tma_load_2d_pair(sa, &tmA, bar, r, i0);
+              tma_load_2d_pair(sb, &tmB, bar, r, j0);
+            } else {
+              const uint32_t bar = full0 + 8 * s;
+              umma::mbar_expect_tx(bar, st_bytes);
+              umma::tma_load_2d(sa, &tmA, bar, r, i0);
+              umma::tma_load_2d(sb, &tmB, bar, r, j0);
+            }
+          }
+        }
+        if (!ok && PAIR) {              // given up: as in linear_gemm_kernel
+          for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+        } else if (!ok) {
+          for (int m = n > stages ? n - stages : 0; m < n; ++m)
+            for (uint32_t it = 0; it < umma::kWaitLimit && !umma::mbar_try_wait(full0 + 8 * (m % stages), (uint32_t)(m / stages) & 1u); ++it) {
+            }
+        }
+      }
+    } else if (warp == 1 && half == 0) {      // the pair's first block issues the products of both
+      if (elect_one()) {
+        const uint32_t idesc = instr_desc(0, 0, 0, NT, PAIR ? 2 * kTileM : kTileM);
+        int n = 0;
+        bool ok = true;
+        for (int w = first; w < tiles && ok; w += step) {
+          for (int kb = 0; kb < nkb; ++kb, ++n) {
+            const int b = n & 1, s = n % stages;
+            ok = umma::mbar_wait_abortable(full0 + 8 * s, (uint32_t)(n / stages) & 1u, limit, abort_flag, A.status, 4u) &&
+                 umma::mbar_wait_abortable(acc_empty0 + 8 * b, ((uint32_t)(n >> 1) & 1u) ^ 1u, limit, abort_flag, A.status, 2u);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t sa = smem0 + s * st_bytes, d = tmem_base + (uint32_t)b * NT;
+            const uint64_t da = desc_k_major(sa), db = desc_k_major(sa + a_bytes);
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {          // 32 codes are 32 bytes: two units of a descriptor's address
+              if (PAIR) mma_codes_pair(d, da + 2 * kk, db + 2 * kk, idesc, kk != 0);
+              else mma_codes(d, da + 2 * kk, db + 2 * kk, idesc, kk != 0);
+            }
+            if (PAIR) {
+              commit_pair(acc_full0 + 8 * b);
+              commit_pair(empty0 + 8 * s);
+            } else {
+              umma::mma_commit(acc_full0 + 8 * b);
+              umma::mma_commit(empty0 + 8 * s);
+            }
+          }
+        }
+        if (!ok) {                      // products under way still read the ring and write tensor memory
+          if (PAIR) commit_pair(drain);
+          else umma::mma_commit(drain);
+          for (uint32_t i = 0; i < umma::kWaitLimit && !umma::mbar_try_wait(drain, 0u); ++i) {
+          }
+        }
+      }
+    }
+    if (warp >= 2) {                    // scales of 64 rows each, and (the first) of the column tiles
+      const bool vec = ((uintptr_t)A.sx & 15u) == 0 && A.ldsx % 4 == 0;
+      int g = 0;
+      bool ok = true;
+      for (int w = first; w < tiles && ok; w += step) {
+        int i0, j0;
+        tile_of<PAIR>(A, w, i0, j0);
+        i0 += half * kTileM;
+        for (int k0 = 0; k0 < nkb; k0 += kScaleGroup, ++g) {
+          const int b = g & 1, n = min(kScaleGroup, nkb - k0);
+          ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(scales_empty0 + 8 * b, ((uint32_t)(g >> 1) & 1u) ^ 1u, limit, abort_flag, A.status, 16u));
+          if (!ok) break;
+          float* to = staged + b * kScaleFloats;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const int r = (warp - 2) * 64 + 32 * h + lane;
+            const float* p = A.sx + (long long)min(i0 + r, A.I - 1) * A.ldsx + k0;
+            if (vec && n == kScaleGroup) {
+              const float4 lo = __ldg(reinterpret_cast<const float4*>(p)), hi = __ldg(reinterpret_cast<const float4*>(p) + 1);
+              to[r] = lo.x, to[kTileM + r] = lo.y, to[2 * kTileM + r] = lo.z, to[3 * kTileM + r] = lo.w;
+              to[4 * kTileM + r] = hi.x, to[5 * kTileM + r] = hi.y, to[6 * kTileM + r] = hi.z, to[7 * kTileM + r] = hi.w;
+            } else {
+              for (int k = 0; k < n; ++k) to[k * kTileM + r] = __ldg(p + k);
+            }
+          }
+          if (warp == 2 && lane < 2 * kScaleGroup && lane % kScaleGroup < n)
+            to[kScaleGroup * kTileM + lane] =
+                __ldg(A.sw + (long long)(min(j0 + lane / kScaleGroup * (NT / 2), A.J - 1) / kBlock) * A.ldsw + k0 + lane % kScaleGroup);
+          __syncwarp();
+          if (lane == 0) umma::mbar_arrive(scales_full0 + 8 * b);
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
+    constexpr int kCols = NT / 4, kPieces = kCols / 16;          // of this thread's row
+    const int q = warp & 3, c_first = (warp - kFirstAdder) / 4 * kCols;
+    const uint32_t mine = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)c_first;
+    const uint32_t back0 = PAIR ? of_leader(acc_empty0) : acc_empty0;
+    uint4* stage4 = reinterpret_cast<uint4*>(codes_smem_raw + (smem0 - base) + stages * st_bytes) + (warp - kFirstAdder) * 128;      // 2 KB
+    const float* my_scale = staged + q * 32 + lane;
+    const float* tile_scale = staged + kScaleGroup * kTileM + (c_first >= NT / 2 ? kScaleGroup : 0);
+    int n = 0, g = 0;
+    bool ok = true;
+    for (int w = first; w < tiles && ok; w += step) {
+      f32x2 sum[kPieces][8];
+#pragma unroll
+      for (int p = 0; p < kPieces; ++p)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum[p][e] = 0ull;
+      for (int kb = 0; kb < nkb; ++kb, ++n) {
+        const int in = kb % kScaleGroup, at = (g & 1) * kScaleFloats;
+        if (in == 0) {
+          ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(scales_full0 + 8 * (g & 1), (uint32_t)(g >> 1) & 1u, limit, abort_flag, A.status, 16u));
+          if (!ok) break;
+        }
+        const float scale = my_scale[at + in * kTileM] * tile_scale[at + in];
+        const f32x2 both = pair_of(scale, scale);
+        const uint32_t b = (uint32_t)n & 1u;
+        ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(n >> 1) & 1u, limit, abort_flag, A.status, 8u));
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (in == kScaleGroup - 1 || kb == nkb - 1) {        // the group's scales have been read (the scale above, before the barrier's wait)
+          __syncwarp();
+          if (lane == 0) umma::mbar_arrive(scales_empty0 + 8 * (g & 1));
+          ++g;
+        }
+        const uint32_t t0 = mine + b * NT;
+#pragma unroll
+        for (int p = 0; p < kPieces; p += 2) {
+          if (kPieces == 1) {
+            uint32_t v[16];
+            tmem_load(t0, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[0][e] = fma2(pair_of(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), both, sum[0][e]);
+          } else {
+            uint32_t v[32];
+            tmem_load(t0 + 16 * p, v);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              f32x2& to = sum[kPieces == 1 ? 0 : p + e / 8][e % 8];
+              to = fma2(pair_of(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), both, to);
+            }
+          }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) arrive_lightly(back0 + 8 * b);
+          else umma::mbar_arrive(back0 + 8 * b);
+        }
+      }
+      if (!ok) break;
+      int i0, j0;
+      tile_of<PAIR>(A, w, i0, j0);
+      i0 += half * kTileM + q * 32;
+      j0 += c_first;
+      const bool vec = all_vectors(A, false), whole = vec && i0 + 32 <= A.I && j0 + kCols <= A.J;
+      // pieces of 32 x 16 through shared memory, after which two lanes share a row
+      const long long row0 = i0 + (lane >> 1);
+      int col = j0 + 8 * (lane & 1);
+      uint4 next[2];                       // the residual of the piece after this one
+      const auto ahead = [&](int c) {
+        const T* rp = reinterpret_cast<const T*>(A.residual) + row0 * A.ldr + c;
+        next[0] = load16(rp);
+        next[1] = load16(rp + 16 * A.ldr);
+      };
+      if (whole && A.residual) ahead(col);
+#pragma unroll 1
+      for (int p = 0; p < kPieces; ++p, col += 16) {
+        const uint4 res[2] = {next[0], next[1]};
+        uint4 bias = make_uint4(0u, 0u, 0u, 0u);
+        if (whole) {
+          if (A.residual && p + 1 < kPieces) ahead(col + 16);
+          if (A.bias) bias = __ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + col));
+        }
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+          float x0, x1, x2, x3;
+          ops::split(sum[0][e], x0, x1);
+          ops::split(sum[0][e + 1], x2, x3);
+          stage4[narrow_piece(lane, e / 2)] = make_uint4(__float_as_uint(x0), __float_as_uint(x1), __float_as_uint(x2), __float_as_uint(x3));
+        }
+        // the next piece moves up: no register can be chosen by a number that is only known at run time
+#pragma unroll
+        for (int m = 0; m + 1 < kPieces; ++m)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sum[m][e] = sum[m + 1][e];
+        __syncwarp();
+        if (whole) {
+          float b[8];
+          Elem<T>::unpack(bias, b);
+#pragma unroll
+          for (int k = 0; k < 2; ++k) {
+            const int r = 16 * k + (lane >> 1);
+            const uint4 lo = stage4[narrow_piece(r, 2 * (lane & 1))], hi = stage4[narrow_piece(r, 2 * (lane & 1) + 1)];
+            float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                          __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += b[e];
+            if (A.z) *reinterpret_cast<uint4*>(reinterpret_cast<T*>(A.z) + (row0 + 16 * k) * A.ldz + col) = Elem<T>::pack(x);
+            activate(x, A.act);
+            if (A.residual) {
+              float y[8];
+              Elem<T>::unpack(res[k], y);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] += y[e];
+            }
+            *reinterpret_cast<uint4*>(reinterpret_cast<T*>(A.out) + (row0 + 16 * k) * A.ldo + col) = Elem<T>::pack(x);
+          }
+          continue;
+        }
+#pragma unroll 1
+        for (int k = 0; k < 2; ++k) {
+          float x[8];
+          if (vec) {
+            const int r = 16 * k + (lane >> 1);
+            const uint4 lo = stage4[narrow_piece(r, 2 * (lane & 1))], hi = stage4[narrow_piece(r, 2 * (lane & 1) + 1)];
+            x[0] = __uint_as_float(lo.x), x[1] = __uint_as_float(lo.y), x[2] = __uint_as_float(lo.z), x[3] = __uint_as_float(lo.w);
+            x[4] = __uint_as_float(hi.x), x[5] = __uint_as_float(hi.y), x[6] = __uint_as_float(hi.z), x[7] = __uint_as_float(hi.w);
+            finish_row<T, false>(A, i0 + r, col, x, residual8<T>(A, i0 + r, col, vec));
+          } else {                         // half a warp has 8 rows of 16 columns
+            const int r = 16 * k + 8 * (lane >> 4), c = lane & 15;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(reinterpret_cast<const uint32_t*>(&stage4[narrow_piece(r + e, c >> 2)])[c & 3]);
+            finish_column<T, false>(A, A.I, A.J, i0 + r, j0 + 16 * p + c, x);
+          }
+        }
+      }
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  if (PAIR) {
+    __syncwarp();
+    cg::this_cluster().sync();                     // neither block's memory is used by the other any more
+  } else {
+    __syncthreads();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(held_cols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(held_cols) : "memory");
+  }
+}
+
 // Codes that a tensor map cannot describe are copied with a pitch of a multiple of 16 bytes.
 __global__ void __launch_bounds__(256) copy_codes_kernel(const uint8_t* src, long long ld, uint8_t* dst, long long pitch, long long rows, long long cols) {
   allow_next();
@@ -397,8 +745,9 @@ void list_block_kernels(const void** list, int& n) {
 }
 template <class T>
 void list_product_kernels(const void** list, int& n) {
-  const void* all[] = {(const void*)linear_gemm_kernel<T, false, false, false, false, kCodes>, (const void*)linear_gemm_kernel<T, true, false, false, false, kCodes>,
-                       (const void*)linear_gemm_kernel<T, false, true, false, false, kCodes>,  (const void*)linear_few_codes_kernel<T, 1>,
+  const void* all[] = {(const void*)linear_gemm_kernel<T, true, false, false, false, kCodes>, (const void*)codes_gemm_kernel<T, true, 256>,
+                       (const void*)codes_gemm_kernel<T, true, 128>, (const void*)codes_gemm_kernel<T, false, 128>,
+                       (const void*)codes_gemm_kernel<T, false, 64>, (const void*)linear_few_codes_kernel<T, 1>,
                        (const void*)linear_few_codes_kernel<T, 2>, (const void*)linear_few_codes_kernel<T, 3>, (const void*)linear_few_codes_kernel<T, 4>};
   for (const void* k : all) list[n++] = k;
 }
@@ -407,6 +756,18 @@ laq_status check_matrix(const Err& e, int64_t rows, int64_t cols) {
   const int64_t most = 0x7fffff00ll;
   if (rows < 0 || rows > most || cols < 1 || cols > most) return fail(e.buf, e.len, LAQ_EINVAL, "rows must be 0..2^31-256, cols 1..2^31-256");
   return LAQ_OK;
+}
+
+template <class T, bool PAIR, int NT>
+laq_status launch_codes(const Err& e, const Product& p, bool follows, cudaStream_t st) {
+  static Raised raised;
+  return launch_tiles(e, codes_gemm_kernel<T, PAIR, NT>, raised, kCodesThreads, PAIR, false, kCodesStaging, p.ma, p.mb, p.A, follows, st);
+}
+template <class T>
+laq_status launch_product(const Err& e, const Product& p, bool follows, cudaStream_t st) {
+  if (p.pl.swap) return launch_gemm<T, true, false, false, false, kCodes>(e, p.ma, p.mb, p.A, follows, st);
+  if (p.pl.pair) return p.pl.nt == 256 ? launch_codes<T, true, 256>(e, p, follows, st) : launch_codes<T, true, 128>(e, p, follows, st);
+  return p.pl.nt == 128 ? launch_codes<T, false, 128>(e, p, follows, st) : launch_codes<T, false, 64>(e, p, follows, st);
 }
 
 bool takes_few_codes(const laq_linear_call* c) { return !(c->flags & LAQ_LINEAR_STARVE) && c->M <= kFewRows; }
@@ -543,7 +904,10 @@ extern "C" laq_status laq_linear_blocks_forward(const laq_linear_call* c, const 
   LAQ_TRY(make_codes_mappable(e, x, ws, st));
   LAQ_TRY(make_codes_mappable(e, w, ws, st));
   const bool follows = ws != d_workspace;
-  return c->dtype == LAQ_BF16 ? product_in_mode<__nv_bfloat16, kCodes>(e, A, x, w, 0, follows, st) : product_in_mode<__half, kCodes>(e, A, x, w, 0, follows, st);
+  Product p;
+  p.A = A;
+  LAQ_TRY(prepare_product(e, kCodes, p, x, w, 0));
+  return c->dtype == LAQ_BF16 ? launch_product<__nv_bfloat16>(e, p, follows, st) : launch_product<__half>(e, p, follows, st);
 }
 
 namespace laq {

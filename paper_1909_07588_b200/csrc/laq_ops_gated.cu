@@ -204,6 +204,13 @@ laq_status few_rows(const Err& e, const GemmArgs& A, const Operand& x, const Ope
 }
 
 template <class T>
+laq_status launch_product(const Err& e, const Product& p, bool follows, cudaStream_t st) {
+  if (p.pl.pair) return launch_gemm<T, false, true, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st);
+  return p.pl.swap ? launch_gemm<T, true, false, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st)
+                   : launch_gemm<T, false, false, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st);
+}
+
+template <class T>
 void list_kernels(const void** list, int& n) {
   const void* all[] = {(const void*)linear_gemm_kernel<T, false, false, false, false, kGated>, (const void*)linear_gemm_kernel<T, true, false, false, false, kGated>,
                        (const void*)linear_gemm_kernel<T, false, true, false, false, kGated>,
@@ -287,8 +294,10 @@ extern "C" laq_status laq_gated_forward(const laq_gated_call* c, void* d_workspa
     LAQ_TRY(make_mappable(e, need.x, ws, st));
     LAQ_TRY(make_mappable(e, need.w, ws, st));
     const bool follows = ws != before;
-    LAQ_TRY(bf16 ? product_in_mode<__nv_bfloat16, kGated>(e, A, need.x, need.w, 1, follows, st)
-                 : product_in_mode<__half, kGated>(e, A, need.x, need.w, 0, follows, st));
+    Product p;
+    p.A = A;
+    LAQ_TRY(prepare_product(e, kGated, p, need.x, need.w, bf16 ? 1 : 0));
+    LAQ_TRY(bf16 ? launch_product<__nv_bfloat16>(e, p, follows, st) : launch_product<__half>(e, p, follows, st));
   }
   if (c->z_blocks) return pack_blocks(e, A.z, c->dtype, c->M, N, A.ldz, *c->z_blocks, st);
   return LAQ_OK;

@@ -61,6 +61,7 @@ enum Mode {
   kGated,       // 16-bit operands, B's rows are gates and then as many ups: a tile holds nt / 2 columns of each
   kCodes        // 8-bit operands with a scale for each block of 128 of the summed axis
 };
+constexpr int kScaleTable = 8 * 64;       // kCodes: scales that an epilogue warp has at hand
 constexpr int kBlock = 128;               // columns (and, of weights, rows) that share a scale of 8-bit codes
 
 struct GemmArgs {
@@ -170,23 +171,13 @@ __device__ __forceinline__ void mma_pair(uint32_t d_tmem, uint64_t da, uint64_t 
       "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// the same on 8-bit codes (e4m3, 32 of the summed axis an instruction), for one block and for a pair
+// 8-bit codes (e4m3, 32 of the summed axis an instruction), for one block
 __device__ __forceinline__ void mma_codes(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
       "{\n"
       ".reg .pred p;\n"
       "setp.ne.b32 p, %4, 0;\n"
       "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n"
-      "}\n" ::"r"(d_tmem),
-      "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
-      : "memory");
-}
-__device__ __forceinline__ void mma_codes_pair(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
-  asm volatile(
-      "{\n"
-      ".reg .pred p;\n"
-      "setp.ne.b32 p, %4, 0;\n"
-      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n"
       "}\n" ::"r"(d_tmem),
       "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
       : "memory");
@@ -199,7 +190,6 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {         // arrives a
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-
 // gelu is the tanh form: 0.5 z (1 + tanh u) = z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
 constexpr float kGeluC = 0.7978845608028654f, kGeluA = 0.044715f;
 __device__ __forceinline__ float sigmoid(float x) {       // 0 and 1 for far x: 2^128 is +inf and its reciprocal 0
@@ -234,6 +224,12 @@ __device__ __forceinline__ void gelu_both(float z, float& value, float& slope) {
   const float s = sigmoid(2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
   value = z * s;
   slope = fmaf(value * (1.f - s), fmaf(6.f * kGeluC * kGeluA, fminf(z * z, 400.f), 2.f * kGeluC), s);
+}
+
+__device__ __forceinline__ float load_scale(const float* p) {      // where it stands, and not later
+  float v;
+  asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
+  return v;
 }
 
 // Eight rows row0.. of column `col` of out (rows x cols): the form for transposed tiles and for tensors that allow no
@@ -382,8 +378,8 @@ __device__ __forceinline__ void tile_of(const GemmArgs& A, int w, int& i0, int& 
   j0 = (in / rows) * A.nt;
 }
 
-// kCodes: the tensor cores add up one block of 128, and the epilogue's threads add it, times its two scales, to sums in their
-// registers (a fused multiply-add each) while the next block is under way.
+// kCodes (few rows of X, so transposed tiles alone): the tensor cores add up one block of 128, and the epilogue's threads add it, times
+// its two scales, to sums in their registers while the next block is under way.
 template <class T, bool TRANS, bool PAIR, bool OUT32, bool LONG, int MODE = kPlain>
 __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                                       const __grid_constant__ CUtensorMap tmB,
@@ -397,6 +393,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
   uint4* ring4 = reinterpret_cast<uint4*>(gemm_smem_raw + (smem0 - base));        // a split tile, once the ring is idle
   static_assert(!(OUT32 && (LONG || TRANS)), "fp32 results have chunks of their own, and their epilogue writes rows");
   static_assert(MODE == kPlain || !(OUT32 || LONG), "the other modes have 16-bit results and no long sums");
+  static_assert(MODE != kCodes || (TRANS && !PAIR), "8-bit tiles that are not transposed have a kernel of their own");
   constexpr int kChunk = MODE == kCodes ? 1 : OUT32 ? kChunk32 : LONG ? kChunkLong : 1 << 30;      // k-blocks that the tensor core adds up
   constexpr bool kSummed = OUT32 || MODE == kCodes;           // the epilogue's registers hold the sum of the chunks
   constexpr int kStageCols = MODE == kCodes ? kBlock : kBlockK;           // of the summed axis in a stage: 128 bytes
@@ -546,10 +543,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
 #pragma unroll
             for (int kk = 0; kk < kBlockK / 16; ++kk) {          // 32 bytes of the summed axis: 16 values, or 32 codes
               const uint32_t more = kb != k0 || kk != 0 ? 1u : 0u;
-              if (MODE == kCodes) {
-                if (PAIR) mma_codes_pair(d, da + kk * step_a, db + kk * step_b, idesc, more);
-                else mma_codes(d, da + kk * step_a, db + kk * step_b, idesc, more);
-              } else if (PAIR) mma_pair(d, da + kk * step_a, db + kk * step_b, idesc, more);
+              if (MODE == kCodes) mma_codes(d, da + kk * step_a, db + kk * step_b, idesc, more);
+              else if (PAIR) mma_pair(d, da + kk * step_a, db + kk * step_b, idesc, more);
               else umma::mma_bf16_ss(d, da + kk * step_a, db + kk * step_b, idesc, more);
             }
             if (PAIR) commit_pair(empty0 + 8 * s);
@@ -610,44 +605,57 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
         }
         ++it;
       };
-      constexpr int kSums = OUT32 ? 2 : MODE == kCodes ? 4 : 1, kWide = MODE == kCodes && TRANS ? 16 : 32;
+      constexpr int kSums = OUT32 ? 2 : MODE == kCodes ? 4 : 1, kWide = MODE == kCodes ? 16 : 32;
       float sum[kSums][kWide];                         // the chunks' sums, this lane's row
       if constexpr (MODE == kCodes) {
 #pragma unroll
         for (int p = 0; p < kSums; ++p)
 #pragma unroll
           for (int e = 0; e < kWide; ++e) sum[p][e] = 0.f;
-        // This lane's scale of X (of the columns' rows in a transposed tile, a lane has one of each group of 16) and the
-        // groups' scales of W, read one block ahead.
-        float mine[TRANS ? kSums : 1], theirs[TRANS ? 1 : kSums];
-        const auto scales_of = [&](int k) {
-          const long long kb = kb0 + k;
-          if constexpr (TRANS) {
-            theirs[0] = __ldg(A.sw + (long long)(i0 / kBlock) * A.ldsw + kb);
+        // The scales of eight blocks of 128 at a time, of this warp's columns (rows of X) times those of W's tile: read while the eight
+        // before are added, put down in shared memory, and taken from there by all lanes.  (One block's read ahead by its lanes and
+        // handed round by shuffles: 128 x 4096 x 4096 in tiles of 64 rows of X and halves of the sum 20.7 us, so 17.9.)
+        float* table = reinterpret_cast<float*>(ring4 + (size_t)stages * st_bytes / 16) + (warp - 2) * kScaleTable;
+        float of_x[kSums][4], of_w;
+        const int at = (lane & 1) * 4;                 // a lane has four blocks' of one column of each 16
+        const auto read_scales = [&](int k0) {
+          of_w = lane < 8 && k0 + lane < nkb ? load_scale(A.sw + (long long)(i0 / kBlock) * A.ldsw + kb0 + k0 + lane) : 0.f;
 #pragma unroll
-            for (int p = 0; p < kSums; ++p) mine[p] = __ldg(A.sx + (long long)min(j0 + 16 * set + 32 * p + (lane & 15), A.J - 1) * A.ldsx + kb);
-          } else {
-            mine[0] = __ldg(A.sx + (long long)min(i0 + row, A.I - 1) * A.ldsx + kb);
+          for (int p = 0; p < kSums; ++p) {
+            const float* from = A.sx + (long long)min(j0 + 16 * set + 32 * p + (lane >> 1), A.J - 1) * A.ldsx + kb0 + k0 + at;
 #pragma unroll
-            for (int p = 0; p < kSums; ++p) theirs[p] = __ldg(A.sw + (long long)(min(j0 + 32 * set + 64 * p, A.J - 1) / kBlock) * A.ldsw + kb);
+            for (int k = 0; k < 4; ++k) of_x[p][k] = 16 * set + 32 * p < nt && k0 + at + k < nkb ? load_scale(from + k) : 0.f;
           }
         };
-        scales_of(0);
+        read_scales(0);
         for (int k0 = 0; k0 < nkb; ++k0) {
-          float s[kSums];
+          if (k0 % 8 == 0) {
+            __syncwarp();
 #pragma unroll
-          for (int p = 0; p < kSums; ++p) s[p] = mine[TRANS ? p : 0] * theirs[TRANS ? 0 : p];
+            for (int k = 0; k < 4; ++k) {
+              const float w8 = __shfl_sync(0xffffffffu, of_w, at + k);
+#pragma unroll
+              for (int p = 0; p < kSums; ++p) table[(at + k) * 64 + 16 * p + (lane >> 1)] = of_x[p][k] * w8;
+            }
+            __syncwarp();
+            if (k0 + 8 < nkb) read_scales(k0 + 8);
+          }
           acquire();
           if (!ok) break;
-          if (k0 + 1 < nkb) scales_of(k0 + 1);
 #pragma unroll
           for (int p = 0; p < kSums; ++p)
-            if (kWide * set + 2 * kWide * p < nt) {
+            if (16 * set + 32 * p < nt) {
               uint32_t v[kWide];
-              tmem_load(t0 + (uint32_t)(kWide * set + 2 * kWide * p), v);
+              tmem_load(t0 + (uint32_t)(16 * set + 32 * p), v);
+              const float4* s4 = reinterpret_cast<const float4*>(table + (k0 % 8) * 64 + 16 * p);
 #pragma unroll
-              for (int e = 0; e < kWide; ++e)
-                sum[p][e] = fmaf(__uint_as_float(v[e]), TRANS ? __shfl_sync(0xffffffffu, s[p], e) : s[p], sum[p][e]);
+              for (int e = 0; e < kWide; e += 4) {
+                const float4 f = s4[e / 4];
+                sum[p][e] = fmaf(__uint_as_float(v[e]), f.x, sum[p][e]);
+                sum[p][e + 1] = fmaf(__uint_as_float(v[e + 1]), f.y, sum[p][e + 1]);
+                sum[p][e + 2] = fmaf(__uint_as_float(v[e + 2]), f.z, sum[p][e + 2]);
+                sum[p][e + 3] = fmaf(__uint_as_float(v[e + 3]), f.w, sum[p][e + 3]);
+              }
             }
           release();
         }
@@ -705,7 +713,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       // the values from column c0 on of this lane's row: the accumulator's, and the sum of the chunks before it
       auto loaded = [&](int c0, auto& v) {
         if constexpr (MODE == kCodes) {
-          const int p = c0 / (2 * kWide);
+          const int p = c0 / (2 * kWide);          // chosen so that the sums stay in registers
 #pragma unroll
           for (int e = 0; e < kWide && e < (int)(sizeof(v) / 4); ++e)
             v[e] = __float_as_uint(p == 0 ? sum[0][e] : p == 1 ? sum[1][e] : p == 2 ? sum[2][e] : sum[3][e]);
@@ -730,6 +738,15 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           loaded(c0, v);
         }
       };
+      // ... through shared memory
+      auto hand_over = [&](int c0) {
+        uint32_t v[32];
+        values(c0, v);
+        __syncwarp();
+#pragma unroll
+        for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+        __syncwarp();
+      };
       if (split > 1 && kSummed && !TRANS) {
         for (int c0 = 32 * set; c0 < nt; c0 += 64) {
           uint32_t v[32];
@@ -752,12 +769,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           float gu[2][4][8];
 #pragma unroll
           for (int part = 0; part < 2; ++part) {
-            uint32_t v[32];
-            values(c0 + part * (nt / 2), v);
-            __syncwarp();
-#pragma unroll
-            for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-            __syncwarp();
+            hand_over(c0 + part * (nt / 2));
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
               float (&x)[8] = gu[part][k];
@@ -804,12 +816,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
             if (A.residual && c0 + 64 < nt) ahead(c0 + 64);
             if (A.bias) Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + j)), bias);
           }
-          uint32_t v[32];
-          values(c0, v);
-          __syncwarp();
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-          __syncwarp();
+          hand_over(c0);
           T* zp = A.z ? reinterpret_cast<T*>(A.z) + row0 * A.ldz + j : nullptr;
           T* yp = reinterpret_cast<T*>(A.out) + row0 * A.ldo + j;
           float* fp = reinterpret_cast<float*>(A.out) + row0 * A.ldo + j;
@@ -843,12 +850,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           uint4 some[4];
 #pragma unroll
           for (int k = 0; k < 4; ++k) some[k] = residual8<T>(A, i0 + q * 32 + 8 * k + (lane >> 2), jl, vec);
-          uint32_t v[32];
-          values(c0, v);
-          __syncwarp();
-#pragma unroll
-          for (int e = 0; e < 32; e += 4) stage4[piece(lane, e / 4, 8)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-          __syncwarp();
+          hand_over(c0);
           if (!vec) {
             for (int k = 0; k < 32 && c0 + lane < nt; k += 8) {
               float x[8];
@@ -887,14 +889,22 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
       if constexpr (MODE == kGated) {
         // eight rows (or, with vectors, columns) of gates and of the ups that lie 64 lanes, or half a tile's columns, on
         const auto parts_of = [&](int r0, int g, float (&x)[8]) {
+          uint4 lo[kMaxSplit], hi[kMaxSplit];               // all blocks' parts on their way at once, added in order
+#pragma unroll
+          for (int r = 0; r < kMaxSplit; ++r)
+            if (r < split) {
+              const uint4* p = cluster.map_shared_rank(ring4, r);
+              lo[r] = p[piece(r0, 2 * g, nt / 4)];
+              hi[r] = p[piece(r0, 2 * g + 1, nt / 4)];
+            }
 #pragma unroll
           for (int e = 0; e < 8; ++e) x[e] = 0.f;
-          for (int r = 0; r < split; ++r) {
-            const uint4* p = cluster.map_shared_rank(ring4, r);
-            const uint4 lo = p[piece(r0, 2 * g, nt / 4)], hi = p[piece(r0, 2 * g + 1, nt / 4)];
-            x[0] += __uint_as_float(lo.x), x[1] += __uint_as_float(lo.y), x[2] += __uint_as_float(lo.z), x[3] += __uint_as_float(lo.w);
-            x[4] += __uint_as_float(hi.x), x[5] += __uint_as_float(hi.y), x[6] += __uint_as_float(hi.z), x[7] += __uint_as_float(hi.w);
-          }
+#pragma unroll
+          for (int r = 0; r < kMaxSplit; ++r)
+            if (r < split) {
+              x[0] += __uint_as_float(lo[r].x), x[1] += __uint_as_float(lo[r].y), x[2] += __uint_as_float(lo[r].z), x[3] += __uint_as_float(lo[r].w);
+              x[4] += __uint_as_float(hi[r].x), x[5] += __uint_as_float(hi[r].y), x[6] += __uint_as_float(hi[r].z), x[7] += __uint_as_float(hi[r].w);
+            }
         };
         float gate[8], up[8];
         if (TRANS) {
@@ -1128,12 +1138,16 @@ struct Plan {
   double cost;
 };
 
+constexpr int kCodesRing = 160 * 1024;       // of the 8-bit product's kernel
+
 // Tile width, split, pairs and orientation by an estimate of the time in SM cycles, whose constants were fitted to all of
 // these forms measured on 26 products (1 to 16384 rows): a stage costs the larger of its products (2.7 cycles per column of
 // the tile, 2 at the tensor pipe's rate) and of its bytes (60 a cycle); a tile's epilogue 2000 and 9 per column, 45 where it
 // writes element by element; the epilogue of one tile runs beside the products of the next.  A pair's start costs 4500
 // more; the join of a split 6500 and 25 per column, and clusters of four and eight reach 136 and 128 SMs.  The form chosen by
 // it is within 3 % of the fastest in 22 of the 26 and at most 25 % slower in the others.
+// The other modes' constants are fitted to all of their forms on 18 and 19 products each, and count a launch's 10000 cycles, which the
+// transposed and split forms, whose blocks take one tile each, have in every wave.
 // `swappable`: the epilogue may write the transposed tile.  An fp32 result's tile is a multiple of 64 wide (its operands are
 // MN-major).
 inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable, bool out32, bool long_sum, Mode mode = kPlain) {
@@ -1149,9 +1163,13 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
     const bool bmn = swap ? a_mn : b_mn;
     static const int widths[] = {16, 32, 64, 96, 112, 128, 160, 192, 208, 224, 256};
     for (int nt : widths) {
+      if (mode == kCodes && !swap && nt == 256 && rows > 1) {          // pairs alone have tiles of 256 columns
+        const double cost = 10000 + (double)((row_pairs * ((j + nt - 1) / nt) + kSMs / 2 - 1) / (kSMs / 2)) * (nkb * 960.0 + 8000);
+        if (cost < best.cost) best = Plan{0, nt, 1, kCodesRing / ((kTileM + nt / 2) * kBlockK * 2), 1, cost};
+      }
       if (bmn && nt % 64) continue;
       if (mode == kGated && !swap && nt % 64) continue;          // pieces of 32 gates and as many ups
-      if (mode == kCodes && !swap && (nt % 32 || nt > 256)) continue;
+      if (mode == kCodes && !swap && nt != 128 && nt != 64) continue;
       if ((swap || out32) && nt > 128) continue;     // fp32 results: 64 sums a thread
       const double mma = 2.7 * nt, epi = 2000 + (swap ? 45.0 : 9.0) * nt;
       const int stage = (kTileM + nt) * kBlockK * 2;
@@ -1161,9 +1179,9 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
         const int split = 1 << log2;
         const bool joined = split > 1 || (mode == kGated && swap);
         const long long kb = (nkb + split - 1) >> log2;
-        if (mode == kCodes && split > 1 && nt > 128) continue;       // two accumulators of two blocks on an SM
+        if (mode == kCodes && !swap && split > 1) continue;          // transposed tiles alone are split
         if (split > 1 && kb * (split - 1) >= nkb) continue;           // a block would have nothing to do
-        int stages = (joined ? 110 * 1024 : kMaxRing) / stage;
+        int stages = (joined ? 110 * 1024 : mode == kCodes && !swap ? kCodesRing : kMaxRing) / stage;
         if (stages > kMaxStages) stages = kMaxStages;
         if (joined)                                                    // the partial tile in the ring
           while (stages * stage < kTileM * nt * 4 || stages < 3) ++stages;
@@ -1174,7 +1192,15 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
         if (split > 1 && long_sum && nt > 128 && stages * stage <= 136 * 1024) continue;
         const double main = kb * per;
         double cost;
-        if (!joined) {
+        if (mode != kPlain && (swap || joined)) {
+          const long long blocks = tiles << log2;
+          const long long waves = split == 8 ? (blocks + 127) / 128 : split == 4 ? (blocks + 135) / 136 : (blocks + kSMs - 1) / kSMs;
+          cost = waves * (mode == kCodes ? 13000 + 112.0 * nt + kb * (700.0 + nt) : swap ? 13500 + 95.0 * nt + kb * 450.0 : 16000 + 24.0 * nt + main);
+        } else if (mode == kCodes) {
+          cost = 10000 + (double)((tiles + kSMs - 1) / kSMs) * (nt == 64 ? kb * 720.0 + 1800 : kb * 870.0 + 3700);
+        } else if (mode == kGated) {
+          cost = 10000 + persistent((double)((tiles + kSMs - 1) / kSMs), main, epi);
+        } else if (!joined) {
           cost = persistent((double)((tiles + kSMs - 1) / kSMs), main, epi);
         } else {
           const long long blocks = tiles << log2;
@@ -1186,10 +1212,11 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
       // pairs of SMs: 256 rows of D
       if (!swap && nt % 128 == 0 && rows > 1) {
         const int half = (kTileM + nt / 2) * kBlockK * 2;
-        int stages = kMaxRing / half;
+        int stages = (mode == kCodes ? kCodesRing : kMaxRing) / half;
         if (stages > kMaxStages) stages = kMaxStages;
         const double main = nkb * (mma > half / 60.0 ? mma : half / 60.0);
-        const double cost = 4500 + persistent((double)((row_pairs * cols + kSMs / 2 - 1) / (kSMs / 2)), main, epi);
+        const double waves = (double)((row_pairs * cols + kSMs / 2 - 1) / (kSMs / 2));
+        const double cost = mode == kCodes ? 10000 + waves * (nkb * 750.0 + 4000) : (mode == kGated ? 14500 : 4500) + persistent(waves, main, epi);
         if (cost < best.cost) best = Plan{0, nt, 1, stages, 1, cost};
       }
     }
@@ -1202,29 +1229,29 @@ struct Err {
   size_t len;
 };
 
-template <class T, bool TRANS, bool PAIR, bool OUT32, bool LONG, int MODE = kPlain>
-laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, bool follows,
-                       cudaStream_t st) {
-  auto kernel = linear_gemm_kernel<T, TRANS, PAIR, OUT32, LONG, MODE>;
-  const size_t smem = (size_t)A.stages * (kTileM + (PAIR ? A.nt / 2 : A.nt)) * kBlockK * 2 + (TRANS || A.split > 1 ? 0 : kStaging) + 1024;
-  const int per_tile = PAIR ? 2 : A.split;
-  // the kernel's shared memory limit is raised once per device
-  static std::atomic<uint64_t> raised{0};
+// A product kernel's shared memory limit is raised once per device.
+struct Raised {
+  std::atomic<uint64_t> devices{0};
+};
+typedef void (*GemmKernel)(const CUtensorMap, const CUtensorMap, const GemmArgs);
+inline laq_status launch_tiles(const Err& e, GemmKernel kernel, Raised& raised, unsigned threads, bool pair, bool joined, int staging, const CUtensorMap& ma,
+                               const CUtensorMap& mb, const GemmArgs& A, bool follows, cudaStream_t st) {
+  const size_t smem = (size_t)A.stages * (kTileM + (pair ? A.nt / 2 : A.nt)) * kBlockK * 2 + staging + 1024;
+  const int per_tile = pair ? 2 : A.split;
   int dev = 0;
   cudaGetDevice(&dev);
   const uint64_t bit = 1ull << (dev & 63);
-  if (dev >= 64 || !(raised.load(std::memory_order_acquire) & bit)) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing + kStaging + 1024) != cudaSuccess) {
+  if (dev >= 64 || !(raised.devices.load(std::memory_order_acquire) & bit)) {
+    if (cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing + kStaging + 1024) != cudaSuccess) {
       cudaGetLastError();
       return fail(e.buf, e.len, LAQ_ECUDA, "shared memory of the product kernel was refused");
     }
-    raised.fetch_or(bit, std::memory_order_release);
+    raised.devices.fetch_or(bit, std::memory_order_release);
   }
   const long long tiles = (long long)A.tiles_i * A.tiles_j;
-  const bool joined = A.split > 1 || (MODE == kGated && TRANS);
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(PAIR ? 2 * (tiles < kSMs / 2 ? tiles : kSMs / 2) : joined ? tiles * A.split : tiles < kSMs ? tiles : kSMs));
-  cfg.blockDim = dim3(kGemmThreads);
+  cfg.gridDim = dim3((unsigned)(pair ? 2 * (tiles < kSMs / 2 ? tiles : kSMs / 2) : joined ? tiles * A.split : tiles < kSMs ? tiles : kSMs));
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = st;
   cudaLaunchAttribute at[2];
@@ -1241,6 +1268,15 @@ laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& m
     ++cfg.numAttrs;
   }
   return launched(e.buf, e.len, cudaLaunchKernelEx(&cfg, kernel, ma, mb, A));
+}
+
+template <class T, bool TRANS, bool PAIR, bool OUT32, bool LONG, int MODE = kPlain>
+laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, bool follows,
+                       cudaStream_t st) {
+  static Raised raised;
+  const bool joined = A.split > 1 || (MODE == kGated && TRANS);
+  return launch_tiles(e, linear_gemm_kernel<T, TRANS, PAIR, OUT32, LONG, MODE>, raised, kGemmThreads, PAIR, joined,
+                      MODE == kCodes ? kEpiWarps * kScaleTable * 4 : TRANS || A.split > 1 ? 0 : kStaging, ma, mb, A, follows, st);
 }
 
 struct Epilogue {
@@ -1264,30 +1300,31 @@ inline bool make_map(CUtensorMap* map, Mode mode, const void* p, long long rows,
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-// X W^T in one of the other modes, X [M][K] and W [N][K] of mappable rows (kGated: N = 2 up).  `A` brings the epilogue, the
-// scales, the status and `up`.
-template <class T, Mode MODE>
-laq_status product_in_mode(const Err& e, GemmArgs A, const Operand& x, const Operand& w, int fmt, bool follows, cudaStream_t st) {
-  const Plan pl = make_plan(x.rows, w.rows, x.cols, false, false, true, false, false, MODE);
-  const Operand &a = pl.swap ? w : x, &b = pl.swap ? x : w;
+// X W^T in one of the other modes, X [M][K] and W [N][K] of mappable rows (kGated: N = 2 up): the tensor maps, and what the plan says
+// to the kernel, added to `A`, which brings the epilogue, the scales, the status and `up`.
+struct Product {
+  Plan pl;
   CUtensorMap ma, mb;
-  const int a_rows = MODE == kGated && pl.swap ? kTileM / 2 : kTileM;
-  const int b_rows = pl.pair || (MODE == kGated && !pl.swap) ? pl.nt / 2 : pl.nt;
-  if (!make_map(&ma, MODE, a.p, a.rows, a.cols, a.ld, a_rows) || !make_map(&mb, MODE, b.p, b.rows, b.cols, b.ld, b_rows))
+  GemmArgs A;
+};
+inline laq_status prepare_product(const Err& e, Mode mode, Product& p, const Operand& x, const Operand& w, int fmt) {
+  const Plan& pl = p.pl = make_plan(x.rows, w.rows, x.cols, false, false, true, false, false, mode);
+  const Operand &a = pl.swap ? w : x, &b = pl.swap ? x : w;
+  const int a_rows = mode == kGated && pl.swap ? kTileM / 2 : kTileM;
+  const int b_rows = pl.pair || (mode == kGated && !pl.swap) ? pl.nt / 2 : pl.nt;
+  if (!make_map(&p.ma, mode, a.p, a.rows, a.cols, a.ld, a_rows) || !make_map(&p.mb, mode, b.p, b.rows, b.cols, b.ld, b_rows))
     return fail(e.buf, e.len, LAQ_ECUDA, "a tensor map was refused");
-  const int stage_cols = MODE == kCodes ? kBlock : kBlockK, tile_rows = pl.pair ? 2 * kTileM : kTileM;
-  A.nkb = (int)((x.cols + stage_cols - 1) / stage_cols);
-  A.nt = pl.nt;
-  A.stages = pl.stages;
-  A.split = pl.split;
-  A.tiles_i = (int)((a.rows + tile_rows - 1) / tile_rows);
-  A.tiles_j = (int)((b.rows + pl.nt - 1) / pl.nt);
-  A.I = (int)a.rows;
-  A.J = (int)b.rows;
-  A.fmt = fmt;
-  if (pl.pair) return launch_gemm<T, false, true, false, false, MODE>(e, ma, mb, A, follows, st);
-  return pl.swap ? launch_gemm<T, true, false, false, false, MODE>(e, ma, mb, A, follows, st)
-                 : launch_gemm<T, false, false, false, false, MODE>(e, ma, mb, A, follows, st);
+  const int stage_cols = mode == kCodes ? kBlock : kBlockK, tile_rows = pl.pair ? 2 * kTileM : kTileM;
+  p.A.nkb = (int)((x.cols + stage_cols - 1) / stage_cols);
+  p.A.nt = pl.nt;
+  p.A.stages = pl.stages;
+  p.A.split = pl.split;
+  p.A.tiles_i = (int)((a.rows + tile_rows - 1) / tile_rows);
+  p.A.tiles_j = (int)((b.rows + pl.nt - 1) / pl.nt);
+  p.A.I = (int)a.rows;
+  p.A.J = (int)b.rows;
+  p.A.fmt = fmt;
+  return LAQ_OK;
 }
 
 // Warps that share four columns: as many as fill the rounds of resident warps best, the fewer the better within a quarter
