@@ -62,26 +62,6 @@ __device__ __forceinline__ float largest_finite(const float (&x)[8]) {
   return m;
 }
 
-// The power of two k >= -126 with largest <= 448 2^k: 448 = 1.75 2^8.
-__device__ __forceinline__ int scale_power(float largest) {
-  const uint32_t b = __float_as_uint(largest);
-  const int k = (int)(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
-  return max(k, -126);
-}
-__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }      // -126..127
-
-__device__ __forceinline__ uint32_t encode2(float lo, float hi) {
-  unsigned short two;
-  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
-  return two;
-}
-// Eight codes of values times `inverse` (a power of two: exact); what is not finite becomes NaN, which e4m3 has and infinity not.
-__device__ __forceinline__ uint2 encode8(const float (&x)[8], float inverse) {
-  float v[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = fabsf(x[e]) < INFINITY ? x[e] * inverse : __uint_as_float(0x7fffffffu);
-  return make_uint2(encode2(v[0], v[1]) | (encode2(v[2], v[3]) << 16), encode2(v[4], v[5]) | (encode2(v[6], v[7]) << 16));
-}
 __device__ __forceinline__ void store_codes(uint8_t* p, uint2 codes, int n, bool vec) {
   if (vec && n == 8) {
     *reinterpret_cast<uint2*>(p) = codes;

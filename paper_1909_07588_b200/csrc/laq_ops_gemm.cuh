@@ -81,6 +81,9 @@ struct GemmArgs {
   const float* sx;               // kCodes: scales of X, [rows][blocks], and of W, [blocks of rows][blocks]
   const float* sw;
   long long ldsx, ldsw;
+  uint8_t* z_codes;              // kGated: z in 8 bits instead of z, or null: whole blocks of 128 columns, 8-byte aligned
+  float* z_scales;
+  long long ld_zc, ld_zs;
 };
 
 __device__ __forceinline__ uint64_t desc_k_major(uint32_t addr) { return umma::smem_desc_sw128(addr); }
@@ -232,6 +235,48 @@ __device__ __forceinline__ float load_scale(const float* p) {      // where it s
   return v;
 }
 
+// The power of two k >= -126 with largest <= 448 2^k: 448 = 1.75 2^8.
+__device__ __forceinline__ int scale_power(float largest) {
+  const uint32_t b = __float_as_uint(largest);
+  const int k = (int)(b >> 23) - 135 + ((b & 0x7fffffu) > 0x600000u ? 1 : 0);
+  return max(k, -126);
+}
+__device__ __forceinline__ float power_of_two(int k) { return __uint_as_float((uint32_t)(k + 127) << 23); }      // -126..127
+
+__device__ __forceinline__ uint32_t encode2(float lo, float hi) {
+  unsigned short two;
+  asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
+  return two;
+}
+// Eight codes of values times `inverse` (a power of two: exact); what is not finite becomes NaN, which e4m3 has and infinity not.
+__device__ __forceinline__ uint2 encode8(const float (&x)[8], float inverse) {
+  float v[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = fabsf(x[e]) < INFINITY ? x[e] * inverse : __uint_as_float(0x7fffffffu);
+  return make_uint2(encode2(v[0], v[1]) | (encode2(v[2], v[3]) << 16), encode2(v[4], v[5]) | (encode2(v[6], v[7]) << 16));
+}
+// The largest finite magnitude of 32 values rounded to T.
+template <class T>
+__device__ __forceinline__ float largest_rounded(const float (&x)[32]) {
+  uint4 v[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float part[8] = {x[8 * i], x[8 * i + 1], x[8 * i + 2], x[8 * i + 3], x[8 * i + 4], x[8 * i + 5], x[8 * i + 6], x[8 * i + 7]};
+    v[i] = Elem<T>::pack(part);
+    v[i].x &= 0x7fff7fffu, v[i].y &= 0x7fff7fffu, v[i].z &= 0x7fff7fffu, v[i].w &= 0x7fff7fffu;
+  }
+  float m = Elem<T>::largest(v);
+  if (!(m < INFINITY)) {                     // some are not finite: one by one
+    m = 0.f;
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float a = fabsf(Elem<T>::to_float(Elem<T>::from_float(x[i])));
+      m = fmaxf(m, a < INFINITY ? a : 0.f);
+    }
+  }
+  return m;
+}
+
 // Eight rows row0.. of column `col` of out (rows x cols): the form for transposed tiles and for tensors that allow no
 // vectors.  Neighbouring lanes hold neighbouring columns.
 template <class T, bool OUT32>
@@ -324,7 +369,7 @@ __device__ __forceinline__ void finish_gated_column(const GemmArgs& A, int rows,
     if (e < n) out[e * A.ldo] = Elem<T>::from_float(g[e] * u[e]);
 }
 template <class T>
-__device__ __forceinline__ void finish_gated_row(const GemmArgs& A, int i, int j0, float (&g)[8], float (&u)[8]) {
+__device__ __forceinline__ void finish_gated_row(const GemmArgs& A, int i, int j0, float (&g)[8], float (&u)[8], float inv_g = 0.f, float inv_u = 0.f) {
   if (i >= A.I || j0 >= A.up) return;              // vectors are allowed: A.up is a multiple of eight
   if (A.bias) {
     const T* bias = reinterpret_cast<const T*>(A.bias) + j0;
@@ -340,6 +385,14 @@ __device__ __forceinline__ void finish_gated_row(const GemmArgs& A, int i, int j
     T* z = reinterpret_cast<T*>(A.z) + (long long)i * A.ldz + j0;
     *reinterpret_cast<uint4*>(z) = Elem<T>::pack(g);
     *reinterpret_cast<uint4*>(z + A.up) = Elem<T>::pack(u);
+  }
+  if (A.z_codes) {               // rounded to T first, as what is packed afterwards is
+    uint8_t* z = A.z_codes + (long long)i * A.ld_zc + j0;
+    float r[8];
+    Elem<T>::unpack(Elem<T>::pack(g), r);
+    *reinterpret_cast<uint2*>(z) = encode8(r, inv_g);
+    Elem<T>::unpack(Elem<T>::pack(u), r);
+    *reinterpret_cast<uint2*>(z + A.up) = encode8(r, inv_u);
   }
   activate(g, A.act);
 #pragma unroll
@@ -764,6 +817,42 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
             ring4[piece(row, (c0 + e) / 4, nt / 4)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
       } else if (MODE == kGated) {
+        // Z in 8 bits: a tile of 256 columns has a block of gates and one of ups.  A lane looks its row's through for their scales.
+        float inv_g = 0.f, inv_u = 0.f;
+        if (A.z_codes) {
+          float largest[2];
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {
+            largest[part] = 0.f;
+#pragma unroll 1
+            for (int c0 = 0; c0 < kBlock; c0 += 32) {
+              uint32_t v[32];
+              float x[32];
+              values(c0 + part * kBlock, v);
+#pragma unroll
+              for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
+              if (A.bias) {
+                const uint4* bias = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + part * A.up + j0 / 2 + c0);
+#pragma unroll
+                for (int b8 = 0; b8 < 4; ++b8) {
+                  float b[8];
+                  Elem<T>::unpack(__ldg(bias + b8), b);
+#pragma unroll
+                  for (int e = 0; e < 8; ++e) x[8 * b8 + e] += b[e];
+                }
+              }
+              largest[part] = fmaxf(largest[part], largest_rounded<T>(x));
+            }
+          }
+          const int kg = scale_power(largest[0]), ku = scale_power(largest[1]);
+          inv_g = power_of_two(-kg);
+          inv_u = power_of_two(-ku);
+          if (set == 0 && i0 + row < A.I) {
+            float* to = A.z_scales + (long long)(i0 + row) * A.ld_zs + j0 / 256;
+            to[0] = power_of_two(kg);
+            to[A.up / kBlock] = power_of_two(ku);
+          }
+        }
         // 32 gates and their ups of 32 rows, handed over as below
         for (int c0 = 32 * set; c0 < nt / 2; c0 += 64) {
           float gu[2][4][8];
@@ -788,7 +877,8 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           const int i = i0 + q * 32, j = j0 / 2 + c0;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            if (vec) finish_gated_row<T>(A, i + 8 * k + (lane >> 2), j + 8 * (lane & 3), gu[0][k], gu[1][k]);
+            const float ig = __shfl_sync(0xffffffffu, inv_g, 8 * k + (lane >> 2)), iu = __shfl_sync(0xffffffffu, inv_u, 8 * k + (lane >> 2));
+            if (vec) finish_gated_row<T>(A, i + 8 * k + (lane >> 2), j + 8 * (lane & 3), gu[0][k], gu[1][k], ig, iu);
             else finish_gated_column<T>(A, A.I, i + 8 * k, j + lane, gu[0][k], gu[1][k]);
           }
         }

@@ -58,6 +58,29 @@ def test_forward(M, F, K, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("M, F, K", [(1000, 2048, 64), (2049, 1280, 136), (777, 4096, 72), (130, 128, 64)])
+def test_projections_packed_where_they_are_made(M, F, K, dtype):
+    """Tiles of whole blocks: bit for bit what pack8 makes of the 16-bit projections, with blocks of zeros, far values and values that
+    are no numbers, and with and without a bias."""
+    dt = DTYPES[dtype]
+    x, w = _randn(M, K, seed=1, dtype=dt), _randn(2 * F, K, seed=2, dtype=dt, scale=K ** -0.5)
+    b = _randn(2 * F, seed=3, dtype=dt)
+    x[3] = 0
+    x[5] *= 2.0 ** 10
+    x[M - 1] *= 2.0 ** -12
+    w[128 % F:128 % F + 128] = 0
+    odd = b.clone()
+    odd[7], odd[F + 9], odd[2 * F - 1] = math.inf, -math.inf, math.nan
+    for bias in (None, b, odd):
+        h, z = ops.gated(x, w, bias, activation="gelu", preact=True)
+        h8, z8 = ops.gated(x, w, bias, activation="gelu", preact="packed")
+        want = ops.pack8(z)
+        assert torch.equal(z8.scales, want.scales) and torch.equal(z8.codes.view(torch.uint8), want.codes.view(torch.uint8))
+        assert torch.equal(h8.view(torch.int16), h.view(torch.int16))
+    ops.check_status()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
 @pytest.mark.parametrize("M, F, K", [(1, 1, 1), (2, 3, 5), (1, 300, 120), (20, 40, 64), (100, 200, 784), (129, 129, 129), (300, 64, 1000),
                                      (600, 520, 136), (2048, 512, 1024), (4100, 16, 24), (64, 1024, 1024)])
 def test_gradient(M, F, K, dtype):
