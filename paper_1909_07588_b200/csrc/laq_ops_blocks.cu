@@ -769,7 +769,7 @@ laq_status few_codes(const Err& e, const GemmArgs& A, const Operand& x, const Op
 
 laq_status load_block_kernels(const Err& e) {
   static Loaded loaded;
-  static const void* list[32];
+  static const void* list[64];
   static const int n = [] {
     int count = 0;
     list_block_kernels<float>(list, count);

@@ -234,7 +234,7 @@ void list_kernels(const void** list, int& n) {
 // Its own kernels, and those of the products and of the 8-bit matrices that its calls may use.
 laq_status load_kernels(const Err& e) {
   static Loaded loaded;
-  static const void* list[32];
+  static const void* list[64];
   static const int n = [] {
     int count = 0;
     list_kernels<__nv_bfloat16>(list, count);
@@ -371,5 +371,5 @@ extern "C" laq_status laq_gated_backward(const laq_gated_call* c, void* d_worksp
     ws += need.x_bytes;
     LAQ_TRY(unpack_blocks(e, *c->x_blocks, c->M, c->K, c->dtype, const_cast<void*>(need.x.p), need.x.ld, st));
   }
-  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, st);
+  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, false, true, st);
 }

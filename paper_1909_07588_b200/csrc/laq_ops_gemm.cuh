@@ -1323,20 +1323,27 @@ struct Err {
 struct Raised {
   std::atomic<uint64_t> devices{0};
 };
+inline laq_status raise_shared_memory(const Err& e, const void* kernel, Raised& raised) {
+  int dev = 0;
+  cudaGetDevice(&dev);
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev >= 64 || !(raised.devices.load(std::memory_order_acquire) & bit)) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing + kStaging + 1024) != cudaSuccess) {
+      cudaGetLastError();
+      return fail(e.buf, e.len, LAQ_ECUDA, "shared memory of the product kernel was refused");
+    }
+    raised.devices.fetch_or(bit, std::memory_order_release);
+  }
+  return LAQ_OK;
+}
 typedef void (*GemmKernel)(const CUtensorMap, const CUtensorMap, const GemmArgs);
 inline laq_status launch_tiles(const Err& e, GemmKernel kernel, Raised& raised, unsigned threads, bool pair, bool joined, int staging, const CUtensorMap& ma,
                                const CUtensorMap& mb, const GemmArgs& A, bool follows, cudaStream_t st) {
   const size_t smem = (size_t)A.stages * (kTileM + (pair ? A.nt / 2 : A.nt)) * kBlockK * 2 + staging + 1024;
   const int per_tile = pair ? 2 : A.split;
-  int dev = 0;
-  cudaGetDevice(&dev);
-  const uint64_t bit = 1ull << (dev & 63);
-  if (dev >= 64 || !(raised.devices.load(std::memory_order_acquire) & bit)) {
-    if (cudaFuncSetAttribute((const void*)kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing + kStaging + 1024) != cudaSuccess) {
-      cudaGetLastError();
-      return fail(e.buf, e.len, LAQ_ECUDA, "shared memory of the product kernel was refused");
-    }
-    raised.devices.fetch_or(bit, std::memory_order_release);
+  {
+    const laq_status st_ = raise_shared_memory(e, (const void*)kernel, raised);
+    if (st_ != LAQ_OK) return st_;
   }
   const long long tiles = (long long)A.tiles_i * A.tiles_j;
   cudaLaunchConfig_t cfg = {};
@@ -1482,8 +1489,14 @@ struct Gradients {
   long long ld_dw;
   int dw_f32;
 };
+// Whether one launch for both (16-bit results, dZ [M][N], K inputs) is the faster by the plans' estimates, and that launch.
+// `in_order`: only where the products by themselves would not split their sums either, so that every bit is as theirs.
+bool both_pay(long long M, long long N, long long K, bool in_order);
+laq_status both_products(const Err& e, int dtype, const Operand& dz, const Operand& x, const Operand& w, const Gradients& to, uint32_t* status, int starve,
+                         bool follows, cudaStream_t st);
+void list_both_kernels(const void** list, int& n);
 laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand x, Operand w, const Gradients& to, char*& ws, uint32_t* status,
-                             int starve, bool follows, cudaStream_t st);
+                             int starve, bool in_order, bool follows, cudaStream_t st);
 // db = the sums of the columns of part [runs][N]; follows a kernel of the same call.
 laq_status column_sums(const Err& e, const float* part, int runs, int N, float* db, cudaStream_t st);
 laq_status zero_gradients(const Err& e, const Gradients& to, float* db, long long N, long long K, cudaStream_t st);   // of no rows

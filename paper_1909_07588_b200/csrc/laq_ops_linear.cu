@@ -329,11 +329,12 @@ void list_kernels(const void** list, int& n) {
 
 laq_status load_layer_kernels(const Err& e) {
   static Loaded loaded;
-  static const void* list[32];
+  static const void* list[64];
   static const int n = [] {
     int count = 0;
     list_kernels<__nv_bfloat16>(list, count);
     list_kernels<__half>(list, count);
+    list_both_kernels(list, count);
     list[count++] = (const void*)linear_db_kernel;
     list[count++] = (const void*)linear_pack_kernel;
     return count;
@@ -355,7 +356,13 @@ laq_status column_sums(const Err& e, const float* part, int runs, int N, float* 
 }
 
 laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand x, Operand w, const Gradients& to, char*& ws, uint32_t* status,
-                             int starve, bool follows, cudaStream_t st) {
+                             int starve, bool in_order, bool follows, cudaStream_t st) {
+  if (to.dx && to.dw && !to.dw_f32 && both_pay(dz.rows, dz.cols, x.cols, in_order)) {
+    const char* before = ws;
+    LAQ_TRY(make_mappable(e, w, ws, st));
+    LAQ_TRY(make_mappable(e, x, ws, st));
+    return both_products(e, dtype, dz, x, w, to, status, starve, follows || ws != before, st);
+  }
   if (to.dx) {
     const char* before = ws;
     LAQ_TRY(make_mappable(e, w, ws, st));
@@ -456,7 +463,7 @@ laq_status layer_backward(const Err& e, const laq_linear_call* c, const laq_bloc
   };
   LAQ_TRY(restored(wq, need.w, need.w_bytes));
   LAQ_TRY(restored(xq, need.x, need.x_bytes));
-  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, starve, follows, st);
+  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, starve, true, follows, st);
 }
 
 }  // namespace
