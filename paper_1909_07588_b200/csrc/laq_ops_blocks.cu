@@ -17,7 +17,10 @@ namespace {
 
 constexpr int kPackThreads = 256;
 constexpr int kLanes = 16;                // threads of a block's 128 columns, eight each
-constexpr int kPackAhead = 4;             // rows that a thread has under way
+// Rows that a thread has under way: as many as keep memory busy where there are many (16-bit values four, 8192 x 4096 19.9 us, by two
+// 21.9; fp32 two, 26.3 us, by four 27.5), one where the blocks are few (64 x 200: 2.3 us, by four 3.5).
+template <class T>
+constexpr int kMostAhead = 16 / sizeof(T) / 2;
 
 // Eight neighbours in fp32; `vec`: they lie on a 16-byte boundary and all exist, else the first n are read one by one.
 template <class T>
@@ -52,6 +55,18 @@ struct Eight {
   }
 };
 
+// The largest magnitude of eight values, +inf or NaN where one is no finite number.
+__device__ __forceinline__ float largest_of(const Eight<float>& in) {
+  uint4 v[2] = {in.v[0], in.v[1]};
+#pragma unroll
+  for (int i = 0; i < 2; ++i) v[i].x &= 0x7fffffffu, v[i].y &= 0x7fffffffu, v[i].z &= 0x7fffffffu, v[i].w &= 0x7fffffffu;
+  return Elem<float>::largest(v);
+}
+template <class T>
+__device__ __forceinline__ float largest_of(const Eight<T>& in) {
+  const uint4 v[1] = {make_uint4(in.v[0].x & 0x7fff7fffu, in.v[0].y & 0x7fff7fffu, in.v[0].z & 0x7fff7fffu, in.v[0].w & 0x7fff7fffu)};
+  return Elem<T>::largest(v);
+}
 __device__ __forceinline__ float largest_finite(const float (&x)[8]) {
   float m = 0.f;
 #pragma unroll
@@ -73,8 +88,8 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint2 codes, int n, bool
 }
 
 // A scale a row and 128 columns: 16 threads take a block.  Bound by memory.  A thread block has 16 such groups, side by side
-// along a row up to 1 << log_across of them, and each has kPackAhead rows under way.
-template <class T>
+// along a row up to 1 << log_across of them, and each has AHEAD rows under way.
+template <class T, int AHEAD>
 __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(const T* x, long long ld, long long rows, long long cols, uint8_t* codes, long long ldc,
                                                                  float* scales, long long lds, int log_across, int vec_in, int vec_out) {
   allow_next();
@@ -84,26 +99,34 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(const T* x, lon
   const long long c0 = block * kBlock + lane * 8;
   const int n = (int)max(0ll, min(8ll, cols - c0));
   const bool there = block * kBlock < cols;
-  const long long step = (long long)gridDim.y * down * kPackAhead;
-  for (long long top = (long long)blockIdx.y * down * kPackAhead; top < rows; top += step) {      // the same turns for a whole warp
+  const long long step = (long long)gridDim.y * down * AHEAD;
+  for (long long top = (long long)blockIdx.y * down * AHEAD; top < rows; top += step) {      // the same turns for a whole warp
     const long long r0 = top + (group >> log_across);
-    Eight<T> in[kPackAhead];
+    Eight<T> in[AHEAD];
 #pragma unroll
-    for (int a = 0; a < kPackAhead; ++a) {
+    for (int a = 0; a < AHEAD; ++a) {
       const long long r = r0 + a * down;
       in[a].read(x + r * ld + c0, r < rows ? n : 0, vec_in);
     }
 #pragma unroll
-    for (int a = 0; a < kPackAhead; ++a) {
+    for (int a = 0; a < AHEAD; ++a) {
       const long long r = r0 + a * down;
       float v[8];
       in[a].get(v);
-      float m = largest_finite(v);
+      float m = largest_of(in[a]);
 #pragma unroll
-      for (int o = kLanes / 2; o > 0; o /= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      for (int o = kLanes / 2; o > 0; o /= 2) m = max_nan(m, __shfl_xor_sync(0xffffffffu, m, o));
+      const bool finite = m < INFINITY;
+      if (__any_sync(0xffffffffu, !finite)) {          // rare: the largest of those that are
+        float f = largest_finite(v);
+#pragma unroll
+        for (int o = kLanes / 2; o > 0; o /= 2) f = fmaxf(f, __shfl_xor_sync(0xffffffffu, f, o));
+        if (!finite) m = f;
+      }
       const int k = scale_power(m);
       if (r < rows && there) {
-        store_codes(codes + r * ldc + c0, encode8(v, power_of_two(-k)), n, vec_out);
+        const uint2 eight = finite ? encode8_finite(v, power_of_two(-k)) : encode8(v, power_of_two(-k));
+        store_codes(codes + r * ldc + c0, eight, n, vec_out);
         if (lane == 0) scales[r * lds + block] = power_of_two(k);
       }
     }
@@ -145,18 +168,16 @@ __global__ void __launch_bounds__(kPackThreads) pack_tiles_kernel(const T* x, lo
   if (threadIdx.x == 0) scales[down * lds + block] = power_of_two(k);
 }
 
-// A value rounded to T; a finite one beyond T's largest is that.
 template <class T>
-__device__ __forceinline__ float within(float v);
-template <>
-__device__ __forceinline__ float within<float>(float v) { return fabsf(v) == INFINITY ? copysignf(FLT_MAX, v) : v; }
-template <>
-__device__ __forceinline__ float within<__nv_bfloat16>(float v) { return fabsf(v) > 3.38953139e38f ? copysignf(3.38953139e38f, v) : v; }
-template <>
-__device__ __forceinline__ float within<__half>(float v) { return fabsf(v) > 65504.f ? copysignf(65504.f, v) : v; }
+__device__ __forceinline__ constexpr float largest_number() {
+  return std::is_same<T, float>::value ? FLT_MAX : std::is_same<T, __half>::value ? 65504.f : 3.38953139e38f;
+}
+// A finite value beyond T's largest is that; NaN stays.
+template <class T>
+__device__ __forceinline__ float within(float v) { return fabsf(v) > largest_number<T>() ? copysignf(largest_number<T>(), v) : v; }
 
 // Codes to values, in the same arrangement.  Bound by memory.
-template <class T>
+template <class T, int AHEAD>
 __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, long long rows, long long cols, T* out, long long ld, int log_across, int vec_in,
                                                               int vec_out) {
   allow_next();
@@ -166,12 +187,12 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
   const long long c0 = block * kBlock + lane * 8;
   const int n = (int)max(0ll, min(8ll, cols - c0));
   if (n == 0) return;
-  const long long step = (long long)gridDim.y * down * kPackAhead;
-  for (long long r0 = (long long)blockIdx.y * down * kPackAhead + (group >> log_across); r0 < rows; r0 += step) {
-    uint2 in[kPackAhead];
-    float scale[kPackAhead];
+  const long long step = (long long)gridDim.y * down * AHEAD;
+  for (long long r0 = (long long)blockIdx.y * down * AHEAD + (group >> log_across); r0 < rows; r0 += step) {
+    uint2 in[AHEAD];
+    float scale[AHEAD];
 #pragma unroll
-    for (int a = 0; a < kPackAhead; ++a) {
+    for (int a = 0; a < AHEAD; ++a) {
       const long long r = r0 + a * down;
       in[a] = make_uint2(0u, 0u);
       scale[a] = 0.f;
@@ -190,13 +211,15 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
       scale[a] = q.scale(r, c0);
     }
 #pragma unroll
-    for (int a = 0; a < kPackAhead; ++a) {
+    for (int a = 0; a < AHEAD; ++a) {
       const long long r = r0 + a * down;
       if (r >= rows) break;
       float v[8];
       decode8(in[a], scale[a], v);
+      if (!(fabsf(scale[a]) <= largest_number<T>() / 448.f)) {          // values may lie beyond T's largest
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = within<T>(v[e]);
+        for (int e = 0; e < 8; ++e) v[e] = within<T>(v[e]);
+      }
       T* o = out + r * ld + c0;
       if (vec_out && n == 8) {
 #pragma unroll
@@ -685,13 +708,15 @@ laq_status make_codes_mappable(const Err& e, Operand& o, char*& ws, cudaStream_t
 }
 
 struct Spread {                // of the 16 groups of a thread block over blocks of columns and rows
-  int log_across;
+  int log_across, ahead;
   dim3 grid;
-  Spread(long long rows, long long cols) {
+  Spread(long long rows, long long cols, int most_ahead) {
     const long long across = blocks_across(cols);
     log_across = across >= 16 ? 4 : across >= 8 ? 3 : across >= 4 ? 2 : across >= 2 ? 1 : 0;
-    const long long down = (kPackThreads / kLanes >> log_across) * kPackAhead, runs = (rows + down - 1) / down;
-    grid = dim3((unsigned)((across + (1 << log_across) - 1) >> log_across), (unsigned)(runs < 65535 ? runs : 65535));
+    const long long gx = (across + (1 << log_across) - 1) >> log_across, high = kPackThreads / kLanes >> log_across;
+    ahead = gx * (rows / (high * most_ahead)) >= 2 * kSMs ? most_ahead : 1;
+    const long long down = high * ahead, runs = (rows + down - 1) / down;
+    grid = dim3((unsigned)gx, (unsigned)(runs < 65535 ? runs : 65535));
   }
 };
 
@@ -705,22 +730,23 @@ laq_status pack_typed(const Err& e, const T* x, long long rows, long long cols, 
     return launched(e.buf, e.len, launch_plain(pack_tiles_kernel<T>, dim3((unsigned)tiles), kPackThreads, st, x, ld, rows, cols, codes, b.ld_codes, scales,
                                                b.ld_scales, across, vec_in, vec_out));
   }
-  const Spread s(rows, cols);
-  return launched(e.buf, e.len, launch_plain(pack_rows_kernel<T>, s.grid, kPackThreads, st, x, ld, rows, cols, codes, b.ld_codes, scales, b.ld_scales,
-                                             s.log_across, vec_in, vec_out));
+  const Spread s(rows, cols, kMostAhead<T>);
+  return launched(e.buf, e.len, launch_plain(s.ahead > 1 ? pack_rows_kernel<T, kMostAhead<T>> : pack_rows_kernel<T, 1>, s.grid, kPackThreads, st, x, ld, rows,
+                                             cols, codes, b.ld_codes, scales, b.ld_scales, s.log_across, vec_in, vec_out));
 }
 
 template <class T>
 laq_status unpack_typed(const Err& e, const laq_blocks& b, long long rows, long long cols, T* out, long long ld, cudaStream_t st) {
-  const Spread s(rows, cols);
+  const Spread s(rows, cols, kMostAhead<T>);
   const int vec_out = ((uintptr_t)out & 15u) == 0 && ld * (long long)sizeof(T) % 16 == 0;
-  return launched(e.buf, e.len, launch_plain(unpack_kernel<T>, s.grid, kPackThreads, st, Codes(&b), rows, cols, out, ld, s.log_across,
-                                             (int)Codes(&b).vectors(8), vec_out));
+  return launched(e.buf, e.len, launch_plain(s.ahead > 1 ? unpack_kernel<T, kMostAhead<T>> : unpack_kernel<T, 1>, s.grid, kPackThreads, st, Codes(&b), rows,
+                                             cols, out, ld, s.log_across, (int)Codes(&b).vectors(8), vec_out));
 }
 
 template <class T>
 void list_block_kernels(const void** list, int& n) {
-  const void* all[] = {(const void*)pack_rows_kernel<T>, (const void*)pack_tiles_kernel<T>, (const void*)unpack_kernel<T>};
+  const void* all[] = {(const void*)pack_rows_kernel<T, 1>, (const void*)pack_rows_kernel<T, kMostAhead<T>>, (const void*)pack_tiles_kernel<T>,
+                       (const void*)unpack_kernel<T, 1>, (const void*)unpack_kernel<T, kMostAhead<T>>};
   for (const void* k : all) list[n++] = k;
 }
 template <class T>

@@ -248,6 +248,10 @@ __device__ __forceinline__ uint32_t encode2(float lo, float hi) {
   asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(two) : "f"(hi), "f"(lo));
   return two;
 }
+__device__ __forceinline__ uint2 encode8_finite(const float (&x)[8], float inverse) {
+  return make_uint2(encode2(x[0] * inverse, x[1] * inverse) | (encode2(x[2] * inverse, x[3] * inverse) << 16),
+                    encode2(x[4] * inverse, x[5] * inverse) | (encode2(x[6] * inverse, x[7] * inverse) << 16));
+}
 // Eight codes of values times `inverse` (a power of two: exact); what is not finite becomes NaN, which e4m3 has and infinity not.
 __device__ __forceinline__ uint2 encode8(const float (&x)[8], float inverse) {
   float v[8];
