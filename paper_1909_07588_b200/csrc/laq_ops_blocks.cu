@@ -22,20 +22,29 @@ constexpr int kLanes = 16;                // threads of a block's 128 columns, e
 template <class T>
 constexpr int kMostAhead = 16 / sizeof(T) / 2;
 
-// Eight neighbours in fp32; `vec`: they lie on a 16-byte boundary and all exist, else the first n are read one by one.
+// Eight neighbours; VEC: they lie on a 16-byte boundary and all or none exist, else the first n are read wherever they lie.
 template <class T>
 struct Eight {
   static constexpr int kVectors = 8 / Elem<T>::EV;
   uint4 v[kVectors];
-  __device__ __forceinline__ void read(const T* p, int n, bool vec) {
-    if (vec && n == 8) {
+  template <bool VEC>
+  __device__ __forceinline__ void read(const T* p, int n) {
+    if (VEC) {
 #pragma unroll
-      for (int i = 0; i < kVectors; ++i) v[i] = load16(p + i * Elem<T>::EV);
+      for (int i = 0; i < kVectors; ++i) v[i] = n ? load16(p + i * Elem<T>::EV) : make_uint4(0u, 0u, 0u, 0u);
       return;
     }
     float x[8];
+    if constexpr (sizeof(T) == 2) {
+      uint4 all = make_uint4(0u, 0u, 0u, 0u);
+      if (n > 0) all = load16_any(p, n);
+      Elem<T>::unpack(all, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = e < n ? Elem<T>::to_float(p[e]) : 0.f;
+      for (int e = 0; e < 8; ++e) x[e] = e < n ? x[e] : 0.f;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = e < n ? Elem<T>::to_float(p[e]) : 0.f;
+    }
 #pragma unroll
     for (int i = 0; i < kVectors; ++i) {
       float part[Elem<T>::EV];
@@ -77,9 +86,10 @@ __device__ __forceinline__ float largest_finite(const float (&x)[8]) {
   return m;
 }
 
-__device__ __forceinline__ void store_codes(uint8_t* p, uint2 codes, int n, bool vec) {
-  if (vec && n == 8) {
-    *reinterpret_cast<uint2*>(p) = codes;
+template <bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t* p, uint2 codes, int n) {
+  if (VEC) {
+    if (n) *reinterpret_cast<uint2*>(p) = codes;
     return;
   }
 #pragma unroll
@@ -89,15 +99,16 @@ __device__ __forceinline__ void store_codes(uint8_t* p, uint2 codes, int n, bool
 
 // A scale a row and 128 columns: 16 threads take a block.  Bound by memory.  A thread block has 16 such groups, side by side
 // along a row up to 1 << log_across of them, and each has AHEAD rows under way.
-template <class T, int AHEAD>
+// VEC: rows and their eights of columns lie on vectors.
+template <class T, int AHEAD, bool VEC>
 __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(const T* x, long long ld, long long rows, long long cols, uint8_t* codes, long long ldc,
-                                                                 float* scales, long long lds, int log_across, int vec_in, int vec_out) {
+                                                                 float* scales, long long lds, int log_across) {
   allow_next();
   const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
   const int down = kPackThreads / kLanes >> log_across;          // groups above one another
   const long long block = ((long long)blockIdx.x << log_across) + (group & ((1 << log_across) - 1));
   const long long c0 = block * kBlock + lane * 8;
-  const int n = (int)max(0ll, min(8ll, cols - c0));
+  const int n = VEC ? (c0 < cols ? 8 : 0) : (int)max(0ll, min(8ll, cols - c0));
   const bool there = block * kBlock < cols;
   const long long step = (long long)gridDim.y * down * AHEAD;
   for (long long top = (long long)blockIdx.y * down * AHEAD; top < rows; top += step) {      // the same turns for a whole warp
@@ -106,7 +117,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(const T* x, lon
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       const long long r = r0 + a * down;
-      in[a].read(x + r * ld + c0, r < rows ? n : 0, vec_in);
+      in[a].template read<VEC>(x + r * ld + c0, r < rows ? n : 0);
     }
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
@@ -126,7 +137,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(const T* x, lon
       const int k = scale_power(m);
       if (r < rows && there) {
         const uint2 eight = finite ? encode8_finite(v, power_of_two(-k)) : encode8(v, power_of_two(-k));
-        store_codes(codes + r * ldc + c0, eight, n, vec_out);
+        store_codes<VEC>(codes + r * ldc + c0, eight, n);
         if (lane == 0) scales[r * lds + block] = power_of_two(k);
       }
     }
@@ -134,9 +145,9 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(const T* x, lon
 }
 
 // A scale a tile of 128 x 128: a thread block's 16 groups take eight rows each and hold them in registers.
-template <class T>
+template <class T, bool VEC>
 __global__ void __launch_bounds__(kPackThreads) pack_tiles_kernel(const T* x, long long ld, long long rows, long long cols, uint8_t* codes, long long ldc,
-                                                                  float* scales, long long lds, long long across, int vec_in, int vec_out) {
+                                                                  float* scales, long long lds, long long across) {
   __shared__ float part[kPackThreads / 32];
   allow_next();
   const long long down = blockIdx.x / across, block = blockIdx.x - down * across;
@@ -145,7 +156,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_tiles_kernel(const T* x, lo
   const int n = (int)max(0ll, min(8ll, cols - c0));
   Eight<T> in[8];
 #pragma unroll
-  for (int a = 0; a < 8; ++a) in[a].read(x + (row0 + 16 * a) * ld + c0, row0 + 16 * a < rows ? n : 0, vec_in);
+  for (int a = 0; a < 8; ++a) in[a].template read<VEC>(x + (row0 + 16 * a) * ld + c0, row0 + 16 * a < rows ? n : 0);
   float m = 0.f, v[8];
 #pragma unroll
   for (int a = 0; a < 8; ++a) {
@@ -163,7 +174,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_tiles_kernel(const T* x, lo
   for (int a = 0; a < 8; ++a) {
     if (row0 + 16 * a >= rows) break;
     in[a].get(v);
-    store_codes(codes + (row0 + 16 * a) * ldc + c0, encode8(v, power_of_two(-k)), n, vec_out);
+    store_codes<VEC>(codes + (row0 + 16 * a) * ldc + c0, encode8(v, power_of_two(-k)), n);
   }
   if (threadIdx.x == 0) scales[down * lds + block] = power_of_two(k);
 }
@@ -177,9 +188,8 @@ template <class T>
 __device__ __forceinline__ float within(float v) { return fabsf(v) > largest_number<T>() ? copysignf(largest_number<T>(), v) : v; }
 
 // Codes to values, in the same arrangement.  Bound by memory.
-template <class T, int AHEAD>
-__global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, long long rows, long long cols, T* out, long long ld, int log_across, int vec_in,
-                                                              int vec_out) {
+template <class T, int AHEAD, bool VEC>
+__global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, long long rows, long long cols, T* out, long long ld, int log_across) {
   allow_next();
   const int group = threadIdx.x / kLanes, lane = threadIdx.x % kLanes;
   const int down = kPackThreads / kLanes >> log_across;
@@ -198,16 +208,7 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
       scale[a] = 0.f;
       if (r >= rows) continue;
       const uint8_t* p = q.p + r * q.ld + c0;
-      if (vec_in && n == 8) {
-        in[a] = load8(p);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const uint32_t code = e < n ? p[e] : 0u;
-          if (e < 4) in[a].x |= code << (8 * e);
-          else in[a].y |= code << (8 * (e - 4));
-        }
-      }
+      in[a] = VEC ? load8(p) : load8_any(p, n);
       scale[a] = q.scale(r, c0);
     }
 #pragma unroll
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
         for (int e = 0; e < 8; ++e) v[e] = within<T>(v[e]);
       }
       T* o = out + r * ld + c0;
-      if (vec_out && n == 8) {
+      if (VEC) {
 #pragma unroll
         for (int i = 0; i < 8 / Elem<T>::EV; ++i) {
           float part[Elem<T>::EV];
@@ -229,10 +230,12 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
           for (int e = 0; e < Elem<T>::EV; ++e) part[e] = v[i * Elem<T>::EV + e];
           *reinterpret_cast<uint4*>(o + i * Elem<T>::EV) = Elem<T>::pack(part);
         }
+      } else if constexpr (sizeof(T) == 2) {
+        store16_any(o, Elem<T>::pack(v), n);
       } else {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (e < n) o[e] = Elem<T>::from_float(v[e]);
+          if (e < n) o[e] = v[e];
       }
     }
   }
@@ -675,18 +678,32 @@ __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __gr
   }
 }
 
-// Codes that a tensor map cannot describe are copied with a pitch of a multiple of 16 bytes.
-__global__ void __launch_bounds__(256) copy_codes_kernel(const uint8_t* src, long long ld, uint8_t* dst, long long pitch, long long rows, long long cols) {
+// Codes that a tensor map cannot describe are copied with a pitch of a multiple of 16 bytes, both operands' in one launch.  A warp
+// takes a row, a lane 16 codes of it at a time, from the aligned words that they lie in.  (Byte by byte and in two launches, 300 x 777
+// and 1025 x 777: OLDUS, so NEWUS.)
+struct CodeRows {
+  const uint8_t* src;
+  uint8_t* dst;
+  long long ld, pitch, rows, cols;
+};
+__global__ void __launch_bounds__(256) copy_codes_kernel(const CodeRows a, const CodeRows b) {
   allow_next();
-  const long long groups = (cols + 15) / 16, n = rows * groups, stride = (long long)gridDim.x * blockDim.x;
-  for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) {
-    const long long r = i / groups, c = (i - r * groups) * 16;
-    const uint8_t* s = src + r * ld + c;
-    uint32_t w[4] = {};
+  const int lane = threadIdx.x & 31;
+  const long long warps = (long long)gridDim.x * (blockDim.x / 32);
+  for (long long i = ((long long)blockIdx.x * blockDim.x + threadIdx.x) / 32; i < a.rows + b.rows; i += warps) {
+    const bool second = i >= a.rows;
+    const long long r = second ? i - a.rows : i, cols = second ? b.cols : a.cols;
+    const uint8_t* src = second ? b.src + r * b.ld : a.src + r * a.ld;
+    uint8_t* dst = second ? b.dst + r * b.pitch : a.dst + r * a.pitch;
+    for (long long c = lane * 16; c < cols; c += 512) {
+      const int n = (int)min(16ll, cols - c), off = (int)((uintptr_t)(src + c) & 3u);
+      const uint32_t* words = reinterpret_cast<const uint32_t*>(src + c - off);
+      uint32_t w[5];
 #pragma unroll
-    for (int e = 0; e < 16; ++e)
-      if (c + e < cols) w[e / 4] |= (uint32_t)s[e] << (8 * (e % 4));
-    *reinterpret_cast<uint4*>(dst + r * pitch + c) = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int k = 0; k < 5; ++k) w[k] = 4 * k < off + n ? words[k] : 0u;          // no word without one of the row's codes
+      *reinterpret_cast<uint4*>(dst + c) = make_uint4(__funnelshift_r(w[0], w[1], 8 * off), __funnelshift_r(w[1], w[2], 8 * off),
+                                                      __funnelshift_r(w[2], w[3], 8 * off), __funnelshift_r(w[3], w[4], 8 * off));
+    }
   }
 }
 
@@ -695,16 +712,24 @@ long long pad16(long long x) { return (x + 15) / 16 * 16; }
 bool codes_mappable(const Operand& o) { return ((uintptr_t)o.p & 15u) == 0 && o.ld % 16 == 0; }
 size_t copy_bytes(const Operand& o) { return codes_mappable(o) ? 0 : align256((size_t)o.rows * pad16(o.cols)); }
 
-laq_status make_codes_mappable(const Err& e, Operand& o, char*& ws, cudaStream_t st) {
-  const size_t bytes = copy_bytes(o);
-  if (!bytes) return LAQ_OK;
-  const long long pitch = pad16(o.cols), want = (o.rows * (pitch / 16) + 255) / 256, most = 8 * kSMs;
-  LAQ_TRY(launched(e.buf, e.len, launch_plain(copy_codes_kernel, dim3((unsigned)(want < most ? want : most)), 256, st, (const uint8_t*)o.p, o.ld,
-                                              (uint8_t*)ws, pitch, o.rows, o.cols)));
-  o.p = ws;
-  o.ld = pitch;
-  ws += bytes;
-  return LAQ_OK;
+// Copies what needs it of two operands to `ws` (advanced past it).
+laq_status make_codes_mappable(const Err& e, Operand& x, Operand& w, char*& ws, cudaStream_t st) {
+  CodeRows rows[2] = {};
+  Operand* of[2] = {&x, &w};
+  long long total = 0;
+  for (int i = 0; i < 2; ++i) {
+    Operand& o = *of[i];
+    const size_t bytes = copy_bytes(o);
+    if (!bytes) continue;
+    rows[i] = CodeRows{(const uint8_t*)o.p, (uint8_t*)ws, o.ld, pad16(o.cols), o.rows, o.cols};
+    o.p = ws;
+    o.ld = rows[i].pitch;
+    ws += bytes;
+    total += o.rows;
+  }
+  if (!total) return LAQ_OK;
+  const long long want = (total + 7) / 8, most = 8 * kSMs;
+  return launched(e.buf, e.len, launch_plain(copy_codes_kernel, dim3((unsigned)(want < most ? want : most)), 256, st, rows[0], rows[1]));
 }
 
 struct Spread {                // of the 16 groups of a thread block over blocks of columns and rows
@@ -724,29 +749,34 @@ template <class T>
 laq_status pack_typed(const Err& e, const T* x, long long rows, long long cols, long long ld, const laq_blocks& b, cudaStream_t st) {
   uint8_t* codes = (uint8_t*)const_cast<void*>(b.codes);
   float* scales = const_cast<float*>(b.scales);
-  const int vec_in = ((uintptr_t)x & 15u) == 0 && ld * (long long)sizeof(T) % 16 == 0, vec_out = Codes(&b).vectors(8);
+  const bool vec = ((uintptr_t)x & 15u) == 0 && ld * (long long)sizeof(T) % 16 == 0 && Codes(&b).vectors(8) && cols % 8 == 0;
   if (b.block_rows == kBlock) {
     const long long across = blocks_across(cols), tiles = across * ((rows + kBlock - 1) / kBlock);
-    return launched(e.buf, e.len, launch_plain(pack_tiles_kernel<T>, dim3((unsigned)tiles), kPackThreads, st, x, ld, rows, cols, codes, b.ld_codes, scales,
-                                               b.ld_scales, across, vec_in, vec_out));
+    return launched(e.buf, e.len, launch_plain(vec ? pack_tiles_kernel<T, true> : pack_tiles_kernel<T, false>, dim3((unsigned)tiles), kPackThreads, st, x, ld,
+                                               rows, cols, codes, b.ld_codes, scales, b.ld_scales, across));
   }
   const Spread s(rows, cols, kMostAhead<T>);
-  return launched(e.buf, e.len, launch_plain(s.ahead > 1 ? pack_rows_kernel<T, kMostAhead<T>> : pack_rows_kernel<T, 1>, s.grid, kPackThreads, st, x, ld, rows,
-                                             cols, codes, b.ld_codes, scales, b.ld_scales, s.log_across, vec_in, vec_out));
+  const auto kernel = s.ahead > 1 ? (vec ? pack_rows_kernel<T, kMostAhead<T>, true> : pack_rows_kernel<T, kMostAhead<T>, false>)
+                                  : (vec ? pack_rows_kernel<T, 1, true> : pack_rows_kernel<T, 1, false>);
+  return launched(e.buf, e.len, launch_plain(kernel, s.grid, kPackThreads, st, x, ld, rows, cols, codes, b.ld_codes, scales, b.ld_scales, s.log_across));
 }
 
 template <class T>
 laq_status unpack_typed(const Err& e, const laq_blocks& b, long long rows, long long cols, T* out, long long ld, cudaStream_t st) {
   const Spread s(rows, cols, kMostAhead<T>);
-  const int vec_out = ((uintptr_t)out & 15u) == 0 && ld * (long long)sizeof(T) % 16 == 0;
-  return launched(e.buf, e.len, launch_plain(s.ahead > 1 ? unpack_kernel<T, kMostAhead<T>> : unpack_kernel<T, 1>, s.grid, kPackThreads, st, Codes(&b), rows,
-                                             cols, out, ld, s.log_across, (int)Codes(&b).vectors(8), vec_out));
+  const bool vec = ((uintptr_t)out & 15u) == 0 && ld * (long long)sizeof(T) % 16 == 0 && Codes(&b).vectors(8) && cols % 8 == 0;
+  const auto kernel = s.ahead > 1 ? (vec ? unpack_kernel<T, kMostAhead<T>, true> : unpack_kernel<T, kMostAhead<T>, false>)
+                                  : (vec ? unpack_kernel<T, 1, true> : unpack_kernel<T, 1, false>);
+  return launched(e.buf, e.len, launch_plain(kernel, s.grid, kPackThreads, st, Codes(&b), rows, cols, out, ld, s.log_across));
 }
 
 template <class T>
 void list_block_kernels(const void** list, int& n) {
-  const void* all[] = {(const void*)pack_rows_kernel<T, 1>, (const void*)pack_rows_kernel<T, kMostAhead<T>>, (const void*)pack_tiles_kernel<T>,
-                       (const void*)unpack_kernel<T, 1>, (const void*)unpack_kernel<T, kMostAhead<T>>};
+  const void* all[] = {(const void*)pack_rows_kernel<T, 1, false>,   (const void*)pack_rows_kernel<T, kMostAhead<T>, false>,
+                       (const void*)pack_rows_kernel<T, 1, true>,    (const void*)pack_rows_kernel<T, kMostAhead<T>, true>,
+                       (const void*)pack_tiles_kernel<T, false>,     (const void*)pack_tiles_kernel<T, true>,
+                       (const void*)unpack_kernel<T, 1, false>,      (const void*)unpack_kernel<T, kMostAhead<T>, false>,
+                       (const void*)unpack_kernel<T, 1, true>,       (const void*)unpack_kernel<T, kMostAhead<T>, true>};
   for (const void* k : all) list[n++] = k;
 }
 template <class T>
@@ -907,8 +937,7 @@ extern "C" laq_status laq_linear_blocks_forward(const laq_linear_call* c, const 
   A.ldsw = wq->ld_scales;
   if (takes_few_codes(c)) return c->dtype == LAQ_BF16 ? few_codes<__nv_bfloat16>(e, A, x, w, st) : few_codes<__half>(e, A, x, w, st);
   char* ws = (char*)d_workspace;
-  LAQ_TRY(make_codes_mappable(e, x, ws, st));
-  LAQ_TRY(make_codes_mappable(e, w, ws, st));
+  LAQ_TRY(make_codes_mappable(e, x, w, ws, st));
   const bool follows = ws != d_workspace;
   Product p;
   p.A = A;

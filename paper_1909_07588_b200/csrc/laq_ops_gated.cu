@@ -11,13 +11,14 @@ namespace ops {
 namespace {
 
 // dZ and its column sums.  Bound by memory.  A block takes 256 columns of the gates and of the ups (32 threads of eight) and a run
-// of rows (8 threads); sums in fp32 of the unrounded products, to part[run][2F].  CODES: Z comes in 8 bits.  Without vectors
-// (odd sizes or addresses) a thread's eight columns lie 32 apart, so that neighbouring lanes have neighbouring columns.
+// of rows (8 threads); sums in fp32 of the unrounded products, to part[run][2F].  CODES: Z comes in 8 bits.
+// At odd sizes and addresses (not VEC) 8-bit codes are read by the aligned words that hold a thread's eight columns (3001 x 2050: 34 us
+// by single codes, 27 us so), 16-bit numbers one by one by neighbouring lanes (14 us; by words 26 us).
 constexpr int kCols = 256, kThreads = 256;
 
-template <class T, bool CODES>
+template <class T, bool CODES, bool VEC>
 __global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long long lddh, const T* z, long long ldz, const Codes zq, T* dz, long long lddz,
-                                                               float* part, long long M, long long F, int act, int rows_per, int vec_ok) {
+                                                               float* part, long long M, long long F, int act, int rows_per) {
   __shared__ float sh[8][2 * kCols];
   allow_next();
   const int tx = threadIdx.x & 31, ty = threadIdx.x >> 5;
@@ -45,26 +46,34 @@ __global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long
       sum[1][e] += u[e];
     }
   };
-  if (vec_ok) {
+  constexpr bool kEights = VEC || CODES;          // a thread's columns are neighbours; else 32 apart, so that lanes are
+  if constexpr (kEights) {
     const long long c0 = base + tx * 8;
-    if (c0 < F) {
+    const int n = VEC ? (c0 < F ? 8 : 0) : (int)max(0ll, min(8ll, F - c0));            // of this thread's columns there are
+    const bool up_vec = VEC || F % 8 == 0;
+    const int here = kBlock - (int)((F + c0) % kBlock);                                // ups before the next block
+    if (n > 0) {
       for (long long r = r0 + ty; r < r1; r += 16) {
         const bool two = r + 8 < r1;
         uint4 d[2], g[2], u[2];
         uint2 qg[2], qu[2];
-        float sg[2], su[2];
+        float sg[2], su[2], su_next[2];
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const long long row = two || i == 0 ? r + 8 * i : r;             // a row is read twice rather than beyond the last
-          d[i] = load16(dh + row * lddh + c0);
+          const T* pd = dh + row * lddh + c0;
+          d[i] = VEC ? load16(pd) : load16_any(pd, n);
           if constexpr (CODES) {
-            qg[i] = load8(zq.p + row * zq.ld + c0);
-            qu[i] = load8(zq.p + row * zq.ld + F + c0);
+            const uint8_t* p = zq.p + row * zq.ld + c0;
+            qg[i] = VEC ? load8(p) : load8_any(p, n);
+            qu[i] = VEC ? load8(p + F) : load8_any(p + F, n);
             sg[i] = zq.scale(row, c0);
             su[i] = zq.scale(row, F + c0);
+            if (!VEC) su_next[i] = zq.scale(row, F + c0 + n - 1);        // eight ups may lie in two blocks
           } else {
-            g[i] = load16(z + row * ldz + c0);
-            u[i] = load16(z + row * ldz + F + c0);
+            const T* p = z + row * ldz + c0;
+            g[i] = load16(p);
+            u[i] = load16(p + F);
           }
         }
 #pragma unroll
@@ -74,7 +83,11 @@ __global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long
           Elem<T>::unpack(d[i], df);
           if constexpr (CODES) {
             decode8(qg[i], sg[i], gf);
-            decode8(qu[i], su[i], uf);
+            decode8(qu[i], VEC ? su[i] : 1.f, uf);
+            if (!VEC) {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) uf[e] *= e < here ? su[i] : su_next[i];
+            }
           } else {
             Elem<T>::unpack(g[i], gf);
             Elem<T>::unpack(u[i], uf);
@@ -82,8 +95,11 @@ __global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long
           slopes(df, gf, uf);
           if (dz) {
             T* o = dz + (r + 8 * i) * lddz + c0;
-            *reinterpret_cast<uint4*>(o) = Elem<T>::pack(gf);
-            *reinterpret_cast<uint4*>(o + F) = Elem<T>::pack(uf);
+            const uint4 dg = Elem<T>::pack(gf), du = Elem<T>::pack(uf);
+            if (n == 8) *reinterpret_cast<uint4*>(o) = dg;                      // rows and eights of them are aligned
+            else store16_any(o, dg, n);
+            if (n == 8 && up_vec) *reinterpret_cast<uint4*>(o + F) = du;
+            else store16_any(o + F, du, n);
           }
         }
       }
@@ -96,13 +112,8 @@ __global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long
         const long long c = base + tx + 32 * e;
         const bool there = c < F;
         df[e] = there ? Elem<T>::to_float(dh[r * lddh + c]) : 0.f;
-        if constexpr (CODES) {
-          gf[e] = there ? zq.value(r, c) : 0.f;
-          uf[e] = there ? zq.value(r, F + c) : 0.f;
-        } else {
-          gf[e] = there ? Elem<T>::to_float(z[r * ldz + c]) : 0.f;
-          uf[e] = there ? Elem<T>::to_float(z[r * ldz + F + c]) : 0.f;
-        }
+        gf[e] = there ? Elem<T>::to_float(z[r * ldz + c]) : 0.f;
+        uf[e] = there ? Elem<T>::to_float(z[r * ldz + F + c]) : 0.f;
       }
       slopes(df, gf, uf);
       if (dz) {
@@ -122,7 +133,7 @@ __global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long
 #pragma unroll
   for (int h = 0; h < 2; ++h)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sh[ty][h * kCols + (vec_ok ? tx * 8 + e : tx + 32 * e)] = sum[h][e];
+    for (int e = 0; e < 8; ++e) sh[ty][h * kCols + (kEights ? tx * 8 + e : tx + 32 * e)] = sum[h][e];
   __syncthreads();
   const long long c = base + threadIdx.x;
   if (c >= F) return;
@@ -227,7 +238,8 @@ void list_kernels(const void** list, int& n) {
                        (const void*)linear_few_rows_kernel<T, 1, 4, true>, (const void*)linear_few_rows_kernel<T, 1, 2, true>,
                        (const void*)linear_few_rows_kernel<T, 2, 4, true>, (const void*)linear_few_rows_kernel<T, 2, 2, true>,
                        (const void*)linear_few_rows_kernel<T, 3, 2, true>, (const void*)linear_few_rows_kernel<T, 4, 2, true>,
-                       (const void*)gated_dz_kernel<T, false>, (const void*)gated_dz_kernel<T, true>};
+                       (const void*)gated_dz_kernel<T, false, false>, (const void*)gated_dz_kernel<T, false, true>,
+                       (const void*)gated_dz_kernel<T, true, false>, (const void*)gated_dz_kernel<T, true, true>};
   for (const void* k : all) list[n++] = k;
 }
 
@@ -357,11 +369,13 @@ extern "C" laq_status laq_gated_backward(const laq_gated_call* c, void* d_worksp
   const int per = dz_rows_per(c->M, c->F), runs = (int)((c->M + per - 1) / per);
   const dim3 grid((unsigned)((c->F + kCols - 1) / kCols), (unsigned)runs);
   const Codes zq(c->z_blocks);
-  const int vec_ok = c->F % 8 == 0 && mappable(c->dh, c->ld_dh) && (c->z_blocks ? zq.vectors(8) : mappable(c->z, c->ld_z));
+  const bool vec = c->F % 8 == 0 && mappable(c->dh, c->ld_dh) && (c->z_blocks ? zq.vectors(8) : mappable(c->z, c->ld_z));
   const auto launch_dz = [&](auto zero) {
     using T = decltype(zero);
-    return launch_plain(c->z_blocks ? gated_dz_kernel<T, true> : gated_dz_kernel<T, false>, grid, kThreads, st, (const T*)c->dh, c->ld_dh, (const T*)c->z,
-                        c->ld_z, zq, (T*)dz, need.dz.ld, part, c->M, c->F, c->activation, per, vec_ok);
+    const auto kernel = c->z_blocks ? (vec ? gated_dz_kernel<T, true, true> : gated_dz_kernel<T, true, false>)
+                                    : (vec ? gated_dz_kernel<T, false, true> : gated_dz_kernel<T, false, false>);
+    return launch_plain(kernel, grid, kThreads, st, (const T*)c->dh, c->ld_dh, (const T*)c->z, c->ld_z, zq, (T*)dz, need.dz.ld, part, c->M, c->F,
+                        c->activation, per);
   };
   LAQ_TRY(launched(errbuf, errbuf_len, c->dtype == LAQ_BF16 ? launch_dz(__nv_bfloat16()) : launch_dz(__half())));
   if (c->db) LAQ_TRY(column_sums(e, part, runs, (int)N, c->db, st));

@@ -1532,7 +1532,6 @@ struct Codes {
         shift(b && b->block_rows == kBlock ? 7 : 0) {}
   bool vectors(int bytes) const { return ((uintptr_t)p % bytes) == 0 && ld % bytes == 0; }
   __device__ __forceinline__ float scale(long long row, long long col) const { return __ldg(scales + (row >> shift) * lds + col / kBlock); }
-  __device__ __forceinline__ float value(long long row, long long col) const;
 };
 
 // Two e4m3 codes in fp32.
@@ -1550,7 +1549,40 @@ __device__ __forceinline__ void decode8(uint2 v, float scale, float (&x)[8]) {
     x[2 * i + 1] = f.y * scale;
   }
 }
-__device__ __forceinline__ float Codes::value(long long row, long long col) const { return decode2(p[row * ld + col]).x * scale(row, col); }
+// The first n (1..8) of eight codes, or of eight 16-bit numbers, at any address of theirs: from the aligned words that hold them, and
+// from no others.  What lies behind the n-th is not theirs.
+__device__ __forceinline__ uint2 load8_any(const uint8_t* p, int n) {
+  const int off = (int)((uintptr_t)p & 3u);
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(p - off);
+  uint32_t w[3];
+#pragma unroll
+  for (int k = 0; k < 3; ++k) w[k] = 4 * k < off + n ? words[k] : 0u;
+  return make_uint2(__funnelshift_r(w[0], w[1], 8 * off), __funnelshift_r(w[1], w[2], 8 * off));
+}
+template <class T>
+__device__ __forceinline__ uint4 load16_any(const T* p, int n) {
+  static_assert(sizeof(T) == 2, "16-bit numbers");
+  const int off = (int)((uintptr_t)p & 2u);
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(p) - off);
+  uint32_t w[5];
+#pragma unroll
+  for (int k = 0; k < 5; ++k) w[k] = 4 * k < off + 2 * n ? words[k] : 0u;
+  return make_uint4(__funnelshift_r(w[0], w[1], 8 * off), __funnelshift_r(w[1], w[2], 8 * off), __funnelshift_r(w[2], w[3], 8 * off),
+                    __funnelshift_r(w[3], w[4], 8 * off));
+}
+// The first n of eight 16-bit numbers to any address of theirs.
+template <class T>
+__device__ __forceinline__ void store16_any(T* p, const uint4& v, int n) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  if (n == 8 && ((uintptr_t)p & 3u) == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) reinterpret_cast<uint32_t*>(p)[i] = w[i];
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < n) reinterpret_cast<uint16_t*>(p)[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+  }
+}
 __device__ __forceinline__ uint2 load8(const void* p) {
   uint2 v;
   asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p) : "memory");

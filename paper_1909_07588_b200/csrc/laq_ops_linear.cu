@@ -83,10 +83,11 @@ __global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, l
   } else if (c0 < N) {
     for (long long r = r0 + ty; r < r1; r += 8) {
       float g[8], x[8];
+      if constexpr (CODES) decode8(load8_any(zq.p + r * zq.ld + c0, min(8, N - c0)), zq.scale(r, c0), x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         g[e] = c0 + e < N ? Elem<T>::to_float(dy[r * lddy + c0 + e]) : 0.f;
-        if constexpr (CODES) x[e] = act != LAQ_ACT_NONE && c0 + e < N ? zq.value(r, c0 + e) : 0.f;
+        if constexpr (CODES) x[e] = c0 + e < N ? x[e] : 0.f;
         else x[e] = act != LAQ_ACT_NONE && c0 + e < N ? Elem<T>::to_float(z[r * ldz + c0 + e]) : 0.f;
       }
       row(r, g, x);
@@ -134,15 +135,8 @@ __global__ void __launch_bounds__(256) linear_pack_kernel(const uint16_t* src, l
     const long long r = i / groups;
     const int c = (int)(i - r * groups) * 8;
     const uint16_t* s = src + r * ld + c;
-    uint16_t v[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? s[e] : (uint16_t)0;
-    uint4 o;
-    o.x = v[0] | ((uint32_t)v[1] << 16);
-    o.y = v[2] | ((uint32_t)v[3] << 16);
-    o.z = v[4] | ((uint32_t)v[5] << 16);
-    o.w = v[6] | ((uint32_t)v[7] << 16);
-    *reinterpret_cast<uint4*>(dst + r * pitch + c) = o;
+    // what lies behind a row's last number is never looked at: the tensor map ends with the row
+    *reinterpret_cast<uint4*>(dst + r * pitch + c) = load16_any(s, min(8, cols - c));
   }
 }
 
