@@ -88,13 +88,13 @@ __device__ __forceinline__ float largest_finite(const float (&x)[8]) {
 
 template <bool VEC>
 __device__ __forceinline__ void store_codes(uint8_t* p, uint2 codes, int n) {
-  if (VEC) {
+  if constexpr (VEC) {
     if (n) *reinterpret_cast<uint2*>(p) = codes;
-    return;
-  }
+  } else {
 #pragma unroll
-  for (int e = 0; e < 8; ++e)
-    if (e < n) p[e] = (uint8_t)((e < 4 ? codes.x : codes.y) >> (8 * (e & 3)));
+    for (int e = 0; e < 8; ++e)
+      if (e < n) p[e] = (uint8_t)((e < 4 ? codes.x : codes.y) >> (8 * (e & 3)));
+  }
 }
 
 // A scale a row and 128 columns: 16 threads take a block.  Bound by memory.  A thread block has 16 such groups, side by side
@@ -332,15 +332,18 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
 
 // ---- the product of two matrices of codes ----------------------------------------------------------------------------------
 // A tile of 128 rows (256 on a pair of SMs) and NT columns.  The tensor cores add up one block of 128 at a time, into two accumulators
-// by turns, and sixteen warps add its sums, times the block's scales, to their own: one fused multiply-add of two numbers for two
-// elements, since a row's scale and a column tile's are one number for a thread's NT / 4 columns of its row.  The sums take up to 64
+// by turns, and sixteen warps add its sums, times the block's scales, to their own: one fused multiply-add an element, since a row's
+// scale and a column tile's are one number for a thread's NT / 4 columns of its row.  (Two elements an instruction are slower: their
+// register pairs have to be put together first.)  The sums take up to 64
 // registers of a thread; the first four warps (a loader, the tensor cores' and two that bring the scales) leave theirs to them:
 // 128 x 32 + 512 x 112 of the block's 640 x 96.  The scales come through shared memory, eight blocks at a time: a load of one block's
 // scale by each lane touches 32 sectors, and the adding warps' own had cost a third of the time.
 constexpr int kAdders = 16, kFirstAdder = 4, kCodesThreads = 32 * (kFirstAdder + kAdders), kFewRegisters = 32, kManyRegisters = 112;
 constexpr int kScaleGroup = 8;                                        // blocks whose scales come together
 constexpr int kScaleFloats = kScaleGroup * (kTileM + 2);              // a group's: of 128 rows and of two column tiles
-constexpr int kCodesStaging = kAdders * 2048 + 2 * kScaleFloats * 4;
+// What an adding warp hands over to itself, or its part of a result that leaves by a copy: 32 rows of 64 columns in 16 bits.
+__host__ __device__ constexpr int handed_bytes(bool copies) { return copies ? 4096 : 2048; }
+constexpr int codes_staging(bool copies) { return kAdders * handed_bytes(copies) + 2 * kScaleFloats * 4; }
 
 __device__ __forceinline__ void mma_codes_pair(uint32_t d_tmem, uint64_t da, uint64_t db, uint32_t idesc, uint32_t accumulate) {
   asm volatile(
@@ -358,17 +361,27 @@ __device__ __forceinline__ void arrive_lightly(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
 
+// A warp's results of 32 rows and 64 columns to memory (what lies outside Y is left out), and the end of all such copies' reading.
+__device__ __forceinline__ void copy_out(const CUtensorMap* map, uint32_t from, int x, int y) {
+  asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(from), "r"(x), "r"(y) : "memory");
+  asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+}
+__device__ __forceinline__ void copies_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
+
 // 32 rows of four 16-byte pieces in shared memory, permuted so that a warp writes 32 rows and reads along rows without bank conflicts.
 __device__ __forceinline__ int narrow_piece(int row, int p) { return row * 4 + (p ^ ((row >> 1) & 3)); }
 
-template <class T, bool PAIR, int NT>
+template <class T, bool PAIR, int NT, bool COPIES>
 __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                                                                      const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmR,
                                                                       const GemmArgs A) {
   extern __shared__ unsigned char codes_smem_raw[];
-  __shared__ uint64_t bars[2 * kMaxStages + 9];
+  __shared__ uint64_t bars[2 * kMaxStages + 9], residual_bars[kAdders];
   __shared__ uint32_t tmem_base_sh;
   __shared__ int abort_sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, stages = A.stages, nkb = A.nkb;
+  constexpr int kHanded = handed_bytes(COPIES);
+  static_assert(!COPIES || NT == 256, "a warp's 64 columns are a copy's 128 bytes");
   const uint32_t base = umma::smem_u32(codes_smem_raw), smem0 = (base + 1023u) & ~1023u;
   constexpr int b_rows = PAIR ? NT / 2 : NT;
   constexpr uint32_t a_bytes = kTileM * kBlock, st_bytes = a_bytes + b_rows * kBlock;
@@ -377,7 +390,7 @@ __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __gr
   const uint32_t full0 = umma::smem_u32(&bars[0]), empty0 = umma::smem_u32(&bars[kMaxStages]);
   const uint32_t acc_full0 = umma::smem_u32(&bars[2 * kMaxStages]), acc_empty0 = acc_full0 + 16, drain = acc_full0 + 32;
   const uint32_t scales_full0 = drain + 8, scales_empty0 = drain + 24;
-  float* const staged = reinterpret_cast<float*>(codes_smem_raw + (smem0 - base) + stages * st_bytes + kAdders * 2048);     // two groups' scales
+  float* const staged = reinterpret_cast<float*>(codes_smem_raw + (smem0 - base) + stages * st_bytes + kAdders * kHanded);     // two groups' scales
   if (threadIdx.x == 0) {
     for (int s = 0; s < stages; ++s) {
       umma::mbar_init(full0 + 8 * s, 1);
@@ -389,6 +402,7 @@ __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __gr
       umma::mbar_init(scales_full0 + 8 * b, 2);
       umma::mbar_init(scales_empty0 + 8 * b, kAdders);
     }
+    for (int i = 0; i < kAdders; ++i) umma::mbar_init(umma::smem_u32(&residual_bars[i]), 1);
     umma::mbar_init(drain, 1);
     abort_sh = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -531,64 +545,127 @@ __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __gr
     const int q = warp & 3, c_first = (warp - kFirstAdder) / 4 * kCols;
     const uint32_t mine = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)c_first;
     const uint32_t back0 = PAIR ? of_leader(acc_empty0) : acc_empty0;
-    uint4* stage4 = reinterpret_cast<uint4*>(codes_smem_raw + (smem0 - base) + stages * st_bytes) + (warp - kFirstAdder) * 128;      // 2 KB
+    uint4* stage4 = reinterpret_cast<uint4*>(codes_smem_raw + (smem0 - base) + stages * st_bytes + (warp - kFirstAdder) * kHanded);
+    // COPIES: results leave by copies of their own, and residuals come by such, in the warp's 4 KB: rows of 128 bytes, their 16-byte
+    // pieces permuted by the copies' swizzle.
+    const uint32_t handed = umma::smem_u32(stage4), residual_bar = umma::smem_u32(&residual_bars[warp - kFirstAdder]);
+    int tile_n = 0;
     const float* my_scale = staged + q * 32 + lane;
     const float* tile_scale = staged + kScaleGroup * kTileM + (c_first >= NT / 2 ? kScaleGroup : 0);
-    int n = 0, g = 0;
+    // The next accumulator (0 or 1) and group of scales (0 or 1), and the phases of their barriers.  What is done once for each block of
+    // 128 is kept short: sixteen warps' instructions, and not the tensor cores, set the pace.
+    uint32_t acc = 0, acc_phase = 0, group = 0, group_phase = 0;
     bool ok = true;
+    const auto wait_for = [&](uint32_t bar, uint32_t phase, uint32_t code) {
+      bool there = umma::mbar_try_wait(bar, phase);
+      if (!there) there = umma::mbar_wait_abortable(bar, phase, limit, abort_flag, A.status, code);
+      return (bool)__all_sync(0xffffffffu, there);
+    };
     for (int w = first; w < tiles && ok; w += step) {
-      f32x2 sum[kPieces][8];
+      float sum[kPieces][16];
 #pragma unroll
       for (int p = 0; p < kPieces; ++p)
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[p][e] = 0ull;
-      for (int kb = 0; kb < nkb; ++kb, ++n) {
-        const int in = kb % kScaleGroup, at = (g & 1) * kScaleFloats;
-        if (in == 0) {
-          ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(scales_full0 + 8 * (g & 1), (uint32_t)(g >> 1) & 1u, limit, abort_flag, A.status, 16u));
-          if (!ok) break;
+        for (int e = 0; e < 16; ++e) sum[p][e] = 0.f;
+      for (int k0 = 0; k0 < nkb && ok; k0 += kScaleGroup) {
+        if (COPIES && A.residual && k0 == (nkb > kScaleGroup ? kScaleGroup : 0) && lane == 0) {      // the last tile's results have left, or nearly
+          int i0, j0;
+          tile_of<PAIR>(A, w, i0, j0);
+          copies_read();
+          umma::mbar_expect_tx(residual_bar, 4096);
+          umma::tma_load_2d(handed, &tmR, residual_bar, j0 + c_first, i0 + half * kTileM + q * 32);
         }
-        const float scale = my_scale[at + in * kTileM] * tile_scale[at + in];
-        const f32x2 both = pair_of(scale, scale);
-        const uint32_t b = (uint32_t)n & 1u;
-        ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(acc_full0 + 8 * b, (uint32_t)(n >> 1) & 1u, limit, abort_flag, A.status, 8u));
+        ok = wait_for(scales_full0 + 8 * group, group_phase, 16u);
         if (!ok) break;
-        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        if (in == kScaleGroup - 1 || kb == nkb - 1) {        // the group's scales have been read (the scale above, before the barrier's wait)
-          __syncwarp();
-          if (lane == 0) umma::mbar_arrive(scales_empty0 + 8 * (g & 1));
-          ++g;
-        }
-        const uint32_t t0 = mine + b * NT;
-#pragma unroll
-        for (int p = 0; p < kPieces; p += 2) {
-          if (kPieces == 1) {
+        const float *mine_at = my_scale + group * kScaleFloats, *tile_at = tile_scale + group * kScaleFloats;
+        const int n = min(kScaleGroup, nkb - k0);
+        for (int in = 0; in < n; ++in, mine_at += kTileM, ++tile_at) {
+          const float scale = *mine_at * *tile_at;
+          ok = wait_for(acc_full0 + 8 * acc, acc_phase, 8u);
+          if (!ok) break;
+          asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+          const uint32_t t0 = mine + acc * NT;
+          // the accumulator goes back as soon as its last columns are in registers, before they are added
+          const auto give_back = [&]() {
+            asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+              if (PAIR) arrive_lightly(back0 + 8 * acc);
+              else umma::mbar_arrive(back0 + 8 * acc);
+            }
+          };
+          if constexpr (kPieces == 1) {
             uint32_t v[16];
             tmem_load(t0, v);
+            give_back();
 #pragma unroll
-            for (int e = 0; e < 8; ++e) sum[0][e] = fma2(pair_of(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), both, sum[0][e]);
+            for (int e = 0; e < 16; ++e) sum[0][e] = fmaf(__uint_as_float(v[e]), scale, sum[0][e]);
           } else {
-            uint32_t v[32];
-            tmem_load(t0 + 16 * p, v);
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              f32x2& to = sum[kPieces == 1 ? 0 : p + e / 8][e % 8];
-              to = fma2(pair_of(__uint_as_float(v[2 * e]), __uint_as_float(v[2 * e + 1])), both, to);
+            for (int p = 0; p < kPieces; p += 2) {
+              uint32_t v[32];
+              tmem_load(t0 + 16 * p, v);
+              if (p + 2 == kPieces) give_back();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) sum[p + e / 16][e % 16] = fmaf(__uint_as_float(v[e]), scale, sum[p + e / 16][e % 16]);
             }
           }
+          acc ^= 1u;
+          acc_phase ^= acc ^ 1u;
         }
-        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-        __syncwarp();
-        if (lane == 0) {
-          if (PAIR) arrive_lightly(back0 + 8 * b);
-          else umma::mbar_arrive(back0 + 8 * b);
-        }
+        if (!ok) break;
+        __syncwarp();                      // all lanes have read the group's scales
+        if (lane == 0) umma::mbar_arrive(scales_empty0 + 8 * group);
+        group ^= 1u;
+        group_phase ^= group ^ 1u;
       }
       if (!ok) break;
       int i0, j0;
       tile_of<PAIR>(A, w, i0, j0);
       i0 += half * kTileM + q * 32;
       j0 += c_first;
+      if constexpr (COPIES) {
+        if (A.residual) {
+          ok = __all_sync(0xffffffffu, umma::mbar_wait_abortable(residual_bar, (uint32_t)tile_n & 1u, limit, abort_flag, A.status, 32u));
+          if (!ok) break;
+        } else {
+          if (lane == 0) copies_read();
+          __syncwarp();
+        }
+        ++tile_n;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {                      // a lane's row, eight columns at a time
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = sum[c / 2][8 * (c % 2) + e];
+          const int col = j0 + 8 * c;
+          if (A.bias) {
+            const T* bias = reinterpret_cast<const T*>(A.bias) + col;
+            float b[8];
+            if (col + 8 <= A.J) {
+              Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(bias)), b);
+            } else {
+#pragma unroll
+              for (int e = 0; e < 8; ++e) b[e] = col + e < A.J ? Elem<T>::to_float(bias[e]) : 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += b[e];
+          }
+          activate(x, A.act);
+          uint4* at = stage4 + lane * 8 + (c ^ (lane & 7));
+          if (A.residual) {
+            float y[8];
+            Elem<T>::unpack(*at, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] += y[e];
+          }
+          *at = Elem<T>::pack(x);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        __syncwarp();
+        if (lane == 0 && i0 < A.I && j0 < A.J) copy_out(&tmY, handed, j0, i0);
+        continue;
+      }
       const bool vec = all_vectors(A, false), whole = vec && i0 + 32 <= A.I && j0 + kCols <= A.J;
       // pieces of 32 x 16 through shared memory, after which two lanes share a row
       const long long row0 = i0 + (lane >> 1);
@@ -610,17 +687,14 @@ __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __gr
         }
         __syncwarp();
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
-          float x0, x1, x2, x3;
-          ops::split(sum[0][e], x0, x1);
-          ops::split(sum[0][e + 1], x2, x3);
-          stage4[narrow_piece(lane, e / 2)] = make_uint4(__float_as_uint(x0), __float_as_uint(x1), __float_as_uint(x2), __float_as_uint(x3));
-        }
+        for (int e = 0; e < 16; e += 4)
+          stage4[narrow_piece(lane, e / 4)] = make_uint4(__float_as_uint(sum[0][e]), __float_as_uint(sum[0][e + 1]), __float_as_uint(sum[0][e + 2]),
+                                                         __float_as_uint(sum[0][e + 3]));
         // the next piece moves up: no register can be chosen by a number that is only known at run time
 #pragma unroll
         for (int m = 0; m + 1 < kPieces; ++m)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) sum[m][e] = sum[m + 1][e];
+          for (int e = 0; e < 16; ++e) sum[m][e] = sum[m + 1][e];
         __syncwarp();
         if (whole) {
           float b[8];
@@ -663,6 +737,14 @@ __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __gr
         }
       }
     }
+    if (COPIES && lane == 0) {
+      if (!ok && A.residual) {             // given up: a residual that was asked for still lands here
+        for (uint32_t it = 0; it < kStarvedLimit && !umma::mbar_try_wait(residual_bar, (uint32_t)tile_n & 1u); ++it) {
+        }
+      }
+      asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
+    }
+    __syncwarp();
   }
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   if (PAIR) {
@@ -781,9 +863,10 @@ void list_block_kernels(const void** list, int& n) {
 }
 template <class T>
 void list_product_kernels(const void** list, int& n) {
-  const void* all[] = {(const void*)linear_gemm_kernel<T, true, false, false, false, kCodes>, (const void*)codes_gemm_kernel<T, true, 256>,
-                       (const void*)codes_gemm_kernel<T, true, 128>, (const void*)codes_gemm_kernel<T, false, 128>,
-                       (const void*)codes_gemm_kernel<T, false, 64>, (const void*)linear_few_codes_kernel<T, 1>,
+  const void* all[] = {(const void*)linear_gemm_kernel<T, true, false, false, false, kCodes>, (const void*)codes_gemm_kernel<T, true, 256, true>,
+                       (const void*)codes_gemm_kernel<T, true, 256, false>, (const void*)codes_gemm_kernel<T, true, 128, false>,
+                       (const void*)codes_gemm_kernel<T, false, 128, false>, (const void*)codes_gemm_kernel<T, false, 64, false>,
+                       (const void*)linear_few_codes_kernel<T, 1>,
                        (const void*)linear_few_codes_kernel<T, 2>, (const void*)linear_few_codes_kernel<T, 3>, (const void*)linear_few_codes_kernel<T, 4>};
   for (const void* k : all) list[n++] = k;
 }
@@ -794,16 +877,23 @@ laq_status check_matrix(const Err& e, int64_t rows, int64_t cols) {
   return LAQ_OK;
 }
 
-template <class T, bool PAIR, int NT>
+template <class T, bool PAIR, int NT, bool COPIES>
 laq_status launch_codes(const Err& e, const Product& p, bool follows, cudaStream_t st) {
   static Raised raised;
-  return launch_tiles(e, codes_gemm_kernel<T, PAIR, NT>, raised, kCodesThreads, PAIR, false, kCodesStaging, p.ma, p.mb, p.A, follows, st);
+  CUtensorMap my = p.ma, mr = p.ma;                // unused without copies or a residual
+  if (COPIES && (!umma::make_map_bf16_2d(&my, p.A.out, p.A.I, p.A.J, p.A.ldo * 2, 32) ||
+                 (p.A.residual && !umma::make_map_bf16_2d(&mr, p.A.residual, p.A.I, p.A.J, p.A.ldr * 2, 32))))
+    return fail(e.buf, e.len, LAQ_ECUDA, "a tensor map was refused");
+  return launch_tiles<CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap>(e, codes_gemm_kernel<T, PAIR, NT, COPIES>, raised, kCodesThreads, PAIR, false,
+                                                                          codes_staging(COPIES), follows, st, p.A, p.ma, p.mb, my, mr);
 }
 template <class T>
 laq_status launch_product(const Err& e, const Product& p, bool follows, cudaStream_t st) {
   if (p.pl.swap) return launch_gemm<T, true, false, false, false, kCodes>(e, p.ma, p.mb, p.A, follows, st);
-  if (p.pl.pair) return p.pl.nt == 256 ? launch_codes<T, true, 256>(e, p, follows, st) : launch_codes<T, true, 128>(e, p, follows, st);
-  return p.pl.nt == 128 ? launch_codes<T, false, 128>(e, p, follows, st) : launch_codes<T, false, 64>(e, p, follows, st);
+  if (!p.pl.pair) return p.pl.nt == 128 ? launch_codes<T, false, 128, false>(e, p, follows, st) : launch_codes<T, false, 64, false>(e, p, follows, st);
+  if (p.pl.nt == 128) return launch_codes<T, true, 128, false>(e, p, follows, st);
+  const bool copies = !p.A.z && mappable(p.A.out, p.A.ldo) && mappable(p.A.residual, p.A.ldr) && mappable(p.A.bias, 8);
+  return copies ? launch_codes<T, true, 256, true>(e, p, follows, st) : launch_codes<T, true, 256, false>(e, p, follows, st);
 }
 
 bool takes_few_codes(const laq_linear_call* c) { return !(c->flags & LAQ_LINEAR_STARVE) && c->M <= kFewRows; }

@@ -1233,6 +1233,7 @@ struct Plan {
 };
 
 constexpr int kCodesRing = 160 * 1024;       // of the 8-bit product's kernel
+constexpr int kWideCodesStages = 4;          // of its tiles of 256 columns, which have results of 64 KB beside the ring
 
 // Tile width, split, pairs and orientation by an estimate of the time in SM cycles, whose constants were fitted to all of
 // these forms measured on 26 products (1 to 16384 rows): a stage costs the larger of its products (2.7 cycles per column of
@@ -1259,7 +1260,7 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
     for (int nt : widths) {
       if (mode == kCodes && !swap && nt == 256 && rows > 1) {          // pairs alone have tiles of 256 columns
         const double cost = 10000 + (double)((row_pairs * ((j + nt - 1) / nt) + kSMs / 2 - 1) / (kSMs / 2)) * (nkb * 960.0 + 8000);
-        if (cost < best.cost) best = Plan{0, nt, 1, kCodesRing / ((kTileM + nt / 2) * kBlockK * 2), 1, cost};
+        if (cost < best.cost) best = Plan{0, nt, 1, kWideCodesStages, 1, cost};
       }
       if (bmn && nt % 64) continue;
       if (mode == kGated && !swap && nt % 64) continue;          // pieces of 32 gates and as many ups
@@ -1340,9 +1341,10 @@ inline laq_status raise_shared_memory(const Err& e, const void* kernel, Raised& 
   }
   return LAQ_OK;
 }
-typedef void (*GemmKernel)(const CUtensorMap, const CUtensorMap, const GemmArgs);
-inline laq_status launch_tiles(const Err& e, GemmKernel kernel, Raised& raised, unsigned threads, bool pair, bool joined, int staging, const CUtensorMap& ma,
-                               const CUtensorMap& mb, const GemmArgs& A, bool follows, cudaStream_t st) {
+// A kernel of maps and, last, the arguments that say how many tiles there are.
+template <class... Maps>
+laq_status launch_tiles(const Err& e, void (*kernel)(Maps..., const GemmArgs), Raised& raised, unsigned threads, bool pair, bool joined, int staging,
+                        bool follows, cudaStream_t st, const GemmArgs& A, const Maps&... maps) {
   const size_t smem = (size_t)A.stages * (kTileM + (pair ? A.nt / 2 : A.nt)) * kBlockK * 2 + staging + 1024;
   const int per_tile = pair ? 2 : A.split;
   {
@@ -1368,7 +1370,7 @@ inline laq_status launch_tiles(const Err& e, GemmKernel kernel, Raised& raised, 
     at[cfg.numAttrs].val.programmaticStreamSerializationAllowed = 1;
     ++cfg.numAttrs;
   }
-  return launched(e.buf, e.len, cudaLaunchKernelEx(&cfg, kernel, ma, mb, A));
+  return launched(e.buf, e.len, cudaLaunchKernelEx(&cfg, kernel, maps..., A));
 }
 
 template <class T, bool TRANS, bool PAIR, bool OUT32, bool LONG, int MODE = kPlain>
@@ -1376,8 +1378,9 @@ laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& m
                        cudaStream_t st) {
   static Raised raised;
   const bool joined = A.split > 1 || (MODE == kGated && TRANS);
-  return launch_tiles(e, linear_gemm_kernel<T, TRANS, PAIR, OUT32, LONG, MODE>, raised, kGemmThreads, PAIR, joined,
-                      MODE == kCodes ? kEpiWarps * kScaleTable * 4 : TRANS || A.split > 1 ? 0 : kStaging, ma, mb, A, follows, st);
+  const int staging = MODE == kCodes ? kEpiWarps * kScaleTable * 4 : TRANS || A.split > 1 ? 0 : kStaging;
+  return launch_tiles<CUtensorMap, CUtensorMap>(e, linear_gemm_kernel<T, TRANS, PAIR, OUT32, LONG, MODE>, raised, kGemmThreads, PAIR, joined, staging, follows,
+                                                st, A, ma, mb);
 }
 
 struct Epilogue {
