@@ -1259,7 +1259,7 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
     static const int widths[] = {16, 32, 64, 96, 112, 128, 160, 192, 208, 224, 256};
     for (int nt : widths) {
       if (mode == kCodes && !swap && nt == 256 && rows > 1) {          // pairs alone have tiles of 256 columns
-        const double cost = 10000 + (double)((row_pairs * ((j + nt - 1) / nt) + kSMs / 2 - 1) / (kSMs / 2)) * (nkb * 960.0 + 8000);
+        const double cost = 10000 + (double)((row_pairs * ((j + nt - 1) / nt) + kSMs / 2 - 1) / (kSMs / 2)) * (nkb * 900.0 + 6000);
         if (cost < best.cost) best = Plan{0, nt, 1, kWideCodesStages, 1, cost};
       }
       if (bmn && nt % 64) continue;
@@ -1292,7 +1292,7 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
           const long long waves = split == 8 ? (blocks + 127) / 128 : split == 4 ? (blocks + 135) / 136 : (blocks + kSMs - 1) / kSMs;
           cost = waves * (mode == kCodes ? 13000 + 112.0 * nt + kb * (700.0 + nt) : swap ? 13500 + 95.0 * nt + kb * 450.0 : 16000 + 24.0 * nt + main);
         } else if (mode == kCodes) {
-          cost = 10000 + (double)((tiles + kSMs - 1) / kSMs) * (nt == 64 ? kb * 720.0 + 1800 : kb * 870.0 + 3700);
+          cost = 10000 + (double)((tiles + kSMs - 1) / kSMs) * (nt == 64 ? kb * 820.0 + 1800 : kb * 930.0 + 3700);
         } else if (mode == kGated) {
           cost = 10000 + persistent((double)((tiles + kSMs - 1) / kSMs), main, epi);
         } else if (!joined) {
@@ -1311,7 +1311,7 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
         if (stages > kMaxStages) stages = kMaxStages;
         const double main = nkb * (mma > half / 60.0 ? mma : half / 60.0);
         const double waves = (double)((row_pairs * cols + kSMs / 2 - 1) / (kSMs / 2));
-        const double cost = mode == kCodes ? 10000 + waves * (nkb * 750.0 + 4000) : (mode == kGated ? 14500 : 4500) + persistent(waves, main, epi);
+        const double cost = mode == kCodes ? 10000 + waves * (nkb * 790.0 + 4500) : (mode == kGated ? 14500 : 4500) + persistent(waves, main, epi);
         if (cost < best.cost) best = Plan{0, nt, 1, stages, 1, cost};
       }
     }

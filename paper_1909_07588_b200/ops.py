@@ -25,7 +25,7 @@ import threading
 import torch
 
 from . import laq
-from .laq import LAQ_OK, LAQ_ETIMEOUT, LaqError
+from .laq import LAQ_OK, LAQ_ETIMEOUT, LAQ_EWORKSPACE, LaqError
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3}
@@ -57,10 +57,12 @@ def _check(t, name, index=None, dtype=None):
 
 def _rows(t, name, index=None, dtype=None, shape=None):
     """A matrix with unit stride within its rows: (pointer, row stride, rows, columns)."""
-    _check(t, name, index, dtype)
-    if t.dim() != 2:
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or (index is not None and t.get_device() != index) or (dtype is not None and t.dtype is not dtype):
+        _check(t, name, index, dtype)
+    size = t.shape
+    if len(size) != 2:
         _refuse("%s must have two dimensions" % name)
-    rows, cols = t.shape
+    rows, cols = size
     if shape is not None and (rows, cols) != shape:
         _refuse("%s must have shape %s, not %s" % (name, shape, (rows, cols)))
     stride, within = t.stride()
@@ -107,10 +109,15 @@ def _on(index, stream, body, *tensors):
     return result
 
 
-def _call(function, *args):
+def _errors():
     err = getattr(_local, "err", None)
     if err is None:
         err = _local.err = C.create_string_buffer(256)
+    return err
+
+
+def _call(function, *args):
+    err = _errors()
     rc = function(*args, err, 256)
     if rc != LAQ_OK:
         raise LaqError(rc, err.value.decode())
@@ -325,6 +332,28 @@ def _layer_call(x, weight, activation, flags, index):
     return c
 
 
+def _result(out, rows, cols, dtype, index, device):
+    """`out` or a new matrix: (matrix, pointer, row stride)."""
+    if out is None:
+        out = _table(rows, cols, dtype, device)
+        return out, out.data_ptr(), cols
+    ptr, stride, _, _ = _rows(out, "out", index, dtype, (rows, cols))
+    return out, ptr, stride
+
+
+def _forward(function, need, call, more, workspace, index, raw):
+    """A call that mostly needs no workspace: one is made if the call asks for it, which it does before it launches anything."""
+    if workspace is None:
+        err = _errors()
+        rc = function(call, *more, None, 0, raw, err, 256)
+        if rc == LAQ_OK:
+            return
+        if rc != LAQ_EWORKSPACE:
+            raise LaqError(rc, err.value.decode())
+    ws, wp, wn = _workspace(need(call, *more, 0), index, workspace)
+    _call(function, call, *more, wp, wn, raw)
+
+
 def _workspace(need, index, given):
     if need == 0:
         return None, None, 0
@@ -453,14 +482,13 @@ def _packed(p, name, index=None, shape=None):
     """A Packed8: (laq_blocks, rows, columns)."""
     if not isinstance(p, Packed8):
         _refuse("%s must be a Packed8" % name)
-    q = laq.laq_blocks()
-    q.codes, q.ld_codes, rows, cols = _rows(p.codes, name + ".codes", index, torch.float8_e4m3fn, shape)
-    q.scales, q.ld_scales, down, across = _rows(p.scales, name + ".scales", p.codes.get_device(), torch.float32)
+    codes, scales = p
+    pc, ld_codes, rows, cols = _rows(codes, name + ".codes", index, torch.float8_e4m3fn, shape)
+    ps, ld_scales, down, across = _rows(scales, name + ".scales", codes.get_device(), torch.float32)
     if across != -(-cols // BLOCK) or (down != rows and down != -(-rows // BLOCK)):
         _refuse("%s.scales must have shape %s or %s, not %s" % (name, (rows, -(-cols // BLOCK)), (-(-rows // BLOCK), -(-cols // BLOCK)),
                                                                (down, across)))
-    q.block_rows = 1 if down == rows else BLOCK
-    return q, rows, cols
+    return laq.laq_blocks(pc, ld_codes, ps, ld_scales, 1 if down == rows else BLOCK), rows, cols
 
 
 def _rows_or_codes(t, name, index, dtype, shape=None):
@@ -476,9 +504,12 @@ def _tensors(t):
 
 
 def _new_packed(rows, cols, tiles, device):
-    """Uninitialised; rows of codes begin 16 bytes apart or multiples of that, as the product reads them best."""
-    codes = torch.empty_strided((rows, cols), (-(-cols // 16) * 16, 1), dtype=torch.float8_e4m3fn, device=device)
-    return Packed8(codes, _table(-(-rows // BLOCK) if tiles else rows, -(-cols // BLOCK), torch.float32, device))
+    """An uninitialised Packed8 and its laq_blocks; rows of codes begin 16 bytes apart or multiples of that, as the product reads
+    them best."""
+    pitch, across = -(-cols // 16) * 16, -(-cols // BLOCK)
+    codes = torch.empty_strided((rows, cols), (pitch, 1), dtype=torch.float8_e4m3fn, device=device)
+    scales = _table(-(-rows // BLOCK) if tiles else rows, across, torch.float32, device)
+    return Packed8(codes, scales), laq.laq_blocks(codes.data_ptr(), pitch, scales.data_ptr(), across, BLOCK if tiles else 1)
 
 
 def pack8(x, tiles=False, out=None, stream=None):
@@ -489,20 +520,20 @@ def pack8(x, tiles=False, out=None, stream=None):
     step of its code alone: 2^-4 of it, or 2^-10 of the scale below 2^-6 of that.  NaN and infinities become NaN.  ``out`` is a
     Packed8 to write to.
     """
-    _check(x, "x")
-    index = x.get_device()
     ptr, stride, rows, cols = _rows(x, "x")
-    dtype = DTYPES.get(x.dtype)
+    index, dtype = x.get_device(), DTYPES.get(x.dtype)
     if dtype is None:
         _refuse("x must be float32, bfloat16 or float16")
     if cols < 1:
         _refuse("x has no columns")
 
     def body(raw):
-        p = _new_packed(rows, cols, tiles, x.device) if out is None else out
-        q, _, _ = _packed(p, "out", index, (rows, cols))
-        if rows > 1 and (q.block_rows != 1) != bool(tiles):
-            _refuse("out.scales are not those of tiles=%s" % bool(tiles))
+        if out is None:
+            p, q = _new_packed(rows, cols, tiles, x.device)
+        else:
+            p, (q, _, _) = out, _packed(out, "out", index, (rows, cols))
+            if rows > 1 and (q.block_rows != 1) != bool(tiles):
+                _refuse("out.scales are not those of tiles=%s" % bool(tiles))
         _call(laq.load_library().laq_pack_blocks, ptr, dtype, rows, cols, stride, C.byref(q), raw)
         return p
 
@@ -523,8 +554,11 @@ def unpack8(packed, dtype=torch.bfloat16, out=None, stream=None):
         _refuse("packed has no columns")
 
     def body(raw):
-        t = _table(rows, cols, dtype, packed.codes.device) if out is None else out
-        ptr, stride, _, _ = _rows(t, "out", index, dtype, (rows, cols))
+        if out is None:
+            t = _table(rows, cols, dtype, packed.codes.device)
+            ptr, stride = t.data_ptr(), cols
+        else:
+            t, (ptr, stride, _, _) = out, _rows(out, "out", index, dtype, (rows, cols))
         _call(laq.load_library().laq_unpack_blocks, C.byref(q), rows, cols, ptr, code, stride, raw)
         return t
 
@@ -557,14 +591,12 @@ def linear8(x, weight, bias=None, activation="none", residual=None, preact=False
 
     def body(raw):
         c.status = _status_word(index).data_ptr()
-        y = _table(M, N, dtype, x.codes.device) if out is None else out
-        c.y, c.ld_y, _, _ = _rows(y, "out", index, dtype, (M, N))
+        y, c.y, c.ld_y = _result(out, M, N, dtype, index, x.codes.device)
         z = None
         if preact:
             z = _table(M, N, dtype, x.codes.device)
             c.z, c.ld_z = z.data_ptr(), N
-        ws, wp, wn = _workspace(L.laq_linear_blocks_workspace_bytes(C.byref(c), xq, wq, 0), index, workspace)
-        _call(L.laq_linear_blocks_forward, C.byref(c), xq, wq, wp, wn, raw)
+        _forward(L.laq_linear_blocks_forward, L.laq_linear_blocks_workspace_bytes, C.byref(c), (C.byref(xq), C.byref(wq)), workspace, index, raw)
         return (y, z) if preact else y
 
     return _on(index, stream, body, *x, *weight, bias, residual, out, workspace)
@@ -592,9 +624,8 @@ def gated(x, weight, bias=None, activation="silu", preact=False, out=None, works
     ``pack8`` of the former.  ``gated_backward`` takes either.
     """
     L = laq.load_library()
-    _check(x, "x")
-    index, dt = x.get_device(), x.dtype
     ptr, ld, M, K = _rows(x, "x")
+    index, dt = x.get_device(), x.dtype
     c = _gated_call(weight, M, K, activation, flags, index, dt)
     c.x, c.ld_x = ptr, ld
     N = 2 * c.F
@@ -604,19 +635,15 @@ def gated(x, weight, bias=None, activation="silu", preact=False, out=None, works
 
     def body(raw):
         c.status = _status_word(index).data_ptr()
-        h = _table(M, c.F, dt, x.device) if out is None else out
-        c.h, c.ld_h, _, _ = _rows(h, "out", index, dt, (M, c.F))
-        z = q = None
+        h, c.h, c.ld_h = _result(out, M, N // 2, dt, index, x.device)
+        z = None
         if preact == "packed":
-            z = _new_packed(M, N, False, x.device)
-            q, _, _ = _packed(z, "z")
-            q.block_rows = 1
+            z, q = _new_packed(M, N, False, x.device)
             c.z_blocks = C.pointer(q)
         elif preact:
             z = _table(M, N, dt, x.device)
             c.z, c.ld_z = z.data_ptr(), N
-        ws, wp, wn = _workspace(L.laq_gated_workspace_bytes(C.byref(c), 0), index, workspace)
-        _call(L.laq_gated_forward, C.byref(c), wp, wn, raw)
+        _forward(L.laq_gated_forward, L.laq_gated_workspace_bytes, C.byref(c), (), workspace, index, raw)
         return (h, z) if preact else h
 
     return _on(index, stream, body, x, weight, bias, out, workspace)
