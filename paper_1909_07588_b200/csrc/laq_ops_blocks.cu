@@ -761,8 +761,7 @@ __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __gr
 }
 
 // Codes that a tensor map cannot describe are copied with a pitch of a multiple of 16 bytes, both operands' in one launch.  A warp
-// takes a row, a lane 16 codes of it at a time, from the aligned words that they lie in.  (Byte by byte and in two launches, 300 x 777
-// and 1025 x 777: OLDUS, so NEWUS.)
+// takes a row, a lane 16 codes of it at a time, from the aligned words that they lie in. 
 struct CodeRows {
   const uint8_t* src;
   uint8_t* dst;
