@@ -291,15 +291,16 @@ laq_status laq_quantize_worker_static(const float* d_g, const float* d_qprev, in
 /* ---- Operators on the way from a worker's samples to its local gradient ----------------------------------------------
  * The models above end at 16 classes and one hidden layer; a larger model's gradients come from outside
  * (LAQ_MODEL_EXTERNAL, laq_set_gradients).  These calls are what such a model needs beside the quantizer: a layer's product
- * with bias, activation and residual, two losses over rows of logits, and the gradients of all three.
+ * with bias, activation and residual, two losses over rows of logits, and the gradients of all three; a gated feed-forward block
+ * and its gradient; matrices in 8 bits, which the gradients read and a layer's product takes.
  *
  * Common rules.  No context: like laq_quantize_worker_static every call takes its stream and, optionally, a HOST buffer for
  * an error text (errbuf, errbuf_len).  All tensors are DEVICE, row-major, on the calling thread's current device (checked
  * for every pointer that the call reads or writes: LAQ_EINVAL otherwise), with unit stride within a row and any row stride
  * (in elements) of at least the row's length; a pointer needs only the alignment of its element.  Calls are asynchronous,
- * allocate nothing, copy nothing to the host and can be captured into a CUDA graph; the first call of a row operator and the
- * first of a layer on a device load the code of all of their kernels, for which the runtime may take device memory (call
- * once with small tensors at start-up where that matters).  Zero rows are allowed and launch nothing.  Results do not depend
+ * allocate nothing, copy nothing to the host and can be captured into a CUDA graph; the first call of a row operator, of a
+ * layer, of a gated block and on 8-bit matrices on a device each load the code of all of their kernels, for which the runtime may take
+ * device memory (call once with small tensors at start-up where that matters).  Zero rows are allowed and launch nothing.  Results do not depend
  * on timing: sums are taken in a fixed order, in fp32, and there are no atomics on device memory. */
 typedef enum {
   LAQ_F32 = 0,
