@@ -13,11 +13,14 @@ namespace {
 // dZ and its column sums.  Bound by memory.  A block takes 256 columns of the gates and of the ups (32 threads of eight) and a run
 // of rows (8 threads); sums in fp32 of the unrounded products, to part[run][2F].  CODES: Z comes in 8 bits.
 // At odd sizes and addresses (not VEC) 8-bit codes are read by the aligned words that hold a thread's eight columns (3001 x 2050: 34 us
-// by single codes, 27 us so), 16-bit numbers one by one by neighbouring lanes (14 us; by words 26 us).
+// by single codes, 14 us so), 16-bit numbers one by one by neighbouring lanes (14 us; by words 26 us).
 constexpr int kCols = 256, kThreads = 256;
+// Blocks that an SM holds: codes at odd places need more registers (3001 x 2050: 17.4 us by three, 13.9 by two; 16-bit numbers in
+// order, 8192 x 4096 with the product behind it: three 91 us, two 96, four 100).
+__host__ __device__ constexpr int blocks_at_once(bool codes, bool vec) { return codes && !vec ? 2 : 3; }
 
 template <class T, bool CODES, bool VEC>
-__global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long long lddh, const T* z, long long ldz, const Codes zq, T* dz, long long lddz,
+__global__ void __launch_bounds__(kThreads, blocks_at_once(CODES, VEC)) gated_dz_kernel(const T* dh, long long lddh, const T* z, long long ldz, const Codes zq, T* dz, long long lddz,
                                                                float* part, long long M, long long F, int act, int rows_per) {
   __shared__ float sh[8][2 * kCols];
   allow_next();
@@ -28,22 +31,31 @@ __global__ void __launch_bounds__(kThreads, 3) gated_dz_kernel(const T* dh, long
   // dG and dU of eight pairs, in place of the gates and the ups
   const auto slopes = [&](const float (&d)[8], float (&g)[8], float (&u)[8]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      float value = g[e], slope = 1.f;
+    for (int e = 0; e < 8; e += 2) {
+      const f32x2 gate = pair_of(g[e], g[e + 1]), up = pair_of(u[e], u[e + 1]), grad = pair_of(d[e], d[e + 1]);
+      f32x2 value = gate, slope = both_of(1.f);
       if (act == LAQ_ACT_RELU) {
-        slope = g[e] > 0.f ? 1.f : (g[e] == g[e] ? 0.f : g[e]);
-        value = max_nan(g[e], 0.f);
+        float a[2], b[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          a[i] = g[e + i] > 0.f ? 1.f : (g[e + i] == g[e + i] ? 0.f : g[e + i]);
+          b[i] = max_nan(g[e + i], 0.f);
+        }
+        slope = pair_of(a[0], a[1]);
+        value = pair_of(b[0], b[1]);
       } else if (act == LAQ_ACT_GELU) {
-        gelu_both(g[e], value, slope);
+        const f32x2 s = gelu_sigmoid2(gate);
+        value = times2(gate, s);
+        slope = fma2(times2(value, one_minus2(s)), gelu_inner2(gate), s);
       } else if (act == LAQ_ACT_SILU) {
-        const float s = sigmoid(g[e]);
-        value = g[e] * s;
-        slope = s * fmaf(g[e], 1.f - s, 1.f);
+        const f32x2 s = sigmoid2(gate);
+        value = times2(gate, s);
+        slope = times2(s, fma2(gate, one_minus2(s), both_of(1.f)));
       }
-      g[e] = d[e] * u[e] * slope;
-      u[e] = d[e] * value;
-      sum[0][e] += g[e];
-      sum[1][e] += u[e];
+      split(times2(times2(grad, up), slope), g[e], g[e + 1]);
+      split(times2(grad, value), u[e], u[e + 1]);
+      sum[0][e] += g[e], sum[0][e + 1] += g[e + 1];
+      sum[1][e] += u[e], sum[1][e + 1] += u[e + 1];
     }
   };
   constexpr bool kEights = VEC || CODES;          // a thread's columns are neighbours; else 32 apart, so that lanes are
@@ -187,12 +199,27 @@ struct ForwardNeeds {
   size_t bytes(const laq_gated_call* c) const { return z_bytes + (takes_few_rows(c) ? 0 : x.pack_bytes() + w.pack_bytes()); }
 };
 
+bool dz_vectors(const laq_gated_call* c) {
+  return c->F % 8 == 0 && mappable(c->dh, c->ld_dh) && (c->z_blocks ? Codes(c->z_blocks).vectors(8) : mappable(c->z, c->ld_z));
+}
+
+// Rows of a run: no more blocks than the SMs hold at once (8192 x 4096 with the product behind it: 592 blocks for 444 places 103 us, so
+// 91 us), and no fewer than 32 rows each.
+int rows_of_a_run(const laq_gated_call* c) {
+  const long long M = c->M, cols = (c->F + kCols - 1) / kCols, fit = blocks_at_once(c->z_blocks != nullptr, dz_vectors(c)) * kSMs / cols;
+  const long long runs = fit > 1 ? fit : 1;
+  long long per = (M + runs - 1) / runs;
+  per = per < 32 ? 32 : per;
+  while ((M + per - 1) / per > 65535) per *= 2;
+  return (int)per;
+}
+
 struct BackwardNeeds {
   size_t dz_bytes, part_bytes, x_bytes;
   Operand x, w, dz;
   explicit BackwardNeeds(const laq_gated_call* c)
       : x{c->x, c->ld_x, c->M, c->K}, w{c->w, c->ld_w, 2 * c->F, c->K}, dz{nullptr, pad8(2 * c->F), c->M, 2 * c->F} {
-    const int per = dz_rows_per(c->M, c->F);
+    const int per = rows_of_a_run(c);
     dz_bytes = c->dx || c->dw ? align256((size_t)c->M * dz.ld * 2) : 0;
     part_bytes = c->db ? align256((size_t)((c->M + per - 1) / per) * 2 * c->F * 4) : 0;
     if (c->x_blocks) x = Operand{nullptr, pad8(c->K), c->M, c->K};
@@ -366,10 +393,10 @@ extern "C" laq_status laq_gated_backward(const laq_gated_call* c, void* d_worksp
   void* dz = need.dz_bytes ? ws : nullptr;
   float* part = c->db ? (float*)(ws + need.dz_bytes) : nullptr;
   ws += need.dz_bytes + need.part_bytes;
-  const int per = dz_rows_per(c->M, c->F), runs = (int)((c->M + per - 1) / per);
+  const int per = rows_of_a_run(c), runs = (int)((c->M + per - 1) / per);
   const dim3 grid((unsigned)((c->F + kCols - 1) / kCols), (unsigned)runs);
   const Codes zq(c->z_blocks);
-  const bool vec = c->F % 8 == 0 && mappable(c->dh, c->ld_dh) && (c->z_blocks ? zq.vectors(8) : mappable(c->z, c->ld_z));
+  const bool vec = dz_vectors(c);
   const auto launch_dz = [&](auto zero) {
     using T = decltype(zero);
     const auto kernel = c->z_blocks ? (vec ? gated_dz_kernel<T, true, true> : gated_dz_kernel<T, true, false>)

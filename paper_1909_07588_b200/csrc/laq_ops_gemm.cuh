@@ -213,20 +213,36 @@ __device__ __forceinline__ void activate(float (&z)[N], int act) {
     for (int e = 0; e < N; ++e) z[e] *= sigmoid(2.f * kGeluC * fmaf(kGeluA * z[e] * z[e], z[e], z[e]));
   }
 }
-__device__ __forceinline__ float slope_silu(float z) {
-  const float s = sigmoid(z);
-  return s * fmaf(z, 1.f - s, 1.f);
+// Slopes, two numbers at a time.  s (1 - s) is 0 long before z^2 passes 400, so that GELU's stays finite however far z is.
+__device__ __forceinline__ f32x2 times2(f32x2 a, f32x2 b) {      // mul2 without its flush of tiny products
+  f32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
 }
-__device__ __forceinline__ float slope_gelu(float z) {
-  const float s = sigmoid(2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
-  // s (1 - s) is 0 long before z^2 passes 400, so that the product stays finite however far z is
-  return fmaf(z * s * (1.f - s), fmaf(6.f * kGeluC * kGeluA, fminf(z * z, 400.f), 2.f * kGeluC), s);
+__device__ __forceinline__ f32x2 both_of(float v) { return pair_of(v, v); }
+__device__ __forceinline__ f32x2 sigmoid2(f32x2 x) {
+  float a, b, ra, rb;
+  split(add2(both_of(1.f), ex2x2(times2(both_of(-1.4426950408889634f), x))), a, b);
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(ra) : "f"(a));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(rb) : "f"(b));
+  return pair_of(ra, rb);
 }
-
-__device__ __forceinline__ void gelu_both(float z, float& value, float& slope) {      // by one sigmoid
-  const float s = sigmoid(2.f * kGeluC * fmaf(kGeluA * z * z, z, z));
-  value = z * s;
-  slope = fmaf(value * (1.f - s), fmaf(6.f * kGeluC * kGeluA, fminf(z * z, 400.f), 2.f * kGeluC), s);
+__device__ __forceinline__ f32x2 one_minus2(f32x2 s) { return fma2(s, both_of(-1.f), both_of(1.f)); }
+__device__ __forceinline__ f32x2 gelu_sigmoid2(f32x2 z) {
+  return sigmoid2(times2(both_of(2.f * kGeluC), fma2(times2(times2(both_of(kGeluA), z), z), z, z)));
+}
+__device__ __forceinline__ f32x2 gelu_inner2(f32x2 z) {
+  float a, b;
+  split(times2(z, z), a, b);
+  return fma2(both_of(6.f * kGeluC * kGeluA), pair_of(fminf(a, 400.f), fminf(b, 400.f)), both_of(2.f * kGeluC));
+}
+__device__ __forceinline__ f32x2 slope_silu2(f32x2 z) {
+  const f32x2 s = sigmoid2(z);
+  return times2(s, fma2(z, one_minus2(s), both_of(1.f)));
+}
+__device__ __forceinline__ f32x2 slope_gelu2(f32x2 z) {
+  const f32x2 s = gelu_sigmoid2(z);
+  return fma2(times2(times2(z, s), one_minus2(s)), gelu_inner2(z), s);
 }
 
 __device__ __forceinline__ float load_scale(const float* p) {      // where it stands, and not later
@@ -1507,7 +1523,6 @@ laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand
 // db = the sums of the columns of part [runs][N]; follows a kernel of the same call.
 laq_status column_sums(const Err& e, const float* part, int runs, int N, float* db, cudaStream_t st);
 laq_status zero_gradients(const Err& e, const Gradients& to, float* db, long long N, long long K, cudaStream_t st);   // of no rows
-int dz_rows_per(long long M, long long N);
 laq_status load_layer_kernels(const Err& e);
 
 // Defined in laq_ops_blocks.cu.

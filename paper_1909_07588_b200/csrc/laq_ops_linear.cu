@@ -36,10 +36,10 @@ __global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, l
       for (int e = 0; e < 8; ++e) g[e] = x[e] > 0.f ? g[e] : (x[e] == x[e] ? 0.f : x[e]);
     } else if (act == LAQ_ACT_GELU) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] *= slope_gelu(x[e]);
+      for (int e = 0; e < 8; e += 2) split(times2(pair_of(g[e], g[e + 1]), slope_gelu2(pair_of(x[e], x[e + 1]))), g[e], g[e + 1]);
     } else if (act == LAQ_ACT_SILU) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) g[e] *= slope_silu(x[e]);
+      for (int e = 0; e < 8; e += 2) split(times2(pair_of(g[e], g[e + 1]), slope_silu2(pair_of(x[e], x[e + 1]))), g[e], g[e + 1]);
     }
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += g[e];

@@ -341,9 +341,10 @@ def _result(out, rows, cols, dtype, index, device):
     return out, ptr, stride
 
 
-def _forward(function, need, call, more, workspace, index, raw):
-    """A call that mostly needs no workspace: one is made if the call asks for it, which it does before it launches anything."""
-    if workspace is None:
+def _forward(function, need, call, more, odd, workspace, index, raw):
+    """A call that needs no workspace unless its operands lie at odd addresses: one is made if the call asks for it, which it does
+    before it launches anything, or at once where they do."""
+    if workspace is None and not odd:
         err = _errors()
         rc = function(call, *more, None, 0, raw, err, 256)
         if rc == LAQ_OK:
@@ -596,7 +597,8 @@ def linear8(x, weight, bias=None, activation="none", residual=None, preact=False
         if preact:
             z = _table(M, N, dtype, x.codes.device)
             c.z, c.ld_z = z.data_ptr(), N
-        _forward(L.laq_linear_blocks_forward, L.laq_linear_blocks_workspace_bytes, C.byref(c), (C.byref(xq), C.byref(wq)), workspace, index, raw)
+        _forward(L.laq_linear_blocks_forward, L.laq_linear_blocks_workspace_bytes, C.byref(c), (C.byref(xq), C.byref(wq)),
+                 (xq.codes | xq.ld_codes | wq.codes | wq.ld_codes) & 15, workspace, index, raw)
         return (y, z) if preact else y
 
     return _on(index, stream, body, *x, *weight, bias, residual, out, workspace)
@@ -643,7 +645,7 @@ def gated(x, weight, bias=None, activation="silu", preact=False, out=None, works
         elif preact:
             z = _table(M, N, dt, x.device)
             c.z, c.ld_z = z.data_ptr(), N
-        _forward(L.laq_gated_forward, L.laq_gated_workspace_bytes, C.byref(c), (), workspace, index, raw)
+        _forward(L.laq_gated_forward, L.laq_gated_workspace_bytes, C.byref(c), (), (c.x | c.ld_x * 2 | c.w | c.ld_w * 2) & 15, workspace, index, raw)
         return (h, z) if preact else h
 
     return _on(index, stream, body, x, weight, bias, out, workspace)
