@@ -598,7 +598,7 @@ def linear8(x, weight, bias=None, activation="none", residual=None, preact=False
             z = _table(M, N, dtype, x.codes.device)
             c.z, c.ld_z = z.data_ptr(), N
         _forward(L.laq_linear_blocks_forward, L.laq_linear_blocks_workspace_bytes, C.byref(c), (C.byref(xq), C.byref(wq)),
-                 (xq.codes | xq.ld_codes | wq.codes | wq.ld_codes) & 15, workspace, index, raw)
+                 ((xq.codes or 0) | xq.ld_codes | wq.codes | wq.ld_codes) & 15, workspace, index, raw)
         return (y, z) if preact else y
 
     return _on(index, stream, body, *x, *weight, bias, residual, out, workspace)
@@ -645,7 +645,7 @@ def gated(x, weight, bias=None, activation="silu", preact=False, out=None, works
         elif preact:
             z = _table(M, N, dt, x.device)
             c.z, c.ld_z = z.data_ptr(), N
-        _forward(L.laq_gated_forward, L.laq_gated_workspace_bytes, C.byref(c), (), (c.x | c.ld_x * 2 | c.w | c.ld_w * 2) & 15, workspace, index, raw)
+        _forward(L.laq_gated_forward, L.laq_gated_workspace_bytes, C.byref(c), (), ((c.x or 0) | c.ld_x * 2 | c.w | c.ld_w * 2) & 15, workspace, index, raw)
         return (h, z) if preact else h
 
     return _on(index, stream, body, x, weight, bias, out, workspace)

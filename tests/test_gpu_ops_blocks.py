@@ -290,3 +290,36 @@ def test_captured_and_replayed_on_another_stream():
     torch.cuda.synchronize()
     assert torch.equal(p.codes.view(torch.uint8), want[0].codes.view(torch.uint8)) and torch.equal(p.scales, want[0].scales * 2)
     assert torch.equal(y, want[1] * 2) and torch.equal(d["dw"], want[2]["dw"] * 2) and torch.equal(d["dx"], want[2]["dx"])
+
+
+def test_scales_that_are_no_powers_of_two():
+    """Another program's scales: the product of two is rounded once (u), which the bound's 16 2^-23 holds; a value is rounded to fp32
+    and then to the type asked for."""
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for M, N, K in ((3, 70, 300), (40, 520, 1000), (700, 1300, 650), (2304, 2304, 512)):
+        x, w = _pair(M, N, K)
+        x.scales.mul_(torch.rand(x.scales.shape, generator=gen, device="cuda") + 0.5)
+        w.scales.mul_(torch.rand(w.scales.shape, generator=gen, device="cuda") + 0.5)
+        _check8(x, w, None, "silu", None, torch.bfloat16, preact=False)
+        for dt in ALL.values():
+            v, half = values(x), torch.finfo(dt).eps / 2
+            _within(ops.unpack8(x, dtype=dt), v, (half + 2 * U) * v.abs() + torch.finfo(dt).smallest_normal * torch.finfo(dt).eps, "values")
+    x, z, w = (ops.pack8(_randn(300, n, seed=n, dtype=torch.bfloat16)) for n in (200, 136, 72))
+    z.scales.mul_(torch.rand(z.scales.shape, generator=gen, device="cuda") + 0.5)
+    dy, wd = _randn(300, 136, seed=5, dtype=torch.bfloat16), _randn(136, 200, seed=6, dtype=torch.bfloat16)
+    dz = dy.double() * _slope(values(z), "silu")             # z is read as it is, in fp32
+    db = ops.linear_backward(dy, x, wd, z=z, activation="silu")["db"]
+    _within(db, dz.sum(0), (302 * U) * dz.abs().sum(0) + 40 * U * (dy.double().abs() * (1 + values(z) ** 2)).sum(0), "db")
+    ops.check_status()
+
+
+def test_gated_gradient_from_tiles():
+    """z with a scale a tile, as pack8(z, tiles=True) makes it."""
+    for F in (136, 131):
+        dh, x, w = _randn(300, F, seed=1, dtype=torch.bfloat16), _randn(300, 72, seed=2, dtype=torch.bfloat16), _randn(2 * F, 72, seed=3, dtype=torch.bfloat16)
+        z = ops.pack8(_randn(300, 2 * F, seed=4, dtype=torch.bfloat16), tiles=True)
+        xt = ops.pack8(x, tiles=True)
+        want = ops.gated_backward(dh, ops.unpack8(xt), w, ops.unpack8(z))
+        got = ops.gated_backward(dh, xt, w, z)
+        for k in want:
+            assert torch.equal(got[k], want[k]), (F, k)
