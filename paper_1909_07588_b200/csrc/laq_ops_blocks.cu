@@ -243,11 +243,21 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
 
 // ---- one to four rows through a layer in 8 bits -----------------------------------------------------------------------
 // W's bytes are read once, by dot products as in linear_few_rows_kernel: a warp takes four columns and a lane 16 codes of each at
-// a time, whose products it adds up and scales together.
+// a time, whose products it adds up and scales together.  4096 x 4096: one row 5.9 us, two 7.3, four 10.2; rows of 4095 codes, which lie
+// anywhere, 12.8, 14.4 and 19.7 (code by code 16.1, 19.2 and 26.9).
 constexpr int kCodesAhead = 2;
-template <class T, int ROWS>
+__device__ __forceinline__ uint4 sixteen_codes(const uint8_t* p) {      // at any address: from the aligned words that hold them
+  const int off = (int)((uintptr_t)p & 3u);
+  const uint32_t* words = reinterpret_cast<const uint32_t*>(p - off);
+  uint32_t w[5];
+#pragma unroll
+  for (int k = 0; k < 5; ++k) w[k] = k < 4 || off ? words[k] : 0u;
+  return make_uint4(__funnelshift_r(w[0], w[1], 8 * off), __funnelshift_r(w[1], w[2], 8 * off), __funnelshift_r(w[2], w[3], 8 * off),
+                    __funnelshift_r(w[3], w[4], 8 * off));
+}
+template <class T, int ROWS, bool VEC>
 __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
-    linear_few_codes_kernel(const GemmArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int vec, int log_parts) {
+    linear_few_codes_kernel(const GemmArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int log_parts) {
   constexpr int kRows2 = ROWS == 3 ? 4 : ROWS, kSums = kFewCols * kRows2, kWarps = kFewThreads / 32;
   __shared__ float part[kWarps][kSums];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, parts = 1 << log_parts;
@@ -259,14 +269,16 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
 #pragma unroll
   for (int c = 0; c < kFewCols; ++c) wr[c] = w + (long long)min(own + c, A.J - 1) * ldw;
   float s[kSums] = {};
-  const int nv = vec ? (int)(K / 16) : 0;
+  const int nv = (int)(K / 16);
   for (int v0 = first; v0 < nv; v0 += kCodesAhead * step) {
     uint4 a[kCodesAhead][kFewCols];
 #pragma unroll
     for (int u = 0; u < kCodesAhead; ++u)
 #pragma unroll
       for (int c = 0; c < kFewCols; ++c)
-        a[u][c] = v0 + u * step < nv ? __ldcs(reinterpret_cast<const uint4*>(wr[c]) + v0 + u * step) : make_uint4(0u, 0u, 0u, 0u);
+        a[u][c] = v0 + u * step >= nv ? make_uint4(0u, 0u, 0u, 0u)
+                  : VEC               ? __ldcs(reinterpret_cast<const uint4*>(wr[c]) + v0 + u * step)
+                                      : sixteen_codes(wr[c] + 16ll * (v0 + u * step));
 #pragma unroll
     for (int u = 0; u < kCodesAhead; ++u) {
       const int v = v0 + u * step;
@@ -276,7 +288,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
       float scale[ROWS];
 #pragma unroll
       for (int m = 0; m < ROWS; ++m) {
-        const uint4 b = __ldg(reinterpret_cast<const uint4*>(x + m * ldx) + v);
+        const uint4 b = VEC ? __ldg(reinterpret_cast<const uint4*>(x + m * ldx) + v) : sixteen_codes(x + m * ldx + 16ll * v);
         const uint32_t words[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -865,8 +877,10 @@ void list_product_kernels(const void** list, int& n) {
   const void* all[] = {(const void*)linear_gemm_kernel<T, true, false, false, false, kCodes>, (const void*)codes_gemm_kernel<T, true, 256, true>,
                        (const void*)codes_gemm_kernel<T, true, 256, false>, (const void*)codes_gemm_kernel<T, true, 128, false>,
                        (const void*)codes_gemm_kernel<T, false, 128, false>, (const void*)codes_gemm_kernel<T, false, 64, false>,
-                       (const void*)linear_few_codes_kernel<T, 1>,
-                       (const void*)linear_few_codes_kernel<T, 2>, (const void*)linear_few_codes_kernel<T, 3>, (const void*)linear_few_codes_kernel<T, 4>};
+                       (const void*)linear_few_codes_kernel<T, 1, true>, (const void*)linear_few_codes_kernel<T, 2, true>,
+                       (const void*)linear_few_codes_kernel<T, 3, true>, (const void*)linear_few_codes_kernel<T, 4, true>,
+                       (const void*)linear_few_codes_kernel<T, 1, false>, (const void*)linear_few_codes_kernel<T, 2, false>,
+                       (const void*)linear_few_codes_kernel<T, 3, false>, (const void*)linear_few_codes_kernel<T, 4, false>};
   for (const void* k : all) list[n++] = k;
 }
 
@@ -901,13 +915,19 @@ Operand codes_of(const laq_blocks* b, long long rows, long long cols) { return O
 
 template <class T>
 laq_status few_codes(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
-  const int vec = codes_mappable(x) && codes_mappable(w);
-  const long long groups = (w.rows + kFewCols - 1) / kFewCols, items = vec ? w.cols / 16 : w.cols;
+  const bool vec = codes_mappable(x) && codes_mappable(w);
+  const long long groups = (w.rows + kFewCols - 1) / kFewCols, items = w.cols / 16;
   const int log_parts = few_log_parts(groups, items < (1 << 30) ? (int)items : 1 << 30), per_block = kFewThreads / 32 >> log_parts;
-  const auto kernel = x.rows == 1 ? linear_few_codes_kernel<T, 1> : x.rows == 2 ? linear_few_codes_kernel<T, 2>
-                      : x.rows == 3 ? linear_few_codes_kernel<T, 3> : linear_few_codes_kernel<T, 4>;
+  const auto of = [&](auto rows) {
+    constexpr int kRows = decltype(rows)::value;
+    return vec ? linear_few_codes_kernel<T, kRows, true> : linear_few_codes_kernel<T, kRows, false>;
+  };
+  const auto kernel = x.rows == 1   ? of(std::integral_constant<int, 1>())
+                      : x.rows == 2 ? of(std::integral_constant<int, 2>())
+                      : x.rows == 3 ? of(std::integral_constant<int, 3>())
+                                    : of(std::integral_constant<int, 4>());
   return launched(e.buf, e.len, launch_plain(kernel, dim3((unsigned)((groups + per_block - 1) / per_block)), kFewThreads, st, A, (const uint8_t*)x.p, x.ld,
-                                             (const uint8_t*)w.p, w.ld, w.cols, vec, log_parts));
+                                             (const uint8_t*)w.p, w.ld, w.cols, log_parts));
 }
 
 }  // namespace
