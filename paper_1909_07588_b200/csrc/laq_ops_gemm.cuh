@@ -1344,12 +1344,12 @@ struct Err {
 struct Raised {
   std::atomic<uint64_t> devices{0};
 };
-inline laq_status raise_shared_memory(const Err& e, const void* kernel, Raised& raised) {
+inline laq_status raise_shared_memory(const Err& e, const void* kernel, Raised& raised, int bytes = kMaxRing + kStaging + 1024) {
   int dev = 0;
   cudaGetDevice(&dev);
   const uint64_t bit = 1ull << (dev & 63);
   if (dev >= 64 || !(raised.devices.load(std::memory_order_acquire) & bit)) {
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxRing + kStaging + 1024) != cudaSuccess) {
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) {
       cudaGetLastError();
       return fail(e.buf, e.len, LAQ_ECUDA, "shared memory of the product kernel was refused");
     }

@@ -1,4 +1,6 @@
 """How calls on 8-bit matrices and of the gated block stand beside each other and beside the rest of a program, and how far they reach."""
+import math
+
 import pytest
 import torch
 
@@ -185,6 +187,37 @@ def test_bounded_wait_of_wide_tiles(residual):
         ops.check_status()
     assert e.value.status == laq.LAQ_ETIMEOUT
     assert torch.equal(ops.linear8(x, w, residual=r), before)
+    ops.check_status()
+
+
+# --- three to 32 rows -------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", [BF, torch.float16])
+@pytest.mark.parametrize("N, K", [(1, 1), (15, 16), (17, 129), (40, 1000), (257, 4096), (33, 900), (130, 385), (20_000, 136), (9_700, 1100)])
+def test_some_rows(N, K, dtype):
+    """Rows of codes that end within a block and within 16 codes, with NaN behind them, more columns than the SMs hold at once, and
+    neighbours of the result that stay as they are."""
+    for M in (3, 4, 8, 9, 16, 17, 32):
+        x, w = _pair(M, N, K)
+
+        def among(p, rows):
+            pitch = -(-K // 16) * 16 + 32
+            codes = torch.full((p.codes.shape[0] + 2 * rows, pitch), 0x7f, dtype=torch.uint8, device="cuda")
+            codes[rows:rows + p.codes.shape[0], 16:16 + K] = p.codes.view(torch.uint8)
+            scales = torch.full((p.scales.shape[0] + 2, p.scales.shape[1] + 3), math.nan, device="cuda")
+            scales[1:-1, 1:-2] = p.scales
+            return ops.Packed8(codes.view(torch.float8_e4m3fn)[rows:rows + p.codes.shape[0], 16:16 + K], scales[1:-1, 1:-2])
+        b, r = _randn(N, seed=3, dtype=dtype), _randn(M, N, seed=4, dtype=dtype)
+        y = _check8(x, w, b, "silu", r, dtype)
+        x, w = among(x, 2), among(w, 1)
+        assert torch.equal(ops.linear8(x, w, b, activation="silu", residual=r, dtype=dtype), y)
+        big = _randn(M + 2, N + 5, seed=5, dtype=dtype)
+        before, inside = big.clone(), big[1:1 + M, 3:3 + N]
+        inside.copy_(r)
+        assert torch.equal(ops.linear8(x, w, b, activation="silu", residual=inside, dtype=dtype, out=inside), y)
+        mark = torch.ones_like(big, dtype=torch.bool)
+        mark[1:1 + M, 3:3 + N] = False
+        assert torch.equal(big[mark], before[mark])
     ops.check_status()
 
 
