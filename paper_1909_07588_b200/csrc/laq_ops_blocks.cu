@@ -244,8 +244,9 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
 // ---- one or two rows through a layer in 8 bits, or four ---------------------------------------------------------------------
 // W's bytes are read once, by dot products as in linear_few_rows_kernel: a warp takes four columns and a lane 16 codes of each at
 // a time, whose products it adds up and scales together.  4096 x 4096: one row 5.9 us, two 7.2 (three and four go by
-// linear_some_codes_kernel, 6.7); rows of 4095 codes, which lie anywhere, 12.8, 14.4 and, four, 19.6 (code by code 16.1, 19.2 and 26.9).
+// linear_some_rows_kernel, 6.7); rows of 4095 codes, which lie anywhere, 12.8, 14.4 and, four, 19.6 (code by code 16.1, 19.2 and 26.9).
 constexpr int kCodesAhead = 2;
+constexpr int kPlainRows = 2, kSomeRows = 32;        // of codes in order: up to these by dot products, by linear_some_rows_kernel
 __device__ __forceinline__ uint4 sixteen_codes(const uint8_t* p) {      // at any address: from the aligned words that hold them
   const int off = (int)((uintptr_t)p & 3u);
   const uint32_t* words = reinterpret_cast<const uint32_t*>(p - off);
@@ -339,150 +340,6 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
 #pragma unroll
       for (int m = 0; m < ROWS; ++m) y[m] += part[(t / kFewCols << log_parts) + i][t % kFewCols * kRows2 + m];
     finish_column<T, false>(A, A.I, A.J, 0, col0 + t, y);
-  }
-}
-
-// ---- some rows through a layer in 8 bits ------------------------------------------------------------------------------
-// Three to 32 rows: W's bytes are what has to be read, and a tile in tensor memory spends most of its time on the launch, the first loads
-// and the join.  Here a warp takes 16 columns of Y and every parts-th block of 128 codes of them; both operands' codes are decoded to
-// fp16, exactly, for a warp's own matrix instructions, and a block's sums join the others by its scales, as elsewhere.  Which codes a
-// lane holds as its k-th is its own affair as long as both operands agree, so a lane takes 16 neighbours.  A warp copies its blocks to
-// shared memory by itself, some ahead, and a thread block goes on to its next columns without a pause.
-// 4096 x 4096, 8, 16 and 32 rows: 7.2, 7.9 and 12.4 us (by tiles 11.9, 11.9, 12.7; four by plain dot products 10.1); 11008 x 4096, 8 rows
-// 13.7 (21.6); 2048 x 4096 5.8 (19.1).  Bound by memory (half of the copy's rate at most) and by decoding and multiplying: fp8 operands in
-// place of fp16 are slower: 16 rows of 11008 x 4096 31 us for 21, before the copies made it 15.4.
-constexpr int kPlainRows = 2, kSomeRows = 32, kSomeThreads = 256, kSomeWarps = kSomeThreads / 32, kSomeCols = 16, kSomePitch = kSomeCols + 4;
-template <int EIGHTS>
-struct Some {
-  static constexpr int kStages = EIGHTS == 1 ? 4 : 3, kPieces = 4 + 2 * EIGHTS, kBlocks = EIGHTS <= 2 ? 2 : 1;
-  static constexpr int kRing = kSomeWarps * kStages * kPieces * 32 * 16;
-};
-__device__ __forceinline__ void mma_halves(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-// Four codes as fp16 numbers, exactly: the lower two and the upper two.
-__device__ __forceinline__ void halves_of(uint32_t codes, uint32_t& lo, uint32_t& hi) {
-  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(codes));
-}
-// The first n of 16 codes to shared memory, zeros behind them.
-__device__ __forceinline__ void copy_codes(uint4* to, const uint8_t* from, long long n) {
-  const int bytes = n >= 16 ? 16 : n > 0 ? (int)n : 0;
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(umma::smem_u32(to)), "l"(from), "r"(bytes) : "memory");
-}
-template <class T, int EIGHTS>
-__global__ void __launch_bounds__(kSomeThreads, Some<EIGHTS>::kBlocks)
-    linear_some_codes_kernel(const GemmArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int log_parts, int sets) {
-  constexpr int kStages = Some<EIGHTS>::kStages, kPieces = Some<EIGHTS>::kPieces;
-  extern __shared__ uint4 some_ring[];
-  __shared__ float sums[kSomeWarps][8 * EIGHTS * kSomePitch];
-  allow_next();
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = 1 << log_parts, part = warp & (parts - 1);
-  const int g = lane >> 2, t = lane & 3, per_set = kSomeWarps >> log_parts;
-  uint4* ring = some_ring + warp * kStages * kPieces * 32;
-  // A stage: rows of eight 16-byte pieces, 16 of W and then X's; every other row's halves are exchanged, so that neither the copies (a
-  // row by eight lanes) nor the reads (two rows' halves by eight lanes) meet in a bank.
-  const int from_row = lane >> 3, from_piece = lane & 7, to_piece = lane ^ (from_row & 1) << 2;
-  const int at_s[2] = {8 * g + (t ^ (g & 1) << 2), 8 * g + ((t + 4) ^ (g & 1) << 2)};
-  const int nkb = (int)((K + kBlock - 1) / kBlock);
-  // where this warp's walk over sets of columns and blocks of codes is
-  struct Place {
-    int set, b;
-  };
-  const auto next = [&](Place& p) {
-    p.b += parts;
-    if (p.b >= nkb) p.b = part, p.set += (int)gridDim.x;
-  };
-  const auto column = [&](int set) { return (set * per_set + (warp >> log_parts)) * kSomeCols; };
-  const auto fetch = [&](const Place& p, int stage) {
-    if (p.set < sets) {
-      uint4* to = ring + stage * kPieces * 32 + to_piece;
-      const long long k = (long long)p.b * kBlock + 16 * from_piece, left = K - k;
-      const int col = column(p.set) + from_row;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) copy_codes(to + 32 * i, w + (long long)min(col + 4 * i, A.J - 1) * ldw + (left > 0 ? k : 0), left);
-#pragma unroll
-      for (int i = 0; i < 2 * EIGHTS; ++i) {
-        const bool there = left > 0 && 4 * i + from_row < A.I;
-        copy_codes(to + 32 * (4 + i), there ? x + (long long)(4 * i + from_row) * ldx + k : x, there ? left : 0);
-      }
-    }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  float of_x[EIGHTS][2], of_w = 0.f;
-  const auto read_scales = [&](const Place& p) {
-    if (p.set >= sets) return;
-    of_w = __ldg(A.sw + (long long)(min(column(p.set), A.J - 1) / kBlock) * A.ldsw + p.b);        // 16 columns lie in one tile
-#pragma unroll
-    for (int f = 0; f < EIGHTS; ++f)
-#pragma unroll
-      for (int e = 0; e < 2; ++e) of_x[f][e] = __ldg(A.sx + min(8 * f + 2 * t + e, A.I - 1) * A.ldsx + p.b);
-  };
-  Place fetched{part < nkb ? (int)blockIdx.x : sets, part}, read = fetched;        // a warp beyond the last block has nothing to fetch
-#pragma unroll
-  for (int i = 0; i < kStages - 1; ++i) {
-    fetch(fetched, i);
-    next(fetched);
-  }
-  read_scales(read);
-  int stage = 0;
-  for (int set = blockIdx.x; set < sets; set += gridDim.x) {
-    float sum[EIGHTS][4] = {};
-    for (int b = part; b < nkb; b += parts) {
-      float scale[EIGHTS][2];
-#pragma unroll
-      for (int f = 0; f < EIGHTS; ++f) scale[f][0] = of_x[f][0] * of_w, scale[f][1] = of_x[f][1] * of_w;
-      next(read);
-      read_scales(read);
-      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
-      __syncwarp();
-      const uint4* at = ring + stage * kPieces * 32;
-      fetch(fetched, stage == 0 ? kStages - 1 : stage - 1);
-      next(fetched);
-      stage = stage + 1 == kStages ? 0 : stage + 1;
-      float of_block[EIGHTS][4] = {};
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        const uint4 v0 = at[at_s[s]], v1 = at[64 + at_s[s]];
-        const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
-        uint32_t h0[4][2], h1[4][2];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          halves_of(w0[i], h0[i][0], h0[i][1]);
-          halves_of(w1[i], h1[i][0], h1[i][1]);
-        }
-#pragma unroll
-        for (int f = 0; f < EIGHTS; ++f) {
-          const uint4 here = at[128 + 64 * f + at_s[s]];
-          const uint32_t words[4] = {here.x, here.y, here.z, here.w};
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t lo, hi;
-            halves_of(words[i], lo, hi);
-            mma_halves(of_block[f], h0[i][0], h1[i][0], h0[i][1], h1[i][1], lo, hi);
-          }
-        }
-      }
-#pragma unroll
-      for (int f = 0; f < EIGHTS; ++f)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[f][e] = fmaf(of_block[f][e], scale[f][e & 1], sum[f][e]);
-    }
-#pragma unroll
-    for (int f = 0; f < EIGHTS; ++f)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sums[warp][(8 * f + 2 * t + (e & 1)) * kSomePitch + g + 8 * (e >> 1)] = sum[f][e];
-    __syncthreads();
-    for (int i = threadIdx.x; i < per_set * EIGHTS * kSomeCols; i += kSomeThreads) {
-      const int c = i % kSomeCols, f = i / kSomeCols % EIGHTS, group = i / (kSomeCols * EIGHTS);
-      float y[8] = {};
-      for (int p = 0; p < parts; ++p)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] += sums[(group << log_parts) + p][(8 * f + e) * kSomePitch + c];
-      finish_column<T, false>(A, A.I, A.J, 8 * f, (set * per_set + group) * kSomeCols + c, y);
-    }
-    __syncthreads();
   }
 }
 
@@ -1023,8 +880,8 @@ void list_product_kernels(const void** list, int& n) {
                        (const void*)codes_gemm_kernel<T, true, 256, false>, (const void*)codes_gemm_kernel<T, true, 128, false>,
                        (const void*)codes_gemm_kernel<T, false, 128, false>, (const void*)codes_gemm_kernel<T, false, 64, false>,
                        (const void*)linear_few_codes_kernel<T, 1, true>, (const void*)linear_few_codes_kernel<T, 2, true>,
-                       (const void*)linear_some_codes_kernel<T, 1>, (const void*)linear_some_codes_kernel<T, 2>,
-                       (const void*)linear_some_codes_kernel<T, 4>,
+                       (const void*)linear_some_rows_kernel<T, 1, true>, (const void*)linear_some_rows_kernel<T, 2, true>,
+                       (const void*)linear_some_rows_kernel<T, 4, true>,
                        (const void*)linear_few_codes_kernel<T, 1, false>, (const void*)linear_few_codes_kernel<T, 2, false>,
                        (const void*)linear_few_codes_kernel<T, 3, false>, (const void*)linear_few_codes_kernel<T, 4, false>};
   for (const void* k : all) list[n++] = k;
@@ -1066,7 +923,7 @@ laq_status few_codes(const Err& e, const GemmArgs& A, const Operand& x, const Op
   const auto of = [&](auto rows) {
     constexpr int kRows = decltype(rows)::value;
     if constexpr (kRows <= kPlainRows) return vec ? linear_few_codes_kernel<T, kRows, true> : linear_few_codes_kernel<T, kRows, false>;
-    else return linear_few_codes_kernel<T, kRows, false>;          // aligned ones go by linear_some_codes_kernel
+    else return linear_few_codes_kernel<T, kRows, false>;          // aligned ones go by linear_some_rows_kernel
   };
   const auto kernel = x.rows == 1   ? of(std::integral_constant<int, 1>())
                       : x.rows == 2 ? of(std::integral_constant<int, 2>())
@@ -1084,31 +941,6 @@ bool takes_some_codes(const laq_linear_call* c, const laq_blocks* xq, const laq_
   if (c->M > 16 && c->K > 8192) return false;
   return codes_mappable(codes_of(xq, c->M, c->K)) && codes_mappable(codes_of(wq, c->N, c->K));
 }
-template <class T, int EIGHTS>
-laq_status launch_some(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
-  static Raised raised;
-  const auto kernel = linear_some_codes_kernel<T, EIGHTS>;
-  LAQ_TRY(raise_shared_memory(e, (const void*)kernel, raised, Some<EIGHTS>::kRing));
-  const long long groups = (w.rows + kSomeCols - 1) / kSomeCols, blocks = (w.cols + kBlock - 1) / kBlock;
-  int log_parts = 0;
-  while (1 << log_parts < kSomeWarps && 1 << log_parts < blocks) ++log_parts;
-  const int per_set = kSomeWarps >> log_parts;
-  const long long sets = (groups + per_set - 1) / per_set, most = (long long)Some<EIGHTS>::kBlocks * kSMs;
-  cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(sets < most ? sets : most));
-  cfg.blockDim = dim3(kSomeThreads);
-  cfg.dynamicSmemBytes = Some<EIGHTS>::kRing;
-  cfg.stream = st;
-  return launched(e.buf, e.len, cudaLaunchKernelEx(&cfg, kernel, A, (const uint8_t*)x.p, (long long)x.ld, (const uint8_t*)w.p, (long long)w.ld, (long long)w.cols,
-                                                   log_parts, (int)sets));
-}
-template <class T>
-laq_status some_codes(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
-  return A.I <= 8    ? launch_some<T, 1>(e, A, x, w, st)
-         : A.I <= 16 ? launch_some<T, 2>(e, A, x, w, st)
-                     : launch_some<T, 4>(e, A, x, w, st);
-}
-
 }  // namespace
 
 laq_status load_block_kernels(const Err& e) {
@@ -1223,7 +1055,9 @@ extern "C" laq_status laq_linear_blocks_forward(const laq_linear_call* c, const 
   A.ldsx = xq->ld_scales;
   A.sw = wq->scales;
   A.ldsw = wq->ld_scales;
-  if (takes_some_codes(c, xq, wq)) return c->dtype == LAQ_BF16 ? some_codes<__nv_bfloat16>(e, A, x, w, st) : some_codes<__half>(e, A, x, w, st);
+  if (takes_some_codes(c, xq, wq))
+    return c->dtype == LAQ_BF16 ? some_rows<__nv_bfloat16, true>(e, A, x.p, x.ld, w.p, w.ld, c->K, st)
+                                : some_rows<__half, true>(e, A, x.p, x.ld, w.p, w.ld, c->K, st);
   if (takes_few_codes(c)) return c->dtype == LAQ_BF16 ? few_codes<__nv_bfloat16>(e, A, x, w, st) : few_codes<__half>(e, A, x, w, st);
   char* ws = (char*)d_workspace;
   LAQ_TRY(make_codes_mappable(e, x, w, ws, st));

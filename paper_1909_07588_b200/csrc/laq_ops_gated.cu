@@ -174,16 +174,27 @@ bool sizes_ok(const laq_gated_call* c) {
          (c->dtype == LAQ_BF16 || c->dtype == LAQ_F16);
 }
 
-// By the same rule as a layer's (laq_ops_linear.cu), for as many rows of W.
+// Plain dot products, by the same rule as a layer's (laq_ops_linear.cu), for as many rows of W, but three and four rows of a large W
+// that lies in order go as below (2 x 11008 x 4096: 38 us, so 32; 2 x 512 x 2048: 3.5 us, 4.1).
+bool some_in_order(const laq_gated_call* c) { return mappable(c->x, c->ld_x) && mappable(c->w, c->ld_w); }
 bool takes_few_rows(const laq_gated_call* c) {
   if (c->flags & LAQ_LINEAR_STARVE) return false;
+  if (c->M > 2 && c->F >= (1ll << 24) / c->K && some_in_order(c)) return false;
   return c->M <= 2 || (c->M <= kFewRows && (c->K >= 1024 || 2 * c->F <= kFewCols * kFewThreads / 32 * kFewBlocks * kSMs));
+}
+// linear_some_rows_kernel.  Where the tiles of tensor memory overtake: 16 rows of 2 x 11008 x 4096 38.3 us (by tiles 38.4), of 2 x 4096 x
+// 4096 16.6 (18.8); 32 rows of 2 x 4096 x 4096 26 us (20), of 2 x 4096 x 1024 12.4 (12.1), of 2 x 1501 x 1000 8.4 (10.9).
+bool takes_some_rows(const laq_gated_call* c) {
+  if ((c->flags & LAQ_LINEAR_STARVE) || takes_few_rows(c) || c->M > 32) return false;
+  if (c->M > 8 && c->F > (c->M > 16 ? 1ll << 21 : 1ll << 25) / c->K) return false;
+  if (c->M > 16 && c->K > 4096) return false;
+  return some_in_order(c);
 }
 
 // Z in 8 bits leaves the epilogue where a tile has whole blocks of gates and of ups: 128 of each, not split, and vectors throughout.
 // Else it is packed from 16 bits afterwards, with the same result.  4096 x 5504 x 2048: 196 us so, 153 us in the epilogue.
 bool packs_in_epilogue(const laq_gated_call* c) {
-  if (!c->z_blocks || takes_few_rows(c) || c->F % kBlock || !mappable(c->h, c->ld_h) || (c->bias && !mappable(c->bias, 8)) ||
+  if (!c->z_blocks || takes_few_rows(c) || takes_some_rows(c) || c->F % kBlock || !mappable(c->h, c->ld_h) || (c->bias && !mappable(c->bias, 8)) ||
       c->z_blocks->block_rows != 1 || !Codes(c->z_blocks).vectors(8))
     return false;
   const Plan pl = make_plan(c->M, 2 * c->F, c->K, false, false, true, false, false, kGated);
@@ -196,7 +207,7 @@ struct ForwardNeeds {
   explicit ForwardNeeds(const laq_gated_call* c) : x{c->x, c->ld_x, c->M, c->K}, w{c->w, c->ld_w, 2 * c->F, c->K} {
     z_bytes = c->z_blocks && !packs_in_epilogue(c) ? align256((size_t)c->M * pad8(2 * c->F) * 2) : 0;
   }
-  size_t bytes(const laq_gated_call* c) const { return z_bytes + (takes_few_rows(c) ? 0 : x.pack_bytes() + w.pack_bytes()); }
+  size_t bytes(const laq_gated_call* c) const { return z_bytes + (takes_few_rows(c) || takes_some_rows(c) ? 0 : x.pack_bytes() + w.pack_bytes()); }
 };
 
 bool dz_vectors(const laq_gated_call* c) {
@@ -265,6 +276,8 @@ void list_kernels(const void** list, int& n) {
                        (const void*)linear_few_rows_kernel<T, 1, 4, true>, (const void*)linear_few_rows_kernel<T, 1, 2, true>,
                        (const void*)linear_few_rows_kernel<T, 2, 4, true>, (const void*)linear_few_rows_kernel<T, 2, 2, true>,
                        (const void*)linear_few_rows_kernel<T, 3, 2, true>, (const void*)linear_few_rows_kernel<T, 4, 2, true>,
+                       (const void*)linear_some_rows_kernel<T, 1, false>, (const void*)linear_some_rows_kernel<T, 2, false>,
+                       (const void*)linear_some_rows_kernel<T, 4, false>,
                        (const void*)gated_dz_kernel<T, false, false>, (const void*)gated_dz_kernel<T, false, true>,
                        (const void*)gated_dz_kernel<T, true, false>, (const void*)gated_dz_kernel<T, true, true>};
   for (const void* k : all) list[n++] = k;
@@ -341,7 +354,10 @@ extern "C" laq_status laq_gated_forward(const laq_gated_call* c, void* d_workspa
     A.ld_zs = c->z_blocks->ld_scales;
   }
   const bool bf16 = c->dtype == LAQ_BF16;
-  if (takes_few_rows(c)) {
+  if (takes_some_rows(c)) {
+    LAQ_TRY(bf16 ? some_rows<__nv_bfloat16, false>(e, A, c->x, 2 * c->ld_x, c->w, 2 * c->ld_w, 2 * c->K, st)
+                 : some_rows<__half, false>(e, A, c->x, 2 * c->ld_x, c->w, 2 * c->ld_w, 2 * c->K, st));
+  } else if (takes_few_rows(c)) {
     LAQ_TRY(bf16 ? few_rows<__nv_bfloat16>(e, A, need.x, need.w, st) : few_rows<__half>(e, A, need.x, need.w, st));
   } else {
     const char* before = ws;

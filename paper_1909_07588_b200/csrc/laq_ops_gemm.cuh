@@ -1607,5 +1607,208 @@ __device__ __forceinline__ uint2 load8(const void* p) {
   return v;
 }
 
+// ---- some rows through a layer in 8 bits or a gated block ----------------------------------------------------------------
+// Three to 32 rows: W's bytes are what has to be read, and a tile in tensor memory spends most of its time on the launch, the first loads
+// and the join.  Here a warp takes 16 columns (or eight gates and their ups) and every parts-th block of 128 bytes of their rows, and
+// multiplies with a warp's own matrix instructions; codes are decoded to fp16 for them, exactly, and a block's sums join the others by its
+// scales, as elsewhere.  Which values a lane holds as its k-th is its own affair as long as both operands agree, so a lane takes 16
+// neighbouring bytes.  A warp copies its blocks to shared memory by itself, some ahead, and a thread block goes on to its next columns
+// without a pause.
+// Codes, 4096 x 4096, 8, 16 and 32 rows: 7.2, 7.9 and 12.4 us (by tiles 11.9, 11.9, 12.7; four by plain dot products 10.1); 11008 x 4096,
+// 8 rows 13.7 (21.6); 2048 x 4096 5.8 (19.1).  Gates and ups in 16 bits, 2 x 4096 x 4096, 8 and 16 rows: 14.5 and 16.6 us (by tiles 19.0,
+// 18.8; 4.6 TB/s); 2 x 1024 x 1024 3.7 (15.9).  Bound by memory and, with codes, by decoding: fp8 operands in place of fp16 are slower
+// (16 rows of 11008 x 4096 31 us for 21, before the copies made it 15.4).
+constexpr int kSomeThreads = 256, kSomeWarps = kSomeThreads / 32, kSomePitch = 20, kRowBytes = 128;
+__host__ __device__ constexpr int some_columns(bool codes) { return codes ? 16 : 8; }
+template <int EIGHTS>
+struct Some {
+  static constexpr int kStages = EIGHTS == 1 ? 4 : 3, kPieces = 4 + 2 * EIGHTS, kBlocks = EIGHTS <= 2 ? 2 : 1;
+  static constexpr int kRing = kSomeWarps * kStages * kPieces * 32 * 16;
+};
+template <class T>
+__device__ __forceinline__ void mma_warp(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (std::is_same<T, __half>::value)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// Four codes as fp16 numbers, exactly: the lower two and the upper two.
+__device__ __forceinline__ void halves_of(uint32_t codes, uint32_t& lo, uint32_t& hi) {
+  asm("{\n.reg .b16 a, b;\nmov.b32 {a, b}, %2;\ncvt.rn.f16x2.e4m3x2 %0, a;\ncvt.rn.f16x2.e4m3x2 %1, b;\n}" : "=r"(lo), "=r"(hi) : "r"(codes));
+}
+// The first n of 16 bytes to shared memory, zeros behind them.
+__device__ __forceinline__ void copy_piece(uint4* to, const uint8_t* from, long long n) {
+  const int bytes = n >= 16 ? 16 : n > 0 ? (int)n : 0;
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(umma::smem_u32(to)), "l"(from), "r"(bytes) : "memory");
+}
+// CODES: 16 columns a warp, else eight gates and their ups; ldx, ldw and K in bytes.
+template <class T, int EIGHTS, bool CODES>
+__global__ void __launch_bounds__(kSomeThreads, Some<EIGHTS>::kBlocks)
+    linear_some_rows_kernel(const GemmArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int log_parts, int sets) {
+  constexpr int kStages = Some<EIGHTS>::kStages, kPieces = Some<EIGHTS>::kPieces, kOwn = some_columns(CODES);
+  extern __shared__ uint4 some_ring[];
+  __shared__ float sums[kSomeWarps][8 * EIGHTS * kSomePitch];
+  allow_next();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, parts = 1 << log_parts, part = warp & (parts - 1);
+  const int g = lane >> 2, t = lane & 3, per_set = kSomeWarps >> log_parts;
+  uint4* ring = some_ring + warp * kStages * kPieces * 32;
+  // A stage: rows of eight 16-byte pieces, 16 of W and then X's; every other row's halves are exchanged, so that neither the copies (a
+  // row by eight lanes) nor the reads (two rows' halves by eight lanes) meet in a bank.
+  const int from_row = lane >> 3, from_piece = lane & 7, to_piece = lane ^ (from_row & 1) << 2;
+  const int at_s[2] = {8 * g + (t ^ (g & 1) << 2), 8 * g + ((t + 4) ^ (g & 1) << 2)};
+  const int nkb = (int)((K + kRowBytes - 1) / kRowBytes);
+  // where this warp's walk over sets of columns and blocks of 128 bytes is
+  struct Place {
+    int set, b;
+  };
+  const auto next = [&](Place& p) {
+    p.b += parts;
+    if (p.b >= nkb) p.b = part, p.set += (int)gridDim.x;
+  };
+  const auto column = [&](int set) { return (set * per_set + (warp >> log_parts)) * kOwn; };
+  const auto fetch = [&](const Place& p, int stage) {
+    if (p.set < sets) {
+      uint4* to = ring + stage * kPieces * 32 + to_piece;
+      const long long k = (long long)p.b * kRowBytes + 16 * from_piece, left = K - k;
+      const int col = column(p.set) + from_row;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const long long row = CODES ? min(col + 4 * i, A.J - 1) : min(col + 4 * (i & 1), A.J - 1) + (i >> 1) * A.up;
+        copy_piece(to + 32 * i, w + row * ldw + (left > 0 ? k : 0), left);
+      }
+#pragma unroll
+      for (int i = 0; i < 2 * EIGHTS; ++i) {
+        const bool there = left > 0 && 4 * i + from_row < A.I;
+        copy_piece(to + 32 * (4 + i), there ? x + (long long)(4 * i + from_row) * ldx + k : x, there ? left : 0);
+      }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  float of_x[EIGHTS][2], of_w = 0.f;
+  const auto read_scales = [&](const Place& p) {
+    if (!CODES || p.set >= sets) return;
+    of_w = __ldg(A.sw + (long long)(min(column(p.set), A.J - 1) / kBlock) * A.ldsw + p.b);        // 16 columns lie in one tile
+#pragma unroll
+    for (int f = 0; f < EIGHTS; ++f)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) of_x[f][e] = __ldg(A.sx + min(8 * f + 2 * t + e, A.I - 1) * A.ldsx + p.b);
+  };
+  Place fetched{part < nkb ? (int)blockIdx.x : sets, part}, read = fetched;        // a warp beyond the last block has nothing to fetch
+#pragma unroll
+  for (int i = 0; i < kStages - 1; ++i) {
+    fetch(fetched, i);
+    next(fetched);
+  }
+  read_scales(read);
+  int stage = 0;
+  for (int set = blockIdx.x; set < sets; set += gridDim.x) {
+    float sum[EIGHTS][4] = {};
+    for (int b = part; b < nkb; b += parts) {
+      float scale[EIGHTS][2];
+      if constexpr (CODES) {
+#pragma unroll
+        for (int f = 0; f < EIGHTS; ++f) scale[f][0] = of_x[f][0] * of_w, scale[f][1] = of_x[f][1] * of_w;
+        next(read);
+        read_scales(read);
+      }
+      asm volatile("cp.async.wait_group %0;" ::"n"(kStages - 2) : "memory");
+      __syncwarp();
+      const uint4* at = ring + stage * kPieces * 32;
+      fetch(fetched, stage == 0 ? kStages - 1 : stage - 1);
+      next(fetched);
+      stage = stage + 1 == kStages ? 0 : stage + 1;
+      if constexpr (CODES) {
+        float of_block[EIGHTS][4] = {};
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const uint4 v0 = at[at_s[s]], v1 = at[64 + at_s[s]];
+          const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
+          uint32_t h0[4][2], h1[4][2];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            halves_of(w0[i], h0[i][0], h0[i][1]);
+            halves_of(w1[i], h1[i][0], h1[i][1]);
+          }
+#pragma unroll
+          for (int f = 0; f < EIGHTS; ++f) {
+            const uint4 here = at[128 + 64 * f + at_s[s]];
+            const uint32_t words[4] = {here.x, here.y, here.z, here.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              uint32_t lo, hi;
+              halves_of(words[i], lo, hi);
+              mma_warp<__half>(of_block[f], h0[i][0], h1[i][0], h0[i][1], h1[i][1], lo, hi);
+            }
+          }
+        }
+#pragma unroll
+        for (int f = 0; f < EIGHTS; ++f)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sum[f][e] = fmaf(of_block[f][e], scale[f][e & 1], sum[f][e]);
+      } else {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const uint4 v0 = at[at_s[s]], v1 = at[64 + at_s[s]];
+#pragma unroll
+          for (int f = 0; f < EIGHTS; ++f) {
+            const uint4 here = at[128 + 64 * f + at_s[s]];
+            mma_warp<T>(sum[f], v0.x, v1.x, v0.y, v1.y, here.x, here.y);
+            mma_warp<T>(sum[f], v0.z, v1.z, v0.w, v1.w, here.z, here.w);
+          }
+        }
+      }
+    }
+#pragma unroll
+    for (int f = 0; f < EIGHTS; ++f)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sums[warp][(8 * f + 2 * t + (e & 1)) * kSomePitch + g + 8 * (e >> 1)] = sum[f][e];
+    __syncthreads();
+    for (int i = threadIdx.x; i < per_set * EIGHTS * kOwn; i += kSomeThreads) {
+      const int c = i % kOwn, f = i / kOwn % EIGHTS, group = i / (kOwn * EIGHTS), col = (set * per_set + group) * kOwn + c;
+      float y[8] = {}, up[8] = {};
+      for (int p = 0; p < parts; ++p) {
+        const float* from = &sums[(group << log_parts) + p][8 * f * kSomePitch + c];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          y[e] += from[e * kSomePitch];
+          if (!CODES) up[e] += from[e * kSomePitch + 8];
+        }
+      }
+      if constexpr (CODES) finish_column<T, false>(A, A.I, A.J, 8 * f, col, y);
+      else finish_gated_column<T>(A, A.I, 8 * f, col, y, up);
+    }
+    __syncthreads();
+  }
+}
+
+template <class T, int EIGHTS, bool CODES>
+laq_status launch_some(const Err& e, const GemmArgs& A, const void* x, long long ldx, const void* w, long long ldw, long long K, cudaStream_t st) {
+  static Raised raised;
+  const auto kernel = linear_some_rows_kernel<T, EIGHTS, CODES>;
+  LAQ_TRY(raise_shared_memory(e, (const void*)kernel, raised, Some<EIGHTS>::kRing));
+  const long long groups = (A.J + some_columns(CODES) - 1) / some_columns(CODES), blocks = (K + kRowBytes - 1) / kRowBytes;
+  int log_parts = 0;
+  while (1 << log_parts < kSomeWarps && 1 << log_parts < blocks) ++log_parts;
+  const int per_set = kSomeWarps >> log_parts;
+  const long long sets = (groups + per_set - 1) / per_set, most = (long long)Some<EIGHTS>::kBlocks * kSMs;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(sets < most ? sets : most));
+  cfg.blockDim = dim3(kSomeThreads);
+  cfg.dynamicSmemBytes = Some<EIGHTS>::kRing;
+  cfg.stream = st;
+  return launched(e.buf, e.len, cudaLaunchKernelEx(&cfg, kernel, A, (const uint8_t*)x, ldx, (const uint8_t*)w, ldw, K, log_parts, (int)sets));
+}
+// Strides and K in bytes, multiples of 16 the former, as the addresses are.
+template <class T, bool CODES>
+laq_status some_rows(const Err& e, const GemmArgs& A, const void* x, long long ldx, const void* w, long long ldw, long long K, cudaStream_t st) {
+  return A.I <= 8    ? launch_some<T, 1, CODES>(e, A, x, ldx, w, ldw, K, st)
+         : A.I <= 16 ? launch_some<T, 2, CODES>(e, A, x, ldx, w, ldw, K, st)
+                     : launch_some<T, 4, CODES>(e, A, x, ldx, w, ldw, K, st);
+}
+
 }  // namespace ops
 }  // namespace laq

@@ -7,6 +7,7 @@ import torch
 from paper_1909_07588_b200 import laq, ops
 from tests.test_gpu_ops_blocks import _check8, _pair, values
 from tests.test_gpu_ops_calls import _run
+from tests.test_gpu_ops_gated import _check as _check_gated
 from tests.test_gpu_ops_linear import _act, _product_bound, _randn, _slope, _within
 
 pytestmark = pytest.mark.gpu
@@ -218,6 +219,31 @@ def test_some_rows(N, K, dtype):
         mark = torch.ones_like(big, dtype=torch.bool)
         mark[1:1 + M, 3:3 + N] = False
         assert torch.equal(big[mark], before[mark])
+    ops.check_status()
+
+
+@pytest.mark.parametrize("dtype", [BF, torch.float16])
+@pytest.mark.parametrize("F, K", [(1, 8), (15, 16), (33, 130), (40, 1000), (130, 4096), (7, 900), (10_000, 72), (4_900, 1100), (4100, 4104)])
+def test_some_rows_of_a_block(F, K, dtype):
+    """The same of gates and ups: rows of numbers that end within a block and within eight of them, with NaN behind them."""
+    for M in (3, 4, 5, 8, 9, 16, 17, 32):
+        x, w, b = _randn(M, K, seed=1, dtype=dtype), _randn(2 * F, K, seed=2, dtype=dtype, scale=K ** -0.5), _randn(2 * F, seed=3, dtype=dtype)
+
+        def among(p):
+            big = torch.full((p.shape[0] + 4, -(-K // 8) * 8 + 16), math.nan, dtype=dtype, device="cuda")
+            big[2:-2, 8:8 + K] = p
+            return big[2:-2, 8:8 + K]
+        x, w = among(x), among(w)
+        big = _randn(M + 2, F + 5, seed=5, dtype=dtype)
+        before, inside = big.clone(), big[1:1 + M, 3:3 + F]
+        h, z = _check_gated(x, w, b, "silu", out=inside)
+        assert torch.equal(h, inside)
+        mark = torch.ones_like(big, dtype=torch.bool)
+        mark[1:1 + M, 3:3 + F] = False
+        assert torch.equal(big[mark], before[mark])
+        h8, z8 = ops.gated(x, w, b, preact="packed")
+        want = ops.pack8(z)
+        assert torch.equal(h8, h) and torch.equal(z8.scales, want.scales) and torch.equal(z8.codes.view(torch.uint8), want.codes.view(torch.uint8))
     ops.check_status()
 
 
