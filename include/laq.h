@@ -453,7 +453,8 @@ laq_status laq_linear_blocks_backward(const laq_linear_call* call /* HOST */, co
 /* A gated feed-forward block's two projections, activation and product:
  *   z = x w^T + bias,  h = act(z[:, :F]) * z[:, F:];   x [M][K], w [2F][K] (the gates' rows first), bias [2F], z [M][2F], h [M][F]
  * in `dtype` (LAQ_BF16 or LAQ_F16), summed in fp32 and rounded once.  Its gradient, with dz = [dh z[:, F:] act'(z[:, :F]) | dh act(z[:, :F])]
- * rounded once to `dtype`:  dx = dz w,  dw = dz^T x,  db = column sums of dz before that rounding.  M = 0 gives dw = 0 and db = 0. */
+ * rounded once to `dtype`:  dx = dz w,  dw = dz^T x,  db = column sums of dz before that rounding.  M = 0 gives dw = 0 and db = 0.
+ * A result is the same whichever others are asked for. */
 typedef struct {
   int32_t dtype;             /* laq_dtype of all tensors but db */
   int32_t activation;        /* laq_activation */

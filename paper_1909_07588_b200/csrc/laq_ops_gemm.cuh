@@ -1512,14 +1512,14 @@ struct Gradients {
   long long ld_dw;
   int dw_f32;
 };
-// Whether one launch for both (16-bit results, dZ [M][N], K inputs) is the faster by the plans' estimates, and that launch.
-// `in_order`: only where the products by themselves would not split their sums either, so that every bit is as theirs.
-bool both_pay(long long M, long long N, long long K, bool in_order);
+// Whether one launch for both (16-bit results, dZ [M][N], K inputs) is the faster by the plans' estimates, and that launch.  Only where
+// the products by themselves would not split their sums either: a result has the same bits whether the other is asked for or not.
+bool both_pay(long long M, long long N, long long K);
 laq_status both_products(const Err& e, int dtype, const Operand& dz, const Operand& x, const Operand& w, const Gradients& to, uint32_t* status, int starve,
                          bool follows, cudaStream_t st);
 void list_both_kernels(const void** list, int& n);
 laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand x, Operand w, const Gradients& to, char*& ws, uint32_t* status,
-                             int starve, bool in_order, bool follows, cudaStream_t st);
+                             int starve, bool follows, cudaStream_t st);
 // db = the sums of the columns of part [runs][N]; follows a kernel of the same call.
 laq_status column_sums(const Err& e, const float* part, int runs, int N, float* db, cudaStream_t st);
 laq_status zero_gradients(const Err& e, const Gradients& to, float* db, long long N, long long K, cudaStream_t st);   // of no rows

@@ -267,10 +267,10 @@ laq_status launch_both(const Err& e, const CUtensorMap (&m)[4], const BothArgs& 
 
 }  // namespace
 
-bool both_pay(long long M, long long N, long long K, bool in_order) {
+bool both_pay(long long M, long long N, long long K) {
   if (M > kLongSum || N > kLongSum) return false;
   const Plan dx = make_plan(M, K, N, false, true, true, false, false), dw = make_plan(N, K, M, true, true, false, false, false);
-  if (in_order && (dx.split > 1 || dw.split > 1)) return false;
+  if (dx.split > 1 || dw.split > 1) return false;
   // The second launch costs 4000 cycles at least.  Of 26 gradients of 1 to 9456 rows the slower way is taken twice, at 6 % more:
   // 300 x 600 x 300 17.7 us apart, 12.3 us together, 18 x 12992 x 3920 74 and 122.
   return both_form(M, N, K).cost < dx.cost + dw.cost + 4000;

@@ -350,8 +350,8 @@ laq_status column_sums(const Err& e, const float* part, int runs, int N, float* 
 }
 
 laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand x, Operand w, const Gradients& to, char*& ws, uint32_t* status,
-                             int starve, bool in_order, bool follows, cudaStream_t st) {
-  if (to.dx && to.dw && !to.dw_f32 && both_pay(dz.rows, dz.cols, x.cols, in_order)) {
+                             int starve, bool follows, cudaStream_t st) {
+  if (to.dx && to.dw && !to.dw_f32 && both_pay(dz.rows, dz.cols, x.cols)) {
     const char* before = ws;
     LAQ_TRY(make_mappable(e, w, ws, st));
     LAQ_TRY(make_mappable(e, x, ws, st));
@@ -457,7 +457,7 @@ laq_status layer_backward(const Err& e, const laq_linear_call* c, const laq_bloc
   };
   LAQ_TRY(restored(wq, need.w, need.w_bytes));
   LAQ_TRY(restored(xq, need.x, need.x_bytes));
-  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, starve, true, follows, st);
+  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, starve, follows, st);
 }
 
 }  // namespace
