@@ -271,9 +271,12 @@ bool both_pay(long long M, long long N, long long K) {
   if (M > kLongSum || N > kLongSum) return false;
   const Plan dx = make_plan(M, K, N, false, true, true, false, false), dw = make_plan(N, K, M, true, true, false, false, false);
   if (dx.split > 1 || dw.split > 1) return false;
-  // The second launch costs 4000 cycles at least.  Of 26 gradients of 1 to 9456 rows the slower way is taken twice, at 6 % more:
-  // 300 x 600 x 300 17.7 us apart, 12.3 us together, 18 x 12992 x 3920 74 and 122.
-  return both_form(M, N, K).cost < dx.cost + dw.cost + 4000;
+  // The second launch costs 4000 cycles at least.  The estimates compare tiles of one width well and those of two widths badly, so that
+  // neither product may take wider tiles by itself.  Measured against two launches, 509 gradients of 16 to 16384 rows that the
+  // estimates alone would join: with tiles as wide as theirs (442) all take 3 to 38 % less (8192 x 4096 x 2048 235 us apart, 227
+  // together, 4096 x 4096 x 512 71 and 44); with narrower ones 23 of 67 took more (8192 x 11008 x 784 363 and 491).
+  const Form form = both_form(M, N, K);
+  return form.nt >= dx.nt && form.nt >= dw.nt && form.cost < dx.cost + dw.cost + 4000;
 }
 
 laq_status both_products(const Err& e, int dtype, const Operand& dz, const Operand& x, const Operand& w, const Gradients& to, uint32_t* status, int starve,
