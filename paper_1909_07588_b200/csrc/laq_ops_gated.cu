@@ -428,5 +428,5 @@ extern "C" laq_status laq_gated_backward(const laq_gated_call* c, void* d_worksp
     ws += need.x_bytes;
     LAQ_TRY(unpack_blocks(e, *c->x_blocks, c->M, c->K, c->dtype, const_cast<void*>(need.x.p), need.x.ld, st));
   }
-  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, st);
+  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, true, st);
 }

@@ -1259,9 +1259,10 @@ constexpr int kWideCodesStages = 4;          // of its tiles of 256 columns, whi
 // it is within 3 % of the fastest in 22 of the 26 and at most 25 % slower in the others.
 // The other modes' constants are fitted to all of their forms on 18 and 19 products each, and count a launch's 10000 cycles, which the
 // transposed and split forms, whose blocks take one tile each, have in every wave.
-// `swappable`: the epilogue may write the transposed tile.  An fp32 result's tile is a multiple of 64 wide (its operands are
+// `swappable`: the epilogue may write the transposed tile.  `whole`: no split.  An fp32 result's tile is a multiple of 64 wide (its operands are
 // MN-major).
-inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable, bool out32, bool long_sum, Mode mode = kPlain) {
+inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_mn, bool swappable, bool out32, bool long_sum, Mode mode = kPlain,
+                      bool whole = false) {
   Plan best{0, 128, 1, 4, 0, 1e300};
   const int stage_cols = mode == kCodes ? kBlock : kBlockK;
   const long long nkb = (R + stage_cols - 1) / stage_cols;
@@ -1286,7 +1287,7 @@ inline Plan make_plan(long long I, long long J, long long R, bool a_mn, bool b_m
       const int stage = (kTileM + nt) * kBlockK * 2;
       const double per = mma > stage / 60.0 ? mma : stage / 60.0;
       const long long cols = (j + nt - 1) / nt, tiles = rows * cols;
-      for (int log2 = 0; log2 <= 3; ++log2) {
+      for (int log2 = 0; log2 <= (whole ? 0 : 3); ++log2) {
         const int split = 1 << log2;
         const bool joined = split > 1 || (mode == kGated && swap);
         const long long kb = (nkb + split - 1) >> log2;
@@ -1497,14 +1498,16 @@ inline laq_status check_layer(const Err& e, int dtype, long long M, long long N,
 }
 
 // Defined in laq_ops_linear.cu.
-// D[i][j] = sum_r A(i, r) B(j, r): a_mn ? A is stored [r][i] : [i][r], the same for B.  Both are mappable.  `follows`: the
-// stream's last work is a kernel of the same call.
+// D[i][j] = sum_r A(i, r) B(j, r): a_mn ? A is stored [r][i] : [i][r], the same for B.  Both are mappable.  `whole`: the sum is not
+// split.  `follows`: the stream's last work is a kernel of the same call.
 laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const Operand& b, bool b_mn, const Epilogue& ep,
-                   uint32_t* status, int starve, bool swappable, bool follows, cudaStream_t st);
+                   uint32_t* status, int starve, bool swappable, bool whole, bool follows, cudaStream_t st);
 // Copies an operand that a tensor map cannot describe to `ws` (advanced past it).
 laq_status make_mappable(const Err& e, Operand& o, char*& ws, cudaStream_t st);
 // The products of a layer's gradient, dX = dZ W and dW = dZ^T X (each if asked for); operands that are not mappable are copied
-// to `ws` (advanced past them).
+// to `ws` (advanced past them).  `whole`: where one launch for both is the faster a product that is asked for by itself has its sum whole,
+// as that launch has (128 x 1024 x 256 dX alone by eight blocks 5 us less, both in one launch 2 us less); else one launch is taken only
+// where both products have whole sums anyway.
 struct Gradients {
   void* dx;
   long long ld_dx;
@@ -1512,14 +1515,15 @@ struct Gradients {
   long long ld_dw;
   int dw_f32;
 };
-// Whether one launch for both (16-bit results, dZ [M][N], K inputs) is the faster by the plans' estimates, and that launch.  Only where
-// the products by themselves would not split their sums either: a result has the same bits whether the other is asked for or not.
-bool both_pay(long long M, long long N, long long K);
+// Whether one launch for both (16-bit results, dZ [M][N], K inputs) is the faster by the plans' estimates, and that launch.  It splits
+// no sum; a result has the same bits whether the other is asked for or not, so that it is taken only where neither product would split
+// its sum by itself, or (`whole`) where the caller has the sum of a product by itself whole, too.
+bool both_pay(long long M, long long N, long long K, bool whole = false);
 laq_status both_products(const Err& e, int dtype, const Operand& dz, const Operand& x, const Operand& w, const Gradients& to, uint32_t* status, int starve,
                          bool follows, cudaStream_t st);
 void list_both_kernels(const void** list, int& n);
 laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand x, Operand w, const Gradients& to, char*& ws, uint32_t* status,
-                             int starve, bool follows, cudaStream_t st);
+                             int starve, bool whole, bool follows, cudaStream_t st);
 // db = the sums of the columns of part [runs][N]; follows a kernel of the same call.
 laq_status column_sums(const Err& e, const float* part, int runs, int N, float* db, cudaStream_t st);
 laq_status zero_gradients(const Err& e, const Gradients& to, float* db, long long N, long long K, cudaStream_t st);   // of no rows

@@ -267,16 +267,17 @@ laq_status launch_both(const Err& e, const CUtensorMap (&m)[4], const BothArgs& 
 
 }  // namespace
 
-bool both_pay(long long M, long long N, long long K) {
+bool both_pay(long long M, long long N, long long K, bool whole) {
   if (M > kLongSum || N > kLongSum) return false;
   const Plan dx = make_plan(M, K, N, false, true, true, false, false), dw = make_plan(N, K, M, true, true, false, false, false);
-  if (dx.split > 1 || dw.split > 1) return false;
-  // The second launch costs 4000 cycles at least.  The estimates compare tiles of one width well and those of two widths badly, so that
-  // neither product may take wider tiles by itself.  Measured against two launches, 509 gradients of 16 to 16384 rows that the
-  // estimates alone would join: with tiles as wide as theirs (442) all take 3 to 38 % less (8192 x 4096 x 2048 235 us apart, 227
-  // together, 4096 x 4096 x 512 71 and 44); with narrower ones 23 of 67 took more (8192 x 11008 x 784 363 and 491).
+  if (!whole && (dx.split > 1 || dw.split > 1)) return false;
+  // The second launch costs 4000 cycles at least.  The estimates compare tiles of one width well and those of two widths badly: where a
+  // product takes wider tiles by itself, one launch has to promise 15 % less.  Measured against two launches, 509 gradients of 16 to
+  // 16384 rows that the estimates alone would join: with tiles as wide as theirs (442) all take 3 to 38 % less (8192 x 4096 x 2048
+  // 235 us apart, 227 together, 4096 x 4096 x 512 71 and 44); with narrower ones that promise as much 12 take 13 % less to 1 % more,
+  // of the 55 others 23 took up to 35 % more (8192 x 11008 x 784 363 and 491) and none took more than 16 % less.
   const Form form = both_form(M, N, K);
-  return form.nt >= dx.nt && form.nt >= dw.nt && form.cost < dx.cost + dw.cost + 4000;
+  return form.cost < (form.nt >= dx.nt && form.nt >= dw.nt ? 1.0 : 0.85) * (dx.cost + dw.cost + 4000);
 }
 
 laq_status both_products(const Err& e, int dtype, const Operand& dz, const Operand& x, const Operand& w, const Gradients& to, uint32_t* status, int starve,

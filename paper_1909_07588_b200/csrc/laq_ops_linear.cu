@@ -161,10 +161,10 @@ laq_status launch_form(const Err& e, const Plan& pl, bool out32, bool long_sum, 
 }  // namespace
 
 laq_status product(const Err& e, int dtype, const Operand& a, bool a_mn, const Operand& b, bool b_mn, const Epilogue& ep,
-                   uint32_t* status, int starve, bool swappable, bool follows, cudaStream_t st) {
+                   uint32_t* status, int starve, bool swappable, bool whole, bool follows, cudaStream_t st) {
   const long long I = a_mn ? a.cols : a.rows, R = a_mn ? a.rows : a.cols, J = b_mn ? b.cols : b.rows;
   const bool out32 = ep.out_f32 != 0, long_sum = !out32 && R > kLongSum;
-  const Plan pl = make_plan(I, J, R, a_mn, b_mn, swappable, out32, long_sum);
+  const Plan pl = make_plan(I, J, R, a_mn, b_mn, swappable, out32, long_sum, kPlain, whole);
   const Operand& A0 = pl.swap ? b : a;
   const Operand& B0 = pl.swap ? a : b;
   const bool amn = pl.swap ? b_mn : a_mn, bmn = pl.swap ? a_mn : b_mn;
@@ -350,8 +350,10 @@ laq_status column_sums(const Err& e, const float* part, int runs, int N, float* 
 }
 
 laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand x, Operand w, const Gradients& to, char*& ws, uint32_t* status,
-                             int starve, bool follows, cudaStream_t st) {
-  if (to.dx && to.dw && !to.dw_f32 && both_pay(dz.rows, dz.cols, x.cols)) {
+                             int starve, bool whole, bool follows, cudaStream_t st) {
+  const bool together = (whole || (to.dx && to.dw && !to.dw_f32)) && both_pay(dz.rows, dz.cols, x.cols, whole);
+  whole = whole && together;
+  if (together && to.dx && to.dw) {
     const char* before = ws;
     LAQ_TRY(make_mappable(e, w, ws, st));
     LAQ_TRY(make_mappable(e, x, ws, st));
@@ -364,7 +366,7 @@ laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand
     Epilogue ep;
     ep.out = to.dx;
     ep.ldo = to.ld_dx;
-    LAQ_TRY(product(e, dtype, dz, false, w, true, ep, status, starve, true, follows, st));
+    LAQ_TRY(product(e, dtype, dz, false, w, true, ep, status, starve, true, whole, follows, st));
     follows = true;
   }
   if (to.dw) {
@@ -375,7 +377,7 @@ laq_status gradient_products(const Err& e, int dtype, const Operand& dz, Operand
     ep.out = to.dw;
     ep.ldo = to.ld_dw;
     ep.out_f32 = to.dw_f32;
-    LAQ_TRY(product(e, dtype, dz, true, x, true, ep, status, starve, false, follows, st));
+    LAQ_TRY(product(e, dtype, dz, true, x, true, ep, status, starve, false, whole, follows, st));
   }
   return LAQ_OK;
 }
@@ -457,7 +459,7 @@ laq_status layer_backward(const Err& e, const laq_linear_call* c, const laq_bloc
   };
   LAQ_TRY(restored(wq, need.w, need.w_bytes));
   LAQ_TRY(restored(xq, need.x, need.x_bytes));
-  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, starve, follows, st);
+  return gradient_products(e, c->dtype, need.dz, need.x, need.w, to, ws, c->status, starve, false, follows, st);
 }
 
 }  // namespace
@@ -511,7 +513,7 @@ extern "C" laq_status laq_linear_forward(const laq_linear_call* c, void* d_works
     return c->dtype == LAQ_BF16 ? few_rows<__nv_bfloat16>(e, x, w, ep, st) : few_rows<__half>(e, x, w, ep, st);
   LAQ_TRY(make_mappable(e, x, ws, st));
   LAQ_TRY(make_mappable(e, w, ws, st));
-  return product(e, c->dtype, x, false, w, false, ep, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, ws != d_workspace,
+  return product(e, c->dtype, x, false, w, false, ep, c->status, (c->flags & LAQ_LINEAR_STARVE) != 0, true, false, ws != d_workspace,
                  st);
 }
 
