@@ -297,7 +297,8 @@ laq_status laq_quantize_worker_static(const float* d_g, const float* d_qprev, in
  * Common rules.  No context: like laq_quantize_worker_static every call takes its stream and, optionally, a HOST buffer for
  * an error text (errbuf, errbuf_len).  All tensors are DEVICE, row-major, on the calling thread's current device (checked
  * for every pointer that the call reads or writes: LAQ_EINVAL otherwise), with unit stride within a row and any row stride
- * (in elements) of at least the row's length; a pointer needs only the alignment of its element.  Calls are asynchronous,
+ * (in elements) of at least the row's length; a pointer needs only the alignment of its element.  Nothing is read before a tensor's
+ * first byte or behind its last; of the bytes between its rows up to three beside a row may be, and are not used.  Calls are asynchronous,
  * allocate nothing, copy nothing to the host and can be captured into a CUDA graph; the first call of a row operator, of a
  * layer, of a gated block and on 8-bit matrices on a device each load the code of all of their kernels, for which the runtime may take
  * device memory (call once with small tensors at start-up where that matters).  Zero rows are allowed and launch nothing.  Results do not depend

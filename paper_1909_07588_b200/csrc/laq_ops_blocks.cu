@@ -22,13 +22,14 @@ constexpr int kLanes = 16;                // threads of a block's 128 columns, e
 template <class T>
 constexpr int kMostAhead = 16 / sizeof(T) / 2;
 
-// Eight neighbours; VEC: they lie on a 16-byte boundary and all or none exist, else the first n are read wherever they lie.
+// Eight neighbours; VEC: they lie on a 16-byte boundary and all or none exist, else the first n are read wherever they lie (`edge` as in
+// load16_any).
 template <class T>
 struct Eight {
   static constexpr int kVectors = 8 / Elem<T>::EV;
   uint4 v[kVectors];
   template <bool VEC>
-  __device__ __forceinline__ void read(const T* p, int n) {
+  __device__ __forceinline__ void read(const T* p, int n, bool edge) {
     if (VEC) {
 #pragma unroll
       for (int i = 0; i < kVectors; ++i) v[i] = n ? load16(p + i * Elem<T>::EV) : make_uint4(0u, 0u, 0u, 0u);
@@ -37,7 +38,7 @@ struct Eight {
     float x[8];
     if constexpr (sizeof(T) == 2) {
       uint4 all = make_uint4(0u, 0u, 0u, 0u);
-      if (n > 0) all = load16_any(p, n);
+      if (n > 0) all = load16_any(p, n, edge);
       Elem<T>::unpack(all, x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = e < n ? x[e] : 0.f;
@@ -117,7 +118,7 @@ __global__ void __launch_bounds__(kPackThreads) pack_rows_kernel(const T* x, lon
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
       const long long r = r0 + a * down;
-      in[a].template read<VEC>(x + r * ld + c0, r < rows ? n : 0);
+      in[a].template read<VEC>(x + r * ld + c0, r < rows ? n : 0, at_edge(r, r, rows, c0, cols - c0 - 8, 2));
     }
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
@@ -156,7 +157,8 @@ __global__ void __launch_bounds__(kPackThreads) pack_tiles_kernel(const T* x, lo
   const int n = (int)max(0ll, min(8ll, cols - c0));
   Eight<T> in[8];
 #pragma unroll
-  for (int a = 0; a < 8; ++a) in[a].template read<VEC>(x + (row0 + 16 * a) * ld + c0, row0 + 16 * a < rows ? n : 0);
+  for (int a = 0; a < 8; ++a)
+    in[a].template read<VEC>(x + (row0 + 16 * a) * ld + c0, row0 + 16 * a < rows ? n : 0, at_edge(row0 + 16 * a, row0 + 16 * a, rows, c0, cols - c0 - 8, 2));
   float m = 0.f, v[8];
 #pragma unroll
   for (int a = 0; a < 8; ++a) {
@@ -208,7 +210,7 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
       scale[a] = 0.f;
       if (r >= rows) continue;
       const uint8_t* p = q.p + r * q.ld + c0;
-      in[a] = VEC ? load8(p) : load8_any(p, n);
+      in[a] = VEC ? load8(p) : load8_any(p, n, at_edge(r, r, rows, c0, cols - c0 - 8, 1));
       scale[a] = q.scale(r, c0);
     }
 #pragma unroll
@@ -247,15 +249,6 @@ __global__ void __launch_bounds__(kPackThreads) unpack_kernel(const Codes q, lon
 // linear_some_rows_kernel, 6.7); rows of 4095 codes, which lie anywhere, 12.8, 14.4 and, four, 19.6 (code by code 16.1, 19.2 and 26.9).
 constexpr int kCodesAhead = 2;
 constexpr int kPlainRows = 2, kSomeRows = 32;        // of codes in order: up to these by dot products, by linear_some_rows_kernel
-__device__ __forceinline__ uint4 sixteen_codes(const uint8_t* p) {      // at any address: from the aligned words that hold them
-  const int off = (int)((uintptr_t)p & 3u);
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(p - off);
-  uint32_t w[5];
-#pragma unroll
-  for (int k = 0; k < 5; ++k) w[k] = k < 4 || off ? words[k] : 0u;
-  return make_uint4(__funnelshift_r(w[0], w[1], 8 * off), __funnelshift_r(w[1], w[2], 8 * off), __funnelshift_r(w[2], w[3], 8 * off),
-                    __funnelshift_r(w[3], w[4], 8 * off));
-}
 template <class T, int ROWS, bool VEC>
 __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
     linear_few_codes_kernel(const GemmArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int log_parts) {
@@ -270,8 +263,11 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
 #pragma unroll
   for (int c = 0; c < kFewCols; ++c) wr[c] = w + (long long)min(own + c, A.J - 1) * ldw;
   float s[kSums] = {};
-  const int nv = (int)(K / 16);
-  for (int v0 = first; v0 < nv; v0 += kCodesAhead * step) {
+  // At any address sixteen codes come by the words that hold them, which may reach three codes further on both sides: the first sixteen,
+  // and the last, one by one.
+  constexpr int kFirst = VEC ? 0 : 1;
+  const int nv = VEC ? (int)(K / 16) : max(kFirst, (int)((K - 3) / 16));
+  for (int v0 = kFirst + first; v0 < nv; v0 += kCodesAhead * step) {
     uint4 a[kCodesAhead][kFewCols];
 #pragma unroll
     for (int u = 0; u < kCodesAhead; ++u)
@@ -279,7 +275,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
       for (int c = 0; c < kFewCols; ++c)
         a[u][c] = v0 + u * step >= nv ? make_uint4(0u, 0u, 0u, 0u)
                   : VEC               ? __ldcs(reinterpret_cast<const uint4*>(wr[c]) + v0 + u * step)
-                                      : sixteen_codes(wr[c] + 16ll * (v0 + u * step));
+                                      : load16_codes_any(wr[c] + 16ll * (v0 + u * step), 16, false);
 #pragma unroll
     for (int u = 0; u < kCodesAhead; ++u) {
       const int v = v0 + u * step;
@@ -289,7 +285,7 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
       float scale[ROWS];
 #pragma unroll
       for (int m = 0; m < ROWS; ++m) {
-        const uint4 b = VEC ? __ldg(reinterpret_cast<const uint4*>(x + m * ldx) + v) : sixteen_codes(x + m * ldx + 16ll * v);
+        const uint4 b = VEC ? __ldg(reinterpret_cast<const uint4*>(x + m * ldx) + v) : load16_codes_any(x + m * ldx + 16ll * v, 16, false);
         const uint32_t words[4] = {b.x, b.y, b.z, b.w};
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -320,7 +316,8 @@ __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
       }
     }
   }
-  for (long long k = (long long)nv * 16 + first; k < K; k += step) {
+  for (long long i = first, by16 = 16ll * (nv - kFirst); i < K - by16; i += step) {
+    const long long k = i < 16 * kFirst ? i : i + by16;
     float q[ROWS];
 #pragma unroll
     for (int m = 0; m < ROWS; ++m) q[m] = decode2(x[m * ldx + k]).x * (__ldg(A.sx + m * A.ldsx + k / kBlock) * __ldg(sw + k / kBlock));
@@ -774,7 +771,7 @@ __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __gr
 }
 
 // Codes that a tensor map cannot describe are copied with a pitch of a multiple of 16 bytes, both operands' in one launch.  A warp
-// takes a row, a lane 16 codes of it at a time, from the aligned words that they lie in. 
+// takes a row, a lane 16 codes of it at a time.
 struct CodeRows {
   const uint8_t* src;
   uint8_t* dst;
@@ -790,13 +787,7 @@ __global__ void __launch_bounds__(256) copy_codes_kernel(const CodeRows a, const
     const uint8_t* src = second ? b.src + r * b.ld : a.src + r * a.ld;
     uint8_t* dst = second ? b.dst + r * b.pitch : a.dst + r * a.pitch;
     for (long long c = lane * 16; c < cols; c += 512) {
-      const int n = (int)min(16ll, cols - c), off = (int)((uintptr_t)(src + c) & 3u);
-      const uint32_t* words = reinterpret_cast<const uint32_t*>(src + c - off);
-      uint32_t w[5];
-#pragma unroll
-      for (int k = 0; k < 5; ++k) w[k] = 4 * k < off + n ? words[k] : 0u;          // no word without one of the row's codes
-      *reinterpret_cast<uint4*>(dst + c) = make_uint4(__funnelshift_r(w[0], w[1], 8 * off), __funnelshift_r(w[1], w[2], 8 * off),
-                                                      __funnelshift_r(w[2], w[3], 8 * off), __funnelshift_r(w[3], w[4], 8 * off));
+      *reinterpret_cast<uint4*>(dst + c) = load16_codes_any(src + c, (int)min(16ll, cols - c), at_edge(r, r, second ? b.rows : a.rows, c, cols - c - 16, 1));
     }
   }
 }

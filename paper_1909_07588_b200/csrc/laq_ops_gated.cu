@@ -64,56 +64,60 @@ __global__ void __launch_bounds__(kThreads, blocks_at_once(CODES, VEC)) gated_dz
     const int n = VEC ? (c0 < F ? 8 : 0) : (int)max(0ll, min(8ll, F - c0));            // of this thread's columns there are
     const bool up_vec = VEC || F % 8 == 0;
     const int here = kBlock - (int)((F + c0) % kBlock);                                // ups before the next block
+    const auto rows = [&](long long r, auto edge) {          // r and, if it is there, r + 8
+      const bool two = r + 8 < r1;
+      uint4 d[2], g[2], u[2];
+      uint2 qg[2], qu[2];
+      float sg[2], su[2], su_next[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const long long row = two || i == 0 ? r + 8 * i : r;             // a row is read twice rather than beyond the last
+        const T* pd = dh + row * lddh + c0;
+        d[i] = VEC ? load16(pd) : load16_any<true>(pd, n, decltype(edge)::value);
+        if constexpr (CODES) {
+          const uint8_t* p = zq.p + row * zq.ld + c0;
+          qg[i] = VEC ? load8(p) : load8_any<true>(p, n, decltype(edge)::value);
+          qu[i] = VEC ? load8(p + F) : load8_any<true>(p + F, n, decltype(edge)::value);
+          sg[i] = zq.scale(row, c0);
+          su[i] = zq.scale(row, F + c0);
+          if (!VEC) su_next[i] = zq.scale(row, F + c0 + n - 1);        // eight ups may lie in two blocks
+        } else {
+          const T* p = z + row * ldz + c0;
+          g[i] = load16(p);
+          u[i] = load16(p + F);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        if (i == 1 && !two) break;
+        float df[8], gf[8], uf[8];
+        Elem<T>::unpack(d[i], df);
+        if constexpr (CODES) {
+          decode8(qg[i], sg[i], gf);
+          decode8(qu[i], VEC ? su[i] : 1.f, uf);
+          if (!VEC) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) uf[e] *= e < here ? su[i] : su_next[i];
+          }
+        } else {
+          Elem<T>::unpack(g[i], gf);
+          Elem<T>::unpack(u[i], uf);
+        }
+        slopes(df, gf, uf);
+        if (dz) {
+          T* o = dz + (r + 8 * i) * lddz + c0;
+          const uint4 dg = Elem<T>::pack(gf), du = Elem<T>::pack(uf);
+          if (n == 8) *reinterpret_cast<uint4*>(o) = dg;                      // rows and eights of them are aligned
+          else store16_any(o, dg, n);
+          if (n == 8 && up_vec) *reinterpret_cast<uint4*>(o + F) = du;
+          else store16_any(o + F, du, n);
+        }
+      }
+    };
     if (n > 0) {
       for (long long r = r0 + ty; r < r1; r += 16) {
-        const bool two = r + 8 < r1;
-        uint4 d[2], g[2], u[2];
-        uint2 qg[2], qu[2];
-        float sg[2], su[2], su_next[2];
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          const long long row = two || i == 0 ? r + 8 * i : r;             // a row is read twice rather than beyond the last
-          const T* pd = dh + row * lddh + c0;
-          d[i] = VEC ? load16(pd) : load16_any(pd, n);
-          if constexpr (CODES) {
-            const uint8_t* p = zq.p + row * zq.ld + c0;
-            qg[i] = VEC ? load8(p) : load8_any(p, n);
-            qu[i] = VEC ? load8(p + F) : load8_any(p + F, n);
-            sg[i] = zq.scale(row, c0);
-            su[i] = zq.scale(row, F + c0);
-            if (!VEC) su_next[i] = zq.scale(row, F + c0 + n - 1);        // eight ups may lie in two blocks
-          } else {
-            const T* p = z + row * ldz + c0;
-            g[i] = load16(p);
-            u[i] = load16(p + F);
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          if (i == 1 && !two) break;
-          float df[8], gf[8], uf[8];
-          Elem<T>::unpack(d[i], df);
-          if constexpr (CODES) {
-            decode8(qg[i], sg[i], gf);
-            decode8(qu[i], VEC ? su[i] : 1.f, uf);
-            if (!VEC) {
-#pragma unroll
-              for (int e = 0; e < 8; ++e) uf[e] *= e < here ? su[i] : su_next[i];
-            }
-          } else {
-            Elem<T>::unpack(g[i], gf);
-            Elem<T>::unpack(u[i], uf);
-          }
-          slopes(df, gf, uf);
-          if (dz) {
-            T* o = dz + (r + 8 * i) * lddz + c0;
-            const uint4 dg = Elem<T>::pack(gf), du = Elem<T>::pack(uf);
-            if (n == 8) *reinterpret_cast<uint4*>(o) = dg;                      // rows and eights of them are aligned
-            else store16_any(o, dg, n);
-            if (n == 8 && up_vec) *reinterpret_cast<uint4*>(o + F) = du;
-            else store16_any(o + F, du, n);
-          }
-        }
+        if (!VEC && at_edge(r, r + 8, M, c0, F - c0 - 8, 1)) rows(r, std::true_type());
+        else rows(r, std::false_type());
       }
     }
   } else {

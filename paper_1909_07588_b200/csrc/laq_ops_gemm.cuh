@@ -1571,26 +1571,68 @@ __device__ __forceinline__ void decode8(uint2 v, float scale, float (&x)[8]) {
     x[2 * i + 1] = f.y * scale;
   }
 }
-// The first n (1..8) of eight codes, or of eight 16-bit numbers, at any address of theirs: from the aligned words that hold them, and
-// from no others.  What lies behind the n-th is not theirs.
-__device__ __forceinline__ uint2 load8_any(const uint8_t* p, int n) {
-  const int off = (int)((uintptr_t)p & 3u);
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(p - off);
-  uint32_t w[3];
-#pragma unroll
-  for (int k = 0; k < 3; ++k) w[k] = 4 * k < off + n ? words[k] : 0u;
-  return make_uint2(__funnelshift_r(w[0], w[1], 8 * off), __funnelshift_r(w[1], w[2], 8 * off));
+// The first n (1..8) of eight codes, or of eight 16-bit numbers, or (1..16) of sixteen codes, at any address of theirs: from the aligned
+// words that hold them.  What lies behind the n-th is not theirs.  `edge`: those words may reach beyond the matrix, before its first row
+// or behind its last, so that single bytes are read in their place.  Between rows they may reach up to three bytes beside a row, which are
+// not used.  (With single bytes at both ends of every row the blocks there set the pace, 3001 x 2050: dZ 26 us for 14.)
+// AT_ONCE: the single bytes are all on their way together, which takes registers: where one branch leads there for all of a thread's loads
+// (dZ so 14.8 us, word by word 16.9; unpack_kernel, 8192 x 4096, so 41 us, word by word 33).
+__host__ __device__ __forceinline__ uint32_t funnel(uint32_t lo, uint32_t hi, int bits) {      // bits 0..24
+#ifdef __CUDA_ARCH__
+  return __funnelshift_r(lo, hi, bits);
+#else
+  return (uint32_t)((((uint64_t)hi << 32) | lo) >> bits);
+#endif
 }
-template <class T>
-__device__ __forceinline__ uint4 load16_any(const T* p, int n) {
-  static_assert(sizeof(T) == 2, "16-bit numbers");
-  const int off = (int)((uintptr_t)p & 2u);
-  const uint32_t* words = reinterpret_cast<const uint32_t*>(reinterpret_cast<const char*>(p) - off);
-  uint32_t w[5];
+// Whether words may reach beyond a matrix: from one of its rows first..last, with so many numbers of `bytes` bytes before and behind the
+// ones that are read in the row.
+__host__ __device__ __forceinline__ bool at_edge(long long first, long long last, long long rows, long long before, long long behind, int bytes) {
+  return (first == 0 && before < 4 / bytes - 1) || (last >= rows - 1 && behind < 4 / bytes - 1);
+}
+template <int BYTES, bool AT_ONCE>      // so many from p on, of which the first n are there
+__host__ __device__ __forceinline__ void bytes_any(const uint8_t* p, int n, bool edge, uint32_t (&v)[BYTES / 4]) {
+  if (AT_ONCE && edge) {
+    uint32_t b[BYTES];
 #pragma unroll
-  for (int k = 0; k < 5; ++k) w[k] = 4 * k < off + 2 * n ? words[k] : 0u;
-  return make_uint4(__funnelshift_r(w[0], w[1], 8 * off), __funnelshift_r(w[1], w[2], 8 * off), __funnelshift_r(w[2], w[3], 8 * off),
-                    __funnelshift_r(w[3], w[4], 8 * off));
+    for (int i = 0; i < BYTES; ++i) b[i] = i < n ? p[i] : 0u;
+#pragma unroll
+    for (int k = 0; k < BYTES / 4; ++k) v[k] = b[4 * k] | b[4 * k + 1] << 8 | b[4 * k + 2] << 16 | b[4 * k + 3] << 24;
+    return;
+  }
+  const int off = (int)((uintptr_t)p & 3u);
+  const uint8_t* first = p - off;
+  uint32_t w[BYTES / 4 + 1];
+  if (edge) {
+#pragma unroll
+    for (int k = 0; k <= BYTES / 4; ++k) {
+      w[k] = 0u;
+#pragma unroll
+      for (int i = 4 * k; i < 4 * k + 4; ++i)
+        if (first + i >= p && first + i < p + n) w[k] |= (uint32_t)first[i] << (8 * (i % 4));
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k <= BYTES / 4; ++k) w[k] = 4 * k < off + n ? reinterpret_cast<const uint32_t*>(first)[k] : 0u;
+  }
+#pragma unroll
+  for (int k = 0; k < BYTES / 4; ++k) v[k] = funnel(w[k], w[k + 1], 8 * off);
+}
+template <bool AT_ONCE = false>
+__host__ __device__ __forceinline__ uint2 load8_any(const uint8_t* p, int n, bool edge) {
+  uint32_t v[2];
+  bytes_any<8, AT_ONCE>(p, n, edge, v);
+  return make_uint2(v[0], v[1]);
+}
+template <bool AT_ONCE = false>
+__host__ __device__ __forceinline__ uint4 load16_codes_any(const uint8_t* p, int n, bool edge) {
+  uint32_t v[4];
+  bytes_any<16, AT_ONCE>(p, n, edge, v);
+  return make_uint4(v[0], v[1], v[2], v[3]);
+}
+template <bool AT_ONCE = false, class T>
+__host__ __device__ __forceinline__ uint4 load16_any(const T* p, int n, bool edge) {
+  static_assert(sizeof(T) == 2, "16-bit numbers");
+  return load16_codes_any<AT_ONCE>(reinterpret_cast<const uint8_t*>(p), 2 * n, edge);
 }
 // The first n of eight 16-bit numbers to any address of theirs.
 template <class T>

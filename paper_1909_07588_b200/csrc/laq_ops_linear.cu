@@ -83,7 +83,7 @@ __global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, l
   } else if (c0 < N) {
     for (long long r = r0 + ty; r < r1; r += 8) {
       float g[8], x[8];
-      if constexpr (CODES) decode8(load8_any(zq.p + r * zq.ld + c0, min(8, N - c0)), zq.scale(r, c0), x);
+      if constexpr (CODES) decode8(load8_any(zq.p + r * zq.ld + c0, min(8, N - c0), at_edge(r, r, M, c0, N - c0 - 8, 1)), zq.scale(r, c0), x);
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         g[e] = c0 + e < N ? Elem<T>::to_float(dy[r * lddy + c0 + e]) : 0.f;
@@ -136,7 +136,7 @@ __global__ void __launch_bounds__(256) linear_pack_kernel(const uint16_t* src, l
     const int c = (int)(i - r * groups) * 8;
     const uint16_t* s = src + r * ld + c;
     // what lies behind a row's last number is never looked at: the tensor map ends with the row
-    *reinterpret_cast<uint4*>(dst + r * pitch + c) = load16_any(s, min(8, cols - c));
+    *reinterpret_cast<uint4*>(dst + r * pitch + c) = load16_any(s, min(8, cols - c), at_edge(r, r, rows, c, cols - c - 8, 2));
   }
 }
 
