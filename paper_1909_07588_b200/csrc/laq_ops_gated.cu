@@ -219,10 +219,14 @@ bool dz_vectors(const laq_gated_call* c) {
 }
 
 // Rows of a run: no more blocks than the SMs hold at once (8192 x 4096 with the product behind it: 592 blocks for 444 places 103 us, so
-// 91 us), and no fewer than 32 rows each.
+// 91 us), or as many rounds of them as leave a tenth less of the places empty; no fewer than 32 rows each, and no more than 2048, so that
+// a thread adds up 256 numbers at most, one after another.
 int rows_of_a_run(const laq_gated_call* c) {
-  const long long M = c->M, cols = (c->F + kCols - 1) / kCols, fit = blocks_at_once(c->z_blocks != nullptr, dz_vectors(c)) * kSMs / cols;
-  const long long runs = fit > 1 ? fit : 1;
+  const long long M = c->M, cols = (c->F + kCols - 1) / kCols, places = blocks_at_once(c->z_blocks != nullptr, dz_vectors(c)) * kSMs;
+  const long long least = M > 2048 ? (M + 2047) / 2048 : 1, first = (cols * least + places - 1) / places;
+  long long runs = first * places / cols, rounds = first;
+  for (long long k = first + 1; k < first + 8; ++k)
+    if (10 * k * runs < 9 * rounds * (k * places / cols)) rounds = k, runs = k * places / cols;
   long long per = (M + runs - 1) / runs;
   per = per < 32 ? 32 : per;
   while ((M + per - 1) / per > 65535) per *= 2;
