@@ -84,11 +84,20 @@ __global__ void __launch_bounds__(kDzThreads, 4) linear_dz_kernel(const T* dy, l
     for (long long r = r0 + ty; r < r1; r += 8) {
       float g[8], x[8];
       if constexpr (CODES) decode8(load8_any(zq.p + r * zq.ld + c0, min(8, N - c0), at_edge(r, r, M, c0, N - c0 - 8, 1)), zq.scale(r, c0), x);
+      // all sixteen numbers before the first is converted (8192 x 4097, SiLU: 51 us, one by one 59)
+      const T *pg = dy + r * lddy + c0, *px = z + r * ldz + c0;
+      T gs[8], xs[8];
+      const bool also = !CODES && act != LAQ_ACT_NONE;
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        g[e] = c0 + e < N ? Elem<T>::to_float(dy[r * lddy + c0 + e]) : 0.f;
+        gs[e] = c0 + e < N ? pg[e] : T(0.f);
+        xs[e] = also && c0 + e < N ? px[e] : T(0.f);
+      }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        g[e] = Elem<T>::to_float(gs[e]);
         if constexpr (CODES) x[e] = c0 + e < N ? x[e] : 0.f;
-        else x[e] = act != LAQ_ACT_NONE && c0 + e < N ? Elem<T>::to_float(z[r * ldz + c0 + e]) : 0.f;
+        else x[e] = Elem<T>::to_float(xs[e]);
       }
       row(r, g, x);
     }
