@@ -251,7 +251,7 @@ constexpr int kCodesAhead = 2;
 constexpr int kPlainRows = 2, kSomeRows = 32;        // of codes in order: up to these by dot products, by linear_some_rows_kernel
 template <class T, int ROWS, bool VEC>
 __global__ void __launch_bounds__(kFewThreads, kFewBlocks)
-    linear_few_codes_kernel(const GemmArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int log_parts) {
+    linear_few_codes_kernel(const CodesArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int log_parts) {
   constexpr int kRows2 = ROWS == 3 ? 4 : ROWS, kSums = kFewCols * kRows2, kWarps = kFewThreads / 32;
   __shared__ float part[kWarps][kSums];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, parts = 1 << log_parts;
@@ -384,7 +384,7 @@ __device__ __forceinline__ int narrow_piece(int row, int p) { return row * 4 + (
 template <class T, bool PAIR, int NT, bool COPIES>
 __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                                                                       const __grid_constant__ CUtensorMap tmY, const __grid_constant__ CUtensorMap tmR,
-                                                                      const GemmArgs A) {
+                                                                      const CodesArgs A) {
   extern __shared__ unsigned char codes_smem_raw[];
   __shared__ uint64_t bars[2 * kMaxStages + 9], residual_bars[kAdders];
   __shared__ uint32_t tmem_base_sh;
@@ -885,17 +885,17 @@ laq_status check_matrix(const Err& e, int64_t rows, int64_t cols) {
 }
 
 template <class T, bool PAIR, int NT, bool COPIES>
-laq_status launch_codes(const Err& e, const Product& p, bool follows, cudaStream_t st) {
+laq_status launch_codes(const Err& e, const Product<kCodes>& p, bool follows, cudaStream_t st) {
   static Raised raised;
   CUtensorMap my = p.ma, mr = p.ma;                // unused without copies or a residual
   if (COPIES && (!umma::make_map_bf16_2d(&my, p.A.out, p.A.I, p.A.J, p.A.ldo * 2, 32) ||
                  (p.A.residual && !umma::make_map_bf16_2d(&mr, p.A.residual, p.A.I, p.A.J, p.A.ldr * 2, 32))))
     return fail(e.buf, e.len, LAQ_ECUDA, "a tensor map was refused");
-  return launch_tiles<CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap>(e, codes_gemm_kernel<T, PAIR, NT, COPIES>, raised, kCodesThreads, PAIR, false,
+  return launch_tiles<CodesArgs, CUtensorMap, CUtensorMap, CUtensorMap, CUtensorMap>(e, codes_gemm_kernel<T, PAIR, NT, COPIES>, raised, kCodesThreads, PAIR, false,
                                                                           codes_staging(COPIES), follows, st, p.A, p.ma, p.mb, my, mr);
 }
 template <class T>
-laq_status launch_product(const Err& e, const Product& p, bool follows, cudaStream_t st) {
+laq_status launch_product(const Err& e, const Product<kCodes>& p, bool follows, cudaStream_t st) {
   if (p.pl.swap) return launch_gemm<T, true, false, false, false, kCodes>(e, p.ma, p.mb, p.A, follows, st);
   if (!p.pl.pair) return p.pl.nt == 128 ? launch_codes<T, false, 128, false>(e, p, follows, st) : launch_codes<T, false, 64, false>(e, p, follows, st);
   if (p.pl.nt == 128) return launch_codes<T, true, 128, false>(e, p, follows, st);
@@ -907,7 +907,7 @@ bool takes_few_codes(const laq_linear_call* c) { return !(c->flags & LAQ_LINEAR_
 
 
 template <class T>
-laq_status few_codes(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
+laq_status few_codes(const Err& e, const CodesArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
   const bool vec = codes_mappable(x) && codes_mappable(w);
   const long long groups = (w.rows + kFewCols - 1) / kFewCols, items = w.cols / 16;
   const int log_parts = few_log_parts(groups, items < (1 << 30) ? (int)items : 1 << 30), per_block = kFewThreads / 32 >> log_parts;
@@ -1029,7 +1029,7 @@ extern "C" laq_status laq_linear_blocks_forward(const laq_linear_call* c, const 
   LAQ_TRY(load_block_kernels(e));
   cudaStream_t st = (cudaStream_t)cuda_stream;
   Operand x = codes_of(xq, c->M, c->K), w = codes_of(wq, c->N, c->K);
-  GemmArgs A = {};
+  CodesArgs A = {};
   A.I = (int)c->M;
   A.J = (int)c->N;
   A.act = c->activation;
@@ -1053,9 +1053,9 @@ extern "C" laq_status laq_linear_blocks_forward(const laq_linear_call* c, const 
   char* ws = (char*)d_workspace;
   LAQ_TRY(make_codes_mappable(e, x, w, ws, st));
   const bool follows = ws != d_workspace;
-  Product p;
+  Product<kCodes> p;
   p.A = A;
-  LAQ_TRY(prepare_product(e, kCodes, p, x, w, 0));
+  LAQ_TRY(prepare_product(e, p, x, w, 0));
   return c->dtype == LAQ_BF16 ? launch_product<__nv_bfloat16>(e, p, follows, st) : launch_product<__half>(e, p, follows, st);
 }
 

@@ -250,7 +250,7 @@ struct BackwardNeeds {
 };
 
 template <class T, int ROWS>
-laq_status launch_few(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
+laq_status launch_few(const Err& e, const GatedArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
   const int K = (int)x.cols, vec = x.mappable_() && w.mappable_(), items = vec ? K / 8 : K;
   const long long groups = (A.up + kFewCols / 2 - 1) / (kFewCols / 2);
   const int log_parts = few_log_parts(groups, items), per_block = kFewThreads / 32 >> log_parts;
@@ -261,7 +261,7 @@ laq_status launch_few(const Err& e, const GemmArgs& A, const Operand& x, const O
 }
 
 template <class T>
-laq_status few_rows(const Err& e, const GemmArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
+laq_status few_rows(const Err& e, const GatedArgs& A, const Operand& x, const Operand& w, cudaStream_t st) {
   switch (x.rows) {
     case 1: return launch_few<T, 1>(e, A, x, w, st);
     case 2: return launch_few<T, 2>(e, A, x, w, st);
@@ -271,7 +271,7 @@ laq_status few_rows(const Err& e, const GemmArgs& A, const Operand& x, const Ope
 }
 
 template <class T>
-laq_status launch_product(const Err& e, const Product& p, bool follows, cudaStream_t st) {
+laq_status launch_product(const Err& e, const Product<kGated>& p, bool follows, cudaStream_t st) {
   if (p.pl.pair) return launch_gemm<T, false, true, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st);
   return p.pl.swap ? launch_gemm<T, true, false, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st)
                    : launch_gemm<T, false, false, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st);
@@ -339,7 +339,7 @@ extern "C" laq_status laq_gated_forward(const laq_gated_call* c, void* d_workspa
   cudaStream_t st = (cudaStream_t)cuda_stream;
   ForwardNeeds need(c);
   char* ws = (char*)d_workspace;
-  GemmArgs A = {};
+  GatedArgs A = {};
   A.I = (int)c->M;
   A.J = (int)c->F;
   A.up = c->F;
@@ -372,9 +372,9 @@ extern "C" laq_status laq_gated_forward(const laq_gated_call* c, void* d_workspa
     LAQ_TRY(make_mappable(e, need.x, ws, st));
     LAQ_TRY(make_mappable(e, need.w, ws, st));
     const bool follows = ws != before;
-    Product p;
+    Product<kGated> p;
     p.A = A;
-    LAQ_TRY(prepare_product(e, kGated, p, need.x, need.w, bf16 ? 1 : 0));
+    LAQ_TRY(prepare_product(e, p, need.x, need.w, bf16 ? 1 : 0));
     LAQ_TRY(bf16 ? launch_product<__nv_bfloat16>(e, p, follows, st) : launch_product<__half>(e, p, follows, st));
   }
   if (need.z_bytes) return pack_blocks(e, A.z, c->dtype, c->M, N, A.ldz, *c->z_blocks, st);

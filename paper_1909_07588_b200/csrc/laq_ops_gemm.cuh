@@ -77,14 +77,22 @@ struct GemmArgs {
   const void* bias;              // or null
   const void* residual;          // or null
   uint32_t* status;
-  long long up;                  // kGated: rows of gates, so where the ups begin (columns of out)
-  const float* sx;               // kCodes: scales of X, [rows][blocks], and of W, [blocks of rows][blocks]
-  const float* sw;
-  long long ldsx, ldsw;
-  uint8_t* z_codes;              // kGated: z in 8 bits instead of z, or null: whole blocks of 128 columns, 8-byte aligned
+};
+// What the other modes have more.  A kernel is given no more than its mode needs: with all of it as arguments a layer's product, whose
+// tiles ask for them again and again, was up to 6 % slower (9000 x 2304 x 400 37.3 us, so 39.7; 16 x 331 x 42 8.1, 8.4).
+struct GatedArgs : GemmArgs {
+  long long up;                  // rows of gates, so where the ups begin (columns of out)
+  uint8_t* z_codes;              // z in 8 bits instead of z, or null: whole blocks of 128 columns, 8-byte aligned
   float* z_scales;
   long long ld_zc, ld_zs;
 };
+struct CodesArgs : GemmArgs {
+  const float* sx;               // scales of X, [rows][blocks], and of W, [blocks of rows][blocks]
+  const float* sw;
+  long long ldsx, ldsw;
+};
+template <int MODE>
+using ArgsOf = std::conditional_t<MODE == kGated, GatedArgs, std::conditional_t<MODE == kCodes, CodesArgs, GemmArgs>>;
 
 __device__ __forceinline__ uint64_t desc_k_major(uint32_t addr) { return umma::smem_desc_sw128(addr); }
 // MN-major tile with the 128-byte swizzle: [64 r][64 free] blocks of 128-byte rows; eight rows of r are 1024 bytes
@@ -363,7 +371,7 @@ __device__ __forceinline__ void finish_row(const GemmArgs& A, int i, int j0, flo
 }
 // The same of a gated block: h = act(gate + bias) (up + bias), gates and ups of A.up columns each, side by side in z and in bias.
 template <class T>
-__device__ __forceinline__ void finish_gated_column(const GemmArgs& A, int rows, int row0, int col, float (&g)[8], float (&u)[8]) {
+__device__ __forceinline__ void finish_gated_column(const GatedArgs& A, int rows, int row0, int col, float (&g)[8], float (&u)[8]) {
   if (col >= A.up || row0 >= rows) return;
   const int n = min(8, rows - row0);
   const T* bias = reinterpret_cast<const T*>(A.bias);
@@ -389,7 +397,7 @@ __device__ __forceinline__ void finish_gated_column(const GemmArgs& A, int rows,
     if (e < n) out[e * A.ldo] = Elem<T>::from_float(g[e] * u[e]);
 }
 template <class T>
-__device__ __forceinline__ void finish_gated_row(const GemmArgs& A, int i, int j0, float (&g)[8], float (&u)[8], float inv_g = 0.f, float inv_u = 0.f) {
+__device__ __forceinline__ void finish_gated_row(const GatedArgs& A, int i, int j0, float (&g)[8], float (&u)[8], float inv_g = 0.f, float inv_u = 0.f) {
   if (i >= A.I || j0 >= A.up) return;              // vectors are allowed: A.up is a multiple of eight
   if (A.bias) {
     const T* bias = reinterpret_cast<const T*>(A.bias) + j0;
@@ -435,9 +443,11 @@ __device__ __forceinline__ bool aligned16(const void* p, long long ld_bytes) {
 }
 
 __device__ __forceinline__ bool all_vectors(const GemmArgs& A, bool out32) {
-  return A.up % 8 == 0 && aligned16(A.out, A.ldo * (out32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
+  return aligned16(A.out, A.ldo * (out32 ? 4 : 2)) && (!A.z || aligned16(A.z, A.ldz * 2)) &&
          (!A.residual || aligned16(A.residual, A.ldr * 2)) && (!A.bias || aligned16(A.bias, 0));
 }
+
+__device__ __forceinline__ bool all_vectors(const GatedArgs& A, bool out32) { return A.up % 8 == 0 && all_vectors(static_cast<const GemmArgs&>(A), out32); }
 
 // Work item `w` -> tile origin.  Tile rows are swept in groups of kGroupTiles, column by column within a group.
 template <bool PAIR>
@@ -456,7 +466,7 @@ __device__ __forceinline__ void tile_of(const GemmArgs& A, int w, int& i0, int& 
 template <class T, bool TRANS, bool PAIR, bool OUT32, bool LONG, int MODE = kPlain>
 __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __grid_constant__ CUtensorMap tmA,
                                                                       const __grid_constant__ CUtensorMap tmB,
-                                                                      const GemmArgs A) {
+                                                                      const ArgsOf<MODE> A) {
   extern __shared__ unsigned char gemm_smem_raw[];
   __shared__ uint64_t bars[2 * kMaxStages + 5];
   __shared__ uint32_t tmem_base_sh;
@@ -538,7 +548,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
         tile_of<PAIR>(A, w, i0, j0);
         i0 += half * kTileM;
         // a pair's second block brings the upper half of the columns: of a gated tile the ups
-        if (MODE == kGated && !TRANS) j0 = j0 / 2 + half * (int)A.up;
+        if constexpr (MODE == kGated && !TRANS) j0 = j0 / 2 + half * (int)A.up;
         else j0 += half * b_rows;
         for (int kb = 0; kb < nkb; ++kb, ++n) {
           const int s = n % stages;
@@ -568,7 +578,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           if (A.a_mn) {
             umma::tma_load_2d(sa, &tmA, bar, i0, r);
             umma::tma_load_2d(sa + 8192, &tmA, bar, i0 + 64, r);
-          } else if (MODE == kGated && TRANS) {      // 64 gates and their ups
+          } else if constexpr (MODE == kGated && TRANS) {      // 64 gates and their ups
             umma::tma_load_2d(sa, &tmA, bar, r, i0 / 2);
             umma::tma_load_2d(sa + 8192, &tmA, bar, r, i0 / 2 + (int)A.up);
           } else {
@@ -576,7 +586,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           }
           if (A.b_mn) {
             for (int b = 0; b < nt; b += 64) umma::tma_load_2d(sb + b * 128, &tmB, bar, j0 + b, r);
-          } else if (MODE == kGated && !TRANS) {
+          } else if constexpr (MODE == kGated && !TRANS) {
             umma::tma_load_2d(sb, &tmB, bar, r, j0);
             umma::tma_load_2d(sb + nt / 2 * 128, &tmB, bar, r, j0 + (int)A.up);
           } else {
@@ -836,7 +846,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           for (int e = 0; e < 16; e += 4)
             ring4[piece(row, (c0 + e) / 4, nt / 4)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
-      } else if (MODE == kGated) {
+      } else if constexpr (MODE == kGated) {
         // Z in 8 bits: a tile of 256 columns has a block of gates and one of ups.  A lane looks its row's through for their scales.
         float inv_g = 0.f, inv_u = 0.f;
         if (A.z_codes) {
@@ -1140,16 +1150,18 @@ __device__ __forceinline__ void fold(float (&s)[N], int lane) {
 // GATED: a warp's four rows of W are two gates and their ups.
 template <class T, int ROWS, int AHEAD, bool GATED = false>
 __global__ void __launch_bounds__(kFewThreads, ROWS <= 2 && AHEAD == 2 ? kFewBlocks + 2 : kFewBlocks)
-    linear_few_rows_kernel(const GemmArgs A, const T* x, long long ldx, const T* w, long long ldw, int K, int vec, int log_parts) {
+    linear_few_rows_kernel(const ArgsOf<GATED ? kGated : kPlain> A, const T* x, long long ldx, const T* w, long long ldw, int K, int vec, int log_parts) {
   constexpr int kOwn = GATED ? kFewCols / 2 : kFewCols;          // columns of the result that a warp has
   constexpr int kRows2 = ROWS == 3 ? 4 : ROWS, kSums = kFewCols * kRows2, kWarps = kFewThreads / 32;
   __shared__ float part[kWarps][kSums];
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5, parts = 1 << log_parts;
   const int col0 = (int)(blockIdx.x * (unsigned)(kWarps >> log_parts)) * kOwn;
   const int first = (warp & (parts - 1)) * 32 + lane, step = 32 << log_parts;
+  long long up = 0;
+  if constexpr (GATED) up = A.up;
   const T* wr[kFewCols];
 #pragma unroll
-  for (int c = 0; c < kFewCols; ++c) wr[c] = w + (min(col0 + (warp >> log_parts) * kOwn + c % kOwn, A.J - 1) + c / kOwn * A.up) * ldw;
+  for (int c = 0; c < kFewCols; ++c) wr[c] = w + (min(col0 + (warp >> log_parts) * kOwn + c % kOwn, A.J - 1) + c / kOwn * up) * ldw;
   f32x2 sum[kFewCols][ROWS];
 #pragma unroll
   for (int c = 0; c < kFewCols; ++c)
@@ -1359,9 +1371,9 @@ inline laq_status raise_shared_memory(const Err& e, const void* kernel, Raised& 
   return LAQ_OK;
 }
 // A kernel of maps and, last, the arguments that say how many tiles there are.
-template <class... Maps>
-laq_status launch_tiles(const Err& e, void (*kernel)(Maps..., const GemmArgs), Raised& raised, unsigned threads, bool pair, bool joined, int staging,
-                        bool follows, cudaStream_t st, const GemmArgs& A, const Maps&... maps) {
+template <class Args, class... Maps>
+laq_status launch_tiles(const Err& e, void (*kernel)(Maps..., const Args), Raised& raised, unsigned threads, bool pair, bool joined, int staging,
+                        bool follows, cudaStream_t st, const Args& A, const Maps&... maps) {
   const size_t smem = (size_t)A.stages * (kTileM + (pair ? A.nt / 2 : A.nt)) * kBlockK * 2 + staging + 1024;
   const int per_tile = pair ? 2 : A.split;
   {
@@ -1391,13 +1403,13 @@ laq_status launch_tiles(const Err& e, void (*kernel)(Maps..., const GemmArgs), R
 }
 
 template <class T, bool TRANS, bool PAIR, bool OUT32, bool LONG, int MODE = kPlain>
-laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const GemmArgs& A, bool follows,
+laq_status launch_gemm(const Err& e, const CUtensorMap& ma, const CUtensorMap& mb, const ArgsOf<MODE>& A, bool follows,
                        cudaStream_t st) {
   static Raised raised;
   const bool joined = A.split > 1 || (MODE == kGated && TRANS);
   const int staging = MODE == kCodes ? kEpiWarps * kScaleTable * 4 : TRANS || A.split > 1 ? 0 : kStaging;
-  return launch_tiles<CUtensorMap, CUtensorMap>(e, linear_gemm_kernel<T, TRANS, PAIR, OUT32, LONG, MODE>, raised, kGemmThreads, PAIR, joined, staging, follows,
-                                                st, A, ma, mb);
+  return launch_tiles<ArgsOf<MODE>, CUtensorMap, CUtensorMap>(e, linear_gemm_kernel<T, TRANS, PAIR, OUT32, LONG, MODE>, raised, kGemmThreads, PAIR, joined,
+                                                              staging, follows, st, A, ma, mb);
 }
 
 struct Epilogue {
@@ -1423,12 +1435,14 @@ inline bool make_map(CUtensorMap* map, Mode mode, const void* p, long long rows,
 
 // X W^T in one of the other modes, X [M][K] and W [N][K] of mappable rows (kGated: N = 2 up): the tensor maps, and what the plan says
 // to the kernel, added to `A`, which brings the epilogue, the scales, the status and `up`.
+template <Mode mode>
 struct Product {
   Plan pl;
   CUtensorMap ma, mb;
-  GemmArgs A;
+  ArgsOf<mode> A;
 };
-inline laq_status prepare_product(const Err& e, Mode mode, Product& p, const Operand& x, const Operand& w, int fmt) {
+template <Mode mode>
+laq_status prepare_product(const Err& e, Product<mode>& p, const Operand& x, const Operand& w, int fmt) {
   const Plan& pl = p.pl = make_plan(x.rows, w.rows, x.cols, false, false, true, false, false, mode);
   const Operand &a = pl.swap ? w : x, &b = pl.swap ? x : w;
   const int a_rows = mode == kGated && pl.swap ? kTileM / 2 : kTileM;
@@ -1694,7 +1708,7 @@ __device__ __forceinline__ void copy_piece(uint4* to, const uint8_t* from, long 
 // CODES: 16 columns a warp, else eight gates and their ups; ldx, ldw and K in bytes.
 template <class T, int EIGHTS, bool CODES>
 __global__ void __launch_bounds__(kSomeThreads, Some<EIGHTS>::kBlocks)
-    linear_some_rows_kernel(const GemmArgs A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int log_parts, int sets) {
+    linear_some_rows_kernel(const ArgsOf<CODES ? kCodes : kGated> A, const uint8_t* x, long long ldx, const uint8_t* w, long long ldw, long long K, int log_parts, int sets) {
   constexpr int kStages = Some<EIGHTS>::kStages, kPieces = Some<EIGHTS>::kPieces, kOwn = some_columns(CODES);
   extern __shared__ uint4 some_ring[];
   __shared__ float sums[kSomeWarps][8 * EIGHTS * kSomePitch];
@@ -1723,7 +1737,8 @@ __global__ void __launch_bounds__(kSomeThreads, Some<EIGHTS>::kBlocks)
       const int col = column(p.set) + from_row;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const long long row = CODES ? min(col + 4 * i, A.J - 1) : min(col + 4 * (i & 1), A.J - 1) + (i >> 1) * A.up;
+        long long row = min(col + 4 * (CODES ? i : i & 1), A.J - 1);
+        if constexpr (!CODES) row += (i >> 1) * A.up;
         copy_piece(to + 32 * i, w + row * ldw + (left > 0 ? k : 0), left);
       }
 #pragma unroll
@@ -1736,12 +1751,14 @@ __global__ void __launch_bounds__(kSomeThreads, Some<EIGHTS>::kBlocks)
   };
   float of_x[EIGHTS][2], of_w = 0.f;
   const auto read_scales = [&](const Place& p) {
-    if (!CODES || p.set >= sets) return;
-    of_w = __ldg(A.sw + (long long)(min(column(p.set), A.J - 1) / kBlock) * A.ldsw + p.b);        // 16 columns lie in one tile
+    if constexpr (CODES) {
+      if (p.set >= sets) return;
+      of_w = __ldg(A.sw + (long long)(min(column(p.set), A.J - 1) / kBlock) * A.ldsw + p.b);        // 16 columns lie in one tile
 #pragma unroll
-    for (int f = 0; f < EIGHTS; ++f)
+      for (int f = 0; f < EIGHTS; ++f)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) of_x[f][e] = __ldg(A.sx + min(8 * f + 2 * t + e, A.I - 1) * A.ldsx + p.b);
+        for (int e = 0; e < 2; ++e) of_x[f][e] = __ldg(A.sx + min(8 * f + 2 * t + e, A.I - 1) * A.ldsx + p.b);
+    }
   };
   Place fetched{part < nkb ? (int)blockIdx.x : sets, part}, read = fetched;        // a warp beyond the last block has nothing to fetch
 #pragma unroll
@@ -1832,7 +1849,7 @@ __global__ void __launch_bounds__(kSomeThreads, Some<EIGHTS>::kBlocks)
 }
 
 template <class T, int EIGHTS, bool CODES>
-laq_status launch_some(const Err& e, const GemmArgs& A, const void* x, long long ldx, const void* w, long long ldw, long long K, cudaStream_t st) {
+laq_status launch_some(const Err& e, const ArgsOf<CODES ? kCodes : kGated>& A, const void* x, long long ldx, const void* w, long long ldw, long long K, cudaStream_t st) {
   static Raised raised;
   const auto kernel = linear_some_rows_kernel<T, EIGHTS, CODES>;
   LAQ_TRY(raise_shared_memory(e, (const void*)kernel, raised, Some<EIGHTS>::kRing));
@@ -1850,7 +1867,7 @@ laq_status launch_some(const Err& e, const GemmArgs& A, const void* x, long long
 }
 // Strides and K in bytes, multiples of 16 the former, as the addresses are.
 template <class T, bool CODES>
-laq_status some_rows(const Err& e, const GemmArgs& A, const void* x, long long ldx, const void* w, long long ldw, long long K, cudaStream_t st) {
+laq_status some_rows(const Err& e, const ArgsOf<CODES ? kCodes : kGated>& A, const void* x, long long ldx, const void* w, long long ldw, long long K, cudaStream_t st) {
   return A.I <= 8    ? launch_some<T, 1, CODES>(e, A, x, ldx, w, ldw, K, st)
          : A.I <= 16 ? launch_some<T, 2, CODES>(e, A, x, ldx, w, ldw, K, st)
                      : launch_some<T, 4, CODES>(e, A, x, ldx, w, ldw, K, st);
