@@ -140,12 +140,21 @@ __global__ void __launch_bounds__(256) linear_pack_kernel(const uint16_t* src, l
   allow_next();
   const int groups = (cols + 7) / 8;
   const long long n = rows * groups, stride = (long long)gridDim.x * blockDim.x;
+  const bool few = n <= 256 * kSMs;
   for (long long i = (long long)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += stride) {
     const long long r = i / groups;
     const int c = (int)(i - r * groups) * 8;
     const uint16_t* s = src + r * ld + c;
-    // what lies behind a row's last number is never looked at: the tensor map ends with the row
-    *reinterpret_cast<uint4*>(dst + r * pitch + c) = load16_any(s, min(8, cols - c), at_edge(r, r, rows, c, cols - c - 8, 2));
+    // What lies behind a row's last number is never looked at: the tensor map ends with the row.  Numbers one by one at the matrix's
+    // two ends, and where the copy is short and takes its latency (16 x 331 x 42 7.8 us, by words 8.2; 8192 x 1001 x 4095 93 us, so 86).
+    if (few || at_edge(r, r, rows, c, cols - c - 8, 2)) {
+      uint32_t v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = c + e < cols ? s[e] : 0u;
+      *reinterpret_cast<uint4*>(dst + r * pitch + c) = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+    } else {
+      *reinterpret_cast<uint4*>(dst + r * pitch + c) = load16_any(s, min(8, cols - c), false);
+    }
   }
 }
 
