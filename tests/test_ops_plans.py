@@ -1,5 +1,6 @@
 """What the products' plans decide, asked of the library's own code by a program that is compiled here for the host."""
 import os
+import random
 import subprocess
 
 import pytest
@@ -55,3 +56,23 @@ def test_two_products_in_one_launch_of_narrower_tiles(plans):
     assert all(a[0] == "apart" for a in plans([("gradient",) + s for s in slower]))
     faster = [(4096, 4096, 512), (8192, 4096, 1024), (8192, 8192, 2048), (300, 512, 1024), (200, 200, 4096), (1817, 176, 1808)]
     assert all(a[0] == "together" for a in plans([("gradient",) + s for s in faster]))
+
+
+WIDTHS = {"gated": {"pair": (128, 256), "lone": (64, 128, 192, 256), "transposed": (16, 32, 64, 96, 112, 128)},
+          "linear8": {"pair": (128, 256), "lone": (64, 128), "transposed": (16, 32, 64, 96, 112, 128)}}
+
+
+@pytest.mark.parametrize("kind", sorted(WIDTHS))
+def test_every_form_is_compared(plans, kind):
+    """The sizes of tests/test_gpu_ops_forms.py take the forms that stand there, which are all that the plans give."""
+    from tests import test_gpu_ops_forms as forms
+    listed = forms.GATED if kind == "gated" else forms.LINEAR8
+    assert dict(zip(listed, map(tuple, plans([(kind,) + s for s in listed])))) == listed
+    forms_of = {(form, nt) for form, nt, _ in listed.values()}
+    assert forms_of == {(form, nt) for form, widths in WIDTHS[kind].items() for nt in widths}
+    rng = random.Random(1)
+    sizes = [tuple(int(2 ** rng.uniform(a, b)) for a, b in ((2.4, 13), (0, 13.5), (0, 14))) for _ in range(5000)]
+    assert {(a[0], a[1]) for a in plans([(kind,) + s for s in sizes])} <= forms_of
+    splits = {(form, nt, split > 1) for form, nt, split in listed.values()}
+    if kind == "gated":                # whole and split sums end differently
+        assert splits >= {("lone", nt, s) for nt in (64, 128, 192, 256) for s in (False, True)} | {("transposed", 128, False), ("transposed", 128, True)}
