@@ -794,7 +794,8 @@ __global__ void __launch_bounds__(256) copy_codes_kernel(const CodeRows a, const
 
 // ---- host -----------------------------------------------------------------------------------------------------------------
 long long pad16(long long x) { return (x + 15) / 16 * 16; }
-Operand codes_of(const laq_blocks* b, long long rows, long long cols) { return Operand{b->codes, b->ld_codes, rows, cols}; }
+// A row by itself has no pitch that matters.
+Operand codes_of(const laq_blocks* b, long long rows, long long cols) { return Operand{b->codes, rows == 1 ? pad16(cols) : b->ld_codes, rows, cols}; }
 bool codes_mappable(const Operand& o) { return ((uintptr_t)o.p & 15u) == 0 && o.ld % 16 == 0; }
 size_t copy_bytes(const Operand& o) { return codes_mappable(o) ? 0 : align256((size_t)o.rows * pad16(o.cols)); }
 

@@ -598,7 +598,7 @@ def linear8(x, weight, bias=None, activation="none", residual=None, preact=False
             z = _table(M, N, dtype, x.codes.device)
             c.z, c.ld_z = z.data_ptr(), N
         _forward(L.laq_linear_blocks_forward, L.laq_linear_blocks_workspace_bytes, C.byref(c), (C.byref(xq), C.byref(wq)),
-                 ((xq.codes or 0) | xq.ld_codes | wq.codes | wq.ld_codes) & 15, workspace, index, raw)
+                 ((xq.codes or 0) | (xq.ld_codes if M > 1 else 0) | wq.codes | (wq.ld_codes if N > 1 else 0)) & 15, workspace, index, raw)
         return (y, z) if preact else y
 
     return _on(index, stream, body, *x, *weight, bias, residual, out, workspace)
