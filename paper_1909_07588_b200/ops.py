@@ -538,7 +538,7 @@ def pack8(x, tiles=False, out=None, stream=None):
         _call(laq.load_library().laq_pack_blocks, ptr, dtype, rows, cols, stride, C.byref(q), raw)
         return p
 
-    return _on(index, stream, body, x, *(out or ()))
+    return _on(index, stream, body, x, *_tensors(out))
 
 
 def unpack8(packed, dtype=torch.bfloat16, out=None, stream=None):
@@ -547,6 +547,7 @@ def unpack8(packed, dtype=torch.bfloat16, out=None, stream=None):
     q, rows, cols = _packed(packed, "packed")
     index = packed.codes.get_device()
     if out is not None:
+        _check(out, "out", index)
         dtype = out.dtype
     code = DTYPES.get(dtype)
     if code is None:
