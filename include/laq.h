@@ -442,7 +442,8 @@ laq_status laq_unpack_blocks(const laq_blocks* x /* HOST */, int64_t rows, int64
  * the call's own, which are not looked at; bias, residual, z and y are in the call's dtype.  Sums of 128 products are added up by the
  * tensor cores, scaled by both blocks' scales (whose product must be finite) and added in fp32 with rounding.
  * Backward: any of x, w and z may come in 8 bits, with either block_rows (NULL: the call's own).  x and w are restored to `dtype` first
- * (as laq_unpack_blocks does), z is read as it is.  The gradient is that of the layer on the restored operands. */
+ * (as laq_unpack_blocks does), z is read as it is.  The gradient is that of the layer on the restored operands: in LAQ_F16, where values
+ * lie beyond its range, not that of what laq_linear_blocks_forward computes from them. */
 size_t laq_linear_blocks_workspace_bytes(const laq_linear_call* call /* HOST */, const laq_blocks* x /* HOST */,
                                          const laq_blocks* w /* HOST */, int32_t backward);
 laq_status laq_linear_blocks_forward(const laq_linear_call* call /* HOST */, const laq_blocks* x /* HOST */, const laq_blocks* w /* HOST */,
@@ -455,7 +456,8 @@ laq_status laq_linear_blocks_backward(const laq_linear_call* call /* HOST */, co
  *   z = x w^T + bias,  h = act(z[:, :F]) * z[:, F:];   x [M][K], w [2F][K] (the gates' rows first), bias [2F], z [M][2F], h [M][F]
  * in `dtype` (LAQ_BF16 or LAQ_F16), summed in fp32 and rounded once.  Its gradient, with dz = [dh z[:, F:] act'(z[:, :F]) | dh act(z[:, :F])]
  * rounded once to `dtype`:  dx = dz w,  dw = dz^T x,  db = column sums of dz before that rounding.  M = 0 gives dw = 0 and db = 0.
- * A result is the same whichever others are asked for. */
+ * dz beyond dtype's largest is infinite (LAQ_F16: dh and z may well be smaller), and dx and dw with it.  A result is the same whichever
+ * others are asked for. */
 typedef struct {
   int32_t dtype;             /* laq_dtype of all tensors but db */
   int32_t activation;        /* laq_activation */

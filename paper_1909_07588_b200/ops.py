@@ -402,7 +402,9 @@ def linear(x, weight, bias=None, activation="none", residual=None, preact=False,
 def linear_backward(dy, x, weight, z=None, activation="none", dx=True, dw=True, db=True, dw_dtype=None, workspace=None,
                     stream=None, flags=0):
     """Gradient of ``linear`` for dy [rows, outputs]; z as linear(preact=True) returned it (not needed for activation none).  Any of
-    x, weight and z may be a ``Packed8``: the gradient is then that of the layer on the values it stands for, in dy's type.
+    x, weight and z may be a ``Packed8``: the gradient is then that of the layer on the values it stands for.  Those of x and weight are
+    taken in dy's type, as ``unpack8`` gives them: exact in bfloat16; in float16 those beyond 65504 are 65504, and below 2^-21 they
+    are rounded to multiples of 2^-24.  z is read as it is.
 
     Returns a dict with those of dx [rows, inputs], dw [outputs, inputs] and db [outputs] float32 that are asked for.
     dw_dtype is the layer's type (default) or float32, the latter for activations none and relu.  The residual's gradient
@@ -571,7 +573,8 @@ def linear8(x, weight, bias=None, activation="none", residual=None, preact=False
             stream=None, flags=0):
     """``linear`` on operands in 8 bits: x [rows, inputs] a ``Packed8`` with a scale for each 128 columns of a row, weight
     [outputs, inputs] one with a scale for each tile (``pack8(w, tiles=True)``); bias, residual and results in dtype, bfloat16 or
-    float16.  Its gradient is ``linear_backward`` with the same x and weight."""
+    float16.  Its gradient is ``linear_backward`` with the same x and weight.  This call reads any code times any scale; that one takes x
+    and weight in dtype, so that in float16, where values lie beyond its range, it is not the gradient of what was computed here."""
     L = laq.load_library()
     xq, M, K = _packed(x, "x")
     index = x.codes.get_device()
@@ -654,7 +657,8 @@ def gated(x, weight, bias=None, activation="silu", preact=False, out=None, works
 
 def gated_backward(dh, x, weight, z, activation="silu", dx=True, dw=True, db=True, workspace=None, stream=None, flags=0):
     """Gradient of ``gated`` for dh [rows, gates]; z as gated(preact=True) or gated(preact="packed") returned it, x as it was or
-    packed (``pack8``).
+    packed (``pack8``; taken in dh's type as by ``linear_backward``).  The gradient of z is rounded to dh's type before the two products:
+    in float16 a product of dh and a gate or an up beyond 65504 is infinite there, and dx and dw with it (db is not).
 
     Returns a dict with those of dx [rows, inputs], dw [2 gates, inputs] and db [2 gates] float32 that are asked for.
     """
