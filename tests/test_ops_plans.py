@@ -76,3 +76,10 @@ def test_every_form_is_compared(plans, kind):
     splits = {(form, nt, split > 1) for form, nt, split in listed.values()}
     if kind == "gated":                # whole and split sums end differently
         assert splits >= {("lone", nt, s) for nt in (64, 128, 192, 256) for s in (False, True)} | {("transposed", 128, False), ("transposed", 128, True)}
+
+
+def test_gradients_that_share_a_launch(plans):
+    """The sizes of tests/test_gpu_ops_gradients_forms.py."""
+    from tests.test_gpu_ops_gradients_forms import SIZES
+    got = plans([("gradient",) + s for s in SIZES])
+    assert {s: a[1] if a[0] == "together" else 0 for s, a in zip(SIZES, got)} == SIZES
