@@ -8,7 +8,7 @@
 //   Y = act(sum_b sx[m][b] sw[n / 128][b] (sum_{k in block b} qx[m][k] qw[n][k]) + bias) + R
 //
 // Products of two codes are exact and the tensor cores add up 128 of them; each block's sum is then scaled and added in fp32,
-// with rounding, by the epilogue's threads (linear_gemm_kernel, kCodes).
+// with rounding, by the epilogue's threads (codes_gemm_kernel; of some rows linear_gemm_kernel, kCodes).
 #include "laq_ops_gemm.cuh"
 
 namespace laq {
@@ -926,7 +926,8 @@ laq_status few_codes(const Err& e, const CodesArgs& A, const Operand& x, const O
 }
 
 // Where the tiles of tensor memory overtake: 16 rows of 8192 x 8192 22.5 us (by tiles 23.7), of 16384 x 16384 77 (72); 32 rows of
-// 4096 x 4096 12.4 (12.7), of 4096 x 8192 20 (17), of 11008 x 4096 27 (22), of 1024 x 65536 64 (79), of 16 x 65536 60 (39).
+// 4096 x 4096 12.4 (12.7), of 4096 x 8192 20 (17), of 11008 x 4096 27 (22), of 16 x 65536 60 (39).  In rows longer than 8192 it is the
+// columns that decide, 32 rows of 1024 x 65536 64 (79): those some microseconds are given up, and all of them go by tiles.
 bool takes_some_codes(const laq_linear_call* c, const laq_blocks* xq, const laq_blocks* wq) {
   if ((c->flags & LAQ_LINEAR_STARVE) || c->M <= kPlainRows || c->M > kSomeRows) return false;
   if (c->M > 8 && c->N > (c->M > 16 ? 1ll << 24 : 1ll << 26) / c->K) return false;

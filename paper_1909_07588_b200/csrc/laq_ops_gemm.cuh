@@ -1,7 +1,10 @@
 // The product kernel of the layer operators (laq_ops_linear.cu, laq_ops_gated.cu, laq_ops_blocks.cu), the plan of its tiles, and
 // what their host sides share.
 //
-// One kernel serves all five products, D[i][j] = sum_r A(i, r) B(j, r).  An operand is "K-major" (the summed index r is
+// D[i][j] = sum_r A(i, r) B(j, r).  linear_gemm_kernel serves a layer's product, its gradient's two where each has a launch of its own, the
+// gated block's, and the 8-bit product of some rows (transposed tiles); gradients_gemm_kernel (laq_ops_gradients.cu) both products of a
+// gradient at once, codes_gemm_kernel (laq_ops_blocks.cu) the 8-bit product of more rows, and without tensor memory linear_few_rows_kernel,
+// linear_few_codes_kernel (laq_ops_blocks.cu) and linear_some_rows_kernel those of few rows.  An operand is "K-major" (the summed index r is
 // contiguous in memory) or "MN-major" (the free index is contiguous); TMA brings 64 values of r a stage in either form
 // with the 128-byte swizzle and the matrix descriptors tell the tensor core which one it is, so nothing is transposed in
 // memory.  Warp 0 loads, warp 1 issues the products, warps 2-9 run the epilogue of one tile from tensor memory while the
@@ -47,7 +50,8 @@ constexpr uint32_t kStarvedLimit = 1u << 12;
 // The tensor core's fp32 sums are cut, not rounded: every 16 terms take up to an ulp off, always towards zero (8192 terms:
 // 9e-6 of the result, 512 terms: 7e-7 with bf16 operands, 2.8e-6 with fp16 ones).  fp32 results are added up in chunks of 512
 // terms, which the epilogue's threads keep in registers and add with rounding while the next chunk is under way.  16-bit
-// results show it in long sums alone: 65536 terms lose 6e-5, an eighth of half a step of fp16, 2^20 would lose 8e-4.  Longer
+// results show it in long sums alone (and in numbers that fall on the other side of a rounding: of the gated block's projections packed to
+// 8 bits 0.008 % of the codes at 2048 terms, for 0.0014 % with rounded sums): 65536 terms lose 6e-5, an eighth of half a step of fp16, 2^20 would lose 8e-4.  Longer
 // ones are added up in chunks of 16384 terms (1.6e-5), whose sums wait in the second accumulator's tensor memory, so that
 // tiles may still be 256 wide: the tensor cores stand still for it for some 2000 cycles in a chunk's 180000.  (131072 rows, dW
 // of 4096 x 1024 bf16: 866 us, without chunks 845 us, with the sums in registers and tiles of 128 columns 1505 us.)
@@ -65,7 +69,7 @@ constexpr int kScaleTable = 8 * 64;       // kCodes: scales that an epilogue war
 constexpr int kBlock = 128;               // columns (and, of weights, rows) that share a scale of 8-bit codes
 
 struct GemmArgs {
-  int I, J, nkb;                 // rows and columns of D; 64-wide blocks of the summed axis
+  int I, J, nkb;                 // rows and columns of D; blocks of the summed axis, 64 wide (kCodes: 128)
   int nt, stages, split;         // tile width, ring depth, blocks per tile
   int tiles_i, tiles_j;
   int a_mn, b_mn;                // 1: the operand is MN-major
@@ -1548,7 +1552,7 @@ laq_status load_layer_kernels(const Err& e);
 laq_status unpack_blocks(const Err& e, const laq_blocks& b, long long rows, long long cols, int dtype, void* out, long long pitch, cudaStream_t st);
 laq_status pack_blocks(const Err& e, const void* x, int dtype, long long rows, long long cols, long long ld, const laq_blocks& b, cudaStream_t st);
 laq_status load_block_kernels(const Err& e);
-// Adds an 8-bit matrix to a call's buffers.  Its name is that of the matrix; of the scales " scales" is added.
+// Adds an 8-bit matrix to a call's buffers: its codes by the first name, its scales by the second.
 laq_status check_blocks(const Err& e, Buffers& buffers, const char* name, const char* scales_name, Access access, const laq_blocks* b, int64_t rows,
                         int64_t cols);
 

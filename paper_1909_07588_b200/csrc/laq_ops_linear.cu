@@ -6,7 +6,8 @@
 // (exact for no activation and for ReLU; with the others dX and dW carry it beside their own, in bf16 0.0023 of the result, root
 // mean square, where one rounding makes 0.0017: two 16-bit parts of dZ would double both products).
 //
-// The products are linear_gemm_kernel (laq_ops_gemm.cuh); one to four rows of X are plain dot products.
+// The products are linear_gemm_kernel (laq_ops_gemm.cuh); both of a gradient are gradients_gemm_kernel (laq_ops_gradients.cu) where that
+// is the faster; one to four rows of X are plain dot products.
 #include "laq_ops_gemm.cuh"
 
 namespace laq {
