@@ -365,21 +365,12 @@ __device__ __forceinline__ void mma_codes_pair(uint32_t d_tmem, uint64_t da, uin
       "l"(da), "l"(db), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// Without a fence over the thread's other memory accesses: what is handed back has been read from tensor memory, which wait::ld and
-// fence::before_thread_sync order.  (With one, 8192 x 4096 x 4096 took half as long again.)
-__device__ __forceinline__ void arrive_lightly(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-
 // A warp's results of 32 rows and 64 columns to memory (what lies outside Y is left out), and the end of all such copies' reading.
 __device__ __forceinline__ void copy_out(const CUtensorMap* map, uint32_t from, int x, int y) {
   asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%2, %3}], [%1];" ::"l"(map), "r"(from), "r"(x), "r"(y) : "memory");
   asm volatile("cp.async.bulk.commit_group;" ::: "memory");
 }
 __device__ __forceinline__ void copies_read() { asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory"); }
-
-// 32 rows of four 16-byte pieces in shared memory, permuted so that a warp writes 32 rows and reads along rows without bank conflicts.
-__device__ __forceinline__ int narrow_piece(int row, int p) { return row * 4 + (p ^ ((row >> 1) & 3)); }
 
 template <class T, bool PAIR, int NT, bool COPIES>
 __global__ void __launch_bounds__(kCodesThreads, 1) codes_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,

@@ -2,7 +2,7 @@
 //   Z = X W^T + b,  W [2F][K]: F rows of gates G, then as many of ups U;   H = act(G) U         X [M][K], Z [M][2F], H [M][F]
 //   dG = dH U act'(G),  dU = dH act(G),  dZ = [dG | dU];   dX = dZ W,  dW = dZ^T X,  db = column sums of dZ
 // The forward pass is one product whose tiles hold as many columns of gates as of the ups that belong to them
-// (linear_gemm_kernel, kGated), so that H leaves the epilogue and Z is written only if it is asked for.  H is rounded once, from
+// (gated_gemm_kernel; with split sums and transposed linear_gemm_kernel, kGated), so that H leaves the epilogue and Z is written only if it is asked for.  H is rounded once, from
 // sums in fp32.  With W as one matrix the gradient is two products as a layer's is; dZ is rounded once to the operands' type, as there.
 #include "laq_ops_gemm.cuh"
 
@@ -10,6 +10,321 @@ namespace laq {
 namespace ops {
 namespace {
 
+// ---- both projections and their product, tiles of whole sums --------------------------------------------------------------
+// A tile of 128 rows (256 on a pair of SMs) and nt columns, half of them gates and half the ups that belong to them.  The tensor cores cut
+// their sums (laq_ops_gemm.cuh), which moves numbers to the other side of a rounding, and of Z in 8 bits such a one is a whole code off: they add up
+// 320 to 640 terms at a time, into two accumulators by turns, and sixteen warps add those sums up with rounding.  A thread has 32 gates and their 32
+// ups of a row, 64 sums (eight warps would need 128 each, more than there are registers); the first four warps, a loader and the tensor
+// cores' among them, leave theirs to them as in codes_gemm_kernel.  Both accumulators are free while a tile's results are written.
+// Packed Z of 2048 x (2 x 2048) x 2048 and x 4096 is 1.7e-4 and 1.9e-4 off the codes of its fp64 values (from sums cut throughout 3.4e-4 and 5.9e-4, from plain fp32 sums
+// 1.3e-4 and 1.8e-4).  8192 x 4096 x 4096 419 us (cut throughout 434), 4096 x 5504 x 2048 144 (139), with Z 175 (166), with Z in 8 bits 182 (175).
+constexpr int kAdders = 16, kFirstAdder = 4, kGatedThreads = 32 * (kFirstAdder + kAdders), kFewRegisters = 32, kManyRegisters = 112;
+constexpr int kChunk = 10, kShortSum = 16;             // k-blocks: 640 and 1024 terms
+// A sum's chunk that begins at k0.  The first two are what the tensor cores can do while the last tile's results are written (of 384 terms 4096 x 5504 x 2048
+// with Z in 8 bits 190 us for 160).  Those after them are shorter in sums that have few of them, for each costs an accumulator's way there and back
+// (8192 x 4096 x 4096 by chunks of 320 terms 438 us for 402, and no nearer than plain fp32 sums in either way).
+__device__ __forceinline__ int chunk_at(int k0, int nkb) { return k0 < 2 * kChunk ? kChunk : max(kChunk / 2, min(kChunk, nkb / 6)); }
+// What an adding warp hands over to itself: 32 rows of W columns.  16 leave the ring its six stages, and 32 make whole 64-byte stretches of what
+// is written, which pays where Z is written too (4096 x 5504 x 2048 with Z in 8 bits 161 us, by 16 columns 181; 512 x 4096 x 4096 without Z 33.7, by 32 34.5).
+__host__ __device__ constexpr int handed_bytes(int w) { return 32 * 4 * w; }
+
+template <class T, bool PAIR, int W>
+__global__ void __launch_bounds__(kGatedThreads, 1) gated_gemm_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
+                                                                      const GatedArgs A) {
+  extern __shared__ unsigned char gated_smem_raw[];
+  __shared__ uint64_t bars[2 * kMaxStages + 9];
+  __shared__ signed char powers[kAdders][64];          // of the scales that each warp's columns ask for: 32 rows' gates and ups
+  __shared__ uint32_t tmem_base_sh;
+  __shared__ int abort_sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, nt = A.nt, stages = A.stages, nkb = A.nkb;
+  const uint32_t base = umma::smem_u32(gated_smem_raw), smem0 = (base + 1023u) & ~1023u;
+  const int b_rows = PAIR ? nt / 2 : nt;           // of W that this block loads: a pair's first block the gates', its second the ups'
+  const uint32_t a_bytes = kTileM * kBlockK * 2, st_bytes = a_bytes + (uint32_t)b_rows * kBlockK * 2;
+  const int half = PAIR ? (int)(blockIdx.x & 1u) : 0;
+  const uint32_t full0 = umma::smem_u32(&bars[0]), empty0 = umma::smem_u32(&bars[kMaxStages]);
+  const uint32_t acc_full0 = umma::smem_u32(&bars[2 * kMaxStages]), acc_empty0 = acc_full0 + 16, drain = acc_full0 + 32, told0 = drain + 8;
+  const uint32_t acc_cols = umma::tmem_cols(nt), held_cols = 2 * acc_cols;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < stages; ++s) {
+      umma::mbar_init(full0 + 8 * s, 1);
+      umma::mbar_init(empty0 + 8 * s, 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      umma::mbar_init(acc_full0 + 8 * b, 1);
+      umma::mbar_init(acc_empty0 + 8 * b, PAIR ? 2 * kAdders : kAdders);
+    }
+    umma::mbar_init(drain, 1);
+    for (int q = 0; q < 4; ++q) umma::mbar_init(told0 + 8 * q, kAdders / 4);
+    abort_sh = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  if (warp == 1) {
+    if (PAIR) {
+      asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(umma::smem_u32(&tmem_base_sh)), "r"(held_cols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+      asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(umma::smem_u32(&tmem_base_sh)), "r"(held_cols) : "memory");
+      asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  if (PAIR) cg::this_cluster().sync();             // both blocks' barriers are there before either signals the other's
+  else __syncthreads();
+  asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+  const uint32_t tmem_base = tmem_base_sh;
+  allow_next();
+  await_previous();
+
+  const int tiles = A.tiles_i * A.tiles_j;
+  const int first = (int)blockIdx.x / (PAIR ? 2 : 1), step = (int)gridDim.x / (PAIR ? 2 : 1);
+  const uint32_t limit = A.starve ? kStarvedLimit : umma::kWaitLimit;
+  volatile int* abort_flag = &abort_sh;
+
+  if (warp < kFirstAdder) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kFewRegisters));
+    if (warp == 0) {
+      if (elect_one()) {
+        int n = 0;                       // stages handed out so far
+        bool ok = !(A.starve && blockIdx.x == 0);
+        for (int w = first; w < tiles && ok; w += step) {
+          int i0, j0;
+          tile_of<PAIR>(A, w, i0, j0);
+          i0 += half * kTileM;
+          j0 = j0 / 2 + half * (int)A.up;
+          for (int kb = 0; kb < nkb; ++kb, ++n) {
+            const int s = n % stages;
+            ok = umma::mbar_wait_abortable(empty0 + 8 * s, ((uint32_t)(n / stages) & 1u) ^ 1u, limit, abort_flag, A.status, 1u);
+            if (!ok) break;
+            const uint32_t sa = smem0 + s * st_bytes, sb = sa + a_bytes;
+            const int r = kb * kBlockK;
+            if (PAIR) {
+              // the pair's first block counts the bytes of both; its phase cannot end before its own arrival here
+              if (half == 0) umma::mbar_expect_tx(full0 + 8 * s, 2 * st_bytes);
+              const uint32_t bar = of_leader(full0 + 8 * s);
+              tma_load_2d_pair(sa, &tmA, bar, r, i0);
+              tma_load_2d_pair(sb, &tmB, bar, r, j0);
+            } else {
+              const uint32_t bar = full0 + 8 * s;
+              umma::mbar_expect_tx(bar, st_bytes);
+              umma::tma_load_2d(sa, &tmA, bar, r, i0);
+              umma::tma_load_2d(sb, &tmB, bar, r, j0);
+              umma::tma_load_2d(sb + nt / 2 * 128, &tmB, bar, r, j0 + (int)A.up);
+            }
+          }
+        }
+        if (!ok && PAIR) {              // given up: as in linear_gemm_kernel
+          for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+        } else if (!ok) {
+          for (int m = n > stages ? n - stages : 0; m < n; ++m)
+            for (uint32_t it = 0; it < umma::kWaitLimit && !umma::mbar_try_wait(full0 + 8 * (m % stages), (uint32_t)(m / stages) & 1u); ++it) {
+            }
+        }
+      }
+    } else if (warp == 1 && half == 0) {      // the pair's first block issues the products of both
+      if (elect_one()) {
+        const uint32_t idesc = instr_desc(A.fmt, 0, 0, nt, PAIR ? 2 * kTileM : kTileM);
+        int n = 0, it = 0;
+        bool ok = true;
+        for (int w = first; w < tiles && ok; w += step) {
+          for (int k0 = 0, k1; k0 < nkb && ok; k0 = k1, ++it) {
+            const int b = it & 1;
+            k1 = min(k0 + chunk_at(k0, nkb), nkb);
+            ok = umma::mbar_wait_abortable(acc_empty0 + 8 * b, ((uint32_t)(it >> 1) & 1u) ^ 1u, limit, abort_flag, A.status, 2u);
+            if (!ok) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t d = tmem_base + (uint32_t)b * acc_cols;
+            for (int kb = k0; kb < k1; ++kb, ++n) {
+              const int s = n % stages;
+              ok = umma::mbar_wait_abortable(full0 + 8 * s, (uint32_t)(n / stages) & 1u, limit, abort_flag, A.status, 4u);
+              if (!ok) break;
+              asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+              const uint32_t sa = smem0 + s * st_bytes;
+              const uint64_t da = desc_k_major(sa), db = desc_k_major(sa + a_bytes);
+#pragma unroll
+              for (int kk = 0; kk < kBlockK / 16; ++kk) {          // 32 bytes of the summed axis: two units of a descriptor's address
+                const uint32_t more = kb != k0 || kk != 0 ? 1u : 0u;
+                if (PAIR) mma_pair(d, da + 2 * kk, db + 2 * kk, idesc, more);
+                else umma::mma_bf16_ss(d, da + 2 * kk, db + 2 * kk, idesc, more);
+              }
+              if (PAIR) commit_pair(empty0 + 8 * s);
+              else umma::mma_commit(empty0 + 8 * s);
+            }
+            if (ok) {
+              if (PAIR) commit_pair(acc_full0 + 8 * b);
+              else umma::mma_commit(acc_full0 + 8 * b);
+            }
+          }
+        }
+        if (!ok) {                      // products under way still read the ring and write tensor memory
+          if (PAIR) commit_pair(drain);
+          else umma::mma_commit(drain);
+          for (uint32_t i = 0; i < umma::kWaitLimit && !umma::mbar_try_wait(drain, 0u); ++i) {
+          }
+        }
+      }
+    }
+    __syncwarp();
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kManyRegisters));
+    const int q = warp & 3, c0 = (warp - kFirstAdder) / 4 * 32;          // this warp's rows, and its first column of the gates and of the ups
+    const bool there = c0 < nt / 2, vec = all_vectors(A, false);
+    const uint32_t mine = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)c0;
+    const uint32_t back0 = PAIR ? of_leader(acc_empty0) : acc_empty0, told = told0 + 8 * q;
+    unsigned char* const staging = gated_smem_raw + (smem0 - base) + stages * st_bytes;
+    uint4* stage4 = reinterpret_cast<uint4*>(staging + (warp - kFirstAdder) * handed_bytes(W));
+    int it = 0;
+    uint32_t told_phase = 0;
+    bool ok = true;
+    const auto wait_for = [&](uint32_t bar, uint32_t phase, uint32_t code) {
+      bool done = umma::mbar_try_wait(bar, phase);
+      if (!done) done = umma::mbar_wait_abortable(bar, phase, limit, abort_flag, A.status, code);
+      return (bool)__all_sync(0xffffffffu, done);
+    };
+    for (int w = first; w < tiles && ok; w += step) {
+      float sum[2][32];                      // of this lane's row: gates, ups
+#pragma unroll
+      for (int part = 0; part < 2; ++part)
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sum[part][e] = 0.f;
+      for (int k0 = 0; k0 < nkb; k0 += chunk_at(k0, nkb), ++it) {
+        const int b = it & 1;
+        ok = wait_for(acc_full0 + 8 * b, (uint32_t)(it >> 1) & 1u, 8u);
+        if (!ok) break;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        if (there) {
+#pragma unroll
+          for (int part = 0; part < 2; ++part) {
+            uint32_t v[32];
+            umma::tmem_load_32(mine + (uint32_t)b * acc_cols + (uint32_t)(part * (nt / 2)), v);
+#pragma unroll
+            for (int e = 0; e < 32; ++e) sum[part][e] += __uint_as_float(v[e]);
+          }
+        }
+        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+        __syncwarp();
+        if (lane == 0) {
+          if (PAIR) arrive_lightly(back0 + 8 * b);
+          else umma::mbar_arrive(back0 + 8 * b);
+        }
+      }
+      if (!ok) break;
+      int i0, j0;
+      tile_of<PAIR>(A, w, i0, j0);
+      i0 += half * kTileM + q * 32;
+      j0 = j0 / 2 + c0;
+      // Z in 8 bits: a tile of 256 columns has a block of gates and one of ups.  A lane looks its row's through for their scales; the three
+      // other warps of these rows have the other columns, and they tell one another what they found.
+      float inv_g = 0.f, inv_u = 0.f;
+      bool finite = true;
+      if (A.z_codes) {
+        float largest[2];
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          float x[32];
+#pragma unroll
+          for (int e = 0; e < 32; ++e) x[e] = sum[part][e];
+          if (A.bias) {
+            const uint4* bias = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + part * A.up + j0);
+#pragma unroll
+            for (int b8 = 0; b8 < 4; ++b8) {
+              float b[8];
+              Elem<T>::unpack(__ldg(bias + b8), b);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[8 * b8 + e] += b[e];
+            }
+          }
+          largest[part] = largest_rounded<T>(x, finite);
+        }
+        finite = __all_sync(0xffffffffu, finite);
+        const int wi = warp - kFirstAdder;
+        const auto all_four = [&]() {
+          __syncwarp();
+          if (lane == 0) umma::mbar_arrive(told);
+          const bool done = wait_for(told, told_phase, 16u);
+          told_phase ^= 1u;
+          return done;
+        };
+        powers[wi][lane] = (signed char)scale_power(largest[0]);
+        powers[wi][32 + lane] = (signed char)scale_power(largest[1]);
+        ok = all_four();
+        if (!ok) break;
+        int kg = -126, ku = -126;
+#pragma unroll
+        for (int other = 0; other < 4; ++other) {
+          kg = max(kg, (int)powers[4 * other + (wi & 3)][lane]);
+          ku = max(ku, (int)powers[4 * other + (wi & 3)][32 + lane]);
+        }
+        // The next tile's are written behind its last chunk, which of three or more comes only when all warps have given back its first, and so
+        // have read these; else they wait for one another.
+        if (nkb <= 2 * kChunk) {
+          ok = all_four();
+          if (!ok) break;
+        }
+        inv_g = power_of_two(-kg);
+        inv_u = power_of_two(-ku);
+        if (c0 == 0 && i0 + lane < A.I) {
+          float* to = A.z_scales + (long long)(i0 + lane) * A.ld_zs + j0 / kBlock;
+          to[0] = power_of_two(kg);
+          to[A.up / kBlock] = power_of_two(ku);
+        }
+      }
+      if (!there) continue;
+      // W gates and their ups of 32 rows through shared memory, after which W / 8 lanes share a row, or W neighbouring lanes have neighbouring
+      // columns of eight rows
+      constexpr int kRow = W / 8, kDown = 32 / kRow;          // lanes that share a row, rows at a time
+      const auto at = [](int r, int p) { return W == 32 ? piece(r, p, 8) : narrow_piece(r, p); };
+#pragma unroll
+      for (int h = 0; h < 32; h += W) {
+        float gu[2][kRow][8];
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+          __syncwarp();
+#pragma unroll
+          for (int e = 0; e < W; e += 4)
+            stage4[at(lane, e / 4)] = make_uint4(__float_as_uint(sum[part][h + e]), __float_as_uint(sum[part][h + e + 1]), __float_as_uint(sum[part][h + e + 2]),
+                                                 __float_as_uint(sum[part][h + e + 3]));
+          __syncwarp();
+#pragma unroll
+          for (int k = 0; k < kRow; ++k) {
+            float (&x)[8] = gu[part][k];
+            if (vec) {
+              const int r = kDown * k + lane / kRow, p = 2 * (lane % kRow);
+              const uint4 lo = stage4[at(r, p)], hi = stage4[at(r, p + 1)];
+              x[0] = __uint_as_float(lo.x), x[1] = __uint_as_float(lo.y), x[2] = __uint_as_float(lo.z), x[3] = __uint_as_float(lo.w);
+              x[4] = __uint_as_float(hi.x), x[5] = __uint_as_float(hi.y), x[6] = __uint_as_float(hi.z), x[7] = __uint_as_float(hi.w);
+            } else {
+              const int r = kDown * k + 8 * (lane / W), c = lane % W;
+#pragma unroll
+              for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(reinterpret_cast<const uint32_t*>(&stage4[at(r + e, c >> 2)])[c & 3]);
+            }
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < kRow; ++k) {
+          const int r = kDown * k + lane / kRow;
+          const float ig = __shfl_sync(0xffffffffu, inv_g, r), iu = __shfl_sync(0xffffffffu, inv_u, r);
+          if (vec) finish_gated_row<T>(A, i0 + r, j0 + h + 8 * (lane % kRow), gu[0][k], gu[1][k], ig, iu, finite);
+          else finish_gated_column<T>(A, A.I, i0 + kDown * k + 8 * (lane / W), j0 + h + lane % W, gu[0][k], gu[1][k]);
+        }
+      }
+    }
+    __syncwarp();
+  }
+  asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+  if (PAIR) {
+    __syncwarp();
+    cg::this_cluster().sync();                     // neither block's memory is used by the other any more
+  } else {
+    __syncthreads();
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    if (PAIR) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(held_cols) : "memory");
+    else asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"(held_cols) : "memory");
+  }
+}
+
+// ---- the gradient of Z ---------------------------------------------------------------------------------------------------
 // dZ and its column sums.  Bound by memory.  A block takes 256 columns of the gates and of the ups (32 threads of eight) and a run
 // of rows (8 threads); sums in fp32 of the unrounded products, to part[run][2F].  CODES: Z comes in 8 bits.
 // At odd sizes and addresses (not VEC) 8-bit codes are read by the aligned words that hold a thread's eight columns (3001 x 2050: 34 us
@@ -270,16 +585,32 @@ laq_status few_rows(const Err& e, const GatedArgs& A, const Operand& x, const Op
   }
 }
 
+template <class T, bool PAIR, int W>
+laq_status launch_whole(const Err& e, const Product<kGated>& p, bool follows, cudaStream_t st) {
+  static Raised raised;
+  GatedArgs A = p.A;
+  const int stage = (kTileM + (PAIR ? A.nt / 2 : A.nt)) * kBlockK * 2, most = (kMaxRing + kStaging - kAdders * handed_bytes(W)) / stage;
+  if (A.stages > most) A.stages = most;
+  return launch_tiles<GatedArgs, CUtensorMap, CUtensorMap>(e, gated_gemm_kernel<T, PAIR, W>, raised, kGatedThreads, PAIR, false, kAdders * handed_bytes(W), follows,
+                                                           st, A, p.ma, p.mb);
+}
+// Whole sums of more than 1024 terms, or Z in 8 bits, take gated_gemm_kernel; shorter ones are up to a tenth faster by linear_gemm_kernel's fewer
+// threads (300 x 64 x 64 5.8 us, 6.6; 517 x 1501 x 1000 14.5, 15.8), and their cuts do not show in 16 bits.
 template <class T>
 laq_status launch_product(const Err& e, const Product<kGated>& p, bool follows, cudaStream_t st) {
-  if (p.pl.pair) return launch_gemm<T, false, true, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st);
-  return p.pl.swap ? launch_gemm<T, true, false, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st)
-                   : launch_gemm<T, false, false, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st);
+  const bool adds = !p.pl.swap && p.pl.split == 1 && (p.A.nkb > kShortSum || p.A.z_codes);
+  if (p.pl.pair)
+    return !adds                      ? launch_gemm<T, false, true, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st)
+           : p.A.z || p.A.z_codes ? launch_whole<T, true, 32>(e, p, follows, st)
+                                      : launch_whole<T, true, 16>(e, p, follows, st);
+  if (p.pl.swap) return launch_gemm<T, true, false, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st);
+  return adds ? launch_whole<T, false, 16>(e, p, follows, st) : launch_gemm<T, false, false, false, false, kGated>(e, p.ma, p.mb, p.A, follows, st);
 }
 
 template <class T>
 void list_kernels(const void** list, int& n) {
   const void* all[] = {(const void*)linear_gemm_kernel<T, false, false, false, false, kGated>, (const void*)linear_gemm_kernel<T, true, false, false, false, kGated>,
+                       (const void*)gated_gemm_kernel<T, true, 16>, (const void*)gated_gemm_kernel<T, true, 32>, (const void*)gated_gemm_kernel<T, false, 16>,
                        (const void*)linear_gemm_kernel<T, false, true, false, false, kGated>,
                        (const void*)linear_few_rows_kernel<T, 1, 4, true>, (const void*)linear_few_rows_kernel<T, 1, 2, true>,
                        (const void*)linear_few_rows_kernel<T, 2, 4, true>, (const void*)linear_few_rows_kernel<T, 2, 2, true>,

@@ -2,8 +2,8 @@
 // what their host sides share.
 //
 // D[i][j] = sum_r A(i, r) B(j, r).  linear_gemm_kernel serves a layer's product, its gradient's two where each has a launch of its own, the
-// gated block's, and the 8-bit product of some rows (transposed tiles); gradients_gemm_kernel (laq_ops_gradients.cu) both products of a
-// gradient at once, codes_gemm_kernel (laq_ops_blocks.cu) the 8-bit product of more rows, and without tensor memory linear_few_rows_kernel,
+// gated block's with short or split sums, and the 8-bit product of some rows (transposed tiles); gradients_gemm_kernel (laq_ops_gradients.cu) both products of a
+// gradient at once, codes_gemm_kernel (laq_ops_blocks.cu) the 8-bit product of more rows, gated_gemm_kernel (laq_ops_gated.cu) the gated block's with long sums, and without tensor memory linear_few_rows_kernel,
 // linear_few_codes_kernel (laq_ops_blocks.cu) and linear_some_rows_kernel those of few rows.  An operand is "K-major" (the summed index r is
 // contiguous in memory) or "MN-major" (the free index is contiguous); TMA brings 64 values of r a stage in either form
 // with the 128-byte swizzle and the matrix descriptors tell the tensor core which one it is, so nothing is transposed in
@@ -50,8 +50,8 @@ constexpr uint32_t kStarvedLimit = 1u << 12;
 // The tensor core's fp32 sums are cut, not rounded: every 16 terms take up to an ulp off, always towards zero (8192 terms:
 // 9e-6 of the result, 512 terms: 7e-7 with bf16 operands, 2.8e-6 with fp16 ones).  fp32 results are added up in chunks of 512
 // terms, which the epilogue's threads keep in registers and add with rounding while the next chunk is under way.  16-bit
-// results show it in long sums alone (and in numbers that fall on the other side of a rounding: of the gated block's projections packed to
-// 8 bits 0.008 % of the codes at 2048 terms, for 0.0014 % with rounded sums): 65536 terms lose 6e-5, an eighth of half a step of fp16, 2^20 would lose 8e-4.  Longer
+// results show it in long sums alone (and in numbers that fall on the other side of a rounding, which 8 bits show, so that the gated block
+// has a kernel of its own where it is not split): 65536 terms lose 6e-5, an eighth of half a step of fp16, 2^20 would lose 8e-4.  Longer
 // ones are added up in chunks of 16384 terms (1.6e-5), whose sums wait in the second accumulator's tensor memory, so that
 // tiles may still be 256 wide: the tensor cores stand still for it for some 2000 cycles in a chunk's 180000.  (131072 rows, dW
 // of 4096 x 1024 bf16: 866 us, without chunks 845 us, with the sums in registers and tiles of 128 columns 1505 us.)
@@ -205,6 +205,12 @@ __device__ __forceinline__ void commit_pair(uint32_t bar) {         // arrives a
 __device__ __forceinline__ void arrive_at(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
+// Without a fence over the thread's other memory accesses: what is handed back has been read from tensor memory, which wait::ld and
+// fence::before_thread_sync order.  (With one, which waits for the results
+// that the thread has written, the 8-bit product of 8192 x 4096 x 4096 took half as long again.)
+__device__ __forceinline__ void arrive_lightly(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
 // gelu is the tanh form: 0.5 z (1 + tanh u) = z sigmoid(2 u), u = sqrt(2/pi) (z + 0.044715 z^3).
 constexpr float kGeluC = 0.7978845608028654f, kGeluA = 0.044715f;
 __device__ __forceinline__ float sigmoid(float x) {       // 0 and 1 for far x: 2^128 is +inf and its reciprocal 0
@@ -287,9 +293,9 @@ __device__ __forceinline__ uint2 encode8(const float (&x)[8], float inverse) {
   for (int e = 0; e < 8; ++e) v[e] = fabsf(x[e]) < INFINITY ? x[e] * inverse : __uint_as_float(0x7fffffffu);
   return make_uint2(encode2(v[0], v[1]) | (encode2(v[2], v[3]) << 16), encode2(v[4], v[5]) | (encode2(v[6], v[7]) << 16));
 }
-// The largest finite magnitude of 32 values rounded to T.
+// The largest finite magnitude of 32 values rounded to T; `finite` becomes false if one is no finite number.
 template <class T>
-__device__ __forceinline__ float largest_rounded(const float (&x)[32]) {
+__device__ __forceinline__ float largest_rounded(const float (&x)[32], bool& finite) {
   uint4 v[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -299,6 +305,7 @@ __device__ __forceinline__ float largest_rounded(const float (&x)[32]) {
   }
   float m = Elem<T>::largest(v);
   if (!(m < INFINITY)) {                     // some are not finite: one by one
+    finite = false;
     m = 0.f;
 #pragma unroll
     for (int i = 0; i < 32; ++i) {
@@ -401,7 +408,8 @@ __device__ __forceinline__ void finish_gated_column(const GatedArgs& A, int rows
     if (e < n) out[e * A.ldo] = Elem<T>::from_float(g[e] * u[e]);
 }
 template <class T>
-__device__ __forceinline__ void finish_gated_row(const GatedArgs& A, int i, int j0, float (&g)[8], float (&u)[8], float inv_g = 0.f, float inv_u = 0.f) {
+__device__ __forceinline__ void finish_gated_row(const GatedArgs& A, int i, int j0, float (&g)[8], float (&u)[8], float inv_g = 0.f, float inv_u = 0.f,
+                                                 bool finite = false) {
   if (i >= A.I || j0 >= A.up) return;              // vectors are allowed: A.up is a multiple of eight
   if (A.bias) {
     const T* bias = reinterpret_cast<const T*>(A.bias) + j0;
@@ -422,9 +430,9 @@ __device__ __forceinline__ void finish_gated_row(const GatedArgs& A, int i, int 
     uint8_t* z = A.z_codes + (long long)i * A.ld_zc + j0;
     float r[8];
     Elem<T>::unpack(Elem<T>::pack(g), r);
-    *reinterpret_cast<uint2*>(z) = encode8(r, inv_g);
+    *reinterpret_cast<uint2*>(z) = finite ? encode8_finite(r, inv_g) : encode8(r, inv_g);
     Elem<T>::unpack(Elem<T>::pack(u), r);
-    *reinterpret_cast<uint2*>(z + A.up) = encode8(r, inv_u);
+    *reinterpret_cast<uint2*>(z + A.up) = finite ? encode8_finite(r, inv_u) : encode8(r, inv_u);
   }
   activate(g, A.act);
 #pragma unroll
@@ -441,6 +449,9 @@ __device__ __forceinline__ uint4 residual8(const GemmArgs& A, int i, int j0, boo
 // The fp32 values of a tile row by row in shared memory, 16-byte pieces permuted within a row so that a warp writes 32 rows
 // and reads along rows without bank conflicts.
 __device__ __forceinline__ int piece(int row, int p, int pieces) { return row * pieces + (p ^ (row & (pieces % 8 == 0 ? 7 : 3))); }
+
+// The same of 32 rows of four 16-byte pieces.
+__device__ __forceinline__ int narrow_piece(int row, int p) { return row * 4 + (p ^ ((row >> 1) & 3)); }
 
 __device__ __forceinline__ bool aligned16(const void* p, long long ld_bytes) {
   return (((uintptr_t)p | (uintptr_t)ld_bytes) & 15u) == 0;
@@ -851,42 +862,6 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
             ring4[piece(row, (c0 + e) / 4, nt / 4)] = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
         }
       } else if constexpr (MODE == kGated) {
-        // Z in 8 bits: a tile of 256 columns has a block of gates and one of ups.  A lane looks its row's through for their scales.
-        float inv_g = 0.f, inv_u = 0.f;
-        if (A.z_codes) {
-          float largest[2];
-#pragma unroll
-          for (int part = 0; part < 2; ++part) {
-            largest[part] = 0.f;
-#pragma unroll 1
-            for (int c0 = 0; c0 < kBlock; c0 += 32) {
-              uint32_t v[32];
-              float x[32];
-              values(c0 + part * kBlock, v);
-#pragma unroll
-              for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(v[e]);
-              if (A.bias) {
-                const uint4* bias = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(A.bias) + part * A.up + j0 / 2 + c0);
-#pragma unroll
-                for (int b8 = 0; b8 < 4; ++b8) {
-                  float b[8];
-                  Elem<T>::unpack(__ldg(bias + b8), b);
-#pragma unroll
-                  for (int e = 0; e < 8; ++e) x[8 * b8 + e] += b[e];
-                }
-              }
-              largest[part] = fmaxf(largest[part], largest_rounded<T>(x));
-            }
-          }
-          const int kg = scale_power(largest[0]), ku = scale_power(largest[1]);
-          inv_g = power_of_two(-kg);
-          inv_u = power_of_two(-ku);
-          if (set == 0 && i0 + row < A.I) {
-            float* to = A.z_scales + (long long)(i0 + row) * A.ld_zs + j0 / 256;
-            to[0] = power_of_two(kg);
-            to[A.up / kBlock] = power_of_two(ku);
-          }
-        }
         // 32 gates and their ups of 32 rows, handed over as below
         for (int c0 = 32 * set; c0 < nt / 2; c0 += 64) {
           float gu[2][4][8];
@@ -911,8 +886,7 @@ __global__ void __launch_bounds__(kGemmThreads, 1) linear_gemm_kernel(const __gr
           const int i = i0 + q * 32, j = j0 / 2 + c0;
 #pragma unroll
           for (int k = 0; k < 4; ++k) {
-            const float ig = __shfl_sync(0xffffffffu, inv_g, 8 * k + (lane >> 2)), iu = __shfl_sync(0xffffffffu, inv_u, 8 * k + (lane >> 2));
-            if (vec) finish_gated_row<T>(A, i + 8 * k + (lane >> 2), j + 8 * (lane & 3), gu[0][k], gu[1][k], ig, iu);
+            if (vec) finish_gated_row<T>(A, i + 8 * k + (lane >> 2), j + 8 * (lane & 3), gu[0][k], gu[1][k]);
             else finish_gated_column<T>(A, A.I, i + 8 * k, j + lane, gu[0][k], gu[1][k]);
           }
         }
