@@ -20,10 +20,13 @@ namespace {
 // 1.3e-4 and 1.8e-4).  8192 x 4096 x 4096 419 us (cut throughout 434), 4096 x 5504 x 2048 144 (139), with Z 175 (166), with Z in 8 bits 182 (175).
 constexpr int kAdders = 16, kFirstAdder = 4, kGatedThreads = 32 * (kFirstAdder + kAdders), kFewRegisters = 32, kManyRegisters = 112;
 constexpr int kChunk = 10, kShortSum = 16;             // k-blocks: 640 and 1024 terms
-// A sum's chunk that begins at k0.  The first two are what the tensor cores can do while the last tile's results are written (of 384 terms 4096 x 5504 x 2048
-// with Z in 8 bits 190 us for 160).  Those after them are shorter in sums that have few of them, for each costs an accumulator's way there and back
+// A sum's chunk that begins at k0: all of a short sum, which linear_gemm_kernel does not cut up either, so that Z in 8 bits is that of the call without.  The
+// first two of a long one are what the tensor cores can do while the last tile's results are written (of 384 terms 4096 x 5504 x 2048 with Z in 8 bits
+// 190 us for 160).  Those after them are shorter in sums that have few of them, for each costs an accumulator's way there and back
 // (8192 x 4096 x 4096 by chunks of 320 terms 438 us for 402, and no nearer than plain fp32 sums in either way).
-__device__ __forceinline__ int chunk_at(int k0, int nkb) { return k0 < 2 * kChunk ? kChunk : max(kChunk / 2, min(kChunk, nkb / 6)); }
+__device__ __forceinline__ int chunk_at(int k0, int nkb) {
+  return nkb <= kShortSum ? kShortSum : k0 < 2 * kChunk ? kChunk : max(kChunk / 2, min(kChunk, nkb / 6));
+}
 // What an adding warp hands over to itself: 32 rows of W columns.  16 leave the ring its six stages, and 32 make whole 64-byte stretches of what
 // is written, which pays where Z is written too (4096 x 5504 x 2048 with Z in 8 bits 161 us, by 16 columns 181; 512 x 4096 x 4096 without Z 33.7, by 32 34.5).
 __host__ __device__ constexpr int handed_bytes(int w) { return 32 * 4 * w; }
@@ -381,9 +384,10 @@ __global__ void __launch_bounds__(kThreads, blocks_at_once(CODES, VEC)) gated_dz
     const int here = kBlock - (int)((F + c0) % kBlock);                                // ups before the next block
     const auto rows = [&](long long r, auto edge) {          // r and, if it is there, r + 8
       const bool two = r + 8 < r1;
-      uint4 d[2], g[2], u[2];
-      uint2 qg[2], qu[2];
-      float sg[2], su[2], su_next[2];
+      uint4 d[2];
+      [[maybe_unused]] uint4 g[2], u[2];                    // 16-bit projections, or
+      [[maybe_unused]] uint2 qg[2], qu[2];                  // codes and their scales
+      [[maybe_unused]] float sg[2], su[2], su_next[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const long long row = two || i == 0 ? r + 8 * i : r;             // a row is read twice rather than beyond the last

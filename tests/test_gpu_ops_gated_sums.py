@@ -23,3 +23,18 @@ def test_sums_of_one_sign(M, F, K):
         wrong += int((z[r:r + 512] != want.to(torch.float16)).sum())
     assert wrong <= 2 * e * 2 ** 11 * z.numel()
     ops.check_status()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("K", [640, 641, 704, 1000, 1024, 1025, 1300, 2500])
+def test_packed_is_pack8_of_the_other(K, dtype):
+    """Whatever the sums' length: with and without Z, in 16 bits and in 8, a call adds up the same numbers in the same order."""
+    for M, F in ((2300, 1408), (6500, 2560), (130, 128), (5000, 384), (4097, 5504)):
+        x, w, b = _randn(M, K, seed=1, dtype=dtype), _randn(2 * F, K, seed=2, dtype=dtype, scale=K ** -0.5), _randn(2 * F, seed=3, dtype=dtype)
+        for bias in (None, b):
+            h, z = ops.gated(x, w, bias, activation="gelu", preact=True)
+            h8, z8 = ops.gated(x, w, bias, activation="gelu", preact="packed")
+            want = ops.pack8(z)
+            assert torch.equal(ops.gated(x, w, bias, activation="gelu").view(torch.int16), h.view(torch.int16)) and torch.equal(h8.view(torch.int16), h.view(torch.int16))
+            assert torch.equal(z8.scales, want.scales) and torch.equal(z8.codes.view(torch.uint8), want.codes.view(torch.uint8)), (M, F)
+    ops.check_status()
